@@ -178,6 +178,56 @@ moe_status moe_plan_routing_from_topk(moe_ctx* ctx, const int32_t* topk_ids, int
                                       void* stream);
 
 /*
+ * Scored routing: the rules fine-grained layers are trained with.  (The paper leaves routing unchanged, Sec. 7; this
+ * entry point exists for the library's users.)  For a token's logits x_e (fp32):
+ *   scores   s_e = softmax(x)_e over all E, or 1 / (1 + exp(-x_e));
+ *   choice   c_e = s_e + bias_e when a bias is given (a balance bias: it moves the choice and never the weight),
+ *            otherwise c_e = x_e (both score maps are monotone, so the order is that of the exact scores);
+ *   groups   expert e belongs to group e / (E / n_group).  A group is worth the largest c of its experts (group_top 1)
+ *            or the sum of its two largest c (group_top 2; without a bias the sum of its two largest scores); the
+ *            topk_group best groups stay, the experts of the others are never chosen;
+ *   top k    the k largest c, ties to the lower expert index, slots in descending order of c; ties between groups go
+ *            to the lower group;
+ *   weights  w_j = weight_scale * s_j / (sum of the chosen s) when renormalise is 1, else weight_scale * s_j.
+ * Scores, choices and weights are fp32.  Then the plan, exactly as in moe_plan_routing.
+ * Masks: a logit of -inf masks its expert.  It adds nothing to the softmax or to its group's worth, is chosen only
+ * when fewer than k experts of the kept groups are unmasked (lowest index first), and has weight 0; a token whose
+ * experts are all masked gets zero weights.  A NaN logit (or +inf under softmax) makes all weights of its token NaN;
+ * the ids stay valid and distinct (NaN ranks with the masked experts).
+ * Limits: n_group divides E, 1 <= n_group <= 32, 1 <= topk_group <= n_group, group_top 1 or 2 and at most E / n_group,
+ * k <= topk_group * (E / n_group), weight_scale finite; otherwise INVALID_ARG.
+ *   logits [T,E] fp32, bias [E] fp32 or NULL -> as moe_plan_routing.
+ */
+enum { MOE_SCORE_SOFTMAX = 0, MOE_SCORE_SIGMOID = 1 };
+typedef struct {
+  int32_t score;        /* MOE_SCORE_SOFTMAX or MOE_SCORE_SIGMOID */
+  int32_t n_group;      /* 1 = no groups */
+  int32_t topk_group;   /* groups kept */
+  int32_t group_top;    /* experts that make a group's worth: 1 or 2 */
+  int32_t renormalise;  /* 0 or 1 */
+  float weight_scale;
+} moe_route_rule;
+moe_status moe_plan_routing_scored(moe_ctx* ctx, const float* logits, const float* bias, const moe_route_rule* rule,
+                                   int32_t* topk_ids, float* topk_w, int32_t* counts, int32_t* offsets, int32_t* perm,
+                                   int32_t* inv_perm, void* stream);
+
+/*
+ * Gradient of the weights of moe_plan_routing_scored with respect to the logits, the choice held fixed (the bias and
+ * the groups act on the choice alone and get no gradient).  With g_j = weight_scale * d_topk_w[t,j]:
+ *   sigmoid               d_x_j = g_j s_j (1 - s_j)
+ *   sigmoid, renormalised d_x_j = (g_j - sum_i g_i s_i / S) / S * s_j (1 - s_j),  S = sum of the chosen s (0 where S = 0)
+ *   softmax               d_x_e = s_e ([e chosen] g_e - sum_i g_i s_i)   for every expert
+ *   softmax, renormalised d_x_j = q_j (g_j - sum_i g_i q_i),  q = softmax over the chosen logits
+ * and 0 for the experts the formulas do not name.  Every entry of d_logits is written.  Masked experts get 0; a token
+ * whose logits hold a NaN (or +inf under softmax) gets a row of NaN.  topk_ids must be distinct per token and in
+ * [0, E); an id outside is reported through the status word (MOE_ERR_BAD_ROUTING, detail = the flat slot t*k+j) and
+ * its slot takes no part.
+ *   logits [T,E] fp32, topk_ids [T,k], d_topk_w [T,k] fp32 -> d_logits [T,E] fp32.
+ */
+moe_status moe_routing_backward(moe_ctx* ctx, const float* logits, const int32_t* topk_ids, const float* d_topk_w,
+                                const moe_route_rule* rule, float* d_logits, void* stream);
+
+/*
  * The routing plan for callers that must not allocate.  (The paper has no counterpart: this entry point
  * exists for the library's users, not for the method.)
  *
@@ -268,6 +318,16 @@ moe_status moe_expert_ffn(moe_ctx* ctx, const void* x_perm, const int32_t* offse
  */
 moe_status moe_combine(moe_ctx* ctx, const void* y_perm, const int32_t* inv_perm, const float* topk_w,
                        void* out, void* stream);
+
+/*
+ * Gradient of moe_combine with respect to the expert rows and the weights:
+ *     d_y_perm[inv_perm[t*k+j], :] = bf16( topk_w[t,j] * float(d_out[t, :]) )
+ *     d_topk_w[t,j]                = sum_c float(d_out[t,c]) * float(y_perm[inv_perm[t*k+j], c])      (fp32, fixed order)
+ * d_y_perm may be NULL (frozen experts: only the weights' gradient is wanted).
+ *   d_out [T,H] bf16, y_perm [R,H] bf16, inv_perm [R], topk_w [T,k] fp32 -> d_y_perm [R,H] bf16, d_topk_w [T,k] fp32.
+ */
+moe_status moe_combine_backward(moe_ctx* ctx, const void* d_out, const void* y_perm, const int32_t* inv_perm,
+                                const float* topk_w, void* d_y_perm, float* d_topk_w, void* stream);
 
 /*
  * The whole layer on one stream: plan_routing, dispatch, expert_ffn, combine (Sec. 4.3, the fused
@@ -420,6 +480,91 @@ moe_status moe_fused_forward_mx(moe_ctx* ctx, const void* x, const float* logits
                                 const uint32_t* sf_gate, const void* wq_up, const uint32_t* sf_up, const void* wq_down,
                                 const uint32_t* sf_down, void* out, void* workspace, size_t workspace_bytes,
                                 void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * FP8 in blocks of 128 (the form fine-grained layers' weights are published in): E4M3 codes with one fp32 scale per
+ * block, 1 x 128 along K for rows (activations), 128 x 128 for weights.  value = code * scale.
+ *   scale = amax(|block|) / 448 (1 for an all-zero block), code = E4M3(value / scale), to nearest even, saturating;
+ *   an infinity makes its block's scale infinite (the block then stands for NaN), a NaN stays a NaN code.
+ * Layouts: codes row-major; row scales [ceil(cols/128)][rows] fp32; weight scales [matrix][ceil(rows/128)][ceil(cols/128)]
+ * fp32.  The last block of a row, and the last row of blocks of a matrix, may be short.  The scales are arbitrary fp32
+ * numbers (a published checkpoint's scales are taken as they are), so the product keeps one fp32 partial sum per block
+ * of K and adds it, scaled, to the running fp32 sum.
+ * ------------------------------------------------------------------------------------------------ */
+
+/* in_bf16 [rows, cols] bf16 (cols a multiple of 16) -> codes [rows, cols], scales [ceil(cols/128)][rows]. */
+moe_status moe_quantize_rows_blk(moe_ctx* ctx, const void* in_bf16, int64_t rows, int32_t cols, void* codes,
+                                 float* scales, void* stream);
+/* in_bf16 [mats, rows, cols] bf16 (cols a multiple of 16) -> codes, scales [mats][ceil(rows/128)][ceil(cols/128)]. */
+moe_status moe_quantize_weights_blk(moe_ctx* ctx, const void* in_bf16, int64_t mats, int32_t rows, int32_t cols,
+                                    void* codes, float* scales, void* stream);
+
+/* Dispatch of quantised token rows: xq_perm[inv_perm[t*k+j], :] = xq[t, :], sx_perm[b][inv_perm[t*k+j]] = sx[b][t].
+ *   xq [T,H] E4M3, sx [H/128][T] -> xq_perm [R,H], sx_perm [H/128][R].  H a multiple of 128. */
+moe_status moe_dispatch_blk(moe_ctx* ctx, const void* xq, const float* sx, const int32_t* inv_perm, void* xq_perm,
+                            float* sx_perm, void* stream);
+
+/*
+ * The product y[r, n] = sum_k a[r, k] b[g, n, k] for the rows offsets[g] <= r < offsets[g+1] of each group g:
+ *     y[r,n] = bf16( sum_b sa[b][r] * sb[g][n/128][b] * sum_{k in block b} code_a[r,k] code_b[g,n,k] )
+ * with fp32 sums.  The shape is the argument's, not the context's (which lends its device, its status word and its
+ * scheduler counters).  offsets NULL: one matrix for all rows (groups must be 1).  Rows outside every group are not
+ * written; a group without rows is not read.  The gradient with respect to a is the same call on the transposed
+ * weights: their blocks and scales are the transposed ones.
+ * Limits: K a multiple of 16, N a multiple of 8, 1 <= groups <= 1024, 0 <= rows < 2^30, groups * N < 2^31.
+ */
+typedef struct {
+  const void* a;            /* E4M3 [rows, K] */
+  const float* sa;          /* fp32 [ceil(K/128)][rows] */
+  const int32_t* offsets;   /* int32 [groups + 1], ascending from 0 to at most rows, or NULL */
+  const void* b;            /* E4M3 [groups, N, K] */
+  const float* sb;          /* fp32 [groups][ceil(N/128)][ceil(K/128)] */
+  void* y;                  /* out: bf16 [rows, N] */
+  int64_t rows;
+  int32_t N, K, groups;
+} moe_gemm_blk_args;
+moe_status moe_gemm_blk(moe_ctx* ctx, const moe_gemm_blk_args* args, void* stream);
+
+typedef struct {
+  const void* xq_perm;      /* E4M3 [R,H] */
+  const float* sx_perm;     /* fp32 [H/128][R] */
+  const int32_t* offsets;   /* int32 [E+1] */
+  const void* wq_gate;      /* E4M3 [E,F,H] */
+  const float* s_gate;      /* fp32 [E][F/128][H/128] */
+  const void* wq_up;        /* E4M3 [E,F,H] */
+  const float* s_up;        /* fp32 [E][F/128][H/128] */
+  const void* wq_down;      /* E4M3 [E,H,F] */
+  const float* s_down;      /* fp32 [E][H/128][F/128] */
+  void* hq_ws;              /* out: E4M3 [R,F]: h = silu(gate) * up, quantised from its fp32 value (Linear-2 input) */
+  float* sh_ws;             /* out: fp32 [F/128][R] */
+  void* y_perm;             /* out: bf16 [R,H] */
+  float* h_fp32_debug;      /* NULL, or fp32 [R,F] that receives h before its quantisation */
+} moe_blk_ffn_args;
+/* Linear-1 (SiLU*mul, h quantised in its epilogue) and Linear-2 of the experts.  H and F multiples of 128
+ * (MOE_ERR_UNSUPPORTED_SHAPE otherwise). */
+moe_status moe_expert_ffn_blk(moe_ctx* ctx, const moe_blk_ffn_args* args, void* stream);
+
+/* Byte offsets of the workspace slices of moe_fused_forward_blk (256-byte aligned). */
+typedef struct {
+  size_t topk_ids, topk_w, counts, offsets, perm, inv_perm;   /* as in moe_workspace_layout */
+  size_t xq;         /* E4M3 [T,H] */
+  size_t sx;         /* fp32 [H/128][T] */
+  size_t xq_perm;    /* E4M3 [R,H] */
+  size_t sx_perm;    /* fp32 [H/128][R] */
+  size_t hq;         /* E4M3 [R,F] */
+  size_t sh;         /* fp32 [F/128][R] */
+  size_t y_perm;     /* bf16 [R,H] */
+  size_t total;
+} moe_workspace_layout_blk;
+moe_status moe_get_workspace_layout_blk(const moe_shape* shape, moe_workspace_layout_blk* out_layout);
+
+/* The whole fine-grained layer on one stream: plan_routing_scored, quantise x, dispatch, expert_ffn_blk, combine.
+ * x [T,H] bf16, logits [T,E] fp32, bias [E] fp32 or NULL; weights in blocks of 128 (moe_quantize_weights_blk, or a
+ * published checkpoint's codes and scales).  Errors: as the calls it is made of, plus WORKSPACE_TOO_SMALL. */
+moe_status moe_fused_forward_blk(moe_ctx* ctx, const void* x, const float* logits, const float* bias,
+                                 const moe_route_rule* rule, const void* wq_gate, const float* s_gate,
+                                 const void* wq_up, const float* s_up, const void* wq_down, const float* s_down,
+                                 void* out, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * The host-buffer call as a two-deep pipeline, for callers that run step after step (serving): consecutive calls

@@ -29,7 +29,9 @@ EXPORTS = (
     "moe_set_active_tokens", "moe_plan_routing_from_topk", "moe_router_weight_bytes", "moe_router_scratch_bytes",
     "moe_router_prepare", "moe_route_tokens", "moe_fused_forward_routed", "moe_quantize_rows_mx", "moe_dispatch_mx",
     "moe_expert_ffn_mx", "moe_get_workspace_layout_mx", "moe_fused_forward_mx", "moe_probe_mma_cycles_kind",
-    "moe_parse_tuning", "moe_get_kernel_times_back",
+    "moe_parse_tuning", "moe_get_kernel_times_back", "moe_plan_routing_scored", "moe_routing_backward",
+    "moe_combine_backward", "moe_quantize_rows_blk", "moe_quantize_weights_blk", "moe_dispatch_blk", "moe_gemm_blk",
+    "moe_expert_ffn_blk", "moe_get_workspace_layout_blk", "moe_fused_forward_blk",
 )
 
 TIMING_SLOTS = 32     # timed calls whose per-kernel events the library keeps (moe_get_kernel_times_back)
@@ -81,6 +83,29 @@ class moe_mx_ffn_args(C.Structure):
 class moe_workspace_layout_mx(C.Structure):
     _fields_ = [(n, C.c_size_t) for n in ("topk_ids", "topk_w", "counts", "offsets", "perm", "inv_perm", "xq", "sfx",
                                           "xq_perm", "sfx_perm", "hq", "sfh", "y_perm", "total")]
+
+
+SCORES = {"softmax": 0, "sigmoid": 1}
+
+
+class moe_route_rule(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("score", "n_group", "topk_group", "group_top", "renormalise")] + [
+        ("weight_scale", C.c_float)]
+
+
+class moe_gemm_blk_args(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("a", "sa", "offsets", "b", "sb", "y")] + [
+        ("rows", C.c_int64), ("N", C.c_int32), ("K", C.c_int32), ("groups", C.c_int32)]
+
+
+class moe_blk_ffn_args(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("xq_perm", "sx_perm", "offsets", "wq_gate", "s_gate", "wq_up", "s_up",
+                                          "wq_down", "s_down", "hq_ws", "sh_ws", "y_perm", "h_fp32_debug")]
+
+
+class moe_workspace_layout_blk(C.Structure):
+    _fields_ = [(n, C.c_size_t) for n in ("topk_ids", "topk_w", "counts", "offsets", "perm", "inv_perm", "xq", "sx",
+                                          "xq_perm", "sx_perm", "hq", "sh", "y_perm", "total")]
 
 
 _lib = None
@@ -135,6 +160,18 @@ def load_library() -> C.CDLL:
     lib.moe_expert_ffn_mx.argtypes = [vp, C.POINTER(moe_mx_ffn_args), vp]
     lib.moe_get_workspace_layout_mx.argtypes = [C.POINTER(moe_shape), C.POINTER(moe_workspace_layout_mx)]
     lib.moe_fused_forward_mx.argtypes = [vp, vp, f32p, vp, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.moe_plan_routing_scored.argtypes = [vp, f32p, f32p, C.POINTER(moe_route_rule), i32p, f32p, i32p, i32p, i32p,
+                                            i32p, vp]
+    lib.moe_routing_backward.argtypes = [vp, f32p, i32p, f32p, C.POINTER(moe_route_rule), f32p, vp]
+    lib.moe_combine_backward.argtypes = [vp, vp, vp, i32p, f32p, vp, f32p, vp]
+    lib.moe_quantize_rows_blk.argtypes = [vp, vp, C.c_int64, C.c_int32, vp, f32p, vp]
+    lib.moe_quantize_weights_blk.argtypes = [vp, vp, C.c_int64, C.c_int32, C.c_int32, vp, f32p, vp]
+    lib.moe_dispatch_blk.argtypes = [vp, vp, f32p, i32p, vp, f32p, vp]
+    lib.moe_gemm_blk.argtypes = [vp, C.POINTER(moe_gemm_blk_args), vp]
+    lib.moe_expert_ffn_blk.argtypes = [vp, C.POINTER(moe_blk_ffn_args), vp]
+    lib.moe_get_workspace_layout_blk.argtypes = [C.POINTER(moe_shape), C.POINTER(moe_workspace_layout_blk)]
+    lib.moe_fused_forward_blk.argtypes = [vp, vp, f32p, f32p, C.POINTER(moe_route_rule), vp, f32p, vp, f32p, vp, f32p,
+                                          vp, vp, C.c_size_t, vp]
     lib.moe_last_device_status.argtypes = [vp, C.POINTER(C.c_int32), C.POINTER(C.c_int32), vp]
     lib.moe_last_launch_count.argtypes = [vp]
     lib.moe_last_launch_count.restype = C.c_int32
@@ -178,6 +215,13 @@ def _check(code: int, where: str):
 
 def make_tuning(store_burst_tiles=1, interleave_mode=0, interleave_k=1, schedule=0, dep_lead_D=0, debug_flags=0):
     return moe_tuning(store_burst_tiles, interleave_mode, interleave_k, schedule, dep_lead_D, debug_flags)
+
+
+def make_route_rule(score="softmax", n_group=1, topk_group=1, group_top=1, renormalise=True, weight_scale=1.0):
+    """A moe_route_rule; score is "softmax" or "sigmoid".  The defaults are the rule of moe_plan_routing."""
+    if score not in SCORES:
+        raise ValueError(f"score must be one of {sorted(SCORES)}, got {score!r}")
+    return moe_route_rule(SCORES[score], n_group, topk_group, group_top, 1 if renormalise else 0, weight_scale)
 
 
 def moe_parse_tuning(text):
@@ -398,6 +442,59 @@ class Context:
                                               _ptr(wq_up), _ptr(sf_up), _ptr(wq_down), _ptr(sf_down), _ptr(out),
                                               _ptr(workspace), workspace.numel() * workspace.element_size(),
                                               _stream(stream)), "moe_fused_forward_mx")
+
+    # ---- scored routing and the gradients of the gate
+    def moe_plan_routing_scored(self, logits, bias, rule, topk_ids, topk_w, counts, offsets, perm, inv_perm,
+                                stream=None):
+        _check(self._lib.moe_plan_routing_scored(self._handle, _ptr(logits), _ptr(bias), C.byref(rule), _ptr(topk_ids),
+                                                 _ptr(topk_w), _ptr(counts), _ptr(offsets), _ptr(perm), _ptr(inv_perm),
+                                                 _stream(stream)), "moe_plan_routing_scored")
+
+    def moe_routing_backward(self, logits, topk_ids, d_topk_w, rule, d_logits, stream=None):
+        _check(self._lib.moe_routing_backward(self._handle, _ptr(logits), _ptr(topk_ids), _ptr(d_topk_w),
+                                              C.byref(rule), _ptr(d_logits), _stream(stream)), "moe_routing_backward")
+
+    def moe_combine_backward(self, d_out, y_perm, inv_perm, topk_w, d_y_perm, d_topk_w, stream=None):
+        """d_y_perm may be None when only the weights' gradient is wanted."""
+        _check(self._lib.moe_combine_backward(self._handle, _ptr(d_out), _ptr(y_perm), _ptr(inv_perm), _ptr(topk_w),
+                                              _ptr(d_y_perm), _ptr(d_topk_w), _stream(stream)), "moe_combine_backward")
+
+    # ---- FP8 in blocks of 128
+    def moe_quantize_rows_blk(self, in_bf16, rows, cols, codes, scales, stream=None):
+        _check(self._lib.moe_quantize_rows_blk(self._handle, _ptr(in_bf16), rows, cols, _ptr(codes), _ptr(scales),
+                                               _stream(stream)), "moe_quantize_rows_blk")
+
+    def moe_quantize_weights_blk(self, in_bf16, mats, rows, cols, codes, scales, stream=None):
+        _check(self._lib.moe_quantize_weights_blk(self._handle, _ptr(in_bf16), mats, rows, cols, _ptr(codes),
+                                                  _ptr(scales), _stream(stream)), "moe_quantize_weights_blk")
+
+    def moe_dispatch_blk(self, xq, sx, inv_perm, xq_perm, sx_perm, stream=None):
+        _check(self._lib.moe_dispatch_blk(self._handle, _ptr(xq), _ptr(sx), _ptr(inv_perm), _ptr(xq_perm),
+                                          _ptr(sx_perm), _stream(stream)), "moe_dispatch_blk")
+
+    def moe_gemm_blk(self, a, sa, b, sb, y, rows, N, K, groups=1, offsets=None, stream=None):
+        args = moe_gemm_blk_args(_ptr(a), _ptr(sa), _ptr(offsets), _ptr(b), _ptr(sb), _ptr(y), rows, N, K, groups)
+        _check(self._lib.moe_gemm_blk(self._handle, C.byref(args), _stream(stream)), "moe_gemm_blk")
+
+    def moe_expert_ffn_blk(self, xq_perm, sx_perm, offsets, wq_gate, s_gate, wq_up, s_up, wq_down, s_down, hq_ws, sh_ws,
+                           y_perm, h_fp32_debug=None, stream=None):
+        args = moe_blk_ffn_args(*[_ptr(t) for t in (xq_perm, sx_perm, offsets, wq_gate, s_gate, wq_up, s_up, wq_down,
+                                                    s_down, hq_ws, sh_ws, y_perm, h_fp32_debug)])
+        _check(self._lib.moe_expert_ffn_blk(self._handle, C.byref(args), _stream(stream)), "moe_expert_ffn_blk")
+
+    def workspace_layout_blk(self) -> dict:
+        L = moe_workspace_layout_blk()
+        _check(self._lib.moe_get_workspace_layout_blk(C.byref(self._shape()), C.byref(L)),
+               "moe_get_workspace_layout_blk")
+        return {n: getattr(L, n) for n, _ in moe_workspace_layout_blk._fields_}
+
+    def moe_fused_forward_blk(self, x, logits, bias, rule, wq_gate, s_gate, wq_up, s_up, wq_down, s_down, out, workspace,
+                              stream=None):
+        _check(self._lib.moe_fused_forward_blk(self._handle, _ptr(x), _ptr(logits), _ptr(bias), C.byref(rule),
+                                               _ptr(wq_gate), _ptr(s_gate), _ptr(wq_up), _ptr(s_up), _ptr(wq_down),
+                                               _ptr(s_down), _ptr(out), _ptr(workspace),
+                                               workspace.numel() * workspace.element_size(), _stream(stream)),
+               "moe_fused_forward_blk")
 
     def moe_last_device_status(self, stream=None):
         code, detail = C.c_int32(0), C.c_int32(0)

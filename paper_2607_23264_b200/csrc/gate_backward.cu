@@ -1,0 +1,148 @@
+// Gradients of the gate: the combine's (to the expert rows and the weights) and the scored routing's (to the logits).
+//
+// combine_backward : a warp per slot (t, j).  It reads the token's d_out row and the slot's y row once, writes the
+//                    slot's d_y row and reduces the dot product (per-lane partial sums in fp32, then a fixed butterfly),
+//                    so nothing is accumulated across warps.  Algorithmic traffic: 2H(T + R) read, 2HR written.
+// routing_backward : a warp per token.  The chosen experts' part is k values, one per lane; the row of d_logits is
+//                    written once, and the chosen entries again by the lanes that hold them.
+#include <cuda_bf16.h>
+
+#include "moe_internal.h"
+#include "route_scored.cuh"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr unsigned kFull = 0xFFFFFFFFu;
+
+__global__ void __launch_bounds__(kThreads)
+combine_backward(const uint4* __restrict__ d_out, const uint4* __restrict__ y_perm, const int32_t* __restrict__ inv_perm,
+                 const float* __restrict__ topk_w, uint4* __restrict__ d_y_perm, float* __restrict__ d_topk_w,
+                 long long slots, int k, int vec_per_row) {
+  const int lane = threadIdx.x & 31;
+  const long long slot = static_cast<long long>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
+  if (slot >= slots) return;
+  const size_t row = static_cast<size_t>(inv_perm[slot]);
+  const float w = topk_w[slot];
+  const uint4* g = d_out + static_cast<size_t>(slot / k) * vec_per_row;
+  const uint4* y = y_perm + row * vec_per_row;
+  uint4* d = d_y_perm ? d_y_perm + row * vec_per_row : nullptr;
+  float dot = 0.f;
+  for (int v = lane; v < vec_per_row; v += 32) {
+    const uint4 gv = __ldg(g + v), yv = __ldg(y + v);
+    const __nv_bfloat162* gp = reinterpret_cast<const __nv_bfloat162*>(&gv);
+    const __nv_bfloat162* yp = reinterpret_cast<const __nv_bfloat162*>(&yv);
+    uint4 o;
+    __nv_bfloat162* op = reinterpret_cast<__nv_bfloat162*>(&o);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 a = __bfloat1622float2(gp[i]), b = __bfloat1622float2(yp[i]);
+      dot = fmaf(a.x, b.x, dot);
+      dot = fmaf(a.y, b.y, dot);
+      op[i] = __floats2bfloat162_rn(w * a.x, w * a.y);
+    }
+    if (d) d[v] = o;
+  }
+  dot = moe::warp_sum(dot);
+  if (lane == 0) d_topk_w[slot] = dot;
+}
+
+__global__ void __launch_bounds__(kThreads)
+routing_backward(const float* __restrict__ logits, const int32_t* __restrict__ topk_ids,
+                 const float* __restrict__ d_topk_w, const moe_route_rule rule, float* __restrict__ d_logits, int T, int E,
+                 int k, int32_t* __restrict__ status) {
+  const int lane = threadIdx.x & 31;
+  const int t = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+  if (t >= T) return;
+  const float* row = logits + static_cast<size_t>(t) * E;
+  float* out = d_logits + static_cast<size_t>(t) * E;
+  const bool sigmoid = rule.score == MOE_SCORE_SIGMOID;
+
+  int id = -1;
+  float g = 0.f;
+  if (lane < k) {
+    const size_t s = static_cast<size_t>(t) * k + lane;
+    id = topk_ids[s];
+    g = d_topk_w[s] * rule.weight_scale;
+    if (id < 0 || id >= E) {
+      atomicCAS(&status[0], 0, MOE_ERR_BAD_ROUTING);
+      atomicCAS(&status[1], 0, static_cast<int>(s));
+      id = -1;
+      g = 0.f;
+    }
+  }
+  const float xs = id >= 0 ? row[id] : -INFINITY;
+
+  // largest logit, NaN test and (softmax over all experts) the sum of exponentials
+  bool bad = false;
+  float top = -INFINITY;
+  for (int e = lane; e < E; e += 32) {
+    const float x = row[e];
+    bad |= x != x || (!sigmoid && x == INFINITY);
+    top = fmaxf(top, x);
+  }
+  bad = __any_sync(kFull, bad);
+  const bool dense = !sigmoid && rule.renormalise == 0;   // every expert has a gradient
+  float dot = 0.f, total = 1.f, d;
+  top = moe::warp_max(top);
+  if (top == -INFINITY) top = 0.f;
+  if (sigmoid) {
+    const float s = id >= 0 && xs > -INFINITY ? moe::route_sigmoid(xs) : 0.f;
+    float gs = g;
+    if (rule.renormalise) {
+      const float sum = moe::warp_sum(s);
+      const float mean = sum > 0.f ? moe::warp_sum(g * s) / sum : 0.f;
+      gs = sum > 0.f ? (g - mean) / sum : 0.f;
+    }
+    d = gs * s * (1.f - s);
+  } else if (!dense) {
+    float m = moe::warp_max(xs);
+    if (m == -INFINITY) m = 0.f;
+    const float p = expf(xs - m);
+    const float sum = moe::warp_sum(p);
+    const float q = sum > 0.f ? p / sum : 0.f;
+    d = q * (g - moe::warp_sum(g * q));
+  } else {
+    float sum = 0.f;
+    for (int e = lane; e < E; e += 32) sum += expf(row[e] - top);
+    total = moe::warp_sum(sum);
+    const float p = total > 0.f ? expf(xs - top) / total : 0.f;
+    dot = moe::warp_sum(g * p);
+    d = p * (g - dot);
+  }
+  for (int e = lane; e < E; e += 32) {
+    float v = 0.f;
+    if (dense && total > 0.f) v = -(expf(row[e] - top) / total) * dot;
+    out[e] = bad ? NAN : v;
+  }
+  __syncwarp();
+  if (id >= 0 && !bad) out[id] = d;
+}
+
+}  // namespace
+
+namespace moe {
+
+cudaError_t launch_combine_backward(moe_ctx* ctx, const void* d_out, const void* y_perm, const int32_t* inv_perm,
+                                    const float* topk_w, void* d_y_perm, float* d_topk_w, cudaStream_t stream) {
+  const moe_shape& s = ctx->shape;
+  const long long slots = static_cast<long long>(s.T) * s.k;
+  const int per_block = kThreads / 32;
+  combine_backward<<<static_cast<unsigned>((slots + per_block - 1) / per_block), kThreads, 0, stream>>>(
+      static_cast<const uint4*>(d_out), static_cast<const uint4*>(y_perm), inv_perm, topk_w,
+      static_cast<uint4*>(d_y_perm), d_topk_w, slots, s.k, s.H / 8);
+  ctx->last_launches += 1;
+  return cudaGetLastError();
+}
+
+cudaError_t launch_routing_backward(moe_ctx* ctx, const float* logits, const int32_t* topk_ids, const float* d_topk_w,
+                                    const moe_route_rule& rule, float* d_logits, cudaStream_t stream) {
+  const moe_shape& s = ctx->shape;
+  const int per_block = kThreads / 32;
+  routing_backward<<<(s.T + per_block - 1) / per_block, kThreads, 0, stream>>>(
+      logits, topk_ids, d_topk_w, rule, d_logits, s.T, s.E, s.k, ctx->d_status);
+  ctx->last_launches += 1;
+  return cudaGetLastError();
+}
+
+}  // namespace moe

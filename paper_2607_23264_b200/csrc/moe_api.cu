@@ -815,6 +815,266 @@ moe_status moe_fused_forward_mx(moe_ctx* ctx, const void* x, const float* logits
   return MOE_OK;
 }
 
+// ------------------------------------------------------------------------------------------------ scored routing
+
+}  // extern "C"
+namespace {
+moe_status check_rule(const moe_ctx* ctx, const moe_route_rule* r) {
+  if (!r) return MOE_ERR_INVALID_ARG;
+  const int E = ctx->shape.E;
+  if (r->score != MOE_SCORE_SOFTMAX && r->score != MOE_SCORE_SIGMOID) return MOE_ERR_INVALID_ARG;
+  if (r->n_group < 1 || r->n_group > 32 || E % r->n_group != 0) return MOE_ERR_INVALID_ARG;
+  if (r->topk_group < 1 || r->topk_group > r->n_group) return MOE_ERR_INVALID_ARG;
+  const int size = E / r->n_group;
+  if ((r->group_top != 1 && r->group_top != 2) || r->group_top > size) return MOE_ERR_INVALID_ARG;
+  if (ctx->shape.k > r->topk_group * size) return MOE_ERR_INVALID_ARG;
+  if (r->renormalise != 0 && r->renormalise != 1) return MOE_ERR_INVALID_ARG;
+  if (!(r->weight_scale > -3.4e38f && r->weight_scale < 3.4e38f)) return MOE_ERR_INVALID_ARG;
+  return MOE_OK;
+}
+}  // namespace
+extern "C" {
+
+moe_status moe_plan_routing_scored(moe_ctx* ctx, const float* logits, const float* bias, const moe_route_rule* rule,
+                                   int32_t* topk_ids, float* topk_w, int32_t* counts, int32_t* offsets, int32_t* perm,
+                                   int32_t* inv_perm, void* stream) {
+  moe_status st = check_ctx(ctx);
+  if (st != MOE_OK) return st;
+  begin_call(ctx, 0, stream);
+  st = check_rule(ctx, rule);
+  if (st != MOE_OK) return st;
+  const moe_shape& s = ctx->shape;
+  if (!counts || !offsets) return MOE_ERR_INVALID_ARG;
+  cudaStream_t cs = static_cast<cudaStream_t>(stream);
+  if (s.T == 0) {
+    if (cudaMemsetAsync(counts, 0, static_cast<size_t>(s.E) * 4, cs) != cudaSuccess) return MOE_ERR_CUDA;
+    if (cudaMemsetAsync(offsets, 0, static_cast<size_t>(s.E + 1) * 4, cs) != cudaSuccess) return MOE_ERR_CUDA;
+    return MOE_OK;
+  }
+  const void* ptrs[] = {logits, topk_ids, topk_w, counts, offsets, perm, inv_perm};
+  for (const void* q : ptrs)
+    if (!q || !aligned16(q)) return MOE_ERR_INVALID_ARG;
+  if (!aligned16(bias)) return MOE_ERR_INVALID_ARG;
+  return moe::launch_plan_routing_scored(ctx, logits, bias, *rule, topk_ids, topk_w, counts, offsets, perm, inv_perm,
+                                         cs) == cudaSuccess
+             ? MOE_OK
+             : MOE_ERR_CUDA;
+}
+
+moe_status moe_routing_backward(moe_ctx* ctx, const float* logits, const int32_t* topk_ids, const float* d_topk_w,
+                                const moe_route_rule* rule, float* d_logits, void* stream) {
+  moe_status st = check_ctx(ctx);
+  if (st != MOE_OK) return st;
+  ctx->last_launches = 0;
+  st = check_rule(ctx, rule);
+  if (st != MOE_OK) return st;
+  if (ctx->shape.T == 0) return MOE_OK;
+  const void* ptrs[] = {logits, topk_ids, d_topk_w, d_logits};
+  for (const void* q : ptrs)
+    if (!q || !aligned16(q)) return MOE_ERR_INVALID_ARG;
+  return moe::launch_routing_backward(ctx, logits, topk_ids, d_topk_w, *rule, d_logits,
+                                      static_cast<cudaStream_t>(stream)) == cudaSuccess
+             ? MOE_OK
+             : MOE_ERR_CUDA;
+}
+
+moe_status moe_combine_backward(moe_ctx* ctx, const void* d_out, const void* y_perm, const int32_t* inv_perm,
+                                const float* topk_w, void* d_y_perm, float* d_topk_w, void* stream) {
+  moe_status st = check_ctx(ctx);
+  if (st != MOE_OK) return st;
+  ctx->last_launches = 0;
+  if (ctx->shape.T == 0) return MOE_OK;
+  const void* ptrs[] = {d_out, y_perm, inv_perm, topk_w, d_topk_w};
+  for (const void* q : ptrs)
+    if (!q || !aligned16(q)) return MOE_ERR_INVALID_ARG;
+  if (!aligned16(d_y_perm)) return MOE_ERR_INVALID_ARG;
+  return moe::launch_combine_backward(ctx, d_out, y_perm, inv_perm, topk_w, d_y_perm, d_topk_w,
+                                      static_cast<cudaStream_t>(stream)) == cudaSuccess
+             ? MOE_OK
+             : MOE_ERR_CUDA;
+}
+
+// ------------------------------------------------------------------------------------------------ FP8, blocks of 128
+
+}  // extern "C"
+namespace {
+void fill_layout_blk(const moe_shape& s, moe_workspace_layout_blk* L) {
+  const size_t T = s.T, H = s.H, F = s.F, E = s.E, k = s.k, R = T * k;
+  size_t off = 0;
+  auto take = [&](size_t bytes) { const size_t at = off; off += up256(bytes); return at; };
+  L->topk_ids = take(R * 4);
+  L->topk_w = take(R * 4);
+  L->counts = take(E * 4);
+  L->offsets = take((E + 1) * 4);
+  L->perm = take(R * 4);
+  L->inv_perm = take(R * 4);
+  L->xq = take(T * H);
+  L->sx = take(H / 128 * T * 4);
+  L->xq_perm = take(R * H);
+  L->sx_perm = take(H / 128 * R * 4);
+  L->hq = take(R * F);
+  L->sh = take(F / 128 * R * 4);
+  L->y_perm = take(R * H * 2);
+  L->total = off;
+}
+moe_status check_blk_shape(const moe_shape& s) {
+  return (s.H % 128 == 0 && s.F % 128 == 0) ? MOE_OK : MOE_ERR_UNSUPPORTED_SHAPE;
+}
+}  // namespace
+extern "C" {
+
+moe_status moe_quantize_rows_blk(moe_ctx* ctx, const void* in_bf16, int64_t rows, int32_t cols, void* codes,
+                                 float* scales, void* stream) {
+  moe_status st = check_ctx(ctx);
+  if (st != MOE_OK) return st;
+  ctx->last_launches = 0;
+  if (rows < 0 || rows >= (1LL << 30) || cols <= 0 || cols % 16 != 0) return MOE_ERR_INVALID_ARG;
+  if (rows == 0) return MOE_OK;
+  if (!in_bf16 || !codes || !scales || !aligned16(in_bf16) || !aligned16(codes) || !aligned16(scales))
+    return MOE_ERR_INVALID_ARG;
+  return moe::launch_quantize_rows_blk(ctx, in_bf16, rows, cols, codes, scales, static_cast<cudaStream_t>(stream)) ==
+                 cudaSuccess
+             ? MOE_OK
+             : MOE_ERR_CUDA;
+}
+
+moe_status moe_quantize_weights_blk(moe_ctx* ctx, const void* in_bf16, int64_t mats, int32_t rows, int32_t cols,
+                                    void* codes, float* scales, void* stream) {
+  moe_status st = check_ctx(ctx);
+  if (st != MOE_OK) return st;
+  ctx->last_launches = 0;
+  if (mats < 0 || mats >= (1LL << 30) || rows < 0 || cols <= 0 || cols % 16 != 0) return MOE_ERR_INVALID_ARG;
+  if (mats == 0 || rows == 0) return MOE_OK;
+  if (!in_bf16 || !codes || !scales || !aligned16(in_bf16) || !aligned16(codes) || !aligned16(scales))
+    return MOE_ERR_INVALID_ARG;
+  return moe::launch_quantize_weights_blk(ctx, in_bf16, mats, rows, cols, codes, scales,
+                                          static_cast<cudaStream_t>(stream)) == cudaSuccess
+             ? MOE_OK
+             : MOE_ERR_CUDA;
+}
+
+moe_status moe_dispatch_blk(moe_ctx* ctx, const void* xq, const float* sx, const int32_t* inv_perm, void* xq_perm,
+                            float* sx_perm, void* stream) {
+  moe_status st = check_ctx(ctx);
+  if (st != MOE_OK) return st;
+  st = check_blk_shape(ctx->shape);
+  if (st != MOE_OK) return st;
+  begin_call(ctx, 3, stream);
+  if (ctx->shape.T == 0) return MOE_OK;
+  const void* ptrs[] = {xq, sx, inv_perm, xq_perm, sx_perm};
+  for (const void* q : ptrs)
+    if (!q || !aligned16(q)) return MOE_ERR_INVALID_ARG;
+  // one 4-byte scale per 128 codes: the row mover of the 32-element blocks, whose four scale bytes are such a word
+  return moe::launch_dispatch_mx(ctx, xq, reinterpret_cast<const uint32_t*>(sx), inv_perm, xq_perm,
+                                 reinterpret_cast<uint32_t*>(sx_perm), static_cast<cudaStream_t>(stream)) == cudaSuccess
+             ? MOE_OK
+             : MOE_ERR_CUDA;
+}
+
+moe_status moe_gemm_blk(moe_ctx* ctx, const moe_gemm_blk_args* a, void* stream) {
+  moe_status st = check_ctx(ctx);
+  if (st != MOE_OK) return st;
+  ctx->last_launches = 0;
+  if (!a) return MOE_ERR_INVALID_ARG;
+  if (a->rows < 0 || a->rows >= (1LL << 30) || a->N <= 0 || a->K <= 0 || a->N % 8 != 0 || a->K % 16 != 0 ||
+      a->groups < 1 || a->groups > 1024 || static_cast<long long>(a->groups) * a->N > 0x7FFFFFFFLL)
+    return MOE_ERR_UNSUPPORTED_SHAPE;
+  if (!a->offsets && a->groups != 1) return MOE_ERR_INVALID_ARG;
+  if (a->rows == 0) return MOE_OK;
+  const void* ptrs[] = {a->a, a->sa, a->b, a->sb, a->y};
+  for (const void* q : ptrs)
+    if (!q || !aligned16(q)) return MOE_ERR_INVALID_ARG;
+  if (!aligned16(a->offsets)) return MOE_ERR_INVALID_ARG;
+  return moe::launch_gemm_blk(ctx, a, static_cast<cudaStream_t>(stream));
+}
+
+moe_status moe_expert_ffn_blk(moe_ctx* ctx, const moe_blk_ffn_args* a, void* stream) {
+  moe_status st = check_ctx(ctx);
+  if (st != MOE_OK) return st;
+  st = check_blk_shape(ctx->shape);
+  if (st != MOE_OK) return st;
+  begin_call(ctx, 4, stream);
+  if (!a) return MOE_ERR_INVALID_ARG;
+  if (ctx->shape.T == 0) return MOE_OK;
+  const void* ptrs[] = {a->xq_perm, a->sx_perm, a->offsets, a->wq_gate, a->s_gate, a->wq_up, a->s_up,
+                        a->wq_down, a->s_down, a->hq_ws, a->sh_ws, a->y_perm};
+  for (const void* q : ptrs)
+    if (!q || !aligned16(q)) return MOE_ERR_INVALID_ARG;
+  if (!aligned16(a->h_fp32_debug)) return MOE_ERR_INVALID_ARG;
+  return moe::launch_expert_ffn_blk(ctx, a, static_cast<cudaStream_t>(stream));
+}
+
+moe_status moe_get_workspace_layout_blk(const moe_shape* shape, moe_workspace_layout_blk* out_layout) {
+  if (!out_layout) return MOE_ERR_INVALID_ARG;
+  std::memset(out_layout, 0, sizeof(*out_layout));
+  moe_status st = check_shape(shape);
+  if (st != MOE_OK) return st;
+  st = check_blk_shape(*shape);
+  if (st != MOE_OK) return st;
+  fill_layout_blk(*shape, out_layout);
+  return MOE_OK;
+}
+
+moe_status moe_fused_forward_blk(moe_ctx* ctx, const void* x, const float* logits, const float* bias,
+                                 const moe_route_rule* rule, const void* wq_gate, const float* s_gate,
+                                 const void* wq_up, const float* s_up, const void* wq_down, const float* s_down,
+                                 void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  moe_status st = check_ctx(ctx);
+  if (st != MOE_OK) return st;
+  const moe_shape& s = ctx->shape;
+  st = check_blk_shape(s);
+  if (st != MOE_OK) return st;
+  st = check_rule(ctx, rule);
+  if (st != MOE_OK) return st;
+  if (s.T == 0) { ctx->last_launches = 0; return MOE_OK; }
+  const void* ptrs[] = {x, logits, wq_gate, s_gate, wq_up, s_up, wq_down, s_down, out};
+  for (const void* q : ptrs)
+    if (!q || !aligned16(q)) return MOE_ERR_INVALID_ARG;
+  if (!aligned16(bias)) return MOE_ERR_INVALID_ARG;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return MOE_ERR_INVALID_ARG;
+  moe_workspace_layout_blk L;
+  fill_layout_blk(s, &L);
+  if (workspace_bytes < L.total) return MOE_ERR_WORKSPACE_TOO_SMALL;
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  int32_t* topk_ids = reinterpret_cast<int32_t*>(ws + L.topk_ids);
+  float* topk_w = reinterpret_cast<float*>(ws + L.topk_w);
+  int32_t* counts = reinterpret_cast<int32_t*>(ws + L.counts);
+  int32_t* offsets = reinterpret_cast<int32_t*>(ws + L.offsets);
+  int32_t* perm = reinterpret_cast<int32_t*>(ws + L.perm);
+  int32_t* inv_perm = reinterpret_cast<int32_t*>(ws + L.inv_perm);
+  float* sx = reinterpret_cast<float*>(ws + L.sx);
+  float* sx_perm = reinterpret_cast<float*>(ws + L.sx_perm);
+  cudaStream_t cs = static_cast<cudaStream_t>(stream);
+  begin_call(ctx, 0, stream);
+  if (moe::launch_plan_routing_scored(ctx, logits, bias, *rule, topk_ids, topk_w, counts, offsets, perm, inv_perm, cs) !=
+      cudaSuccess)
+    return MOE_ERR_CUDA;
+  if (moe::launch_quantize_rows_blk(ctx, x, s.T, s.H, ws + L.xq, sx, cs) != cudaSuccess) return MOE_ERR_CUDA;
+  if (moe::launch_dispatch_mx(ctx, ws + L.xq, reinterpret_cast<const uint32_t*>(sx), inv_perm, ws + L.xq_perm,
+                              reinterpret_cast<uint32_t*>(sx_perm), cs) != cudaSuccess)
+    return MOE_ERR_CUDA;
+  moe_blk_ffn_args a{};
+  a.xq_perm = ws + L.xq_perm;
+  a.sx_perm = sx_perm;
+  a.offsets = offsets;
+  a.wq_gate = wq_gate;
+  a.s_gate = s_gate;
+  a.wq_up = wq_up;
+  a.s_up = s_up;
+  a.wq_down = wq_down;
+  a.s_down = s_down;
+  a.hq_ws = ws + L.hq;
+  a.sh_ws = reinterpret_cast<float*>(ws + L.sh);
+  a.y_perm = ws + L.y_perm;
+  a.h_fp32_debug = nullptr;
+  st = moe::launch_expert_ffn_blk(ctx, &a, cs);
+  if (st != MOE_OK) return st;
+  if (moe::launch_combine(ctx, ws + L.y_perm, inv_perm, topk_w, out, cs) != cudaSuccess) return MOE_ERR_CUDA;
+  return MOE_OK;
+}
+
+// ------------------------------------------------------------------------------------------------ host buffers
+
 moe_status moe_fused_forward_host(moe_ctx* ctx, const void* x_host, const float* logits_host,
                                   const void* w_gate, const void* w_up, const void* w_down,
                                   void* out_host, void* workspace, size_t workspace_bytes,

@@ -112,6 +112,16 @@ cudaError_t launch_plan_routing(moe_ctx* ctx, const float* logits, int32_t* topk
 cudaError_t launch_plan_from_topk(moe_ctx* ctx, const int32_t* topk_ids, int32_t* ids_checked, int32_t* counts,
                                   int32_t* offsets, int32_t* perm, int32_t* inv_perm, cudaStream_t stream);
 
+// Plan by a scored rule (moe_route_rule already checked).
+cudaError_t launch_plan_routing_scored(moe_ctx* ctx, const float* logits, const float* bias, const moe_route_rule& rule,
+                                       int32_t* topk_ids, float* topk_w, int32_t* counts, int32_t* offsets,
+                                       int32_t* perm, int32_t* inv_perm, cudaStream_t stream);
+// Gradients of the scored weights (to the logits) and of the combine (to the expert rows and the weights).
+cudaError_t launch_routing_backward(moe_ctx* ctx, const float* logits, const int32_t* topk_ids, const float* d_topk_w,
+                                    const moe_route_rule& rule, float* d_logits, cudaStream_t stream);
+cudaError_t launch_combine_backward(moe_ctx* ctx, const void* d_out, const void* y_perm, const int32_t* inv_perm,
+                                    const float* topk_w, void* d_y_perm, float* d_topk_w, cudaStream_t stream);
+
 cudaError_t launch_dispatch(moe_ctx* ctx, const void* x, const int32_t* inv_perm, void* x_perm,
                             cudaStream_t stream);
 
@@ -151,6 +161,14 @@ cudaError_t launch_dispatch_mx(moe_ctx* ctx, const void* xq, const uint32_t* sfx
                                void* xq_perm, uint32_t* sfx_perm, cudaStream_t stream);
 moe_status launch_expert_ffn_mx(moe_ctx* ctx, const moe_mx_ffn_args* args, cudaStream_t stream);
 cudaError_t prepare_expert_ffn_mx(moe_ctx* ctx);
+
+// FP8 in blocks of 128: quantisation of rows (1 x 128) and weights (128 x 128), the grouped product, the two GEMMs.
+cudaError_t launch_quantize_rows_blk(moe_ctx* ctx, const void* in_bf16, long long rows, int cols, void* codes,
+                                     float* scales, cudaStream_t stream);
+cudaError_t launch_quantize_weights_blk(moe_ctx* ctx, const void* in_bf16, long long mats, int rows, int cols,
+                                        void* codes, float* scales, cudaStream_t stream);
+moe_status launch_gemm_blk(moe_ctx* ctx, const moe_gemm_blk_args* args, cudaStream_t stream);
+moe_status launch_expert_ffn_blk(moe_ctx* ctx, const moe_blk_ffn_args* args, cudaStream_t stream);
 
 cudaError_t prepare_expert_ffn(moe_ctx* ctx);  // one-time kernel attributes (dynamic shared memory size)
 

@@ -1,0 +1,397 @@
+"""FP8 in blocks of 128 on the GPU against the oracle.
+
+Codes and scales are fp32 decisions on both sides: compared bit for bit.  Products are compared on identical operands:
+the bf16 rounding (2^-8 of the value at most) and fp32 sums (one rounding per 32-deep instruction, one for aligning its
+products, one per block: (K/16 + K/128 + 8) 2^-23 of the sum of magnitudes).  The layer is compared element by element
+on the GPU's own h codes, and in norm against the independent oracle, where a last-bit difference in h can move a code."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import blk_oracle as blk
+from oracle import moe_oracle as orc
+from oracle import scored_router_oracle as sro
+from oracle.scored_router_oracle import Rule
+from paper_2607_23264_b200 import binding, inputs as gen
+from moe_testlib import DEV, TOL_FRO, Layer, assert_out_close, bits_to_dev, dev_bf16_to_f64, rel_fro
+
+pytestmark = pytest.mark.gpu
+
+
+def dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(DEV)
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    return binding.Context(1, 64, 64, 1, 1)
+
+
+def spread(rng, rows, cols):
+    return (rng.standard_normal((rows, cols)) * np.exp(rng.uniform(-8, 8, (rows, 1)))).astype(np.float32)
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 16), (1, 128), (7, 144), (37, 256), (300, 1040), (5, 7168), (1001, 112)])
+def test_quantize_rows_bits(ctx, rows, cols):
+    rng = np.random.default_rng(rows + cols)
+    v = spread(rng, rows, cols)
+    v[0, :128] = 0.0
+    if rows > 2:
+        v[2, :16] = 448.0 * 2.0 ** rng.integers(-5, 5, 16)
+    bits = gen.f32_to_bf16_bits(v)
+    nb = -(-cols // 128)
+    codes = torch.full((rows, cols), 0x7F, dtype=torch.uint8, device=DEV)
+    scales = torch.full((nb, rows), float("nan"), device=DEV)
+    ctx.moe_quantize_rows_blk(bits_to_dev(bits), rows, cols, codes, scales)
+    torch.cuda.synchronize()
+    ref_c, ref_s = blk.quantize_rows(gen.bf16_bits_to_f32(bits))
+    assert np.array_equal(scales.cpu().numpy(), ref_s)
+    assert np.array_equal(codes.cpu().numpy(), ref_c)
+
+
+@pytest.mark.parametrize("mats,rows,cols", [(1, 1, 16), (2, 128, 128), (3, 136, 272), (1, 1000, 1040), (5, 64, 384)])
+def test_quantize_weights_bits(ctx, mats, rows, cols):
+    rng = np.random.default_rng(rows + cols)
+    v = np.stack([spread(rng, rows, cols) for _ in range(mats)])
+    v[0, :128, :128] = 0.0
+    bits = gen.f32_to_bf16_bits(v)
+    codes = torch.full((mats, rows, cols), 0x7F, dtype=torch.uint8, device=DEV)
+    scales = torch.full((mats, -(-rows // 128), -(-cols // 128)), float("nan"), device=DEV)
+    ctx.moe_quantize_weights_blk(bits_to_dev(bits), mats, rows, cols, codes, scales)
+    torch.cuda.synchronize()
+    for m in range(mats):
+        ref_c, ref_s = blk.quantize_weights(gen.bf16_bits_to_f32(bits[m]))
+        assert np.array_equal(scales[m].cpu().numpy(), ref_s)
+        assert np.array_equal(codes[m].cpu().numpy(), ref_c)
+
+
+def test_quantize_keeps_nan_and_infinity_visible(ctx):
+    v = np.ones((2, 256), dtype=np.float32)
+    v[0, 3], v[0, 130], v[1, 255] = np.nan, np.inf, -np.inf
+    x = torch.from_numpy(v).to(torch.bfloat16).to(DEV)
+    codes = torch.zeros(2, 256, dtype=torch.uint8, device=DEV)
+    scales = torch.zeros(2, 2, device=DEV)
+    ctx.moe_quantize_rows_blk(x, 2, 256, codes, scales)
+    torch.cuda.synchronize()
+    back = codes.view(torch.float8_e4m3fn).float().cpu() * scales.t().cpu().repeat_interleave(128, 1)
+    assert bool(back[0, 3].isnan()) and torch.equal(back[0, :3], torch.ones(3)) and torch.equal(back[1, :128], torch.ones(128))
+    assert not back[0, 128:].isfinite().any() and not back[1, 128:].isfinite().any()
+
+
+def make_product(rng, counts, N, K, tail=0):
+    """Random operands of a grouped product: (a codes, sa, offsets, [b codes], [sb])."""
+    rows = int(sum(counts)) + tail
+    a, sa = blk.quantize_rows(spread(rng, max(rows, 1), K))
+    b = [blk.quantize_weights((rng.standard_normal((N, K)) * np.exp(rng.uniform(-2, 2))).astype(np.float32)) for _ in counts]
+    offsets = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+    return a, sa, offsets, b
+
+
+def run_product(ctx, a, sa, offsets, b, N, K, use_offsets=True, stream=None):
+    rows, G = a.shape[0], len(b)
+    y = torch.full((rows, N), float("nan"), dtype=torch.bfloat16, device=DEV)
+    args = (dev(a), dev(sa), dev(np.stack([c for c, _ in b])), dev(np.stack([s for _, s in b])))
+    off = dev(offsets)
+    torch.cuda.synchronize()
+    ctx.moe_gemm_blk(*args, y, rows, N, K, groups=G, offsets=off if use_offsets else None, stream=stream)
+    torch.cuda.synchronize()
+    assert ctx.moe_last_device_status()[0] == 0
+    return y
+
+
+def check_product(y, a, sa, offsets, b, N, K):
+    got = dev_bf16_to_f64(y)
+    assert np.isnan(got[offsets[-1]:]).all(), "rows outside every group were written"
+    for g, (bc, bs) in enumerate(b):
+        lo, hi = offsets[g], offsets[g + 1]
+        if hi == lo:
+            continue
+        ref = blk.gemm(a[lo:hi], sa[:, lo:hi], bc, bs)
+        mag = blk.magnitude(a[lo:hi], sa[:, lo:hi], bc, bs)
+        bound = 2.0 ** -8 * np.abs(ref) + (K / 16 + K / 128 + 8) * 2.0 ** -23 * mag
+        err = np.abs(got[lo:hi] - ref)
+        assert (err <= bound).all(), (g, np.nanmax(err / bound))
+
+
+@pytest.mark.parametrize("counts,N,K", [
+    ([1], 8, 16), ([1], 128, 128), ([17], 136, 144), ([64], 256, 256), ([65], 264, 272), ([128], 1024, 384),
+    ([129], 520, 1040), ([200], 384, 640), ([257], 256, 2048), ([700], 512, 512), ([1], 4096, 7168), ([33], 2104, 4112),
+    ([0, 1, 0, 5, 16], 136, 256), ([3, 0, 40, 130, 0, 64], 264, 400), ([17, 15, 48, 49, 96, 97, 112, 113], 128, 128),
+    ([300, 2, 0, 270], 640, 1152), ([1] * 200, 64, 128), ([0] * 9 + [2] + [0] * 1000, 72, 128),
+])
+def test_product(ctx, counts, N, K):
+    rng = np.random.default_rng(N + K + len(counts))
+    a, sa, offsets, b = make_product(rng, counts, N, K, tail=3 if len(counts) > 1 else 0)
+    y = run_product(ctx, a, sa, offsets, b, N, K)
+    check_product(y, a, sa, offsets, b, N, K)
+    if len(counts) == 1:
+        assert torch.equal(run_product(ctx, a, sa, offsets, b, N, K, use_offsets=False).view(torch.int16), y.view(torch.int16))
+    again = run_product(ctx, a, sa, offsets, b, N, K, stream=torch.cuda.Stream())
+    assert torch.equal(again.view(torch.int16), y.view(torch.int16)), "not the same bits on another stream"
+
+
+def test_product_random_shapes(ctx):
+    rng = np.random.default_rng(21)
+    for trial in range(24):
+        G = int(rng.integers(1, 9)) if trial % 2 else 1
+        counts = [int(rng.integers(0, 2) * np.exp(rng.uniform(0, 6))) for _ in range(G)]
+        if not sum(counts):
+            counts[0] = 1 + trial
+        N, K = 8 * int(np.exp(rng.uniform(0, 5))), 16 * int(np.exp(rng.uniform(0, 5)))
+        a, sa, offsets, b = make_product(rng, counts, N, K)
+        check_product(run_product(ctx, a, sa, offsets, b, N, K), a, sa, offsets, b, N, K)
+
+
+def test_product_scales_of_all_sizes(ctx):
+    """Scales far apart between blocks: the running sum must not lose the small ones to a common exponent."""
+    rng = np.random.default_rng(8)
+    N, K, M = 128, 512, 40
+    a, sa, offsets, b = make_product(rng, [M], N, K)
+    sa *= np.array([2.0 ** -60, 1.0, 2.0 ** 40, 2.0 ** -20], dtype=np.float32)[:, None]
+    sb = b[0][1] * np.array([2.0 ** 50, 1.0, 2.0 ** -50, 2.0 ** 10], dtype=np.float32)
+    b = [(b[0][0], sb)]
+    check_product(run_product(ctx, a, sa, offsets, b, N, K), a, sa, offsets, b, N, K)
+
+
+def test_nan_rows_stay_in_their_rows(ctx):
+    rng = np.random.default_rng(12)
+    a, sa, offsets, b = make_product(rng, [20, 30], 128, 256)
+    a[7, 5], a[25, 200] = 0x7F, 0xFF
+    y = dev_bf16_to_f64(run_product(ctx, a, sa, offsets, b, 128, 256))
+    bad = np.isnan(y).all(axis=1)
+    assert list(np.flatnonzero(bad)) == [7, 25] and np.isfinite(np.delete(y, [7, 25], axis=0)).all()
+
+
+def test_input_gradient_is_the_product_with_transposed_weights(ctx):
+    """d_a = d_y . b is the same call on the transposed codes and scales; against differences of the fp64 product."""
+    rng = np.random.default_rng(30)
+    N, K, M = 256, 384, 20
+    (bc, bs) = blk.quantize_weights(rng.standard_normal((N, K)).astype(np.float32))
+    g, sg = blk.quantize_rows(rng.standard_normal((M, N)).astype(np.float32))
+    off = np.array([0, M], dtype=np.int32)
+    bt = [(np.ascontiguousarray(bc.T), np.ascontiguousarray(bs.T))]
+    y = run_product(ctx, g, sg, off, bt, K, N)
+    check_product(y, g, sg, off, bt, K, N)
+    w, gv = blk.dequantize_weights(bc, bs), blk.dequantize_rows(g, sg)
+    x = rng.standard_normal((M, K))
+    got = dev_bf16_to_f64(y)
+    for r, c in ((0, 0), (3, 200), (19, 383)):
+        e = np.zeros((M, K))
+        e[r, c] = 1e-3
+        diff = (((x + e) @ w.T * gv).sum() - ((x - e) @ w.T * gv).sum()) / 2e-3
+        assert abs(diff - got[r, c]) <= 2.0 ** -8 * abs(diff) + 1e-3
+
+
+def test_product_refusals(ctx):
+    t8, t4 = torch.zeros(4096, dtype=torch.uint8, device=DEV), torch.zeros(64, device=DEV)
+    y = torch.zeros(256, dtype=torch.bfloat16, device=DEV)
+    off = torch.zeros(8, dtype=torch.int32, device=DEV)
+
+    def call(a=t8, sa=t4, b=t8, sb=t4, y=y, rows=2, N=16, K=32, groups=1, offsets=None):
+        ctx.moe_gemm_blk(a, sa, b, sb, y, rows, N, K, groups=groups, offsets=offsets)
+
+    call()
+    call(rows=0)
+    for bad, code in ((dict(N=12), 2), (dict(K=24), 2), (dict(N=0), 2), (dict(K=0), 2), (dict(rows=-1), 2),
+                      (dict(groups=0), 2), (dict(groups=1025, offsets=off), 2), (dict(rows=1 << 30), 2),
+                      (dict(groups=2), 1), (dict(a=None), 1), (dict(sb=None), 1), (dict(y=None), 1),
+                      (dict(a=t8[1:2049]), 1), (dict(sa=t4[1:33]), 1), (dict(offsets=off[1:3], groups=1), 1)):
+        with pytest.raises(binding.MoeError) as e:
+            call(**bad)
+        assert e.value.code == code, bad
+    for f in (lambda: ctx.moe_quantize_rows_blk(y, 1, 24, t8, t4), lambda: ctx.moe_quantize_rows_blk(y, -1, 16, t8, t4),
+              lambda: ctx.moe_quantize_rows_blk(None, 1, 16, t8, t4), lambda: ctx.moe_quantize_weights_blk(y, 1, 1, 8, t8, t4),
+              lambda: ctx.moe_quantize_weights_blk(y, -1, 1, 16, t8, t4)):
+        with pytest.raises(binding.MoeError) as e:
+            f()
+        assert e.value.code == 1
+    odd = binding.Context(4, 192, 128, 2, 1)                 # H is not a multiple of 128
+    with pytest.raises(binding.MoeError) as e:
+        odd.workspace_layout_blk()
+    assert e.value.code == 2
+    for f in (lambda: odd.moe_dispatch_blk(t8, t4, off, t8, t4),
+              lambda: odd.moe_expert_ffn_blk(*[t8] * 12),
+              lambda: odd.moe_fused_forward_blk(t8, t4, None, binding.make_route_rule(), *[t8] * 6, y, t8)):
+        with pytest.raises(binding.MoeError) as e:
+            f()
+        assert e.value.code == 2
+    small = binding.Context(4, 128, 128, 2, 1)
+    with pytest.raises(binding.MoeError) as e:
+        small.moe_fused_forward_blk(t8, t4, None, binding.make_route_rule(), *[t8] * 6, y, t8[:256])
+    assert e.value.code == 3
+    with pytest.raises(binding.MoeError) as e:
+        small.moe_fused_forward_blk(t8, t4, None, binding.make_route_rule(n_group=3), *[t8] * 6, y, t8)
+    assert e.value.code == 1
+
+
+class BlkLayer:
+    """A layer whose weights are quantised on the GPU, with the oracle's own quantisation beside it."""
+
+    def __init__(self, cfg, x_bits=None):
+        self.cfg = cfg
+        self.L = Layer(cfg, x_bits=x_bits)
+        L, E, F, H = self.L, cfg.E, cfg.F, cfg.H
+        self.q = {}
+        for name, t, rows, cols in (("gate", L.w_gate, F, H), ("up", L.w_up, F, H), ("down", L.w_down, H, F)):
+            codes = torch.full((E, rows, cols), 0x7F, dtype=torch.uint8, device=DEV)
+            scales = torch.full((E, rows // 128, cols // 128), float("nan"), device=DEV)
+            L.ctx.moe_quantize_weights_blk(t, E, rows, cols, codes, scales)
+            self.q[name] = (codes, scales)
+        torch.cuda.synchronize()
+        self._wq = {}
+
+    def weights(self):
+        return [t for n in ("gate", "up", "down") for t in self.q[n]]
+
+    def oracle_weights(self, e):
+        if e not in self._wq:
+            self._wq[e] = [blk.quantize_weights(gen.bf16_bits_to_f32(w)) for w in self.L.weights(e)]
+        return self._wq[e]
+
+
+def cfg_of(T, H, F, E, k, seed, router="xWr"):
+    return gen.MoEConfig(name="blk", T=T, H=H, F=F, E=E, k=k, seed=seed, router=router)
+
+
+@pytest.mark.parametrize("T,H,F,E,k,router", [
+    (64, 128, 128, 4, 2, "xWr"),
+    (300, 512, 384, 8, 2, "xWr"),
+    (129, 256, 640, 16, 4, "xWr_zipf"),
+    (5, 384, 256, 6, 6, "xWr"),
+    (1, 256, 128, 3, 1, "xWr"),
+    (70, 128, 128, 1024, 32, "xWr"),
+    (700, 256, 384, 2, 2, "xWr"),
+])
+def test_expert_ffn_parity(T, H, F, E, k, router):
+    cfg = cfg_of(T, H, F, E, k, seed=T + H, router=router)
+    M = BlkLayer(cfg)
+    L, ctx = M.L, M.L.ctx
+    L.plan()
+    R = cfg.R
+    xq = torch.full((T, H), 0x7F, dtype=torch.uint8, device=DEV)
+    sx = torch.full((H // 128, T), float("nan"), device=DEV)
+    ctx.moe_quantize_rows_blk(L.x, T, H, xq, sx)
+    xq_perm = torch.full((R, H), 0x7F, dtype=torch.uint8, device=DEV)
+    sx_perm = torch.full((H // 128, R), float("nan"), device=DEV)
+    ctx.moe_dispatch_blk(xq, sx, L.inv_perm, xq_perm, sx_perm)
+    torch.cuda.synchronize()
+    ref_c, ref_s = blk.quantize_rows(gen.bf16_bits_to_f32(L.x_bits))
+    tok = L.perm.cpu().numpy().astype(np.int64) // k
+    assert np.array_equal(xq_perm.cpu().numpy(), ref_c[tok]) and np.array_equal(sx_perm.cpu().numpy(), ref_s[:, tok])
+    for e in (0, E - 1):
+        for (c, s), name in zip(M.oracle_weights(e), ("gate", "up", "down")):
+            assert np.array_equal(M.q[name][0][e].cpu().numpy(), c) and np.array_equal(M.q[name][1][e].cpu().numpy(), s)
+    hq = torch.full((R, F), 0x7F, dtype=torch.uint8, device=DEV)
+    sh = torch.full((F // 128, R), float("nan"), device=DEV)
+    y = L.nan_bf16(R, H)
+    h_dbg = torch.full((R, F), float("nan"), device=DEV)
+    ctx.moe_expert_ffn_blk(xq_perm, sx_perm, L.offsets, *M.weights(), hq, sh, y, h_dbg)
+    torch.cuda.synchronize()
+    L.check_device_status()
+    offsets = L.offsets.cpu().numpy()
+    xc, xs = ref_c[tok], ref_s[:, tok]
+    h_gpu = h_dbg.cpu().numpy()
+    assert np.isfinite(h_gpu).all()
+    # h's codes and scales are the oracle's quantisation of the GPU's own fp32 h
+    req_c, req_s = blk.quantize_rows(h_gpu)
+    assert np.array_equal(hq.cpu().numpy(), req_c) and np.array_equal(sh.cpu().numpy(), req_s)
+    y_gpu = dev_bf16_to_f64(y)
+    for e in range(E):
+        lo, hi = int(offsets[e]), int(offsets[e + 1])
+        if hi == lo:
+            continue
+        gate, up, down = M.oracle_weights(e)
+        h_ref = blk.expert_rows(xc[lo:hi], xs[:, lo:hi], gate, up)
+        assert rel_fro(h_gpu[lo:hi].astype(np.float64), h_ref) <= TOL_FRO / 50, e
+        ref = blk.gemm(req_c[lo:hi], req_s[:, lo:hi], *down)
+        mag = blk.magnitude(req_c[lo:hi], req_s[:, lo:hi], *down)
+        assert (np.abs(y_gpu[lo:hi] - ref) <= 2.0 ** -8 * np.abs(ref) + (F / 16 + F / 128 + 8) * 2.0 ** -23 * mag).all(), e
+
+
+def check_fused(M, rule, bias, ws, out, tokens, samples=40):
+    """out of a fused call against the oracle on the GPU's own h codes, and in norm against the independent oracle."""
+    cfg, L, ctx = M.cfg, M.L, M.L.ctx
+    H, F, E, k = cfg.H, cfg.F, cfg.E, cfg.k
+    lay = ctx.workspace_layout_blk()
+    R = tokens * k
+    part = lambda n, count, kind: ws[lay[n]:lay[n] + 4 * count].view(kind).cpu().numpy()  # noqa: E731
+    ids, w = part("topk_ids", R, torch.int32).reshape(tokens, k), part("topk_w", R, torch.float32).reshape(tokens, k)
+    inv = part("inv_perm", R, torch.int32)
+    ref_ids, _ = sro.route(L.logits[:tokens], bias, rule, k)
+    assert (ids == ref_ids).all(1).mean() >= 0.97
+    counts, offsets, perm, inv_ref = orc.plan_permutation(ids, E)
+    assert np.array_equal(inv, inv_ref)
+    hq = ws[lay["hq"]:lay["hq"] + R * F].view(R, F).cpu().numpy()
+    sh = part("sh", F // 128 * R, torch.float32).reshape(F // 128, R)
+    toks = np.unique(np.linspace(0, tokens - 1, min(tokens, samples)).astype(int))
+    xc, xs = blk.quantize_rows(gen.bf16_bits_to_f32(L.x_bits[toks]))
+    own, free = np.zeros((len(toks), H)), np.zeros((len(toks), H))
+    for i, t in enumerate(toks):
+        for j in range(k):
+            gate, up, down = M.oracle_weights(int(ids[t, j]))
+            row = int(inv[t * k + j])
+            own[i] += w[t, j] * blk.gemm(hq[row:row + 1], sh[:, row:row + 1], *down)[0]
+            hc, hs = blk.quantize_rows(blk.expert_rows(xc[i:i + 1], xs[:, i:i + 1], gate, up))
+            free[i] += w[t, j] * blk.gemm(hc, hs, *down)[0]
+    got = dev_bf16_to_f64(out)[toks]
+    assert np.isfinite(got).all()
+    assert_out_close(got, own, f"out, {tokens} tokens, on the GPU's h codes")
+    if tokens >= 33:
+        assert rel_fro(got, free) <= 2e-2
+
+
+def test_fused_forward_and_smaller_batches():
+    cfg = cfg_of(300, 384, 256, 16, 4, seed=31)
+    M = BlkLayer(cfg)
+    L, ctx = M.L, M.L.ctx
+    rule = Rule("sigmoid", 4, 2, 2, True, 2.5)
+    r = binding.make_route_rule("sigmoid", 4, 2, 2, True, 2.5)
+    bias = (np.arange(cfg.E) % 5 / 32).astype(np.float32)
+    d_bias = dev(bias)
+    ws = torch.empty(ctx.workspace_layout_blk()["total"], dtype=torch.uint8, device=DEV)
+    for tokens in (300, 33, 1, 0):
+        ctx.moe_set_active_tokens(tokens)
+        out = L.nan_bf16(max(tokens, 1), cfg.H)
+        x, logits = L.x[:max(tokens, 1)].contiguous(), L.d_logits[:max(tokens, 1)].contiguous()
+        ctx.moe_fused_forward_blk(x, logits, d_bias, r, *M.weights(), out, ws)
+        torch.cuda.synchronize()
+        L.check_device_status()
+        if tokens == 0:
+            assert ctx.moe_last_launch_count() == 0
+            continue
+        check_fused(M, rule, bias, ws, out, tokens)
+        again = L.nan_bf16(tokens, cfg.H)
+        ctx.moe_fused_forward_blk(x, logits, d_bias, r, *M.weights(), again, ws, stream=torch.cuda.Stream())
+        torch.cuda.synchronize()
+        assert torch.equal(out.view(torch.int16), again.view(torch.int16))
+
+
+def test_fused_forward_long_k_loops():
+    # K loops of 32 and 11 blocks, 11 column tiles of Linear-1, hundreds of rows per expert
+    cfg = cfg_of(1024, 4096, 1408, 2, 2, seed=9)
+    M = BlkLayer(cfg)
+    L, ctx = M.L, M.L.ctx
+    ws = torch.empty(ctx.workspace_layout_blk()["total"], dtype=torch.uint8, device=DEV)
+    out = L.nan_bf16(cfg.T, cfg.H)
+    ctx.moe_fused_forward_blk(L.x, L.d_logits, None, binding.make_route_rule(), *M.weights(), out, ws)
+    torch.cuda.synchronize()
+    L.check_device_status()
+    check_fused(M, Rule(), None, ws, out, cfg.T, samples=16)
+
+
+def test_fused_forward_of_a_token_with_every_expert_masked_is_zero():
+    cfg = cfg_of(40, 128, 128, 8, 2, seed=3)
+    M = BlkLayer(cfg)
+    L, ctx = M.L, M.L.ctx
+    logits = L.d_logits.clone()
+    logits[7] = -float("inf")
+    ws = torch.empty(ctx.workspace_layout_blk()["total"], dtype=torch.uint8, device=DEV)
+    out, ref = L.nan_bf16(cfg.T, cfg.H), L.nan_bf16(cfg.T, cfg.H)
+    rule = binding.make_route_rule("sigmoid")
+    ctx.moe_fused_forward_blk(L.x, L.d_logits, None, rule, *M.weights(), ref, ws)
+    ctx.moe_fused_forward_blk(L.x, logits, None, rule, *M.weights(), out, ws)
+    torch.cuda.synchronize()
+    L.check_device_status()
+    assert out[7].eq(0).all()
+    keep = [t for t in range(cfg.T) if t != 7]
+    assert torch.equal(out[keep].view(torch.int16), ref[keep].view(torch.int16))
