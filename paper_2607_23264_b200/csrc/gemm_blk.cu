@@ -1,182 +1,644 @@
-// Grouped product of E4M3 rows and weights with fp32 scales per block of 128, and the two expert GEMMs on it.
+// Grouped product of E4M3 rows and weights with fp32 scales per block of 128, and the two expert GEMMs on it:
+//     y[r,n] = sum_b sa[b][r] sb[n/128][b] * P_b[r,n],     P_b[r,n] = sum_{k in block b} a[r,k] w[n,k]
+// The scales are arbitrary fp32 numbers, which the tensor pipe cannot apply, so each block's P_b is an accumulator of its
+// own in tensor memory (four MMAs, fp32), and epilogue warps add it, scaled, to the running sum in their registers
+// while the tensor pipe computes the next block into the other half of tensor memory.
 //
-// One thread per output column, 16 rows per CTA: per block of 128 along K the rows' codes are widened into shared
-// memory, each thread walks its weight row's 128 codes and keeps one fp32 partial sum per row, which is then scaled
-// into the running sum.  Linear-1 carries two such sums (gate, up) and quantises its 128 columns of h in the epilogue.
+// Operands are swapped: 256 weight rows (Linear-1: 128 gate and the matching 128 up rows) are the M side of two MMAs,
+// the rows of a, padded to 16, 32, 64, 96 or 128, their N side.  So an expert of few rows costs few multiply-adds and
+// its weights are read once, whatever its size up to 128 rows; more rows are split evenly into blocks that run side by
+// side and share the weights in L2.
+//
+// Roles (384 threads, 168 registers each at launch, moved to where they are needed): warp 0 = TMA producer, warp 1 =
+// MMA issuer, warps 2-3 = scale loaders (sa * sb per row and weight box, a ring of four blocks in shared memory),
+// warps 4-11 = epilogue (four lane quarters x two halves of the rows; 128 running sums per thread at most).
+// Shapes with too few tiles for the SMs split K over a cluster of 2, 4 or 8 CTAs, which add their running sums through
+// distributed shared memory in rank order: no scratch memory, no atomics, the same bits every time.
+// Every wait is bounded; a wait that gives up is reported through the status word and the CTA unwinds.
 #include <cuda_bf16.h>
-#include <cuda_fp8.h>
+
+#include <type_traits>
 
 #include "blk_quant.cuh"
 #include "ffn_math.cuh"
 #include "moe_internal.h"
+#include "ptx_sm100.cuh"
 
 namespace {
 
-constexpr int kCols = 128;   // output columns (threads) per CTA
-constexpr int kRows = 16;    // rows per CTA
+constexpr int kThreads = 384;
+constexpr int kEpilogueThreads = 256;
+constexpr int BW = 128;                  // rows of one weight box (M of an MMA)
+constexpr int BK = 128;                  // K elements (= bytes) per block: one 128-byte swizzle row, one scale
+constexpr int UMMA_K = 32;
+constexpr int kWBoxBytes = BW * BK;
+constexpr int kRowBox = 16;              // rows of a per TMA box
+constexpr int kMaxStages = 6;
+constexpr int kScaleSlots = 4;
+constexpr int kScaleThreads = 64;
+constexpr int kTmemCols = 512;           // two buffers x two weight boxes x 128 columns
+constexpr int kTmemBuf = 256;
+constexpr int kOutTokens = 8;            // rows of a staged per step of the tile's end, per epilogue half
+constexpr int kMaxSmem = 227 * 1024;
+constexpr int kKernelIdBlk = 10;         // in the detail word of a time-out: 10 * 65536 + role
 
 struct BlkParams {
-  const unsigned char* a;    // [rows, K]
-  const float* sa;           // [kb][rows]
-  const int32_t* offsets;    // [groups + 1] or null
-  const unsigned char* b0;   // [groups, N, K]
-  const unsigned char* b1;   // gated: the up matrix
-  const float* sb0;          // [groups][nb][kb]
-  const float* sb1;
-  __nv_bfloat16* y;          // [rows, N]
-  unsigned char* hq;         // gated: [rows, N]
-  float* sh;                 // gated: [N/128][rows]
-  float* h_dbg;
-  long long rows;
-  int N, K, groups;
+  const int32_t* offsets;   // [groups + 1] or null: one group of all rows
+  int groups;
+  int N;                    // output columns: F (Linear-1) or the product's N
+  int n_tiles;              // column tiles: ceil(N / 128) gated, ceil(N / 256) otherwise
+  int k_blocks;             // ceil(K / 128)
+  int n_blocks;             // ceil(N / 128): pitch of the weight scales
+  int rows;
+  int stages;
+  int split;                // CTAs per tile along K (the cluster size)
+  const float* sa;          // [k_blocks][rows]
+  const float* sb0;         // [groups][n_blocks][k_blocks]; gated: gate
+  const float* sb1;         // gated: up
+  __nv_bfloat16* y;         // [rows, N]
+  uint32_t* hq;             // gated: E4M3 [rows, N], four codes per word
+  float* sh;                // gated: [N/128][rows]
+  float* h_dbg;             // gated: optional fp32 [rows, N]
+  int32_t* status;
 };
 
-__device__ __forceinline__ float fp8_value(unsigned char c) {
-  return __half2float(__half(__nv_cvt_fp8_to_halfraw(c, __NV_E4M3)));
+struct BlkTail {
+  uint64_t full[kMaxStages];
+  uint64_t empty[kMaxStages];
+  uint64_t acc_full[2];
+  uint64_t acc_empty[2];
+  uint64_t sc_full[kScaleSlots];
+  uint64_t sc_empty[kScaleSlots];
+  uint64_t out_sync[2];     // meeting points of an epilogue half's four warps
+  uint32_t tmem_base;
+  int abort_flag;
+};
+
+struct BlkTile {
+  int row0, rows;    // rows of a: row0 .. row0 + rows - 1
+  int n_pad;         // their number padded to 16, 32, 64, 96 or 128
+  int n0;            // first output column
+  int group;
+  int single;        // no other tile reads these weights
+};
+
+__device__ __forceinline__ void blk_timeout(const BlkParams& p, int role) {
+  atomicCAS(&p.status[0], 0, MOE_ERR_TIMEOUT);
+  atomicCAS(&p.status[1], 0, kKernelIdBlk * 65536 + role);
+}
+
+// Tile t of the list ordered by (group, column tile, row block): the row blocks of a group and column tile are
+// neighbours, so CTAs that run side by side share the weight boxes in L2.
+template <bool kGated, int kMaxN>
+__device__ __forceinline__ BlkTile blk_decode(int t, const int32_t* prefix, const int32_t* offs, const BlkParams& p) {
+  int lo = 0, hi = p.groups;   // invariant: prefix[lo] * n_tiles <= t < prefix[hi] * n_tiles
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (prefix[mid] * p.n_tiles <= t) lo = mid; else hi = mid;
+  }
+  const int blocks = prefix[lo + 1] - prefix[lo];
+  const int local = t - prefix[lo] * p.n_tiles;
+  const int nb = local / blocks, mb = local - nb * blocks;
+  const int rows = offs[2 * lo + 1] - offs[2 * lo];
+  const int per = ((rows + blocks - 1) / blocks + 15) & ~15;   // even blocks: a short last one would waste a tile
+  BlkTile tile;
+  tile.row0 = offs[2 * lo] + mb * per;
+  tile.rows = max(0, min(per, rows - mb * per));
+  const int n = tile.rows;
+  tile.n_pad = n <= 16 ? 16 : n <= 32 ? 32 : n <= 64 ? 64 : n <= 96 ? 96 : 128;
+  tile.n0 = nb * (kGated ? BW : 2 * BW);
+  tile.group = lo;
+  tile.single = blocks == 1 ? 1 : 0;
+  return tile;
+}
+
+// One row of the output from its running sums: lane l holds columns n0 + 4 l .. + 3 of each weight box.
+template <bool kGated>
+__device__ __forceinline__ void blk_finish_row(const BlkParams& p, int row, int n0, int lane, const float4& a,
+                                               const float4& b) {
+  if constexpr (kGated) {
+    // silu(g) * u with an exponential and a division good to 2 ulp each: h is quantised from here, and an error of
+    // 2^-11 (a hardware tanh) would move one code in a hundred
+    const float g[4] = {a.x, a.y, a.z, a.w}, u[4] = {b.x, b.y, b.z, b.w};
+    float h[4], amax = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      h[i] = __fdividef(g[i], 1.0f + __expf(-g[i])) * u[i];
+      amax = fmaxf(amax, fabsf(h[i]));
+    }
+    amax = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(amax)));
+    const float sc = blk::scale_of(amax);
+    const size_t at = static_cast<size_t>(row) * p.N + n0 + 4 * lane;
+    p.hq[at >> 2] = blk::pack4(h[0], h[1], h[2], h[3], sc);
+    if (lane == 0) p.sh[static_cast<size_t>(n0 / BW) * p.rows + row] = sc;
+    if (p.h_dbg != nullptr) *reinterpret_cast<float4*>(p.h_dbg + at) = make_float4(h[0], h[1], h[2], h[3]);
+  } else {
+    const int c0 = n0 + 4 * lane, c1 = c0 + BW;
+    __nv_bfloat16* y = p.y + static_cast<size_t>(row) * p.N;
+    if (c0 < p.N) *reinterpret_cast<uint2*>(y + c0) = make_uint2(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w));
+    if (c1 < p.N) *reinterpret_cast<uint2*>(y + c1) = make_uint2(pack_bf16(b.x, b.y), pack_bf16(b.z, b.w));
+  }
+}
+
+template <int kCols>
+__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[kCols]) {
+  if constexpr (kCols == 8) ptx::tmem_ld_32x8(taddr, r);
+  else if constexpr (kCols == 16) ptx::tmem_ld_32x16(taddr, r);
+  else ptx::tmem_ld_32x32(taddr, r);
+}
+
+// acc[0 .. kCols) += P * f for kCols columns of tensor memory; f are the columns' scales in shared memory.
+template <int kCols>
+__device__ __forceinline__ void blk_add_cols(uint32_t taddr, const float* f, uint64_t* acc) {
+  uint32_t v[kCols];
+  tmem_ld_cols<kCols>(taddr, v);
+  ptx::tmem_ld_wait();
+#pragma unroll
+  for (int i = 0; i < kCols; i += 4) {
+    const ulonglong2 s = *reinterpret_cast<const ulonglong2*>(f + i);
+    acc[i / 2] = ptx::fma_f32x2(ptx::pack_f32x2(v[i], v[i + 1]), s.x, acc[i / 2]);
+    acc[i / 2 + 1] = ptx::fma_f32x2(ptx::pack_f32x2(v[i + 2], v[i + 3]), s.y, acc[i / 2 + 1]);
+  }
+}
+
+template <bool kGated, int kMaxN>
+__global__ void __launch_bounds__(kThreads, 1)
+gemm_blk_swapped(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b0,
+                 const __grid_constant__ CUtensorMap tm_b1, const BlkParams p) {
+  constexpr int kStageBytes = 2 * kWBoxBytes + kMaxN * BK;
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t raw = ptx::smem_u32(smem_raw);
+  const uint32_t pad = (1024u - (raw & 1023u)) & 1023u;
+  unsigned char* base = smem_raw + pad;                      // 1024-byte aligned: required by the swizzle
+  const uint32_t ring_u32 = raw + pad;
+  float* s_out = reinterpret_cast<float*>(base + p.stages * kStageBytes);      // [2][kOutTokens][256]
+  float* s_scale = s_out + 2 * kOutTokens * 256;                               // [kScaleSlots][2][kMaxN]
+  BlkTail* st = reinterpret_cast<BlkTail*>(s_scale + kScaleSlots * 2 * kMaxN);
+  int32_t* prefix = reinterpret_cast<int32_t*>(st + 1);                        // [groups + 1] row blocks before a group
+  int32_t* offs = prefix + p.groups + 1;                                       // [groups][2] first row, end
+
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+
+  if (tid == 0) {
+    for (int s = 0; s < p.stages; ++s) {
+      ptx::mbar_init(ptx::smem_u32(&st->full[s]), 1);
+      ptx::mbar_init(ptx::smem_u32(&st->empty[s]), 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      ptx::mbar_init(ptx::smem_u32(&st->acc_full[a]), 1);
+      ptx::mbar_init(ptx::smem_u32(&st->acc_empty[a]), kEpilogueThreads / 32);
+    }
+    for (int s = 0; s < kScaleSlots; ++s) {
+      ptx::mbar_init(ptx::smem_u32(&st->sc_full[s]), kScaleThreads);
+      ptx::mbar_init(ptx::smem_u32(&st->sc_empty[s]), kEpilogueThreads / 32);
+    }
+    for (int h = 0; h < 2; ++h) ptx::mbar_init(ptx::smem_u32(&st->out_sync[h]), kEpilogueThreads / 64);
+    st->abort_flag = 0;
+    prefix[0] = 0;
+    ptx::fence_barrier_init();
+    ptx::fence_proxy_async_smem();
+  }
+  if (warp == 0) {
+    int32_t run = 0;
+    for (int b0 = 0; b0 < p.groups; b0 += 32) {
+      const int e = b0 + lane;
+      int32_t v = 0;
+      if (e < p.groups) {
+        // clamped: whatever the offsets hold, no row outside [0, rows) is touched
+        int32_t lo = p.offsets ? p.offsets[e] : 0, hi = p.offsets ? p.offsets[e + 1] : p.rows;
+        lo = min(max(lo, 0), p.rows);
+        hi = min(max(hi, lo), p.rows);
+        offs[2 * e] = lo;
+        offs[2 * e + 1] = hi;
+        v = (hi - lo + kMaxN - 1) / kMaxN;
+      }
+#pragma unroll
+      for (int off = 1; off < 32; off <<= 1) {
+        const int32_t o = __shfl_up_sync(0xFFFFFFFFu, v, off);
+        if (lane >= off) v += o;
+      }
+      if (e < p.groups) prefix[e + 1] = run + v;
+      run += __shfl_sync(0xFFFFFFFFu, v, 31);
+    }
+    if (lane == 0) {
+      ptx::prefetch_tensormap(&tm_a);
+      ptx::prefetch_tensormap(&tm_b0);
+      if (kGated) ptx::prefetch_tensormap(&tm_b1);
+    }
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc(ptx::smem_u32(&st->tmem_base), kTmemCols);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  ptx::tc_fence_after_sync();
+
+  const uint32_t tmem_base = st->tmem_base;
+  const int total_tiles = prefix[p.groups] * p.n_tiles;
+  volatile int* abort_flag = &st->abort_flag;
+  // this CTA's tiles and its part of K
+  const int rank = p.split > 1 ? static_cast<int>(ptx::cluster_ctarank()) : 0;
+  const int first = blockIdx.x / p.split, step = gridDim.x / p.split;
+  const int kb0 = static_cast<int>(static_cast<long long>(rank) * p.k_blocks / p.split);
+  const int kb1 = static_cast<int>(static_cast<long long>(rank + 1) * p.k_blocks / p.split);
+
+  if (warp < 4) {
+    ptx::setmaxnreg_dec<48>();
+    if (warp == 0) {
+      // ---------------------------------------------------------------- TMA producer
+      if (lane == 0) {
+        int stage = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        const uint64_t pol_first = ptx::l2_policy_evict_first(), pol_last = ptx::l2_policy_evict_last();
+        for (int t = first; ok && t < total_tiles; t += step) {
+          const BlkTile tile = blk_decode<kGated, kMaxN>(t, prefix, offs, p);
+          const int w_row = tile.group * p.N + tile.n0;
+          // the second box: the up rows of the same columns, or the next 128 columns where there are any
+          const bool second = kGated || tile.n0 + BW < p.N;
+          const uint32_t bytes = (second ? 2 : 1) * kWBoxBytes + tile.n_pad * BK;
+          const uint64_t pol_w = tile.single ? pol_first : pol_last;   // weights another tile reads again stay in L2
+          for (int kb = kb0; kb < kb1; ++kb) {
+            if (!ptx::mbar_wait(ptx::smem_u32(&st->empty[stage]), phase ^ 1u, abort_flag)) {
+              blk_timeout(p, 1);
+              ok = false;
+              break;
+            }
+            const uint32_t full = ptx::smem_u32(&st->full[stage]);
+            const uint32_t s = ring_u32 + stage * kStageBytes;
+            ptx::mbar_expect_tx(full, bytes);
+            ptx::tma_load_2d_hint(s, &tm_b0, full, kb * BK, w_row, pol_w);
+            if (second)
+              ptx::tma_load_2d_hint(s + kWBoxBytes, kGated ? &tm_b1 : &tm_b0, full, kb * BK, kGated ? w_row : w_row + BW,
+                                    pol_w);
+            for (int r = 0; r < tile.n_pad; r += kRowBox)
+              ptx::tma_load_2d_hint(s + 2 * kWBoxBytes + r * BK, &tm_a, full, kb * BK, tile.row0 + r, pol_last);
+            if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+          }
+        }
+      }
+      __syncwarp();
+    } else if (warp == 1) {
+      // ---------------------------------------------------------------- MMA issuer
+      if (lane == 0) {
+        int stage = 0, buf = 0;
+        uint32_t phase = 0, buf_phase = 0;
+        bool ok = true;
+        for (int t = first; ok && t < total_tiles; t += step) {
+          const uint32_t idesc = ptx::idesc_e4m3_f32(BW, blk_decode<kGated, kMaxN>(t, prefix, offs, p).n_pad);
+          for (int kb = kb0; kb < kb1; ++kb) {
+            if (!ptx::mbar_wait(ptx::smem_u32(&st->full[stage]), phase, abort_flag) ||
+                !ptx::mbar_wait(ptx::smem_u32(&st->acc_empty[buf]), buf_phase ^ 1u, abort_flag)) {
+              blk_timeout(p, 2);
+              ok = false;
+              break;
+            }
+            ptx::tc_fence_after_sync();
+            const uint32_t s = ring_u32 + stage * kStageBytes;
+            const uint64_t w0 = ptx::smem_desc_sw128(s), w1 = ptx::smem_desc_sw128(s + kWBoxBytes);
+            const uint64_t a = ptx::smem_desc_sw128(s + 2 * kWBoxBytes);
+            const uint32_t d = tmem_base + static_cast<uint32_t>(buf * kTmemBuf);
+#pragma unroll
+            for (int k4 = 0; k4 < BK / UMMA_K; ++k4) {
+              const uint64_t adv = static_cast<uint64_t>(2 * k4);      // +32 bytes along K inside the swizzle row
+              ptx::tc_mma_e4m3(d, w0 + adv, a + adv, idesc, k4 != 0 ? 1u : 0u);
+              ptx::tc_mma_e4m3(d + BW, w1 + adv, a + adv, idesc, k4 != 0 ? 1u : 0u);
+            }
+            ptx::tc_commit(ptx::smem_u32(&st->empty[stage]));
+            ptx::tc_commit(ptx::smem_u32(&st->acc_full[buf]));
+            if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+            if (++buf == 2) { buf = 0; buf_phase ^= 1u; }
+          }
+        }
+      }
+      __syncwarp();
+    } else {
+      // ---------------------------------------------------------------- scale loaders
+      constexpr int kPer = (kMaxN + kScaleThreads - 1) / kScaleThreads;   // rows of a per thread
+      constexpr int kBatch = 4;                                          // blocks whose loads are in flight together
+      const int idx = tid - 64;
+      int slot = 0;
+      uint32_t slot_phase = 0;
+      bool ok = true;
+      for (int t = first; ok && t < total_tiles; t += step) {
+        const BlkTile tile = blk_decode<kGated, kMaxN>(t, prefix, offs, p);
+        const int nb = tile.n0 / BW;
+        const size_t w_at = (static_cast<size_t>(tile.group) * p.n_blocks + nb) * p.k_blocks;
+        const float* sb0 = p.sb0 + w_at;
+        const float* sb1 = kGated ? p.sb1 + w_at : nb + 1 < p.n_blocks ? sb0 + p.k_blocks : nullptr;
+        for (int kb = kb0; ok && kb < kb1; kb += kBatch) {
+          float va[kBatch][kPer], vb0[kBatch], vb1[kBatch];
+#pragma unroll
+          for (int u = 0; u < kBatch; ++u) {
+            const bool in = kb + u < kb1;
+            vb0[u] = in ? __ldg(sb0 + kb + u) : 0.f;
+            vb1[u] = in && sb1 ? __ldg(sb1 + kb + u) : 0.f;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+              const int r = idx + i * kScaleThreads;
+              va[u][i] = in && r < tile.rows ? __ldg(p.sa + static_cast<size_t>(kb + u) * p.rows + tile.row0 + r) : 0.f;
+            }
+          }
+#pragma unroll
+          for (int u = 0; u < kBatch; ++u) {
+            if (kb + u >= kb1) break;
+            if (!__all_sync(0xFFFFFFFFu, ptx::mbar_wait(ptx::smem_u32(&st->sc_empty[slot]), slot_phase ^ 1u, abort_flag))) {
+              if (lane == 0) blk_timeout(p, 3);
+              ok = false;
+              break;
+            }
+            float* f = s_scale + slot * 2 * kMaxN;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+              const int r = idx + i * kScaleThreads;
+              if (r < kMaxN) {
+                f[r] = va[u][i] * vb0[u];
+                f[kMaxN + r] = va[u][i] * vb1[u];
+              }
+            }
+            ptx::mbar_arrive(ptx::smem_u32(&st->sc_full[slot]));
+            if (++slot == kScaleSlots) { slot = 0; slot_phase ^= 1u; }
+          }
+        }
+      }
+    }
+    if (p.split > 1) {
+      __syncwarp();
+      ptx::cluster_sync();
+      ptx::cluster_sync();
+    }
+  } else {
+    // ------------------------------------------------------------------ epilogue
+    ptx::setmaxnreg_inc<224>();
+    const int quarter = warp & 3;                 // TMEM lane quarter this warp may read: weight rows 32 quarter ..
+    const int half = (warp - 4) >> 2;             // half of the tile's rows of a
+    int buf = 0, slot = 0;
+    uint32_t buf_phase = 0, slot_phase = 0, out_phase = 0;
+    bool ok = true;
+    BlkTile tile{};
+    // one verdict for the warp: lanes that gave up must not part from lanes that did not
+    auto all_wait = [&](uint32_t bar, uint32_t parity) -> bool {
+      return __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar, parity, abort_flag));
+    };
+    // the four warps of a half meet (a bounded wait: a plain barrier would hang on a warp that gave up)
+    auto meet = [&]() -> bool {
+      const uint32_t bar = ptx::smem_u32(&st->out_sync[half]);
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(bar);
+      if (!all_wait(bar, out_phase)) {
+        if (lane == 0) blk_timeout(p, 5);
+        ok = false;
+      }
+      out_phase ^= 1u;
+      return ok;
+    };
+    // the running sums of one tile, then the tile's end
+    auto run = [&](auto tag) {
+      constexpr int kCols = decltype(tag)::value;          // rows of a this thread sums: half of n_pad
+      uint64_t acc[2][kCols / 2];
+#pragma unroll
+      for (int i = 0; i < kCols / 2; ++i) acc[0][i] = acc[1][i] = 0ull;
+      const uint32_t t_lane = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(half * kCols);
+      for (int kb = kb0; kb < kb1; ++kb) {
+        if (!all_wait(ptx::smem_u32(&st->sc_full[slot]), slot_phase) ||
+            !all_wait(ptx::smem_u32(&st->acc_full[buf]), buf_phase)) {
+          if (lane == 0) blk_timeout(p, 4);
+          ok = false;
+          return;
+        }
+        ptx::tc_fence_after_sync();
+        const uint32_t ta = t_lane + static_cast<uint32_t>(buf * kTmemBuf);
+        const float* f = s_scale + slot * 2 * kMaxN + half * kCols;
+        constexpr int kChunk = kCols < 32 ? kCols : kCols == 48 ? 16 : 32;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int c = 0; c < kCols; c += kChunk)
+            blk_add_cols<kChunk>(ta + b * BW + c, f + b * kMaxN + c, &acc[b][c / 2]);
+        ptx::tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) {
+          ptx::mbar_arrive(ptx::smem_u32(&st->acc_empty[buf]));
+          ptx::mbar_arrive(ptx::smem_u32(&st->sc_empty[slot]));
+        }
+        if (++buf == 2) { buf = 0; buf_phase ^= 1u; }
+        if (++slot == kScaleSlots) { slot = 0; slot_phase ^= 1u; }
+      }
+      if (p.split > 1) {
+        // the ring is idle (the last block's MMAs are done): it takes this CTA's sums, [row][256 weight rows]
+        float* part = reinterpret_cast<float*>(base);
+#pragma unroll
+        for (int i = 0; i < kCols / 2; ++i)
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            float lo, hi;
+            ptx::unpack_f32x2(acc[b][i], lo, hi);
+            float* dst = part + (half * kCols + 2 * i) * 256 + b * BW + quarter * 32 + lane;
+            dst[0] = lo;
+            dst[256] = hi;
+          }
+        return;
+      }
+      // kOutTokens rows at a time through shared memory: weight rows become neighbouring columns of an output row
+      float* mine = s_out + half * kOutTokens * 256;
+#pragma unroll
+      for (int c = 0; c < kCols; c += kOutTokens) {
+        if (half * kCols + c >= tile.rows) break;            // (the same for the four warps of a half)
+#pragma unroll
+        for (int i = 0; i < kOutTokens; i += 2)
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            float lo, hi;
+            ptx::unpack_f32x2(acc[b][(c + i) / 2], lo, hi);
+            float* dst = mine + i * 256 + b * BW + quarter * 32 + lane;
+            dst[0] = lo;
+            dst[256] = hi;
+          }
+        if (!meet()) return;
+#pragma unroll
+        for (int i = 0; i < kOutTokens / 4; ++i) {
+          const int j = quarter * (kOutTokens / 4) + i, r = half * kCols + c + j;
+          if (r < tile.rows) {
+            const float4 a = *reinterpret_cast<const float4*>(mine + j * 256 + 4 * lane);
+            const float4 b = *reinterpret_cast<const float4*>(mine + j * 256 + BW + 4 * lane);
+            blk_finish_row<kGated>(p, tile.row0 + r, tile.n0, lane, a, b);
+          }
+        }
+        if (!meet()) return;
+      }
+    };
+    for (int t = first; ok && t < total_tiles; t += step) {
+      tile = blk_decode<kGated, kMaxN>(t, prefix, offs, p);
+      switch (tile.n_pad) {
+        case 16: run(std::integral_constant<int, 8>{}); break;
+        case 32: run(std::integral_constant<int, 16>{}); break;
+        case 64: if constexpr (kMaxN >= 64) run(std::integral_constant<int, 32>{}); break;
+        case 96: if constexpr (kMaxN >= 96) run(std::integral_constant<int, 48>{}); break;
+        default: if constexpr (kMaxN >= 128) run(std::integral_constant<int, 64>{}); break;
+      }
+      if (p.split > 1) break;                              // one tile per cluster
+    }
+    if (p.split > 1) {
+      __syncwarp();
+      ptx::cluster_sync();
+      if (ok && first < total_tiles) {
+        // each CTA finishes every split-th row, its eight epilogue warps in turn; partial sums in rank order
+        for (int r = rank + p.split * (warp - 4); r < tile.rows; r += p.split * (kEpilogueThreads / 32)) {
+          float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+          for (int c = 0; c < p.split; ++c) {
+            const uint32_t at = ptx::map_to_cta(ring_u32 + static_cast<uint32_t>(r * 256 + 4 * lane) * 4, c);
+            const float4 va = ptx::ld_cluster_f4(at), vb = ptx::ld_cluster_f4(at + BW * 4);
+            a.x += va.x; a.y += va.y; a.z += va.z; a.w += va.w;
+            b.x += vb.x; b.y += vb.y; b.z += vb.z; b.w += vb.w;
+          }
+          blk_finish_row<kGated>(p, tile.row0 + r, tile.n0, lane, a, b);
+        }
+      }
+      __syncwarp();
+      ptx::cluster_sync();
+    }
+  }
+
+  __syncthreads();
+  if (st->abort_flag) {
+    // a wait gave up: give copies still in flight time to land before the shared memory is released
+    for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+    __syncthreads();
+  }
+  if (warp == 1) {
+    ptx::tc_fence_after_sync();
+    ptx::tmem_dealloc(tmem_base, kTmemCols);
+  }
+}
+
+// Tensor map over a row-major [rows, cols] matrix of E4M3 bytes: boxes of box_rows x 128 bytes, 128-byte swizzle; what
+// lies outside reads as zero.
+CUresult encode_bytes(moe_ctx* ctx, CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows) {
+  const cuuint64_t dims[2] = {cols, rows};
+  const cuuint64_t strides[1] = {cols};
+  const cuuint32_t box[2] = {static_cast<cuuint32_t>(BK), box_rows};
+  const cuuint32_t elem[2] = {1u, 1u};
+  return ctx->encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, elem,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+
+struct BlkProduct {       // one GEMM: operands and shape
+  const void *a, *b0, *b1;
+  int K;
+};
+
+template <bool kGated, int kMaxN>
+moe_status launch_swapped(moe_ctx* ctx, const BlkProduct& g, BlkParams p, cudaStream_t stream) {
+  const uint64_t w_rows = static_cast<uint64_t>(p.groups) * p.N;
+  CUtensorMap tm_a, tm_b0, tm_b1;
+  if (encode_bytes(ctx, &tm_a, g.a, p.rows, g.K, kRowBox) != CUDA_SUCCESS ||
+      encode_bytes(ctx, &tm_b0, g.b0, w_rows, g.K, BW) != CUDA_SUCCESS ||
+      encode_bytes(ctx, &tm_b1, kGated ? g.b1 : g.b0, w_rows, g.K, BW) != CUDA_SUCCESS)
+    return MOE_ERR_CUDA;
+  constexpr size_t kStageBytes = 2 * kWBoxBytes + kMaxN * BK;
+  const size_t rest = 1024 + 2 * kOutTokens * 256 * 4 + kScaleSlots * 2 * kMaxN * 4 + sizeof(BlkTail) +
+                      (3 * static_cast<size_t>(p.groups) + 1) * 4 + 16;
+  int stages = static_cast<int>((kMaxSmem - rest) / kStageBytes);
+  if (stages > kMaxStages) stages = kMaxStages;
+  p.stages = stages;
+  const size_t smem = rest + stages * kStageBytes;
+  // the most tiles the rows can make; the kernel counts the real ones from the offsets
+  const long long blocks = p.rows / kMaxN + (p.groups < p.rows ? p.groups : p.rows);
+  const long long tiles = blocks * p.n_tiles;
+  p.split = 1;
+  while (p.split < 8 && 2 * p.split * tiles <= ctx->num_sms && 2 * p.split <= p.k_blocks) p.split *= 2;
+  const long long grid = tiles * p.split < ctx->num_sms ? tiles * p.split : ctx->num_sms;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(static_cast<unsigned>(grid));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = p.split;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = p.split > 1 ? 1 : 0;
+  ctx->last_launches += 1;
+  return cudaLaunchKernelEx(&cfg, gemm_blk_swapped<kGated, kMaxN>, tm_a, tm_b0, tm_b1, p) == cudaSuccess ? MOE_OK
+                                                                                                     : MOE_ERR_CUDA;
 }
 
 template <bool kGated>
-__global__ void __launch_bounds__(kCols)
-gemm_blk_kernel(const BlkParams p) {
-  __shared__ float s_a[kRows][128];
-  __shared__ float s_sa[kRows];
-  __shared__ float s_part[kCols / 32];
-  __shared__ long long s_row0, s_end;
-  __shared__ int s_group;
-  const int tid = threadIdx.x;
-  if (tid == 0) {
-    s_group = -1;
-    long long tile = blockIdx.y;
-    for (int g = 0; g < p.groups; ++g) {
-      long long lo = p.offsets ? p.offsets[g] : 0, hi = p.offsets ? p.offsets[g + 1] : p.rows;
-      lo = lo < 0 ? 0 : lo;
-      hi = hi > p.rows ? p.rows : hi;
-      const long long n = hi > lo ? (hi - lo + kRows - 1) / kRows : 0;
-      if (tile < n) {
-        s_group = g;
-        s_row0 = lo + tile * kRows;
-        s_end = hi;
-        break;
-      }
-      tile -= n;
-    }
-  }
-  __syncthreads();
-  if (s_group < 0) return;
-  const int g = s_group, n = blockIdx.x * kCols + tid;
-  const long long row0 = s_row0;
-  const int live = static_cast<int>(min(static_cast<long long>(kRows), s_end - row0));
-  const int kb_count = (p.K + 127) / 128, nb_count = (p.N + 127) / 128;
-  const bool col_ok = n < p.N;
-  float acc0[kRows], acc1[kRows];
-#pragma unroll
-  for (int r = 0; r < kRows; ++r) acc0[r] = acc1[r] = 0.f;
-  for (int kb = 0; kb < kb_count; ++kb) {
-    const int kn = min(128, p.K - kb * 128);
-    __syncthreads();
-    for (int r = 0; r < kRows; ++r)
-      s_a[r][tid] = (r < live && tid < kn) ? fp8_value(p.a[(row0 + r) * p.K + kb * 128 + tid]) : 0.f;
-    if (tid < kRows) s_sa[tid] = tid < live ? p.sa[static_cast<size_t>(kb) * p.rows + row0 + tid] : 0.f;
-    __syncthreads();
-    if (!col_ok) continue;
-    const size_t w_at = (static_cast<size_t>(g) * p.N + n) * p.K + kb * 128;
-    const size_t s_at = (static_cast<size_t>(g) * nb_count + blockIdx.x) * kb_count + kb;
-    float part0[kRows], part1[kRows];
-#pragma unroll
-    for (int r = 0; r < kRows; ++r) part0[r] = part1[r] = 0.f;
-    for (int c = 0; c < kn; ++c) {
-      const float w0 = fp8_value(p.b0[w_at + c]);
-      const float w1 = kGated ? fp8_value(p.b1[w_at + c]) : 0.f;
-#pragma unroll
-      for (int r = 0; r < kRows; ++r) {
-        part0[r] = fmaf(s_a[r][c], w0, part0[r]);
-        if (kGated) part1[r] = fmaf(s_a[r][c], w1, part1[r]);
-      }
-    }
-    const float sb0 = p.sb0[s_at], sb1 = kGated ? p.sb1[s_at] : 0.f;
-#pragma unroll
-    for (int r = 0; r < kRows; ++r) {
-      acc0[r] = fmaf(part0[r], s_sa[r] * sb0, acc0[r]);
-      if (kGated) acc1[r] = fmaf(part1[r], s_sa[r] * sb1, acc1[r]);
-    }
-  }
-  if constexpr (!kGated) {
-    if (col_ok)
-      for (int r = 0; r < live; ++r) p.y[(row0 + r) * p.N + n] = __float2bfloat16_rn(acc0[r]);
-  } else {
-    for (int r = 0; r < live; ++r) {
-      const float h = acc0[r] / (1.f + expf(-acc0[r])) * acc1[r];
-      float amax = fabsf(h);
-#pragma unroll
-      for (int off = 16; off > 0; off >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, off));
-      if ((tid & 31) == 0) s_part[tid >> 5] = amax;
-      __syncthreads();
-      amax = fmaxf(fmaxf(s_part[0], s_part[1]), fmaxf(s_part[2], s_part[3]));
-      __syncthreads();
-      const float sc = blk::scale_of(amax);
-      p.hq[(row0 + r) * p.N + n] =
-          static_cast<unsigned char>(__nv_cvt_float_to_fp8(__fdiv_rn(h, sc), __NV_SATFINITE, __NV_E4M3));
-      if (tid == 0) p.sh[static_cast<size_t>(blockIdx.x) * p.rows + row0 + r] = sc;
-      if (p.h_dbg) p.h_dbg[(row0 + r) * p.N + n] = h;
-    }
-  }
-}
-
-dim3 grid_of(const BlkParams& p) {
-  return dim3((p.N + kCols - 1) / kCols, static_cast<unsigned>(p.rows / kRows + p.groups));
+moe_status launch_product(moe_ctx* ctx, const BlkProduct& g, const BlkParams& p, cudaStream_t stream) {
+  // short stages (more of them) where the groups average few rows
+  if (p.rows <= 16LL * p.groups) return launch_swapped<kGated, 32>(ctx, g, p, stream);
+  return launch_swapped<kGated, 128>(ctx, g, p, stream);
 }
 
 }  // namespace
 
 namespace moe {
 
+cudaError_t prepare_gemm_blk(moe_ctx* ctx) {
+  (void)ctx;
+  const void* kernels[] = {reinterpret_cast<const void*>(gemm_blk_swapped<true, 32>),
+                           reinterpret_cast<const void*>(gemm_blk_swapped<false, 32>),
+                           reinterpret_cast<const void*>(gemm_blk_swapped<true, 128>),
+                           reinterpret_cast<const void*>(gemm_blk_swapped<false, 128>)};
+  for (const void* k : kernels) {
+    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
 moe_status launch_gemm_blk(moe_ctx* ctx, const moe_gemm_blk_args* a, cudaStream_t stream) {
   BlkParams p{};
-  p.a = static_cast<const unsigned char*>(a->a);
-  p.sa = a->sa;
   p.offsets = a->offsets;
-  p.b0 = static_cast<const unsigned char*>(a->b);
+  p.groups = a->groups;
+  p.N = a->N;
+  p.n_tiles = (a->N + 2 * BW - 1) / (2 * BW);
+  p.k_blocks = (a->K + BK - 1) / BK;
+  p.n_blocks = (a->N + BW - 1) / BW;
+  p.rows = static_cast<int>(a->rows);
+  p.sa = a->sa;
   p.sb0 = a->sb;
   p.y = static_cast<__nv_bfloat16*>(a->y);
-  p.rows = a->rows;
-  p.N = a->N;
-  p.K = a->K;
-  p.groups = a->groups;
-  gemm_blk_kernel<false><<<grid_of(p), kCols, 0, stream>>>(p);
-  ctx->last_launches += 1;
-  return cudaGetLastError() == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+  p.status = ctx->d_status;
+  return launch_product<false>(ctx, BlkProduct{a->a, a->b, a->b, a->K}, p, stream);
 }
 
 moe_status launch_expert_ffn_blk(moe_ctx* ctx, const moe_blk_ffn_args* a, cudaStream_t stream) {
   const moe_shape& s = ctx->shape;
   BlkParams p{};
-  p.a = static_cast<const unsigned char*>(a->xq_perm);
-  p.sa = a->sx_perm;
   p.offsets = a->offsets;
-  p.b0 = static_cast<const unsigned char*>(a->wq_gate);
-  p.b1 = static_cast<const unsigned char*>(a->wq_up);
-  p.sb0 = a->s_gate;
-  p.sb1 = a->s_up;
-  p.hq = static_cast<unsigned char*>(a->hq_ws);
-  p.sh = a->sh_ws;
-  p.h_dbg = a->h_fp32_debug;
-  p.rows = static_cast<long long>(s.T) * s.k;
-  p.N = s.F;
-  p.K = s.H;
   p.groups = s.E;
-  gemm_blk_kernel<true><<<grid_of(p), kCols, 0, stream>>>(p);
+  p.rows = static_cast<int>(static_cast<long long>(s.T) * s.k);
+  p.status = ctx->d_status;
+  BlkParams p1 = p;
+  p1.N = s.F;
+  p1.n_tiles = p1.n_blocks = s.F / BW;
+  p1.k_blocks = s.H / BK;
+  p1.sa = a->sx_perm;
+  p1.sb0 = a->s_gate;
+  p1.sb1 = a->s_up;
+  p1.hq = static_cast<uint32_t*>(a->hq_ws);
+  p1.sh = a->sh_ws;
+  p1.h_dbg = a->h_fp32_debug;
+  moe_status st = launch_product<true>(ctx, BlkProduct{a->xq_perm, a->wq_gate, a->wq_up, s.H}, p1, stream);
+  if (st != MOE_OK) return st;
   moe_mark(ctx, 5, stream);
-  p.a = static_cast<const unsigned char*>(a->hq_ws);
-  p.sa = a->sh_ws;
-  p.b0 = static_cast<const unsigned char*>(a->wq_down);
-  p.sb0 = a->s_down;
-  p.y = static_cast<__nv_bfloat16*>(a->y_perm);
-  p.N = s.H;
-  p.K = s.F;
-  gemm_blk_kernel<false><<<grid_of(p), kCols, 0, stream>>>(p);
+  BlkParams p2 = p;
+  p2.N = s.H;
+  p2.n_tiles = (s.H + 2 * BW - 1) / (2 * BW);
+  p2.n_blocks = s.H / BW;
+  p2.k_blocks = s.F / BK;
+  p2.sa = a->sh_ws;
+  p2.sb0 = a->s_down;
+  p2.y = static_cast<__nv_bfloat16*>(a->y_perm);
+  st = launch_product<false>(ctx, BlkProduct{a->hq_ws, a->wq_down, a->wq_down, s.F}, p2, stream);
+  if (st != MOE_OK) return st;
   moe_mark(ctx, 6, stream);
-  ctx->last_launches += 2;
-  return cudaGetLastError() == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+  return MOE_OK;
 }
 
 }  // namespace moe

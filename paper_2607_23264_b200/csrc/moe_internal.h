@@ -167,6 +167,7 @@ cudaError_t launch_quantize_rows_blk(moe_ctx* ctx, const void* in_bf16, long lon
                                      float* scales, cudaStream_t stream);
 cudaError_t launch_quantize_weights_blk(moe_ctx* ctx, const void* in_bf16, long long mats, int rows, int cols,
                                         void* codes, float* scales, cudaStream_t stream);
+cudaError_t prepare_gemm_blk(moe_ctx* ctx);   // one-time kernel attributes
 moe_status launch_gemm_blk(moe_ctx* ctx, const moe_gemm_blk_args* args, cudaStream_t stream);
 moe_status launch_expert_ffn_blk(moe_ctx* ctx, const moe_blk_ffn_args* args, cudaStream_t stream);
 
