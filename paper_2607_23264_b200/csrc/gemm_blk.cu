@@ -34,7 +34,8 @@ constexpr int UMMA_K = 32;
 constexpr int kWBoxBytes = BW * BK;
 constexpr int kRowBox = 16;              // rows of a per TMA box
 constexpr int kMaxStages = 6;
-constexpr int kScaleSlots = 4;
+constexpr int kScaleSlots = 2;           // scale ring: slots of kScaleBatch blocks of K each
+constexpr int kScaleBatch = 4;
 constexpr int kScaleThreads = 64;
 constexpr int kTmemCols = 512;           // two buffers x two weight boxes x 128 columns
 constexpr int kTmemBuf = 256;
@@ -112,24 +113,26 @@ __device__ __forceinline__ BlkTile blk_decode(int t, const int32_t* prefix, cons
   return tile;
 }
 
+// silu(g) * u with an exponential and a division good to a few ulp: h is quantised from here, and the error of the hardware
+// tanh (2^-11) would move one code in a hundred.
+__device__ __forceinline__ float blk_silu_mul(float g, float u) { return __fdividef(g, 1.0f + __expf(-g)) * u; }
+
 // One row of the output from its running sums: lane l holds columns n0 + 4 l .. + 3 of each weight box.
 template <bool kGated>
 __device__ __forceinline__ void blk_finish_row(const BlkParams& p, int row, int n0, int lane, const float4& a,
                                                const float4& b) {
   if constexpr (kGated) {
-    // silu(g) * u with an exponential and a division good to 2 ulp each: h is quantised from here, and an error of
-    // 2^-11 (a hardware tanh) would move one code in a hundred
     const float g[4] = {a.x, a.y, a.z, a.w}, u[4] = {b.x, b.y, b.z, b.w};
     float h[4], amax = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      h[i] = __fdividef(g[i], 1.0f + __expf(-g[i])) * u[i];
+      h[i] = blk_silu_mul(g[i], u[i]);
       amax = fmaxf(amax, fabsf(h[i]));
     }
     amax = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(amax)));
     const float sc = blk::scale_of(amax);
     const size_t at = static_cast<size_t>(row) * p.N + n0 + 4 * lane;
-    p.hq[at >> 2] = blk::pack4(h[0], h[1], h[2], h[3], sc);
+    p.hq[at >> 2] = blk::pack4(h[0], h[1], h[2], h[3], blk::Divider(sc));
     if (lane == 0) p.sh[static_cast<size_t>(n0 / BW) * p.rows + row] = sc;
     if (p.h_dbg != nullptr) *reinterpret_cast<float4*>(p.h_dbg + at) = make_float4(h[0], h[1], h[2], h[3]);
   } else {
@@ -140,24 +143,104 @@ __device__ __forceinline__ void blk_finish_row(const BlkParams& p, int row, int 
   }
 }
 
+// One warp: row blocks (of `most` rows) before each group, and each group's first row and end.  Offsets are clamped:
+// whatever they hold, no row outside [0, rows) is touched.
+__device__ __forceinline__ void blk_prefixes(const BlkParams& p, int most, int32_t* prefix, int32_t* offs, int lane) {
+  int32_t run = 0;
+  for (int b0 = 0; b0 < p.groups; b0 += 32) {
+    const int e = b0 + lane;
+    int32_t v = 0;
+    if (e < p.groups) {
+      int32_t lo = p.offsets ? p.offsets[e] : 0, hi = p.offsets ? p.offsets[e + 1] : p.rows;
+      lo = min(max(lo, 0), p.rows);
+      hi = min(max(hi, lo), p.rows);
+      offs[2 * e] = lo;
+      offs[2 * e + 1] = hi;
+      v = (hi - lo + most - 1) / most;
+    }
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int32_t o = __shfl_up_sync(0xFFFFFFFFu, v, off);
+      if (lane >= off) v += o;
+    }
+    if (e < p.groups) prefix[e + 1] = run + v;
+    run += __shfl_sync(0xFFFFFFFFu, v, 31);
+  }
+}
+
+struct ScaleRows {
+  int row0, rows, n0, group;
+};
+
+// The scale loaders' whole run: for kScaleBatch blocks of K at a time, row r of the tile gets sa * sb of each weight box in
+// the next slot of the ring.  A slot's loads are in flight together and the ring lets the loaders run ahead of the
+// epilogue, across tiles too; the epilogue waits for scales once per slot.
+template <bool kGated, int kMaxN, typename Decode>
+__device__ __forceinline__ void blk_load_scales(const BlkParams& p, int first, int step, int total_tiles, int kb0, int kb1,
+                                                int idx, float* s_scale, uint64_t* sc_full, uint64_t* sc_empty,
+                                                volatile int* abort_flag, Decode decode) {
+  constexpr int kPer = (kMaxN + kScaleThreads - 1) / kScaleThreads;   // rows per thread
+  int slot = 0;
+  uint32_t slot_phase = 0;
+  for (int t = first; t < total_tiles; t += step) {
+    const ScaleRows tile = decode(t);
+    const int nb = tile.n0 / BW;
+    const size_t w_at = (static_cast<size_t>(tile.group) * p.n_blocks + nb) * p.k_blocks;
+    const float* sb0 = p.sb0 + w_at;
+    const float* sb1 = kGated ? p.sb1 + w_at : nb + 1 < p.n_blocks ? sb0 + p.k_blocks : nullptr;
+    for (int kb = kb0; kb < kb1; kb += kScaleBatch) {
+      float va[kScaleBatch][kPer], vb0[kScaleBatch], vb1[kScaleBatch];
+#pragma unroll
+      for (int u = 0; u < kScaleBatch; ++u) {
+        const bool in = kb + u < kb1;
+        vb0[u] = in ? __ldg(sb0 + kb + u) : 0.f;
+        vb1[u] = in && sb1 ? __ldg(sb1 + kb + u) : 0.f;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          const int r = idx + i * kScaleThreads;
+          va[u][i] = in && r < tile.rows ? __ldg(p.sa + static_cast<size_t>(kb + u) * p.rows + tile.row0 + r) : 0.f;
+        }
+      }
+      if (!__all_sync(0xFFFFFFFFu, ptx::mbar_wait(ptx::smem_u32(&sc_empty[slot]), slot_phase ^ 1u, abort_flag))) {
+        if ((idx & 31) == 0) blk_timeout(p, 3);
+        return;
+      }
+      float* f = s_scale + slot * kScaleBatch * 2 * kMaxN;
+#pragma unroll
+      for (int u = 0; u < kScaleBatch; ++u)
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          const int r = idx + i * kScaleThreads;
+          if (r < kMaxN) {
+            f[u * 2 * kMaxN + r] = va[u][i] * vb0[u];
+            f[u * 2 * kMaxN + kMaxN + r] = va[u][i] * vb1[u];
+          }
+        }
+      ptx::mbar_arrive(ptx::smem_u32(&sc_full[slot]));
+      if (++slot == kScaleSlots) { slot = 0; slot_phase ^= 1u; }
+    }
+  }
+}
+
 template <int kCols>
 __device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[kCols]) {
   if constexpr (kCols == 8) ptx::tmem_ld_32x8(taddr, r);
-  else if constexpr (kCols == 16) ptx::tmem_ld_32x16(taddr, r);
-  else ptx::tmem_ld_32x32(taddr, r);
+  else ptx::tmem_ld_32x16(taddr, r);
 }
 
 // acc[0 .. kCols) += P * f for kCols columns of tensor memory; f are the columns' scales in shared memory.
 template <int kCols>
-__device__ __forceinline__ void blk_add_cols(uint32_t taddr, const float* f, uint64_t* acc) {
+__device__ __forceinline__ void blk_add_cols(uint32_t taddr, const float* f, float* acc) {
   uint32_t v[kCols];
   tmem_ld_cols<kCols>(taddr, v);
   ptx::tmem_ld_wait();
 #pragma unroll
   for (int i = 0; i < kCols; i += 4) {
-    const ulonglong2 s = *reinterpret_cast<const ulonglong2*>(f + i);
-    acc[i / 2] = ptx::fma_f32x2(ptx::pack_f32x2(v[i], v[i + 1]), s.x, acc[i / 2]);
-    acc[i / 2 + 1] = ptx::fma_f32x2(ptx::pack_f32x2(v[i + 2], v[i + 3]), s.y, acc[i / 2 + 1]);
+    const float4 s = *reinterpret_cast<const float4*>(f + i);
+    acc[i] = fmaf(__uint_as_float(v[i]), s.x, acc[i]);
+    acc[i + 1] = fmaf(__uint_as_float(v[i + 1]), s.y, acc[i + 1]);
+    acc[i + 2] = fmaf(__uint_as_float(v[i + 2]), s.z, acc[i + 2]);
+    acc[i + 3] = fmaf(__uint_as_float(v[i + 3]), s.w, acc[i + 3]);
   }
 }
 
@@ -172,8 +255,8 @@ gemm_blk_swapped(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
   unsigned char* base = smem_raw + pad;                      // 1024-byte aligned: required by the swizzle
   const uint32_t ring_u32 = raw + pad;
   float* s_out = reinterpret_cast<float*>(base + p.stages * kStageBytes);      // [2][kOutTokens][256]
-  float* s_scale = s_out + 2 * kOutTokens * 256;                               // [kScaleSlots][2][kMaxN]
-  BlkTail* st = reinterpret_cast<BlkTail*>(s_scale + kScaleSlots * 2 * kMaxN);
+  float* s_scale = s_out + 2 * kOutTokens * 256;                               // [kScaleSlots][kScaleBatch][2][kMaxN]
+  BlkTail* st = reinterpret_cast<BlkTail*>(s_scale + kScaleSlots * kScaleBatch * 2 * kMaxN);
   int32_t* prefix = reinterpret_cast<int32_t*>(st + 1);                        // [groups + 1] row blocks before a group
   int32_t* offs = prefix + p.groups + 1;                                       // [groups][2] first row, end
 
@@ -199,27 +282,7 @@ gemm_blk_swapped(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
     ptx::fence_proxy_async_smem();
   }
   if (warp == 0) {
-    int32_t run = 0;
-    for (int b0 = 0; b0 < p.groups; b0 += 32) {
-      const int e = b0 + lane;
-      int32_t v = 0;
-      if (e < p.groups) {
-        // clamped: whatever the offsets hold, no row outside [0, rows) is touched
-        int32_t lo = p.offsets ? p.offsets[e] : 0, hi = p.offsets ? p.offsets[e + 1] : p.rows;
-        lo = min(max(lo, 0), p.rows);
-        hi = min(max(hi, lo), p.rows);
-        offs[2 * e] = lo;
-        offs[2 * e + 1] = hi;
-        v = (hi - lo + kMaxN - 1) / kMaxN;
-      }
-#pragma unroll
-      for (int off = 1; off < 32; off <<= 1) {
-        const int32_t o = __shfl_up_sync(0xFFFFFFFFu, v, off);
-        if (lane >= off) v += o;
-      }
-      if (e < p.groups) prefix[e + 1] = run + v;
-      run += __shfl_sync(0xFFFFFFFFu, v, 31);
-    }
+    blk_prefixes(p, kMaxN, prefix, offs, lane);
     if (lane == 0) {
       ptx::prefetch_tensormap(&tm_a);
       ptx::prefetch_tensormap(&tm_b0);
@@ -315,53 +378,12 @@ gemm_blk_swapped(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
       __syncwarp();
     } else {
       // ---------------------------------------------------------------- scale loaders
-      constexpr int kPer = (kMaxN + kScaleThreads - 1) / kScaleThreads;   // rows of a per thread
-      constexpr int kBatch = 4;                                          // blocks whose loads are in flight together
-      const int idx = tid - 64;
-      int slot = 0;
-      uint32_t slot_phase = 0;
-      bool ok = true;
-      for (int t = first; ok && t < total_tiles; t += step) {
+      auto decode = [&](int t) {
         const BlkTile tile = blk_decode<kGated, kMaxN>(t, prefix, offs, p);
-        const int nb = tile.n0 / BW;
-        const size_t w_at = (static_cast<size_t>(tile.group) * p.n_blocks + nb) * p.k_blocks;
-        const float* sb0 = p.sb0 + w_at;
-        const float* sb1 = kGated ? p.sb1 + w_at : nb + 1 < p.n_blocks ? sb0 + p.k_blocks : nullptr;
-        for (int kb = kb0; ok && kb < kb1; kb += kBatch) {
-          float va[kBatch][kPer], vb0[kBatch], vb1[kBatch];
-#pragma unroll
-          for (int u = 0; u < kBatch; ++u) {
-            const bool in = kb + u < kb1;
-            vb0[u] = in ? __ldg(sb0 + kb + u) : 0.f;
-            vb1[u] = in && sb1 ? __ldg(sb1 + kb + u) : 0.f;
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-              const int r = idx + i * kScaleThreads;
-              va[u][i] = in && r < tile.rows ? __ldg(p.sa + static_cast<size_t>(kb + u) * p.rows + tile.row0 + r) : 0.f;
-            }
-          }
-#pragma unroll
-          for (int u = 0; u < kBatch; ++u) {
-            if (kb + u >= kb1) break;
-            if (!__all_sync(0xFFFFFFFFu, ptx::mbar_wait(ptx::smem_u32(&st->sc_empty[slot]), slot_phase ^ 1u, abort_flag))) {
-              if (lane == 0) blk_timeout(p, 3);
-              ok = false;
-              break;
-            }
-            float* f = s_scale + slot * 2 * kMaxN;
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-              const int r = idx + i * kScaleThreads;
-              if (r < kMaxN) {
-                f[r] = va[u][i] * vb0[u];
-                f[kMaxN + r] = va[u][i] * vb1[u];
-              }
-            }
-            ptx::mbar_arrive(ptx::smem_u32(&st->sc_full[slot]));
-            if (++slot == kScaleSlots) { slot = 0; slot_phase ^= 1u; }
-          }
-        }
-      }
+        return ScaleRows{tile.row0, tile.rows, tile.n0, tile.group};
+      };
+      blk_load_scales<kGated, kMaxN>(p, first, step, total_tiles, kb0, kb1, tid - 64, s_scale, st->sc_full, st->sc_empty,
+                                     abort_flag, decode);
     }
     if (p.split > 1) {
       __syncwarp();
@@ -396,48 +418,47 @@ gemm_blk_swapped(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
     // the running sums of one tile, then the tile's end
     auto run = [&](auto tag) {
       constexpr int kCols = decltype(tag)::value;          // rows of a this thread sums: half of n_pad
-      uint64_t acc[2][kCols / 2];
+      float acc[2][kCols];
 #pragma unroll
-      for (int i = 0; i < kCols / 2; ++i) acc[0][i] = acc[1][i] = 0ull;
+      for (int i = 0; i < kCols; ++i) acc[0][i] = acc[1][i] = 0.f;
       const uint32_t t_lane = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(half * kCols);
-      for (int kb = kb0; kb < kb1; ++kb) {
-        if (!all_wait(ptx::smem_u32(&st->sc_full[slot]), slot_phase) ||
-            !all_wait(ptx::smem_u32(&st->acc_full[buf]), buf_phase)) {
+      for (int kb = kb0; kb < kb1; kb += kScaleBatch) {
+        if (!all_wait(ptx::smem_u32(&st->sc_full[slot]), slot_phase)) {
           if (lane == 0) blk_timeout(p, 4);
           ok = false;
           return;
         }
-        ptx::tc_fence_after_sync();
-        const uint32_t ta = t_lane + static_cast<uint32_t>(buf * kTmemBuf);
-        const float* f = s_scale + slot * 2 * kMaxN + half * kCols;
-        constexpr int kChunk = kCols < 32 ? kCols : kCols == 48 ? 16 : 32;
+        const float* f = s_scale + slot * kScaleBatch * 2 * kMaxN + half * kCols;
+        const int batch = min(kScaleBatch, kb1 - kb);
+        for (int u = 0; u < batch; ++u, f += 2 * kMaxN) {
+          if (!all_wait(ptx::smem_u32(&st->acc_full[buf]), buf_phase)) {
+            if (lane == 0) blk_timeout(p, 4);
+            ok = false;
+            return;
+          }
+          ptx::tc_fence_after_sync();
+          const uint32_t ta = t_lane + static_cast<uint32_t>(buf * kTmemBuf);
+          constexpr int kChunk = kCols < 16 ? kCols : 16;
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+          for (int b = 0; b < 2; ++b)
 #pragma unroll
-          for (int c = 0; c < kCols; c += kChunk)
-            blk_add_cols<kChunk>(ta + b * BW + c, f + b * kMaxN + c, &acc[b][c / 2]);
-        ptx::tc_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) {
-          ptx::mbar_arrive(ptx::smem_u32(&st->acc_empty[buf]));
-          ptx::mbar_arrive(ptx::smem_u32(&st->sc_empty[slot]));
+            for (int c = 0; c < kCols; c += kChunk)
+              blk_add_cols<kChunk>(ta + b * BW + c, f + b * kMaxN + c, &acc[b][c]);
+          ptx::tc_fence_before_sync();
+          ptx::mbar_arrive_if(ptx::smem_u32(&st->acc_empty[buf]), lane == 0);
+          if (++buf == 2) { buf = 0; buf_phase ^= 1u; }
         }
-        if (++buf == 2) { buf = 0; buf_phase ^= 1u; }
+        __syncwarp();
+        ptx::mbar_arrive_if(ptx::smem_u32(&st->sc_empty[slot]), lane == 0);
         if (++slot == kScaleSlots) { slot = 0; slot_phase ^= 1u; }
       }
       if (p.split > 1) {
         // the ring is idle (the last block's MMAs are done): it takes this CTA's sums, [row][256 weight rows]
         float* part = reinterpret_cast<float*>(base);
 #pragma unroll
-        for (int i = 0; i < kCols / 2; ++i)
+        for (int i = 0; i < kCols; ++i)
 #pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            float lo, hi;
-            ptx::unpack_f32x2(acc[b][i], lo, hi);
-            float* dst = part + (half * kCols + 2 * i) * 256 + b * BW + quarter * 32 + lane;
-            dst[0] = lo;
-            dst[256] = hi;
-          }
+          for (int b = 0; b < 2; ++b) part[(half * kCols + i) * 256 + b * BW + quarter * 32 + lane] = acc[b][i];
         return;
       }
       // kOutTokens rows at a time through shared memory: weight rows become neighbouring columns of an output row
@@ -446,15 +467,9 @@ gemm_blk_swapped(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
       for (int c = 0; c < kCols; c += kOutTokens) {
         if (half * kCols + c >= tile.rows) break;            // (the same for the four warps of a half)
 #pragma unroll
-        for (int i = 0; i < kOutTokens; i += 2)
+        for (int i = 0; i < kOutTokens; ++i)
 #pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            float lo, hi;
-            ptx::unpack_f32x2(acc[b][(c + i) / 2], lo, hi);
-            float* dst = mine + i * 256 + b * BW + quarter * 32 + lane;
-            dst[0] = lo;
-            dst[256] = hi;
-          }
+          for (int b = 0; b < 2; ++b) mine[i * 256 + b * BW + quarter * 32 + lane] = acc[b][c + i];
         if (!meet()) return;
 #pragma unroll
         for (int i = 0; i < kOutTokens / 4; ++i) {
@@ -512,6 +527,328 @@ gemm_blk_swapped(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
   }
 }
 
+// ---------------------------------------------------------------------------------------------------------------
+// Many rows per group: CTA pairs (clusters of two, cta_group::2) on tiles of 256 rows of a x 256 accumulator columns.
+// Rows are the M side here, so a thread of the epilogue owns one row and the scales are one factor per weight box.
+// Each CTA stages its 128 rows and one of the two weight boxes (32 KB per block of K: 64 bytes per clock at the tensor
+// rate, what an SM takes in from L2, where a single CTA's 128 x 256 tile would need 96), the leader issues the MMAs of
+// both, and every CTA's eight epilogue warps keep 128 running sums per thread.  Tensor memory holds two blocks of K.
+// Handing a block back crosses the pair once per block and warp: those arrivals carry no cluster-wide release (it costs
+// about a thousand clocks), the loads from tensor memory have completed before them and there is nothing else to publish.
+constexpr int kPairRows = 256;
+constexpr int kPairRowBox = 32;          // rows of a per TMA box
+constexpr int kPairStages = 6;
+constexpr int kPairStageBytes = BW * BK + kWBoxBytes;
+
+struct PairTail {
+  uint64_t full[kPairStages];
+  uint64_t empty[kPairStages];
+  uint64_t acc_full[2];
+  uint64_t acc_empty[2];
+  uint64_t sc_full[kScaleSlots];
+  uint64_t sc_empty[kScaleSlots];
+  uint64_t row_sync[4];     // meeting points of the two warps that share 32 rows
+  uint32_t tmem_base;
+  int abort_flag;
+  float amax[2][2][BW];     // [tile parity][half][row]
+};
+
+struct PairTile {
+  int row0, rows;           // this CTA's rows: row0 .. row0 + rows - 1 (rows <= 0: none)
+  int peer_rows;            // the other CTA's
+  int n0, group, single;
+};
+
+template <bool kGated>
+__device__ __forceinline__ PairTile pair_decode(int t, int rank, const int32_t* prefix, const int32_t* offs,
+                                                const BlkParams& p) {
+  int lo = 0, hi = p.groups;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (prefix[mid] * p.n_tiles <= t) lo = mid; else hi = mid;
+  }
+  const int blocks = prefix[lo + 1] - prefix[lo];
+  const int local = t - prefix[lo] * p.n_tiles;
+  const int nb = local / blocks, mb = local - nb * blocks;
+  const int rows = offs[2 * lo + 1] - offs[2 * lo] - mb * kPairRows;     // rows from this block on
+  PairTile tile;
+  tile.row0 = offs[2 * lo] + mb * kPairRows + rank * BW;
+  tile.rows = min(BW, rows - rank * BW);
+  tile.peer_rows = min(BW, rows - (rank ^ 1) * BW);
+  tile.n0 = nb * (kGated ? BW : 2 * BW);
+  tile.group = lo;
+  tile.single = blocks == 1 ? 1 : 0;
+  return tile;
+}
+
+template <bool kGated>
+__global__ void __launch_bounds__(kThreads, 1)
+gemm_blk_pair(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b0,
+              const __grid_constant__ CUtensorMap tm_b1, const BlkParams p) {
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t raw = ptx::smem_u32(smem_raw);
+  const uint32_t pad = (1024u - (raw & 1023u)) & 1023u;
+  unsigned char* base = smem_raw + pad;
+  const uint32_t ring_u32 = raw + pad;
+  float* s_scale = reinterpret_cast<float*>(base + kPairStages * kPairStageBytes);     // [kScaleSlots][kScaleBatch][2][BW]
+  PairTail* st = reinterpret_cast<PairTail*>(s_scale + kScaleSlots * kScaleBatch * 2 * BW);
+  int32_t* prefix = reinterpret_cast<int32_t*>(st + 1);
+  int32_t* offs = prefix + p.groups + 1;
+
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int rank = static_cast<int>(ptx::cluster_ctarank());            // 0 = leader
+  const int first = blockIdx.x >> 1, step = gridDim.x >> 1;
+
+  if (tid == 0) {
+    for (int s = 0; s < kPairStages; ++s) {
+      ptx::mbar_init(ptx::smem_u32(&st->full[s]), 1);
+      ptx::mbar_init(ptx::smem_u32(&st->empty[s]), 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      ptx::mbar_init(ptx::smem_u32(&st->acc_full[a]), 1);
+      ptx::mbar_init(ptx::smem_u32(&st->acc_empty[a]), 2 * kEpilogueThreads / 32);   // the warps of both CTAs
+    }
+    for (int s = 0; s < kScaleSlots; ++s) {
+      ptx::mbar_init(ptx::smem_u32(&st->sc_full[s]), kScaleThreads);
+      ptx::mbar_init(ptx::smem_u32(&st->sc_empty[s]), kEpilogueThreads / 32);
+    }
+    for (int q = 0; q < 4; ++q) ptx::mbar_init(ptx::smem_u32(&st->row_sync[q]), 2);
+    st->abort_flag = 0;
+    prefix[0] = 0;
+    ptx::fence_barrier_init();
+    ptx::fence_proxy_async_smem();
+  }
+  if (warp == 0) {
+    blk_prefixes(p, kPairRows, prefix, offs, lane);
+    if (lane == 0) {
+      ptx::prefetch_tensormap(&tm_a);
+      ptx::prefetch_tensormap(rank == 0 ? &tm_b0 : &tm_b1);
+    }
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc_pair(ptx::smem_u32(&st->tmem_base), kTmemCols);
+    ptx::tmem_relinquish_pair();
+  }
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  ptx::cluster_sync();            // both CTAs' barriers exist before anything signals across the pair
+  ptx::tc_fence_after_sync();
+
+  const uint32_t tmem_base = st->tmem_base;
+  const int total_tiles = prefix[p.groups] * p.n_tiles;
+  volatile int* abort_flag = &st->abort_flag;
+
+  if (warp < 4) {
+    ptx::setmaxnreg_dec<48>();
+    if (warp == 0) {
+      // ---------------------------------------------------------------- TMA producer (both CTAs)
+      if (lane == 0) {
+        int stage = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        const uint64_t pol_first = ptx::l2_policy_evict_first(), pol_last = ptx::l2_policy_evict_last();
+        const CUtensorMap* mb = rank == 0 ? &tm_b0 : &tm_b1;
+        for (int t = first; ok && t < total_tiles; t += step) {
+          const PairTile tile = pair_decode<kGated>(t, rank, prefix, offs, p);
+          // the leader's box: gate rows, or the tile's first 128 columns; the peer's: up rows, or the next 128 (what
+          // lies beyond N is computed and not stored; beyond the last group it reads as zero)
+          const int w_row = tile.group * p.N + tile.n0 + (kGated ? 0 : rank * BW);
+          const uint64_t pol_w = tile.single ? pol_first : pol_last;
+          const int my_rows = (max(tile.rows, 0) + kPairRowBox - 1) / kPairRowBox * kPairRowBox;
+          const int peer_rows = (max(tile.peer_rows, 0) + kPairRowBox - 1) / kPairRowBox * kPairRowBox;
+          for (int kb = 0; kb < p.k_blocks; ++kb) {
+            if (!ptx::mbar_wait(ptx::smem_u32(&st->empty[stage]), phase ^ 1u, abort_flag)) {
+              blk_timeout(p, 6);
+              ok = false;
+              break;
+            }
+            const uint32_t full = ptx::smem_u32(&st->full[stage]);
+            const uint32_t full_leader = ptx::map_to_cta(full, 0);
+            const uint32_t s = ring_u32 + stage * kPairStageBytes;
+            if (rank == 0) ptx::mbar_expect_tx(full, 2 * kWBoxBytes + (my_rows + peer_rows) * BK);   // both CTAs' bytes
+            ptx::tma_load_2d_pair_hint(s + BW * BK, mb, full_leader, kb * BK, w_row, pol_w);
+            for (int r = 0; r < my_rows; r += kPairRowBox)
+              ptx::tma_load_2d_pair_hint(s + r * BK, &tm_a, full_leader, kb * BK, tile.row0 + r, pol_last);
+            if (++stage == kPairStages) { stage = 0; phase ^= 1u; }
+          }
+        }
+      }
+      __syncwarp();
+    } else if (warp == 1) {
+      // ---------------------------------------------------------------- MMA issuer (leader only)
+      if (lane == 0 && rank == 0) {
+        constexpr uint32_t idesc = ptx::idesc_e4m3_f32(kPairRows, 2 * BW);
+        int stage = 0, buf = 0;
+        uint32_t phase = 0, buf_phase = 0;
+        bool ok = true;
+        for (int t = first; ok && t < total_tiles; t += step) {
+          for (int kb = 0; kb < p.k_blocks; ++kb) {
+            if (!ptx::mbar_wait(ptx::smem_u32(&st->full[stage]), phase, abort_flag) ||
+                !ptx::mbar_wait(ptx::smem_u32(&st->acc_empty[buf]), buf_phase ^ 1u, abort_flag)) {
+              blk_timeout(p, 7);
+              ok = false;
+              break;
+            }
+            ptx::tc_fence_after_sync();
+            const uint32_t s = ring_u32 + stage * kPairStageBytes;
+            const uint64_t a = ptx::smem_desc_sw128(s), b = ptx::smem_desc_sw128(s + BW * BK);
+            const uint32_t d = tmem_base + static_cast<uint32_t>(buf * kTmemBuf);
+#pragma unroll
+            for (int k4 = 0; k4 < BK / UMMA_K; ++k4)
+              ptx::tc_mma_e4m3_pair(d, a + 2 * k4, b + 2 * k4, idesc, k4 != 0 ? 1u : 0u);
+            ptx::tc_commit_pair(ptx::smem_u32(&st->empty[stage]), 3);    // in both CTAs
+            ptx::tc_commit_pair(ptx::smem_u32(&st->acc_full[buf]), 3);
+            if (++stage == kPairStages) { stage = 0; phase ^= 1u; }
+            if (++buf == 2) { buf = 0; buf_phase ^= 1u; }
+          }
+        }
+      }
+      __syncwarp();
+    } else {
+      // ---------------------------------------------------------------- scale loaders
+      auto decode = [&](int t) {
+        const PairTile tile = pair_decode<kGated>(t, rank, prefix, offs, p);
+        return ScaleRows{tile.row0, tile.rows, tile.n0, tile.group};
+      };
+      blk_load_scales<kGated, BW>(p, first, step, total_tiles, 0, p.k_blocks, tid - 64, s_scale, st->sc_full, st->sc_empty,
+                                  abort_flag, decode);
+    }
+  } else {
+    // ------------------------------------------------------------------ epilogue (both CTAs, own 128 rows)
+    ptx::setmaxnreg_inc<224>();
+    const int quarter = warp & 3, half = (warp - 4) >> 2;
+    const int r_tile = quarter * 32 + lane;
+    const uint32_t t_lane = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(half * 64);
+    const uint32_t empty0 = ptx::map_to_cta(ptx::smem_u32(&st->acc_empty[0]), 0);
+    const uint32_t empty1 = ptx::map_to_cta(ptx::smem_u32(&st->acc_empty[1]), 0);
+    int buf = 0, slot = 0, parity = 0;
+    uint32_t buf_phase = 0, slot_phase = 0, row_phase = 0;
+    bool ok = true;
+    auto all_wait = [&](uint32_t bar, uint32_t phase) -> bool {
+      return __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar, phase, abort_flag));
+    };
+    for (int t = first; ok && t < total_tiles; t += step) {
+      const PairTile tile = pair_decode<kGated>(t, rank, prefix, offs, p);
+      const bool live = quarter * 32 < tile.rows;           // any row of this warp
+      // columns half * 64 .. + 63 of each weight box: sums 0..63 of the first box, 64..127 of the second
+      float acc[128];
+#pragma unroll
+      for (int i = 0; i < 128; ++i) acc[i] = 0.f;
+      for (int kb = 0; ok && kb < p.k_blocks; kb += kScaleBatch) {
+        if (!all_wait(ptx::smem_u32(&st->sc_full[slot]), slot_phase)) {
+          ok = false;
+          break;
+        }
+        const float* f = s_scale + slot * kScaleBatch * 2 * BW + r_tile;
+        const int batch = min(kScaleBatch, p.k_blocks - kb);
+        for (int u = 0; u < batch; ++u, f += 2 * BW) {
+          const float s0 = f[0], s1 = f[BW];
+          if (!all_wait(ptx::smem_u32(&st->acc_full[buf]), buf_phase)) {
+            ok = false;
+            break;
+          }
+          ptx::tc_fence_after_sync();
+          const uint32_t empty = buf == 0 ? empty0 : empty1;
+          if (live) {
+            // the next 16 columns are on their way while the last 16 are added
+            const uint32_t ta = t_lane + static_cast<uint32_t>(buf * kTmemBuf);
+            uint32_t v[2][16];
+            ptx::tmem_ld_32x16(ta, v[0]);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+              ptx::tmem_ld_wait();
+              if (c < 7) ptx::tmem_ld_32x16(ta + ((c + 1) >> 2) * BW + ((c + 1) & 3) * 16, v[(c + 1) & 1]);
+              if (c == 7) {
+                ptx::tc_fence_before_sync();
+                ptx::mbar_arrive_cluster_if(empty, lane == 0);     // the warp's loads from this block have completed
+              }
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                acc[16 * c + i] = fmaf(__uint_as_float(v[c & 1][i]), c < 4 ? s0 : s1, acc[16 * c + i]);
+            }
+          } else {
+            ptx::mbar_arrive_cluster_if(empty, lane == 0);
+          }
+          if (++buf == 2) { buf = 0; buf_phase ^= 1u; }
+        }
+        __syncwarp();
+        ptx::mbar_arrive_if(ptx::smem_u32(&st->sc_empty[slot]), lane == 0);
+        if (++slot == kScaleSlots) { slot = 0; slot_phase ^= 1u; }
+      }
+      if (!ok) {
+        if (lane == 0) blk_timeout(p, 8);
+        break;
+      }
+      const int row = tile.row0 + r_tile;
+      const bool row_ok = r_tile < tile.rows;
+      if constexpr (kGated) {
+        float h[64], amax = 0.f;
+#pragma unroll
+        for (int i = 0; i < 64; ++i) {
+          h[i] = blk_silu_mul(acc[i], acc[64 + i]);
+          amax = fmaxf(amax, fabsf(h[i]));
+        }
+        // a block of h is 128 columns: the row's other 64 are the other half's
+        st->amax[parity][half][r_tile] = amax;
+        __syncwarp();
+        const uint32_t bar = ptx::smem_u32(&st->row_sync[quarter]);
+        if (lane == 0) ptx::mbar_arrive(bar);
+        if (!all_wait(bar, row_phase)) {
+          if (lane == 0) blk_timeout(p, 9);
+          ok = false;
+          break;
+        }
+        row_phase ^= 1u;
+        amax = fmaxf(amax, st->amax[parity][half ^ 1][r_tile]);
+        parity ^= 1;
+        const float sc = blk::scale_of(amax);
+        const blk::Divider by(sc);
+        if (row_ok) {
+          const size_t at = static_cast<size_t>(row) * p.N + tile.n0 + half * 64;
+          uint4* dst = reinterpret_cast<uint4*>(p.hq + (at >> 2));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float* v = h + 16 * i + 4 * j;
+              w[j] = blk::pack4(v[0], v[1], v[2], v[3], by);
+            }
+            dst[i] = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+          if (half == 0) p.sh[static_cast<size_t>(tile.n0 / BW) * p.rows + row] = sc;
+          if (p.h_dbg != nullptr) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              *reinterpret_cast<float4*>(p.h_dbg + at + 4 * i) = make_float4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
+          }
+        }
+      } else if (row_ok) {
+        __nv_bfloat16* y = p.y + static_cast<size_t>(row) * p.N;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int col = tile.n0 + (i >> 3) * BW + half * 64 + 8 * (i & 7);
+          uint32_t w[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) w[j] = pack_bf16(acc[8 * i + 2 * j], acc[8 * i + 2 * j + 1]);
+          if (col < p.N) *reinterpret_cast<uint4*>(y + col) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+      }
+    }
+  }
+
+  __syncthreads();
+  if (st->abort_flag) {
+    for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+    __syncthreads();
+  }
+  ptx::cluster_sync();            // the peer's shared memory and barriers stay alive until both CTAs are done
+  if (warp == 1) {
+    ptx::tc_fence_after_sync();
+    ptx::tmem_dealloc_pair(tmem_base, kTmemCols);
+  }
+}
+
 // Tensor map over a row-major [rows, cols] matrix of E4M3 bytes: boxes of box_rows x 128 bytes, 128-byte swizzle; what
 // lies outside reads as zero.
 CUresult encode_bytes(moe_ctx* ctx, CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows) {
@@ -538,7 +875,7 @@ moe_status launch_swapped(moe_ctx* ctx, const BlkProduct& g, BlkParams p, cudaSt
       encode_bytes(ctx, &tm_b1, kGated ? g.b1 : g.b0, w_rows, g.K, BW) != CUDA_SUCCESS)
     return MOE_ERR_CUDA;
   constexpr size_t kStageBytes = 2 * kWBoxBytes + kMaxN * BK;
-  const size_t rest = 1024 + 2 * kOutTokens * 256 * 4 + kScaleSlots * 2 * kMaxN * 4 + sizeof(BlkTail) +
+  const size_t rest = 1024 + 2 * kOutTokens * 256 * 4 + kScaleSlots * kScaleBatch * 2 * kMaxN * 4 + sizeof(BlkTail) +
                       (3 * static_cast<size_t>(p.groups) + 1) * 4 + 16;
   int stages = static_cast<int>((kMaxSmem - rest) / kStageBytes);
   if (stages > kMaxStages) stages = kMaxStages;
@@ -568,7 +905,37 @@ moe_status launch_swapped(moe_ctx* ctx, const BlkProduct& g, BlkParams p, cudaSt
 }
 
 template <bool kGated>
+moe_status launch_pair(moe_ctx* ctx, const BlkProduct& g, const BlkParams& p, cudaStream_t stream) {
+  const uint64_t w_rows = static_cast<uint64_t>(p.groups) * p.N;
+  CUtensorMap tm_a, tm_b0, tm_b1;
+  if (encode_bytes(ctx, &tm_a, g.a, p.rows, g.K, kPairRowBox) != CUDA_SUCCESS ||
+      encode_bytes(ctx, &tm_b0, g.b0, w_rows, g.K, BW) != CUDA_SUCCESS ||
+      encode_bytes(ctx, &tm_b1, kGated ? g.b1 : g.b0, w_rows, g.K, BW) != CUDA_SUCCESS)
+    return MOE_ERR_CUDA;
+  const size_t smem = 1024 + kPairStages * kPairStageBytes + kScaleSlots * kScaleBatch * 2 * BW * 4 + sizeof(PairTail) +
+                      (3 * static_cast<size_t>(p.groups) + 1) * 4 + 16;
+  const long long tiles = (p.rows / kPairRows + static_cast<long long>(p.groups < p.rows ? p.groups : p.rows)) * p.n_tiles;
+  const long long pairs = tiles < ctx->max_pairs ? tiles : ctx->max_pairs;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(static_cast<unsigned>(2 * pairs));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  ctx->last_launches += 1;
+  return cudaLaunchKernelEx(&cfg, gemm_blk_pair<kGated>, tm_a, tm_b0, tm_b1, p) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+}
+
+template <bool kGated>
 moe_status launch_product(moe_ctx* ctx, const BlkProduct& g, const BlkParams& p, cudaStream_t stream) {
+  const int pair_rows = moe_knob_value(ctx, "blk_pair_rows", 32);
+  if (p.rows > static_cast<long long>(pair_rows) * p.groups) return launch_pair<kGated>(ctx, g, p, stream);
   // short stages (more of them) where the groups average few rows
   if (p.rows <= 16LL * p.groups) return launch_swapped<kGated, 32>(ctx, g, p, stream);
   return launch_swapped<kGated, 128>(ctx, g, p, stream);
@@ -583,7 +950,9 @@ cudaError_t prepare_gemm_blk(moe_ctx* ctx) {
   const void* kernels[] = {reinterpret_cast<const void*>(gemm_blk_swapped<true, 32>),
                            reinterpret_cast<const void*>(gemm_blk_swapped<false, 32>),
                            reinterpret_cast<const void*>(gemm_blk_swapped<true, 128>),
-                           reinterpret_cast<const void*>(gemm_blk_swapped<false, 128>)};
+                           reinterpret_cast<const void*>(gemm_blk_swapped<false, 128>),
+                           reinterpret_cast<const void*>(gemm_blk_pair<true>),
+                           reinterpret_cast<const void*>(gemm_blk_pair<false>)};
   for (const void* k : kernels) {
     const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
     if (e != cudaSuccess) return e;

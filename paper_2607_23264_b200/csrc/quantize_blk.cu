@@ -51,9 +51,10 @@ quantize_rows_blk(const uint4* __restrict__ in, long long rows, int vec_per_row,
 #pragma unroll
     for (int off = 8; off > 0; off >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, off));
     const float sc = blk::scale_of(amax);
+    const blk::Divider by(sc);
     if (mine)
       codes[row * vec_per_row + v] =
-          make_uint2(blk::pack4(f[0], f[1], f[2], f[3], sc), blk::pack4(f[4], f[5], f[6], f[7], sc));
+          make_uint2(blk::pack4(f[0], f[1], f[2], f[3], by), blk::pack4(f[4], f[5], f[6], f[7], by));
     if (live && sub == 0) scales[static_cast<size_t>(b) * rows + row] = sc;
   }
 }
@@ -89,6 +90,7 @@ quantize_weights_blk(const uint4* __restrict__ in, int rows, int vec_per_row, in
 #pragma unroll
   for (int i = 0; i < kThreads / 32; ++i) amax = fmaxf(amax, s_part[i]);
   const float sc = blk::scale_of(amax);
+  const blk::Divider by(sc);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int r = rb * 128 + i * 16 + (tid >> 4);
@@ -96,7 +98,7 @@ quantize_weights_blk(const uint4* __restrict__ in, int rows, int vec_per_row, in
       float f[8];
       unpack8(q[i], f);
       codes[(mat * rows + r) * vec_per_row + v] =
-          make_uint2(blk::pack4(f[0], f[1], f[2], f[3], sc), blk::pack4(f[4], f[5], f[6], f[7], sc));
+          make_uint2(blk::pack4(f[0], f[1], f[2], f[3], by), blk::pack4(f[4], f[5], f[6], f[7], by));
     }
   }
   if (tid == 0) scales[(mat * row_blocks + rb) * col_blocks + cb] = sc;
