@@ -344,24 +344,26 @@ gemm_blk_swapped(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
       __syncwarp();
     } else if (warp == 1) {
       // ---------------------------------------------------------------- MMA issuer
-      if (lane == 0) {
-        int stage = 0, buf = 0;
-        uint32_t phase = 0, buf_phase = 0;
-        bool ok = true;
-        for (int t = first; ok && t < total_tiles; t += step) {
-          const uint32_t idesc = ptx::idesc_e4m3_f32(BW, blk_decode<kGated, kMaxN>(t, prefix, offs, p).n_pad);
-          for (int kb = kb0; kb < kb1; ++kb) {
-            if (!ptx::mbar_wait(ptx::smem_u32(&st->full[stage]), phase, abort_flag) ||
-                !ptx::mbar_wait(ptx::smem_u32(&st->acc_empty[buf]), buf_phase ^ 1u, abort_flag)) {
-              blk_timeout(p, 2);
-              ok = false;
-              break;
-            }
-            ptx::tc_fence_after_sync();
-            const uint32_t s = ring_u32 + stage * kStageBytes;
-            const uint64_t w0 = ptx::smem_desc_sw128(s), w1 = ptx::smem_desc_sw128(s + kWBoxBytes);
-            const uint64_t a = ptx::smem_desc_sw128(s + 2 * kWBoxBytes);
-            const uint32_t d = tmem_base + static_cast<uint32_t>(buf * kTmemBuf);
+      // The whole warp runs the loop and one elected lane issues: with the loop's values warp-uniform the operands are in
+      // the registers the MMA reads them from, and issuing four costs half as much as from a single-lane branch.
+      int stage = 0, buf = 0;
+      uint32_t phase = 0, buf_phase = 1;
+      bool ok = true;
+      for (int t = first; ok && t < total_tiles; t += step) {
+        const uint32_t idesc = ptx::idesc_e4m3_f32(BW, blk_decode<kGated, kMaxN>(t, prefix, offs, p).n_pad);
+        for (int kb = kb0; kb < kb1; ++kb) {
+          if (!ptx::mbar_wait_warp(ptx::smem_u32(&st->full[stage]), phase, abort_flag) ||
+              !ptx::mbar_wait_warp(ptx::smem_u32(&st->acc_empty[buf]), buf_phase, abort_flag)) {
+            if (lane == 0) blk_timeout(p, 2);
+            ok = false;
+            break;
+          }
+          ptx::tc_fence_after_sync();
+          const uint32_t s = ring_u32 + stage * kStageBytes;
+          const uint64_t w0 = ptx::smem_desc_sw128(s), w1 = ptx::smem_desc_sw128(s + kWBoxBytes);
+          const uint64_t a = ptx::smem_desc_sw128(s + 2 * kWBoxBytes);
+          const uint32_t d = tmem_base + static_cast<uint32_t>(buf * kTmemBuf);
+          if (ptx::elect_one()) {
 #pragma unroll
             for (int k4 = 0; k4 < BK / UMMA_K; ++k4) {
               const uint64_t adv = static_cast<uint64_t>(2 * k4);      // +32 bytes along K inside the swizzle row
@@ -370,12 +372,13 @@ gemm_blk_swapped(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
             }
             ptx::tc_commit(ptx::smem_u32(&st->empty[stage]));
             ptx::tc_commit(ptx::smem_u32(&st->acc_full[buf]));
-            if (++stage == p.stages) { stage = 0; phase ^= 1u; }
-            if (++buf == 2) { buf = 0; buf_phase ^= 1u; }
           }
+          __syncwarp();
+          if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+          buf ^= 1;
+          buf_phase ^= buf == 0 ? 1u : 0u;
         }
       }
-      __syncwarp();
     } else {
       // ---------------------------------------------------------------- scale loaders
       auto decode = [&](int t) {
@@ -532,13 +535,16 @@ gemm_blk_swapped(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
 // Rows are the M side here, so a thread of the epilogue owns one row and the scales are one factor per weight box.
 // Each CTA stages its 128 rows and one of the two weight boxes (32 KB per block of K: 64 bytes per clock at the tensor
 // rate, what an SM takes in from L2, where a single CTA's 128 x 256 tile would need 96), the leader issues the MMAs of
-// both, and every CTA's eight epilogue warps keep 128 running sums per thread.  Tensor memory holds two blocks of K.
-// Handing a block back crosses the pair once per block and warp: those arrivals carry no cluster-wide release (it costs
-// about a thousand clocks), the loads from tensor memory have completed before them and there is nothing else to publish.
+// both, and every CTA's eight epilogue warps keep 128 running sums per thread.
+// Tensor memory holds two blocks of K.  Handing one back crosses the pair once per block and warp: those arrivals carry
+// no cluster-wide release (300 clocks more), the loads from tensor memory have completed before them and there is nothing
+// else to publish.
 constexpr int kPairRows = 256;
 constexpr int kPairRowBox = 32;          // rows of a per TMA box
-constexpr int kPairStages = 6;
+constexpr int kPairStages = 5;
 constexpr int kPairStageBytes = BW * BK + kWBoxBytes;
+constexpr int kStoreBoxCols = 64;        // output box of a warp: 32 rows x 64 bf16 columns (128 bytes, swizzled)
+constexpr int kStoreBoxBytes = 32 * kStoreBoxCols * 2;
 
 struct PairTail {
   uint64_t full[kPairStages];
@@ -584,13 +590,15 @@ __device__ __forceinline__ PairTile pair_decode(int t, int rank, const int32_t* 
 template <bool kGated>
 __global__ void __launch_bounds__(kThreads, 1)
 gemm_blk_pair(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b0,
-              const __grid_constant__ CUtensorMap tm_b1, const BlkParams p) {
+              const __grid_constant__ CUtensorMap tm_b1, const __grid_constant__ CUtensorMap tm_y, const BlkParams p) {
   extern __shared__ unsigned char smem_raw[];
   const uint32_t raw = ptx::smem_u32(smem_raw);
   const uint32_t pad = (1024u - (raw & 1023u)) & 1023u;
   unsigned char* base = smem_raw + pad;
   const uint32_t ring_u32 = raw + pad;
-  float* s_scale = reinterpret_cast<float*>(base + kPairStages * kPairStageBytes);     // [kScaleSlots][kScaleBatch][2][BW]
+  const uint32_t store_u32 = ring_u32 + kPairStages * kPairStageBytes;                 // one output box per epilogue warp
+  unsigned char* s_store = base + kPairStages * kPairStageBytes;
+  float* s_scale = reinterpret_cast<float*>(s_store + kEpilogueThreads / 32 * kStoreBoxBytes);   // [kScaleSlots][kScaleBatch][2][BW]
   PairTail* st = reinterpret_cast<PairTail*>(s_scale + kScaleSlots * kScaleBatch * 2 * BW);
   int32_t* prefix = reinterpret_cast<int32_t*>(st + 1);
   int32_t* offs = prefix + p.groups + 1;
@@ -675,17 +683,17 @@ gemm_blk_pair(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ 
       }
       __syncwarp();
     } else if (warp == 1) {
-      // ---------------------------------------------------------------- MMA issuer (leader only)
-      if (lane == 0 && rank == 0) {
+      // ---------------------------------------------------------------- MMA issuer (leader only; whole warp, see above)
+      if (rank == 0) {
         constexpr uint32_t idesc = ptx::idesc_e4m3_f32(kPairRows, 2 * BW);
         int stage = 0, buf = 0;
-        uint32_t phase = 0, buf_phase = 0;
+        uint32_t phase = 0, buf_phase = 1;
         bool ok = true;
         for (int t = first; ok && t < total_tiles; t += step) {
           for (int kb = 0; kb < p.k_blocks; ++kb) {
-            if (!ptx::mbar_wait(ptx::smem_u32(&st->full[stage]), phase, abort_flag) ||
-                !ptx::mbar_wait(ptx::smem_u32(&st->acc_empty[buf]), buf_phase ^ 1u, abort_flag)) {
-              blk_timeout(p, 7);
+            if (!ptx::mbar_wait_warp(ptx::smem_u32(&st->full[stage]), phase, abort_flag) ||
+                !ptx::mbar_wait_warp(ptx::smem_u32(&st->acc_empty[buf]), buf_phase, abort_flag)) {
+              if (lane == 0) blk_timeout(p, 7);
               ok = false;
               break;
             }
@@ -693,17 +701,20 @@ gemm_blk_pair(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ 
             const uint32_t s = ring_u32 + stage * kPairStageBytes;
             const uint64_t a = ptx::smem_desc_sw128(s), b = ptx::smem_desc_sw128(s + BW * BK);
             const uint32_t d = tmem_base + static_cast<uint32_t>(buf * kTmemBuf);
+            if (ptx::elect_one()) {
 #pragma unroll
-            for (int k4 = 0; k4 < BK / UMMA_K; ++k4)
-              ptx::tc_mma_e4m3_pair(d, a + 2 * k4, b + 2 * k4, idesc, k4 != 0 ? 1u : 0u);
-            ptx::tc_commit_pair(ptx::smem_u32(&st->empty[stage]), 3);    // in both CTAs
-            ptx::tc_commit_pair(ptx::smem_u32(&st->acc_full[buf]), 3);
+              for (int k4 = 0; k4 < BK / UMMA_K; ++k4)
+                ptx::tc_mma_e4m3_pair(d, a + 2 * k4, b + 2 * k4, idesc, k4 != 0 ? 1u : 0u);
+              ptx::tc_commit_pair(ptx::smem_u32(&st->empty[stage]), 3);    // in both CTAs
+              ptx::tc_commit_pair(ptx::smem_u32(&st->acc_full[buf]), 3);
+            }
+            __syncwarp();
             if (++stage == kPairStages) { stage = 0; phase ^= 1u; }
-            if (++buf == 2) { buf = 0; buf_phase ^= 1u; }
+            buf ^= 1;
+            buf_phase ^= buf == 0 ? 1u : 0u;
           }
         }
       }
-      __syncwarp();
     } else {
       // ---------------------------------------------------------------- scale loaders
       auto decode = [&](int t) {
@@ -750,8 +761,8 @@ gemm_blk_pair(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ 
           ptx::tc_fence_after_sync();
           const uint32_t empty = buf == 0 ? empty0 : empty1;
           if (live) {
-            // the next 16 columns are on their way while the last 16 are added
             const uint32_t ta = t_lane + static_cast<uint32_t>(buf * kTmemBuf);
+            // the next 16 columns are on their way while the last 16 are added (more in flight does not fit the registers)
             uint32_t v[2][16];
             ptx::tmem_ld_32x16(ta, v[0]);
 #pragma unroll
@@ -760,7 +771,7 @@ gemm_blk_pair(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ 
               if (c < 7) ptx::tmem_ld_32x16(ta + ((c + 1) >> 2) * BW + ((c + 1) & 3) * 16, v[(c + 1) & 1]);
               if (c == 7) {
                 ptx::tc_fence_before_sync();
-                ptx::mbar_arrive_cluster_if(empty, lane == 0);     // the warp's loads from this block have completed
+                ptx::mbar_arrive_cluster_if(empty, lane == 0);     // the warp's loads from this accumulator have completed
               }
 #pragma unroll
               for (int i = 0; i < 16; ++i)
@@ -823,18 +834,41 @@ gemm_blk_pair(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ 
               *reinterpret_cast<float4*>(p.h_dbg + at + 4 * i) = make_float4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
           }
         }
-      } else if (row_ok) {
+      } else {
         __nv_bfloat16* y = p.y + static_cast<size_t>(row) * p.N;
+        const bool whole = quarter * 32 + 32 <= tile.rows;       // all 32 rows are the group's: one bulk store per box
+        const uint32_t box = store_u32 + static_cast<uint32_t>(warp - 4) * kStoreBoxBytes;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int col = tile.n0 + (i >> 3) * BW + half * 64 + 8 * (i & 7);
-          uint32_t w[4];
+        for (int c = 0; c < 2; ++c) {
+          const int col0 = tile.n0 + c * BW + half * 64;
+          if (col0 >= p.N) continue;
+          if (whole) {
+            if (lane == 0) ptx::bulk_wait_group_read_all();      // the box's last store has read it
+            __syncwarp();
+          }
 #pragma unroll
-          for (int j = 0; j < 4; ++j) w[j] = pack_bf16(acc[8 * i + 2 * j], acc[8 * i + 2 * j + 1]);
-          if (col < p.N) *reinterpret_cast<uint4*>(y + col) = make_uint4(w[0], w[1], w[2], w[3]);
+          for (int i = 0; i < 8; ++i) {
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = pack_bf16(acc[64 * c + 8 * i + 2 * j], acc[64 * c + 8 * i + 2 * j + 1]);
+            const uint4 q = make_uint4(w[0], w[1], w[2], w[3]);
+            if (whole)
+              *reinterpret_cast<uint4*>(s_store + (box - store_u32) + lane * 128 + ((i ^ (lane & 7)) << 4)) = q;
+            else if (row_ok && col0 + 8 * i < p.N)
+              *reinterpret_cast<uint4*>(y + col0 + 8 * i) = q;
+          }
+          if (whole) {
+            ptx::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+              ptx::tma_store_2d(&tm_y, box, col0, row - lane);   // what lies beyond N is not written
+              ptx::bulk_commit_group();
+            }
+          }
         }
       }
     }
+    if (lane == 0) ptx::bulk_wait_group_all();                   // this warp's stores have landed
   }
 
   __syncthreads();
@@ -907,12 +941,23 @@ moe_status launch_swapped(moe_ctx* ctx, const BlkProduct& g, BlkParams p, cudaSt
 template <bool kGated>
 moe_status launch_pair(moe_ctx* ctx, const BlkProduct& g, const BlkParams& p, cudaStream_t stream) {
   const uint64_t w_rows = static_cast<uint64_t>(p.groups) * p.N;
-  CUtensorMap tm_a, tm_b0, tm_b1;
+  CUtensorMap tm_a, tm_b0, tm_b1, tm_y;
   if (encode_bytes(ctx, &tm_a, g.a, p.rows, g.K, kPairRowBox) != CUDA_SUCCESS ||
       encode_bytes(ctx, &tm_b0, g.b0, w_rows, g.K, BW) != CUDA_SUCCESS ||
       encode_bytes(ctx, &tm_b1, kGated ? g.b1 : g.b0, w_rows, g.K, BW) != CUDA_SUCCESS)
     return MOE_ERR_CUDA;
-  const size_t smem = 1024 + kPairStages * kPairStageBytes + kScaleSlots * kScaleBatch * 2 * BW * 4 + sizeof(PairTail) +
+  if (kGated) {
+    tm_y = tm_a;                                             // (not used)
+  } else {
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(p.N), static_cast<cuuint64_t>(p.rows)};
+    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(p.N) * 2};
+    const cuuint32_t box[2] = {kStoreBoxCols, 32u}, elem[2] = {1u, 1u};
+    if (ctx->encode_tiled(&tm_y, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.y, dims, strides, box, elem,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return MOE_ERR_CUDA;
+  }
+  const size_t smem = 1024 + kPairStages * kPairStageBytes + kEpilogueThreads / 32 * kStoreBoxBytes + kScaleSlots * kScaleBatch * 2 * BW * 4 + sizeof(PairTail) +
                       (3 * static_cast<size_t>(p.groups) + 1) * 4 + 16;
   const long long tiles = (p.rows / kPairRows + static_cast<long long>(p.groups < p.rows ? p.groups : p.rows)) * p.n_tiles;
   const long long pairs = tiles < ctx->max_pairs ? tiles : ctx->max_pairs;
@@ -929,7 +974,7 @@ moe_status launch_pair(moe_ctx* ctx, const BlkProduct& g, const BlkParams& p, cu
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   ctx->last_launches += 1;
-  return cudaLaunchKernelEx(&cfg, gemm_blk_pair<kGated>, tm_a, tm_b0, tm_b1, p) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, gemm_blk_pair<kGated>, tm_a, tm_b0, tm_b1, tm_y, p) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
 template <bool kGated>
