@@ -9,9 +9,9 @@
 // its weights are read once, whatever its size up to 128 rows; more rows are split evenly into blocks that run side by
 // side and share the weights in L2.
 //
-// Roles (384 threads, 168 registers each at launch, moved to where they are needed): warp 0 = TMA producer, warp 1 =
-// MMA issuer, warps 2-3 = scale loaders (sa * sb per row and weight box, a ring of four blocks in shared memory),
-// warps 4-11 = epilogue (four lane quarters x two halves of the rows; 128 running sums per thread at most).
+// Roles (384 threads, 168 registers each at launch, moved to where they are needed): warp 0 = TMA producer, warps 1 and
+// 3 = MMA issuers, warp 2 = scale loader (sa * sb per row and weight box, through a ring in shared memory), warps 4-11 =
+// epilogue (four lane quarters x two halves of the rows; 128 running sums per thread at most).
 // Shapes with too few tiles for the SMs split K over a cluster of 2, 4 or 8 CTAs, which add their running sums through
 // distributed shared memory in rank order: no scratch memory, no atomics, the same bits every time.
 // Every wait is bounded; a wait that gives up is reported through the status word and the CTA unwinds.
@@ -36,7 +36,7 @@ constexpr int kRowBox = 16;              // rows of a per TMA box
 constexpr int kMaxStages = 6;
 constexpr int kScaleSlots = 2;           // scale ring: slots of kScaleBatch blocks of K each
 constexpr int kScaleBatch = 4;
-constexpr int kScaleThreads = 64;
+constexpr int kScaleThreads = 32;
 constexpr int kTmemCols = 512;           // two buffers x two weight boxes x 128 columns
 constexpr int kTmemBuf = 256;
 constexpr int kOutTokens = 8;            // rows of a staged per step of the tile's end, per epilogue half
@@ -83,7 +83,9 @@ struct BlkTile {
   int single;        // no other tile reads these weights
 };
 
-__device__ __forceinline__ void blk_timeout(const BlkParams& p, int role) {
+// The roles whose waits may give up; the flag holds the first that did, and the kernel's end reports it.
+enum BlkRole { kRoleTma = 1, kRoleMma = 2, kRoleScale = 3, kRoleEpilogue = 4 };
+__device__ __forceinline__ void blk_report(const BlkParams& p, int role) {
   atomicCAS(&p.status[0], 0, MOE_ERR_TIMEOUT);
   atomicCAS(&p.status[1], 0, kKernelIdBlk * 65536 + role);
 }
@@ -183,6 +185,7 @@ __device__ __forceinline__ void blk_load_scales(const BlkParams& p, int first, i
   int slot = 0;
   uint32_t slot_phase = 0;
   for (int t = first; t < total_tiles; t += step) {
+    if (__any_sync(0xFFFFFFFFu, *abort_flag)) return;
     const ScaleRows tile = decode(t);
     const int nb = tile.n0 / BW;
     const size_t w_at = (static_cast<size_t>(tile.group) * p.n_blocks + nb) * p.k_blocks;
@@ -201,10 +204,7 @@ __device__ __forceinline__ void blk_load_scales(const BlkParams& p, int first, i
           va[u][i] = in && r < tile.rows ? __ldg(p.sa + static_cast<size_t>(kb + u) * p.rows + tile.row0 + r) : 0.f;
         }
       }
-      if (!__all_sync(0xFFFFFFFFu, ptx::mbar_wait(ptx::smem_u32(&sc_empty[slot]), slot_phase ^ 1u, abort_flag))) {
-        if ((idx & 31) == 0) blk_timeout(p, 3);
-        return;
-      }
+      ptx::mbar_wait_or_flag(ptx::smem_u32(&sc_empty[slot]), slot_phase ^ 1u, abort_flag, kRoleScale);
       float* f = s_scale + slot * kScaleBatch * 2 * kMaxN;
 #pragma unroll
       for (int u = 0; u < kScaleBatch; ++u)
@@ -309,27 +309,22 @@ gemm_blk_swapped(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
   if (warp < 4) {
     ptx::setmaxnreg_dec<48>();
     if (warp == 0) {
-      // ---------------------------------------------------------------- TMA producer
-      if (lane == 0) {
-        int stage = 0;
-        uint32_t phase = 0;
-        bool ok = true;
-        const uint64_t pol_first = ptx::l2_policy_evict_first(), pol_last = ptx::l2_policy_evict_last();
-        for (int t = first; ok && t < total_tiles; t += step) {
-          const BlkTile tile = blk_decode<kGated, kMaxN>(t, prefix, offs, p);
-          const int w_row = tile.group * p.N + tile.n0;
-          // the second box: the up rows of the same columns, or the next 128 columns where there are any
-          const bool second = kGated || tile.n0 + BW < p.N;
-          const uint32_t bytes = (second ? 2 : 1) * kWBoxBytes + tile.n_pad * BK;
-          const uint64_t pol_w = tile.single ? pol_first : pol_last;   // weights another tile reads again stay in L2
-          for (int kb = kb0; kb < kb1; ++kb) {
-            if (!ptx::mbar_wait(ptx::smem_u32(&st->empty[stage]), phase ^ 1u, abort_flag)) {
-              blk_timeout(p, 1);
-              ok = false;
-              break;
-            }
-            const uint32_t full = ptx::smem_u32(&st->full[stage]);
-            const uint32_t s = ring_u32 + stage * kStageBytes;
+      // ---------------------------------------------------------------- TMA producer (whole warp, one lane issues)
+      int stage = 0;
+      uint32_t phase = 1;
+      const uint64_t pol_first = ptx::l2_policy_evict_first(), pol_last = ptx::l2_policy_evict_last();
+      for (int t = first; t < total_tiles; t += step) {
+        const BlkTile tile = blk_decode<kGated, kMaxN>(t, prefix, offs, p);
+        const int w_row = tile.group * p.N + tile.n0;
+        // the second box: the up rows of the same columns, or the next 128 columns where there are any
+        const bool second = kGated || tile.n0 + BW < p.N;
+        const uint32_t bytes = (second ? 2 : 1) * kWBoxBytes + tile.n_pad * BK;
+        const uint64_t pol_w = tile.single ? pol_first : pol_last;   // weights another tile reads again stay in L2
+        for (int kb = kb0; kb < kb1; ++kb) {
+          ptx::mbar_wait_or_flag(ptx::smem_u32(&st->empty[stage]), phase, abort_flag, kRoleTma);
+          const uint32_t full = ptx::smem_u32(&st->full[stage]);
+          const uint32_t s = ring_u32 + stage * kStageBytes;
+          if (ptx::elect_one()) {
             ptx::mbar_expect_tx(full, bytes);
             ptx::tma_load_2d_hint(s, &tm_b0, full, kb * BK, w_row, pol_w);
             if (second)
@@ -337,46 +332,48 @@ gemm_blk_swapped(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
                                     pol_w);
             for (int r = 0; r < tile.n_pad; r += kRowBox)
               ptx::tma_load_2d_hint(s + 2 * kWBoxBytes + r * BK, &tm_a, full, kb * BK, tile.row0 + r, pol_last);
-            if (++stage == p.stages) { stage = 0; phase ^= 1u; }
-          }
-        }
-      }
-      __syncwarp();
-    } else if (warp == 1) {
-      // ---------------------------------------------------------------- MMA issuer
-      // The whole warp runs the loop and one elected lane issues: with the loop's values warp-uniform the operands are in
-      // the registers the MMA reads them from, and issuing four costs half as much as from a single-lane branch.
-      int stage = 0, buf = 0;
-      uint32_t phase = 0, buf_phase = 1;
-      bool ok = true;
-      for (int t = first; ok && t < total_tiles; t += step) {
-        const uint32_t idesc = ptx::idesc_e4m3_f32(BW, blk_decode<kGated, kMaxN>(t, prefix, offs, p).n_pad);
-        for (int kb = kb0; kb < kb1; ++kb) {
-          if (!ptx::mbar_wait_warp(ptx::smem_u32(&st->full[stage]), phase, abort_flag) ||
-              !ptx::mbar_wait_warp(ptx::smem_u32(&st->acc_empty[buf]), buf_phase, abort_flag)) {
-            if (lane == 0) blk_timeout(p, 2);
-            ok = false;
-            break;
-          }
-          ptx::tc_fence_after_sync();
-          const uint32_t s = ring_u32 + stage * kStageBytes;
-          const uint64_t w0 = ptx::smem_desc_sw128(s), w1 = ptx::smem_desc_sw128(s + kWBoxBytes);
-          const uint64_t a = ptx::smem_desc_sw128(s + 2 * kWBoxBytes);
-          const uint32_t d = tmem_base + static_cast<uint32_t>(buf * kTmemBuf);
-          if (ptx::elect_one()) {
-#pragma unroll
-            for (int k4 = 0; k4 < BK / UMMA_K; ++k4) {
-              const uint64_t adv = static_cast<uint64_t>(2 * k4);      // +32 bytes along K inside the swizzle row
-              ptx::tc_mma_e4m3(d, w0 + adv, a + adv, idesc, k4 != 0 ? 1u : 0u);
-              ptx::tc_mma_e4m3(d + BW, w1 + adv, a + adv, idesc, k4 != 0 ? 1u : 0u);
-            }
-            ptx::tc_commit(ptx::smem_u32(&st->empty[stage]));
-            ptx::tc_commit(ptx::smem_u32(&st->acc_full[buf]));
           }
           __syncwarp();
           if (++stage == p.stages) { stage = 0; phase ^= 1u; }
-          buf ^= 1;
-          buf_phase ^= buf == 0 ? 1u : 0u;
+        }
+        if (__any_sync(0xFFFFFFFFu, *abort_flag)) break;
+      }
+    } else if (warp != 2) {
+      // ---------------------------------------------------------------- MMA issuers: warp 1 even blocks of K, warp 3 odd
+      // A block's two waits, MMAs and commits are a chain of 450 to 700 clocks for the issuing warp, more while the
+      // epilogue's sums share its scheduler; blocks accumulate apart, so two warps take them in turn.  Each runs its loop
+      // as a whole and one elected lane issues: with warp-uniform values the operands already are in the registers the
+      // MMA reads them from, which halves the cost against a single-lane branch.
+      const int odd = warp >> 1;
+      int stage = 0, next = 0;                     // ring position, and which issuer takes it
+      uint32_t phase = 0, buf_phase = 1;
+      const uint32_t d = tmem_base + static_cast<uint32_t>(odd * kTmemBuf);
+      for (int t = first; t < total_tiles; t += step) {
+        if (__any_sync(0xFFFFFFFFu, *abort_flag)) break;
+        const uint32_t idesc = ptx::idesc_e4m3_f32(BW, blk_decode<kGated, kMaxN>(t, prefix, offs, p).n_pad);
+        for (int kb = kb0; kb < kb1; ++kb) {
+          if (next == odd) {
+            ptx::mbar_wait_or_flag(ptx::smem_u32(&st->acc_empty[odd]), buf_phase, abort_flag, kRoleMma);
+            ptx::mbar_wait_or_flag(ptx::smem_u32(&st->full[stage]), phase, abort_flag, kRoleMma);
+            buf_phase ^= 1u;
+            ptx::tc_fence_after_sync();
+            const uint32_t s = ring_u32 + stage * kStageBytes;
+            const uint64_t w0 = ptx::smem_desc_sw128(s), w1 = ptx::smem_desc_sw128(s + kWBoxBytes);
+            const uint64_t a = ptx::smem_desc_sw128(s + 2 * kWBoxBytes);
+            if (ptx::elect_one()) {
+#pragma unroll
+              for (int k4 = 0; k4 < BK / UMMA_K; ++k4) {
+                const uint64_t adv = static_cast<uint64_t>(2 * k4);    // +32 bytes along K inside the swizzle row
+                ptx::tc_mma_e4m3(d, w0 + adv, a + adv, idesc, k4 != 0 ? 1u : 0u);
+                ptx::tc_mma_e4m3(d + BW, w1 + adv, a + adv, idesc, k4 != 0 ? 1u : 0u);
+              }
+              ptx::tc_commit(ptx::smem_u32(&st->empty[stage]));
+              ptx::tc_commit(ptx::smem_u32(&st->acc_full[odd]));
+            }
+            __syncwarp();
+          }
+          next ^= 1;
+          if (++stage == p.stages) { stage = 0; phase ^= 1u; }
         }
       }
     } else {
@@ -385,7 +382,7 @@ gemm_blk_swapped(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
         const BlkTile tile = blk_decode<kGated, kMaxN>(t, prefix, offs, p);
         return ScaleRows{tile.row0, tile.rows, tile.n0, tile.group};
       };
-      blk_load_scales<kGated, kMaxN>(p, first, step, total_tiles, kb0, kb1, tid - 64, s_scale, st->sc_full, st->sc_empty,
+      blk_load_scales<kGated, kMaxN>(p, first, step, total_tiles, kb0, kb1, lane, s_scale, st->sc_full, st->sc_empty,
                                      abort_flag, decode);
     }
     if (p.split > 1) {
@@ -400,23 +397,14 @@ gemm_blk_swapped(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
     const int half = (warp - 4) >> 2;             // half of the tile's rows of a
     int buf = 0, slot = 0;
     uint32_t buf_phase = 0, slot_phase = 0, out_phase = 0;
-    bool ok = true;
     BlkTile tile{};
-    // one verdict for the warp: lanes that gave up must not part from lanes that did not
-    auto all_wait = [&](uint32_t bar, uint32_t parity) -> bool {
-      return __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar, parity, abort_flag));
-    };
     // the four warps of a half meet (a bounded wait: a plain barrier would hang on a warp that gave up)
-    auto meet = [&]() -> bool {
+    auto meet = [&]() {
       const uint32_t bar = ptx::smem_u32(&st->out_sync[half]);
       __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(bar);
-      if (!all_wait(bar, out_phase)) {
-        if (lane == 0) blk_timeout(p, 5);
-        ok = false;
-      }
+      ptx::mbar_arrive_if(bar, lane == 0);
+      ptx::mbar_wait_or_flag(bar, out_phase, abort_flag, kRoleEpilogue);
       out_phase ^= 1u;
-      return ok;
     };
     // the running sums of one tile, then the tile's end
     auto run = [&](auto tag) {
@@ -426,19 +414,11 @@ gemm_blk_swapped(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
       for (int i = 0; i < kCols; ++i) acc[0][i] = acc[1][i] = 0.f;
       const uint32_t t_lane = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(half * kCols);
       for (int kb = kb0; kb < kb1; kb += kScaleBatch) {
-        if (!all_wait(ptx::smem_u32(&st->sc_full[slot]), slot_phase)) {
-          if (lane == 0) blk_timeout(p, 4);
-          ok = false;
-          return;
-        }
+        ptx::mbar_wait_or_flag(ptx::smem_u32(&st->sc_full[slot]), slot_phase, abort_flag, kRoleEpilogue);
         const float* f = s_scale + slot * kScaleBatch * 2 * kMaxN + half * kCols;
         const int batch = min(kScaleBatch, kb1 - kb);
         for (int u = 0; u < batch; ++u, f += 2 * kMaxN) {
-          if (!all_wait(ptx::smem_u32(&st->acc_full[buf]), buf_phase)) {
-            if (lane == 0) blk_timeout(p, 4);
-            ok = false;
-            return;
-          }
+          ptx::mbar_wait_or_flag(ptx::smem_u32(&st->acc_full[buf]), buf_phase, abort_flag, kRoleEpilogue);
           ptx::tc_fence_after_sync();
           const uint32_t ta = t_lane + static_cast<uint32_t>(buf * kTmemBuf);
           constexpr int kChunk = kCols < 16 ? kCols : 16;
@@ -473,7 +453,7 @@ gemm_blk_swapped(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
         for (int i = 0; i < kOutTokens; ++i)
 #pragma unroll
           for (int b = 0; b < 2; ++b) mine[i * 256 + b * BW + quarter * 32 + lane] = acc[b][c + i];
-        if (!meet()) return;
+        meet();
 #pragma unroll
         for (int i = 0; i < kOutTokens / 4; ++i) {
           const int j = quarter * (kOutTokens / 4) + i, r = half * kCols + c + j;
@@ -483,10 +463,11 @@ gemm_blk_swapped(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
             blk_finish_row<kGated>(p, tile.row0 + r, tile.n0, lane, a, b);
           }
         }
-        if (!meet()) return;
+        meet();
       }
     };
-    for (int t = first; ok && t < total_tiles; t += step) {
+    for (int t = first; t < total_tiles; t += step) {
+      if (__any_sync(0xFFFFFFFFu, *abort_flag)) break;
       tile = blk_decode<kGated, kMaxN>(t, prefix, offs, p);
       switch (tile.n_pad) {
         case 16: run(std::integral_constant<int, 8>{}); break;
@@ -500,7 +481,7 @@ gemm_blk_swapped(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
     if (p.split > 1) {
       __syncwarp();
       ptx::cluster_sync();
-      if (ok && first < total_tiles) {
+      if (first < total_tiles) {
         // each CTA finishes every split-th row, its eight epilogue warps in turn; partial sums in rank order
         for (int r = rank + p.split * (warp - 4); r < tile.rows; r += p.split * (kEpilogueThreads / 32)) {
           float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
@@ -520,6 +501,7 @@ gemm_blk_swapped(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
 
   __syncthreads();
   if (st->abort_flag) {
+    if (tid == 0) blk_report(p, st->abort_flag);
     // a wait gave up: give copies still in flight time to land before the shared memory is released
     for (int i = 0; i < 2000; ++i) __nanosleep(1000);
     __syncthreads();
@@ -589,7 +571,8 @@ __device__ __forceinline__ PairTile pair_decode(int t, int rank, const int32_t* 
 
 template <bool kGated>
 __global__ void __launch_bounds__(kThreads, 1)
-gemm_blk_pair(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b0,
+gemm_blk_pair(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_a32,
+              const __grid_constant__ CUtensorMap tm_b0,
               const __grid_constant__ CUtensorMap tm_b1, const __grid_constant__ CUtensorMap tm_y, const BlkParams p) {
   extern __shared__ unsigned char smem_raw[];
   const uint32_t raw = ptx::smem_u32(smem_raw);
@@ -630,6 +613,7 @@ gemm_blk_pair(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ 
     blk_prefixes(p, kPairRows, prefix, offs, lane);
     if (lane == 0) {
       ptx::prefetch_tensormap(&tm_a);
+      ptx::prefetch_tensormap(&tm_a32);
       ptx::prefetch_tensormap(rank == 0 ? &tm_b0 : &tm_b1);
     }
   }
@@ -649,69 +633,70 @@ gemm_blk_pair(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ 
   if (warp < 4) {
     ptx::setmaxnreg_dec<48>();
     if (warp == 0) {
-      // ---------------------------------------------------------------- TMA producer (both CTAs)
-      if (lane == 0) {
-        int stage = 0;
-        uint32_t phase = 0;
-        bool ok = true;
-        const uint64_t pol_first = ptx::l2_policy_evict_first(), pol_last = ptx::l2_policy_evict_last();
-        const CUtensorMap* mb = rank == 0 ? &tm_b0 : &tm_b1;
-        for (int t = first; ok && t < total_tiles; t += step) {
-          const PairTile tile = pair_decode<kGated>(t, rank, prefix, offs, p);
-          // the leader's box: gate rows, or the tile's first 128 columns; the peer's: up rows, or the next 128 (what
-          // lies beyond N is computed and not stored; beyond the last group it reads as zero)
-          const int w_row = tile.group * p.N + tile.n0 + (kGated ? 0 : rank * BW);
-          const uint64_t pol_w = tile.single ? pol_first : pol_last;
-          const int my_rows = (max(tile.rows, 0) + kPairRowBox - 1) / kPairRowBox * kPairRowBox;
-          const int peer_rows = (max(tile.peer_rows, 0) + kPairRowBox - 1) / kPairRowBox * kPairRowBox;
-          for (int kb = 0; kb < p.k_blocks; ++kb) {
-            if (!ptx::mbar_wait(ptx::smem_u32(&st->empty[stage]), phase ^ 1u, abort_flag)) {
-              blk_timeout(p, 6);
-              ok = false;
-              break;
-            }
-            const uint32_t full = ptx::smem_u32(&st->full[stage]);
-            const uint32_t full_leader = ptx::map_to_cta(full, 0);
-            const uint32_t s = ring_u32 + stage * kPairStageBytes;
-            if (rank == 0) ptx::mbar_expect_tx(full, 2 * kWBoxBytes + (my_rows + peer_rows) * BK);   // both CTAs' bytes
+      // ---------------------------------------------------------------- TMA producer (both CTAs; whole warp, one lane issues)
+      int stage = 0;
+      uint32_t phase = 1;
+      const uint64_t pol_first = ptx::l2_policy_evict_first(), pol_last = ptx::l2_policy_evict_last();
+      const CUtensorMap* mb = rank == 0 ? &tm_b0 : &tm_b1;
+      for (int t = first; t < total_tiles; t += step) {
+        const PairTile tile = pair_decode<kGated>(t, rank, prefix, offs, p);
+        // the leader's box: gate rows, or the tile's first 128 columns; the peer's: up rows, or the next 128 (what
+        // lies beyond N is computed and not stored; beyond the last group it reads as zero)
+        const int w_row = tile.group * p.N + tile.n0 + (kGated ? 0 : rank * BW);
+        const uint64_t pol_w = tile.single ? pol_first : pol_last;
+        // rows of a: one copy of 128, or as many of 32 as hold rows (each copy costs the issuing lane about 100 clocks)
+        const int my_rows = (max(tile.rows, 0) + kPairRowBox - 1) / kPairRowBox * kPairRowBox;
+        const int peer_rows = (max(tile.peer_rows, 0) + kPairRowBox - 1) / kPairRowBox * kPairRowBox;
+        const uint32_t bytes = 2 * kWBoxBytes + (my_rows + peer_rows) * BK;                  // of both CTAs
+        for (int kb = 0; kb < p.k_blocks; ++kb) {
+          ptx::mbar_wait_or_flag(ptx::smem_u32(&st->empty[stage]), phase, abort_flag, kRoleTma);
+          const uint32_t full = ptx::smem_u32(&st->full[stage]);
+          const uint32_t full_leader = ptx::map_to_cta(full, 0);
+          const uint32_t s = ring_u32 + stage * kPairStageBytes;
+          if (ptx::elect_one()) {
+            if (rank == 0) ptx::mbar_expect_tx(full, bytes);
             ptx::tma_load_2d_pair_hint(s + BW * BK, mb, full_leader, kb * BK, w_row, pol_w);
-            for (int r = 0; r < my_rows; r += kPairRowBox)
-              ptx::tma_load_2d_pair_hint(s + r * BK, &tm_a, full_leader, kb * BK, tile.row0 + r, pol_last);
-            if (++stage == kPairStages) { stage = 0; phase ^= 1u; }
+            if (my_rows == BW) {
+              ptx::tma_load_2d_pair_hint(s, &tm_a, full_leader, kb * BK, tile.row0, pol_last);
+            } else {
+              for (int r = 0; r < my_rows; r += kPairRowBox)
+                ptx::tma_load_2d_pair_hint(s + r * BK, &tm_a32, full_leader, kb * BK, tile.row0 + r, pol_last);
+            }
           }
+          __syncwarp();
+          if (++stage == kPairStages) { stage = 0; phase ^= 1u; }
         }
+        if (__any_sync(0xFFFFFFFFu, *abort_flag)) break;
       }
-      __syncwarp();
-    } else if (warp == 1) {
-      // ---------------------------------------------------------------- MMA issuer (leader only; whole warp, see above)
+    } else if (warp != 2) {
+      // ---------------------------------------------------------------- MMA issuers of the leader (two warps in turn, as above)
       if (rank == 0) {
         constexpr uint32_t idesc = ptx::idesc_e4m3_f32(kPairRows, 2 * BW);
-        int stage = 0, buf = 0;
+        const int odd = warp >> 1;
+        int stage = 0, next = 0;
         uint32_t phase = 0, buf_phase = 1;
-        bool ok = true;
-        for (int t = first; ok && t < total_tiles; t += step) {
+        const uint32_t d = tmem_base + static_cast<uint32_t>(odd * kTmemBuf);
+        for (int t = first; t < total_tiles; t += step) {
+          if (__any_sync(0xFFFFFFFFu, *abort_flag)) break;
           for (int kb = 0; kb < p.k_blocks; ++kb) {
-            if (!ptx::mbar_wait_warp(ptx::smem_u32(&st->full[stage]), phase, abort_flag) ||
-                !ptx::mbar_wait_warp(ptx::smem_u32(&st->acc_empty[buf]), buf_phase, abort_flag)) {
-              if (lane == 0) blk_timeout(p, 7);
-              ok = false;
-              break;
-            }
-            ptx::tc_fence_after_sync();
-            const uint32_t s = ring_u32 + stage * kPairStageBytes;
-            const uint64_t a = ptx::smem_desc_sw128(s), b = ptx::smem_desc_sw128(s + BW * BK);
-            const uint32_t d = tmem_base + static_cast<uint32_t>(buf * kTmemBuf);
-            if (ptx::elect_one()) {
+            if (next == odd) {
+              ptx::mbar_wait_or_flag(ptx::smem_u32(&st->acc_empty[odd]), buf_phase, abort_flag, kRoleMma);
+              ptx::mbar_wait_or_flag(ptx::smem_u32(&st->full[stage]), phase, abort_flag, kRoleMma);
+              buf_phase ^= 1u;
+              ptx::tc_fence_after_sync();
+              const uint32_t s = ring_u32 + stage * kPairStageBytes;
+              const uint64_t a = ptx::smem_desc_sw128(s), b = ptx::smem_desc_sw128(s + BW * BK);
+              if (ptx::elect_one()) {
 #pragma unroll
-              for (int k4 = 0; k4 < BK / UMMA_K; ++k4)
-                ptx::tc_mma_e4m3_pair(d, a + 2 * k4, b + 2 * k4, idesc, k4 != 0 ? 1u : 0u);
-              ptx::tc_commit_pair(ptx::smem_u32(&st->empty[stage]), 3);    // in both CTAs
-              ptx::tc_commit_pair(ptx::smem_u32(&st->acc_full[buf]), 3);
+                for (int k4 = 0; k4 < BK / UMMA_K; ++k4)
+                  ptx::tc_mma_e4m3_pair(d, a + 2 * k4, b + 2 * k4, idesc, k4 != 0 ? 1u : 0u);
+                ptx::tc_commit_pair(ptx::smem_u32(&st->empty[stage]), 3);    // in both CTAs
+                ptx::tc_commit_pair(ptx::smem_u32(&st->acc_full[odd]), 3);
+              }
+              __syncwarp();
             }
-            __syncwarp();
+            next ^= 1;
             if (++stage == kPairStages) { stage = 0; phase ^= 1u; }
-            buf ^= 1;
-            buf_phase ^= buf == 0 ? 1u : 0u;
           }
         }
       }
@@ -721,7 +706,7 @@ gemm_blk_pair(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ 
         const PairTile tile = pair_decode<kGated>(t, rank, prefix, offs, p);
         return ScaleRows{tile.row0, tile.rows, tile.n0, tile.group};
       };
-      blk_load_scales<kGated, BW>(p, first, step, total_tiles, 0, p.k_blocks, tid - 64, s_scale, st->sc_full, st->sc_empty,
+      blk_load_scales<kGated, BW>(p, first, step, total_tiles, 0, p.k_blocks, lane, s_scale, st->sc_full, st->sc_empty,
                                   abort_flag, decode);
     }
   } else {
@@ -734,30 +719,21 @@ gemm_blk_pair(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ 
     const uint32_t empty1 = ptx::map_to_cta(ptx::smem_u32(&st->acc_empty[1]), 0);
     int buf = 0, slot = 0, parity = 0;
     uint32_t buf_phase = 0, slot_phase = 0, row_phase = 0;
-    bool ok = true;
-    auto all_wait = [&](uint32_t bar, uint32_t phase) -> bool {
-      return __all_sync(0xFFFFFFFFu, ptx::mbar_wait(bar, phase, abort_flag));
-    };
-    for (int t = first; ok && t < total_tiles; t += step) {
+    for (int t = first; t < total_tiles; t += step) {
+      if (__any_sync(0xFFFFFFFFu, *abort_flag)) break;
       const PairTile tile = pair_decode<kGated>(t, rank, prefix, offs, p);
       const bool live = quarter * 32 < tile.rows;           // any row of this warp
       // columns half * 64 .. + 63 of each weight box: sums 0..63 of the first box, 64..127 of the second
       float acc[128];
 #pragma unroll
       for (int i = 0; i < 128; ++i) acc[i] = 0.f;
-      for (int kb = 0; ok && kb < p.k_blocks; kb += kScaleBatch) {
-        if (!all_wait(ptx::smem_u32(&st->sc_full[slot]), slot_phase)) {
-          ok = false;
-          break;
-        }
+      for (int kb = 0; kb < p.k_blocks; kb += kScaleBatch) {
+        ptx::mbar_wait_or_flag(ptx::smem_u32(&st->sc_full[slot]), slot_phase, abort_flag, kRoleEpilogue);
         const float* f = s_scale + slot * kScaleBatch * 2 * BW + r_tile;
         const int batch = min(kScaleBatch, p.k_blocks - kb);
         for (int u = 0; u < batch; ++u, f += 2 * BW) {
           const float s0 = f[0], s1 = f[BW];
-          if (!all_wait(ptx::smem_u32(&st->acc_full[buf]), buf_phase)) {
-            ok = false;
-            break;
-          }
+          ptx::mbar_wait_or_flag(ptx::smem_u32(&st->acc_full[buf]), buf_phase, abort_flag, kRoleEpilogue);
           ptx::tc_fence_after_sync();
           const uint32_t empty = buf == 0 ? empty0 : empty1;
           if (live) {
@@ -786,10 +762,6 @@ gemm_blk_pair(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ 
         ptx::mbar_arrive_if(ptx::smem_u32(&st->sc_empty[slot]), lane == 0);
         if (++slot == kScaleSlots) { slot = 0; slot_phase ^= 1u; }
       }
-      if (!ok) {
-        if (lane == 0) blk_timeout(p, 8);
-        break;
-      }
       const int row = tile.row0 + r_tile;
       const bool row_ok = r_tile < tile.rows;
       if constexpr (kGated) {
@@ -804,11 +776,7 @@ gemm_blk_pair(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ 
         __syncwarp();
         const uint32_t bar = ptx::smem_u32(&st->row_sync[quarter]);
         if (lane == 0) ptx::mbar_arrive(bar);
-        if (!all_wait(bar, row_phase)) {
-          if (lane == 0) blk_timeout(p, 9);
-          ok = false;
-          break;
-        }
+        ptx::mbar_wait_or_flag(bar, row_phase, abort_flag, kRoleEpilogue);
         row_phase ^= 1u;
         amax = fmaxf(amax, st->amax[parity][half ^ 1][r_tile]);
         parity ^= 1;
@@ -873,6 +841,7 @@ gemm_blk_pair(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ 
 
   __syncthreads();
   if (st->abort_flag) {
+    if (tid == 0) blk_report(p, st->abort_flag);
     for (int i = 0; i < 2000; ++i) __nanosleep(1000);
     __syncthreads();
   }
@@ -941,8 +910,9 @@ moe_status launch_swapped(moe_ctx* ctx, const BlkProduct& g, BlkParams p, cudaSt
 template <bool kGated>
 moe_status launch_pair(moe_ctx* ctx, const BlkProduct& g, const BlkParams& p, cudaStream_t stream) {
   const uint64_t w_rows = static_cast<uint64_t>(p.groups) * p.N;
-  CUtensorMap tm_a, tm_b0, tm_b1, tm_y;
-  if (encode_bytes(ctx, &tm_a, g.a, p.rows, g.K, kPairRowBox) != CUDA_SUCCESS ||
+  CUtensorMap tm_a, tm_a32, tm_b0, tm_b1, tm_y;
+  if (encode_bytes(ctx, &tm_a, g.a, p.rows, g.K, BW) != CUDA_SUCCESS ||
+      encode_bytes(ctx, &tm_a32, g.a, p.rows, g.K, kPairRowBox) != CUDA_SUCCESS ||
       encode_bytes(ctx, &tm_b0, g.b0, w_rows, g.K, BW) != CUDA_SUCCESS ||
       encode_bytes(ctx, &tm_b1, kGated ? g.b1 : g.b0, w_rows, g.K, BW) != CUDA_SUCCESS)
     return MOE_ERR_CUDA;
@@ -974,7 +944,7 @@ moe_status launch_pair(moe_ctx* ctx, const BlkProduct& g, const BlkParams& p, cu
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   ctx->last_launches += 1;
-  return cudaLaunchKernelEx(&cfg, gemm_blk_pair<kGated>, tm_a, tm_b0, tm_b1, tm_y, p) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, gemm_blk_pair<kGated>, tm_a, tm_a32, tm_b0, tm_b1, tm_y, p) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
 template <bool kGated>

@@ -90,9 +90,22 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   }
 }
 
-// The same for a converged warp, with one verdict for all its lanes.
-__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  return __any_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag));
+// The same without a verdict, for the inner loops of a whole warp: a wait that gives up raises the flag (to `role`) and
+// returns like one that succeeded, and so do all later ones, at once.  No lane parts from its warp, and nothing has to be
+// voted on per wait; the caller looks at the flag once per tile, and what was computed since is void.
+__device__ __forceinline__ void mbar_wait_or_flag(uint32_t bar, uint32_t parity, volatile int* abort_flag, int role) {
+  if (mbar_try_wait(bar, parity)) return;
+  const long long t0 = clock64();
+  for (uint32_t it = 1;; ++it) {
+    if (mbar_try_wait(bar, parity)) return;
+    if ((it & 0xFu) == 0) {
+      if (*abort_flag) return;
+      if (clock64() - t0 > kWaitClockBudget) {
+        *abort_flag = role;
+        return;
+      }
+    }
+  }
 }
 
 // Same, adding the clocks spent waiting (zero when the phase had already completed) to *waited.
