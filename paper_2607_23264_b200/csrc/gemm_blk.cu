@@ -32,7 +32,6 @@ constexpr int BW = 128;                  // rows of one weight box (M of an MMA)
 constexpr int BK = 128;                  // K elements (= bytes) per block: one 128-byte swizzle row, one scale
 constexpr int UMMA_K = 32;
 constexpr int kWBoxBytes = BW * BK;
-constexpr int kRowBox = 16;              // rows of a per TMA box
 constexpr int kMaxStages = 6;
 constexpr int kScaleSlots = 2;           // scale ring: slots of kScaleBatch blocks of K each
 constexpr int kScaleBatch = 4;
@@ -62,6 +61,16 @@ struct BlkParams {
   float* h_dbg;             // gated: optional fp32 [rows, N]
   int32_t* status;
 };
+
+// The rows of a, as boxes of each height a tile can have: one copy per block of K whatever the height (a copy costs the
+// issuing warp about 100 clocks, and eight copies of 16 rows were what bound tiles of 128).
+constexpr int kHeights = 5;
+struct RowMaps {
+  CUtensorMap of[kHeights];   // 16, 32, 64, 96, 128 rows
+};
+__host__ __device__ constexpr int blk_height(int i) { return i == 0 ? 16 : 32 * (i < 3 ? i : i < 4 ? 3 : 4); }
+static_assert(blk_height(0) == 16 && blk_height(1) == 32 && blk_height(2) == 64 && blk_height(3) == 96 && blk_height(4) == 128, "");
+__device__ __forceinline__ int blk_height_index(int rows) { return rows <= 16 ? 0 : rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 96 ? 3 : 4; }
 
 struct BlkTail {
   uint64_t full[kMaxStages];
@@ -107,8 +116,7 @@ __device__ __forceinline__ BlkTile blk_decode(int t, const int32_t* prefix, cons
   BlkTile tile;
   tile.row0 = offs[2 * lo] + mb * per;
   tile.rows = max(0, min(per, rows - mb * per));
-  const int n = tile.rows;
-  tile.n_pad = n <= 16 ? 16 : n <= 32 ? 32 : n <= 64 ? 64 : n <= 96 ? 96 : 128;
+  tile.n_pad = blk_height(blk_height_index(tile.rows));
   tile.n0 = nb * (kGated ? BW : 2 * BW);
   tile.group = lo;
   tile.single = blocks == 1 ? 1 : 0;
@@ -246,7 +254,7 @@ __device__ __forceinline__ void blk_add_cols(uint32_t taddr, const float* f, flo
 
 template <bool kGated, int kMaxN>
 __global__ void __launch_bounds__(kThreads, 1)
-gemm_blk_swapped(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b0,
+gemm_blk_swapped(const __grid_constant__ RowMaps tm_a, const __grid_constant__ CUtensorMap tm_b0,
                  const __grid_constant__ CUtensorMap tm_b1, const BlkParams p) {
   constexpr int kStageBytes = 2 * kWBoxBytes + kMaxN * BK;
   extern __shared__ unsigned char smem_raw[];
@@ -284,7 +292,7 @@ gemm_blk_swapped(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
   if (warp == 0) {
     blk_prefixes(p, kMaxN, prefix, offs, lane);
     if (lane == 0) {
-      ptx::prefetch_tensormap(&tm_a);
+      for (int i = 0; i < kHeights && blk_height(i) <= kMaxN; ++i) ptx::prefetch_tensormap(&tm_a.of[i]);
       ptx::prefetch_tensormap(&tm_b0);
       if (kGated) ptx::prefetch_tensormap(&tm_b1);
     }
@@ -320,6 +328,7 @@ gemm_blk_swapped(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
         const bool second = kGated || tile.n0 + BW < p.N;
         const uint32_t bytes = (second ? 2 : 1) * kWBoxBytes + tile.n_pad * BK;
         const uint64_t pol_w = tile.single ? pol_first : pol_last;   // weights another tile reads again stay in L2
+        const CUtensorMap* ma = &tm_a.of[blk_height_index(tile.rows)];
         for (int kb = kb0; kb < kb1; ++kb) {
           ptx::mbar_wait_or_flag(ptx::smem_u32(&st->empty[stage]), phase, abort_flag, kRoleTma);
           const uint32_t full = ptx::smem_u32(&st->full[stage]);
@@ -330,8 +339,7 @@ gemm_blk_swapped(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
             if (second)
               ptx::tma_load_2d_hint(s + kWBoxBytes, kGated ? &tm_b1 : &tm_b0, full, kb * BK, kGated ? w_row : w_row + BW,
                                     pol_w);
-            for (int r = 0; r < tile.n_pad; r += kRowBox)
-              ptx::tma_load_2d_hint(s + 2 * kWBoxBytes + r * BK, &tm_a, full, kb * BK, tile.row0 + r, pol_last);
+            ptx::tma_load_2d_hint(s + 2 * kWBoxBytes, ma, full, kb * BK, tile.row0, pol_last);
           }
           __syncwarp();
           if (++stage == p.stages) { stage = 0; phase ^= 1u; }
@@ -522,7 +530,6 @@ gemm_blk_swapped(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
 // no cluster-wide release (300 clocks more), the loads from tensor memory have completed before them and there is nothing
 // else to publish.
 constexpr int kPairRows = 256;
-constexpr int kPairRowBox = 32;          // rows of a per TMA box
 constexpr int kPairStages = 5;
 constexpr int kPairStageBytes = BW * BK + kWBoxBytes;
 constexpr int kStoreBoxCols = 64;        // output box of a warp: 32 rows x 64 bf16 columns (128 bytes, swizzled)
@@ -571,8 +578,7 @@ __device__ __forceinline__ PairTile pair_decode(int t, int rank, const int32_t* 
 
 template <bool kGated>
 __global__ void __launch_bounds__(kThreads, 1)
-gemm_blk_pair(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_a32,
-              const __grid_constant__ CUtensorMap tm_b0,
+gemm_blk_pair(const __grid_constant__ RowMaps tm_a, const __grid_constant__ CUtensorMap tm_b0,
               const __grid_constant__ CUtensorMap tm_b1, const __grid_constant__ CUtensorMap tm_y, const BlkParams p) {
   extern __shared__ unsigned char smem_raw[];
   const uint32_t raw = ptx::smem_u32(smem_raw);
@@ -612,8 +618,7 @@ gemm_blk_pair(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ 
   if (warp == 0) {
     blk_prefixes(p, kPairRows, prefix, offs, lane);
     if (lane == 0) {
-      ptx::prefetch_tensormap(&tm_a);
-      ptx::prefetch_tensormap(&tm_a32);
+      for (int i = 0; i < kHeights; ++i) ptx::prefetch_tensormap(&tm_a.of[i]);
       ptx::prefetch_tensormap(rank == 0 ? &tm_b0 : &tm_b1);
     }
   }
@@ -644,9 +649,9 @@ gemm_blk_pair(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ 
         // lies beyond N is computed and not stored; beyond the last group it reads as zero)
         const int w_row = tile.group * p.N + tile.n0 + (kGated ? 0 : rank * BW);
         const uint64_t pol_w = tile.single ? pol_first : pol_last;
-        // rows of a: one copy of 128, or as many of 32 as hold rows (each copy costs the issuing lane about 100 clocks)
-        const int my_rows = (max(tile.rows, 0) + kPairRowBox - 1) / kPairRowBox * kPairRowBox;
-        const int peer_rows = (max(tile.peer_rows, 0) + kPairRowBox - 1) / kPairRowBox * kPairRowBox;
+        const int my_rows = tile.rows > 0 ? blk_height(blk_height_index(tile.rows)) : 0;
+        const int peer_rows = tile.peer_rows > 0 ? blk_height(blk_height_index(tile.peer_rows)) : 0;
+        const CUtensorMap* ma = &tm_a.of[blk_height_index(tile.rows)];
         const uint32_t bytes = 2 * kWBoxBytes + (my_rows + peer_rows) * BK;                  // of both CTAs
         for (int kb = 0; kb < p.k_blocks; ++kb) {
           ptx::mbar_wait_or_flag(ptx::smem_u32(&st->empty[stage]), phase, abort_flag, kRoleTma);
@@ -656,12 +661,7 @@ gemm_blk_pair(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ 
           if (ptx::elect_one()) {
             if (rank == 0) ptx::mbar_expect_tx(full, bytes);
             ptx::tma_load_2d_pair_hint(s + BW * BK, mb, full_leader, kb * BK, w_row, pol_w);
-            if (my_rows == BW) {
-              ptx::tma_load_2d_pair_hint(s, &tm_a, full_leader, kb * BK, tile.row0, pol_last);
-            } else {
-              for (int r = 0; r < my_rows; r += kPairRowBox)
-                ptx::tma_load_2d_pair_hint(s + r * BK, &tm_a32, full_leader, kb * BK, tile.row0 + r, pol_last);
-            }
+            if (my_rows > 0) ptx::tma_load_2d_pair_hint(s, ma, full_leader, kb * BK, tile.row0, pol_last);
           }
           __syncwarp();
           if (++stage == kPairStages) { stage = 0; phase ^= 1u; }
@@ -869,11 +869,18 @@ struct BlkProduct {       // one GEMM: operands and shape
   int K;
 };
 
+bool encode_rows(moe_ctx* ctx, RowMaps* maps, const BlkProduct& g, int rows) {
+  for (int i = 0; i < kHeights; ++i)
+    if (encode_bytes(ctx, &maps->of[i], g.a, rows, g.K, blk_height(i)) != CUDA_SUCCESS) return false;
+  return true;
+}
+
 template <bool kGated, int kMaxN>
 moe_status launch_swapped(moe_ctx* ctx, const BlkProduct& g, BlkParams p, cudaStream_t stream) {
   const uint64_t w_rows = static_cast<uint64_t>(p.groups) * p.N;
-  CUtensorMap tm_a, tm_b0, tm_b1;
-  if (encode_bytes(ctx, &tm_a, g.a, p.rows, g.K, kRowBox) != CUDA_SUCCESS ||
+  RowMaps tm_a;
+  CUtensorMap tm_b0, tm_b1;
+  if (!encode_rows(ctx, &tm_a, g, p.rows) ||
       encode_bytes(ctx, &tm_b0, g.b0, w_rows, g.K, BW) != CUDA_SUCCESS ||
       encode_bytes(ctx, &tm_b1, kGated ? g.b1 : g.b0, w_rows, g.K, BW) != CUDA_SUCCESS)
     return MOE_ERR_CUDA;
@@ -910,14 +917,14 @@ moe_status launch_swapped(moe_ctx* ctx, const BlkProduct& g, BlkParams p, cudaSt
 template <bool kGated>
 moe_status launch_pair(moe_ctx* ctx, const BlkProduct& g, const BlkParams& p, cudaStream_t stream) {
   const uint64_t w_rows = static_cast<uint64_t>(p.groups) * p.N;
-  CUtensorMap tm_a, tm_a32, tm_b0, tm_b1, tm_y;
-  if (encode_bytes(ctx, &tm_a, g.a, p.rows, g.K, BW) != CUDA_SUCCESS ||
-      encode_bytes(ctx, &tm_a32, g.a, p.rows, g.K, kPairRowBox) != CUDA_SUCCESS ||
+  RowMaps tm_a;
+  CUtensorMap tm_b0, tm_b1, tm_y;
+  if (!encode_rows(ctx, &tm_a, g, p.rows) ||
       encode_bytes(ctx, &tm_b0, g.b0, w_rows, g.K, BW) != CUDA_SUCCESS ||
       encode_bytes(ctx, &tm_b1, kGated ? g.b1 : g.b0, w_rows, g.K, BW) != CUDA_SUCCESS)
     return MOE_ERR_CUDA;
   if (kGated) {
-    tm_y = tm_a;                                             // (not used)
+    tm_y = tm_b0;                                            // (not used)
   } else {
     const cuuint64_t dims[2] = {static_cast<cuuint64_t>(p.N), static_cast<cuuint64_t>(p.rows)};
     const cuuint64_t strides[1] = {static_cast<cuuint64_t>(p.N) * 2};
@@ -944,7 +951,7 @@ moe_status launch_pair(moe_ctx* ctx, const BlkProduct& g, const BlkParams& p, cu
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   ctx->last_launches += 1;
-  return cudaLaunchKernelEx(&cfg, gemm_blk_pair<kGated>, tm_a, tm_a32, tm_b0, tm_b1, tm_y, p) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, gemm_blk_pair<kGated>, tm_a, tm_b0, tm_b1, tm_y, p) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
 template <bool kGated>
