@@ -521,23 +521,28 @@ gemm_blk_swapped(const __grid_constant__ RowMaps tm_a, const __grid_constant__ C
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// Many rows per group: CTA pairs (clusters of two, cta_group::2) on tiles of 256 rows of a x 256 accumulator columns.
-// Rows are the M side here, so a thread of the epilogue owns one row and the scales are one factor per weight box.
-// Each CTA stages its 128 rows and one of the two weight boxes (32 KB per block of K: 64 bytes per clock at the tensor
-// rate, what an SM takes in from L2, where a single CTA's 128 x 256 tile would need 96), the leader issues the MMAs of
-// both, and every CTA's eight epilogue warps keep 128 running sums per thread.
+// Many rows per group: the rows of a are the M side, so a thread of the epilogue owns one row and the scales are one factor
+// per weight box (with swapped operands each column has its own, read from shared memory: at 128 rows those broadcasts
+// take as long as the sums).  Tiles of 128 rows (one CTA) or 256 (a CTA pair, cta_group::2) x 256 accumulator columns.
+// A pair's CTA stages its 128 rows and one of the two weight boxes: 32 KB per block of K, 64 bytes per clock at the tensor
+// rate, which is what an SM takes in from L2, where the single CTA's 48 KB would need 96.  A single CTA keeps twice the
+// weight bytes in flight, which is what counts while the weights come from HBM (see launch_product for the measured rule).
+// The leader issues the MMAs of both CTAs, and every CTA's eight epilogue warps keep 128 running sums per thread.
 // Tensor memory holds two blocks of K.  Handing one back crosses the pair once per block and warp: those arrivals carry
 // no cluster-wide release (300 clocks more), the loads from tensor memory have completed before them and there is nothing
 // else to publish.
-constexpr int kPairRows = 256;
-constexpr int kPairStages = 5;
-constexpr int kPairStageBytes = BW * BK + kWBoxBytes;
-constexpr int kStoreBoxCols = 64;        // output box of a warp: 32 rows x 64 bf16 columns (128 bytes, swizzled)
-constexpr int kStoreBoxBytes = 32 * kStoreBoxCols * 2;
+constexpr int kStoreCols = 32;           // output box of a warp: 32 rows x 32 bf16 columns, 64-byte swizzle
+constexpr int kStoreBoxBytes = 32 * kStoreCols * 2;
+template <int kCtas>
+struct RowGeom {
+  static constexpr int kRows = kCtas * BW;                                  // rows of a per tile
+  static constexpr int kStageBytes = BW * BK + (kCtas == 2 ? 1 : 2) * kWBoxBytes;
+  static constexpr int kStages = kCtas == 2 ? 6 : 4;                        // 192 KB
+};
 
 struct PairTail {
-  uint64_t full[kPairStages];
-  uint64_t empty[kPairStages];
+  uint64_t full[kMaxStages];
+  uint64_t empty[kMaxStages];
   uint64_t acc_full[2];
   uint64_t acc_empty[2];
   uint64_t sc_full[kScaleSlots];
@@ -554,7 +559,7 @@ struct PairTile {
   int n0, group, single;
 };
 
-template <bool kGated>
+template <bool kGated, int kCtas>
 __device__ __forceinline__ PairTile pair_decode(int t, int rank, const int32_t* prefix, const int32_t* offs,
                                                 const BlkParams& p) {
   int lo = 0, hi = p.groups;
@@ -565,45 +570,48 @@ __device__ __forceinline__ PairTile pair_decode(int t, int rank, const int32_t* 
   const int blocks = prefix[lo + 1] - prefix[lo];
   const int local = t - prefix[lo] * p.n_tiles;
   const int nb = local / blocks, mb = local - nb * blocks;
-  const int rows = offs[2 * lo + 1] - offs[2 * lo] - mb * kPairRows;     // rows from this block on
+  const int rows = offs[2 * lo + 1] - offs[2 * lo] - mb * RowGeom<kCtas>::kRows;     // rows from this block on
   PairTile tile;
-  tile.row0 = offs[2 * lo] + mb * kPairRows + rank * BW;
+  tile.row0 = offs[2 * lo] + mb * RowGeom<kCtas>::kRows + rank * BW;
   tile.rows = min(BW, rows - rank * BW);
-  tile.peer_rows = min(BW, rows - (rank ^ 1) * BW);
+  tile.peer_rows = kCtas == 2 ? min(BW, rows - (rank ^ 1) * BW) : 0;
   tile.n0 = nb * (kGated ? BW : 2 * BW);
   tile.group = lo;
   tile.single = blocks == 1 ? 1 : 0;
   return tile;
 }
 
-template <bool kGated>
+template <bool kGated, int kCtas>
 __global__ void __launch_bounds__(kThreads, 1)
-gemm_blk_pair(const __grid_constant__ RowMaps tm_a, const __grid_constant__ CUtensorMap tm_b0,
+gemm_blk_rows(const __grid_constant__ RowMaps tm_a, const __grid_constant__ CUtensorMap tm_b0,
               const __grid_constant__ CUtensorMap tm_b1, const __grid_constant__ CUtensorMap tm_y, const BlkParams p) {
+  constexpr int kStageBytes = RowGeom<kCtas>::kStageBytes;
+  const int stages = p.stages;
+  constexpr bool kPair = kCtas == 2;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t raw = ptx::smem_u32(smem_raw);
   const uint32_t pad = (1024u - (raw & 1023u)) & 1023u;
   unsigned char* base = smem_raw + pad;
   const uint32_t ring_u32 = raw + pad;
-  const uint32_t store_u32 = ring_u32 + kPairStages * kPairStageBytes;                 // one output box per epilogue warp
-  unsigned char* s_store = base + kPairStages * kPairStageBytes;
+  const uint32_t store_u32 = ring_u32 + stages * kStageBytes;                 // one output box per epilogue warp
+  unsigned char* s_store = base + stages * kStageBytes;
   float* s_scale = reinterpret_cast<float*>(s_store + kEpilogueThreads / 32 * kStoreBoxBytes);   // [kScaleSlots][kScaleBatch][2][BW]
   PairTail* st = reinterpret_cast<PairTail*>(s_scale + kScaleSlots * kScaleBatch * 2 * BW);
   int32_t* prefix = reinterpret_cast<int32_t*>(st + 1);
   int32_t* offs = prefix + p.groups + 1;
 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int rank = static_cast<int>(ptx::cluster_ctarank());            // 0 = leader
-  const int first = blockIdx.x >> 1, step = gridDim.x >> 1;
+  const int rank = kPair ? static_cast<int>(ptx::cluster_ctarank()) : 0;   // 0 = leader
+  const int first = blockIdx.x / kCtas, step = gridDim.x / kCtas;
 
   if (tid == 0) {
-    for (int s = 0; s < kPairStages; ++s) {
+    for (int s = 0; s < stages; ++s) {
       ptx::mbar_init(ptx::smem_u32(&st->full[s]), 1);
       ptx::mbar_init(ptx::smem_u32(&st->empty[s]), 1);
     }
     for (int a = 0; a < 2; ++a) {
       ptx::mbar_init(ptx::smem_u32(&st->acc_full[a]), 1);
-      ptx::mbar_init(ptx::smem_u32(&st->acc_empty[a]), 2 * kEpilogueThreads / 32);   // the warps of both CTAs
+      ptx::mbar_init(ptx::smem_u32(&st->acc_empty[a]), kCtas * kEpilogueThreads / 32);   // the warps of both CTAs
     }
     for (int s = 0; s < kScaleSlots; ++s) {
       ptx::mbar_init(ptx::smem_u32(&st->sc_full[s]), kScaleThreads);
@@ -616,19 +624,25 @@ gemm_blk_pair(const __grid_constant__ RowMaps tm_a, const __grid_constant__ CUte
     ptx::fence_proxy_async_smem();
   }
   if (warp == 0) {
-    blk_prefixes(p, kPairRows, prefix, offs, lane);
+    blk_prefixes(p, RowGeom<kCtas>::kRows, prefix, offs, lane);
     if (lane == 0) {
       for (int i = 0; i < kHeights; ++i) ptx::prefetch_tensormap(&tm_a.of[i]);
-      ptx::prefetch_tensormap(rank == 0 ? &tm_b0 : &tm_b1);
+      ptx::prefetch_tensormap(&tm_b0);
+      if (kGated) ptx::prefetch_tensormap(&tm_b1);
     }
   }
   if (warp == 1) {
-    ptx::tmem_alloc_pair(ptx::smem_u32(&st->tmem_base), kTmemCols);
-    ptx::tmem_relinquish_pair();
+    if constexpr (kPair) {
+      ptx::tmem_alloc_pair(ptx::smem_u32(&st->tmem_base), kTmemCols);
+      ptx::tmem_relinquish_pair();
+    } else {
+      ptx::tmem_alloc(ptx::smem_u32(&st->tmem_base), kTmemCols);
+      ptx::tmem_relinquish();
+    }
   }
   ptx::tc_fence_before_sync();
   __syncthreads();
-  ptx::cluster_sync();            // both CTAs' barriers exist before anything signals across the pair
+  if (kPair) ptx::cluster_sync();   // both CTAs' barriers exist before anything signals across the pair
   ptx::tc_fence_after_sync();
 
   const uint32_t tmem_base = st->tmem_base;
@@ -644,34 +658,44 @@ gemm_blk_pair(const __grid_constant__ RowMaps tm_a, const __grid_constant__ CUte
       const uint64_t pol_first = ptx::l2_policy_evict_first(), pol_last = ptx::l2_policy_evict_last();
       const CUtensorMap* mb = rank == 0 ? &tm_b0 : &tm_b1;
       for (int t = first; t < total_tiles; t += step) {
-        const PairTile tile = pair_decode<kGated>(t, rank, prefix, offs, p);
-        // the leader's box: gate rows, or the tile's first 128 columns; the peer's: up rows, or the next 128 (what
-        // lies beyond N is computed and not stored; beyond the last group it reads as zero)
-        const int w_row = tile.group * p.N + tile.n0 + (kGated ? 0 : rank * BW);
+        const PairTile tile = pair_decode<kGated, kCtas>(t, rank, prefix, offs, p);
+        // The first box: gate rows, or the tile's first 128 columns; the second: up rows, or the next 128 columns (what
+        // lies beyond N is computed and not stored; beyond the last group it reads as zero).  In a pair the leader takes
+        // the first and the peer the second.
+        const int w_row0 = tile.group * p.N + tile.n0, w_row1 = kGated ? w_row0 : w_row0 + BW;
+        const bool second = kPair || kGated || tile.n0 + BW < p.N;
         const uint64_t pol_w = tile.single ? pol_first : pol_last;
         const int my_rows = tile.rows > 0 ? blk_height(blk_height_index(tile.rows)) : 0;
         const int peer_rows = tile.peer_rows > 0 ? blk_height(blk_height_index(tile.peer_rows)) : 0;
         const CUtensorMap* ma = &tm_a.of[blk_height_index(tile.rows)];
-        const uint32_t bytes = 2 * kWBoxBytes + (my_rows + peer_rows) * BK;                  // of both CTAs
+        const uint32_t bytes = (second ? 2 : 1) * kWBoxBytes + (my_rows + peer_rows) * BK;   // of both CTAs
         for (int kb = 0; kb < p.k_blocks; ++kb) {
           ptx::mbar_wait_or_flag(ptx::smem_u32(&st->empty[stage]), phase, abort_flag, kRoleTma);
           const uint32_t full = ptx::smem_u32(&st->full[stage]);
-          const uint32_t full_leader = ptx::map_to_cta(full, 0);
-          const uint32_t s = ring_u32 + stage * kPairStageBytes;
-          if (ptx::elect_one()) {
-            if (rank == 0) ptx::mbar_expect_tx(full, bytes);
-            ptx::tma_load_2d_pair_hint(s + BW * BK, mb, full_leader, kb * BK, w_row, pol_w);
-            if (my_rows > 0) ptx::tma_load_2d_pair_hint(s, ma, full_leader, kb * BK, tile.row0, pol_last);
+          const uint32_t s = ring_u32 + stage * kStageBytes;
+          if constexpr (kPair) {
+            const uint32_t full_leader = ptx::map_to_cta(full, 0);
+            if (ptx::elect_one()) {
+              if (rank == 0) ptx::mbar_expect_tx(full, bytes);
+              ptx::tma_load_2d_pair_hint(s + BW * BK, mb, full_leader, kb * BK, rank == 0 ? w_row0 : w_row1, pol_w);
+              if (my_rows > 0) ptx::tma_load_2d_pair_hint(s, ma, full_leader, kb * BK, tile.row0, pol_last);
+            }
+          } else if (ptx::elect_one()) {
+            ptx::mbar_expect_tx(full, bytes);
+            ptx::tma_load_2d_hint(s + BW * BK, &tm_b0, full, kb * BK, w_row0, pol_w);
+            if (second)
+              ptx::tma_load_2d_hint(s + BW * BK + kWBoxBytes, kGated ? &tm_b1 : &tm_b0, full, kb * BK, w_row1, pol_w);
+            ptx::tma_load_2d_hint(s, ma, full, kb * BK, tile.row0, pol_last);
           }
           __syncwarp();
-          if (++stage == kPairStages) { stage = 0; phase ^= 1u; }
+          if (++stage == stages) { stage = 0; phase ^= 1u; }
         }
         if (__any_sync(0xFFFFFFFFu, *abort_flag)) break;
       }
     } else if (warp != 2) {
       // ---------------------------------------------------------------- MMA issuers of the leader (two warps in turn, as above)
       if (rank == 0) {
-        constexpr uint32_t idesc = ptx::idesc_e4m3_f32(kPairRows, 2 * BW);
+        constexpr uint32_t idesc = ptx::idesc_e4m3_f32(RowGeom<kCtas>::kRows, 2 * BW);
         const int odd = warp >> 1;
         int stage = 0, next = 0;
         uint32_t phase = 0, buf_phase = 1;
@@ -684,26 +708,33 @@ gemm_blk_pair(const __grid_constant__ RowMaps tm_a, const __grid_constant__ CUte
               ptx::mbar_wait_or_flag(ptx::smem_u32(&st->full[stage]), phase, abort_flag, kRoleMma);
               buf_phase ^= 1u;
               ptx::tc_fence_after_sync();
-              const uint32_t s = ring_u32 + stage * kPairStageBytes;
+              const uint32_t s = ring_u32 + stage * kStageBytes;
               const uint64_t a = ptx::smem_desc_sw128(s), b = ptx::smem_desc_sw128(s + BW * BK);
               if (ptx::elect_one()) {
 #pragma unroll
-                for (int k4 = 0; k4 < BK / UMMA_K; ++k4)
-                  ptx::tc_mma_e4m3_pair(d, a + 2 * k4, b + 2 * k4, idesc, k4 != 0 ? 1u : 0u);
-                ptx::tc_commit_pair(ptx::smem_u32(&st->empty[stage]), 3);    // in both CTAs
-                ptx::tc_commit_pair(ptx::smem_u32(&st->acc_full[odd]), 3);
+                for (int k4 = 0; k4 < BK / UMMA_K; ++k4) {
+                  if constexpr (kPair) ptx::tc_mma_e4m3_pair(d, a + 2 * k4, b + 2 * k4, idesc, k4 != 0 ? 1u : 0u);
+                  else ptx::tc_mma_e4m3(d, a + 2 * k4, b + 2 * k4, idesc, k4 != 0 ? 1u : 0u);
+                }
+                if constexpr (kPair) {
+                  ptx::tc_commit_pair(ptx::smem_u32(&st->empty[stage]), 3);    // in both CTAs
+                  ptx::tc_commit_pair(ptx::smem_u32(&st->acc_full[odd]), 3);
+                } else {
+                  ptx::tc_commit(ptx::smem_u32(&st->empty[stage]));
+                  ptx::tc_commit(ptx::smem_u32(&st->acc_full[odd]));
+                }
               }
               __syncwarp();
             }
             next ^= 1;
-            if (++stage == kPairStages) { stage = 0; phase ^= 1u; }
+            if (++stage == stages) { stage = 0; phase ^= 1u; }
           }
         }
       }
     } else {
       // ---------------------------------------------------------------- scale loaders
       auto decode = [&](int t) {
-        const PairTile tile = pair_decode<kGated>(t, rank, prefix, offs, p);
+        const PairTile tile = pair_decode<kGated, kCtas>(t, rank, prefix, offs, p);
         return ScaleRows{tile.row0, tile.rows, tile.n0, tile.group};
       };
       blk_load_scales<kGated, BW>(p, first, step, total_tiles, 0, p.k_blocks, lane, s_scale, st->sc_full, st->sc_empty,
@@ -715,13 +746,20 @@ gemm_blk_pair(const __grid_constant__ RowMaps tm_a, const __grid_constant__ CUte
     const int quarter = warp & 3, half = (warp - 4) >> 2;
     const int r_tile = quarter * 32 + lane;
     const uint32_t t_lane = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(half * 64);
-    const uint32_t empty0 = ptx::map_to_cta(ptx::smem_u32(&st->acc_empty[0]), 0);
-    const uint32_t empty1 = ptx::map_to_cta(ptx::smem_u32(&st->acc_empty[1]), 0);
+    uint32_t empty0 = ptx::smem_u32(&st->acc_empty[0]), empty1 = ptx::smem_u32(&st->acc_empty[1]);
+    if constexpr (kPair) {
+      empty0 = ptx::map_to_cta(empty0, 0);
+      empty1 = ptx::map_to_cta(empty1, 0);
+    }
+    auto hand_back = [&](uint32_t bar) {
+      if constexpr (kPair) ptx::mbar_arrive_cluster_if(bar, lane == 0);
+      else ptx::mbar_arrive_if(bar, lane == 0);
+    };
     int buf = 0, slot = 0, parity = 0;
     uint32_t buf_phase = 0, slot_phase = 0, row_phase = 0;
     for (int t = first; t < total_tiles; t += step) {
       if (__any_sync(0xFFFFFFFFu, *abort_flag)) break;
-      const PairTile tile = pair_decode<kGated>(t, rank, prefix, offs, p);
+      const PairTile tile = pair_decode<kGated, kCtas>(t, rank, prefix, offs, p);
       const bool live = quarter * 32 < tile.rows;           // any row of this warp
       // columns half * 64 .. + 63 of each weight box: sums 0..63 of the first box, 64..127 of the second
       float acc[128];
@@ -747,14 +785,14 @@ gemm_blk_pair(const __grid_constant__ RowMaps tm_a, const __grid_constant__ CUte
               if (c < 7) ptx::tmem_ld_32x16(ta + ((c + 1) >> 2) * BW + ((c + 1) & 3) * 16, v[(c + 1) & 1]);
               if (c == 7) {
                 ptx::tc_fence_before_sync();
-                ptx::mbar_arrive_cluster_if(empty, lane == 0);     // the warp's loads from this accumulator have completed
+                hand_back(empty);                  // the warp's loads from this accumulator have completed
               }
 #pragma unroll
               for (int i = 0; i < 16; ++i)
                 acc[16 * c + i] = fmaf(__uint_as_float(v[c & 1][i]), c < 4 ? s0 : s1, acc[16 * c + i]);
             }
           } else {
-            ptx::mbar_arrive_cluster_if(empty, lane == 0);
+            hand_back(empty);
           }
           if (++buf == 2) { buf = 0; buf_phase ^= 1u; }
         }
@@ -807,21 +845,21 @@ gemm_blk_pair(const __grid_constant__ RowMaps tm_a, const __grid_constant__ CUte
         const bool whole = quarter * 32 + 32 <= tile.rows;       // all 32 rows are the group's: one bulk store per box
         const uint32_t box = store_u32 + static_cast<uint32_t>(warp - 4) * kStoreBoxBytes;
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int col0 = tile.n0 + c * BW + half * 64;
+        for (int c = 0; c < 4; ++c) {                            // 32 columns at a time, two of each weight box
+          const int col0 = tile.n0 + (c >> 1) * BW + half * 64 + (c & 1) * kStoreCols;
           if (col0 >= p.N) continue;
           if (whole) {
             if (lane == 0) ptx::bulk_wait_group_read_all();      // the box's last store has read it
             __syncwarp();
           }
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
+          for (int i = 0; i < kStoreCols / 8; ++i) {
             uint32_t w[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = pack_bf16(acc[64 * c + 8 * i + 2 * j], acc[64 * c + 8 * i + 2 * j + 1]);
+            for (int j = 0; j < 4; ++j) w[j] = pack_bf16(acc[32 * c + 8 * i + 2 * j], acc[32 * c + 8 * i + 2 * j + 1]);
             const uint4 q = make_uint4(w[0], w[1], w[2], w[3]);
             if (whole)
-              *reinterpret_cast<uint4*>(s_store + (box - store_u32) + lane * 128 + ((i ^ (lane & 7)) << 4)) = q;
+              *reinterpret_cast<uint4*>(s_store + (box - store_u32) + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4)) = q;
             else if (row_ok && col0 + 8 * i < p.N)
               *reinterpret_cast<uint4*>(y + col0 + 8 * i) = q;
           }
@@ -845,10 +883,11 @@ gemm_blk_pair(const __grid_constant__ RowMaps tm_a, const __grid_constant__ CUte
     for (int i = 0; i < 2000; ++i) __nanosleep(1000);
     __syncthreads();
   }
-  ptx::cluster_sync();            // the peer's shared memory and barriers stay alive until both CTAs are done
+  if (kPair) ptx::cluster_sync();   // the peer's shared memory and barriers stay alive until both CTAs are done
   if (warp == 1) {
     ptx::tc_fence_after_sync();
-    ptx::tmem_dealloc_pair(tmem_base, kTmemCols);
+    if constexpr (kPair) ptx::tmem_dealloc_pair(tmem_base, kTmemCols);
+    else ptx::tmem_dealloc(tmem_base, kTmemCols);
   }
 }
 
@@ -914,8 +953,8 @@ moe_status launch_swapped(moe_ctx* ctx, const BlkProduct& g, BlkParams p, cudaSt
                                                                                                      : MOE_ERR_CUDA;
 }
 
-template <bool kGated>
-moe_status launch_pair(moe_ctx* ctx, const BlkProduct& g, const BlkParams& p, cudaStream_t stream) {
+template <bool kGated, int kCtas>
+moe_status launch_rows(moe_ctx* ctx, const BlkProduct& g, BlkParams p, cudaStream_t stream) {
   const uint64_t w_rows = static_cast<uint64_t>(p.groups) * p.N;
   RowMaps tm_a;
   CUtensorMap tm_b0, tm_b1, tm_y;
@@ -928,36 +967,42 @@ moe_status launch_pair(moe_ctx* ctx, const BlkProduct& g, const BlkParams& p, cu
   } else {
     const cuuint64_t dims[2] = {static_cast<cuuint64_t>(p.N), static_cast<cuuint64_t>(p.rows)};
     const cuuint64_t strides[1] = {static_cast<cuuint64_t>(p.N) * 2};
-    const cuuint32_t box[2] = {kStoreBoxCols, 32u}, elem[2] = {1u, 1u};
+    const cuuint32_t box[2] = {kStoreCols, 32u}, elem[2] = {1u, 1u};
     if (ctx->encode_tiled(&tm_y, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.y, dims, strides, box, elem,
-                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
       return MOE_ERR_CUDA;
   }
-  const size_t smem = 1024 + kPairStages * kPairStageBytes + kEpilogueThreads / 32 * kStoreBoxBytes + kScaleSlots * kScaleBatch * 2 * BW * 4 + sizeof(PairTail) +
-                      (3 * static_cast<size_t>(p.groups) + 1) * 4 + 16;
-  const long long tiles = (p.rows / kPairRows + static_cast<long long>(p.groups < p.rows ? p.groups : p.rows)) * p.n_tiles;
-  const long long pairs = tiles < ctx->max_pairs ? tiles : ctx->max_pairs;
+  using G = RowGeom<kCtas>;
+  const size_t rest = 1024 + kEpilogueThreads / 32 * kStoreBoxBytes + kScaleSlots * kScaleBatch * 2 * BW * 4 +
+                      sizeof(PairTail) + (3 * static_cast<size_t>(p.groups) + 1) * 4 + 16;
+  p.stages = static_cast<int>((kMaxSmem - rest) / G::kStageBytes);           // (one less beyond some 600 groups)
+  if (p.stages > G::kStages) p.stages = G::kStages;
+  const size_t smem = rest + static_cast<size_t>(p.stages) * G::kStageBytes;
+  const long long tiles = (p.rows / G::kRows + static_cast<long long>(p.groups < p.rows ? p.groups : p.rows)) * p.n_tiles;
+  const long long room = kCtas == 2 ? ctx->max_pairs : ctx->num_sms;
+  const long long teams = tiles < room ? tiles : room;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(static_cast<unsigned>(2 * pairs));
+  cfg.gridDim = dim3(static_cast<unsigned>(kCtas * teams));
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.x = kCtas;
   attr[0].val.clusterDim.y = 1;
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = kCtas == 2 ? 1 : 0;
   ctx->last_launches += 1;
-  return cudaLaunchKernelEx(&cfg, gemm_blk_pair<kGated>, tm_a, tm_b0, tm_b1, tm_y, p) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, gemm_blk_rows<kGated, kCtas>, tm_a, tm_b0, tm_b1, tm_y, p) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
 template <bool kGated>
 moe_status launch_product(moe_ctx* ctx, const BlkProduct& g, const BlkParams& p, cudaStream_t stream) {
-  const int pair_rows = moe_knob_value(ctx, "blk_pair_rows", 32);
-  if (p.rows > static_cast<long long>(pair_rows) * p.groups) return launch_pair<kGated>(ctx, g, p, stream);
+  const int pair_rows = moe_knob_value(ctx, "blk_pair_rows", 192), row_rows = moe_knob_value(ctx, "blk_rows", 64);
+  if (p.rows > static_cast<long long>(pair_rows) * p.groups) return launch_rows<kGated, 2>(ctx, g, p, stream);
+  if (p.rows > static_cast<long long>(row_rows) * p.groups) return launch_rows<kGated, 1>(ctx, g, p, stream);
   // short stages (more of them) where the groups average few rows
   if (p.rows <= 16LL * p.groups) return launch_swapped<kGated, 32>(ctx, g, p, stream);
   return launch_swapped<kGated, 128>(ctx, g, p, stream);
@@ -973,8 +1018,10 @@ cudaError_t prepare_gemm_blk(moe_ctx* ctx) {
                            reinterpret_cast<const void*>(gemm_blk_swapped<false, 32>),
                            reinterpret_cast<const void*>(gemm_blk_swapped<true, 128>),
                            reinterpret_cast<const void*>(gemm_blk_swapped<false, 128>),
-                           reinterpret_cast<const void*>(gemm_blk_pair<true>),
-                           reinterpret_cast<const void*>(gemm_blk_pair<false>)};
+                           reinterpret_cast<const void*>(gemm_blk_rows<true, 1>),
+                           reinterpret_cast<const void*>(gemm_blk_rows<false, 1>),
+                           reinterpret_cast<const void*>(gemm_blk_rows<true, 2>),
+                           reinterpret_cast<const void*>(gemm_blk_rows<false, 2>)};
   for (const void* k : kernels) {
     const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
     if (e != cudaSuccess) return e;
