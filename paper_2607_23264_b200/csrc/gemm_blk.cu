@@ -99,15 +99,25 @@ __device__ __forceinline__ void blk_report(const BlkParams& p, int role) {
   atomicCAS(&p.status[1], 0, kKernelIdBlk * 65536 + role);
 }
 
+// The group of tile t: the last one whose tiles start at or before it.  By a whole warp, 32 candidates at a time (two
+// rounds for up to 1024 groups; a binary search by each lane cost 300 clocks per tile and role).
+__device__ __forceinline__ int blk_group_of(int t, const int32_t* prefix, const BlkParams& p) {
+  const int lane = threadIdx.x & 31;
+  const int step = (p.groups + 31) >> 5;
+  int i = lane * step;
+  const uint32_t coarse = __ballot_sync(0xFFFFFFFFu, i < p.groups && prefix[min(i, p.groups)] * p.n_tiles <= t);
+  const int base = (__popc(coarse) - 1) * step;
+  i = base + lane;
+  const uint32_t fine =
+      __ballot_sync(0xFFFFFFFFu, lane < step && i < p.groups && prefix[min(i, p.groups)] * p.n_tiles <= t);
+  return base + __popc(fine) - 1;
+}
+
 // Tile t of the list ordered by (group, column tile, row block): the row blocks of a group and column tile are
 // neighbours, so CTAs that run side by side share the weight boxes in L2.
 template <bool kGated, int kMaxN>
 __device__ __forceinline__ BlkTile blk_decode(int t, const int32_t* prefix, const int32_t* offs, const BlkParams& p) {
-  int lo = 0, hi = p.groups;   // invariant: prefix[lo] * n_tiles <= t < prefix[hi] * n_tiles
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (prefix[mid] * p.n_tiles <= t) lo = mid; else hi = mid;
-  }
+  const int lo = blk_group_of(t, prefix, p);
   const int blocks = prefix[lo + 1] - prefix[lo];
   const int local = t - prefix[lo] * p.n_tiles;
   const int nb = local / blocks, mb = local - nb * blocks;
@@ -123,9 +133,13 @@ __device__ __forceinline__ BlkTile blk_decode(int t, const int32_t* prefix, cons
   return tile;
 }
 
-// silu(g) * u with an exponential and a division good to a few ulp: h is quantised from here, and the error of the hardware
-// tanh (2^-11) would move one code in a hundred.
-__device__ __forceinline__ float blk_silu_mul(float g, float u) { return __fdividef(g, 1.0f + __expf(-g)) * u; }
+// silu(g) * u with an exponential and a reciprocal good to a few ulp: h is quantised from here, and the error of the
+// hardware tanh (2^-11) would move one code in a hundred.
+__device__ __forceinline__ float blk_silu_mul(float g, float u) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + __expf(-g)));
+  return g * r * u;
+}
 
 // One row of the output from its running sums: lane l holds columns n0 + 4 l .. + 3 of each weight box.
 template <bool kGated>
@@ -531,8 +545,8 @@ gemm_blk_swapped(const __grid_constant__ RowMaps tm_a, const __grid_constant__ C
 // Tensor memory holds two blocks of K.  Handing one back crosses the pair once per block and warp: those arrivals carry
 // no cluster-wide release (300 clocks more), the loads from tensor memory have completed before them and there is nothing
 // else to publish.
-constexpr int kStoreCols = 32;           // output box of a warp: 32 rows x 32 bf16 columns, 64-byte swizzle
-constexpr int kStoreBoxBytes = 32 * kStoreCols * 2;
+constexpr int kStoreBoxBytes = 32 * 64;  // a warp's staging box: 32 rows x 64 bytes of output
+
 template <int kCtas>
 struct RowGeom {
   static constexpr int kRows = kCtas * BW;                                  // rows of a per tile
@@ -562,11 +576,7 @@ struct PairTile {
 template <bool kGated, int kCtas>
 __device__ __forceinline__ PairTile pair_decode(int t, int rank, const int32_t* prefix, const int32_t* offs,
                                                 const BlkParams& p) {
-  int lo = 0, hi = p.groups;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (prefix[mid] * p.n_tiles <= t) lo = mid; else hi = mid;
-  }
+  const int lo = blk_group_of(t, prefix, p);
   const int blocks = prefix[lo + 1] - prefix[lo];
   const int local = t - prefix[lo] * p.n_tiles;
   const int nb = local / blocks, mb = local - nb * blocks;
@@ -581,10 +591,29 @@ __device__ __forceinline__ PairTile pair_decode(int t, int rank, const int32_t* 
   return tile;
 }
 
+// 64 bytes of each of the warp's 32 rows (16 words per lane, its row) through the warp's box in shared memory, so that a
+// store instruction covers 64 contiguous bytes of eight rows instead of 16 bytes of 32.  dst: the byte address of row 0 of
+// the warp; rows and 16-byte pieces beyond `rows` and `pieces` are left out.  (A bulk copy from the box does it in fewer
+// instructions, but the box cannot be filled again for some 600 clocks: 3800 clocks per tile against 1700.)
+__device__ __forceinline__ void store_rows_64(unsigned char* box, const uint4 (&w)[4], unsigned char* dst, size_t pitch,
+                                              int rows, int pieces, int lane) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(box + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4)) = w[i];
+  __syncwarp();
+  const int piece = lane & 3;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = 8 * i + (lane >> 2);
+    const uint4 q = *reinterpret_cast<const uint4*>(box + r * 64 + ((piece ^ ((r >> 1) & 3)) << 4));
+    if (r < rows && piece < pieces) *reinterpret_cast<uint4*>(dst + r * pitch + 16 * piece) = q;
+  }
+  __syncwarp();
+}
+
 template <bool kGated, int kCtas>
 __global__ void __launch_bounds__(kThreads, 1)
 gemm_blk_rows(const __grid_constant__ RowMaps tm_a, const __grid_constant__ CUtensorMap tm_b0,
-              const __grid_constant__ CUtensorMap tm_b1, const __grid_constant__ CUtensorMap tm_y, const BlkParams p) {
+              const __grid_constant__ CUtensorMap tm_b1, const BlkParams p) {
   constexpr int kStageBytes = RowGeom<kCtas>::kStageBytes;
   const int stages = p.stages;
   constexpr bool kPair = kCtas == 2;
@@ -593,8 +622,7 @@ gemm_blk_rows(const __grid_constant__ RowMaps tm_a, const __grid_constant__ CUte
   const uint32_t pad = (1024u - (raw & 1023u)) & 1023u;
   unsigned char* base = smem_raw + pad;
   const uint32_t ring_u32 = raw + pad;
-  const uint32_t store_u32 = ring_u32 + stages * kStageBytes;                 // one output box per epilogue warp
-  unsigned char* s_store = base + stages * kStageBytes;
+  unsigned char* s_store = base + stages * kStageBytes;                       // one box per epilogue warp
   float* s_scale = reinterpret_cast<float*>(s_store + kEpilogueThreads / 32 * kStoreBoxBytes);   // [kScaleSlots][kScaleBatch][2][BW]
   PairTail* st = reinterpret_cast<PairTail*>(s_scale + kScaleSlots * kScaleBatch * 2 * BW);
   int32_t* prefix = reinterpret_cast<int32_t*>(st + 1);
@@ -802,6 +830,8 @@ gemm_blk_rows(const __grid_constant__ RowMaps tm_a, const __grid_constant__ CUte
       }
       const int row = tile.row0 + r_tile;
       const bool row_ok = r_tile < tile.rows;
+      const int warp_rows = tile.rows - quarter * 32;            // the group's rows among this warp's 32 (may be more, or none)
+      unsigned char* box = s_store + (warp - 4) * kStoreBoxBytes;
       if constexpr (kGated) {
         float h[64], amax = 0.f;
 #pragma unroll
@@ -813,26 +843,24 @@ gemm_blk_rows(const __grid_constant__ RowMaps tm_a, const __grid_constant__ CUte
         st->amax[parity][half][r_tile] = amax;
         __syncwarp();
         const uint32_t bar = ptx::smem_u32(&st->row_sync[quarter]);
-        if (lane == 0) ptx::mbar_arrive(bar);
+        ptx::mbar_arrive_if(bar, lane == 0);
         ptx::mbar_wait_or_flag(bar, row_phase, abort_flag, kRoleEpilogue);
         row_phase ^= 1u;
         amax = fmaxf(amax, st->amax[parity][half ^ 1][r_tile]);
         parity ^= 1;
         const float sc = blk::scale_of(amax);
         const blk::Divider by(sc);
+        const size_t at = static_cast<size_t>(row) * p.N + tile.n0 + half * 64;
+        uint4 w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float* v = h + 16 * i;
+          w[i] = make_uint4(blk::pack4(v[0], v[1], v[2], v[3], by), blk::pack4(v[4], v[5], v[6], v[7], by),
+                            blk::pack4(v[8], v[9], v[10], v[11], by), blk::pack4(v[12], v[13], v[14], v[15], by));
+        }
+        store_rows_64(box, w, reinterpret_cast<unsigned char*>(p.hq) + at - static_cast<size_t>(lane) * p.N, p.N, warp_rows, 4,
+                      lane);
         if (row_ok) {
-          const size_t at = static_cast<size_t>(row) * p.N + tile.n0 + half * 64;
-          uint4* dst = reinterpret_cast<uint4*>(p.hq + (at >> 2));
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint32_t w[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float* v = h + 16 * i + 4 * j;
-              w[j] = blk::pack4(v[0], v[1], v[2], v[3], by);
-            }
-            dst[i] = make_uint4(w[0], w[1], w[2], w[3]);
-          }
           if (half == 0) p.sh[static_cast<size_t>(tile.n0 / BW) * p.rows + row] = sc;
           if (p.h_dbg != nullptr) {
 #pragma unroll
@@ -840,41 +868,22 @@ gemm_blk_rows(const __grid_constant__ RowMaps tm_a, const __grid_constant__ CUte
               *reinterpret_cast<float4*>(p.h_dbg + at + 4 * i) = make_float4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
           }
         }
-      } else {
-        __nv_bfloat16* y = p.y + static_cast<size_t>(row) * p.N;
-        const bool whole = quarter * 32 + 32 <= tile.rows;       // all 32 rows are the group's: one bulk store per box
-        const uint32_t box = store_u32 + static_cast<uint32_t>(warp - 4) * kStoreBoxBytes;
+      } else if (live) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) {                            // 32 columns at a time, two of each weight box
-          const int col0 = tile.n0 + (c >> 1) * BW + half * 64 + (c & 1) * kStoreCols;
+          const int col0 = tile.n0 + (c >> 1) * BW + half * 64 + (c & 1) * 32;
           if (col0 >= p.N) continue;
-          if (whole) {
-            if (lane == 0) ptx::bulk_wait_group_read_all();      // the box's last store has read it
-            __syncwarp();
-          }
+          uint4 w[4];
 #pragma unroll
-          for (int i = 0; i < kStoreCols / 8; ++i) {
-            uint32_t w[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = pack_bf16(acc[32 * c + 8 * i + 2 * j], acc[32 * c + 8 * i + 2 * j + 1]);
-            const uint4 q = make_uint4(w[0], w[1], w[2], w[3]);
-            if (whole)
-              *reinterpret_cast<uint4*>(s_store + (box - store_u32) + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4)) = q;
-            else if (row_ok && col0 + 8 * i < p.N)
-              *reinterpret_cast<uint4*>(y + col0 + 8 * i) = q;
+          for (int i = 0; i < 4; ++i) {
+            const float* v = acc + 32 * c + 8 * i;
+            w[i] = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
           }
-          if (whole) {
-            ptx::fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-              ptx::tma_store_2d(&tm_y, box, col0, row - lane);   // what lies beyond N is not written
-              ptx::bulk_commit_group();
-            }
-          }
+          store_rows_64(box, w, reinterpret_cast<unsigned char*>(p.y + static_cast<size_t>(row - lane) * p.N + col0),
+                        static_cast<size_t>(p.N) * 2, warp_rows, (p.N - col0) / 8, lane);
         }
       }
     }
-    if (lane == 0) ptx::bulk_wait_group_all();                   // this warp's stores have landed
   }
 
   __syncthreads();
@@ -957,22 +966,11 @@ template <bool kGated, int kCtas>
 moe_status launch_rows(moe_ctx* ctx, const BlkProduct& g, BlkParams p, cudaStream_t stream) {
   const uint64_t w_rows = static_cast<uint64_t>(p.groups) * p.N;
   RowMaps tm_a;
-  CUtensorMap tm_b0, tm_b1, tm_y;
+  CUtensorMap tm_b0, tm_b1;
   if (!encode_rows(ctx, &tm_a, g, p.rows) ||
       encode_bytes(ctx, &tm_b0, g.b0, w_rows, g.K, BW) != CUDA_SUCCESS ||
       encode_bytes(ctx, &tm_b1, kGated ? g.b1 : g.b0, w_rows, g.K, BW) != CUDA_SUCCESS)
     return MOE_ERR_CUDA;
-  if (kGated) {
-    tm_y = tm_b0;                                            // (not used)
-  } else {
-    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(p.N), static_cast<cuuint64_t>(p.rows)};
-    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(p.N) * 2};
-    const cuuint32_t box[2] = {kStoreCols, 32u}, elem[2] = {1u, 1u};
-    if (ctx->encode_tiled(&tm_y, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.y, dims, strides, box, elem,
-                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
-                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-      return MOE_ERR_CUDA;
-  }
   using G = RowGeom<kCtas>;
   const size_t rest = 1024 + kEpilogueThreads / 32 * kStoreBoxBytes + kScaleSlots * kScaleBatch * 2 * BW * 4 +
                       sizeof(PairTail) + (3 * static_cast<size_t>(p.groups) + 1) * 4 + 16;
@@ -995,7 +993,7 @@ moe_status launch_rows(moe_ctx* ctx, const BlkProduct& g, BlkParams p, cudaStrea
   cfg.attrs = attr;
   cfg.numAttrs = kCtas == 2 ? 1 : 0;
   ctx->last_launches += 1;
-  return cudaLaunchKernelEx(&cfg, gemm_blk_rows<kGated, kCtas>, tm_a, tm_b0, tm_b1, tm_y, p) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, gemm_blk_rows<kGated, kCtas>, tm_a, tm_b0, tm_b1, p) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
 template <bool kGated>
