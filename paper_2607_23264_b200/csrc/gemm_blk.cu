@@ -1,19 +1,27 @@
 // Grouped product of E4M3 rows and weights with fp32 scales per block of 128, and the two expert GEMMs on it:
 //     y[r,n] = sum_b sa[b][r] sb[n/128][b] * P_b[r,n],     P_b[r,n] = sum_{k in block b} a[r,k] w[n,k]
 // The scales are arbitrary fp32 numbers, which the tensor pipe cannot apply, so each block's P_b is an accumulator of its
-// own in tensor memory (four MMAs, fp32), and epilogue warps add it, scaled, to the running sum in their registers
-// while the tensor pipe computes the next block into the other half of tensor memory.
+// own in tensor memory (fp32), and epilogue warps add it, scaled, to the running sums in their registers while the
+// tensor pipe computes the next block into the other half of tensor memory.  A tile is some rows of a group x 256
+// accumulator columns: two weight boxes of 128 rows (Linear-1: 128 gate rows and the matching 128 up rows, so that a tile
+// yields 128 columns of h, one whole block, which the epilogue quantises from the fp32 sums).
 //
-// Operands are swapped: 256 weight rows (Linear-1: 128 gate and the matching 128 up rows) are the M side of two MMAs,
-// the rows of a, padded to 16, 32, 64, 96 or 128, their N side.  So an expert of few rows costs few multiply-adds and
-// its weights are read once, whatever its size up to 128 rows; more rows are split evenly into blocks that run side by
-// side and share the weights in L2.
-//
-// Roles (384 threads, 168 registers each at launch, moved to where they are needed): warp 0 = TMA producer, warps 1 and
-// 3 = MMA issuers, warp 2 = scale loader (sa * sb per row and weight box, through a ring in shared memory), warps 4-11 =
-// epilogue (four lane quarters x two halves of the rows; 128 running sums per thread at most).
+// Three kinds of tile, because the rows per group decide what bounds the work:
+//   * few rows (at most 64): operands swapped.  The weight boxes are the M side of two MMAs, the rows, padded to 16, 32 or
+//     64, their N side; an expert of few rows costs few multiply-adds, which under the power cap is what counts beside
+//     the weights' bytes.  Each accumulator column has its own scale, read from shared memory.
+//   * more rows (at most 128): the rows are the M side, an epilogue thread owns one row and a scale is one factor per
+//     weight box (at 128 rows the swapped form's scale reads took as long as the sums).
+//   * many rows per group: CTA pairs (clusters of two, cta_group::2) on tiles of 256 rows.  Each CTA stages its 128 rows
+//     and one of the two weight boxes: 32 KB per block of K, 64 bytes per clock at the tensor rate, which is what an SM
+//     takes in from L2, where a single CTA's 48 KB would need 96.  A single CTA keeps twice the weight bytes in flight,
+//     which is what counts while the weights come from HBM (launch_product gives the measured rule).
 // Shapes with too few tiles for the SMs split K over a cluster of 2, 4 or 8 CTAs, which add their running sums through
 // distributed shared memory in rank order: no scratch memory, no atomics, the same bits every time.
+//
+// Roles (384 threads, 168 registers each at launch, moved to where they are needed): warp 0 = TMA producer, warps 1 and
+// 3 = MMA issuers (even and odd blocks of K), warp 2 = scale loader (sa * sb per row and weight box, through a ring in
+// shared memory), warps 4-11 = epilogue (four lane quarters x two halves; 128 running sums per thread at most).
 // Every wait is bounded; a wait that gives up is reported through the status word and the CTA unwinds.
 #include <cuda_bf16.h>
 
@@ -38,7 +46,12 @@ constexpr int kScaleBatch = 4;
 constexpr int kScaleThreads = 32;
 constexpr int kTmemCols = 512;           // two buffers x two weight boxes x 128 columns
 constexpr int kTmemBuf = 256;
-constexpr int kOutTokens = 8;            // rows of a staged per step of the tile's end, per epilogue half
+constexpr int kOutTokens = 8;            // swapped tiles: rows staged per step of the tile's end, per epilogue half
+constexpr int kStoreBoxBytes = 32 * 64;  // other tiles: a warp's staging box, 32 rows x 64 bytes of output
+constexpr int kStagingBytes = 2 * kOutTokens * 256 * 4;
+static_assert(kStagingBytes == kEpilogueThreads / 32 * kStoreBoxBytes, "one staging area serves both");
+constexpr int kSwapRows = 64;            // blocks of at most this many rows run with swapped operands
+constexpr int kPartPitch = 260;          // floats per row of a K split's partial sums (conflict-free for both tile kinds)
 constexpr int kMaxSmem = 227 * 1024;
 constexpr int kKernelIdBlk = 10;         // in the detail word of a time-out: 10 * 65536 + role
 
@@ -63,7 +76,7 @@ struct BlkParams {
 };
 
 // The rows of a, as boxes of each height a tile can have: one copy per block of K whatever the height (a copy costs the
-// issuing warp about 100 clocks, and eight copies of 16 rows were what bound tiles of 128).
+// issuing warp about 100 clocks).
 constexpr int kHeights = 5;
 struct RowMaps {
   CUtensorMap of[kHeights];   // 16, 32, 64, 96, 128 rows
@@ -79,17 +92,28 @@ struct BlkTail {
   uint64_t acc_empty[2];
   uint64_t sc_full[kScaleSlots];
   uint64_t sc_empty[kScaleSlots];
-  uint64_t out_sync[2];     // meeting points of an epilogue half's four warps
+  uint64_t out_sync[2];     // meeting points of an epilogue half's four warps (swapped tiles)
+  uint64_t row_sync[4];     // meeting points of the two warps that share 32 rows
   uint32_t tmem_base;
   int abort_flag;
+  float amax[2][2][BW];     // [tile parity][half][row]
+};
+
+// Per tile: kCtas CTAs x kMaxN rows of a.
+template <int kCtas, int kMaxN>
+struct BlkGeom {
+  static constexpr int kWBoxes = kCtas == 2 ? 1 : 2;                        // weight boxes a CTA stages
+  static constexpr int kRowsAt = kWBoxes * kWBoxBytes;                      // the rows' place in a stage
+  static constexpr int kStageBytes = kRowsAt + kMaxN * BK;
 };
 
 struct BlkTile {
-  int row0, rows;    // rows of a: row0 .. row0 + rows - 1
-  int n_pad;         // their number padded to 16, 32, 64, 96 or 128
+  int row0, rows;    // this CTA's rows of a: row0 .. row0 + rows - 1 (none: rows <= 0)
+  int peer_rows;     // pairs: the other CTA's
   int n0;            // first output column
   int group;
-  int single;        // no other tile reads these weights
+  bool single;       // no other tile reads these weights
+  bool swapped;
 };
 
 // The roles whose waits may give up; the flag holds the first that did, and the kernel's end reports it.
@@ -113,23 +137,32 @@ __device__ __forceinline__ int blk_group_of(int t, const int32_t* prefix, const 
   return base + __popc(fine) - 1;
 }
 
-// Tile t of the list ordered by (group, column tile, row block): the row blocks of a group and column tile are
-// neighbours, so CTAs that run side by side share the weight boxes in L2.
-template <bool kGated, int kMaxN>
-__device__ __forceinline__ BlkTile blk_decode(int t, const int32_t* prefix, const int32_t* offs, const BlkParams& p) {
+// Tile t of the list ordered by (group, chunk of column tiles, row block, column tile): the row blocks of a group and column
+// tile run within one round of the CTAs and share the weight boxes in L2.  Pairs, whose tiles all cost the same, take
+// chunks of one (a Mixtral-like group of 2048 rows is 2.5 % slower with eight).  Single CTAs take chunks of four, so that
+// a group's short last block, which costs less, falls to other CTAs than its whole ones: with the row blocks next to each
+// other and an even number of CTAs half of the CTAs get all the short ones (64 groups of 140 rows, 7168 x 2048: 330 us
+// against 231, 243 with chunks of sixteen).
+template <bool kGated, int kCtas, int kMaxN>
+__device__ __forceinline__ BlkTile blk_decode(int t, int rank, const int32_t* prefix, const int32_t* offs,
+                                              const BlkParams& p) {
   const int lo = blk_group_of(t, prefix, p);
   const int blocks = prefix[lo + 1] - prefix[lo];
   const int local = t - prefix[lo] * p.n_tiles;
-  const int nb = local / blocks, mb = local - nb * blocks;
-  const int rows = offs[2 * lo + 1] - offs[2 * lo];
-  const int per = ((rows + blocks - 1) / blocks + 15) & ~15;   // even blocks: a short last one would waste a tile
+  constexpr int kColChunk = kCtas == 2 ? 1 : 4;
+  const int chunk = local / (blocks * kColChunk), in_chunk = local - chunk * blocks * kColChunk;
+  const int width = min(kColChunk, p.n_tiles - chunk * kColChunk);
+  const int mb = in_chunk / width, nb = chunk * kColChunk + in_chunk - mb * width;
+  const int first = offs[2 * lo] + mb * kCtas * kMaxN;
+  const int left = offs[2 * lo + 1] - first;                 // rows from this block on
   BlkTile tile;
-  tile.row0 = offs[2 * lo] + mb * per;
-  tile.rows = max(0, min(per, rows - mb * per));
-  tile.n_pad = blk_height(blk_height_index(tile.rows));
+  tile.row0 = first + rank * kMaxN;
+  tile.rows = min(kMaxN, left - rank * kMaxN);
+  tile.peer_rows = kCtas == 2 ? min(kMaxN, left - (rank ^ 1) * kMaxN) : 0;
   tile.n0 = nb * (kGated ? BW : 2 * BW);
   tile.group = lo;
-  tile.single = blocks == 1 ? 1 : 0;
+  tile.single = blocks == 1;
+  tile.swapped = kCtas == 1 && tile.rows <= kSwapRows;
   return tile;
 }
 
@@ -192,23 +225,20 @@ __device__ __forceinline__ void blk_prefixes(const BlkParams& p, int most, int32
   }
 }
 
-struct ScaleRows {
-  int row0, rows, n0, group;
-};
-
-// The scale loaders' whole run: for kScaleBatch blocks of K at a time, row r of the tile gets sa * sb of each weight box in
-// the next slot of the ring.  A slot's loads are in flight together and the ring lets the loaders run ahead of the
+// The scale loader's whole run: for kScaleBatch blocks of K at a time, row r of the tile gets sa * sb of each weight box in
+// the next slot of the ring.  A slot's loads are in flight together and the ring lets the loader run ahead of the
 // epilogue, across tiles too; the epilogue waits for scales once per slot.
-template <bool kGated, int kMaxN, typename Decode>
-__device__ __forceinline__ void blk_load_scales(const BlkParams& p, int first, int step, int total_tiles, int kb0, int kb1,
-                                                int idx, float* s_scale, uint64_t* sc_full, uint64_t* sc_empty,
-                                                volatile int* abort_flag, Decode decode) {
+template <bool kGated, int kCtas, int kMaxN>
+__device__ __forceinline__ void blk_load_scales(const BlkParams& p, int rank, int first, int step, int total_tiles,
+                                                int kb0, int kb1, int lane, const int32_t* prefix, const int32_t* offs,
+                                                float* s_scale, BlkTail* st) {
+  volatile int* abort_flag = &st->abort_flag;
   constexpr int kPer = (kMaxN + kScaleThreads - 1) / kScaleThreads;   // rows per thread
   int slot = 0;
   uint32_t slot_phase = 0;
   for (int t = first; t < total_tiles; t += step) {
     if (__any_sync(0xFFFFFFFFu, *abort_flag)) return;
-    const ScaleRows tile = decode(t);
+    const BlkTile tile = blk_decode<kGated, kCtas, kMaxN>(t, rank, prefix, offs, p);
     const int nb = tile.n0 / BW;
     const size_t w_at = (static_cast<size_t>(tile.group) * p.n_blocks + nb) * p.k_blocks;
     const float* sb0 = p.sb0 + w_at;
@@ -222,23 +252,23 @@ __device__ __forceinline__ void blk_load_scales(const BlkParams& p, int first, i
         vb1[u] = in && sb1 ? __ldg(sb1 + kb + u) : 0.f;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-          const int r = idx + i * kScaleThreads;
+          const int r = lane + i * kScaleThreads;
           va[u][i] = in && r < tile.rows ? __ldg(p.sa + static_cast<size_t>(kb + u) * p.rows + tile.row0 + r) : 0.f;
         }
       }
-      ptx::mbar_wait_or_flag(ptx::smem_u32(&sc_empty[slot]), slot_phase ^ 1u, abort_flag, kRoleScale);
+      ptx::mbar_wait_or_flag(ptx::smem_u32(&st->sc_empty[slot]), slot_phase ^ 1u, abort_flag, kRoleScale);
       float* f = s_scale + slot * kScaleBatch * 2 * kMaxN;
 #pragma unroll
       for (int u = 0; u < kScaleBatch; ++u)
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-          const int r = idx + i * kScaleThreads;
+          const int r = lane + i * kScaleThreads;
           if (r < kMaxN) {
             f[u * 2 * kMaxN + r] = va[u][i] * vb0[u];
             f[u * 2 * kMaxN + kMaxN + r] = va[u][i] * vb1[u];
           }
         }
-      ptx::mbar_arrive(ptx::smem_u32(&sc_full[slot]));
+      ptx::mbar_arrive(ptx::smem_u32(&st->sc_full[slot]));
       if (++slot == kScaleSlots) { slot = 0; slot_phase ^= 1u; }
     }
   }
@@ -266,331 +296,6 @@ __device__ __forceinline__ void blk_add_cols(uint32_t taddr, const float* f, flo
   }
 }
 
-template <bool kGated, int kMaxN>
-__global__ void __launch_bounds__(kThreads, 1)
-gemm_blk_swapped(const __grid_constant__ RowMaps tm_a, const __grid_constant__ CUtensorMap tm_b0,
-                 const __grid_constant__ CUtensorMap tm_b1, const BlkParams p) {
-  constexpr int kStageBytes = 2 * kWBoxBytes + kMaxN * BK;
-  extern __shared__ unsigned char smem_raw[];
-  const uint32_t raw = ptx::smem_u32(smem_raw);
-  const uint32_t pad = (1024u - (raw & 1023u)) & 1023u;
-  unsigned char* base = smem_raw + pad;                      // 1024-byte aligned: required by the swizzle
-  const uint32_t ring_u32 = raw + pad;
-  float* s_out = reinterpret_cast<float*>(base + p.stages * kStageBytes);      // [2][kOutTokens][256]
-  float* s_scale = s_out + 2 * kOutTokens * 256;                               // [kScaleSlots][kScaleBatch][2][kMaxN]
-  BlkTail* st = reinterpret_cast<BlkTail*>(s_scale + kScaleSlots * kScaleBatch * 2 * kMaxN);
-  int32_t* prefix = reinterpret_cast<int32_t*>(st + 1);                        // [groups + 1] row blocks before a group
-  int32_t* offs = prefix + p.groups + 1;                                       // [groups][2] first row, end
-
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-
-  if (tid == 0) {
-    for (int s = 0; s < p.stages; ++s) {
-      ptx::mbar_init(ptx::smem_u32(&st->full[s]), 1);
-      ptx::mbar_init(ptx::smem_u32(&st->empty[s]), 1);
-    }
-    for (int a = 0; a < 2; ++a) {
-      ptx::mbar_init(ptx::smem_u32(&st->acc_full[a]), 1);
-      ptx::mbar_init(ptx::smem_u32(&st->acc_empty[a]), kEpilogueThreads / 32);
-    }
-    for (int s = 0; s < kScaleSlots; ++s) {
-      ptx::mbar_init(ptx::smem_u32(&st->sc_full[s]), kScaleThreads);
-      ptx::mbar_init(ptx::smem_u32(&st->sc_empty[s]), kEpilogueThreads / 32);
-    }
-    for (int h = 0; h < 2; ++h) ptx::mbar_init(ptx::smem_u32(&st->out_sync[h]), kEpilogueThreads / 64);
-    st->abort_flag = 0;
-    prefix[0] = 0;
-    ptx::fence_barrier_init();
-    ptx::fence_proxy_async_smem();
-  }
-  if (warp == 0) {
-    blk_prefixes(p, kMaxN, prefix, offs, lane);
-    if (lane == 0) {
-      for (int i = 0; i < kHeights && blk_height(i) <= kMaxN; ++i) ptx::prefetch_tensormap(&tm_a.of[i]);
-      ptx::prefetch_tensormap(&tm_b0);
-      if (kGated) ptx::prefetch_tensormap(&tm_b1);
-    }
-  }
-  if (warp == 1) {
-    ptx::tmem_alloc(ptx::smem_u32(&st->tmem_base), kTmemCols);
-    ptx::tmem_relinquish();
-  }
-  ptx::tc_fence_before_sync();
-  __syncthreads();
-  ptx::tc_fence_after_sync();
-
-  const uint32_t tmem_base = st->tmem_base;
-  const int total_tiles = prefix[p.groups] * p.n_tiles;
-  volatile int* abort_flag = &st->abort_flag;
-  // this CTA's tiles and its part of K
-  const int rank = p.split > 1 ? static_cast<int>(ptx::cluster_ctarank()) : 0;
-  const int first = blockIdx.x / p.split, step = gridDim.x / p.split;
-  const int kb0 = static_cast<int>(static_cast<long long>(rank) * p.k_blocks / p.split);
-  const int kb1 = static_cast<int>(static_cast<long long>(rank + 1) * p.k_blocks / p.split);
-
-  if (warp < 4) {
-    ptx::setmaxnreg_dec<48>();
-    if (warp == 0) {
-      // ---------------------------------------------------------------- TMA producer (whole warp, one lane issues)
-      int stage = 0;
-      uint32_t phase = 1;
-      const uint64_t pol_first = ptx::l2_policy_evict_first(), pol_last = ptx::l2_policy_evict_last();
-      for (int t = first; t < total_tiles; t += step) {
-        const BlkTile tile = blk_decode<kGated, kMaxN>(t, prefix, offs, p);
-        const int w_row = tile.group * p.N + tile.n0;
-        // the second box: the up rows of the same columns, or the next 128 columns where there are any
-        const bool second = kGated || tile.n0 + BW < p.N;
-        const uint32_t bytes = (second ? 2 : 1) * kWBoxBytes + tile.n_pad * BK;
-        const uint64_t pol_w = tile.single ? pol_first : pol_last;   // weights another tile reads again stay in L2
-        const CUtensorMap* ma = &tm_a.of[blk_height_index(tile.rows)];
-        for (int kb = kb0; kb < kb1; ++kb) {
-          ptx::mbar_wait_or_flag(ptx::smem_u32(&st->empty[stage]), phase, abort_flag, kRoleTma);
-          const uint32_t full = ptx::smem_u32(&st->full[stage]);
-          const uint32_t s = ring_u32 + stage * kStageBytes;
-          if (ptx::elect_one()) {
-            ptx::mbar_expect_tx(full, bytes);
-            ptx::tma_load_2d_hint(s, &tm_b0, full, kb * BK, w_row, pol_w);
-            if (second)
-              ptx::tma_load_2d_hint(s + kWBoxBytes, kGated ? &tm_b1 : &tm_b0, full, kb * BK, kGated ? w_row : w_row + BW,
-                                    pol_w);
-            ptx::tma_load_2d_hint(s + 2 * kWBoxBytes, ma, full, kb * BK, tile.row0, pol_last);
-          }
-          __syncwarp();
-          if (++stage == p.stages) { stage = 0; phase ^= 1u; }
-        }
-        if (__any_sync(0xFFFFFFFFu, *abort_flag)) break;
-      }
-    } else if (warp != 2) {
-      // ---------------------------------------------------------------- MMA issuers: warp 1 even blocks of K, warp 3 odd
-      // A block's two waits, MMAs and commits are a chain of 450 to 700 clocks for the issuing warp, more while the
-      // epilogue's sums share its scheduler; blocks accumulate apart, so two warps take them in turn.  Each runs its loop
-      // as a whole and one elected lane issues: with warp-uniform values the operands already are in the registers the
-      // MMA reads them from, which halves the cost against a single-lane branch.
-      const int odd = warp >> 1;
-      int stage = 0, next = 0;                     // ring position, and which issuer takes it
-      uint32_t phase = 0, buf_phase = 1;
-      const uint32_t d = tmem_base + static_cast<uint32_t>(odd * kTmemBuf);
-      for (int t = first; t < total_tiles; t += step) {
-        if (__any_sync(0xFFFFFFFFu, *abort_flag)) break;
-        const uint32_t idesc = ptx::idesc_e4m3_f32(BW, blk_decode<kGated, kMaxN>(t, prefix, offs, p).n_pad);
-        for (int kb = kb0; kb < kb1; ++kb) {
-          if (next == odd) {
-            ptx::mbar_wait_or_flag(ptx::smem_u32(&st->acc_empty[odd]), buf_phase, abort_flag, kRoleMma);
-            ptx::mbar_wait_or_flag(ptx::smem_u32(&st->full[stage]), phase, abort_flag, kRoleMma);
-            buf_phase ^= 1u;
-            ptx::tc_fence_after_sync();
-            const uint32_t s = ring_u32 + stage * kStageBytes;
-            const uint64_t w0 = ptx::smem_desc_sw128(s), w1 = ptx::smem_desc_sw128(s + kWBoxBytes);
-            const uint64_t a = ptx::smem_desc_sw128(s + 2 * kWBoxBytes);
-            if (ptx::elect_one()) {
-#pragma unroll
-              for (int k4 = 0; k4 < BK / UMMA_K; ++k4) {
-                const uint64_t adv = static_cast<uint64_t>(2 * k4);    // +32 bytes along K inside the swizzle row
-                ptx::tc_mma_e4m3(d, w0 + adv, a + adv, idesc, k4 != 0 ? 1u : 0u);
-                ptx::tc_mma_e4m3(d + BW, w1 + adv, a + adv, idesc, k4 != 0 ? 1u : 0u);
-              }
-              ptx::tc_commit(ptx::smem_u32(&st->empty[stage]));
-              ptx::tc_commit(ptx::smem_u32(&st->acc_full[odd]));
-            }
-            __syncwarp();
-          }
-          next ^= 1;
-          if (++stage == p.stages) { stage = 0; phase ^= 1u; }
-        }
-      }
-    } else {
-      // ---------------------------------------------------------------- scale loaders
-      auto decode = [&](int t) {
-        const BlkTile tile = blk_decode<kGated, kMaxN>(t, prefix, offs, p);
-        return ScaleRows{tile.row0, tile.rows, tile.n0, tile.group};
-      };
-      blk_load_scales<kGated, kMaxN>(p, first, step, total_tiles, kb0, kb1, lane, s_scale, st->sc_full, st->sc_empty,
-                                     abort_flag, decode);
-    }
-    if (p.split > 1) {
-      __syncwarp();
-      ptx::cluster_sync();
-      ptx::cluster_sync();
-    }
-  } else {
-    // ------------------------------------------------------------------ epilogue
-    ptx::setmaxnreg_inc<224>();
-    const int quarter = warp & 3;                 // TMEM lane quarter this warp may read: weight rows 32 quarter ..
-    const int half = (warp - 4) >> 2;             // half of the tile's rows of a
-    int buf = 0, slot = 0;
-    uint32_t buf_phase = 0, slot_phase = 0, out_phase = 0;
-    BlkTile tile{};
-    // the four warps of a half meet (a bounded wait: a plain barrier would hang on a warp that gave up)
-    auto meet = [&]() {
-      const uint32_t bar = ptx::smem_u32(&st->out_sync[half]);
-      __syncwarp();
-      ptx::mbar_arrive_if(bar, lane == 0);
-      ptx::mbar_wait_or_flag(bar, out_phase, abort_flag, kRoleEpilogue);
-      out_phase ^= 1u;
-    };
-    // the running sums of one tile, then the tile's end
-    auto run = [&](auto tag) {
-      constexpr int kCols = decltype(tag)::value;          // rows of a this thread sums: half of n_pad
-      float acc[2][kCols];
-#pragma unroll
-      for (int i = 0; i < kCols; ++i) acc[0][i] = acc[1][i] = 0.f;
-      const uint32_t t_lane = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(half * kCols);
-      for (int kb = kb0; kb < kb1; kb += kScaleBatch) {
-        ptx::mbar_wait_or_flag(ptx::smem_u32(&st->sc_full[slot]), slot_phase, abort_flag, kRoleEpilogue);
-        const float* f = s_scale + slot * kScaleBatch * 2 * kMaxN + half * kCols;
-        const int batch = min(kScaleBatch, kb1 - kb);
-        for (int u = 0; u < batch; ++u, f += 2 * kMaxN) {
-          ptx::mbar_wait_or_flag(ptx::smem_u32(&st->acc_full[buf]), buf_phase, abort_flag, kRoleEpilogue);
-          ptx::tc_fence_after_sync();
-          const uint32_t ta = t_lane + static_cast<uint32_t>(buf * kTmemBuf);
-          constexpr int kChunk = kCols < 16 ? kCols : 16;
-#pragma unroll
-          for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int c = 0; c < kCols; c += kChunk)
-              blk_add_cols<kChunk>(ta + b * BW + c, f + b * kMaxN + c, &acc[b][c]);
-          ptx::tc_fence_before_sync();
-          ptx::mbar_arrive_if(ptx::smem_u32(&st->acc_empty[buf]), lane == 0);
-          if (++buf == 2) { buf = 0; buf_phase ^= 1u; }
-        }
-        __syncwarp();
-        ptx::mbar_arrive_if(ptx::smem_u32(&st->sc_empty[slot]), lane == 0);
-        if (++slot == kScaleSlots) { slot = 0; slot_phase ^= 1u; }
-      }
-      if (p.split > 1) {
-        // the ring is idle (the last block's MMAs are done): it takes this CTA's sums, [row][256 weight rows]
-        float* part = reinterpret_cast<float*>(base);
-#pragma unroll
-        for (int i = 0; i < kCols; ++i)
-#pragma unroll
-          for (int b = 0; b < 2; ++b) part[(half * kCols + i) * 256 + b * BW + quarter * 32 + lane] = acc[b][i];
-        return;
-      }
-      // kOutTokens rows at a time through shared memory: weight rows become neighbouring columns of an output row
-      float* mine = s_out + half * kOutTokens * 256;
-#pragma unroll
-      for (int c = 0; c < kCols; c += kOutTokens) {
-        if (half * kCols + c >= tile.rows) break;            // (the same for the four warps of a half)
-#pragma unroll
-        for (int i = 0; i < kOutTokens; ++i)
-#pragma unroll
-          for (int b = 0; b < 2; ++b) mine[i * 256 + b * BW + quarter * 32 + lane] = acc[b][c + i];
-        meet();
-#pragma unroll
-        for (int i = 0; i < kOutTokens / 4; ++i) {
-          const int j = quarter * (kOutTokens / 4) + i, r = half * kCols + c + j;
-          if (r < tile.rows) {
-            const float4 a = *reinterpret_cast<const float4*>(mine + j * 256 + 4 * lane);
-            const float4 b = *reinterpret_cast<const float4*>(mine + j * 256 + BW + 4 * lane);
-            blk_finish_row<kGated>(p, tile.row0 + r, tile.n0, lane, a, b);
-          }
-        }
-        meet();
-      }
-    };
-    for (int t = first; t < total_tiles; t += step) {
-      if (__any_sync(0xFFFFFFFFu, *abort_flag)) break;
-      tile = blk_decode<kGated, kMaxN>(t, prefix, offs, p);
-      switch (tile.n_pad) {
-        case 16: run(std::integral_constant<int, 8>{}); break;
-        case 32: run(std::integral_constant<int, 16>{}); break;
-        case 64: if constexpr (kMaxN >= 64) run(std::integral_constant<int, 32>{}); break;
-        case 96: if constexpr (kMaxN >= 96) run(std::integral_constant<int, 48>{}); break;
-        default: if constexpr (kMaxN >= 128) run(std::integral_constant<int, 64>{}); break;
-      }
-      if (p.split > 1) break;                              // one tile per cluster
-    }
-    if (p.split > 1) {
-      __syncwarp();
-      ptx::cluster_sync();
-      if (first < total_tiles) {
-        // each CTA finishes every split-th row, its eight epilogue warps in turn; partial sums in rank order
-        for (int r = rank + p.split * (warp - 4); r < tile.rows; r += p.split * (kEpilogueThreads / 32)) {
-          float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
-          for (int c = 0; c < p.split; ++c) {
-            const uint32_t at = ptx::map_to_cta(ring_u32 + static_cast<uint32_t>(r * 256 + 4 * lane) * 4, c);
-            const float4 va = ptx::ld_cluster_f4(at), vb = ptx::ld_cluster_f4(at + BW * 4);
-            a.x += va.x; a.y += va.y; a.z += va.z; a.w += va.w;
-            b.x += vb.x; b.y += vb.y; b.z += vb.z; b.w += vb.w;
-          }
-          blk_finish_row<kGated>(p, tile.row0 + r, tile.n0, lane, a, b);
-        }
-      }
-      __syncwarp();
-      ptx::cluster_sync();
-    }
-  }
-
-  __syncthreads();
-  if (st->abort_flag) {
-    if (tid == 0) blk_report(p, st->abort_flag);
-    // a wait gave up: give copies still in flight time to land before the shared memory is released
-    for (int i = 0; i < 2000; ++i) __nanosleep(1000);
-    __syncthreads();
-  }
-  if (warp == 1) {
-    ptx::tc_fence_after_sync();
-    ptx::tmem_dealloc(tmem_base, kTmemCols);
-  }
-}
-
-// ---------------------------------------------------------------------------------------------------------------
-// Many rows per group: the rows of a are the M side, so a thread of the epilogue owns one row and the scales are one factor
-// per weight box (with swapped operands each column has its own, read from shared memory: at 128 rows those broadcasts
-// take as long as the sums).  Tiles of 128 rows (one CTA) or 256 (a CTA pair, cta_group::2) x 256 accumulator columns.
-// A pair's CTA stages its 128 rows and one of the two weight boxes: 32 KB per block of K, 64 bytes per clock at the tensor
-// rate, which is what an SM takes in from L2, where the single CTA's 48 KB would need 96.  A single CTA keeps twice the
-// weight bytes in flight, which is what counts while the weights come from HBM (see launch_product for the measured rule).
-// The leader issues the MMAs of both CTAs, and every CTA's eight epilogue warps keep 128 running sums per thread.
-// Tensor memory holds two blocks of K.  Handing one back crosses the pair once per block and warp: those arrivals carry
-// no cluster-wide release (300 clocks more), the loads from tensor memory have completed before them and there is nothing
-// else to publish.
-constexpr int kStoreBoxBytes = 32 * 64;  // a warp's staging box: 32 rows x 64 bytes of output
-
-template <int kCtas>
-struct RowGeom {
-  static constexpr int kRows = kCtas * BW;                                  // rows of a per tile
-  static constexpr int kStageBytes = BW * BK + (kCtas == 2 ? 1 : 2) * kWBoxBytes;
-  static constexpr int kStages = kCtas == 2 ? 6 : 4;                        // 192 KB
-};
-
-struct PairTail {
-  uint64_t full[kMaxStages];
-  uint64_t empty[kMaxStages];
-  uint64_t acc_full[2];
-  uint64_t acc_empty[2];
-  uint64_t sc_full[kScaleSlots];
-  uint64_t sc_empty[kScaleSlots];
-  uint64_t row_sync[4];     // meeting points of the two warps that share 32 rows
-  uint32_t tmem_base;
-  int abort_flag;
-  float amax[2][2][BW];     // [tile parity][half][row]
-};
-
-struct PairTile {
-  int row0, rows;           // this CTA's rows: row0 .. row0 + rows - 1 (rows <= 0: none)
-  int peer_rows;            // the other CTA's
-  int n0, group, single;
-};
-
-template <bool kGated, int kCtas>
-__device__ __forceinline__ PairTile pair_decode(int t, int rank, const int32_t* prefix, const int32_t* offs,
-                                                const BlkParams& p) {
-  const int lo = blk_group_of(t, prefix, p);
-  const int blocks = prefix[lo + 1] - prefix[lo];
-  const int local = t - prefix[lo] * p.n_tiles;
-  const int nb = local / blocks, mb = local - nb * blocks;
-  const int rows = offs[2 * lo + 1] - offs[2 * lo] - mb * RowGeom<kCtas>::kRows;     // rows from this block on
-  PairTile tile;
-  tile.row0 = offs[2 * lo] + mb * RowGeom<kCtas>::kRows + rank * BW;
-  tile.rows = min(BW, rows - rank * BW);
-  tile.peer_rows = kCtas == 2 ? min(BW, rows - (rank ^ 1) * BW) : 0;
-  tile.n0 = nb * (kGated ? BW : 2 * BW);
-  tile.group = lo;
-  tile.single = blocks == 1 ? 1 : 0;
-  return tile;
-}
-
 // 64 bytes of each of the warp's 32 rows (16 words per lane, its row) through the warp's box in shared memory, so that a
 // store instruction covers 64 contiguous bytes of eight rows instead of 16 bytes of 32.  dst: the byte address of row 0 of
 // the warp; rows and 16-byte pieces beyond `rows` and `pieces` are left out.  (A bulk copy from the box does it in fewer
@@ -610,36 +315,231 @@ __device__ __forceinline__ void store_rows_64(unsigned char* box, const uint4 (&
   __syncwarp();
 }
 
-template <bool kGated, int kCtas>
+// What an epilogue warp carries from tile to tile.
+struct EpilogueState {
+  int buf = 0, slot = 0, parity = 0;
+  uint32_t buf_phase = 0, slot_phase = 0, out_phase = 0, row_phase = 0;
+};
+
+// A tile with swapped operands: this thread's lane is a row of each weight box, its sums are kCols rows of a (one half of
+// the tile's padded rows).  Either the tile's end, or, with K split, this CTA's sums to `part`.
+template <bool kGated, int kMaxN, int kCols>
+__device__ __forceinline__ void blk_swapped_tile(const BlkParams& p, const BlkTile& tile, int kb0, int kb1, uint32_t tmem_base,
+                                                 const float* s_scale, float* s_out, float* part, BlkTail* st,
+                                                 EpilogueState& es) {
+  volatile int* abort_flag = &st->abort_flag;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int quarter = warp & 3, half = (warp - 4) >> 2;
+  float acc[2][kCols];
+#pragma unroll
+  for (int i = 0; i < kCols; ++i) acc[0][i] = acc[1][i] = 0.f;
+  const uint32_t t_lane = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(half * kCols);
+  for (int kb = kb0; kb < kb1; kb += kScaleBatch) {
+    ptx::mbar_wait_or_flag(ptx::smem_u32(&st->sc_full[es.slot]), es.slot_phase, abort_flag, kRoleEpilogue);
+    const float* f = s_scale + es.slot * kScaleBatch * 2 * kMaxN + half * kCols;
+    const int batch = min(kScaleBatch, kb1 - kb);
+    for (int u = 0; u < batch; ++u, f += 2 * kMaxN) {
+      ptx::mbar_wait_or_flag(ptx::smem_u32(&st->acc_full[es.buf]), es.buf_phase, abort_flag, kRoleEpilogue);
+      ptx::tc_fence_after_sync();
+      const uint32_t ta = t_lane + static_cast<uint32_t>(es.buf * kTmemBuf);
+      constexpr int kChunk = kCols < 16 ? kCols : 16;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int c = 0; c < kCols; c += kChunk) blk_add_cols<kChunk>(ta + b * BW + c, f + b * kMaxN + c, &acc[b][c]);
+      ptx::tc_fence_before_sync();
+      ptx::mbar_arrive_if(ptx::smem_u32(&st->acc_empty[es.buf]), lane == 0);
+      if (++es.buf == 2) { es.buf = 0; es.buf_phase ^= 1u; }
+    }
+    __syncwarp();
+    ptx::mbar_arrive_if(ptx::smem_u32(&st->sc_empty[es.slot]), lane == 0);
+    if (++es.slot == kScaleSlots) { es.slot = 0; es.slot_phase ^= 1u; }
+  }
+  if (part != nullptr) {
+#pragma unroll
+    for (int i = 0; i < kCols; ++i)
+#pragma unroll
+      for (int b = 0; b < 2; ++b) part[(half * kCols + i) * kPartPitch + b * BW + quarter * 32 + lane] = acc[b][i];
+    return;
+  }
+  // the four warps of a half meet (a bounded wait: a plain barrier would hang on a warp that gave up)
+  auto meet = [&]() {
+    const uint32_t bar = ptx::smem_u32(&st->out_sync[half]);
+    __syncwarp();
+    ptx::mbar_arrive_if(bar, lane == 0);
+    ptx::mbar_wait_or_flag(bar, es.out_phase, abort_flag, kRoleEpilogue);
+    es.out_phase ^= 1u;
+  };
+  // kOutTokens rows at a time through shared memory: weight rows become neighbouring columns of an output row
+  float* mine = s_out + half * kOutTokens * 256;
+#pragma unroll
+  for (int c = 0; c < kCols; c += kOutTokens) {
+    if (half * kCols + c >= tile.rows) break;            // (the same for the four warps of a half)
+#pragma unroll
+    for (int i = 0; i < kOutTokens; ++i)
+#pragma unroll
+      for (int b = 0; b < 2; ++b) mine[i * 256 + b * BW + quarter * 32 + lane] = acc[b][c + i];
+    meet();
+#pragma unroll
+    for (int i = 0; i < kOutTokens / 4; ++i) {
+      const int j = quarter * (kOutTokens / 4) + i, r = half * kCols + c + j;
+      if (r < tile.rows) {
+        const float4 a = *reinterpret_cast<const float4*>(mine + j * 256 + 4 * lane);
+        const float4 b = *reinterpret_cast<const float4*>(mine + j * 256 + BW + 4 * lane);
+        blk_finish_row<kGated>(p, tile.row0 + r, tile.n0, lane, a, b);
+      }
+    }
+    meet();
+  }
+}
+
+// A tile with the rows of a as the M side: this thread owns one row, its sums are columns 64 half .. + 63 of each weight box.
+template <bool kGated, bool kPair>
+__device__ __forceinline__ void blk_row_tile(const BlkParams& p, const BlkTile& tile, int kb0, int kb1, uint32_t tmem_base,
+                                             uint32_t empty0, uint32_t empty1, const float* s_scale, unsigned char* s_store,
+                                             float* part, BlkTail* st, EpilogueState& es) {
+  volatile int* abort_flag = &st->abort_flag;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int quarter = warp & 3, half = (warp - 4) >> 2;
+  const int r_tile = quarter * 32 + lane;
+  const uint32_t t_lane = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(half * 64);
+  const int warp_rows = tile.rows - quarter * 32;         // the group's rows among this warp's 32 (may be more, or none)
+  const bool live = warp_rows > 0;
+  float acc[128];                                         // 0..63: the first box, 64..127: the second
+#pragma unroll
+  for (int i = 0; i < 128; ++i) acc[i] = 0.f;
+  for (int kb = kb0; kb < kb1; kb += kScaleBatch) {
+    ptx::mbar_wait_or_flag(ptx::smem_u32(&st->sc_full[es.slot]), es.slot_phase, abort_flag, kRoleEpilogue);
+    const float* f = s_scale + es.slot * kScaleBatch * 2 * BW + r_tile;
+    const int batch = min(kScaleBatch, kb1 - kb);
+    for (int u = 0; u < batch; ++u, f += 2 * BW) {
+      const float s0 = f[0], s1 = f[BW];
+      ptx::mbar_wait_or_flag(ptx::smem_u32(&st->acc_full[es.buf]), es.buf_phase, abort_flag, kRoleEpilogue);
+      ptx::tc_fence_after_sync();
+      const uint32_t empty = es.buf == 0 ? empty0 : empty1;
+      auto hand_back = [&]() {
+        ptx::tc_fence_before_sync();
+        // in a pair the arrival crosses it, without a cluster-wide release (300 clocks more): the loads from tensor
+        // memory have completed and there is nothing else to publish
+        if constexpr (kPair) ptx::mbar_arrive_cluster_if(empty, lane == 0);
+        else ptx::mbar_arrive_if(empty, lane == 0);
+      };
+      if (live) {
+        const uint32_t ta = t_lane + static_cast<uint32_t>(es.buf * kTmemBuf);
+        // the next 16 columns are on their way while the last 16 are added (32 at a time was 4 % slower: register moves)
+        uint32_t v[2][16];
+        ptx::tmem_ld_32x16(ta, v[0]);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          ptx::tmem_ld_wait();
+          if (c < 7) ptx::tmem_ld_32x16(ta + ((c + 1) >> 2) * BW + ((c + 1) & 3) * 16, v[(c + 1) & 1]);
+          else hand_back();                               // the warp's loads from this accumulator have completed
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            acc[16 * c + i] = fmaf(__uint_as_float(v[c & 1][i]), c < 4 ? s0 : s1, acc[16 * c + i]);
+        }
+      } else {
+        hand_back();
+      }
+      if (++es.buf == 2) { es.buf = 0; es.buf_phase ^= 1u; }
+    }
+    __syncwarp();
+    ptx::mbar_arrive_if(ptx::smem_u32(&st->sc_empty[es.slot]), lane == 0);
+    if (++es.slot == kScaleSlots) { es.slot = 0; es.slot_phase ^= 1u; }
+  }
+  if (part != nullptr) {
+    float* dst = part + r_tile * kPartPitch + half * 64;
+#pragma unroll
+    for (int i = 0; i < 128; i += 4)
+      *reinterpret_cast<float4*>(dst + (i >> 6) * BW + (i & 63)) = make_float4(acc[i], acc[i + 1], acc[i + 2], acc[i + 3]);
+    return;
+  }
+  const int row = tile.row0 + r_tile;
+  unsigned char* box = s_store + (warp - 4) * kStoreBoxBytes;
+  if constexpr (kGated) {
+    float h[64], amax = 0.f;
+#pragma unroll
+    for (int i = 0; i < 64; ++i) {
+      h[i] = blk_silu_mul(acc[i], acc[64 + i]);
+      amax = fmaxf(amax, fabsf(h[i]));
+    }
+    // a block of h is 128 columns: the row's other 64 are the other half's
+    st->amax[es.parity][half][r_tile] = amax;
+    __syncwarp();
+    const uint32_t bar = ptx::smem_u32(&st->row_sync[quarter]);
+    ptx::mbar_arrive_if(bar, lane == 0);
+    ptx::mbar_wait_or_flag(bar, es.row_phase, abort_flag, kRoleEpilogue);
+    es.row_phase ^= 1u;
+    amax = fmaxf(amax, st->amax[es.parity][half ^ 1][r_tile]);
+    es.parity ^= 1;
+    if (!live) return;
+    const float sc = blk::scale_of(amax);
+    const blk::Divider by(sc);
+    const size_t at = static_cast<size_t>(row) * p.N + tile.n0 + half * 64;
+    uint4 w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float* v = h + 16 * i;
+      w[i] = make_uint4(blk::pack4(v[0], v[1], v[2], v[3], by), blk::pack4(v[4], v[5], v[6], v[7], by),
+                        blk::pack4(v[8], v[9], v[10], v[11], by), blk::pack4(v[12], v[13], v[14], v[15], by));
+    }
+    store_rows_64(box, w, reinterpret_cast<unsigned char*>(p.hq) + at - static_cast<size_t>(lane) * p.N, p.N, warp_rows, 4, lane);
+    if (lane < warp_rows) {
+      if (half == 0) p.sh[static_cast<size_t>(tile.n0 / BW) * p.rows + row] = sc;
+      if (p.h_dbg != nullptr) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          *reinterpret_cast<float4*>(p.h_dbg + at + 4 * i) = make_float4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
+      }
+    }
+  } else if (live) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {                            // 32 columns at a time, two of each weight box
+      const int col0 = tile.n0 + (c >> 1) * BW + half * 64 + (c & 1) * 32;
+      if (col0 >= p.N) continue;
+      uint4 w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float* v = acc + 32 * c + 8 * i;
+        w[i] = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+      }
+      store_rows_64(box, w, reinterpret_cast<unsigned char*>(p.y + static_cast<size_t>(row - lane) * p.N + col0),
+                    static_cast<size_t>(p.N) * 2, warp_rows, (p.N - col0) / 8, lane);
+    }
+  }
+}
+
+template <bool kGated, int kCtas, int kMaxN>
 __global__ void __launch_bounds__(kThreads, 1)
-gemm_blk_rows(const __grid_constant__ RowMaps tm_a, const __grid_constant__ CUtensorMap tm_b0,
-              const __grid_constant__ CUtensorMap tm_b1, const BlkParams p) {
-  constexpr int kStageBytes = RowGeom<kCtas>::kStageBytes;
-  const int stages = p.stages;
+gemm_blk(const __grid_constant__ RowMaps tm_a, const __grid_constant__ CUtensorMap tm_b0,
+         const __grid_constant__ CUtensorMap tm_b1, const BlkParams p) {
+  using G = BlkGeom<kCtas, kMaxN>;
   constexpr bool kPair = kCtas == 2;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t raw = ptx::smem_u32(smem_raw);
   const uint32_t pad = (1024u - (raw & 1023u)) & 1023u;
-  unsigned char* base = smem_raw + pad;
+  unsigned char* base = smem_raw + pad;                      // 1024-byte aligned: required by the swizzle
   const uint32_t ring_u32 = raw + pad;
-  unsigned char* s_store = base + stages * kStageBytes;                       // one box per epilogue warp
-  float* s_scale = reinterpret_cast<float*>(s_store + kEpilogueThreads / 32 * kStoreBoxBytes);   // [kScaleSlots][kScaleBatch][2][BW]
-  PairTail* st = reinterpret_cast<PairTail*>(s_scale + kScaleSlots * kScaleBatch * 2 * BW);
-  int32_t* prefix = reinterpret_cast<int32_t*>(st + 1);
-  int32_t* offs = prefix + p.groups + 1;
+  unsigned char* s_staging = base + p.stages * G::kStageBytes;
+  float* s_scale = reinterpret_cast<float*>(s_staging + kStagingBytes);        // [kScaleSlots][kScaleBatch][2][kMaxN]
+  BlkTail* st = reinterpret_cast<BlkTail*>(s_scale + kScaleSlots * kScaleBatch * 2 * kMaxN);
+  int32_t* prefix = reinterpret_cast<int32_t*>(st + 1);                        // [groups + 1] row blocks before a group
+  int32_t* offs = prefix + p.groups + 1;                                       // [groups][2] first row, end
 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int rank = kPair ? static_cast<int>(ptx::cluster_ctarank()) : 0;   // 0 = leader
-  const int first = blockIdx.x / kCtas, step = gridDim.x / kCtas;
+  const bool in_cluster = kPair || p.split > 1;
+  const int cta = in_cluster ? static_cast<int>(ptx::cluster_ctarank()) : 0;
+  const int rank = kPair ? cta : 0;                          // of a pair: 0 = leader, which issues the MMAs
 
   if (tid == 0) {
-    for (int s = 0; s < stages; ++s) {
+    for (int s = 0; s < p.stages; ++s) {
       ptx::mbar_init(ptx::smem_u32(&st->full[s]), 1);
       ptx::mbar_init(ptx::smem_u32(&st->empty[s]), 1);
     }
     for (int a = 0; a < 2; ++a) {
       ptx::mbar_init(ptx::smem_u32(&st->acc_full[a]), 1);
-      ptx::mbar_init(ptx::smem_u32(&st->acc_empty[a]), kCtas * kEpilogueThreads / 32);   // the warps of both CTAs
+      ptx::mbar_init(ptx::smem_u32(&st->acc_empty[a]), kCtas * kEpilogueThreads / 32);   // a pair: the warps of both CTAs
+      ptx::mbar_init(ptx::smem_u32(&st->out_sync[a]), kEpilogueThreads / 64);
     }
     for (int s = 0; s < kScaleSlots; ++s) {
       ptx::mbar_init(ptx::smem_u32(&st->sc_full[s]), kScaleThreads);
@@ -652,9 +552,9 @@ gemm_blk_rows(const __grid_constant__ RowMaps tm_a, const __grid_constant__ CUte
     ptx::fence_proxy_async_smem();
   }
   if (warp == 0) {
-    blk_prefixes(p, RowGeom<kCtas>::kRows, prefix, offs, lane);
+    blk_prefixes(p, kCtas * kMaxN, prefix, offs, lane);
     if (lane == 0) {
-      for (int i = 0; i < kHeights; ++i) ptx::prefetch_tensormap(&tm_a.of[i]);
+      for (int i = 0; i < kHeights && blk_height(i) <= kMaxN; ++i) ptx::prefetch_tensormap(&tm_a.of[i]);
       ptx::prefetch_tensormap(&tm_b0);
       if (kGated) ptx::prefetch_tensormap(&tm_b1);
     }
@@ -676,78 +576,101 @@ gemm_blk_rows(const __grid_constant__ RowMaps tm_a, const __grid_constant__ CUte
   const uint32_t tmem_base = st->tmem_base;
   const int total_tiles = prefix[p.groups] * p.n_tiles;
   volatile int* abort_flag = &st->abort_flag;
+  // this CTA's (pair's, cluster's) tiles and its part of K
+  const int team = kPair ? 2 : p.split;
+  const int first = blockIdx.x / team, step = gridDim.x / team;
+  const int kb0 = kPair ? 0 : static_cast<int>(static_cast<long long>(cta) * p.k_blocks / p.split);
+  const int kb1 = kPair ? p.k_blocks : static_cast<int>(static_cast<long long>(cta + 1) * p.k_blocks / p.split);
+  auto decode = [&](int t) { return blk_decode<kGated, kCtas, kMaxN>(t, rank, prefix, offs, p); };
 
+  // The TMA and MMA warps run their loops as a whole and one elected lane issues: with warp-uniform values the operands
+  // already are in the registers such instructions read them from, which halves the cost against a single-lane branch.
   if (warp < 4) {
     ptx::setmaxnreg_dec<48>();
     if (warp == 0) {
-      // ---------------------------------------------------------------- TMA producer (both CTAs; whole warp, one lane issues)
+      // ---------------------------------------------------------------- TMA producer
       int stage = 0;
       uint32_t phase = 1;
       const uint64_t pol_first = ptx::l2_policy_evict_first(), pol_last = ptx::l2_policy_evict_last();
-      const CUtensorMap* mb = rank == 0 ? &tm_b0 : &tm_b1;
       for (int t = first; t < total_tiles; t += step) {
-        const PairTile tile = pair_decode<kGated, kCtas>(t, rank, prefix, offs, p);
-        // The first box: gate rows, or the tile's first 128 columns; the second: up rows, or the next 128 columns (what
-        // lies beyond N is computed and not stored; beyond the last group it reads as zero).  In a pair the leader takes
-        // the first and the peer the second.
+        const BlkTile tile = decode(t);
+        // The first box: gate rows, or the tile's first 128 columns; the second: up rows, or the next 128 columns where
+        // there are any (a pair loads it anyway: what lies beyond N is computed and not stored, beyond the last group it
+        // reads as zero).  In a pair the leader takes the first and the peer the second.
         const int w_row0 = tile.group * p.N + tile.n0, w_row1 = kGated ? w_row0 : w_row0 + BW;
         const bool second = kPair || kGated || tile.n0 + BW < p.N;
-        const uint64_t pol_w = tile.single ? pol_first : pol_last;
+        const uint64_t pol_w = tile.single ? pol_first : pol_last;   // weights another tile reads again stay in L2
         const int my_rows = tile.rows > 0 ? blk_height(blk_height_index(tile.rows)) : 0;
         const int peer_rows = tile.peer_rows > 0 ? blk_height(blk_height_index(tile.peer_rows)) : 0;
-        const CUtensorMap* ma = &tm_a.of[blk_height_index(tile.rows)];
         const uint32_t bytes = (second ? 2 : 1) * kWBoxBytes + (my_rows + peer_rows) * BK;   // of both CTAs
-        for (int kb = 0; kb < p.k_blocks; ++kb) {
+        const CUtensorMap* ma = &tm_a.of[blk_height_index(tile.rows)];
+        for (int kb = kb0; kb < kb1; ++kb) {
           ptx::mbar_wait_or_flag(ptx::smem_u32(&st->empty[stage]), phase, abort_flag, kRoleTma);
           const uint32_t full = ptx::smem_u32(&st->full[stage]);
-          const uint32_t s = ring_u32 + stage * kStageBytes;
+          const uint32_t s = ring_u32 + stage * G::kStageBytes;
           if constexpr (kPair) {
             const uint32_t full_leader = ptx::map_to_cta(full, 0);
+            const CUtensorMap* mb = rank == 0 ? &tm_b0 : &tm_b1;
             if (ptx::elect_one()) {
               if (rank == 0) ptx::mbar_expect_tx(full, bytes);
-              ptx::tma_load_2d_pair_hint(s + BW * BK, mb, full_leader, kb * BK, rank == 0 ? w_row0 : w_row1, pol_w);
-              if (my_rows > 0) ptx::tma_load_2d_pair_hint(s, ma, full_leader, kb * BK, tile.row0, pol_last);
+              ptx::tma_load_2d_pair_hint(s, mb, full_leader, kb * BK, rank == 0 ? w_row0 : w_row1, pol_w);
+              if (my_rows > 0) ptx::tma_load_2d_pair_hint(s + G::kRowsAt, ma, full_leader, kb * BK, tile.row0, pol_last);
             }
           } else if (ptx::elect_one()) {
             ptx::mbar_expect_tx(full, bytes);
-            ptx::tma_load_2d_hint(s + BW * BK, &tm_b0, full, kb * BK, w_row0, pol_w);
-            if (second)
-              ptx::tma_load_2d_hint(s + BW * BK + kWBoxBytes, kGated ? &tm_b1 : &tm_b0, full, kb * BK, w_row1, pol_w);
-            ptx::tma_load_2d_hint(s, ma, full, kb * BK, tile.row0, pol_last);
+            ptx::tma_load_2d_hint(s, &tm_b0, full, kb * BK, w_row0, pol_w);
+            if (second) ptx::tma_load_2d_hint(s + kWBoxBytes, kGated ? &tm_b1 : &tm_b0, full, kb * BK, w_row1, pol_w);
+            ptx::tma_load_2d_hint(s + G::kRowsAt, ma, full, kb * BK, tile.row0, pol_last);
           }
           __syncwarp();
-          if (++stage == stages) { stage = 0; phase ^= 1u; }
+          if (++stage == p.stages) { stage = 0; phase ^= 1u; }
         }
         if (__any_sync(0xFFFFFFFFu, *abort_flag)) break;
       }
     } else if (warp != 2) {
-      // ---------------------------------------------------------------- MMA issuers of the leader (two warps in turn, as above)
+      // ---------------------------------------------------------------- MMA issuers: warp 1 even blocks of K, warp 3 odd
+      // A block's two waits, MMAs and commits are a chain of 450 to 700 clocks for the issuing warp, more while the
+      // epilogue's sums share its scheduler; blocks accumulate apart, so two warps take them in turn.
       if (rank == 0) {
-        constexpr uint32_t idesc = ptx::idesc_e4m3_f32(RowGeom<kCtas>::kRows, 2 * BW);
         const int odd = warp >> 1;
-        int stage = 0, next = 0;
+        int stage = 0, next = 0;                   // ring position, and which issuer takes it
         uint32_t phase = 0, buf_phase = 1;
         const uint32_t d = tmem_base + static_cast<uint32_t>(odd * kTmemBuf);
         for (int t = first; t < total_tiles; t += step) {
           if (__any_sync(0xFFFFFFFFu, *abort_flag)) break;
-          for (int kb = 0; kb < p.k_blocks; ++kb) {
+          const BlkTile tile = decode(t);
+          const uint32_t idesc = tile.swapped ? ptx::idesc_e4m3_f32(BW, blk_height(blk_height_index(tile.rows)))
+                                              : ptx::idesc_e4m3_f32(kCtas * BW, 2 * BW);
+          for (int kb = kb0; kb < kb1; ++kb) {
             if (next == odd) {
               ptx::mbar_wait_or_flag(ptx::smem_u32(&st->acc_empty[odd]), buf_phase, abort_flag, kRoleMma);
               ptx::mbar_wait_or_flag(ptx::smem_u32(&st->full[stage]), phase, abort_flag, kRoleMma);
               buf_phase ^= 1u;
               ptx::tc_fence_after_sync();
-              const uint32_t s = ring_u32 + stage * kStageBytes;
-              const uint64_t a = ptx::smem_desc_sw128(s), b = ptx::smem_desc_sw128(s + BW * BK);
+              const uint32_t s = ring_u32 + stage * G::kStageBytes;
+              const uint64_t w0 = ptx::smem_desc_sw128(s), w1 = ptx::smem_desc_sw128(s + kWBoxBytes);
+              const uint64_t a = ptx::smem_desc_sw128(s + G::kRowsAt);
               if (ptx::elect_one()) {
-#pragma unroll
-                for (int k4 = 0; k4 < BK / UMMA_K; ++k4) {
-                  if constexpr (kPair) ptx::tc_mma_e4m3_pair(d, a + 2 * k4, b + 2 * k4, idesc, k4 != 0 ? 1u : 0u);
-                  else ptx::tc_mma_e4m3(d, a + 2 * k4, b + 2 * k4, idesc, k4 != 0 ? 1u : 0u);
-                }
+                // +32 bytes along K inside the swizzle row per MMA; the two boxes lie one behind the other, so as the N
+                // side they are one operand of 256 rows
                 if constexpr (kPair) {
+#pragma unroll
+                  for (int k4 = 0; k4 < BK / UMMA_K; ++k4)
+                    ptx::tc_mma_e4m3_pair(d, a + 2 * k4, w0 + 2 * k4, idesc, k4 != 0 ? 1u : 0u);
                   ptx::tc_commit_pair(ptx::smem_u32(&st->empty[stage]), 3);    // in both CTAs
                   ptx::tc_commit_pair(ptx::smem_u32(&st->acc_full[odd]), 3);
                 } else {
+                  if (tile.swapped) {
+#pragma unroll
+                    for (int k4 = 0; k4 < BK / UMMA_K; ++k4) {
+                      ptx::tc_mma_e4m3(d, w0 + 2 * k4, a + 2 * k4, idesc, k4 != 0 ? 1u : 0u);
+                      ptx::tc_mma_e4m3(d + BW, w1 + 2 * k4, a + 2 * k4, idesc, k4 != 0 ? 1u : 0u);
+                    }
+                  } else {
+#pragma unroll
+                    for (int k4 = 0; k4 < BK / UMMA_K; ++k4)
+                      ptx::tc_mma_e4m3(d, a + 2 * k4, w0 + 2 * k4, idesc, k4 != 0 ? 1u : 0u);
+                  }
                   ptx::tc_commit(ptx::smem_u32(&st->empty[stage]));
                   ptx::tc_commit(ptx::smem_u32(&st->acc_full[odd]));
                 }
@@ -755,140 +678,71 @@ gemm_blk_rows(const __grid_constant__ RowMaps tm_a, const __grid_constant__ CUte
               __syncwarp();
             }
             next ^= 1;
-            if (++stage == stages) { stage = 0; phase ^= 1u; }
+            if (++stage == p.stages) { stage = 0; phase ^= 1u; }
           }
         }
       }
     } else {
-      // ---------------------------------------------------------------- scale loaders
-      auto decode = [&](int t) {
-        const PairTile tile = pair_decode<kGated, kCtas>(t, rank, prefix, offs, p);
-        return ScaleRows{tile.row0, tile.rows, tile.n0, tile.group};
-      };
-      blk_load_scales<kGated, BW>(p, first, step, total_tiles, 0, p.k_blocks, lane, s_scale, st->sc_full, st->sc_empty,
-                                  abort_flag, decode);
+      blk_load_scales<kGated, kCtas, kMaxN>(p, rank, first, step, total_tiles, kb0, kb1, lane, prefix, offs, s_scale, st);
+    }
+    if (!kPair && p.split > 1) {
+      __syncwarp();
+      ptx::cluster_sync();
+      ptx::cluster_sync();
     }
   } else {
-    // ------------------------------------------------------------------ epilogue (both CTAs, own 128 rows)
+    // ------------------------------------------------------------------ epilogue
     ptx::setmaxnreg_inc<224>();
-    const int quarter = warp & 3, half = (warp - 4) >> 2;
-    const int r_tile = quarter * 32 + lane;
-    const uint32_t t_lane = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(half * 64);
+    EpilogueState es;
     uint32_t empty0 = ptx::smem_u32(&st->acc_empty[0]), empty1 = ptx::smem_u32(&st->acc_empty[1]);
     if constexpr (kPair) {
       empty0 = ptx::map_to_cta(empty0, 0);
       empty1 = ptx::map_to_cta(empty1, 0);
     }
-    auto hand_back = [&](uint32_t bar) {
-      if constexpr (kPair) ptx::mbar_arrive_cluster_if(bar, lane == 0);
-      else ptx::mbar_arrive_if(bar, lane == 0);
-    };
-    int buf = 0, slot = 0, parity = 0;
-    uint32_t buf_phase = 0, slot_phase = 0, row_phase = 0;
+    // With K split (one tile per cluster) the ring is idle once the last block's MMAs are done: it takes the partial sums.
+    float* part = !kPair && p.split > 1 ? reinterpret_cast<float*>(base) : nullptr;
+    float* s_out = reinterpret_cast<float*>(s_staging);
+    BlkTile tile{};
     for (int t = first; t < total_tiles; t += step) {
       if (__any_sync(0xFFFFFFFFu, *abort_flag)) break;
-      const PairTile tile = pair_decode<kGated, kCtas>(t, rank, prefix, offs, p);
-      const bool live = quarter * 32 < tile.rows;           // any row of this warp
-      // columns half * 64 .. + 63 of each weight box: sums 0..63 of the first box, 64..127 of the second
-      float acc[128];
-#pragma unroll
-      for (int i = 0; i < 128; ++i) acc[i] = 0.f;
-      for (int kb = 0; kb < p.k_blocks; kb += kScaleBatch) {
-        ptx::mbar_wait_or_flag(ptx::smem_u32(&st->sc_full[slot]), slot_phase, abort_flag, kRoleEpilogue);
-        const float* f = s_scale + slot * kScaleBatch * 2 * BW + r_tile;
-        const int batch = min(kScaleBatch, p.k_blocks - kb);
-        for (int u = 0; u < batch; ++u, f += 2 * BW) {
-          const float s0 = f[0], s1 = f[BW];
-          ptx::mbar_wait_or_flag(ptx::smem_u32(&st->acc_full[buf]), buf_phase, abort_flag, kRoleEpilogue);
-          ptx::tc_fence_after_sync();
-          const uint32_t empty = buf == 0 ? empty0 : empty1;
-          if (live) {
-            const uint32_t ta = t_lane + static_cast<uint32_t>(buf * kTmemBuf);
-            // the next 16 columns are on their way while the last 16 are added (more in flight does not fit the registers)
-            uint32_t v[2][16];
-            ptx::tmem_ld_32x16(ta, v[0]);
-#pragma unroll
-            for (int c = 0; c < 8; ++c) {
-              ptx::tmem_ld_wait();
-              if (c < 7) ptx::tmem_ld_32x16(ta + ((c + 1) >> 2) * BW + ((c + 1) & 3) * 16, v[(c + 1) & 1]);
-              if (c == 7) {
-                ptx::tc_fence_before_sync();
-                hand_back(empty);                  // the warp's loads from this accumulator have completed
-              }
-#pragma unroll
-              for (int i = 0; i < 16; ++i)
-                acc[16 * c + i] = fmaf(__uint_as_float(v[c & 1][i]), c < 4 ? s0 : s1, acc[16 * c + i]);
-            }
-          } else {
-            hand_back(empty);
-          }
-          if (++buf == 2) { buf = 0; buf_phase ^= 1u; }
-        }
-        __syncwarp();
-        ptx::mbar_arrive_if(ptx::smem_u32(&st->sc_empty[slot]), lane == 0);
-        if (++slot == kScaleSlots) { slot = 0; slot_phase ^= 1u; }
+      tile = decode(t);
+      if (!tile.swapped) {
+        if constexpr (kMaxN == BW)
+          blk_row_tile<kGated, kPair>(p, tile, kb0, kb1, tmem_base, empty0, empty1, s_scale, s_staging, part, st, es);
+      } else if constexpr (!kPair) {
+        const int height = blk_height_index(tile.rows);
+        if (height == 0) blk_swapped_tile<kGated, kMaxN, 8>(p, tile, kb0, kb1, tmem_base, s_scale, s_out, part, st, es);
+        else if (height == 1) blk_swapped_tile<kGated, kMaxN, 16>(p, tile, kb0, kb1, tmem_base, s_scale, s_out, part, st, es);
+        else if constexpr (kMaxN >= kSwapRows)
+          blk_swapped_tile<kGated, kMaxN, 32>(p, tile, kb0, kb1, tmem_base, s_scale, s_out, part, st, es);
       }
-      const int row = tile.row0 + r_tile;
-      const bool row_ok = r_tile < tile.rows;
-      const int warp_rows = tile.rows - quarter * 32;            // the group's rows among this warp's 32 (may be more, or none)
-      unsigned char* box = s_store + (warp - 4) * kStoreBoxBytes;
-      if constexpr (kGated) {
-        float h[64], amax = 0.f;
-#pragma unroll
-        for (int i = 0; i < 64; ++i) {
-          h[i] = blk_silu_mul(acc[i], acc[64 + i]);
-          amax = fmaxf(amax, fabsf(h[i]));
-        }
-        // a block of h is 128 columns: the row's other 64 are the other half's
-        st->amax[parity][half][r_tile] = amax;
-        __syncwarp();
-        const uint32_t bar = ptx::smem_u32(&st->row_sync[quarter]);
-        ptx::mbar_arrive_if(bar, lane == 0);
-        ptx::mbar_wait_or_flag(bar, row_phase, abort_flag, kRoleEpilogue);
-        row_phase ^= 1u;
-        amax = fmaxf(amax, st->amax[parity][half ^ 1][r_tile]);
-        parity ^= 1;
-        const float sc = blk::scale_of(amax);
-        const blk::Divider by(sc);
-        const size_t at = static_cast<size_t>(row) * p.N + tile.n0 + half * 64;
-        uint4 w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float* v = h + 16 * i;
-          w[i] = make_uint4(blk::pack4(v[0], v[1], v[2], v[3], by), blk::pack4(v[4], v[5], v[6], v[7], by),
-                            blk::pack4(v[8], v[9], v[10], v[11], by), blk::pack4(v[12], v[13], v[14], v[15], by));
-        }
-        store_rows_64(box, w, reinterpret_cast<unsigned char*>(p.hq) + at - static_cast<size_t>(lane) * p.N, p.N, warp_rows, 4,
-                      lane);
-        if (row_ok) {
-          if (half == 0) p.sh[static_cast<size_t>(tile.n0 / BW) * p.rows + row] = sc;
-          if (p.h_dbg != nullptr) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              *reinterpret_cast<float4*>(p.h_dbg + at + 4 * i) = make_float4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
+      if (part != nullptr) break;
+    }
+    if (part != nullptr) {
+      __syncwarp();
+      ptx::cluster_sync();
+      if (first < total_tiles) {
+        // each CTA finishes every split-th row, its eight epilogue warps in turn; partial sums in rank order
+        for (int r = cta + p.split * (warp - 4); r < tile.rows; r += p.split * (kEpilogueThreads / 32)) {
+          float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+          for (int c = 0; c < p.split; ++c) {
+            const uint32_t at = ptx::map_to_cta(ring_u32 + static_cast<uint32_t>(r * kPartPitch + 4 * lane) * 4, c);
+            const float4 va = ptx::ld_cluster_f4(at), vb = ptx::ld_cluster_f4(at + BW * 4);
+            a.x += va.x; a.y += va.y; a.z += va.z; a.w += va.w;
+            b.x += vb.x; b.y += vb.y; b.z += vb.z; b.w += vb.w;
           }
-        }
-      } else if (live) {
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {                            // 32 columns at a time, two of each weight box
-          const int col0 = tile.n0 + (c >> 1) * BW + half * 64 + (c & 1) * 32;
-          if (col0 >= p.N) continue;
-          uint4 w[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float* v = acc + 32 * c + 8 * i;
-            w[i] = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-          }
-          store_rows_64(box, w, reinterpret_cast<unsigned char*>(p.y + static_cast<size_t>(row - lane) * p.N + col0),
-                        static_cast<size_t>(p.N) * 2, warp_rows, (p.N - col0) / 8, lane);
+          blk_finish_row<kGated>(p, tile.row0 + r, tile.n0, lane, a, b);
         }
       }
+      __syncwarp();
+      ptx::cluster_sync();
     }
   }
 
   __syncthreads();
   if (st->abort_flag) {
     if (tid == 0) blk_report(p, st->abort_flag);
+    // a wait gave up: give copies still in flight time to land before the shared memory is released
     for (int i = 0; i < 2000; ++i) __nanosleep(1000);
     __syncthreads();
   }
@@ -923,87 +777,51 @@ bool encode_rows(moe_ctx* ctx, RowMaps* maps, const BlkProduct& g, int rows) {
   return true;
 }
 
-template <bool kGated, int kMaxN>
-moe_status launch_swapped(moe_ctx* ctx, const BlkProduct& g, BlkParams p, cudaStream_t stream) {
+template <bool kGated, int kCtas, int kMaxN>
+moe_status launch_tiles(moe_ctx* ctx, const BlkProduct& g, BlkParams p, cudaStream_t stream) {
+  using G = BlkGeom<kCtas, kMaxN>;
   const uint64_t w_rows = static_cast<uint64_t>(p.groups) * p.N;
   RowMaps tm_a;
   CUtensorMap tm_b0, tm_b1;
-  if (!encode_rows(ctx, &tm_a, g, p.rows) ||
-      encode_bytes(ctx, &tm_b0, g.b0, w_rows, g.K, BW) != CUDA_SUCCESS ||
+  if (!encode_rows(ctx, &tm_a, g, p.rows) || encode_bytes(ctx, &tm_b0, g.b0, w_rows, g.K, BW) != CUDA_SUCCESS ||
       encode_bytes(ctx, &tm_b1, kGated ? g.b1 : g.b0, w_rows, g.K, BW) != CUDA_SUCCESS)
     return MOE_ERR_CUDA;
-  constexpr size_t kStageBytes = 2 * kWBoxBytes + kMaxN * BK;
-  const size_t rest = 1024 + 2 * kOutTokens * 256 * 4 + kScaleSlots * kScaleBatch * 2 * kMaxN * 4 + sizeof(BlkTail) +
+  const size_t rest = 1024 + kStagingBytes + kScaleSlots * kScaleBatch * 2 * kMaxN * 4 + sizeof(BlkTail) +
                       (3 * static_cast<size_t>(p.groups) + 1) * 4 + 16;
-  int stages = static_cast<int>((kMaxSmem - rest) / kStageBytes);
-  if (stages > kMaxStages) stages = kMaxStages;
-  p.stages = stages;
-  const size_t smem = rest + stages * kStageBytes;
+  p.stages = static_cast<int>((kMaxSmem - rest) / G::kStageBytes);           // 3 to 6
+  if (p.stages > kMaxStages) p.stages = kMaxStages;
+  const size_t smem = rest + static_cast<size_t>(p.stages) * G::kStageBytes;
   // the most tiles the rows can make; the kernel counts the real ones from the offsets
-  const long long blocks = p.rows / kMaxN + (p.groups < p.rows ? p.groups : p.rows);
+  const long long blocks = p.rows / (kCtas * kMaxN) + (p.groups < p.rows ? p.groups : p.rows);
   const long long tiles = blocks * p.n_tiles;
   p.split = 1;
-  while (p.split < 8 && 2 * p.split * tiles <= ctx->num_sms && 2 * p.split <= p.k_blocks) p.split *= 2;
-  const long long grid = tiles * p.split < ctx->num_sms ? tiles * p.split : ctx->num_sms;
+  if (kCtas == 1)
+    while (p.split < 8 && 2 * p.split * tiles <= ctx->num_sms && 2 * p.split <= p.k_blocks) p.split *= 2;
+  const int team = kCtas == 2 ? 2 : p.split;
+  const long long room = kCtas == 2 ? ctx->max_pairs : ctx->num_sms / team;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(static_cast<unsigned>(grid));
+  cfg.gridDim = dim3(static_cast<unsigned>(team * (tiles < room ? tiles : room)));
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = p.split;
+  attr[0].val.clusterDim.x = team;
   attr[0].val.clusterDim.y = 1;
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = p.split > 1 ? 1 : 0;
+  cfg.numAttrs = team > 1 ? 1 : 0;
   ctx->last_launches += 1;
-  return cudaLaunchKernelEx(&cfg, gemm_blk_swapped<kGated, kMaxN>, tm_a, tm_b0, tm_b1, p) == cudaSuccess ? MOE_OK
+  return cudaLaunchKernelEx(&cfg, gemm_blk<kGated, kCtas, kMaxN>, tm_a, tm_b0, tm_b1, p) == cudaSuccess ? MOE_OK
                                                                                                      : MOE_ERR_CUDA;
-}
-
-template <bool kGated, int kCtas>
-moe_status launch_rows(moe_ctx* ctx, const BlkProduct& g, BlkParams p, cudaStream_t stream) {
-  const uint64_t w_rows = static_cast<uint64_t>(p.groups) * p.N;
-  RowMaps tm_a;
-  CUtensorMap tm_b0, tm_b1;
-  if (!encode_rows(ctx, &tm_a, g, p.rows) ||
-      encode_bytes(ctx, &tm_b0, g.b0, w_rows, g.K, BW) != CUDA_SUCCESS ||
-      encode_bytes(ctx, &tm_b1, kGated ? g.b1 : g.b0, w_rows, g.K, BW) != CUDA_SUCCESS)
-    return MOE_ERR_CUDA;
-  using G = RowGeom<kCtas>;
-  const size_t rest = 1024 + kEpilogueThreads / 32 * kStoreBoxBytes + kScaleSlots * kScaleBatch * 2 * BW * 4 +
-                      sizeof(PairTail) + (3 * static_cast<size_t>(p.groups) + 1) * 4 + 16;
-  p.stages = static_cast<int>((kMaxSmem - rest) / G::kStageBytes);           // (one less beyond some 600 groups)
-  if (p.stages > G::kStages) p.stages = G::kStages;
-  const size_t smem = rest + static_cast<size_t>(p.stages) * G::kStageBytes;
-  const long long tiles = (p.rows / G::kRows + static_cast<long long>(p.groups < p.rows ? p.groups : p.rows)) * p.n_tiles;
-  const long long room = kCtas == 2 ? ctx->max_pairs : ctx->num_sms;
-  const long long teams = tiles < room ? tiles : room;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(static_cast<unsigned>(kCtas * teams));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = kCtas;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = kCtas == 2 ? 1 : 0;
-  ctx->last_launches += 1;
-  return cudaLaunchKernelEx(&cfg, gemm_blk_rows<kGated, kCtas>, tm_a, tm_b0, tm_b1, p) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
 template <bool kGated>
 moe_status launch_product(moe_ctx* ctx, const BlkProduct& g, const BlkParams& p, cudaStream_t stream) {
-  const int pair_rows = moe_knob_value(ctx, "blk_pair_rows", 192), row_rows = moe_knob_value(ctx, "blk_rows", 64);
-  if (p.rows > static_cast<long long>(pair_rows) * p.groups) return launch_rows<kGated, 2>(ctx, g, p, stream);
-  if (p.rows > static_cast<long long>(row_rows) * p.groups) return launch_rows<kGated, 1>(ctx, g, p, stream);
-  // short stages (more of them) where the groups average few rows
-  if (p.rows <= 16LL * p.groups) return launch_swapped<kGated, 32>(ctx, g, p, stream);
-  return launch_swapped<kGated, 128>(ctx, g, p, stream);
+  const long long pair_rows = moe_knob_value(ctx, "blk_pair_rows", 192), few_rows = moe_knob_value(ctx, "blk_few_rows", 16);
+  if (p.rows > pair_rows * p.groups) return launch_tiles<kGated, 2, 128>(ctx, g, p, stream);
+  if (p.rows > few_rows * p.groups) return launch_tiles<kGated, 1, 128>(ctx, g, p, stream);
+  return launch_tiles<kGated, 1, 32>(ctx, g, p, stream);
 }
 
 }  // namespace
@@ -1012,14 +830,10 @@ namespace moe {
 
 cudaError_t prepare_gemm_blk(moe_ctx* ctx) {
   (void)ctx;
-  const void* kernels[] = {reinterpret_cast<const void*>(gemm_blk_swapped<true, 32>),
-                           reinterpret_cast<const void*>(gemm_blk_swapped<false, 32>),
-                           reinterpret_cast<const void*>(gemm_blk_swapped<true, 128>),
-                           reinterpret_cast<const void*>(gemm_blk_swapped<false, 128>),
-                           reinterpret_cast<const void*>(gemm_blk_rows<true, 1>),
-                           reinterpret_cast<const void*>(gemm_blk_rows<false, 1>),
-                           reinterpret_cast<const void*>(gemm_blk_rows<true, 2>),
-                           reinterpret_cast<const void*>(gemm_blk_rows<false, 2>)};
+  const void* kernels[] = {
+      reinterpret_cast<const void*>(gemm_blk<true, 1, 32>),  reinterpret_cast<const void*>(gemm_blk<false, 1, 32>),
+      reinterpret_cast<const void*>(gemm_blk<true, 1, 128>), reinterpret_cast<const void*>(gemm_blk<false, 1, 128>),
+      reinterpret_cast<const void*>(gemm_blk<true, 2, 128>), reinterpret_cast<const void*>(gemm_blk<false, 2, 128>)};
   for (const void* k : kernels) {
     const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
     if (e != cudaSuccess) return e;
