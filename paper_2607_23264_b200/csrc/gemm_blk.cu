@@ -138,18 +138,18 @@ __device__ __forceinline__ int blk_group_of(int t, const int32_t* prefix, const 
 }
 
 // Tile t of the list ordered by (group, chunk of column tiles, row block, column tile): the row blocks of a group and column
-// tile run within one round of the CTAs and share the weight boxes in L2.  Pairs, whose tiles all cost the same, take
-// chunks of one (a Mixtral-like group of 2048 rows is 2.5 % slower with eight).  Single CTAs take chunks of four, so that
-// a group's short last block, which costs less, falls to other CTAs than its whole ones: with the row blocks next to each
-// other and an even number of CTAs half of the CTAs get all the short ones (64 groups of 140 rows, 7168 x 2048: 330 us
-// against 231, 243 with chunks of sixteen).
+// tile run within one round of the CTAs and share the weight boxes in L2.  Pairs take chunks of sixteen (one group of 8192
+// rows, 4096 x 7168: 221 us, 225 with eight, 231 with one, the row blocks next to each other).  Single CTAs take chunks of
+// four, so that a group's short last block, which costs less, falls to other CTAs than its whole ones: with the row
+// blocks next to each other and an even number of CTAs half of the CTAs get all the short ones (64 groups of 140 rows,
+// 7168 x 2048: 330 us against 231, 243 with chunks of sixteen).
 template <bool kGated, int kCtas, int kMaxN>
 __device__ __forceinline__ BlkTile blk_decode(int t, int rank, const int32_t* prefix, const int32_t* offs,
                                               const BlkParams& p) {
   const int lo = blk_group_of(t, prefix, p);
   const int blocks = prefix[lo + 1] - prefix[lo];
   const int local = t - prefix[lo] * p.n_tiles;
-  constexpr int kColChunk = kCtas == 2 ? 1 : 4;
+  constexpr int kColChunk = kCtas == 2 ? 16 : 4;
   const int chunk = local / (blocks * kColChunk), in_chunk = local - chunk * blocks * kColChunk;
   const int width = min(kColChunk, p.n_tiles - chunk * kColChunk);
   const int mb = in_chunk / width, nb = chunk * kColChunk + in_chunk - mb * width;
@@ -408,46 +408,51 @@ __device__ __forceinline__ void blk_row_tile(const BlkParams& p, const BlkTile& 
   float acc[128];                                         // 0..63: the first box, 64..127: the second
 #pragma unroll
   for (int i = 0; i < 128; ++i) acc[i] = 0.f;
-  for (int kb = kb0; kb < kb1; kb += kScaleBatch) {
-    ptx::mbar_wait_or_flag(ptx::smem_u32(&st->sc_full[es.slot]), es.slot_phase, abort_flag, kRoleEpilogue);
-    const float* f = s_scale + es.slot * kScaleBatch * 2 * BW + r_tile;
-    const int batch = min(kScaleBatch, kb1 - kb);
-    for (int u = 0; u < batch; ++u, f += 2 * BW) {
-      const float s0 = f[0], s1 = f[BW];
-      ptx::mbar_wait_or_flag(ptx::smem_u32(&st->acc_full[es.buf]), es.buf_phase, abort_flag, kRoleEpilogue);
-      ptx::tc_fence_after_sync();
-      const uint32_t empty = es.buf == 0 ? empty0 : empty1;
-      auto hand_back = [&]() {
-        ptx::tc_fence_before_sync();
-        // in a pair the arrival crosses it, without a cluster-wide release (300 clocks more): the loads from tensor
-        // memory have completed and there is nothing else to publish
-        if constexpr (kPair) ptx::mbar_arrive_cluster_if(empty, lane == 0);
-        else ptx::mbar_arrive_if(empty, lane == 0);
-      };
-      if (live) {
-        const uint32_t ta = t_lane + static_cast<uint32_t>(es.buf * kTmemBuf);
-        // the next 16 columns are on their way while the last 16 are added (32 at a time was 4 % slower: register moves)
-        uint32_t v[2][16];
-        ptx::tmem_ld_32x16(ta, v[0]);
+  // the loop over the blocks of K, with the sums or (warps without rows) without: a branch inside it cost 5 %
+  auto blocks = [&](auto with_sums) {
+    for (int kb = kb0; kb < kb1; kb += kScaleBatch) {
+      ptx::mbar_wait_or_flag(ptx::smem_u32(&st->sc_full[es.slot]), es.slot_phase, abort_flag, kRoleEpilogue);
+      const float* f = s_scale + es.slot * kScaleBatch * 2 * BW + r_tile;
+      const int batch = min(kScaleBatch, kb1 - kb);
+      for (int u = 0; u < batch; ++u, f += 2 * BW) {
+        const float s0 = f[0], s1 = f[BW];
+        ptx::mbar_wait_or_flag(ptx::smem_u32(&st->acc_full[es.buf]), es.buf_phase, abort_flag, kRoleEpilogue);
+        ptx::tc_fence_after_sync();
+        const uint32_t empty = es.buf == 0 ? empty0 : empty1;
+        auto hand_back = [&]() {
+          ptx::tc_fence_before_sync();
+          // in a pair the arrival crosses it, without a cluster-wide release (300 clocks more): the loads from tensor
+          // memory have completed and there is nothing else to publish
+          if constexpr (kPair) ptx::mbar_arrive_cluster_if(empty, lane == 0);
+          else ptx::mbar_arrive_if(empty, lane == 0);
+        };
+        if constexpr (decltype(with_sums)::value) {
+          const uint32_t ta = t_lane + static_cast<uint32_t>(es.buf * kTmemBuf);
+          // the next 16 columns are on their way while the last 16 are added (32 at a time was 4 % slower: register moves)
+          uint32_t v[2][16];
+          ptx::tmem_ld_32x16(ta, v[0]);
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          ptx::tmem_ld_wait();
-          if (c < 7) ptx::tmem_ld_32x16(ta + ((c + 1) >> 2) * BW + ((c + 1) & 3) * 16, v[(c + 1) & 1]);
-          else hand_back();                               // the warp's loads from this accumulator have completed
+          for (int c = 0; c < 8; ++c) {
+            ptx::tmem_ld_wait();
+            if (c < 7) ptx::tmem_ld_32x16(ta + ((c + 1) >> 2) * BW + ((c + 1) & 3) * 16, v[(c + 1) & 1]);
+            else hand_back();                             // the warp's loads from this accumulator have completed
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            acc[16 * c + i] = fmaf(__uint_as_float(v[c & 1][i]), c < 4 ? s0 : s1, acc[16 * c + i]);
+            for (int i = 0; i < 16; ++i)
+              acc[16 * c + i] = fmaf(__uint_as_float(v[c & 1][i]), c < 4 ? s0 : s1, acc[16 * c + i]);
+          }
+        } else {
+          hand_back();
         }
-      } else {
-        hand_back();
+        if (++es.buf == 2) { es.buf = 0; es.buf_phase ^= 1u; }
       }
-      if (++es.buf == 2) { es.buf = 0; es.buf_phase ^= 1u; }
+      __syncwarp();
+      ptx::mbar_arrive_if(ptx::smem_u32(&st->sc_empty[es.slot]), lane == 0);
+      if (++es.slot == kScaleSlots) { es.slot = 0; es.slot_phase ^= 1u; }
     }
-    __syncwarp();
-    ptx::mbar_arrive_if(ptx::smem_u32(&st->sc_empty[es.slot]), lane == 0);
-    if (++es.slot == kScaleSlots) { es.slot = 0; es.slot_phase ^= 1u; }
-  }
-  if (part != nullptr) {
+  };
+  if (live) blocks(std::true_type{});
+  else blocks(std::false_type{});
+  if (!kPair && part != nullptr) {
     float* dst = part + r_tile * kPartPitch + half * 64;
 #pragma unroll
     for (int i = 0; i < 128; i += 4)
