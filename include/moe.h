@@ -547,8 +547,6 @@ moe_status moe_expert_ffn_blk(moe_ctx* ctx, const moe_blk_ffn_args* args, void* 
 /* Byte offsets of the workspace slices of moe_fused_forward_blk (256-byte aligned). */
 typedef struct {
   size_t topk_ids, topk_w, counts, offsets, perm, inv_perm;   /* as in moe_workspace_layout */
-  size_t xq;         /* E4M3 [T,H] */
-  size_t sx;         /* fp32 [H/128][T] */
   size_t xq_perm;    /* E4M3 [R,H] */
   size_t sx_perm;    /* fp32 [H/128][R] */
   size_t hq;         /* E4M3 [R,F] */
@@ -558,7 +556,8 @@ typedef struct {
 } moe_workspace_layout_blk;
 moe_status moe_get_workspace_layout_blk(const moe_shape* shape, moe_workspace_layout_blk* out_layout);
 
-/* The whole fine-grained layer on one stream: plan_routing_scored, quantise x, dispatch, expert_ffn_blk, combine.
+/* The whole fine-grained layer on one stream: plan_routing_scored, x quantised and dispatched in one pass,
+ * expert_ffn_blk, combine.
  * x [T,H] bf16, logits [T,E] fp32, bias [E] fp32 or NULL; weights in blocks of 128 (moe_quantize_weights_blk, or a
  * published checkpoint's codes and scales).  Errors: as the calls it is made of, plus WORKSPACE_TOO_SMALL. */
 moe_status moe_fused_forward_blk(moe_ctx* ctx, const void* x, const float* logits, const float* bias,

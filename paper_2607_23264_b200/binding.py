@@ -104,8 +104,8 @@ class moe_blk_ffn_args(C.Structure):
 
 
 class moe_workspace_layout_blk(C.Structure):
-    _fields_ = [(n, C.c_size_t) for n in ("topk_ids", "topk_w", "counts", "offsets", "perm", "inv_perm", "xq", "sx",
-                                          "xq_perm", "sx_perm", "hq", "sh", "y_perm", "total")]
+    _fields_ = [(n, C.c_size_t) for n in ("topk_ids", "topk_w", "counts", "offsets", "perm", "inv_perm", "xq_perm",
+                                          "sx_perm", "hq", "sh", "y_perm", "total")]
 
 
 _lib = None

@@ -189,7 +189,9 @@ __device__ __forceinline__ void blk_finish_row(const BlkParams& p, int row, int 
     amax = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(amax)));
     const float sc = blk::scale_of(amax);
     const size_t at = static_cast<size_t>(row) * p.N + n0 + 4 * lane;
-    p.hq[at >> 2] = blk::pack4(h[0], h[1], h[2], h[3], blk::Divider(sc));
+    uint32_t w[1];
+    blk::pack(h, sc, w);
+    p.hq[at >> 2] = w[0];
     if (lane == 0) p.sh[static_cast<size_t>(n0 / BW) * p.rows + row] = sc;
     if (p.h_dbg != nullptr) *reinterpret_cast<float4*>(p.h_dbg + at) = make_float4(h[0], h[1], h[2], h[3]);
   } else {
@@ -479,15 +481,12 @@ __device__ __forceinline__ void blk_row_tile(const BlkParams& p, const BlkTile& 
     es.parity ^= 1;
     if (!live) return;
     const float sc = blk::scale_of(amax);
-    const blk::Divider by(sc);
     const size_t at = static_cast<size_t>(row) * p.N + tile.n0 + half * 64;
+    uint32_t codes[16];
+    blk::pack(h, sc, codes);
     uint4 w[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float* v = h + 16 * i;
-      w[i] = make_uint4(blk::pack4(v[0], v[1], v[2], v[3], by), blk::pack4(v[4], v[5], v[6], v[7], by),
-                        blk::pack4(v[8], v[9], v[10], v[11], by), blk::pack4(v[12], v[13], v[14], v[15], by));
-    }
+    for (int i = 0; i < 4; ++i) w[i] = make_uint4(codes[4 * i], codes[4 * i + 1], codes[4 * i + 2], codes[4 * i + 3]);
     store_rows_64(box, w, reinterpret_cast<unsigned char*>(p.hq) + at - static_cast<size_t>(lane) * p.N, p.N, warp_rows, 4, lane);
     if (lane < warp_rows) {
       if (half == 0) p.sh[static_cast<size_t>(tile.n0 / BW) * p.rows + row] = sc;

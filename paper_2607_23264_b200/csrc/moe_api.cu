@@ -909,8 +909,6 @@ void fill_layout_blk(const moe_shape& s, moe_workspace_layout_blk* L) {
   L->offsets = take((E + 1) * 4);
   L->perm = take(R * 4);
   L->inv_perm = take(R * 4);
-  L->xq = take(T * H);
-  L->sx = take(H / 128 * T * 4);
   L->xq_perm = take(R * H);
   L->sx_perm = take(H / 128 * R * 4);
   L->hq = take(R * F);
@@ -1043,16 +1041,13 @@ moe_status moe_fused_forward_blk(moe_ctx* ctx, const void* x, const float* logit
   int32_t* offsets = reinterpret_cast<int32_t*>(ws + L.offsets);
   int32_t* perm = reinterpret_cast<int32_t*>(ws + L.perm);
   int32_t* inv_perm = reinterpret_cast<int32_t*>(ws + L.inv_perm);
-  float* sx = reinterpret_cast<float*>(ws + L.sx);
   float* sx_perm = reinterpret_cast<float*>(ws + L.sx_perm);
   cudaStream_t cs = static_cast<cudaStream_t>(stream);
   begin_call(ctx, 0, stream);
   if (moe::launch_plan_routing_scored(ctx, logits, bias, *rule, topk_ids, topk_w, counts, offsets, perm, inv_perm, cs) !=
       cudaSuccess)
     return MOE_ERR_CUDA;
-  if (moe::launch_quantize_rows_blk(ctx, x, s.T, s.H, ws + L.xq, sx, cs) != cudaSuccess) return MOE_ERR_CUDA;
-  if (moe::launch_dispatch_mx(ctx, ws + L.xq, reinterpret_cast<const uint32_t*>(sx), inv_perm, ws + L.xq_perm,
-                              reinterpret_cast<uint32_t*>(sx_perm), cs) != cudaSuccess)
+  if (moe::launch_quantize_dispatch_blk(ctx, x, inv_perm, ws + L.xq_perm, sx_perm, cs) != cudaSuccess)
     return MOE_ERR_CUDA;
   moe_blk_ffn_args a{};
   a.xq_perm = ws + L.xq_perm;

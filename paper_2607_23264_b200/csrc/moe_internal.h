@@ -165,6 +165,9 @@ cudaError_t prepare_expert_ffn_mx(moe_ctx* ctx);
 // FP8 in blocks of 128: quantisation of rows (1 x 128) and weights (128 x 128), the grouped product, the two GEMMs.
 cudaError_t launch_quantize_rows_blk(moe_ctx* ctx, const void* in_bf16, long long rows, int cols, void* codes,
                                      float* scales, cudaStream_t stream);
+// x quantised and written to its k rows of the expert-contiguous buffer (moe_quantize_rows_blk and moe_dispatch_blk in one).
+cudaError_t launch_quantize_dispatch_blk(moe_ctx* ctx, const void* x, const int32_t* inv_perm, void* xq_perm,
+                                         float* sx_perm, cudaStream_t stream);
 cudaError_t launch_quantize_weights_blk(moe_ctx* ctx, const void* in_bf16, long long mats, int rows, int cols,
                                         void* codes, float* scales, cudaStream_t stream);
 cudaError_t prepare_gemm_blk(moe_ctx* ctx);   // one-time kernel attributes
