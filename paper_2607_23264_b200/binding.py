@@ -192,20 +192,23 @@ def load_library() -> C.CDLL:
 
 def _ptr(t):
     """Device (or host) address of a tensor, None -> NULL."""
-    if t is None:
-        return None
-    if isinstance(t, int):
-        return C.c_void_p(t)
+    if t is None or isinstance(t, int):
+        return t
     if not t.is_contiguous():
         raise ValueError("tensors passed to the MoE library must be contiguous")
-    return C.c_void_p(t.data_ptr())
+    return t.data_ptr()
+
+
+_torch = None
 
 
 def _stream(stream):
-    import torch
     if stream is None:
-        stream = torch.cuda.current_stream()
-    return C.c_void_p(stream.cuda_stream)
+        global _torch
+        if _torch is None:
+            import torch as _torch
+        stream = _torch.cuda.current_stream()
+    return stream.cuda_stream
 
 
 def _check(code: int, where: str):

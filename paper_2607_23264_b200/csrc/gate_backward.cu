@@ -13,6 +13,7 @@
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kAhead = 4;                 // 16-byte vectors of each row a lane has in flight
 constexpr unsigned kFull = 0xFFFFFFFFu;
 
 __global__ void __launch_bounds__(kThreads)
@@ -28,25 +29,40 @@ combine_backward(const uint4* __restrict__ d_out, const uint4* __restrict__ y_pe
   const uint4* y = y_perm + row * vec_per_row;
   uint4* d = d_y_perm ? d_y_perm + row * vec_per_row : nullptr;
   float dot = 0.f;
-  for (int v = lane; v < vec_per_row; v += 32) {
-    const uint4 gv = __ldg(g + v), yv = __ldg(y + v);
-    const __nv_bfloat162* gp = reinterpret_cast<const __nv_bfloat162*>(&gv);
-    const __nv_bfloat162* yp = reinterpret_cast<const __nv_bfloat162*>(&yv);
-    uint4 o;
-    __nv_bfloat162* op = reinterpret_cast<__nv_bfloat162*>(&o);
+  for (int v0 = lane; v0 < vec_per_row; v0 += 32 * kAhead) {
+    uint4 gv[kAhead], yv[kAhead];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 a = __bfloat1622float2(gp[i]), b = __bfloat1622float2(yp[i]);
-      dot = fmaf(a.x, b.x, dot);
-      dot = fmaf(a.y, b.y, dot);
-      op[i] = __floats2bfloat162_rn(w * a.x, w * a.y);
+    for (int u = 0; u < kAhead; ++u) {
+      const int v = v0 + 32 * u;
+      gv[u] = yv[u] = make_uint4(0u, 0u, 0u, 0u);
+      if (v < vec_per_row) {
+        gv[u] = __ldg(g + v);
+        yv[u] = __ldg(y + v);
+      }
     }
-    if (d) d[v] = o;
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int v = v0 + 32 * u;
+      const __nv_bfloat162* gp = reinterpret_cast<const __nv_bfloat162*>(&gv[u]);
+      const __nv_bfloat162* yp = reinterpret_cast<const __nv_bfloat162*>(&yv[u]);
+      uint4 o;
+      __nv_bfloat162* op = reinterpret_cast<__nv_bfloat162*>(&o);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float2 a = __bfloat1622float2(gp[i]), b = __bfloat1622float2(yp[i]);
+        dot = fmaf(a.x, b.x, dot);
+        dot = fmaf(a.y, b.y, dot);
+        op[i] = __floats2bfloat162_rn(w * a.x, w * a.y);
+      }
+      if (d && v < vec_per_row) d[v] = o;
+    }
   }
   dot = moe::warp_sum(dot);
   if (lane == 0) d_topk_w[slot] = dot;
 }
 
+// Lane l holds the logits l, l + 32, ... of the token (EL of them, E <= 32 * EL): the row is read once and written once.
+template <int EL>
 __global__ void __launch_bounds__(kThreads)
 routing_backward(const float* __restrict__ logits, const int32_t* __restrict__ topk_ids,
                  const float* __restrict__ d_topk_w, const moe_route_rule rule, float* __restrict__ d_logits, int T, int E,
@@ -71,21 +87,20 @@ routing_backward(const float* __restrict__ logits, const int32_t* __restrict__ t
       g = 0.f;
     }
   }
-  const float xs = id >= 0 ? row[id] : -INFINITY;
-
-  // largest logit, NaN test and (softmax over all experts) the sum of exponentials
+  float x[EL];
   bool bad = false;
-  float top = -INFINITY;
-  for (int e = lane; e < E; e += 32) {
-    const float x = row[e];
-    bad |= x != x || (!sigmoid && x == INFINITY);
-    top = fmaxf(top, x);
+#pragma unroll
+  for (int i = 0; i < EL; ++i) {
+    const int e = lane + 32 * i;
+    x[i] = e < E ? row[e] : -INFINITY;
   }
+  const float xs = id >= 0 ? row[id] : -INFINITY;
+#pragma unroll
+  for (int i = 0; i < EL; ++i) bad |= x[i] != x[i] || (!sigmoid && x[i] == INFINITY);
   bad = __any_sync(kFull, bad);
+
   const bool dense = !sigmoid && rule.renormalise == 0;   // every expert has a gradient
-  float dot = 0.f, total = 1.f, d;
-  top = moe::warp_max(top);
-  if (top == -INFINITY) top = 0.f;
+  float d, dot = 0.f;
   if (sigmoid) {
     const float s = id >= 0 && xs > -INFINITY ? moe::route_sigmoid(xs) : 0.f;
     float gs = g;
@@ -103,17 +118,28 @@ routing_backward(const float* __restrict__ logits, const int32_t* __restrict__ t
     const float q = sum > 0.f ? p / sum : 0.f;
     d = q * (g - moe::warp_sum(g * q));
   } else {
+    float top = x[0];
+#pragma unroll
+    for (int i = 1; i < EL; ++i) top = fmaxf(top, x[i]);
+    top = moe::warp_max(top);
+    if (top == -INFINITY) top = 0.f;                       // every expert masked: all probabilities 0
     float sum = 0.f;
-    for (int e = lane; e < E; e += 32) sum += expf(row[e] - top);
-    total = moe::warp_sum(sum);
-    const float p = total > 0.f ? expf(xs - top) / total : 0.f;
+#pragma unroll
+    for (int i = 0; i < EL; ++i) {
+      x[i] = expf(x[i] - top);
+      sum += x[i];
+    }
+    sum = moe::warp_sum(sum);
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    const float p = expf(xs - top) * inv;
     dot = moe::warp_sum(g * p);
     d = p * (g - dot);
+    dot *= -inv;
   }
-  for (int e = lane; e < E; e += 32) {
-    float v = 0.f;
-    if (dense && total > 0.f) v = -(expf(row[e] - top) / total) * dot;
-    out[e] = bad ? NAN : v;
+#pragma unroll
+  for (int i = 0; i < EL; ++i) {
+    const int e = lane + 32 * i;
+    if (e < E) out[e] = bad ? NAN : dense ? x[i] * dot : 0.f;
   }
   __syncwarp();
   if (id >= 0 && !bad) out[id] = d;
@@ -139,8 +165,10 @@ cudaError_t launch_routing_backward(moe_ctx* ctx, const float* logits, const int
                                     const moe_route_rule& rule, float* d_logits, cudaStream_t stream) {
   const moe_shape& s = ctx->shape;
   const int per_block = kThreads / 32;
-  routing_backward<<<(s.T + per_block - 1) / per_block, kThreads, 0, stream>>>(
-      logits, topk_ids, d_topk_w, rule, d_logits, s.T, s.E, s.k, ctx->d_status);
+  auto kernel = s.E <= 32 ? routing_backward<1> : s.E <= 64 ? routing_backward<2> : s.E <= 128 ? routing_backward<4>
+                : s.E <= 256 ? routing_backward<8> : s.E <= 512 ? routing_backward<16> : routing_backward<32>;
+  kernel<<<(s.T + per_block - 1) / per_block, kThreads, 0, stream>>>(logits, topk_ids, d_topk_w, rule, d_logits, s.T, s.E,
+                                                                      s.k, ctx->d_status);
   ctx->last_launches += 1;
   return cudaGetLastError();
 }

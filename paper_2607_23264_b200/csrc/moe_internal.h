@@ -116,6 +116,7 @@ cudaError_t launch_plan_from_topk(moe_ctx* ctx, const int32_t* topk_ids, int32_t
 cudaError_t launch_plan_routing_scored(moe_ctx* ctx, const float* logits, const float* bias, const moe_route_rule& rule,
                                        int32_t* topk_ids, float* topk_w, int32_t* counts, int32_t* offsets,
                                        int32_t* perm, int32_t* inv_perm, cudaStream_t stream);
+cudaError_t prepare_plan_scored(moe_ctx* ctx);  // one-time kernel attributes
 // Gradients of the scored weights (to the logits) and of the combine (to the expert rows and the weights).
 cudaError_t launch_routing_backward(moe_ctx* ctx, const float* logits, const int32_t* topk_ids, const float* d_topk_w,
                                     const moe_route_rule& rule, float* d_logits, cudaStream_t stream);

@@ -12,7 +12,7 @@ namespace moe {
 
 // 1 / (1 + e^-x) with correctly rounded operations around expf: the choice compares these values, so they are the ones
 // a plain fp32 program computes, not an approximation of them.
-__device__ __forceinline__ float route_sigmoid(float x) { return __fdiv_rn(1.0f, 1.0f + expf(-x)); }
+__device__ __forceinline__ float route_sigmoid(float x) { return __frcp_rn(1.0f + expf(-x)); }
 
 __device__ __forceinline__ float warp_max(float v) {
 #pragma unroll
@@ -31,116 +31,208 @@ __device__ __forceinline__ void merge_top2(float& a1, float& a2, float b1, float
   a1 = fmaxf(a1, b1);
 }
 
-// Lane l holds the logits l, l + 32, ... (EL per lane, E <= 32 * EL).  `rank` is E floats of shared memory of this
-// warp, used when there are groups.  Lane j < k returns slot j's expert and weight.
+// A rule with what the kernels need of it per expert: expert e is in group (e * inv_size) >> 20 (exact for e < 1024: the
+// rounded-up reciprocal is off by less than 1 / (2^20 / size) per expert), `lanes` lanes scan a group, and a group starts
+// every `pitch` floats in the warp's shared memory (pitch = size + lanes: lanes of different groups read different banks).
+struct RouteRule {
+  moe_route_rule r;
+  int size, lanes, pitch;
+  uint32_t inv_size;
+};
+inline RouteRule make_route_rule(const moe_route_rule& r, int E) {
+  RouteRule q{r, E / r.n_group, 32, 0, 0};
+  while (q.lanes * r.n_group > 32) q.lanes >>= 1;
+  q.pitch = q.size + q.lanes;
+  q.inv_size = ((1u << 20) + q.size - 1) / q.size;
+  return q;
+}
+// Floats of shared memory a warp needs for the selection: the groups' ranking values and the list of kept groups.
+inline int route_smem_floats(const RouteRule& q) { return q.r.n_group > 1 ? q.r.n_group * q.pitch + 32 : 0; }
+
+// Top k of EL keys per lane (key[i] of the expert expert[i], rising with i and, across lanes, with the candidate index
+// lane + 32 i; 0 = none): every lane sorts its own, then k rounds take the largest head.  Lane j returns slot j's expert.
+// Ties go to the lower candidate index, hence to the lower expert.
 template <int EL>
-__device__ __forceinline__ void warp_select_scored(const float* __restrict__ row, const float* __restrict__ bias,
-                                                   const moe_route_rule& r, int E, int k, int lane, float* rank, int& id,
-                                                   float& w) {
+__device__ __forceinline__ int warp_topk(uint32_t (&key)[EL], int (&expert)[EL], int k, int lane) {
   constexpr unsigned kFull = 0xFFFFFFFFu;
-  const bool sigmoid = r.score == MOE_SCORE_SIGMOID;
+  int id = 0;
+  if constexpr (EL <= 8) {
+    // odd-even transposition on neighbours with a strict comparison: stable, so equal keys keep the lower expert first
+#pragma unroll
+    for (int round = 0; round < EL; ++round)
+#pragma unroll
+      for (int i = round & 1; i + 1 < EL; i += 2) {
+        const bool swap = key[i + 1] > key[i];
+        const uint32_t ka = swap ? key[i + 1] : key[i], kb = swap ? key[i] : key[i + 1];
+        const int ea = swap ? expert[i + 1] : expert[i], eb = swap ? expert[i] : expert[i + 1];
+        key[i] = ka; key[i + 1] = kb; expert[i] = ea; expert[i + 1] = eb;
+      }
+    for (int j = 0; j < k; ++j) {
+      const uint32_t largest = __reduce_max_sync(kFull, key[0]);
+      const uint32_t heads = __ballot_sync(kFull, key[0] == largest);
+      int pick;
+      if (__popc(heads) == 1) pick = __shfl_sync(kFull, expert[0], __ffs(heads) - 1);
+      else pick = __reduce_min_sync(kFull, key[0] == largest ? expert[0] : 0x7FFFFFFF);
+      if (lane == j) id = pick;
+      if (key[0] == largest && expert[0] == pick) {        // the owner's next
+#pragma unroll
+        for (int i = 0; i + 1 < EL; ++i) { key[i] = key[i + 1]; expert[i] = expert[i + 1]; }
+        key[EL - 1] = 0u;
+      }
+    }
+  } else {
+    for (int j = 0; j < k; ++j) {
+      uint32_t best = 0u;
+      int best_e = 0x7FFFFFFF;
+#pragma unroll
+      for (int i = 0; i < EL; ++i)
+        if (key[i] > best) { best = key[i]; best_e = expert[i]; }
+      const uint32_t largest = __reduce_max_sync(kFull, best);
+      const int pick = __reduce_min_sync(kFull, best == largest ? best_e : 0x7FFFFFFF);
+      if (lane == j) id = pick;
+#pragma unroll
+      for (int i = 0; i < EL; ++i)
+        if (expert[i] == pick) key[i] = 0u;
+    }
+  }
+  return id;
+}
+
+// The candidates of the kept groups, EL per lane (in ascending expert order), and their top k.
+template <int EL>
+__device__ __forceinline__ int warp_topk_of_groups(const float* __restrict__ row, const RouteRule& q, bool by_score,
+                                                   int count, int k, int lane, const float* rank, const int* kept) {
+  uint32_t key[EL];
+  int expert[EL];
+#pragma unroll
+  for (int i = 0; i < EL; ++i) {
+    const int c = lane + 32 * i;
+    key[i] = 0u;
+    expert[i] = 0x7FFFFFFF;
+    if (c < count) {
+      const int at = static_cast<int>((c * q.inv_size) >> 20), in = c - at * q.size;
+      const int g = kept[at];
+      expert[i] = g * q.size + in;
+      float v = rank[g * q.pitch + in];
+      if (by_score) {                                      // ranked by scores, chosen by logits (NaN among the masked)
+        v = row[expert[i]];
+        if (v != v) v = -INFINITY;
+      }
+      key[i] = order_key(v);
+    }
+  }
+  return warp_topk<EL>(key, expert, k, lane);
+}
+
+// Lane l reads the logits l, l + 32, ... (EL per lane, E <= 32 * EL).  `mem` is route_smem_floats floats of shared memory
+// of this warp.  Lane j < k returns slot j's expert and weight.
+template <int EL, bool kSigmoid, bool kGroups>
+__device__ __forceinline__ void warp_select_scored(const float* __restrict__ row, const float* __restrict__ bias,
+                                                   const RouteRule& q, int E, int k, int lane, float* mem, int& id, float& w) {
+  constexpr unsigned kFull = 0xFFFFFFFFu;
+  const moe_route_rule& r = q.r;
   float x[EL];
   bool bad = false;
 #pragma unroll
   for (int i = 0; i < EL; ++i) {
     const int e = lane + 32 * i;
     x[i] = e < E ? row[e] : -INFINITY;
-    bad |= x[i] != x[i] || (!sigmoid && x[i] == INFINITY);
   }
+#pragma unroll
+  for (int i = 0; i < EL; ++i) bad |= x[i] != x[i] || (!kSigmoid && x[i] == INFINITY);
   bad = __any_sync(kFull, bad);
 
-  // softmax: largest logit and the sum of the exponentials (fp32; exponents are at most 0)
+  // softmax: largest logit and the sum of the exponentials (fp32; exponents are at most 0), where a score is used
   float top = 0.f, total = 1.f;
-  if (!sigmoid) {
+  if (!kSigmoid) {
     top = x[0];
 #pragma unroll
     for (int i = 1; i < EL; ++i) top = fmaxf(top, x[i]);
     top = warp_max(top);
     if (top == -INFINITY) top = 0.f;               // every expert masked: all exponentials are 0
-    float sum = 0.f;
+    if (bias != nullptr || r.renormalise == 0) {
+      float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < EL; ++i) sum += expf(x[i] - top);
-    total = warp_sum(sum);
+      for (int i = 0; i < EL; ++i) sum += expf(x[i] - top);
+      total = warp_sum(sum);
+    }
   }
 
-  // choice values, and what the groups are ranked by
-  const bool by_score = bias == nullptr && r.n_group > 1 && r.group_top == 2;
+  // choice values
   float c[EL];
+  if (bias != nullptr) {
 #pragma unroll
-  for (int i = 0; i < EL; ++i) {
-    const int e = lane + 32 * i;
-    c[i] = x[i];
-    if (bias != nullptr && e < E && x[i] > -INFINITY)
-      c[i] = (sigmoid ? route_sigmoid(x[i]) : __fdiv_rn(expf(x[i] - top), total)) + bias[e];
-    if (c[i] != c[i]) c[i] = -INFINITY;            // NaN ranks with the masked experts
-    if (r.n_group > 1 && e < E)
-      rank[e] = !by_score || x[i] == -INFINITY ? c[i] : sigmoid ? route_sigmoid(x[i]) : expf(x[i] - top);
+    for (int i = 0; i < EL; ++i) {
+      const int e = lane + 32 * i;
+      c[i] = x[i];
+      if (e < E && x[i] > -INFINITY) c[i] = (kSigmoid ? route_sigmoid(x[i]) : __fdiv_rn(expf(x[i] - top), total)) + bias[e];
+      if (c[i] != c[i]) c[i] = -INFINITY;          // NaN ranks with the masked experts
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < EL; ++i) c[i] = x[i] != x[i] ? -INFINITY : x[i];
   }
-  uint32_t kept = 0xFFFFFFFFu;                     // bit g: group g stays
-  if (r.n_group > 1) {
-    __syncwarp();
-    // a power of two of lanes per group, each scanning every lanes-th expert of it; the start is rotated by the group
-    // so that lanes of different groups read different banks
-    const int size = E / r.n_group;
-    int lanes = 32;
-    while (lanes * r.n_group > 32) lanes >>= 1;
-    const int g = lane / lanes, sub = lane % lanes;
-    float v1 = -INFINITY, v2 = -INFINITY;
-    if (g < r.n_group) {
-      const int steps = (size + lanes - 1) / lanes;
-      int i = g % steps;
-      for (int n = 0; n < steps; ++n) {
-        const int m = sub + i * lanes;
-        if (m < size) merge_top2(v1, v2, rank[g * size + m], -INFINITY);
-        if (++i == steps) i = 0;
+
+  if constexpr (!kGroups) {
+    uint32_t key[EL];
+    int expert[EL];
+#pragma unroll
+    for (int i = 0; i < EL; ++i) {
+      expert[i] = lane + 32 * i;
+      key[i] = expert[i] < E ? order_key(c[i]) : 0u;       // 0 is below every key
+    }
+    id = warp_topk<EL>(key, expert, k, lane);
+  } else {
+    // what the groups are ranked by, to shared memory in group order
+    const bool by_score = bias == nullptr && r.group_top == 2;
+    int* kept = reinterpret_cast<int*>(mem + r.n_group * q.pitch);
+#pragma unroll
+    for (int i = 0; i < EL; ++i) {
+      const int e = lane + 32 * i;
+      if (e < E) {
+        float v = c[i];
+        if (by_score && v > -INFINITY) v = kSigmoid ? route_sigmoid(x[i]) : expf(x[i] - top);
+        mem[e + ((e * q.inv_size) >> 20) * q.lanes] = v;
       }
     }
-    for (int off = lanes >> 1; off > 0; off >>= 1) {
+    __syncwarp();
+    // `lanes` lanes per group (a power of two), each scanning every lanes-th expert of it
+    const int g = lane / q.lanes, sub = lane - g * q.lanes;
+    float v1 = -INFINITY, v2 = -INFINITY;
+    if (g < r.n_group) {
+      const float* mine = mem + g * q.pitch;
+      for (int m = sub; m < q.size; m += q.lanes) merge_top2(v1, v2, mine[m], -INFINITY);
+    }
+    for (int off = q.lanes >> 1; off > 0; off >>= 1) {
       const float b1 = __shfl_xor_sync(kFull, v1, off), b2 = __shfl_xor_sync(kFull, v2, off);
       merge_top2(v1, v2, b1, b2);
     }
-    // worth of the group, held by its first lane; a masked second expert adds nothing
+    // a group's worth (a masked second expert adds nothing) and its place among the groups, ties to the lower group
     float worth = v1;
     if (r.group_top == 2 && v2 > -INFINITY) worth = v1 + v2;
-    uint32_t key = (g < r.n_group && sub == 0) ? order_key(worth) : 0u;
-    kept = 0u;
-    for (int j = 0; j < r.topk_group; ++j) {
-      const uint32_t best = __reduce_max_sync(kFull, key);
-      const int pick = __reduce_min_sync(kFull, key == best ? g : 0x7FFFFFFF);
-      kept |= 1u << pick;
-      if (g == pick) key = 0u;
+    const uint32_t key = order_key(worth);
+    int better = 0;
+    for (int h = 0; h < r.n_group; ++h) {
+      const uint32_t other = __shfl_sync(kFull, key, h * q.lanes);
+      better += (other > key || (other == key && h < g)) ? 1 : 0;
     }
+    const bool stays = g < r.n_group && sub == 0 && better < r.topk_group;
+    const uint32_t staying = __ballot_sync(kFull, stays);
+    if (stays) kept[__popc(staying & ((1u << lane) - 1u))] = g;
+    __syncwarp();
+    const int count = r.topk_group * q.size;
+    if (count <= 32) id = warp_topk_of_groups<1>(row, q, by_score, count, k, lane, mem, kept);
+    else if (EL >= 2 && count <= 64) id = warp_topk_of_groups<2>(row, q, by_score, count, k, lane, mem, kept);
+    else if (EL >= 4 && count <= 128) id = warp_topk_of_groups<4>(row, q, by_score, count, k, lane, mem, kept);
+    else id = warp_topk_of_groups<EL>(row, q, by_score, count, k, lane, mem, kept);
     __syncwarp();
   }
-
-  uint32_t key[EL];
-#pragma unroll
-  for (int i = 0; i < EL; ++i) {
-    const int e = lane + 32 * i;
-    bool open = e < E;
-    if (r.n_group > 1 && open) open = (kept >> (e / (E / r.n_group))) & 1u;
-    key[i] = open ? order_key(c[i]) : 0u;          // 0 is below every key
-  }
-  id = 0;
-  for (int j = 0; j < k; ++j) {
-    uint32_t best = 0;
-    int best_e = 0x7FFFFFFF;
-#pragma unroll
-    for (int i = 0; i < EL; ++i)
-      if (key[i] > best) { best = key[i]; best_e = lane + 32 * i; }
-    const uint32_t largest = __reduce_max_sync(kFull, best);
-    int pick = __reduce_min_sync(kFull, best == largest ? best_e : 0x7FFFFFFF);
-    if (pick >= E) pick = E - 1;                   // nothing left (cannot happen for an allowed k): stay in range
-#pragma unroll
-    for (int i = 0; i < EL; ++i)
-      if (pick == lane + 32 * i) key[i] = 0u;
-    if (lane == j) id = pick;
-  }
+  if (id >= E) id = E - 1;                         // nothing left (cannot happen for an allowed k): stay in range
 
   // weights from the unbiased scores of the chosen
   const float xs = lane < k ? row[id] : -INFINITY;
   float s;
-  if (sigmoid) {
+  if (kSigmoid) {
     s = xs > -INFINITY ? route_sigmoid(xs) : 0.f;
   } else if (r.renormalise) {
     float m = warp_max(xs);                        // relative to the largest chosen logit: never all underflowed
@@ -154,16 +246,6 @@ __device__ __forceinline__ void warp_select_scored(const float* __restrict__ row
     s = sum > 0.f ? __fdiv_rn(s, sum) : 0.f;
   }
   w = bad ? NAN : s * r.weight_scale;
-}
-
-__device__ __forceinline__ void warp_select_scored_any(const float* row, const float* bias, const moe_route_rule& r, int E,
-                                                       int k, int lane, float* rank, int& id, float& w) {
-  if (E <= 32) warp_select_scored<1>(row, bias, r, E, k, lane, rank, id, w);
-  else if (E <= 64) warp_select_scored<2>(row, bias, r, E, k, lane, rank, id, w);
-  else if (E <= 128) warp_select_scored<4>(row, bias, r, E, k, lane, rank, id, w);
-  else if (E <= 256) warp_select_scored<8>(row, bias, r, E, k, lane, rank, id, w);
-  else if (E <= 512) warp_select_scored<16>(row, bias, r, E, k, lane, rank, id, w);
-  else warp_select_scored<32>(row, bias, r, E, k, lane, rank, id, w);
 }
 
 }  // namespace moe

@@ -14,7 +14,6 @@
 #include <atomic>
 
 #include "moe_internal.h"
-#include "route_scored.cuh"
 #include "route_select.cuh"
 
 namespace {
@@ -40,41 +39,6 @@ route_topk_hist(const float* __restrict__ logits, int T, int E, int k, int token
     int sel_id;
     float sel_w;
     moe::warp_select_topk(logits + static_cast<size_t>(t) * E, E, k, lane, &sel_id, &sel_w);
-    if (lane < k) {
-      const size_t s = static_cast<size_t>(t) * k + lane;
-      topk_ids[s] = sel_id;
-      topk_w[s] = sel_w;
-      s_ids[(t - t_begin) * k + lane] = sel_id;
-    }
-  }
-  __syncthreads();
-  const int n_slots = (t_end - t_begin) * k;
-  if (tid < n_slots) atomicAdd(&s_hist[s_ids[tid]], 1);   // integer counts: order does not matter
-  __syncthreads();
-  for (int e = tid; e < E; e += kRouteThreads) chunk_hist[static_cast<size_t>(chunk) * E + e] = s_hist[e];
-}
-
-// The same for a scored rule.
-__global__ void __launch_bounds__(kRouteThreads)
-route_scored_hist(const float* __restrict__ logits, const float* __restrict__ bias, const moe_route_rule rule, int T,
-                  int E, int k, int tokens_per_chunk, int32_t* __restrict__ topk_ids, float* __restrict__ topk_w,
-                  int32_t* __restrict__ chunk_hist) {
-  extern __shared__ __align__(16) unsigned char smem_raw[];
-  const int warps = kRouteThreads / 32;
-  int32_t* s_hist = reinterpret_cast<int32_t*>(smem_raw);                 // [E]
-  int32_t* s_ids = s_hist + E;                                            // [256]
-  float* s_rank = reinterpret_cast<float*>(s_ids + kRouteThreads);        // [warps][E]
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int chunk = blockIdx.x;
-  const int t_begin = chunk * tokens_per_chunk;
-  const int t_end = min(T, t_begin + tokens_per_chunk);
-
-  for (int e = tid; e < E; e += kRouteThreads) s_hist[e] = 0;
-  for (int t = t_begin + warp; t < t_end; t += warps) {
-    int sel_id;
-    float sel_w;
-    moe::warp_select_scored_any(logits + static_cast<size_t>(t) * E, bias, rule, E, k, lane, s_rank + warp * E, sel_id,
-                                sel_w);
     if (lane < k) {
       const size_t s = static_cast<size_t>(t) * k + lane;
       topk_ids[s] = sel_id;
@@ -284,25 +248,6 @@ cudaError_t launch_plan_routing(moe_ctx* ctx, const float* logits, int32_t* topk
   const size_t smem3 = static_cast<size_t>(warps) * s.E * 4;
   route_topk_hist<<<ctx->num_chunks, kRouteThreads, smem1, stream>>>(logits, s.T, s.E, s.k, ctx->tokens_per_chunk,
                                                                      topk_ids, topk_w, ctx->d_chunk_hist);
-  moe_mark(ctx, 1, stream);
-  route_scan<<<1, 1024, 0, stream>>>(ctx->d_chunk_hist, ctx->d_chunk_base, ctx->num_chunks, s.E, counts, offsets);
-  moe_mark(ctx, 2, stream);
-  route_scatter<<<ctx->num_chunks, kRouteThreads, smem3, stream>>>(topk_ids, offsets, ctx->d_chunk_base, s.T, s.E,
-                                                                   s.k, ctx->tokens_per_chunk, perm, inv_perm);
-  moe_mark(ctx, 3, stream);
-  ctx->last_launches += 3;
-  return cudaGetLastError();
-}
-
-cudaError_t launch_plan_routing_scored(moe_ctx* ctx, const float* logits, const float* bias, const moe_route_rule& rule,
-                                       int32_t* topk_ids, float* topk_w, int32_t* counts, int32_t* offsets,
-                                       int32_t* perm, int32_t* inv_perm, cudaStream_t stream) {
-  const moe_shape& s = ctx->shape;
-  const int warps = kRouteThreads / 32;
-  const size_t smem1 = (static_cast<size_t>(s.E) + kRouteThreads + (rule.n_group > 1 ? warps * s.E : 0)) * 4;
-  const size_t smem3 = static_cast<size_t>(warps) * s.E * 4;
-  route_scored_hist<<<ctx->num_chunks, kRouteThreads, smem1, stream>>>(
-      logits, bias, rule, s.T, s.E, s.k, ctx->tokens_per_chunk, topk_ids, topk_w, ctx->d_chunk_hist);
   moe_mark(ctx, 1, stream);
   route_scan<<<1, 1024, 0, stream>>>(ctx->d_chunk_hist, ctx->d_chunk_base, ctx->num_chunks, s.E, counts, offsets);
   moe_mark(ctx, 2, stream);
