@@ -203,12 +203,16 @@ _torch = None
 
 
 def _stream(stream):
-    if stream is None:
-        global _torch
-        if _torch is None:
-            import torch as _torch
-        stream = _torch.cuda.current_stream()
-    return stream.cuda_stream
+    """cudaStream_t of a torch stream, by default the current one."""
+    if stream is not None:
+        return stream.cuda_stream
+    global _torch
+    if _torch is None:
+        import torch as _torch
+    raw = getattr(_torch._C, "_cuda_getCurrentRawStream", None)      # the handle without a Stream object around it
+    if raw is None:
+        return _torch.cuda.current_stream().cuda_stream
+    return raw(_torch.cuda.current_device())
 
 
 def _check(code: int, where: str):

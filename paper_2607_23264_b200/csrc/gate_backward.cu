@@ -1,8 +1,9 @@
 // Gradients of the gate: the combine's (to the expert rows and the weights) and the scored routing's (to the logits).
 //
-// combine_backward : a warp per slot (t, j).  It reads the token's d_out row and the slot's y row once, writes the
-//                    slot's d_y row and reduces the dot product (per-lane partial sums in fp32, then a fixed butterfly),
-//                    so nothing is accumulated across warps.  Algorithmic traffic: 2H(T + R) read, 2HR written.
+// combine_backward : one warp per slot (t, j), four where that leaves the SMs short of loads in flight.  They read the
+//                    token's d_out row and the slot's y row once, write the slot's d_y row and reduce the dot product
+//                    (per-lane partial sums in fp32, a fixed butterfly, then the warps in order).  Algorithmic traffic:
+//                    2H(T + R) read, 2HR written.
 // routing_backward : a warp per token.  The chosen experts' part is k values, one per lane; the row of d_logits is
 //                    written once, and the chosen entries again by the lanes that hold them.
 #include <cuda_bf16.h>
@@ -16,20 +17,22 @@ constexpr int kThreads = 256;
 constexpr int kAhead = 4;                 // 16-byte vectors of each row a lane has in flight
 constexpr unsigned kFull = 0xFFFFFFFFu;
 
+template <int kWarpsPerSlot>
 __global__ void __launch_bounds__(kThreads)
 combine_backward(const uint4* __restrict__ d_out, const uint4* __restrict__ y_perm, const int32_t* __restrict__ inv_perm,
                  const float* __restrict__ topk_w, uint4* __restrict__ d_y_perm, float* __restrict__ d_topk_w,
                  long long slots, int k, int vec_per_row) {
-  const int lane = threadIdx.x & 31;
-  const long long slot = static_cast<long long>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
-  if (slot >= slots) return;
+  __shared__ float s_part[kThreads / 32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % kWarpsPerSlot;
+  const long long slot = static_cast<long long>(blockIdx.x) * (kThreads / 32 / kWarpsPerSlot) + warp / kWarpsPerSlot;
+  if (slot >= slots) return;                                // (all warps of a slot alike)
   const size_t row = static_cast<size_t>(inv_perm[slot]);
   const float w = topk_w[slot];
   const uint4* g = d_out + static_cast<size_t>(slot / k) * vec_per_row;
   const uint4* y = y_perm + row * vec_per_row;
   uint4* d = d_y_perm ? d_y_perm + row * vec_per_row : nullptr;
   float dot = 0.f;
-  for (int v0 = lane; v0 < vec_per_row; v0 += 32 * kAhead) {
+  for (int v0 = part * 32 * kAhead + lane; v0 < vec_per_row; v0 += kWarpsPerSlot * 32 * kAhead) {
     uint4 gv[kAhead], yv[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
@@ -58,7 +61,14 @@ combine_backward(const uint4* __restrict__ d_out, const uint4* __restrict__ y_pe
     }
   }
   dot = moe::warp_sum(dot);
-  if (lane == 0) d_topk_w[slot] = dot;
+  if constexpr (kWarpsPerSlot > 1) {
+    if (lane == 0) s_part[warp] = dot;
+    // the warps of the slot only: the last CTA's others may be gone
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + warp / kWarpsPerSlot), "r"(32 * kWarpsPerSlot) : "memory");
+    dot = 0.f;
+    for (int i = 0; i < kWarpsPerSlot; ++i) dot += s_part[warp - part + i];
+  }
+  if (part == 0 && lane == 0) d_topk_w[slot] = dot;
 }
 
 // Lane l holds the logits l, l + 32, ... of the token (EL of them, E <= 32 * EL): the row is read once and written once.
@@ -153,8 +163,10 @@ cudaError_t launch_combine_backward(moe_ctx* ctx, const void* d_out, const void*
                                     const float* topk_w, void* d_y_perm, float* d_topk_w, cudaStream_t stream) {
   const moe_shape& s = ctx->shape;
   const long long slots = static_cast<long long>(s.T) * s.k;
-  const int per_block = kThreads / 32;
-  combine_backward<<<static_cast<unsigned>((slots + per_block - 1) / per_block), kThreads, 0, stream>>>(
+  // 301 tokens x 8 experts of 7168: 21 us with one warp per slot
+  const int warps = slots < 24LL * ctx->num_sms ? 4 : 1, per_block = kThreads / 32 / warps;
+  auto kernel = warps == 4 ? combine_backward<4> : combine_backward<1>;
+  kernel<<<static_cast<unsigned>((slots + per_block - 1) / per_block), kThreads, 0, stream>>>(
       static_cast<const uint4*>(d_out), static_cast<const uint4*>(y_perm), inv_perm, topk_w,
       static_cast<uint4*>(d_y_perm), d_topk_w, slots, s.k, s.H / 8);
   ctx->last_launches += 1;

@@ -610,6 +610,7 @@ gemm_blk(const __grid_constant__ RowMaps tm_a, const __grid_constant__ CUtensorM
         const CUtensorMap* ma = &tm_a.of[blk_height_index(tile.rows)];
         for (int kb = kb0; kb < kb1; ++kb) {
           ptx::mbar_wait_or_flag(ptx::smem_u32(&st->empty[stage]), phase, abort_flag, kRoleTma);
+          if (__any_sync(0xFFFFFFFFu, *abort_flag)) break;           // no copies into stages that are not free
           const uint32_t full = ptx::smem_u32(&st->full[stage]);
           const uint32_t s = ring_u32 + stage * G::kStageBytes;
           if constexpr (kPair) {

@@ -127,7 +127,7 @@ scored_prefix(const ScoredParams p, int chunks) {
   const int lane = threadIdx.x & 31, e = blockIdx.x * kWarps + (threadIdx.x >> 5);
   if (e >= p.E) return;
   int run = 0;
-  constexpr int kAhead = 4;                                 // 32-chunk groups whose loads are in flight together
+  constexpr int kAhead = 16;                                // 32-chunk groups whose loads are in flight together
   for (int c0 = 0; c0 < chunks; c0 += 32 * kAhead) {
     int v[kAhead];
 #pragma unroll

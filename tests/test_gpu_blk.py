@@ -118,6 +118,7 @@ def check_product(y, a, sa, offsets, b, N, K):
     ([129], 520, 1040), ([200], 384, 640), ([257], 256, 2048), ([700], 512, 512), ([1], 4096, 7168), ([33], 2104, 4112),
     ([0, 1, 0, 5, 16], 136, 256), ([3, 0, 40, 130, 0, 64], 264, 400), ([17, 15, 48, 49, 96, 97, 112, 113], 128, 128),
     ([300, 2, 0, 270], 640, 1152), ([1] * 200, 64, 128), ([0] * 9 + [2] + [0] * 1000, 72, 128),
+    ([20] * 700, 8, 16), ([193] * 660, 8, 16), ([128, 140, 64, 65, 66, 129], 520, 784), ([1025, 900, 1], 264, 272),
 ])
 def test_product(ctx, counts, N, K):
     rng = np.random.default_rng(N + K + len(counts))
@@ -261,6 +262,8 @@ def cfg_of(T, H, F, E, k, seed, router="xWr"):
     (1, 256, 128, 3, 1, "xWr"),
     (70, 128, 128, 1024, 32, "xWr"),
     (700, 256, 384, 2, 2, "xWr"),
+    (600, 384, 256, 8, 2, "xWr"),
+    (256, 256, 384, 3, 2, "xWr"),
 ])
 def test_expert_ffn_parity(T, H, F, E, k, router):
     cfg = cfg_of(T, H, F, E, k, seed=T + H, router=router)
@@ -395,3 +398,62 @@ def test_fused_forward_of_a_token_with_every_expert_masked_is_zero():
     assert out[7].eq(0).all()
     keep = [t for t in range(cfg.T) if t != 7]
     assert torch.equal(out[keep].view(torch.int16), ref[keep].view(torch.int16))
+
+
+def test_router_tuning_example_learns():
+    """The example runs every new call as a training loop would: 20 steps take the loss clearly down."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "tune_router.py")
+    spec = importlib.util.spec_from_file_location("tune_router", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    losses = example.main(["--steps", "20"])
+    assert losses[-1] < 0.9 * losses[0]
+
+
+def test_layer_equals_its_separate_calls():
+    """moe_fused_forward_blk gives the bits of plan, quantise, dispatch, experts and combine called one by one."""
+    cfg = cfg_of(200, 512, 256, 16, 3, seed=44)
+    M = BlkLayer(cfg)
+    L, ctx = M.L, M.L.ctx
+    T, H, F, R = cfg.T, cfg.H, cfg.F, cfg.R
+    rule = binding.make_route_rule("sigmoid", 4, 3, 1, True, 1.5)
+    bias = dev((np.arange(cfg.E) % 3 / 16).astype(np.float32))
+    ws = torch.empty(ctx.workspace_layout_blk()["total"], dtype=torch.uint8, device=DEV)
+    fused, apart = L.nan_bf16(T, H), L.nan_bf16(T, H)
+    ctx.moe_fused_forward_blk(L.x, L.d_logits, bias, rule, *M.weights(), fused, ws)
+    assert ctx.moe_last_launch_count() in (5, 7)
+    ctx.moe_plan_routing_scored(L.d_logits, bias, rule, L.topk_ids, L.topk_w, L.counts, L.offsets, L.perm, L.inv_perm)
+    u8 = dict(dtype=torch.uint8, device=DEV)
+    xq, sx, xp, sxp = torch.empty(T, H, **u8), torch.empty(H // 128, T, device=DEV), torch.empty(R, H, **u8), torch.empty(H // 128, R, device=DEV)
+    hq, sh, y = torch.empty(R, F, **u8), torch.empty(F // 128, R, device=DEV), L.nan_bf16(R, H)
+    ctx.moe_quantize_rows_blk(L.x, T, H, xq, sx)
+    ctx.moe_dispatch_blk(xq, sx, L.inv_perm, xp, sxp)
+    ctx.moe_expert_ffn_blk(xp, sxp, L.offsets, *M.weights(), hq, sh, y)
+    ctx.moe_combine(y, L.inv_perm, L.topk_w, apart)
+    torch.cuda.synchronize()
+    L.check_device_status()
+    assert torch.equal(fused.view(torch.int16), apart.view(torch.int16))
+    lay = ctx.workspace_layout_blk()
+    assert torch.equal(ws[lay["xq_perm"]:lay["xq_perm"] + R * H], xp.view(-1))
+    assert torch.equal(ws[lay["sx_perm"]:lay["sx_perm"] + 4 * R * (H // 128)].view(torch.float32), sxp.view(-1))
+
+
+def test_calls_can_be_captured_in_a_graph():
+    cfg = cfg_of(48, 256, 128, 8, 2, seed=45)
+    M = BlkLayer(cfg)
+    L, ctx = M.L, M.L.ctx
+    rule = binding.make_route_rule("softmax")
+    ws = torch.empty(ctx.workspace_layout_blk()["total"], dtype=torch.uint8, device=DEV)
+    eager, out = L.nan_bf16(cfg.T, cfg.H), L.nan_bf16(cfg.T, cfg.H)
+    ctx.moe_fused_forward_blk(L.x, L.d_logits, None, rule, *M.weights(), eager, ws)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            ctx.moe_fused_forward_blk(L.x, L.d_logits, None, rule, *M.weights(), out, ws)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out.view(torch.int16), eager.view(torch.int16))
