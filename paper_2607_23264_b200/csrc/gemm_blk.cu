@@ -16,7 +16,7 @@
 //     and one of the two weight boxes: 32 KB per block of K, 64 bytes per clock at the tensor rate, which is what an SM
 //     takes in from L2, where a single CTA's 48 KB would need 96.  A single CTA keeps twice the weight bytes in flight,
 //     which is what counts while the weights come from HBM (launch_product gives the measured rule).
-// Shapes with too few tiles for the SMs split K over a cluster of 2, 4 or 8 CTAs, which add their running sums through
+// Shapes with too few tiles for the SMs split K over a cluster of up to eight CTAs, which add their running sums through
 // distributed shared memory in rank order: no scratch memory, no atomics, the same bits every time.
 //
 // Roles (384 threads, 168 registers each at launch, moved to where they are needed): warp 0 = TMA producer, warps 1 and
@@ -782,6 +782,23 @@ bool encode_rows(moe_ctx* ctx, RowMaps* maps, const BlkProduct& g, int rows) {
   return true;
 }
 
+// The most tiles the rows can make (exact for one group): ceil(r / b) <= (r - 1) / b + 1 for each of at most `some` groups
+// with rows.  The kernel counts the real ones from the offsets.
+long long most_tiles(const BlkParams& p, int block_rows) {
+  const long long some = p.groups < p.rows ? p.groups : p.rows;
+  return ((p.rows - some) / block_rows + some) * p.n_tiles;
+}
+
+// CTAs per tile along K: the most, up to eight, for which every tile's cluster is resident at once, and no more than give
+// each CTA fewer blocks.  (A cluster lies within a GPC: sixteen clusters of eight do not fit, and a second wave costs more
+// than the longer loops: 17 rows, 4096 x 7168 took 18 us with eight CTAs per tile and 12 with four.)
+int k_split(const moe_ctx* ctx, long long tiles, int k_blocks) {
+  int split = 8;
+  while (split > 1 && (split > k_blocks || tiles > ctx->blk_clusters[split])) --split;
+  while (split > 1 && (k_blocks + split - 2) / (split - 1) == (k_blocks + split - 1) / split) --split;
+  return split;
+}
+
 template <bool kGated, int kCtas, int kMaxN>
 moe_status launch_tiles(moe_ctx* ctx, const BlkProduct& g, BlkParams p, cudaStream_t stream) {
   using G = BlkGeom<kCtas, kMaxN>;
@@ -796,12 +813,8 @@ moe_status launch_tiles(moe_ctx* ctx, const BlkProduct& g, BlkParams p, cudaStre
   p.stages = static_cast<int>((kMaxSmem - rest) / G::kStageBytes);           // 3 to 6
   if (p.stages > kMaxStages) p.stages = kMaxStages;
   const size_t smem = rest + static_cast<size_t>(p.stages) * G::kStageBytes;
-  // the most tiles the rows can make; the kernel counts the real ones from the offsets
-  const long long blocks = p.rows / (kCtas * kMaxN) + (p.groups < p.rows ? p.groups : p.rows);
-  const long long tiles = blocks * p.n_tiles;
-  p.split = 1;
-  if (kCtas == 1)
-    while (p.split < 8 && 2 * p.split * tiles <= ctx->num_sms && 2 * p.split <= p.k_blocks) p.split *= 2;
+  const long long tiles = most_tiles(p, kCtas * kMaxN);
+  p.split = kCtas == 2 ? 1 : k_split(ctx, tiles, p.k_blocks);
   const int team = kCtas == 2 ? 2 : p.split;
   const long long room = kCtas == 2 ? ctx->max_pairs : ctx->num_sms / team;
   cudaLaunchConfig_t cfg{};
@@ -824,7 +837,15 @@ moe_status launch_tiles(moe_ctx* ctx, const BlkProduct& g, BlkParams p, cudaStre
 template <bool kGated>
 moe_status launch_product(moe_ctx* ctx, const BlkProduct& g, const BlkParams& p, cudaStream_t stream) {
   const long long pair_rows = moe_knob_value(ctx, "blk_pair_rows", 192), few_rows = moe_knob_value(ctx, "blk_few_rows", 16);
-  if (p.rows > pair_rows * p.groups) return launch_tiles<kGated, 2, 128>(ctx, g, p, stream);
+  if (p.rows > pair_rows * p.groups) {
+    // Where the pairs have one tile each at most, single CTAs with K split may be done sooner (their blocks of K take
+    // about a fifth longer): 512 rows, 4096 x 7168.
+    const long long pair_tiles = most_tiles(p, 256), tiles = most_tiles(p, 128);
+    const int split = k_split(ctx, tiles, p.k_blocks);
+    if (pair_tiles > ctx->max_pairs || tiles > ctx->num_sms || 6LL * ((p.k_blocks + split - 1) / split) >= 5LL * p.k_blocks)
+      return launch_tiles<kGated, 2, 128>(ctx, g, p, stream);
+    return launch_tiles<kGated, 1, 128>(ctx, g, p, stream);
+  }
   if (p.rows > few_rows * p.groups) return launch_tiles<kGated, 1, 128>(ctx, g, p, stream);
   return launch_tiles<kGated, 1, 32>(ctx, g, p, stream);
 }
@@ -834,13 +855,27 @@ moe_status launch_product(moe_ctx* ctx, const BlkProduct& g, const BlkParams& p,
 namespace moe {
 
 cudaError_t prepare_gemm_blk(moe_ctx* ctx) {
-  (void)ctx;
   const void* kernels[] = {
       reinterpret_cast<const void*>(gemm_blk<true, 1, 32>),  reinterpret_cast<const void*>(gemm_blk<false, 1, 32>),
       reinterpret_cast<const void*>(gemm_blk<true, 1, 128>), reinterpret_cast<const void*>(gemm_blk<false, 1, 128>),
       reinterpret_cast<const void*>(gemm_blk<true, 2, 128>), reinterpret_cast<const void*>(gemm_blk<false, 2, 128>)};
   for (const void* k : kernels) {
     const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
+    if (e != cudaSuccess) return e;
+  }
+  for (int n = 1; n <= 8; ++n) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(n);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kMaxSmem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = n;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaOccupancyMaxActiveClusters(&ctx->blk_clusters[n], gemm_blk<false, 1, 128>, &cfg);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;

@@ -50,6 +50,7 @@ struct moe_ctx {
   moe_knob knobs[kMoeMaxKnobs];
   int device;
   int num_sms;
+  int blk_clusters[9];   // clusters of n CTAs of the block-scaled product that can be resident at once (n = 1..8)
   int max_pairs;         // CTA pairs (clusters of two) of the pair kernel that can be resident at once
   int max_tokens;        // T given at creation: the size of the routing scratch; shape.T is the active batch
   int tokens_per_chunk;  // routing: tokens handled by one CTA, so that a chunk has at most 256 slots
