@@ -11,12 +11,13 @@ __device__ __forceinline__ float scale_of(float amax) { return amax > 0.f ? __fd
 
 // Division of many values by one scale: quotient from the correctly rounded reciprocal, its remainder by one fused
 // multiply-add, and the correction by another (Markstein's scheme), three instructions per value where a general division
-// takes about ten.
+// takes about ten.  The remainder is taken with its sign turned, q scale - v: so a negative zero keeps its sign (v - q scale
+// would be +0 + -0 = +0 and turn it).
 struct FastDivider {
   float scale, reciprocal;
   __device__ __forceinline__ float operator()(float v) const {
     const float q = v * reciprocal;
-    return fmaf(fmaf(-q, scale, v), reciprocal, q);
+    return fmaf(fmaf(q, scale, -v), -reciprocal, q);
   }
 };
 // Scales so small that the reciprocal or the remainder leaves the normal range, and infinite ones (2^-100 .. 2^100 are

@@ -65,6 +65,19 @@ def test_quantize_weights_bits(ctx, mats, rows, cols):
         assert np.array_equal(codes[m].cpu().numpy(), ref_c)
 
 
+def test_quantize_keeps_the_sign_of_zero(ctx):
+    v = np.tile(np.array([-0.0, 0.0, 1.0, -1e-30], dtype=np.float32), (128, 32))
+    codes = torch.full((128, 128), 0x7F, dtype=torch.uint8, device=DEV)
+    scales = torch.zeros(1, 128, device=DEV)
+    x = bits_to_dev(gen.f32_to_bf16_bits(v))
+    ctx.moe_quantize_rows_blk(x, 128, 128, codes, scales)
+    torch.cuda.synchronize()
+    assert np.array_equal(codes.cpu().numpy(), blk.quantize_rows(v)[0])
+    ctx.moe_quantize_weights_blk(x, 1, 128, 128, codes, scales)
+    torch.cuda.synchronize()
+    assert np.array_equal(codes.cpu().numpy(), blk.quantize_weights(v)[0])
+
+
 def test_quantize_keeps_nan_and_infinity_visible(ctx):
     v = np.ones((2, 256), dtype=np.float32)
     v[0, 3], v[0, 130], v[1, 255] = np.nan, np.inf, -np.inf
@@ -119,6 +132,7 @@ def check_product(y, a, sa, offsets, b, N, K):
     ([0, 1, 0, 5, 16], 136, 256), ([3, 0, 40, 130, 0, 64], 264, 400), ([17, 15, 48, 49, 96, 97, 112, 113], 128, 128),
     ([300, 2, 0, 270], 640, 1152), ([1] * 200, 64, 128), ([0] * 9 + [2] + [0] * 1000, 72, 128),
     ([20] * 700, 8, 16), ([193] * 660, 8, 16), ([128, 140, 64, 65, 66, 129], 520, 784), ([1025, 900, 1], 264, 272),
+    ([1025, 1300], 264, 272), ([2000], 520, 1040),
 ])
 def test_product(ctx, counts, N, K):
     rng = np.random.default_rng(N + K + len(counts))
@@ -129,6 +143,21 @@ def test_product(ctx, counts, N, K):
         assert torch.equal(run_product(ctx, a, sa, offsets, b, N, K, use_offsets=False).view(torch.int16), y.view(torch.int16))
     again = run_product(ctx, a, sa, offsets, b, N, K, stream=torch.cuda.Stream())
     assert torch.equal(again.view(torch.int16), y.view(torch.int16)), "not the same bits on another stream"
+
+
+@pytest.mark.parametrize("knobs", ["x.blk_pair_rows=0", "x.blk_pair_rows=1073741824,x.blk_few_rows=0",
+                                   "x.blk_pair_rows=1073741824,x.blk_few_rows=1073741824"])
+@pytest.mark.parametrize("counts,N,K", [
+    ([1, 0, 31, 33, 64, 65], 136, 144), ([127, 128, 129, 255, 256, 257], 264, 1040), ([513], 1032, 2064),
+    ([1300, 1100], 520, 400),
+])
+def test_product_by_every_kind_of_tile(monkeypatch, knobs, counts, N, K):
+    """The tile is chosen by the average rows per group; each kind has to be right for every group all the same."""
+    monkeypatch.setenv("MOE_TUNING", knobs)
+    forced = binding.Context(1, 64, 64, 1, 1)
+    rng = np.random.default_rng(N + K)
+    a, sa, offsets, b = make_product(rng, counts, N, K, tail=2)
+    check_product(run_product(forced, a, sa, offsets, b, N, K), a, sa, offsets, b, N, K)
 
 
 def test_product_random_shapes(ctx):
@@ -264,6 +293,8 @@ def cfg_of(T, H, F, E, k, seed, router="xWr"):
     (700, 256, 384, 2, 2, "xWr"),
     (600, 384, 256, 8, 2, "xWr"),
     (256, 256, 384, 3, 2, "xWr"),
+    (1900, 256, 384, 2, 2, "xWr"),
+    (2300, 128, 256, 4, 2, "xWr"),
 ])
 def test_expert_ffn_parity(T, H, F, E, k, router):
     cfg = cfg_of(T, H, F, E, k, seed=T + H, router=router)
