@@ -507,9 +507,9 @@ moe_status moe_dispatch_blk(moe_ctx* ctx, const void* xq, const float* sx, const
 /*
  * The product y[r, n] = sum_k a[r, k] b[g, n, k] for the rows offsets[g] <= r < offsets[g+1] of each group g:
  *     y[r,n] = bf16( sum_b sa[b][r] * sb[g][n/128][b] * sum_{k in block b} code_a[r,k] code_b[g,n,k] )
- * with fp32 sums.  The shape is the argument's, not the context's (which lends its device, its status word and its
- * scheduler counters).  offsets NULL: one matrix for all rows (groups must be 1).  Rows outside every group are not
- * written; a group without rows is not read.  The gradient with respect to a is the same call on the transposed
+ * with fp32 sums.  The shape is the argument's, not the context's (which lends its device and its status word).
+ * offsets NULL: one matrix for all rows (groups must be 1).  Rows outside every group are not written; a group without
+ * rows is not read.  The gradient with respect to a is the same call on the transposed
  * weights: their blocks and scales are the transposed ones.
  * Limits: K a multiple of 16, N a multiple of 8, 1 <= groups <= 1024, 0 <= rows < 2^30, groups * N < 2^31.
  */

@@ -836,7 +836,19 @@ moe_status launch_tiles(moe_ctx* ctx, const BlkProduct& g, BlkParams p, cudaStre
 
 template <bool kGated>
 moe_status launch_product(moe_ctx* ctx, const BlkProduct& g, const BlkParams& p, cudaStream_t stream) {
-  const long long pair_rows = moe_knob_value(ctx, "blk_pair_rows", 192), few_rows = moe_knob_value(ctx, "blk_few_rows", 16);
+  // By the average rows per group, us, equal groups, CTA pairs / single CTAs:
+  //     64 groups, 2048 x 7168:  128 rows 238/185   192 251/246   256 265/276   300 448/361   384 507/388   512 527/496
+  //      8 groups, 4096 x 7168:  512 rows 127/132   600 177/161   700 181/184   800 216/209  1024 225/236  2048 434/461
+  //     16 groups, 7168 x 2048:  512 rows 142/145  1024 260/272  2048 500/529
+  // A pair's tile has 256 rows, and the last of a group is padded to them: from about four full tiles on, the pair's 2 to
+  // 6 % outweigh that whatever the remainder (a layer of 64 experts with 128 rows each on average: 3.50 ms with pairs,
+  // 2.59 ms without).
+  const long long pair_rows = moe_knob_value(ctx, "blk_pair_rows", 900);
+  // Single CTAs with boxes of at most 32 rows have room for five stages, those of 128 rows for four, which do more rows
+  // with each read of the weights; us, 32 / 128: 64 groups, 2048 x 7168: 2 rows 144.7/149.8, 16 144.7/148.2, 32
+  // 147.3/151.2, 40 164.6/154.3; 128 groups, 7168 x 2048: 2 rows 281/281, 16 287/286, 24 300/296, 32 314/303.  On average
+  // 16, because groups above 32 rows are the rule when the average is 32.
+  const long long few_rows = moe_knob_value(ctx, "blk_few_rows", 16);
   if (p.rows > pair_rows * p.groups) {
     // Where the pairs have one tile each at most, single CTAs with K split may be done sooner (their blocks of K take
     // about a fifth longer): 512 rows, 4096 x 7168.
