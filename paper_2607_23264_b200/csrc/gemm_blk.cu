@@ -19,6 +19,18 @@
 // Shapes with too few tiles for the SMs split K over a cluster of up to eight CTAs, which add their running sums through
 // distributed shared memory in rank order: no scratch memory, no atomics, the same bits every time.
 //
+// What bounds it and what it measured (E4M3 both, 2 x rows x N x K operations, events over back-to-back runs):
+//   few rows: the weights' bytes.  64 groups of 2 rows, 2048 x 7168: 143 us, 6.56 TB/s; 17 rows, 4096 x 7168: 11.7 us,
+//     of which about 5 are the launch and the cluster's sums.
+//   128 rows a group: 184 us, 5.6 TB/s, 1.3 PFLOP/s: the drain of the accumulators, 256 x 128 multiply-adds per block of
+//     K and 128-row tile on the CUDA cores beside the loads.
+//   many rows: 8 groups of 2048, 4096 x 7168: 437 us, 2.2 PFLOP/s.  The scale per block of 128 makes every accumulator
+//     leave tensor memory after four instructions, so the epilogue's loads and multiply-adds (about 800 clocks per block
+//     and SM, against 512 of the tensor pipe) bound the tile; under a long load the power cap does: 8192 rows, 4096 x
+//     7168 take 212 us from rest and 256 sustained.
+// Measured and not kept: prefetching the weights into L2 some blocks ahead (143 -> 180 us at 2 rows), 32 accumulator
+// columns per load and packed pairs of multiply-adds (more registers, slower), sixteen epilogue warps.
+//
 // Roles (384 threads, 168 registers each at launch, moved to where they are needed): warp 0 = TMA producer, warps 1 and
 // 3 = MMA issuers (even and odd blocks of K), warp 2 = scale loader (sa * sb per row and weight box, through a ring in
 // shared memory), warps 4-11 = epilogue (four lane quarters x two halves; 128 running sums per thread at most).

@@ -1,12 +1,17 @@
 // The routing plan by a scored rule (moe_plan_routing_scored): selection, histogram, prefixes, stable permutation.
 //
-// Small batches are planned by one launch, a cluster of eight CTAs: every CTA selects the experts of its eighth of the tokens (a warp per token at a time), the histograms of all eight are read through distributed shared
-// memory, and every CTA scans the totals and places its own slots.  Larger ones take three launches:
+// Small batches are planned by one launch, a cluster of eight CTAs: every CTA selects the experts of its eighth of the
+// tokens (a warp per token at a time), the histograms of all eight are read through distributed shared memory, and every
+// CTA scans the totals and places its own slots.  Larger ones take three launches:
 //   1. scored_select : a CTA per chunk of at most 256 slots; a warp per token; the chunk's histogram.
 //   2. scored_prefix : a warp per expert; exclusive prefix of the chunk histograms over the chunks, and the total.
 //   3. scored_place  : a CTA per chunk; scans the totals over the experts (every CTA for itself: 1024 at most) and places
 //                      its slots: (slots of earlier chunks) + (of earlier warps in the chunk) + (of earlier lanes).
 // Integer work on decisions that are reproducible bit for bit, so the plan is too.
+//
+// Bound by instructions, not by bytes: 16384 tokens over 256 experts move 19 MB (2.9 us at the copy rate), and the plan
+// takes 34.6 us (graph replay): 27 us of selection, about 1000 warp instructions a token at two thirds of the issue rate,
+// then two short launches.  4099 tokens over 96 experts: 15.6 us.  64 tokens over 256 experts, one launch: 7.1 us.
 #include <type_traits>
 
 #include "moe_internal.h"
@@ -40,15 +45,21 @@ struct ScoredParams {
 };
 
 // Tokens [t_begin, t_end) of this CTA: ids and weights to global memory, ids to s_ids, their histogram to s_hist (zero).
-template <int EL, bool kSigmoid, bool kGroups>
+template <int EL, bool kSigmoid, int kLayout>
 __device__ __forceinline__ void select_chunk(const ScoredParams& p, int t_begin, int t_end, int32_t* s_ids, int32_t* s_hist,
                                              float* s_sel) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  float next[EL];
+  if (t_begin + warp < t_end) moe::load_logits<EL, kLayout>(p.logits + static_cast<size_t>(t_begin + warp) * p.E, p.E, lane, next);
   for (int t = t_begin + warp; t < t_end; t += kWarps) {
+    const float* row = p.logits + static_cast<size_t>(t) * p.E;
+    float x[EL];
+#pragma unroll
+    for (int i = 0; i < EL; ++i) x[i] = next[i];
+    if (t + kWarps < t_end) moe::load_logits<EL, kLayout>(row + static_cast<size_t>(kWarps) * p.E, p.E, lane, next);
     int id;
     float w;
-    moe::warp_select_scored<EL, kSigmoid, kGroups>(p.logits + static_cast<size_t>(t) * p.E, p.bias, p.rule, p.E, p.k, lane,
-                                                   s_sel + warp * p.warp_floats, id, w);
+    moe::warp_select_scored<EL, kSigmoid, kLayout>(row, x, p.bias, p.rule, p.E, p.k, lane, s_sel + warp * p.warp_floats, id, w);
     if (lane < p.k) {
       const size_t s = static_cast<size_t>(t) * p.k + lane;
       p.topk_ids[s] = id;
@@ -107,7 +118,7 @@ __device__ __forceinline__ void place_slots(const int32_t* s_ids, int n_slots, i
   }
 }
 
-template <int EL, bool kSigmoid, bool kGroups>
+template <int EL, bool kSigmoid, int kLayout>
 __global__ void __launch_bounds__(kRouteThreads)
 scored_select(const ScoredParams p) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
@@ -117,7 +128,7 @@ scored_select(const ScoredParams p) {
   const int t_begin = blockIdx.x * p.tokens_per_chunk, t_end = min(p.T, t_begin + p.tokens_per_chunk);
   for (int e = threadIdx.x; e < p.E; e += kRouteThreads) s_hist[e] = 0;
   __syncthreads();
-  select_chunk<EL, kSigmoid, kGroups>(p, t_begin, t_end, s_ids, s_hist, s_sel);
+  select_chunk<EL, kSigmoid, kLayout>(p, t_begin, t_end, s_ids, s_hist, s_sel);
   __syncthreads();
   for (int e = threadIdx.x; e < p.E; e += kRouteThreads) p.chunk_hist[static_cast<size_t>(blockIdx.x) * p.E + e] = s_hist[e];
 }
@@ -177,7 +188,7 @@ scored_place(const ScoredParams p) {
   place_slots(s_ids, n_slots, t_begin * p.k, s_start, p.E, s_cnt, p.perm, p.inv_perm);
 }
 
-template <int EL, bool kSigmoid, bool kGroups>
+template <int EL, bool kSigmoid, int kLayout>
 __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kRouteThreads)
 scored_plan_small(const ScoredParams p) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
@@ -193,7 +204,7 @@ scored_plan_small(const ScoredParams p) {
   for (int e = tid; e < p.E; e += kRouteThreads) s_hist[e] = 0;
   for (int i = tid; i < kWarps * p.E; i += kRouteThreads) s_cnt[i] = 0;
   __syncthreads();
-  select_chunk<EL, kSigmoid, kGroups>(p, t_begin, t_end, s_ids, s_hist, s_sel);
+  select_chunk<EL, kSigmoid, kLayout>(p, t_begin, t_end, s_ids, s_hist, s_sel);
   __syncthreads();
   ptx::cluster_sync();                                      // every CTA's histogram stands
   const uint32_t hist_u32 = ptx::smem_u32(s_hist);
@@ -225,20 +236,28 @@ scored_plan_small(const ScoredParams p) {
   place_slots(s_ids, (t_end - t_begin) * p.k, t_begin * p.k, s_start, p.E, s_cnt, p.perm, p.inv_perm);
 }
 
-// Calls f with the selection's template arguments: entries per lane, sigmoid, groups.
+// Calls f with the selection's template arguments: entries per lane, sigmoid, layout (bias_on_grid: the bias can be read
+// 16 bytes at a time, as the logits always can).
 template <typename F>
-cudaError_t with_rule(int E, const moe_route_rule& r, F f) {
-  auto by_el = [&](auto sigmoid, auto groups) {
-    if (E <= 32) return f(std::integral_constant<int, 1>{}, sigmoid, groups);
-    if (E <= 64) return f(std::integral_constant<int, 2>{}, sigmoid, groups);
-    if (E <= 128) return f(std::integral_constant<int, 4>{}, sigmoid, groups);
-    if (E <= 256) return f(std::integral_constant<int, 8>{}, sigmoid, groups);
-    if (E <= 512) return f(std::integral_constant<int, 16>{}, sigmoid, groups);
-    return f(std::integral_constant<int, 32>{}, sigmoid, groups);
+cudaError_t with_rule(int E, const moe_route_rule& r, bool bias_on_grid, F f) {
+  auto by_el = [&](auto sigmoid, auto layout) {
+    if constexpr (decltype(layout)::value != moe::kOwnGroups) {
+      if (E <= 32) return f(std::integral_constant<int, 1>{}, sigmoid, layout);
+      if (E <= 64) return f(std::integral_constant<int, 2>{}, sigmoid, layout);
+    }
+    if (E <= 128) return f(std::integral_constant<int, 4>{}, sigmoid, layout);
+    if (E <= 256) return f(std::integral_constant<int, 8>{}, sigmoid, layout);
+    if (E <= 512) return f(std::integral_constant<int, 16>{}, sigmoid, layout);
+    return f(std::integral_constant<int, 32>{}, sigmoid, layout);
   };
-  if (r.score == MOE_SCORE_SIGMOID)
-    return r.n_group > 1 ? by_el(std::true_type{}, std::true_type{}) : by_el(std::true_type{}, std::false_type{});
-  return r.n_group > 1 ? by_el(std::false_type{}, std::true_type{}) : by_el(std::false_type{}, std::false_type{});
+  auto by_layout = [&](auto sigmoid) {
+    const bool powers = (E & (E - 1)) == 0 && (r.n_group & (r.n_group - 1)) == 0;
+    if (r.n_group == 1) return by_el(sigmoid, std::integral_constant<int, moe::kNoGroups>{});
+    if (powers && E >= 128 && bias_on_grid)
+      return by_el(sigmoid, std::integral_constant<int, moe::kOwnGroups>{});
+    return by_el(sigmoid, std::integral_constant<int, moe::kAnyGroups>{});
+  };
+  return r.score == MOE_SCORE_SIGMOID ? by_layout(std::true_type{}) : by_layout(std::false_type{});
 }
 
 }  // namespace
@@ -265,13 +284,14 @@ cudaError_t launch_plan_routing_scored(moe_ctx* ctx, const float* logits, const 
   p.offsets = offsets;
   p.perm = perm;
   p.inv_perm = inv_perm;
+  const bool bias_on_grid = (reinterpret_cast<uintptr_t>(bias) & 15u) == 0;
   const size_t select_bytes = static_cast<size_t>(kWarps) * p.warp_floats * 4;
   const int per_cta = (s.T + kCluster - 1) / kCluster;
   if (per_cta <= kSmallTokens && per_cta * s.k <= kRouteThreads) {
     p.tokens_per_chunk = per_cta;
     const size_t smem = (3 * static_cast<size_t>(s.E) + kWarps + kRouteThreads) * 4 + select_bytes + kWarps * s.E;
-    const cudaError_t e = with_rule(s.E, rule, [&](auto el, auto sigmoid, auto groups) {
-      auto kernel = scored_plan_small<decltype(el)::value, decltype(sigmoid)::value, decltype(groups)::value>;
+    const cudaError_t e = with_rule(s.E, rule, bias_on_grid, [&](auto el, auto sigmoid, auto layout) {
+      auto kernel = scored_plan_small<decltype(el)::value, decltype(sigmoid)::value, decltype(layout)::value>;
       kernel<<<kCluster, kRouteThreads, smem, stream>>>(p);
       return cudaGetLastError();
     });
@@ -284,8 +304,8 @@ cudaError_t launch_plan_routing_scored(moe_ctx* ctx, const float* logits, const 
   p.tokens_per_chunk = ctx->tokens_per_chunk;
   const size_t smem1 = (static_cast<size_t>(s.E) + kRouteThreads) * 4 + select_bytes;
   const size_t smem3 = (2 * static_cast<size_t>(s.E) + kWarps + kRouteThreads) * 4 + kWarps * s.E;
-  const cudaError_t e = with_rule(s.E, rule, [&](auto el, auto sigmoid, auto groups) {
-    auto kernel = scored_select<decltype(el)::value, decltype(sigmoid)::value, decltype(groups)::value>;
+  const cudaError_t e = with_rule(s.E, rule, bias_on_grid, [&](auto el, auto sigmoid, auto layout) {
+    auto kernel = scored_select<decltype(el)::value, decltype(sigmoid)::value, decltype(layout)::value>;
     kernel<<<ctx->num_chunks, kRouteThreads, smem1, stream>>>(p);
     return cudaGetLastError();
   });
@@ -302,15 +322,17 @@ cudaError_t launch_plan_routing_scored(moe_ctx* ctx, const float* logits, const 
 // One-time kernel attributes: the selection's shared memory passes 48 KB at the largest E with many groups.
 cudaError_t prepare_plan_scored(moe_ctx* ctx) {
   const int E = ctx->shape.E;
-  moe_route_rule rules[4] = {{MOE_SCORE_SOFTMAX, 1, 1, 1, 0, 1.f}, {MOE_SCORE_SIGMOID, 1, 1, 1, 0, 1.f},
-                             {MOE_SCORE_SOFTMAX, 2, 1, 1, 0, 1.f}, {MOE_SCORE_SIGMOID, 2, 1, 1, 0, 1.f}};
-  for (const moe_route_rule& r : rules) {
-    const cudaError_t e = with_rule(E, r, [&](auto el, auto sigmoid, auto groups) {
-      constexpr int kEl = decltype(el)::value;
-      constexpr bool kS = decltype(sigmoid)::value, kG = decltype(groups)::value;
-      const cudaError_t a = cudaFuncSetAttribute(scored_select<kEl, kS, kG>, cudaFuncAttributeMaxDynamicSharedMemorySize, 96 * 1024);
+  // one rule for each kernel there is at this E: two scores, one group, two and, where E allows another layout, three
+  for (int score : {MOE_SCORE_SOFTMAX, MOE_SCORE_SIGMOID})
+  for (int groups = 1; groups <= 2; ++groups)
+  for (bool bias_on_grid : {false, true}) {
+    const moe_route_rule r{score, groups, 1, 1, 0, 1.f};
+    const cudaError_t e = with_rule(E, r, bias_on_grid, [&](auto el, auto sigmoid, auto layout) {
+      constexpr int kEl = decltype(el)::value, kL = decltype(layout)::value;
+      constexpr bool kS = decltype(sigmoid)::value;
+      const cudaError_t a = cudaFuncSetAttribute(scored_select<kEl, kS, kL>, cudaFuncAttributeMaxDynamicSharedMemorySize, 96 * 1024);
       if (a != cudaSuccess) return a;
-      return cudaFuncSetAttribute(scored_plan_small<kEl, kS, kG>, cudaFuncAttributeMaxDynamicSharedMemorySize, 96 * 1024);
+      return cudaFuncSetAttribute(scored_plan_small<kEl, kS, kL>, cudaFuncAttributeMaxDynamicSharedMemorySize, 96 * 1024);
     });
     if (e != cudaSuccess) return e;
   }

