@@ -236,10 +236,9 @@ scored_plan_small(const ScoredParams p) {
   place_slots(s_ids, (t_end - t_begin) * p.k, t_begin * p.k, s_start, p.E, s_cnt, p.perm, p.inv_perm);
 }
 
-// Calls f with the selection's template arguments: entries per lane, sigmoid, layout (bias_on_grid: the bias can be read
-// 16 bytes at a time, as the logits always can).
+// Calls f with the selection's template arguments: entries per lane, sigmoid, layout.
 template <typename F>
-cudaError_t with_rule(int E, const moe_route_rule& r, bool bias_on_grid, F f) {
+cudaError_t with_rule(int E, const moe_route_rule& r, F f) {
   auto by_el = [&](auto sigmoid, auto layout) {
     if constexpr (decltype(layout)::value != moe::kOwnGroups) {
       if (E <= 32) return f(std::integral_constant<int, 1>{}, sigmoid, layout);
@@ -251,10 +250,9 @@ cudaError_t with_rule(int E, const moe_route_rule& r, bool bias_on_grid, F f) {
     return f(std::integral_constant<int, 32>{}, sigmoid, layout);
   };
   auto by_layout = [&](auto sigmoid) {
-    const bool powers = (E & (E - 1)) == 0 && (r.n_group & (r.n_group - 1)) == 0;
     if (r.n_group == 1) return by_el(sigmoid, std::integral_constant<int, moe::kNoGroups>{});
-    if (powers && E >= 128 && bias_on_grid)
-      return by_el(sigmoid, std::integral_constant<int, moe::kOwnGroups>{});
+    // a power of two has no other group sizes, so a lane's share of 4 to 32 neighbours never straddles groups
+    if ((E & (E - 1)) == 0 && E >= 128) return by_el(sigmoid, std::integral_constant<int, moe::kOwnGroups>{});
     return by_el(sigmoid, std::integral_constant<int, moe::kAnyGroups>{});
   };
   return r.score == MOE_SCORE_SIGMOID ? by_layout(std::true_type{}) : by_layout(std::false_type{});
@@ -284,13 +282,12 @@ cudaError_t launch_plan_routing_scored(moe_ctx* ctx, const float* logits, const 
   p.offsets = offsets;
   p.perm = perm;
   p.inv_perm = inv_perm;
-  const bool bias_on_grid = (reinterpret_cast<uintptr_t>(bias) & 15u) == 0;
   const size_t select_bytes = static_cast<size_t>(kWarps) * p.warp_floats * 4;
   const int per_cta = (s.T + kCluster - 1) / kCluster;
   if (per_cta <= kSmallTokens && per_cta * s.k <= kRouteThreads) {
     p.tokens_per_chunk = per_cta;
     const size_t smem = (3 * static_cast<size_t>(s.E) + kWarps + kRouteThreads) * 4 + select_bytes + kWarps * s.E;
-    const cudaError_t e = with_rule(s.E, rule, bias_on_grid, [&](auto el, auto sigmoid, auto layout) {
+    const cudaError_t e = with_rule(s.E, rule, [&](auto el, auto sigmoid, auto layout) {
       auto kernel = scored_plan_small<decltype(el)::value, decltype(sigmoid)::value, decltype(layout)::value>;
       kernel<<<kCluster, kRouteThreads, smem, stream>>>(p);
       return cudaGetLastError();
@@ -304,7 +301,7 @@ cudaError_t launch_plan_routing_scored(moe_ctx* ctx, const float* logits, const 
   p.tokens_per_chunk = ctx->tokens_per_chunk;
   const size_t smem1 = (static_cast<size_t>(s.E) + kRouteThreads) * 4 + select_bytes;
   const size_t smem3 = (2 * static_cast<size_t>(s.E) + kWarps + kRouteThreads) * 4 + kWarps * s.E;
-  const cudaError_t e = with_rule(s.E, rule, bias_on_grid, [&](auto el, auto sigmoid, auto layout) {
+  const cudaError_t e = with_rule(s.E, rule, [&](auto el, auto sigmoid, auto layout) {
     auto kernel = scored_select<decltype(el)::value, decltype(sigmoid)::value, decltype(layout)::value>;
     kernel<<<ctx->num_chunks, kRouteThreads, smem1, stream>>>(p);
     return cudaGetLastError();
@@ -322,12 +319,10 @@ cudaError_t launch_plan_routing_scored(moe_ctx* ctx, const float* logits, const 
 // One-time kernel attributes: the selection's shared memory passes 48 KB at the largest E with many groups.
 cudaError_t prepare_plan_scored(moe_ctx* ctx) {
   const int E = ctx->shape.E;
-  // one rule for each kernel there is at this E: two scores, one group, two and, where E allows another layout, three
-  for (int score : {MOE_SCORE_SOFTMAX, MOE_SCORE_SIGMOID})
-  for (int groups = 1; groups <= 2; ++groups)
-  for (bool bias_on_grid : {false, true}) {
-    const moe_route_rule r{score, groups, 1, 1, 0, 1.f};
-    const cudaError_t e = with_rule(E, r, bias_on_grid, [&](auto el, auto sigmoid, auto layout) {
+  const moe_route_rule rules[4] = {{MOE_SCORE_SOFTMAX, 1, 1, 1, 0, 1.f}, {MOE_SCORE_SIGMOID, 1, 1, 1, 0, 1.f},
+                                   {MOE_SCORE_SOFTMAX, 2, 1, 1, 0, 1.f}, {MOE_SCORE_SIGMOID, 2, 1, 1, 0, 1.f}};
+  for (const moe_route_rule& r : rules) {
+    const cudaError_t e = with_rule(E, r, [&](auto el, auto sigmoid, auto layout) {
       constexpr int kEl = decltype(el)::value, kL = decltype(layout)::value;
       constexpr bool kS = decltype(sigmoid)::value;
       const cudaError_t a = cudaFuncSetAttribute(scored_select<kEl, kS, kL>, cudaFuncAttributeMaxDynamicSharedMemorySize, 96 * 1024);

@@ -61,6 +61,7 @@ SHAPES = [  # T, E, k, n_group, topk_group
     (1, 1, 1, 1, 1), (1, 256, 8, 8, 4), (3, 7, 3, 1, 1), (70, 32, 4, 4, 2), (33, 33, 5, 3, 2), (65, 64, 6, 1, 1),
     (129, 96, 6, 6, 3), (40, 160, 6, 8, 3), (257, 256, 8, 8, 4), (50, 300, 32, 10, 3), (20, 512, 9, 32, 5),
     (37, 1000, 32, 25, 7), (600, 8, 2, 2, 1), (300, 24, 12, 24, 12), (2000, 48, 3, 1, 1),
+    (130, 128, 7, 2, 1), (60, 1024, 12, 8, 5), (300, 256, 10, 16, 3), (9, 128, 4, 32, 32), (77, 512, 20, 4, 4),
 ]
 
 
@@ -130,8 +131,9 @@ def test_the_plain_rule_is_moe_plan_routing():
 @pytest.mark.parametrize("renormalise", [True, False])
 @pytest.mark.parametrize("n_group,topk_group,group_top", [(1, 1, 1), (4, 2, 2), (4, 3, 1)])
 @pytest.mark.parametrize("with_bias", [False, True])
-def test_masked_infinite_and_nan_logits(score, renormalise, n_group, topk_group, group_top, with_bias):
-    E, k = 40, 6
+@pytest.mark.parametrize("E", [40, 128])
+def test_masked_infinite_and_nan_logits(score, renormalise, n_group, topk_group, group_top, with_bias, E):
+    k = 6
     rng = np.random.default_rng(6)
     x = (rng.integers(-8, 9, (10, E)) / 4).astype(np.float32)
     x[0, :] = -math.inf                                 # nothing left
@@ -141,7 +143,7 @@ def test_masked_infinite_and_nan_logits(score, renormalise, n_group, topk_group,
     x[4, 5] = math.nan
     x[5, 9] = math.inf
     x[6, :] = math.nan
-    x[7, 10:30] = -math.inf                             # two whole groups masked
+    x[7, E // 4:3 * E // 4] = -math.inf                             # two whole groups masked
     x[8, :] = 100.0 * np.sign(x[8] + 0.125)             # saturated scores
     x[9, 0], x[9, 1] = math.inf, math.inf
     bias = (rng.integers(-2, 3, E) / 2).astype(np.float32) if with_bias else None
