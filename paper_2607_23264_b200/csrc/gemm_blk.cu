@@ -384,8 +384,12 @@ __device__ __forceinline__ void blk_swapped_tile(const BlkParams& p, const BlkTi
     ptx::mbar_wait_or_flag(bar, es.out_phase, abort_flag, kRoleEpilogue);
     es.out_phase ^= 1u;
   };
-  // kOutTokens rows at a time through shared memory: weight rows become neighbouring columns of an output row
+  // kOutTokens rows at a time through shared memory: weight rows become neighbouring columns of an output row.  The half's
+  // area of it also is its warps' boxes of a row tile (store_rows_64), and with one or two blocks of K nothing else holds a
+  // warp back from the next tile's end while another still stores the last one's: so the warps meet before the first write
+  // too, wherever tiles of both kinds can follow each other.
   float* mine = s_out + half * kOutTokens * 256;
+  if constexpr (kMaxN > kSwapRows) meet();
 #pragma unroll
   for (int c = 0; c < kCols; c += kOutTokens) {
     if (half * kCols + c >= tile.rows) break;            // (the same for the four warps of a half)

@@ -488,3 +488,51 @@ def test_calls_can_be_captured_in_a_graph():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(out.view(torch.int16), eager.view(torch.int16))
+
+
+@pytest.mark.parametrize("N,K", [(128, 16), (128, 128), (264, 256), (520, 272), (136, 240), (384, 144)])
+def test_product_of_mixed_tiles_with_few_blocks_of_k(ctx, N, K):
+    """Hundreds of groups of 1 to 128 rows: every CTA goes from tiles with the rows on the M side (65 to 128 rows) to tiles
+    with swapped operands and back, and with one or two blocks of K its warps may be a tile apart."""
+    rng = np.random.default_rng(N + K)
+    counts = [int(c) for c in rng.integers(1, 129, 600)]
+    a, sa, offsets, b = make_product(rng, counts, N, K)
+    y = run_product(ctx, a, sa, offsets, b, N, K)
+    check_product(y, a, sa, offsets, b, N, K)
+    for _ in range(5):
+        again = run_product(ctx, a, sa, offsets, b, N, K)
+        assert torch.equal(again.view(torch.int16), y.view(torch.int16)), "not the same bits every time"
+
+
+@pytest.mark.parametrize("H,F", [(128, 256), (256, 128), (256, 256)])
+def test_experts_of_mixed_tiles_with_few_blocks_of_k(H, F):
+    """The same through both GEMMs of a layer: 400 experts with loads from about 12 to 130 rows."""
+    cfg = cfg_of(6000, H, F, 400, 4, seed=H + F)
+    M = BlkLayer(cfg)
+    L, ctx = M.L, M.L.ctx
+    L.plan()
+    R = cfg.R
+    xq, sx = torch.empty(cfg.T, H, dtype=torch.uint8, device=DEV), torch.empty(H // 128, cfg.T, device=DEV)
+    xp, sxp = torch.empty(R, H, dtype=torch.uint8, device=DEV), torch.empty(H // 128, R, device=DEV)
+    ctx.moe_quantize_rows_blk(L.x, cfg.T, H, xq, sx)
+    ctx.moe_dispatch_blk(xq, sx, L.inv_perm, xp, sxp)
+    counts = L.counts.cpu().numpy()
+    assert ((counts > 0) & (counts <= 64)).sum() > 100 and (counts > 64).sum() > 100     # both kinds of tile
+    hq = torch.full((R, F), 0x7F, dtype=torch.uint8, device=DEV)
+    sh = torch.full((F // 128, R), float("nan"), device=DEV)
+    y, h = L.nan_bf16(R, H), torch.full((R, F), float("nan"), device=DEV)
+    ctx.moe_expert_ffn_blk(xp, sxp, L.offsets, *M.weights(), hq, sh, y, h)
+    torch.cuda.synchronize()
+    L.check_device_status()
+    offsets, xc, xs = L.offsets.cpu().numpy(), xp.cpu().numpy(), sxp.cpu().numpy()
+    h_gpu, hc, hs, y_gpu = h.cpu().numpy(), hq.cpu().numpy(), sh.cpu().numpy(), dev_bf16_to_f64(y)
+    req_c, req_s = blk.quantize_rows(h_gpu)
+    assert np.array_equal(hc, req_c) and np.array_equal(hs, req_s)
+    for e in range(cfg.E):
+        lo, hi = int(offsets[e]), int(offsets[e + 1])
+        if hi == lo:
+            continue
+        gate, up, down = M.oracle_weights(e)
+        assert rel_fro(h_gpu[lo:hi].astype(np.float64), blk.expert_rows(xc[lo:hi], xs[:, lo:hi], gate, up)) <= TOL_FRO / 50, e
+        ref, mag = blk.gemm(hc[lo:hi], hs[:, lo:hi], *down), blk.magnitude(hc[lo:hi], hs[:, lo:hi], *down)
+        assert (np.abs(y_gpu[lo:hi] - ref) <= 2.0 ** -8 * np.abs(ref) + (F / 16 + F / 128 + 8) * 2.0 ** -23 * mag).all(), e
