@@ -115,13 +115,16 @@ routing_backward(const float* __restrict__ logits, const int32_t* __restrict__ t
   float d, dot = 0.f;
   if (sigmoid) {
     const float s = id >= 0 && xs > -INFINITY ? moe::route_sigmoid(xs) : 0.f;
-    float gs = g;
+    // 1 - s as the sigmoid of -x (the difference loses its digits from x = 10 on and is 0 from 17), and each score's share
+    // of the sum before anything is multiplied by it (1 / S leaves fp32 where all chosen logits are near -88).  0.1 us of
+    // 2.1 more at 301 tokens, 0.5 of 7.0 at 16384 (256 experts, logits in L2).
+    float share = s, mean = 0.f;
     if (rule.renormalise) {
       const float sum = moe::warp_sum(s);
-      const float mean = sum > 0.f ? moe::warp_sum(g * s) / sum : 0.f;
-      gs = sum > 0.f ? (g - mean) / sum : 0.f;
+      share = sum > 0.f ? s / sum : 0.f;
+      mean = moe::warp_sum(g * share);
     }
-    d = gs * s * (1.f - s);
+    d = share * (g - mean) * moe::route_sigmoid(-xs);
   } else if (!dense) {
     float m = moe::warp_max(xs);
     if (m == -INFINITY) m = 0.f;

@@ -339,3 +339,59 @@ def test_refusals():
         call(binding.make_route_rule(**ok), x=torch.zeros(E, T, device=DEV).t())
     with pytest.raises(binding.MoeError):
         ctx.moe_combine_backward(None, x, inv, w, None, w)
+
+
+def sigmoid_gradient_parts(x, ids, g, rule):
+    """Per chosen slot, in 64 bits and from sigmoids of both signs (no 1 - s): the gradient, and the factor that its
+    rounding errors are relative to."""
+    xs = np.take_along_axis(x.astype(np.float64), ids.astype(np.int64), 1)
+    e = np.exp(-np.abs(xs))
+    s, c = np.where(xs >= 0, 1 / (1 + e), e / (1 + e)), np.where(xs >= 0, e / (1 + e), 1 / (1 + e))
+    g = g.astype(np.float64) * rule.weight_scale
+    if not rule.renormalise:
+        return g * s * c, np.abs(g) * s * c
+    q = s / s.sum(1, keepdims=True)
+    return q * (g - (g * q).sum(1, keepdims=True)) * c, q * c * (np.abs(g) + (np.abs(g) * q).sum(1, keepdims=True))
+
+
+@pytest.mark.parametrize("E,k", [(8, 2), (96, 6), (256, 8), (1024, 32)])
+@pytest.mark.parametrize("renormalise", [True, False])
+def test_sigmoid_gradient_of_saturated_logits(E, k, renormalise):
+    """Every element against its own size where scores are near 0 or 1.  expf is within 2 ulp and a sigmoid adds two
+    roundings, so s and 1 - s carry 3.6e-7; a product of them with g 1e-6, a share of a sum of 32 another 8e-7 and the mean
+    of g as much again: 1.5e-6 without the sum, 4e-6 with it."""
+    rng = np.random.default_rng(E + k)
+    levels = np.array([-88.0, -80.0, -30.0, -4.0, 0.0, 5.0, 12.0, 17.0, 20.0, 40.0, 80.0, 88.0])
+    x = (levels.repeat(4)[:, None] + rng.uniform(-0.5, 0.5, (48, E))).astype(np.float32)
+    mixed = rng.choice(levels, (16, E)) + rng.uniform(-0.5, 0.5, (16, E))
+    x = np.concatenate([x, mixed.astype(np.float32)])
+    ids = np.stack([rng.permutation(E)[:k] for _ in x]).astype(np.int32)
+    g = (rng.standard_normal((len(x), k)) * 10.0 ** rng.uniform(-2, 2, (len(x), 1))).astype(np.float32)
+    rule = Rule("sigmoid", 1, 1, 1, renormalise, 2.5)
+    got = run_backward(x, ids, g, rule)
+    ref, size = sigmoid_gradient_parts(x, ids, g, rule)
+    err = np.abs(np.take_along_axis(got, ids.astype(np.int64), 1) - ref)
+    assert (err <= (4e-6 if renormalise else 1.5e-6) * size + 1e-44).all(), np.nanmax(err / (size + 1e-44))
+    others = got.copy()
+    np.put_along_axis(others, ids.astype(np.int64), 0.0, 1)
+    assert not others.any()
+
+
+def test_sigmoid_gradient_of_saturated_logits_against_differences():
+    """The same where the slope is all that is left of the score: central differences of the fp64 weights."""
+    x = np.array([[12.0, 12.5, 11.5, -3.0], [20.0, 19.0, 21.0, 0.0], [-20.0, -21.0, -19.5, 4.0]], dtype=np.float32)
+    ids = np.tile(np.array([0, 1, 2], dtype=np.int32), (3, 1))
+    g = np.array([[1.0, -2.0, 0.5]] * 3, dtype=np.float32)
+    for renormalise in (True, False):
+        rule = Rule("sigmoid", 1, 1, 1, renormalise, 1.0)
+        got = run_backward(x, ids, g, rule)
+        for t in range(3):
+            for e in range(3):
+                w = []
+                for step in (1e-2, -1e-2):
+                    v = x[t].astype(np.float64)
+                    v[e] += step
+                    w.append(sro.weights(v, ids[t], rule))
+                # third derivative of a weight: at most its slope, so the difference is off by step^2 / 6 of it
+                diff = float(((w[0] - w[1]) * g[t]).sum() / 2e-2)
+                assert abs(got[t, e] - diff) <= 1e-4 * np.abs(got[t]).max(), (renormalise, t, e, got[t, e], diff)
