@@ -914,9 +914,9 @@ moe_status launch_gemm_blk(moe_ctx* ctx, const moe_gemm_blk_args* a, cudaStream_
   p.offsets = a->offsets;
   p.groups = a->groups;
   p.N = a->N;
-  p.n_tiles = (a->N + 2 * BW - 1) / (2 * BW);
-  p.k_blocks = (a->K + BK - 1) / BK;
-  p.n_blocks = (a->N + BW - 1) / BW;
+  p.n_tiles = blocks_of(a->N, 2 * BW);
+  p.k_blocks = blocks_of(a->K, BK);
+  p.n_blocks = blocks_of(a->N, BW);
   p.rows = static_cast<int>(a->rows);
   p.sa = a->sa;
   p.sb0 = a->sb;
@@ -947,7 +947,7 @@ moe_status launch_expert_ffn_blk(moe_ctx* ctx, const moe_blk_ffn_args* a, cudaSt
   moe_mark(ctx, 5, stream);
   BlkParams p2 = p;
   p2.N = s.H;
-  p2.n_tiles = (s.H + 2 * BW - 1) / (2 * BW);
+  p2.n_tiles = blocks_of(s.H, 2 * BW);
   p2.n_blocks = s.H / BW;
   p2.k_blocks = s.F / BK;
   p2.sa = a->sh_ws;

@@ -105,6 +105,9 @@ inline void moe_mark(moe_ctx* ctx, int i, cudaStream_t stream) {
 // Launchers (each returns the cudaError_t of its launches).  `stream` is the caller's stream.
 namespace moe {
 
+// Blocks of `block` that n >= 1 elements fill or begin; n may be any int (n + block - 1 may not be one).
+inline int blocks_of(int n, int block) { return (n - 1) / block + 1; }
+
 cudaError_t launch_plan_routing(moe_ctx* ctx, const float* logits, int32_t* topk_ids, float* topk_w,
                                 int32_t* counts, int32_t* offsets, int32_t* perm, int32_t* inv_perm,
                                 cudaStream_t stream);

@@ -173,7 +173,7 @@ namespace moe {
 cudaError_t launch_quantize_rows_blk(moe_ctx* ctx, const void* in_bf16, long long rows, int cols, void* codes,
                                      float* scales, cudaStream_t stream) {
   if (rows == 0) return cudaSuccess;
-  const int blocks_per_row = (cols + 127) / 128;
+  const int blocks_per_row = blocks_of(cols, 128);
   const int span = span_of(ctx, rows, blocks_per_row), spans = (blocks_per_row + span - 1) / span;
   const long long grid = (rows * spans + kThreads / 32 - 1) / (kThreads / 32);
   if (rows * spans > 0x7FFFFFFFLL - kThreads) return cudaErrorInvalidConfiguration;
@@ -201,9 +201,10 @@ cudaError_t launch_quantize_dispatch_blk(moe_ctx* ctx, const void* x, const int3
 
 cudaError_t launch_quantize_weights_blk(moe_ctx* ctx, const void* in_bf16, long long mats, int rows, int cols,
                                         void* codes, float* scales, cudaStream_t stream) {
-  const int rb = (rows + 127) / 128, cb = (cols + 127) / 128;
-  const long long grid = mats * rb * cb;
-  if (grid > 0x7FFFFFFFLL) return cudaErrorInvalidConfiguration;
+  const int rb = blocks_of(rows, 128), cb = blocks_of(cols, 128);
+  const long long per_mat = static_cast<long long>(rb) * cb;
+  if (per_mat > 0x7FFFFFFFLL / mats) return cudaErrorInvalidConfiguration;
+  const long long grid = mats * per_mat;
   quantize_weights_blk<<<static_cast<unsigned>(grid), kThreads, 0, stream>>>(
       static_cast<const uint4*>(in_bf16), rows, cols / 8, rb, cb, static_cast<uint2*>(codes), scales);
   ctx->last_launches += 1;

@@ -536,3 +536,54 @@ def test_experts_of_mixed_tiles_with_few_blocks_of_k(H, F):
         assert rel_fro(h_gpu[lo:hi].astype(np.float64), blk.expert_rows(xc[lo:hi], xs[:, lo:hi], gate, up)) <= TOL_FRO / 50, e
         ref, mag = blk.gemm(hc[lo:hi], hs[:, lo:hi], *down), blk.magnitude(hc[lo:hi], hs[:, lo:hi], *down)
         assert (np.abs(y_gpu[lo:hi] - ref) <= 2.0 ** -8 * np.abs(ref) + (F / 16 + F / 128 + 8) * 2.0 ** -23 * mag).all(), e
+
+
+LONGEST = 2 ** 31 - 16               # the last multiple of 16 an int32 holds
+
+
+def test_quantize_the_longest_row(ctx):
+    """One row of 2^31 - 16 values: a period of 2^20 over and over, so that the codes are those of one short call."""
+    period = 1 << 20
+    g = torch.Generator(device=DEV).manual_seed(3)
+    part = torch.randn(period, generator=g, device=DEV).to(torch.bfloat16)
+    x = part.repeat(LONGEST // period + 1)[:LONGEST]
+    codes, scales = torch.empty(LONGEST, dtype=torch.uint8, device=DEV), torch.empty(1 << 24, device=DEV)
+    small_c, small_s = torch.empty(period, dtype=torch.uint8, device=DEV), torch.empty(period // 128, device=DEV)
+    ctx.moe_quantize_rows_blk(part, 1, period, small_c, small_s)
+    whole = LONGEST // period * period
+    tail_c, tail_s = torch.empty(LONGEST - whole, dtype=torch.uint8, device=DEV), torch.empty(period // 128, device=DEV)
+    ctx.moe_quantize_rows_blk(part, 1, LONGEST - whole, tail_c, tail_s)
+    # as a matrix of one row too: its blocks of 128 x 128 are the same 128 values
+    for call in (lambda: ctx.moe_quantize_rows_blk(x, 1, LONGEST, codes, scales),
+                 lambda: ctx.moe_quantize_weights_blk(x, 1, 1, LONGEST, codes, scales)):
+        codes.fill_(0x7F)
+        scales.fill_(float("nan"))
+        call()
+        torch.cuda.synchronize()
+        assert bool((codes[:whole].view(-1, period) == small_c).all()) and torch.equal(codes[whole:], tail_c)
+        assert bool((scales[:whole // 128].view(-1, period // 128) == small_s).all())
+        assert torch.equal(scales[whole // 128:], tail_s)
+
+
+def test_product_with_the_longest_k(ctx):
+    """K = 2^31 - 16: ones in a few places of a against small whole numbers in b, first block, middle and short last one."""
+    N = 8
+    a = torch.zeros(1, LONGEST, dtype=torch.uint8, device=DEV)
+    b = torch.full((N, LONGEST), 0x38, dtype=torch.uint8, device=DEV)                       # 1.0
+    where = torch.tensor([0, 5, 127, 128, 2 ** 30 + 1, 2 ** 31 - 129, 2 ** 31 - 128, LONGEST - 1], device=DEV)
+    a[0, where] = 0x38
+    b[:, LONGEST - 1] = torch.arange(N, device=DEV).float().to(torch.float8_e4m3fn).view(torch.uint8)
+    y = torch.full((1, N), float("nan"), dtype=torch.bfloat16, device=DEV)
+    ones = torch.ones(1 << 24, device=DEV)
+    ctx.moe_gemm_blk(a, ones, b, ones, y, 1, N, LONGEST)
+    torch.cuda.synchronize()
+    assert ctx.moe_last_device_status()[0] == 0
+    assert y[0].tolist() == [7.0 + n for n in range(N)]
+
+
+def test_more_blocks_than_a_grid_holds_are_refused(ctx):
+    t8, t4 = torch.zeros(4096, dtype=torch.uint8, device=DEV), torch.zeros(64, device=DEV)
+    for mats, rows, cols in ((1 << 29, 2 ** 31 - 1, LONGEST), (1 << 29, 2 ** 30, 2 ** 24), (1, 2 ** 31 - 1, LONGEST)):
+        with pytest.raises(binding.MoeError) as e:
+            ctx.moe_quantize_weights_blk(t8, mats, rows, cols, t8, t4)
+        assert e.value.code == 5, (mats, rows, cols)
