@@ -859,7 +859,7 @@ moe_status launch_product(moe_ctx* ctx, const BlkProduct& g, const BlkParams& p,
   // A pair's tile has 256 rows, and the last of a group is padded to them: from about four full tiles on, the pair's 2 to
   // 6 % outweigh that whatever the remainder (a layer of 64 experts with 128 rows each on average: 3.50 ms with pairs,
   // 2.59 ms without).
-  const long long pair_rows = moe_knob_value(ctx, "blk_pair_rows", 900);
+  const long long pair_rows = moe_knob_value(ctx, "blk_pair_rows", 900);   // (0: pairs for every product, for tests)
   // Single CTAs with boxes of at most 32 rows have room for five stages, those of 128 rows for four, which do more rows
   // with each read of the weights; us, 32 / 128: 64 groups, 2048 x 7168: 2 rows 144.7/149.8, 16 144.7/148.2, 32
   // 147.3/151.2, 40 164.6/154.3; 128 groups, 7168 x 2048: 2 rows 281/281, 16 287/286, 24 300/296, 32 314/303.  On average
@@ -870,7 +870,8 @@ moe_status launch_product(moe_ctx* ctx, const BlkProduct& g, const BlkParams& p,
     // about a fifth longer): 512 rows, 4096 x 7168.
     const long long pair_tiles = most_tiles(p, 256), tiles = most_tiles(p, 128);
     const int split = k_split(ctx, tiles, p.k_blocks);
-    if (pair_tiles > ctx->max_pairs || tiles > ctx->num_sms || 6LL * ((p.k_blocks + split - 1) / split) >= 5LL * p.k_blocks)
+    if (pair_rows == 0 || pair_tiles > ctx->max_pairs || tiles > ctx->num_sms ||
+        6LL * ((p.k_blocks + split - 1) / split) >= 5LL * p.k_blocks)
       return launch_tiles<kGated, 2, 128>(ctx, g, p, stream);
     return launch_tiles<kGated, 1, 128>(ctx, g, p, stream);
   }

@@ -587,3 +587,56 @@ def test_more_blocks_than_a_grid_holds_are_refused(ctx):
         with pytest.raises(binding.MoeError) as e:
             ctx.moe_quantize_weights_blk(t8, mats, rows, cols, t8, t4)
         assert e.value.code == 5, (mats, rows, cols)
+
+
+def product_and_kernel(ctx, *args):
+    """y of run_product, and the name of the kernel that it launched (None where no launch can be recorded here)."""
+    from torch.profiler import ProfilerActivity, profile
+    with profile(activities=[ProfilerActivity.CUDA], acc_events=True) as seen:
+        y = run_product(ctx, *args)
+    names = [e.name for e in seen.events()]
+    mine = [n for n in names if "gemm_blk" in n]
+    assert len(mine) == 1 or not names, names
+    return y, mine[0] if mine else None
+
+
+def assert_pair_kernel(name):
+    if name is None:
+        pytest.skip("the result is right; which kernel computed it could not be recorded")
+    assert "<false, 2, 128>" in name.replace("(bool)0", "false").replace("(int)", ""), name
+
+
+# ragged and empty groups; second weight boxes beyond N and beyond the last group, K that ends inside a block, last tiles of
+# 1 to 128 rows (the peer CTA has none) and of 129 to 255
+PAIR_SHAPES = [([1, 0, 31, 33, 64, 65], 136, 144), ([127, 128, 129, 255, 256, 257, 0], 264, 1040), ([513], 1032, 2064),
+               ([1300, 1100], 520, 400), ([0, 385, 0, 0, 640, 2], 904, 1168), ([1], 8, 16), ([300], 136, 4112),
+               ([5] * 300, 264, 272), ([200] * 150, 392, 144), ([0, 0, 769], 2056, 528)]
+
+
+@pytest.mark.parametrize("counts,N,K", PAIR_SHAPES)
+def test_product_by_pairs_of_ctas(monkeypatch, counts, N, K):
+    """The pair kernel on shapes that the rule gives to other kernels as well as on its own."""
+    monkeypatch.setenv("MOE_TUNING", "x.blk_pair_rows=0")
+    forced = binding.Context(1, 64, 64, 1, 1)
+    rng = np.random.default_rng(N + K + len(counts))
+    a, sa, offsets, b = make_product(rng, counts, N, K, tail=2)
+    y, kernel = product_and_kernel(forced, a, sa, offsets, b, N, K)
+    check_product(y, a, sa, offsets, b, N, K)
+    assert_pair_kernel(kernel)
+
+
+@pytest.mark.parametrize("counts,N,K", [([1100, 901, 0, 1700], 136, 112), ([3333], 264, 128), ([2000, 2100, 1, 1900], 5128, 272)])
+def test_product_by_pairs_without_being_forced(ctx, counts, N, K):
+    """More than 900 rows a group on average, and K that a split cannot shorten or more tiles than SMs."""
+    rng = np.random.default_rng(N + K)
+    a, sa, offsets, b = make_product(rng, counts, N, K)
+    y, kernel = product_and_kernel(ctx, a, sa, offsets, b, N, K)
+    check_product(y, a, sa, offsets, b, N, K)
+    assert_pair_kernel(kernel)
+
+
+@pytest.mark.parametrize("T,H,F,E,k", [(300, 384, 256, 6, 2), (513, 256, 384, 2, 1), (40, 512, 128, 12, 3)])
+def test_experts_by_pairs_of_ctas(monkeypatch, T, H, F, E, k):
+    """Both GEMMs of a layer by the pair kernel: the bits of h's codes, and y on them."""
+    monkeypatch.setenv("MOE_TUNING", "x.blk_pair_rows=0")
+    test_expert_ffn_parity(T, H, F, E, k, "xWr")
