@@ -395,3 +395,107 @@ def test_sigmoid_gradient_of_saturated_logits_against_differences():
                 # third derivative of a weight: at most its slope, so the difference is off by step^2 / 6 of it
                 diff = float(((w[0] - w[1]) * g[t]).sum() / 2e-2)
                 assert abs(got[t, e] - diff) <= 1e-4 * np.abs(got[t]).max(), (renormalise, t, e, got[t, e], diff)
+
+
+def softmax_gradient_bound(x, ids, g, rule):
+    """Per element [T,E]: what the rounding errors of a softmax gradient are relative to, s_e (|g_e| + sum_i |g_i| s_i)."""
+    T, E = x.shape
+    size = np.zeros((T, E))
+    for t in range(T):
+        sel = list(ids[t])
+        a = np.abs(g[t].astype(np.float64)) * rule.weight_scale
+        if rule.renormalise:
+            q = sro.scores(x[t, sel], rule)
+            size[t, sel] = q * (a + (a * q).sum())
+        else:
+            s = sro.scores(x[t], rule)
+            full = np.zeros(E)
+            full[sel] = a
+            size[t] = s * (full + (a * s[sel]).sum())
+    return size
+
+
+@pytest.mark.parametrize("T,E,k,n_group,topk_group", SHAPES)
+@pytest.mark.parametrize("renormalise", [True, False])
+def test_softmax_gradient_element_by_element(T, E, k, n_group, topk_group, renormalise):
+    """Every element against its own size, so that the small gradients of unchosen experts count.  For |x - max| <= 30: the
+    argument's rounding 1.8e-6 and expf 2.4e-7 relative in an exponential; a sum of 1024 of them adds 37 roundings: 6.3e-6 in
+    a score, 6.7e-6 in the weighted sum of k gradients: 1.5e-5 of the element's size with the remaining products."""
+    rng = np.random.default_rng(T * 3 + E)
+    x = np.clip(3 * rng.standard_normal((T, E)), -14, 14).astype(np.float32)
+    rule = Rule("softmax", 1, 1, 1, renormalise, 2.5)
+    ids = np.stack([rng.permutation(E)[:k] for _ in range(T)]).astype(np.int32)
+    g = rng.standard_normal((T, k)).astype(np.float32)
+    got = run_backward(x, ids, g, rule)
+    ref = sro.routing_backward(x.astype(np.float64), ids, g, rule)
+    size = softmax_gradient_bound(x, ids, g, rule)
+    err = np.abs(got - ref)
+    assert (err <= 1.5e-5 * size + 1e-37).all(), np.max(err / (size + 1e-37))
+
+
+def admissible(ids, x, bias, rule, k):
+    """Whether an fp32 choice may hold these experts: with choice values and groups' worths (fp64) that are off by at most
+    2e-6 each, every expert is in a group that stays and among the k best of such groups."""
+    c = sro.choice_values(x, bias, rule)
+    E, size = len(c), len(c) // rule.n_group
+    rank = c
+    if bias is None and rule.group_top == 2:
+        rank = np.where(np.isneginf(c), -math.inf, sro.scores(x, rule))
+    worth = np.array([np.sort(rank[j * size:(j + 1) * size])[::-1][:rule.group_top].sum() for j in range(rule.n_group)])
+    edge = np.sort(worth)[::-1][rule.topk_group - 1]
+    may, must = worth >= edge - 4e-6, worth > edge + 4e-6
+    mine = set(int(e) // size for e in ids)
+    if not all(may[j] for j in mine) or len(set(ids)) != k:
+        return False
+    # the kept groups: all that have to stay, those that were used, and the best of the others
+    kept = sorted(range(rule.n_group), key=lambda j: (not (must[j] or j in mine), -worth[j]))[:rule.topk_group]
+    if must.sum() == rule.topk_group or may.sum() == rule.topk_group:
+        kept = list(np.flatnonzero(may if may.sum() == rule.topk_group else must))
+    open_ = np.concatenate([np.arange(j * size, (j + 1) * size) for j in kept])
+    if not set(int(e) for e in ids) <= set(open_):
+        return False
+    if may.sum() > rule.topk_group:
+        return True                                        # more than one set of groups may stay
+    return bool(np.abs(np.sort(c[ids])[::-1] - np.sort(c[open_])[::-1][:k]).max() <= 4e-6)
+
+
+@pytest.mark.parametrize("T,E,k,n_group,topk_group,group_top", [
+    (2000, 256, 8, 8, 4, 2), (2000, 256, 8, 8, 4, 1), (1500, 128, 6, 4, 2, 2), (1500, 160, 6, 8, 3, 2),
+    (1500, 96, 6, 6, 3, 1), (700, 512, 20, 16, 4, 2), (700, 1000, 32, 25, 7, 2), (400, 1024, 12, 32, 5, 2),
+    (1000, 64, 4, 32, 9, 2), (1000, 24, 12, 24, 12, 1),
+])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("with_bias", [True, False])
+def test_grouped_choices_differ_only_within_rounding(T, E, k, n_group, topk_group, group_top, score, with_bias):
+    rng = np.random.default_rng(T + 11 * E + k)
+    rule = Rule(score, n_group, topk_group, group_top, True, 1.0)
+    x = (3 * rng.standard_normal((T, E))).astype(np.float32)
+    bias = (0.1 * rng.standard_normal(E)).astype(np.float32) if with_bias else None
+    o = run_route(x, bias, rule, k)
+    ids, _ = sro.route(x, bias, rule, k)
+    differ = np.flatnonzero((o["topk_ids"] != ids).any(1))
+    assert len(differ) <= 0.01 * T
+    for t in differ:
+        assert admissible(o["topk_ids"][t], x[t], bias, rule, k), t
+    check_plan(o, E)
+
+
+def test_the_grouped_check_refuses_wrong_choices():
+    """The check above on the oracle's own choices and on choices that are wrong (no kernel involved)."""
+    rng = np.random.default_rng(2)
+    rule, k = Rule("sigmoid", 8, 4, 2, True, 1.0), 8
+    refused = 0
+    for _ in range(200):
+        x, bias = (3 * rng.standard_normal(256)).astype(np.float32), (0.1 * rng.standard_normal(256)).astype(np.float32)
+        ids, c = sro.select(x, bias, rule, k)
+        ids = np.array(ids)
+        assert admissible(ids, x, bias, rule, k)
+        groups = set(ids // 32)
+        closed = [e for e in range(256) if e // 32 not in groups]
+        best_closed = max(closed, key=lambda e: c[e])
+        other = ids.copy()
+        other[-1] = best_closed                                # an expert of a group that does not stay
+        worse = ids.copy()
+        worse[0] = min((e for e in range(256) if e // 32 == ids[0] // 32), key=lambda e: c[e])
+        refused += (not admissible(other, x, bias, rule, k)) + (not admissible(worse, x, bias, rule, k))
+    assert refused >= 390
