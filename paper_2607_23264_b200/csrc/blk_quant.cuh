@@ -20,13 +20,13 @@ struct FastDivider {
     return fmaf(fmaf(q, scale, -v), -reciprocal, q);
   }
 };
-// Scales so small that the reciprocal or the remainder leaves the normal range, and infinite ones (2^-100 .. 2^100 are
-// neither), take the general division.
+// From 2^-90 to 2^100 the reciprocal is a normal number and the remainder of a quotient of at least 2^-12 (a quarter of the
+// smallest code) exact: its last bit is worth 2^-35 2^-113 or more.  Other scales, infinite ones among them, take the general division.
 struct GeneralDivider {
   float scale;
   __device__ __forceinline__ float operator()(float v) const { return __fdiv_rn(v, scale); }
 };
-__device__ __forceinline__ bool general_scale(float scale) { return !(scale >= 7.9e-31f && scale <= 1.2e30f); }
+__device__ __forceinline__ bool general_scale(float scale) { return !(scale >= 0x1p-90f && scale <= 0x1p100f); }
 
 // Four values over one scale -> four E4M3 codes in a word (lowest byte first), nearest-even, saturating; NaN stays NaN.
 template <typename Divider>
