@@ -14,16 +14,18 @@ namespace moe {
 // a plain fp32 program computes, not an approximation of them.
 __device__ __forceinline__ float route_sigmoid(float x) { return __frcp_rn(1.0f + expf(-x)); }
 
-// The same bits for x >= -kNearSigmoid, without the branch of a general reciprocal: 1 + e^-x is at least 1 and its
-// reciprocal a normal number, and one step of Newton's method takes the approximate reciprocal to the correctly rounded
-// one (for each of the 2^23 mantissas: compared one by one).
-constexpr float kNearSigmoid = 80.0f;
-__device__ __forceinline__ float route_sigmoid_near(float x) {
-  const float d = 1.0f + expf(-x);
+// 1 / d, correctly rounded, for 1 <= d < 2^116 without the branches of a general reciprocal: nothing leaves the normal range,
+// and one step of Newton's method takes the approximate reciprocal to the correctly rounded one
+// (tests/exact_arithmetic.cu compares all 2^23 mantissas at several exponents).
+__device__ __forceinline__ float reciprocal_from_one(float d) {
   float y;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(d));
   return fmaf(fmaf(-d, y, 1.0f), y, y);
 }
+
+// The same bits as route_sigmoid for x >= -kNearSigmoid.
+constexpr float kNearSigmoid = 80.0f;
+__device__ __forceinline__ float route_sigmoid_near(float x) { return reciprocal_from_one(1.0f + expf(-x)); }
 
 __device__ __forceinline__ float warp_max(float v) {
 #pragma unroll

@@ -1,6 +1,7 @@
-// Device arithmetic that E4M3 codes rest on bit for bit, against the general operations.  Compiled and
+// Device arithmetic that the library's choices and codes rest on bit for bit, against the general operations.  Compiled and
 // run by test_gpu_exact_arithmetic.py.  Every function returns how many results differ (or -1 for a failed launch).
 #include "../paper_2607_23264_b200/csrc/blk_quant.cuh"
+#include "../paper_2607_23264_b200/csrc/route_scored.cuh"
 
 namespace {
 
@@ -10,6 +11,19 @@ __device__ uint32_t mix(uint32_t x) {          // a bijection of 32 bits, for va
 }
 __device__ bool same(float a, float b) { return __float_as_uint(a) == __float_as_uint(b); }
 
+// every mantissa of d in [1, 2), at exponent `e`
+__global__ void reciprocals(int e, unsigned long long* differ) {
+  const uint32_t m = blockIdx.x * blockDim.x + threadIdx.x;
+  const float d = __uint_as_float((static_cast<uint32_t>(127 + e) << 23) | m);
+  if (!same(moe::reciprocal_from_one(d), __frcp_rn(d))) atomicAdd(differ, 1ull);
+}
+// x from -80 to 106 in steps of 2^-17 and a little between them
+__global__ void sigmoids(unsigned long long* differ) {
+  const uint32_t i = blockIdx.x * blockDim.x + threadIdx.x;
+  const float x = -moe::kNearSigmoid + (static_cast<float>(i) + static_cast<float>(mix(i) >> 8) * 0x1p-24f) * 0x1p-17f;
+  if (!same(moe::route_sigmoid_near(fmaxf(x, -moe::kNearSigmoid)), moe::route_sigmoid(fmaxf(x, -moe::kNearSigmoid))))
+    atomicAdd(differ, 1ull);
+}
 // quotients from 2^-12 (a quarter of the smallest code) to 448, for scales of every exponent the fast division takes; the
 // operands are two hashes of a number of 32 bits whose top four are `part16`
 __global__ void quotients(uint32_t part16, unsigned long long* differ) {
@@ -54,6 +68,12 @@ long long count(Launch launch) {
 }  // namespace
 
 extern "C" {
+long long exact_reciprocals(int e) {
+  return count([&](unsigned long long* d) { reciprocals<<<(1 << 23) / 256, 256>>>(e, d); });
+}
+long long exact_sigmoids() {
+  return count([&](unsigned long long* d) { sigmoids<<<186 * (1 << 17) / 256, 256>>>(d); });
+}
 long long exact_quotients(uint32_t part16) {
   return count([&](unsigned long long* d) { quotients<<<1 << 20, 256>>>(part16, d); });
 }

@@ -1,4 +1,4 @@
-"""Arithmetic that has to be exact, on the GPU: the division behind E4M3 codes.
+"""Arithmetic that has to be exact, on the GPU: the reciprocal behind the choice of experts, the division behind E4M3 codes.
 
 Helpers of the library's headers are compared with the general operations in a small library of their own
 (exact_arithmetic.cu); the quantisation calls with the oracle, on every pair of bf16 mantissas of a block's maximum and a
@@ -27,9 +27,18 @@ def exact(tmp_path_factory):
     except FileNotFoundError:
         pytest.skip("no nvcc here")
     lib = ctypes.CDLL(out)
-    for name in ("exact_quotients", "exact_codes"):
+    for name in ("exact_reciprocals", "exact_sigmoids", "exact_quotients", "exact_codes"):
         getattr(lib, name).restype = ctypes.c_longlong
     return lib
+
+
+@pytest.mark.parametrize("exponent", [0, 1, 2, 37, 63, 115])
+def test_reciprocal_of_every_mantissa(exact, exponent):
+    assert exact.exact_reciprocals(exponent) == 0
+
+
+def test_sigmoid_without_branches(exact):
+    assert exact.exact_sigmoids() == 0
 
 
 def test_quotients(exact):
