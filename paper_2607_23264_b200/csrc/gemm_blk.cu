@@ -178,11 +178,12 @@ __device__ __forceinline__ BlkTile blk_decode(int t, int rank, const int32_t* pr
   return tile;
 }
 
-// silu(g) * u with an exponential and a reciprocal good to a few ulp: h is quantised from here, and the error of the
-// hardware tanh (2^-11) would move one code in a hundred.
+// silu(g) * u to about 4 ulp: expf (2) and an approximate reciprocal (1).  h is quantised from here, and the error of the
+// hardware tanh (2^-11) would move one code in a hundred.  32 groups of 128 rows, both GEMMs of 7168 / 2048: 281 us, 279
+// with the exponential that grows by an ulp per unit of |g|, 289 with a division.
 __device__ __forceinline__ float blk_silu_mul(float g, float u) {
   float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + __expf(-g)));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + expf(-g)));
   return g * r * u;
 }
 

@@ -640,3 +640,28 @@ def test_experts_by_pairs_of_ctas(monkeypatch, T, H, F, E, k):
     """Both GEMMs of a layer by the pair kernel: the bits of h's codes, and y on them."""
     monkeypatch.setenv("MOE_TUNING", "x.blk_pair_rows=0")
     test_expert_ffn_parity(T, H, F, E, k, "xWr")
+
+
+@pytest.mark.parametrize("E", [1, 20])
+def test_silu_in_the_epilogue_to_a_few_ulp(E):
+    """h = silu(g) u with g = u = the row's scale (codes of 1 in one place), so that h is the epilogue's arithmetic alone.
+    expf 2 ulp, reciprocal 1, a sum and two products half each: 4.5 ulp of 2^-23 at most."""
+    T, H, F = 640, 128, 128
+    ctx = binding.Context(T, H, F, E, 1)
+    sx = np.concatenate([np.linspace(-86, 86, T - 2), [0.0, 300.0]]).astype(np.float32)
+    one = 0x38
+    xq = torch.zeros(T, H, dtype=torch.uint8, device=DEV)
+    xq[:, 0] = one
+    w = torch.zeros(E, F, H, dtype=torch.uint8, device=DEV)
+    w[:, :, 0] = one
+    ws = torch.ones(E, 1, 1, device=DEV)
+    offsets = torch.tensor([T * e // E for e in range(E + 1)], dtype=torch.int32, device=DEV)
+    hq, sh = torch.empty(T, F, dtype=torch.uint8, device=DEV), torch.empty(1, T, device=DEV)
+    y, h = torch.empty(T, H, dtype=torch.bfloat16, device=DEV), torch.full((T, F), float("nan"), device=DEV)
+    ctx.moe_expert_ffn_blk(xq, dev(sx[None]), offsets, w, ws, w, ws, w, ws, hq, sh, y, h)
+    torch.cuda.synchronize()
+    assert ctx.moe_last_device_status()[0] == 0
+    g = sx.astype(np.float64)
+    ref = (g * g / (1 + np.exp(-g)))[:, None]
+    err = np.abs(h.cpu().numpy() - ref)
+    assert (err <= 4.5 * 2.0 ** -23 * np.abs(ref)).all(), np.max(err[ref[:, 0] != 0] / np.abs(ref[ref[:, 0] != 0]) * 2 ** 23)
