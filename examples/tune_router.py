@@ -1,9 +1,10 @@
 """Tunes the router of a fine-grained MoE layer whose experts are frozen in FP8 blocks of 128.
 
-A teacher router defines the layer's target outputs; a student router starts from another matrix and is trained on the
-mean squared error, step by step with the library's calls: scored plan, quantise, dispatch, experts, combine, then the
-gradient of the combine (to the weights) and of the scores (to the logits).  The router matrix itself, its product with x
-and the update are plain torch.  The balance bias moves towards even loads, as it does in training.
+The layer's inputs come from a frozen dense projection in the same form.  A teacher router defines the target outputs; a
+student router starts from another matrix and is trained on the mean squared error, step by step with the library's calls:
+scored plan, quantise, dispatch, experts, combine, then the gradient of the combine (to the weights) and of the scores (to
+the logits).  The router matrix itself, its product with x and the update are plain torch.  The balance bias moves towards
+even loads, as it does in training.  The tuned router then answers through the fused layer, as it would be served.
 
     python examples/tune_router.py [--steps 40]
 """
@@ -17,6 +18,15 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 from paper_2607_23264_b200 import binding  # noqa: E402
 
 
+def frozen_matrix(ctx, mats, rows, cols, g):
+    """Random matrices in blocks of 128: codes and scales."""
+    w = (torch.randn(mats, rows, cols, generator=g, device="cuda") / cols ** 0.5).to(torch.bfloat16)
+    codes = torch.empty(mats, rows, cols, dtype=torch.uint8, device="cuda")
+    scales = torch.empty(mats, rows // 128, cols // 128, device="cuda")
+    ctx.moe_quantize_weights_blk(w, mats, rows, cols, codes, scales)
+    return codes, scales
+
+
 class FrozenLayer:
     """The experts, quantised once, and the buffers that a training loop keeps."""
 
@@ -26,11 +36,8 @@ class FrozenLayer:
         g = torch.Generator(device="cuda").manual_seed(seed)
         self.weights = []
         for rows, cols in ((F, H), (F, H), (H, F)):                     # gate, up, down
-            w = (torch.randn(E, rows, cols, generator=g, device="cuda") / cols ** 0.5).to(torch.bfloat16)
-            codes = torch.empty(E, rows, cols, dtype=torch.uint8, device="cuda")
-            scales = torch.empty(E, rows // 128, cols // 128, device="cuda")
-            self.ctx.moe_quantize_weights_blk(w, E, rows, cols, codes, scales)
-            self.weights += [codes, scales]
+            self.weights += frozen_matrix(self.ctx, E, rows, cols, g)
+        self.projection = frozen_matrix(self.ctx, 1, H, H, g)
         R, i32 = T * k, dict(dtype=torch.int32, device="cuda")
         self.ids, self.w = torch.empty(T, k, **i32), torch.empty(T, k, device="cuda")
         self.counts, self.offsets = torch.empty(E, **i32), torch.empty(E + 1, **i32)
@@ -41,6 +48,14 @@ class FrozenLayer:
         self.hq, self.sh = torch.empty(R, F, **u8), torch.empty(F // 128, R, device="cuda")
         self.y = torch.empty(R, H, dtype=torch.bfloat16, device="cuda")
         self.d_w, self.d_logits = torch.empty(T, k, device="cuda"), torch.empty(T, E, device="cuda")
+        self.workspace = torch.empty(self.ctx.workspace_layout_blk()["total"], **u8)
+
+    def project(self, x):
+        """The frozen dense projection in front of the layer."""
+        out = torch.empty_like(x)
+        self.ctx.moe_quantize_rows_blk(x, self.T, self.H, self.xq, self.sx)
+        self.ctx.moe_gemm_blk(self.xq, self.sx, *self.projection, out, self.T, self.H, self.H)
+        return out
 
     def forward(self, x, logits, bias, rule):
         c, out = self.ctx, torch.empty_like(x)
@@ -49,6 +64,12 @@ class FrozenLayer:
         c.moe_dispatch_blk(self.xq, self.sx, self.inv, self.xp, self.sxp)
         c.moe_expert_ffn_blk(self.xp, self.sxp, self.offsets, *self.weights, self.hq, self.sh, self.y)
         c.moe_combine(self.y, self.inv, self.w, out)
+        return out
+
+    def serve(self, x, logits, bias, rule):
+        """The same output by one call."""
+        out = torch.empty_like(x)
+        self.ctx.moe_fused_forward_blk(x, logits, bias, rule, *self.weights, out, self.workspace)
         return out
 
     def backward_to_logits(self, logits, rule, d_out):
@@ -67,7 +88,7 @@ def main(argv=None):
     layer = FrozenLayer(T, H, F, E, k)
     rule = binding.make_route_rule("sigmoid", n_group=4, topk_group=2, group_top=2, renormalise=True, weight_scale=2.0)
     g = torch.Generator(device="cuda").manual_seed(1)
-    x = torch.randn(T, H, generator=g, device="cuda").to(torch.bfloat16)
+    x = layer.project(torch.randn(T, H, generator=g, device="cuda").to(torch.bfloat16))
     xf = x.float()
     teacher = 2 * torch.randn(H, E, generator=g, device="cuda") / H ** 0.5
     router = teacher + 0.5 * torch.randn(H, E, generator=g, device="cuda") / H ** 0.5
@@ -88,6 +109,9 @@ def main(argv=None):
         if step % 10 == 0 or step == 1:
             spread = layer.counts.float().std() / (T * k / E)
             print(f"step {step:4d}  loss {losses[-1]:.5f}  load spread {float(spread):.3f}", flush=True)
+    tuned = layer.serve(x, xf @ router, bias, rule)
+    losses.append(float((tuned.float() - target).square().mean()))
+    print(f"the tuned router, served: loss {losses[-1]:.5f}", flush=True)
     code, _ = layer.ctx.moe_last_device_status()
     assert code == 0, code
     return losses
