@@ -22,12 +22,14 @@
 // What bounds it and what it measured (E4M3 both, 2 x rows x N x K operations, events over back-to-back runs):
 //   few rows: the weights' bytes.  64 groups of 2 rows, 2048 x 7168: 143 us, 6.56 TB/s; 17 rows, 4096 x 7168: 11.7 us,
 //     of which about 5 are the launch and the cluster's sums.
-//   128 rows a group: 184 us, 5.6 TB/s, 1.3 PFLOP/s: the drain of the accumulators, 256 x 128 multiply-adds per block of
-//     K and 128-row tile on the CUDA cores beside the loads.
-//   many rows: 8 groups of 2048, 4096 x 7168: 437 us, 2.2 PFLOP/s.  The scale per block of 128 makes every accumulator
-//     leave tensor memory after four instructions, so the epilogue's loads and multiply-adds (about 800 clocks per block
-//     and SM, against 512 of the tensor pipe) bound the tile; under a long load the power cap does: 8192 rows, 4096 x
-//     7168 take 212 us from rest and 256 sustained.
+//   128 rows a group, 64 groups, 2048 x 7168: 182 us, 5.6 TB/s, 1.3 PFLOP/s: the copies and the MMAs.  Without the drain's
+//     multiply-adds, and without its loads from tensor memory too, it takes 177.
+//   many rows: one group of 8192, 4096 x 7168: 224 us from rest.  Without the drain's loads from tensor memory 228, without
+//     its multiply-adds 181, without both 162 (147 at twice the cuBLAS bf16 rate): 40 to 60 us are the multiply-adds: the
+//     scale per block of 128 makes every accumulator leave tensor memory after four instructions and it is handed back when
+//     seven eighths of it are added.  Under a long load the power cap bounds it (256 us sustained).  8 groups of 2048: 434 us,
+//     2.2 PFLOP/s; 440, 361 and 333 in the same way.
+//   16 groups of 256, 4096 x 4096: 88 us; without multiply-adds 80, without loads 84.
 // Measured and not kept: prefetching the weights into L2 some blocks ahead (143 -> 180 us at 2 rows), 32 accumulator
 // columns per load and packed pairs of multiply-adds (more registers, slower), sixteen epilogue warps.
 //
@@ -80,7 +82,9 @@ struct BlkParams {
   const float* sa;          // [k_blocks][rows]
   const float* sb0;         // [groups][n_blocks][k_blocks]; gated: gate
   const float* sb1;         // gated: up
-  __nv_bfloat16* y;         // [rows, N]
+  __nv_bfloat16* y;         // [rows, N]: the product's one rounding.  In a layer it precedes the weighted sum of a token's rows,
+                            // as in the library's other forms: combine then reads half the bytes of fp32 rows, and the
+                            // rounding (1.7e-3 of the norm) joins that of the quantised h (3.5e-3) as independent error
   uint32_t* hq;             // gated: E4M3 [rows, N], four codes per word
   float* sh;                // gated: [N/128][rows]
   float* h_dbg;             // gated: optional fp32 [rows, N]
@@ -808,7 +812,7 @@ long long most_tiles(const BlkParams& p, int block_rows) {
 
 // CTAs per tile along K: the most, up to eight, for which every tile's cluster is resident at once, and no more than give
 // each CTA fewer blocks.  (A cluster lies within a GPC: sixteen clusters of eight do not fit, and a second wave costs more
-// than the longer loops: 17 rows, 4096 x 7168 took 18 us with eight CTAs per tile and 12 with four.)
+// than the longer loops: 17 rows, 4096 x 7168 took 18 us with eight CTAs per tile and 12 with six, 96 CTAs.)
 int k_split(const moe_ctx* ctx, long long tiles, int k_blocks) {
   int split = 8;
   while (split > 1 && (split > k_blocks || tiles > ctx->blk_clusters[split])) --split;

@@ -563,6 +563,8 @@ def test_quantize_the_longest_row(ctx):
         assert bool((codes[:whole].view(-1, period) == small_c).all()) and torch.equal(codes[whole:], tail_c)
         assert bool((scales[:whole // 128].view(-1, period // 128) == small_s).all())
         assert torch.equal(scales[whole // 128:], tail_s)
+    del x, codes, scales
+    torch.cuda.empty_cache()
 
 
 def test_product_with_the_longest_k(ctx):
@@ -579,6 +581,8 @@ def test_product_with_the_longest_k(ctx):
     torch.cuda.synchronize()
     assert ctx.moe_last_device_status()[0] == 0
     assert y[0].tolist() == [7.0 + n for n in range(N)]
+    del a, b, ones
+    torch.cuda.empty_cache()
 
 
 def test_more_blocks_than_a_grid_holds_are_refused(ctx):
