@@ -34,8 +34,8 @@ typedef enum {
   MOE_ERR_INVALID_ARG = 1,         /* null pointer, misaligned pointer, wrong device, bad tuning value */
   MOE_ERR_UNSUPPORTED_SHAPE = 2,   /* H or F not a multiple of 64, k or E out of range, T < 0 */
   MOE_ERR_WORKSPACE_TOO_SMALL = 3,
-  MOE_ERR_BAD_ROUTING = 4,         /* device status: an expert id given to moe_plan_routing_from_topk is outside
-                                      [0, E); returned by a call only from the debug check of the logits
+  MOE_ERR_BAD_ROUTING = 4,         /* device status: an expert id given to moe_plan_routing_from_topk (or to a call that
+                                      says so) is outside [0, E), or an adapter's index; returned by a call only from the debug check of the logits
                                       (MOE_TUNING entry x.check_logits=1: non-finite logits, tested on the host) */
   MOE_ERR_CUDA = 5,                /* a CUDA runtime or driver call failed */
   MOE_ERR_TIMEOUT = 6,             /* device status only: a bounded on-device wait expired */
@@ -564,6 +564,138 @@ moe_status moe_fused_forward_blk(moe_ctx* ctx, const void* x, const float* logit
                                  const moe_route_rule* rule, const void* wq_gate, const float* s_gate,
                                  const void* wq_up, const float* s_up, const void* wq_down, const float* s_down,
                                  void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Residual addition and RMS norm: what stands in front of the layer.  For a row of x (and of residual, when given):
+ *     s      = bf16(x + residual)                       (the stream as the next layer reads it; s = x without a residual)
+ *     n_c    = s_c * rsqrt(mean(s^2) + eps) * (gain_c + gain_offset)
+ *     out    = bf16(n), codes and scales = n in 8 bits, in the form its reader takes:
+ *       MOE_FORM_ROWS  fp32 scales [rows]                                (moe_dispatch_fp8)
+ *       MOE_FORM_MX    scale bytes as uint32 words [cols/128][rows]      (moe_dispatch_mx)
+ *       MOE_FORM_BLK   fp32 scales [ceil(cols/128)][rows]                (moe_dispatch_blk, moe_gemm_blk)
+ * with the scale and rounding rules of moe_quantize_rows, moe_quantize_rows_mx and moe_quantize_rows_blk, applied to n
+ * before it is rounded to bf16.  Statistics and n are fp32.  A row of zeros gives zeros.  An infinite or NaN element makes its row
+ * NaN where torch's fp32 formula does; a row whose sum of squares leaves fp32 (elements above 1e19) gives zeros.
+ * Limits: 0 <= rows < 2^30, 8 <= cols <= 32768, cols a multiple of 8 (16 for MOE_FORM_BLK, 128 for MOE_FORM_MX), else
+ * UNSUPPORTED_SHAPE; eps positive and finite, gain_offset finite, at least one output, else INVALID_ARG.
+ * sum_out and out may be the buffers of x or residual; no other buffers may overlap.
+ * ------------------------------------------------------------------------------------------------ */
+enum { MOE_FORM_NONE = 0, MOE_FORM_ROWS = 1, MOE_FORM_MX = 2, MOE_FORM_BLK = 3 };
+typedef struct {
+  const void* x;            /* bf16 [rows, cols] */
+  const void* residual;     /* bf16 [rows, cols], or NULL: nothing is added */
+  const void* gain;         /* [cols], bf16 or (gain_fp32 1) fp32 */
+  void* sum_out;            /* out: bf16 [rows, cols] s, or NULL */
+  void* out;                /* out: bf16 [rows, cols], or NULL */
+  void* codes;              /* out: E4M3 [rows, cols]; NULL with MOE_FORM_NONE */
+  void* scales;             /* out: by form; NULL with MOE_FORM_NONE */
+  int64_t rows;
+  int32_t cols;
+  int32_t gain_fp32;        /* 0 or 1 */
+  int32_t form;             /* MOE_FORM_* */
+  float eps;
+  float gain_offset;        /* 0, or 1 for gains stored as their distance from one */
+} moe_rms_norm_args;
+moe_status moe_add_rms_norm(moe_ctx* ctx, const moe_rms_norm_args* args, void* stream);
+
+/*
+ * Gradient of that norm (an 8-bit output passes its reader's gradient on as it comes).  With h = s rstd and
+ * g_c = (gain_c + gain_offset) d_out_c of a row:
+ *     d_x    = bf16( d_sum + rstd (g - h mean(g h)) )   (the gradient of x and of residual alike)
+ *     d_gain = sum over rows of d_out h                 (fp32, fixed order)
+ * scratch: moe_rms_norm_scratch_bytes bytes on the device when d_gain is asked for (undefined after).  d_x may be the buffer of
+ * d_out or d_sum.  rows == 0 gives a d_gain of zeros.  Limits as above.  Errors: as above, and WORKSPACE_TOO_SMALL.
+ */
+typedef struct {
+  const void* s;            /* bf16 [rows, cols]: what the forward call normalised (its sum_out, or x) */
+  const void* gain;         /* as in the forward call */
+  const void* d_out;        /* bf16 [rows, cols]: gradient of the normalised rows */
+  const void* d_sum;        /* bf16 [rows, cols]: gradient that reaches s past the norm, or NULL */
+  void* d_x;                /* out: bf16 [rows, cols], or NULL (only d_gain is wanted) */
+  float* d_gain;            /* out: fp32 [cols], or NULL (frozen gain) */
+  void* scratch;
+  size_t scratch_bytes;
+  int64_t rows;
+  int32_t cols;
+  int32_t gain_fp32;
+  float eps;
+  float gain_offset;
+} moe_rms_norm_grad_args;
+size_t moe_rms_norm_scratch_bytes(const moe_ctx* ctx, int64_t rows, int32_t cols);   /* 0 for sizes the call refuses */
+moe_status moe_rms_norm_backward(moe_ctx* ctx, const moe_rms_norm_grad_args* args, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Balance loss of a router, its counts and gradient, over the context's active tokens, E experts and k slots.  A token counts
+ * when its mask is not 0 and it lies in a sequence: seq_offsets[q] <= t < seq_offsets[q+1].  For sequence q with n_q counted
+ * tokens:
+ *     p_te    = softmax(x_t)_e, or sigma(x_te) / sum_i sigma(x_ti)
+ *     c_qe    = slots of its counted tokens that chose e,   P_qe = mean of p_te over them
+ *     loss[0] = coef / sequences * sum_q sum_e (E c_qe / (k n_q)) P_qe       (an empty sequence adds 0)
+ *     loss[1] = z_coef * mean over all counted tokens of (log sum_e exp x_te)^2
+ * One sequence of all tokens is the loss over the batch; even loads and probabilities give coef.  The choice is held fixed,
+ * so the gradient reaches the logits through P and through the logarithm: for d = d_loss[0] (1 when NULL) times both losses,
+ *     u_e = d coef E c_qe / (sequences k n_q^2),   d_x_e = p_e (u_e - sum_i u_i p_i) [softmax], times sigma(-x_e) [sigmoid],
+ *           + d 2 z_coef / n * log(sum exp x) * softmax(x)_e
+ * and 0 for tokens that do not count.  d_logits = add + that (add: e.g. the gradient moe_routing_backward wrote; NULL for 0;
+ * may be d_logits itself).
+ * Masks: a logit of -inf takes no part and gets no gradient; a token whose logits are all -inf has p = 0 and adds nothing to either
+ * loss (it counts in n).  A NaN logit (or +inf: see moe_routing_backward) of a counted token makes its own row of d_logits
+ * and the losses NaN.  An id outside [0, E) is reported through the status word (MOE_ERR_BAD_ROUTING, detail = the flat slot
+ * t*k+j) and not counted.
+ * Sums are fp32 in a fixed order: the same bits every time.  scratch: moe_balance_scratch_bytes bytes (undefined after);
+ * two calls that overlap on the GPU need one each.
+ * Limits: 1 <= sequences <= 2^20; coef, z_coef finite; seq_offsets NULL only with one sequence.
+ * ------------------------------------------------------------------------------------------------ */
+typedef struct {
+  const float* logits;        /* fp32 [T, E] */
+  const int32_t* topk_ids;    /* int32 [T, k] (not read by the gradient) */
+  const int32_t* seq_offsets; /* int32 [sequences + 1], ascending from 0 to at most T, or NULL: one sequence of all tokens */
+  const uint8_t* token_mask;  /* [T], 0 = the token does not count, or NULL */
+  int32_t sequences;
+  int32_t score;              /* MOE_SCORE_SOFTMAX or MOE_SCORE_SIGMOID */
+  float coef, z_coef;
+} moe_balance_args;
+size_t moe_balance_scratch_bytes(const moe_ctx* ctx, int32_t sequences);
+/* -> counts [sequences, E] int32, tokens [sequences + 1] int32 (n_q, then their sum), mean [sequences, E] fp32 (P; 0 for an
+ * empty sequence), loss [2] fp32. */
+moe_status moe_balance_loss(moe_ctx* ctx, const moe_balance_args* args, int32_t* counts, int32_t* tokens, float* mean,
+                            float* loss, void* scratch, size_t scratch_bytes, void* stream);
+/* counts and tokens as the forward call wrote them; d_loss: device fp32 [1], or NULL; add: fp32 [T, E], or NULL. */
+moe_status moe_balance_loss_backward(moe_ctx* ctx, const moe_balance_args* args, const int32_t* counts,
+                                     const int32_t* tokens, const float* d_loss, const float* add, float* d_logits,
+                                     void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Low-rank adapters of many requests beside a shared projection (moe_gemm_blk, or any other).  Rows belong to segments
+ * (requests), a segment to an adapter i or to none:
+ *     y_out[r,n] = bf16( y_in[r,n] + scale_i * sum_j b[i,n,j] t[r,j] ),   t[r,j] = sum_k x[r,k] a[i,j,k]
+ * with fp32 sums (t enters the second product as two bf16 terms, 16 bits of it).  Rows without an adapter, and rows behind
+ * the last segment, are copied bit for bit.  Prompts are long segments, decoded tokens segments of one row (offsets NULL: every
+ * row is a segment), in any mixture; neighbouring rows of one adapter share its reads.  The gradient with respect to x is the
+ * same call with a and b exchanged, each transposed.
+ *   x [rows, K] bf16, a [adapters, rank, K] bf16, b [adapters, N, rank] bf16, y_in, y_out [rows, N] bf16 (y_out may be y_in).
+ * An adapter index >= adapters is reported through the status word (MOE_ERR_BAD_ROUTING, detail = the segment) and its rows
+ * are copied.  A lower-ranked adapter is padded with zeros.
+ * scratch: moe_adapter_scratch_bytes bytes (undefined after); two calls that overlap on the GPU need one each.
+ * Limits: 0 <= rows < 2^30; N, K multiples of 8; rank a multiple of 8, at most 128; 1 <= adapters, adapters * rank and
+ * adapters * N < 2^31; 0 <= segments <= rows (segments == rows when offsets is NULL), else UNSUPPORTED_SHAPE.
+ * ------------------------------------------------------------------------------------------------ */
+typedef struct {
+  const void* x;              /* bf16 [rows, K] */
+  const void* a;              /* bf16 [adapters, rank, K] */
+  const void* b;              /* bf16 [adapters, N, rank] */
+  const float* scale;         /* fp32 [adapters], or NULL: 1 */
+  const int32_t* offsets;     /* int32 [segments + 1], ascending from 0 to at most rows, or NULL */
+  const int32_t* adapter_of;  /* int32 [segments]; negative: none */
+  const void* y_in;           /* bf16 [rows, N] */
+  void* y_out;                /* out: bf16 [rows, N] */
+  void* scratch;
+  size_t scratch_bytes;
+  int64_t rows;
+  int32_t N, K, rank, adapters, segments;
+} moe_adapter_args;
+size_t moe_adapter_scratch_bytes(const moe_ctx* ctx, int64_t rows, int32_t K, int32_t rank);   /* 0 for refused sizes */
+moe_status moe_add_adapters(moe_ctx* ctx, const moe_adapter_args* args, void* stream);
 
 /*
  * The host-buffer call as a two-deep pipeline, for callers that run step after step (serving): consecutive calls

@@ -31,7 +31,9 @@ EXPORTS = (
     "moe_expert_ffn_mx", "moe_get_workspace_layout_mx", "moe_fused_forward_mx", "moe_probe_mma_cycles_kind",
     "moe_parse_tuning", "moe_get_kernel_times_back", "moe_plan_routing_scored", "moe_routing_backward",
     "moe_combine_backward", "moe_quantize_rows_blk", "moe_quantize_weights_blk", "moe_dispatch_blk", "moe_gemm_blk",
-    "moe_expert_ffn_blk", "moe_get_workspace_layout_blk", "moe_fused_forward_blk",
+    "moe_expert_ffn_blk", "moe_get_workspace_layout_blk", "moe_fused_forward_blk", "moe_add_rms_norm",
+    "moe_rms_norm_backward", "moe_rms_norm_scratch_bytes", "moe_balance_loss", "moe_balance_loss_backward",
+    "moe_balance_scratch_bytes", "moe_add_adapters", "moe_adapter_scratch_bytes",
 )
 
 TIMING_SLOTS = 32     # timed calls whose per-kernel events the library keeps (moe_get_kernel_times_back)
@@ -108,6 +110,32 @@ class moe_workspace_layout_blk(C.Structure):
                                           "sx_perm", "hq", "sh", "y_perm", "total")]
 
 
+FORMS = {"none": 0, "rows": 1, "mx": 2, "blk": 3}
+
+
+class moe_rms_norm_args(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("x", "residual", "gain", "sum_out", "out", "codes", "scales")] + [
+        ("rows", C.c_int64), ("cols", C.c_int32), ("gain_fp32", C.c_int32), ("form", C.c_int32), ("eps", C.c_float),
+        ("gain_offset", C.c_float)]
+
+
+class moe_rms_norm_grad_args(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("s", "gain", "d_out", "d_sum", "d_x", "d_gain", "scratch")] + [
+        ("scratch_bytes", C.c_size_t), ("rows", C.c_int64), ("cols", C.c_int32), ("gain_fp32", C.c_int32),
+        ("eps", C.c_float), ("gain_offset", C.c_float)]
+
+
+class moe_balance_args(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("logits", "topk_ids", "seq_offsets", "token_mask")] + [
+        ("sequences", C.c_int32), ("score", C.c_int32), ("coef", C.c_float), ("z_coef", C.c_float)]
+
+
+class moe_adapter_args(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("x", "a", "b", "scale", "offsets", "adapter_of", "y_in", "y_out", "scratch")] + [
+        ("scratch_bytes", C.c_size_t), ("rows", C.c_int64)] + [
+        (n, C.c_int32) for n in ("N", "K", "rank", "adapters", "segments")]
+
+
 _lib = None
 
 
@@ -172,6 +200,16 @@ def load_library() -> C.CDLL:
     lib.moe_get_workspace_layout_blk.argtypes = [C.POINTER(moe_shape), C.POINTER(moe_workspace_layout_blk)]
     lib.moe_fused_forward_blk.argtypes = [vp, vp, f32p, f32p, C.POINTER(moe_route_rule), vp, f32p, vp, f32p, vp, f32p,
                                           vp, vp, C.c_size_t, vp]
+    lib.moe_add_rms_norm.argtypes = [vp, C.POINTER(moe_rms_norm_args), vp]
+    lib.moe_rms_norm_backward.argtypes = [vp, C.POINTER(moe_rms_norm_grad_args), vp]
+    lib.moe_balance_loss.argtypes = [vp, C.POINTER(moe_balance_args), i32p, i32p, f32p, f32p, vp, C.c_size_t, vp]
+    lib.moe_balance_loss_backward.argtypes = [vp, C.POINTER(moe_balance_args), i32p, i32p, f32p, f32p, f32p, vp]
+    lib.moe_add_adapters.argtypes = [vp, C.POINTER(moe_adapter_args), vp]
+    lib.moe_rms_norm_scratch_bytes.argtypes = [vp, C.c_int64, C.c_int32]
+    lib.moe_balance_scratch_bytes.argtypes = [vp, C.c_int32]
+    lib.moe_adapter_scratch_bytes.argtypes = [vp, C.c_int64, C.c_int32, C.c_int32]
+    for name in ("moe_rms_norm_scratch_bytes", "moe_balance_scratch_bytes", "moe_adapter_scratch_bytes"):
+        getattr(lib, name).restype = C.c_size_t
     lib.moe_last_device_status.argtypes = [vp, C.POINTER(C.c_int32), C.POINTER(C.c_int32), vp]
     lib.moe_last_launch_count.argtypes = [vp]
     lib.moe_last_launch_count.restype = C.c_int32
@@ -184,7 +222,8 @@ def load_library() -> C.CDLL:
     lib.moe_get_ffn_trace.argtypes = [vp, C.POINTER(C.c_uint64), C.c_int32, C.POINTER(C.c_int32), vp]
     for name in EXPORTS:
         if name not in ("moe_status_string", "moe_destroy", "moe_workspace_bytes", "moe_last_launch_count",
-                        "moe_router_weight_bytes", "moe_router_scratch_bytes"):
+                        "moe_router_weight_bytes", "moe_router_scratch_bytes", "moe_rms_norm_scratch_bytes",
+                        "moe_balance_scratch_bytes", "moe_adapter_scratch_bytes"):
             getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib
@@ -229,6 +268,23 @@ def make_route_rule(score="softmax", n_group=1, topk_group=1, group_top=1, renor
     if score not in SCORES:
         raise ValueError(f"score must be one of {sorted(SCORES)}, got {score!r}")
     return moe_route_rule(SCORES[score], n_group, topk_group, group_top, 1 if renormalise else 0, weight_scale)
+
+
+def _lookup(table, name, what):
+    if name not in table:
+        raise ValueError(f"{what} must be one of {sorted(table)}, got {name!r}")
+    return table[name]
+
+
+def _gain_fp32(gain):
+    """1 for an fp32 gain, 0 for a bf16 one."""
+    if gain is None or gain.element_size() not in (2, 4):
+        raise ValueError("the gain is a bf16 or fp32 tensor")
+    return 1 if gain.element_size() == 4 else 0
+
+
+def _size(t):
+    return 0 if t is None else t.numel() * t.element_size()
 
 
 def moe_parse_tuning(text):
@@ -502,6 +558,56 @@ class Context:
                                                _ptr(s_down), _ptr(out), _ptr(workspace),
                                                workspace.numel() * workspace.element_size(), _stream(stream)),
                "moe_fused_forward_blk")
+
+    # ---- in front of the layer: residual addition and RMS norm
+    def moe_add_rms_norm(self, x, residual, gain, rows, cols, sum_out=None, out=None, codes=None, scales=None,
+                         form="none", eps=1e-6, gain_offset=0.0, stream=None):
+        """residual may be None; form is "none", "rows", "mx" or "blk"; the gain is bf16 or fp32."""
+        args = moe_rms_norm_args(_ptr(x), _ptr(residual), _ptr(gain), _ptr(sum_out), _ptr(out), _ptr(codes), _ptr(scales),
+                                 rows, cols, _gain_fp32(gain), _lookup(FORMS, form, "form"), eps, gain_offset)
+        _check(self._lib.moe_add_rms_norm(self._handle, C.byref(args), _stream(stream)), "moe_add_rms_norm")
+
+    def rms_norm_scratch_bytes(self, rows, cols) -> int:
+        """Bytes of the scratch moe_rms_norm_backward needs when d_gain is asked for."""
+        return int(self._lib.moe_rms_norm_scratch_bytes(self._handle, rows, cols))
+
+    def moe_rms_norm_backward(self, s, gain, d_out, rows, cols, d_x, d_gain, scratch=None, d_sum=None, eps=1e-6,
+                              gain_offset=0.0, stream=None):
+        """d_x or d_gain may be None; scratch is needed for d_gain only."""
+        args = moe_rms_norm_grad_args(_ptr(s), _ptr(gain), _ptr(d_out), _ptr(d_sum), _ptr(d_x), _ptr(d_gain),
+                                      _ptr(scratch), _size(scratch), rows, cols, _gain_fp32(gain), eps, gain_offset)
+        _check(self._lib.moe_rms_norm_backward(self._handle, C.byref(args), _stream(stream)), "moe_rms_norm_backward")
+
+    # ---- balance loss of the router
+    def balance_scratch_bytes(self, sequences=1) -> int:
+        return int(self._lib.moe_balance_scratch_bytes(self._handle, sequences))
+
+    def moe_balance_loss(self, logits, topk_ids, counts, tokens, mean, loss, scratch, score="softmax", coef=1.0,
+                         z_coef=0.0, sequences=1, seq_offsets=None, token_mask=None, stream=None):
+        args = moe_balance_args(_ptr(logits), _ptr(topk_ids), _ptr(seq_offsets), _ptr(token_mask), sequences,
+                                _lookup(SCORES, score, "score"), coef, z_coef)
+        _check(self._lib.moe_balance_loss(self._handle, C.byref(args), _ptr(counts), _ptr(tokens), _ptr(mean), _ptr(loss),
+                                          _ptr(scratch), _size(scratch), _stream(stream)), "moe_balance_loss")
+
+    def moe_balance_loss_backward(self, logits, counts, tokens, d_logits, d_loss=None, add=None, score="softmax", coef=1.0,
+                                  z_coef=0.0, sequences=1, seq_offsets=None, token_mask=None, stream=None):
+        """d_loss: one fp32 on the device (None: 1); add: a gradient to add to, d_logits itself allowed."""
+        args = moe_balance_args(_ptr(logits), None, _ptr(seq_offsets), _ptr(token_mask), sequences,
+                                _lookup(SCORES, score, "score"), coef, z_coef)
+        _check(self._lib.moe_balance_loss_backward(self._handle, C.byref(args), _ptr(counts), _ptr(tokens), _ptr(d_loss),
+                                                   _ptr(add), _ptr(d_logits), _stream(stream)),
+               "moe_balance_loss_backward")
+
+    # ---- adapters beside a shared projection
+    def adapter_scratch_bytes(self, rows, K, rank) -> int:
+        return int(self._lib.moe_adapter_scratch_bytes(self._handle, rows, K, rank))
+
+    def moe_add_adapters(self, x, a, b, adapter_of, y_in, y_out, scratch, rows, N, K, rank, adapters, segments, offsets=None,
+                         scale=None, stream=None):
+        """offsets None: every row is a segment of its own; scale None: 1."""
+        args = moe_adapter_args(_ptr(x), _ptr(a), _ptr(b), _ptr(scale), _ptr(offsets), _ptr(adapter_of), _ptr(y_in),
+                                _ptr(y_out), _ptr(scratch), _size(scratch), rows, N, K, rank, adapters, segments)
+        _check(self._lib.moe_add_adapters(self._handle, C.byref(args), _stream(stream)), "moe_add_adapters")
 
     def moe_last_device_status(self, stream=None):
         code, detail = C.c_int32(0), C.c_int32(0)

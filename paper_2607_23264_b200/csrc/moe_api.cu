@@ -1,4 +1,5 @@
 // Host side of the C ABI (include/moe.h): argument validation, context, workspace carving, call order.
+#include <cfloat>
 #include <climits>
 #include <cstdio>
 #include <cstdlib>
@@ -1068,6 +1069,146 @@ moe_status moe_fused_forward_blk(moe_ctx* ctx, const void* x, const float* logit
   if (st != MOE_OK) return st;
   if (moe::launch_combine(ctx, ws + L.y_perm, inv_perm, topk_w, out, cs) != cudaSuccess) return MOE_ERR_CUDA;
   return MOE_OK;
+}
+
+// ------------------------------------------------------------------------------------------------ around the layer
+
+namespace {
+
+moe_status check_norm_sizes(int64_t rows, int32_t cols) {
+  return rows < 0 || rows >= (1LL << 30) || cols < 8 || cols > 32768 || cols % 8 != 0 ? MOE_ERR_UNSUPPORTED_SHAPE : MOE_OK;
+}
+bool positive_finite(float v) { return v > 0.f && v <= FLT_MAX; }
+bool finite(float v) { return v >= -FLT_MAX && v <= FLT_MAX; }
+
+moe_status check_balance(const moe_ctx* ctx, const moe_balance_args* a) {
+  if (!a) return MOE_ERR_INVALID_ARG;
+  if (a->score != MOE_SCORE_SOFTMAX && a->score != MOE_SCORE_SIGMOID) return MOE_ERR_INVALID_ARG;
+  if (!finite(a->coef) || !finite(a->z_coef)) return MOE_ERR_INVALID_ARG;
+  if (a->sequences < 1 || a->sequences > (1 << 20)) return MOE_ERR_UNSUPPORTED_SHAPE;
+  if (!a->seq_offsets && a->sequences != 1) return MOE_ERR_INVALID_ARG;
+  if (!aligned16(a->seq_offsets) || !aligned16(a->token_mask)) return MOE_ERR_INVALID_ARG;
+  if (ctx->shape.T > 0 && (!a->logits || !aligned16(a->logits))) return MOE_ERR_INVALID_ARG;
+  return MOE_OK;
+}
+
+bool adapter_sizes_ok(int64_t rows, int32_t K, int32_t rank) {
+  return rows >= 0 && rows < (1LL << 30) && K >= 8 && K % 8 == 0 && rank >= 8 && rank <= 128 && rank % 8 == 0;
+}
+
+}  // namespace
+
+moe_status moe_add_rms_norm(moe_ctx* ctx, const moe_rms_norm_args* a, void* stream) {
+  moe_status st = check_ctx(ctx);
+  if (st != MOE_OK) return st;
+  ctx->last_launches = 0;
+  if (!a) return MOE_ERR_INVALID_ARG;
+  st = check_norm_sizes(a->rows, a->cols);
+  if (st != MOE_OK) return st;
+  if (a->form < MOE_FORM_NONE || a->form > MOE_FORM_BLK || (a->gain_fp32 & ~1) != 0 || !positive_finite(a->eps) ||
+      !finite(a->gain_offset))
+    return MOE_ERR_INVALID_ARG;
+  if ((a->form == MOE_FORM_BLK && a->cols % 16 != 0) || (a->form == MOE_FORM_MX && a->cols % 128 != 0))
+    return MOE_ERR_UNSUPPORTED_SHAPE;
+  if (a->rows == 0) return MOE_OK;
+  const bool coded = a->form != MOE_FORM_NONE;
+  if (!a->x || !a->gain || coded != (a->codes != nullptr) || coded != (a->scales != nullptr)) return MOE_ERR_INVALID_ARG;
+  if (!a->sum_out && !a->out && !coded) return MOE_ERR_INVALID_ARG;
+  if (a->sum_out && a->sum_out == a->out) return MOE_ERR_INVALID_ARG;
+  const void* ptrs[] = {a->x, a->residual, a->gain, a->sum_out, a->out, a->codes, a->scales};
+  for (const void* q : ptrs)
+    if (!aligned16(q)) return MOE_ERR_INVALID_ARG;
+  return moe::launch_add_rms_norm(ctx, *a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+}
+
+size_t moe_rms_norm_scratch_bytes(const moe_ctx* ctx, int64_t rows, int32_t cols) {
+  if (!ctx || check_norm_sizes(rows, cols) != MOE_OK) return 0;
+  return moe::rms_norm_scratch_bytes(ctx, rows, cols);
+}
+
+moe_status moe_rms_norm_backward(moe_ctx* ctx, const moe_rms_norm_grad_args* a, void* stream) {
+  moe_status st = check_ctx(ctx);
+  if (st != MOE_OK) return st;
+  ctx->last_launches = 0;
+  if (!a) return MOE_ERR_INVALID_ARG;
+  st = check_norm_sizes(a->rows, a->cols);
+  if (st != MOE_OK) return st;
+  if ((a->gain_fp32 & ~1) != 0 || !positive_finite(a->eps) || !finite(a->gain_offset)) return MOE_ERR_INVALID_ARG;
+  const void* ptrs[] = {a->s, a->gain, a->d_out, a->d_sum, a->d_x, a->d_gain, a->scratch};
+  for (const void* q : ptrs)
+    if (!aligned16(q)) return MOE_ERR_INVALID_ARG;
+  if (a->rows > 0) {
+    if (!a->s || !a->gain || !a->d_out || (!a->d_x && !a->d_gain) || (a->d_gain && !a->scratch)) return MOE_ERR_INVALID_ARG;
+    if (a->d_gain && a->scratch_bytes < moe::rms_norm_scratch_bytes(ctx, a->rows, a->cols))
+      return MOE_ERR_WORKSPACE_TOO_SMALL;
+  }
+  return moe::launch_rms_norm_backward(ctx, *a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+}
+
+size_t moe_balance_scratch_bytes(const moe_ctx* ctx, int32_t sequences) {
+  if (!ctx || sequences < 1 || sequences > (1 << 20)) return 0;
+  return moe::balance_scratch_bytes(ctx, sequences);
+}
+
+moe_status moe_balance_loss(moe_ctx* ctx, const moe_balance_args* a, int32_t* counts, int32_t* tokens, float* mean,
+                            float* loss, void* scratch, size_t scratch_bytes, void* stream) {
+  moe_status st = check_ctx(ctx);
+  if (st != MOE_OK) return st;
+  ctx->last_launches = 0;
+  st = check_balance(ctx, a);
+  if (st != MOE_OK) return st;
+  if (ctx->shape.T > 0 && (!a->topk_ids || !aligned16(a->topk_ids))) return MOE_ERR_INVALID_ARG;
+  const void* ptrs[] = {counts, tokens, mean, loss, scratch};
+  for (const void* q : ptrs)
+    if (!q || !aligned16(q)) return MOE_ERR_INVALID_ARG;
+  if (scratch_bytes < moe::balance_scratch_bytes(ctx, a->sequences)) return MOE_ERR_WORKSPACE_TOO_SMALL;
+  return moe::launch_balance_loss(ctx, *a, counts, tokens, mean, loss, scratch, static_cast<cudaStream_t>(stream)) ==
+                 cudaSuccess
+             ? MOE_OK
+             : MOE_ERR_CUDA;
+}
+
+moe_status moe_balance_loss_backward(moe_ctx* ctx, const moe_balance_args* a, const int32_t* counts,
+                                     const int32_t* tokens, const float* d_loss, const float* add, float* d_logits,
+                                     void* stream) {
+  moe_status st = check_ctx(ctx);
+  if (st != MOE_OK) return st;
+  ctx->last_launches = 0;
+  st = check_balance(ctx, a);
+  if (st != MOE_OK) return st;
+  if (ctx->shape.T == 0) return MOE_OK;
+  const void* ptrs[] = {counts, tokens, d_logits};
+  for (const void* q : ptrs)
+    if (!q || !aligned16(q)) return MOE_ERR_INVALID_ARG;
+  if (!aligned16(d_loss) || !aligned16(add)) return MOE_ERR_INVALID_ARG;
+  return moe::launch_balance_loss_backward(ctx, *a, counts, tokens, d_loss, add, d_logits,
+                                           static_cast<cudaStream_t>(stream)) == cudaSuccess
+             ? MOE_OK
+             : MOE_ERR_CUDA;
+}
+
+size_t moe_adapter_scratch_bytes(const moe_ctx* ctx, int64_t rows, int32_t K, int32_t rank) {
+  return ctx && adapter_sizes_ok(rows, K, rank) ? moe::adapter_scratch_bytes(ctx, rows, K, rank) : 0;
+}
+
+moe_status moe_add_adapters(moe_ctx* ctx, const moe_adapter_args* a, void* stream) {
+  moe_status st = check_ctx(ctx);
+  if (st != MOE_OK) return st;
+  ctx->last_launches = 0;
+  if (!a) return MOE_ERR_INVALID_ARG;
+  if (!adapter_sizes_ok(a->rows, a->K, a->rank) || a->N < 8 || a->N % 8 != 0 || a->adapters < 1 ||
+      static_cast<long long>(a->adapters) * a->rank > 0x7FFFFFFFLL ||
+      static_cast<long long>(a->adapters) * a->N > 0x7FFFFFFFLL || a->segments < 0 || a->segments > a->rows)
+    return MOE_ERR_UNSUPPORTED_SHAPE;
+  if (!a->offsets && a->segments != a->rows) return MOE_ERR_INVALID_ARG;
+  if (a->rows == 0) return MOE_OK;
+  const void* ptrs[] = {a->x, a->a, a->b, a->y_in, a->y_out, a->scratch};
+  for (const void* q : ptrs)
+    if (!q || !aligned16(q)) return MOE_ERR_INVALID_ARG;
+  if (a->segments > 0 && !a->adapter_of) return MOE_ERR_INVALID_ARG;
+  if (!aligned16(a->adapter_of) || !aligned16(a->offsets) || !aligned16(a->scale)) return MOE_ERR_INVALID_ARG;
+  if (a->scratch_bytes < moe::adapter_scratch_bytes(ctx, a->rows, a->K, a->rank)) return MOE_ERR_WORKSPACE_TOO_SMALL;
+  return moe::launch_add_adapters(ctx, *a, static_cast<cudaStream_t>(stream));
 }
 
 // ------------------------------------------------------------------------------------------------ host buffers

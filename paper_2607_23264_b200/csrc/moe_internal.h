@@ -179,6 +179,23 @@ cudaError_t prepare_gemm_blk(moe_ctx* ctx);   // one-time kernel attributes
 moe_status launch_gemm_blk(moe_ctx* ctx, const moe_gemm_blk_args* args, cudaStream_t stream);
 moe_status launch_expert_ffn_blk(moe_ctx* ctx, const moe_blk_ffn_args* args, cudaStream_t stream);
 
+// Residual addition and RMS norm with its outputs, and its gradients (arguments already checked).
+cudaError_t launch_add_rms_norm(moe_ctx* ctx, const moe_rms_norm_args& args, cudaStream_t stream);
+size_t rms_norm_scratch_bytes(const moe_ctx* ctx, long long rows, int cols);
+cudaError_t launch_rms_norm_backward(moe_ctx* ctx, const moe_rms_norm_grad_args& args, cudaStream_t stream);
+
+// Balance loss and its gradient.
+size_t balance_scratch_bytes(const moe_ctx* ctx, int sequences);
+cudaError_t launch_balance_loss(moe_ctx* ctx, const moe_balance_args& args, int32_t* counts, int32_t* tokens, float* mean,
+                                float* loss, void* scratch, cudaStream_t stream);
+cudaError_t launch_balance_loss_backward(moe_ctx* ctx, const moe_balance_args& args, const int32_t* counts,
+                                         const int32_t* tokens, const float* d_loss, const float* add, float* d_logits,
+                                         cudaStream_t stream);
+
+// Low-rank adapters added to a projection's output.
+size_t adapter_scratch_bytes(const moe_ctx* ctx, long long rows, int K, int rank);
+moe_status launch_add_adapters(moe_ctx* ctx, const moe_adapter_args& args, cudaStream_t stream);
+
 cudaError_t prepare_expert_ffn(moe_ctx* ctx);  // one-time kernel attributes (dynamic shared memory size)
 
 }  // namespace moe
