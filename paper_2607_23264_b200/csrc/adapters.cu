@@ -5,56 +5,16 @@
 //          global memory: a lane's 16 bytes of a row are eight neighbouring k, and as x and a are permuted along k alike, no
 //          shuffle is needed.
 // expand : y += scale t b^T, a CTA per 16 rows and 256 columns, a column per thread: fp32 dot products over the rank.
-#include <cuda_bf16.h>
-
-#include "moe_internal.h"
+#include "adapters.cuh"
 
 namespace {
+
+using moe::AdapterParams;
 
 constexpr unsigned kFull = 0xFFFFFFFFu;
 constexpr int kRows = 16;                 // rows of a CTA
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxSplits = 16;
-
-struct AdapterParams {
-  const __nv_bfloat16* x;
-  const __nv_bfloat16* a;
-  const __nv_bfloat16* b;
-  const float* scale;
-  const int32_t* offsets;
-  const int32_t* adapter_of;
-  const __nv_bfloat16* y_in;
-  __nv_bfloat16* y_out;
-  float* t;                               // [splits][rows][rank]
-  int32_t* status;
-  long long rows;
-  int N, K, rank, adapters, segments, splits;
-};
-
-// The adapter of a row, -1 without one.
-__device__ __forceinline__ int adapter_of_row(const AdapterParams& p, long long row, bool report) {
-  if (row >= p.rows) return -1;
-  int seg = static_cast<int>(row);
-  if (p.offsets != nullptr) {
-    int lo = -1, hi = p.segments;                          // the last segment that begins at or before the row
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (__ldg(p.offsets + mid) <= row) lo = mid;
-      else hi = mid;
-    }
-    if (lo < 0 || row >= __ldg(p.offsets + lo + 1)) return -1;
-    seg = lo;
-  }
-  const int id = __ldg(p.adapter_of + seg);
-  if (id >= p.adapters) {
-    if (report) {
-      atomicCAS(&p.status[0], 0, MOE_ERR_BAD_ROUTING);
-      atomicCAS(&p.status[1], 0, seg);
-    }
-    return -1;
-  }
-  return id < 0 ? -1 : id;
-}
 
 __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                          uint32_t b1) {
@@ -73,7 +33,7 @@ adapter_shrink(const AdapterParams p) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
   const long long row0 = static_cast<long long>(blockIdx.x) * kRows;
   const int split = blockIdx.y;
-  if (threadIdx.x < kRows) s_id[threadIdx.x] = adapter_of_row(p, row0 + threadIdx.x, split == 0);
+  if (threadIdx.x < kRows) s_id[threadIdx.x] = moe::adapter_of_row(p, p.offsets, row0 + threadIdx.x, split == 0);
   __syncthreads();
   const int my_id = s_id[lane & 15];
   unsigned left = __ballot_sync(kFull, my_id >= 0) & 0xFFFFu;
@@ -137,7 +97,7 @@ adapter_expand(const AdapterParams p) {
   const int tid = threadIdx.x;
   const long long row0 = static_cast<long long>(blockIdx.x) * kRows;
   const int n = blockIdx.y * kThreads + tid;
-  if (tid < kRows) s_id[tid] = adapter_of_row(p, row0 + tid, false);
+  if (tid < kRows) s_id[tid] = moe::adapter_of_row(p, p.offsets, row0 + tid, false);
   __syncthreads();
   for (int i = tid; i < kRows * p.rank; i += kThreads) {
     const int r = i / p.rank, j = i - r * p.rank;
@@ -188,7 +148,8 @@ int splits_of(const moe_ctx* ctx, long long rows, int K) {
 namespace moe {
 
 size_t adapter_scratch_bytes(const moe_ctx* ctx, long long rows, int K, int rank) {
-  return static_cast<size_t>(splits_of(ctx, rows, K)) * static_cast<size_t>(rows) * rank * 4;
+  const int a = splits_of(ctx, rows, K), b = adapter_tile_splits(ctx, rows, K, rank);
+  return static_cast<size_t>(a > b ? a : b) * static_cast<size_t>(rows) * rank * 4;
 }
 
 moe_status launch_add_adapters(moe_ctx* ctx, const moe_adapter_args& a, cudaStream_t stream) {
@@ -209,6 +170,7 @@ moe_status launch_add_adapters(moe_ctx* ctx, const moe_adapter_args& a, cudaStre
   p.rank = a.rank;
   p.adapters = a.adapters;
   p.segments = a.segments;
+  if (a.segments > 0 && a.rows >= 128 && a.rows / a.segments >= 16) return launch_adapter_tiles(ctx, p, stream);
   p.splits = splits_of(ctx, a.rows, a.K);
   const unsigned blocks = static_cast<unsigned>((a.rows + kRows - 1) / kRows);
   const unsigned chunks = static_cast<unsigned>((a.N - 1) / kThreads + 1);
