@@ -32,7 +32,7 @@ constexpr int kAtomA = kTileRows * 128;   // 64 ranks of one term of t
 constexpr int kAtomB = kBN * 128;         // 64 ranks of b
 constexpr int kYStages = 3, kBStages = 3;
 constexpr int kCachedOffsets = 513;
-constexpr int kMaxSplits = 16;
+constexpr int kMaxSplits = 8;            // CTAs of a cluster
 
 struct alignas(16) TileIds {
   int id[kTileRows];                      // adapter of each row, -1 without one
@@ -43,7 +43,7 @@ struct alignas(16) TileIds {
   int32_t offsets[kCachedOffsets];
 };
 struct Barriers {
-  uint64_t full[kMaxStages], empty[kMaxStages], y_full[kYStages], y_empty[kYStages], acc_full[2], acc_empty[2];
+  uint64_t full[kMaxStages], empty[kMaxStages], y_full[kYStages], acc_full[2], acc_empty[2], t_full;
   uint32_t tmem;
   int abort_flag;
 };
@@ -108,127 +108,6 @@ __device__ __forceinline__ void finish(Barriers* bar, int warp) {
   }
 }
 
-__global__ void __launch_bounds__(kThreads)
-adapter_shrink_tiles(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_a, const AdapterParams p,
-                     int stages, int rank16) {
-  extern __shared__ unsigned char smem_raw[];
-  __shared__ TileIds ids;
-  __shared__ Barriers bar;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int tile = blockIdx.x / p.splits, split = blockIdx.x - tile * p.splits;
-  const long long row0 = static_cast<long long>(tile) * kTileRows;
-  const uint32_t ring = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
-  ptx::launch_dependents();
-  if (threadIdx.x == 0) {
-    ptx::prefetch_tensormap(&tm_x);
-    ptx::prefetch_tensormap(&tm_a);
-    for (int i = 0; i < stages; ++i) {
-      ptx::mbar_init(ptx::smem_u32(&bar.full[i]), 1);
-      ptx::mbar_init(ptx::smem_u32(&bar.empty[i]), 1);
-    }
-    ptx::mbar_init(ptx::smem_u32(&bar.acc_full[0]), 1);
-    ptx::mbar_init(ptx::smem_u32(&bar.acc_empty[0]), 4);
-    bar.abort_flag = 0;
-    ptx::fence_barrier_init();
-  }
-  if (warp == 1) {
-    ptx::tmem_alloc(ptx::smem_u32(&bar.tmem), kCols);
-    ptx::tmem_relinquish();
-    ptx::tc_fence_before_sync();
-  }
-  const int count = collect(p, row0, &ids, split == 0);    // (its barriers order the initialisation above as well)
-  ptx::tc_fence_after_sync();
-  const uint32_t tmem = bar.tmem;
-  volatile int* abort_flag = &bar.abort_flag;
-  const int blocks = (p.K + kBK - 1) / kBK;
-  const int kb0 = static_cast<int>(static_cast<long long>(blocks) * split / p.splits);
-  const int kb1 = static_cast<int>(static_cast<long long>(blocks) * (split + 1) / p.splits);
-  const int per_pass = kCols / rank16;                     // adapters
-
-  if (warp == 0) {
-    if (lane == 0) {
-      int stage = 0;
-      uint32_t phase = 1;
-      bool ok = true;
-      for (int s0 = 0; s0 < count && ok; s0 += per_pass) {
-        const int n = min(per_pass, count - s0);
-        for (int kb = kb0; kb < kb1; ++kb) {
-          if (!ptx::mbar_wait(ptx::smem_u32(&bar.empty[stage]), phase, abort_flag)) {
-            timed_out(p, 1);
-            ok = false;
-            break;
-          }
-          const uint32_t full = ptx::smem_u32(&bar.full[stage]), at = ring + stage * kStageBytes;
-          ptx::mbar_expect_tx(full, kXBytes + n * rank16 * 128);
-          ptx::tma_load_2d(at, &tm_x, full, kb * kBK, static_cast<int>(row0));
-          for (int i = 0; i < n; ++i)
-            ptx::tma_load_2d(at + kXBytes + i * rank16 * 128, &tm_a, full, kb * kBK, ids.list[s0 + i] * p.rank);
-          if (++stage == stages) { stage = 0; phase ^= 1u; }
-        }
-      }
-    }
-    __syncwarp();
-  } else if (warp == 1) {
-    if (lane == 0) {
-      int stage = 0;
-      uint32_t phase = 0, pass_phase = 1;
-      bool ok = true;
-      for (int s0 = 0; s0 < count && ok; s0 += per_pass) {
-        const int n = min(per_pass, count - s0);
-        const uint32_t idesc = ptx::idesc_bf16_f32(kTileRows, n * rank16);
-        ok = ptx::mbar_wait(ptx::smem_u32(&bar.acc_empty[0]), pass_phase, abort_flag);
-        pass_phase ^= 1u;
-        ptx::tc_fence_after_sync();
-        for (int kb = kb0; kb < kb1 && ok; ++kb) {
-          ok = ptx::mbar_wait(ptx::smem_u32(&bar.full[stage]), phase, abort_flag);
-          if (!ok) break;
-          ptx::tc_fence_after_sync();
-          const uint32_t at = ring + stage * kStageBytes;
-          const uint64_t a = ptx::smem_desc_sw128(at), b = ptx::smem_desc_sw128(at + kXBytes);
-#pragma unroll
-          for (int k = 0; k < kBK / 16; ++k) ptx::tc_mma_bf16(tmem, a + 2 * k, b + 2 * k, idesc, kb > kb0 || k > 0);
-          ptx::tc_commit(ptx::smem_u32(&bar.empty[stage]));
-          if (++stage == stages) { stage = 0; phase ^= 1u; }
-        }
-        if (ok) ptx::tc_commit(ptx::smem_u32(&bar.acc_full[0]));
-        else timed_out(p, 2);
-      }
-    }
-    __syncwarp();
-  } else {
-    const int quarter = warp & 3, r = quarter * 32 + lane, slot = ids.slot[r];
-    float* dst = p.t + (static_cast<size_t>(split) * p.rows + row0 + r) * p.rank;
-    const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
-    uint32_t phase = 0;
-    for (int s0 = 0; s0 < count; s0 += per_pass) {
-      const int n = min(per_pass, count - s0);
-      if (!__all_sync(kFull, ptx::mbar_wait(ptx::smem_u32(&bar.acc_full[0]), phase, abort_flag))) {
-        if (lane == 0) timed_out(p, 3);
-        break;
-      }
-      phase ^= 1u;
-      ptx::tc_fence_after_sync();
-      for (int i = 0; i < n; ++i) {
-        const bool mine = slot == s0 + i;
-        if (!__any_sync(kFull, mine)) continue;
-        for (int j = 0; j < p.rank; j += 8) {
-          uint32_t v[8];
-          ptx::tmem_ld_32x8(lanes + i * rank16 + j, v);
-          ptx::tmem_ld_wait();
-          if (mine) {
-            *reinterpret_cast<uint4*>(dst + j) = make_uint4(v[0], v[1], v[2], v[3]);
-            *reinterpret_cast<uint4*>(dst + j + 4) = make_uint4(v[4], v[5], v[6], v[7]);
-          }
-        }
-      }
-      ptx::tc_fence_before_sync();
-      __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&bar.acc_empty[0]));
-    }
-  }
-  finish(&bar, warp);
-}
-
 // Eight values as two terms of bf16: v - hi is exact, so hi + lo keeps 16 bits.
 __device__ __forceinline__ uint32_t pair(float a, float b) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
@@ -249,6 +128,164 @@ __device__ __forceinline__ void two_terms(const float (&v)[8], uint4& hi, uint4&
   lo = make_uint4(l[0], l[1], l[2], l[3]);
 }
 
+// Grid: a cluster of p.splits CTAs per tile.
+__global__ void __launch_bounds__(kThreads)
+adapter_shrink_tiles(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_a, const AdapterParams p,
+                     int stages, int rank16) {
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ TileIds ids;
+  __shared__ Barriers bar;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int tile = blockIdx.x / p.splits, split = blockIdx.x - tile * p.splits;
+  const long long row0 = static_cast<long long>(tile) * kTileRows;
+  unsigned char* base = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
+  const uint32_t ring = ptx::smem_u32(base);
+  const int blocks = (p.K + kBK - 1) / kBK;
+  const int kb0 = static_cast<int>(static_cast<long long>(blocks) * split / p.splits);
+  const int kb1 = static_cast<int>(static_cast<long long>(blocks) * (split + 1) / p.splits);
+  const int ahead = min(stages, kb1 - kb0);                // stages whose x is on its way before the adapters are known
+  ptx::launch_dependents();
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < stages; ++i) {
+      ptx::mbar_init(ptx::smem_u32(&bar.full[i]), 2);      // x and the factors report on their own
+      ptx::mbar_init(ptx::smem_u32(&bar.empty[i]), 1);
+    }
+    ptx::mbar_init(ptx::smem_u32(&bar.acc_full[0]), 1);
+    bar.abort_flag = 0;
+    ptx::fence_barrier_init();
+    for (int i = 0; i < ahead; ++i) {
+      ptx::mbar_expect_tx(ptx::smem_u32(&bar.full[i]), kXBytes);
+      ptx::tma_load_2d(ring + i * kStageBytes, &tm_x, ptx::smem_u32(&bar.full[i]), (kb0 + i) * kBK, static_cast<int>(row0));
+    }
+  }
+  if (warp == 1) {
+    ptx::tmem_alloc(ptx::smem_u32(&bar.tmem), kCols);
+    ptx::tmem_relinquish();
+    ptx::tc_fence_before_sync();
+  }
+  const int count = collect(p, row0, &ids, split == 0);    // (its barriers order the initialisation above as well)
+  ptx::tc_fence_after_sync();
+  const uint32_t tmem = bar.tmem;
+  volatile int* abort_flag = &bar.abort_flag;
+  const int per_round = kCols / rank16;                    // adapters
+  const int pitch = p.rank + 4;                            // floats of a row of the exchanged sums: an odd number of 16 bytes
+
+  int stage = 0;
+  uint32_t phase = warp == 0 ? 1 : 0;
+  for (int s0 = 0, round = 0; s0 < count; s0 += per_round, ++round) {
+    const int n = min(per_round, count - s0);
+    if (warp == 0) {
+      if (lane == 0) {
+        for (int kb = kb0; kb < kb1; ++kb) {
+          if (!ptx::mbar_wait(ptx::smem_u32(&bar.empty[stage]), phase, abort_flag)) {
+            timed_out(p, 1);
+            break;
+          }
+          const uint32_t full = ptx::smem_u32(&bar.full[stage]), at = ring + stage * kStageBytes;
+          if (round > 0 || kb >= kb0 + ahead) {
+            ptx::mbar_expect_tx(full, kXBytes);
+            ptx::tma_load_2d(at, &tm_x, full, kb * kBK, static_cast<int>(row0));
+          }
+          ptx::mbar_expect_tx(full, n * rank16 * 128);
+          for (int i = 0; i < n; ++i)
+            ptx::tma_load_2d(at + kXBytes + i * rank16 * 128, &tm_a, full, kb * kBK, ids.list[s0 + i] * p.rank);
+          if (++stage == stages) { stage = 0; phase ^= 1u; }
+        }
+      }
+      __syncwarp();
+    } else if (warp == 1) {
+      if (lane == 0) {
+        const uint32_t idesc = ptx::idesc_bf16_f32(kTileRows, n * rank16);
+        bool ok = true;
+        for (int kb = kb0; kb < kb1; ++kb) {
+          ok = ptx::mbar_wait(ptx::smem_u32(&bar.full[stage]), phase, abort_flag);
+          if (!ok) break;
+          ptx::tc_fence_after_sync();
+          const uint32_t at = ring + stage * kStageBytes;
+          const uint64_t a = ptx::smem_desc_sw128(at), b = ptx::smem_desc_sw128(at + kXBytes);
+#pragma unroll
+          for (int k = 0; k < kBK / 16; ++k) ptx::tc_mma_bf16(tmem, a + 2 * k, b + 2 * k, idesc, kb > kb0 || k > 0);
+          ptx::tc_commit(ptx::smem_u32(&bar.empty[stage]));
+          if (++stage == stages) { stage = 0; phase ^= 1u; }
+        }
+        if (ok) ptx::tc_commit(ptx::smem_u32(&bar.acc_full[0]));
+        else timed_out(p, 2);
+      }
+      __syncwarp();
+    } else {
+      // each row's sums into the ring's place: every stage has been consumed when the accumulator is complete
+      const int quarter = warp & 3, r = quarter * 32 + lane, slot = ids.slot[r];
+      const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
+      if (!__all_sync(kFull, ptx::mbar_wait(ptx::smem_u32(&bar.acc_full[0]), round & 1, abort_flag))) {
+        if (lane == 0) timed_out(p, 3);
+      } else {
+        ptx::tc_fence_after_sync();
+        float* dst = reinterpret_cast<float*>(base) + r * pitch;
+        for (int i = 0; i < n; ++i) {
+          const bool mine = slot == s0 + i;
+          if (!__any_sync(kFull, mine)) continue;
+          for (int j = 0; j < p.rank; j += 8) {
+            uint32_t v[8];
+            ptx::tmem_ld_32x8(lanes + i * rank16 + j, v);
+            ptx::tmem_ld_wait();
+            if (mine) {
+              *reinterpret_cast<uint4*>(dst + j) = make_uint4(v[0], v[1], v[2], v[3]);
+              *reinterpret_cast<uint4*>(dst + j + 4) = make_uint4(v[4], v[5], v[6], v[7]);
+            }
+          }
+        }
+        ptx::tc_fence_before_sync();
+      }
+    }
+    // the cluster's sums over its parts of K, a share of the rows per CTA; two terms of bf16
+    ptx::cluster_sync();
+    ptx::tc_fence_after_sync();
+    const int r0 = kTileRows * split / p.splits, r1 = kTileRows * (split + 1) / p.splits, chunks = p.rank / 8;
+    for (int i = threadIdx.x; i < (r1 - r0) * chunks; i += kThreads) {
+      const int r = r0 + i / chunks, j = 8 * (i % chunks), slot = ids.slot[r];
+      if (slot < s0 || slot >= s0 + n) continue;
+      const uint32_t at = ring + (r * pitch + j) * 4;
+      float4 a[kMaxSplits], b[kMaxSplits];
+#pragma unroll
+      for (int s = 0; s < kMaxSplits; ++s) {
+        a[s] = b[s] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (s < p.splits) {
+          const uint32_t from = ptx::map_to_cta(at, s);
+          a[s] = ptx::ld_cluster_f4(from);
+          b[s] = ptx::ld_cluster_f4(from + 16);
+        }
+      }
+      float v[8] = {a[0].x, a[0].y, a[0].z, a[0].w, b[0].x, b[0].y, b[0].z, b[0].w};
+#pragma unroll
+      for (int s = 1; s < kMaxSplits; ++s) {
+        if (s < p.splits) {
+          v[0] += a[s].x; v[1] += a[s].y; v[2] += a[s].z; v[3] += a[s].w;
+          v[4] += b[s].x; v[5] += b[s].y; v[6] += b[s].z; v[7] += b[s].w;
+        }
+      }
+      if (p.scale != nullptr) {
+        const float f = __ldg(p.scale + ids.id[r]);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] *= f;
+      }
+      uint4 hi, lo;
+      two_terms(v, hi, lo);
+      __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(p.t) + (row0 + r) * p.rank + j;
+      *reinterpret_cast<uint4*>(to) = hi;
+      *reinterpret_cast<uint4*>(to + static_cast<size_t>(p.rows) * p.rank) = lo;
+    }
+    ptx::fence_proxy_async_smem();                         // the sums' place becomes the ring again
+    ptx::cluster_sync();
+  }
+  if (count == 0 && threadIdx.x == 0) {                    // nothing asks for the x on its way: it lands first
+    for (int i = 0; i < ahead; ++i) {
+      ptx::mbar_arrive(ptx::smem_u32(&bar.full[i]));
+      ptx::mbar_wait(ptx::smem_u32(&bar.full[i]), 0, abort_flag);
+    }
+  }
+  finish(&bar, warp);
+}
+
 // The four epilogue warps meet; whether any of them has given up.
 __device__ __forceinline__ bool epilogue_meets(bool gave_up) {
   uint32_t any;
@@ -266,8 +303,9 @@ __device__ __forceinline__ bool epilogue_meets(bool gave_up) {
 }
 
 __global__ void __launch_bounds__(kThreads)
-adapter_expand_tiles(const __grid_constant__ CUtensorMap tm_b, const __grid_constant__ CUtensorMap tm_in,
-                     const __grid_constant__ CUtensorMap tm_out, const AdapterParams p, int groups) {
+adapter_expand_tiles(const __grid_constant__ CUtensorMap tm_t, const __grid_constant__ CUtensorMap tm_b,
+                     const __grid_constant__ CUtensorMap tm_in, const __grid_constant__ CUtensorMap tm_out,
+                     const AdapterParams p, int groups) {
   extern __shared__ unsigned char smem_raw[];
   __shared__ TileIds ids;
   __shared__ Barriers bar;
@@ -278,24 +316,27 @@ adapter_expand_tiles(const __grid_constant__ CUtensorMap tm_b, const __grid_cons
   unsigned char* base = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
   unsigned char* ybase = base + 2 * atoms * kAtomA;        // A: the atoms of the first terms, then of the second
   const uint32_t a_at = ptx::smem_u32(base), y_at = ptx::smem_u32(ybase), b_at = y_at + kYStages * kYBytes;
+  const int tiles = (p.N - 1) / kBN + 1;
+  const int n0 = static_cast<int>(static_cast<long long>(tiles) * group / groups);
+  const int n1 = static_cast<int>(static_cast<long long>(tiles) * (group + 1) / groups);
+  const int ahead = min(kYStages, n1 - n0);                // tiles of y on their way before the adapters are known
   if (threadIdx.x == 0) {
-    ptx::prefetch_tensormap(&tm_b);
-    ptx::prefetch_tensormap(&tm_in);
-    ptx::prefetch_tensormap(&tm_out);
     for (int i = 0; i < kBStages; ++i) {
       ptx::mbar_init(ptx::smem_u32(&bar.full[i]), 1);
       ptx::mbar_init(ptx::smem_u32(&bar.empty[i]), 1);
     }
-    for (int i = 0; i < kYStages; ++i) {
-      ptx::mbar_init(ptx::smem_u32(&bar.y_full[i]), 1);
-      ptx::mbar_init(ptx::smem_u32(&bar.y_empty[i]), 1);
-    }
+    for (int i = 0; i < kYStages; ++i) ptx::mbar_init(ptx::smem_u32(&bar.y_full[i]), 1);
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(ptx::smem_u32(&bar.acc_full[i]), 1);
       ptx::mbar_init(ptx::smem_u32(&bar.acc_empty[i]), 4);
     }
+    ptx::mbar_init(ptx::smem_u32(&bar.t_full), 1);
     bar.abort_flag = 0;
     ptx::fence_barrier_init();
+    for (int i = 0; i < ahead; ++i) {
+      ptx::mbar_expect_tx(ptx::smem_u32(&bar.y_full[i]), kYBytes);
+      ptx::tma_load_2d(y_at + i * kYBytes, &tm_in, ptx::smem_u32(&bar.y_full[i]), (n0 + i) * kBN, static_cast<int>(row0));
+    }
   }
   if (warp == 1) {
     ptx::tmem_alloc(ptx::smem_u32(&bar.tmem), kCols);
@@ -306,24 +347,14 @@ adapter_expand_tiles(const __grid_constant__ CUtensorMap tm_b, const __grid_cons
   ptx::tc_fence_after_sync();
   const uint32_t tmem = bar.tmem;
   volatile int* abort_flag = &bar.abort_flag;
-  const int tiles = (p.N - 1) / kBN + 1;
-  int n0 = static_cast<int>(static_cast<long long>(tiles) * group / groups);
-  const int n1 = static_cast<int>(static_cast<long long>(tiles) * (group + 1) / groups);
-  if (count == 0 && p.y_in == p.y_out) n0 = n1;            // nothing to add and nothing to copy
 
   if (warp == 0) {
     if (lane == 0) {
-      int ys = 0, bs = 0;
-      uint32_t y_phase = 1, b_phase = 1;
+      int bs = 0;
+      uint32_t b_phase = 1;
       bool ok = true;
       for (int i = n0; i < n1 && ok; ++i) {
-        ok = ptx::mbar_wait(ptx::smem_u32(&bar.y_empty[ys]), y_phase, abort_flag);
-        if (!ok) break;
-        const uint32_t y_full = ptx::smem_u32(&bar.y_full[ys]);
-        ptx::mbar_expect_tx(y_full, kYBytes);
-        ptx::tma_load_2d(y_at + ys * kYBytes, &tm_in, y_full, i * kBN, static_cast<int>(row0));
-        if (++ys == kYStages) { ys = 0; y_phase ^= 1u; }
-        for (int s = 0; s < count && ok; ++s) {
+        for (int s = 0; s < count; ++s) {
           ok = ptx::mbar_wait(ptx::smem_u32(&bar.empty[bs]), b_phase, abort_flag);
           if (!ok) break;
           const uint32_t full = ptx::smem_u32(&bar.full[bs]);
@@ -336,118 +367,99 @@ adapter_expand_tiles(const __grid_constant__ CUtensorMap tm_b, const __grid_cons
       if (!ok) timed_out(p, 4);
     }
     __syncwarp();
-  } else {
-    // t, summed over the parts of K and scaled, as the A operand; eight ranks a step
-    ptx::wait_for_previous_kernel();
-    const int chunks = (p.rank + 15) / 16 * 2;             // 16-byte pieces of a row: whole steps of the product
-    const int work = count > 0 && n0 < n1 ? kTileRows * chunks : 0;
-    for (int i = threadIdx.x - 32; i < work; i += kThreads - 32) {
-      const int r = i / chunks, j = i - r * chunks, id = ids.id[r];
-      float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      if (id >= 0 && 8 * j < p.rank) {
-        const float* src = p.t + static_cast<size_t>(row0 + r) * p.rank + 8 * j;
-        const size_t pitch = static_cast<size_t>(p.rows) * p.rank;
-        for (int s = 0; s < p.splits; ++s) {
-          const float4 a = __ldcg(reinterpret_cast<const float4*>(src + s * pitch));
-          const float4 b = __ldcg(reinterpret_cast<const float4*>(src + s * pitch) + 1);
-          v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
-          v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
-        }
-        if (p.scale != nullptr) {
-          const float f = __ldg(p.scale + id);
-#pragma unroll
-          for (int q = 0; q < 8; ++q) v[q] *= f;
-        }
-      }
-      uint4 hi, lo;
-      two_terms(v, hi, lo);
-      unsigned char* at = base + (j >> 3) * kAtomA + r * 128 + (((j & 7) ^ (r & 7)) << 4);
-      *reinterpret_cast<uint4*>(at) = hi;
-      *reinterpret_cast<uint4*>(at + atoms * kAtomA) = lo;
-    }
-    ptx::fence_proxy_async_smem();
-    asm volatile("bar.sync 1, %0;" ::"r"(kThreads - 32) : "memory");
-
-    if (warp == 1) {
-      if (lane == 0) {
-        const uint32_t idesc = ptx::idesc_bf16_f32(kTileRows, kBN);
-        const int steps = (p.rank + 15) / 16;
-        int bs = 0, acc = 0;
-        uint32_t b_phase = 0, acc_phase = 1;
-        bool ok = true;
-        const int units = (n1 - n0) * count;
-        for (int u = 0; u < units && ok; ++u) {
-          ok = ptx::mbar_wait(ptx::smem_u32(&bar.full[bs]), b_phase, abort_flag) &&
-               ptx::mbar_wait(ptx::smem_u32(&bar.acc_empty[acc]), acc_phase, abort_flag);
-          if (!ok) break;
-          ptx::tc_fence_after_sync();
-          for (int term = 0; term < 2; ++term) {
-            for (int k = 0; k < steps; ++k) {
-              const uint64_t a = ptx::smem_desc_sw128(a_at + (term * atoms + (k >> 2)) * kAtomA) + 2 * (k & 3);
-              const uint64_t b = ptx::smem_desc_sw128(b_at + (bs * atoms + (k >> 2)) * kAtomB) + 2 * (k & 3);
-              ptx::tc_mma_bf16(tmem + acc * kBN, a, b, idesc, term > 0 || k > 0);
-            }
+  } else if (warp == 1) {
+    if (lane == 0 && count > 0) {
+      ptx::wait_for_previous_kernel();
+      ptx::mbar_expect_tx(ptx::smem_u32(&bar.t_full), 2 * atoms * kAtomA);
+      for (int term = 0; term < 2; ++term)
+        for (int k = 0; k < atoms; ++k)
+          ptx::tma_load_2d(a_at + (term * atoms + k) * kAtomA, &tm_t, ptx::smem_u32(&bar.t_full), k * 64,
+                           static_cast<int>(term * p.rows + row0));
+      const uint32_t idesc = ptx::idesc_bf16_f32(kTileRows, kBN);
+      const int steps = (p.rank + 15) / 16;
+      int bs = 0, acc = 0;
+      uint32_t b_phase = 0, acc_phase = 1;
+      bool ok = ptx::mbar_wait(ptx::smem_u32(&bar.t_full), 0, abort_flag);
+      const int units = (n1 - n0) * count;
+      for (int u = 0; u < units && ok; ++u) {
+        ok = ptx::mbar_wait(ptx::smem_u32(&bar.full[bs]), b_phase, abort_flag) &&
+             ptx::mbar_wait(ptx::smem_u32(&bar.acc_empty[acc]), acc_phase, abort_flag);
+        if (!ok) break;
+        ptx::tc_fence_after_sync();
+        for (int term = 0; term < 2; ++term) {
+          for (int k = 0; k < steps; ++k) {
+            const uint64_t a = ptx::smem_desc_sw128(a_at + (term * atoms + (k >> 2)) * kAtomA) + 2 * (k & 3);
+            const uint64_t b = ptx::smem_desc_sw128(b_at + (bs * atoms + (k >> 2)) * kAtomB) + 2 * (k & 3);
+            ptx::tc_mma_bf16(tmem + acc * kBN, a, b, idesc, term > 0 || k > 0);
           }
-          ptx::tc_commit(ptx::smem_u32(&bar.empty[bs]));
-          ptx::tc_commit(ptx::smem_u32(&bar.acc_full[acc]));
-          if (++bs == kBStages) { bs = 0; b_phase ^= 1u; }
-          if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
         }
-        if (!ok) timed_out(p, 5);
+        ptx::tc_commit(ptx::smem_u32(&bar.empty[bs]));
+        ptx::tc_commit(ptx::smem_u32(&bar.acc_full[acc]));
+        if (++bs == kBStages) { bs = 0; b_phase ^= 1u; }
+        if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
       }
-      __syncwarp();
-    } else {
-      const int quarter = warp & 3, r = quarter * 32 + lane, slot = ids.slot[r];
-      const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
-      int ys = 0, acc = 0;
-      uint32_t y_phase = 0, acc_phase = 0;
-      bool ok = true;
-      for (int i = n0; i < n1; ++i) {
-        ok = __all_sync(kFull, ptx::mbar_wait(ptx::smem_u32(&bar.y_full[ys]), y_phase, abort_flag));
-        unsigned char* row = ybase + ys * kYBytes + r * 128;
-        for (int s = 0; s < count && ok; ++s) {
-          ok = __all_sync(kFull, ptx::mbar_wait(ptx::smem_u32(&bar.acc_full[acc]), acc_phase, abort_flag));
-          const bool mine = slot == s;
-          if (ok && __any_sync(kFull, mine)) {
-            ptx::tc_fence_after_sync();
+      if (!ok) timed_out(p, 5);
+    }
+    __syncwarp();
+  } else {
+    ptx::wait_for_previous_kernel();
+    const int quarter = warp & 3, r = quarter * 32 + lane, slot = ids.slot[r];
+    const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
+    int ys = 0, acc = 0;
+    uint32_t y_phase = 0, acc_phase = 0;
+    bool ok = true;
+    const bool idle = count == 0 && p.y_in == p.y_out;     // nothing to add and nothing to copy: what was asked for lands
+    for (int i = 0; idle && i < ahead; ++i) ptx::mbar_wait(ptx::smem_u32(&bar.y_full[i]), 0, abort_flag);
+    for (int i = n0; i < n1 && !idle; ++i) {
+      ok = __all_sync(kFull, ptx::mbar_wait(ptx::smem_u32(&bar.y_full[ys]), y_phase, abort_flag));
+      unsigned char* row = ybase + ys * kYBytes + r * 128;
+      for (int s = 0; s < count && ok; ++s) {
+        ok = __all_sync(kFull, ptx::mbar_wait(ptx::smem_u32(&bar.acc_full[acc]), acc_phase, abort_flag));
+        const bool mine = slot == s;
+        if (ok && __any_sync(kFull, mine)) {
+          ptx::tc_fence_after_sync();
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              uint32_t v[32];
-              ptx::tmem_ld_32x32(lanes + acc * kBN + half * 32, v);
-              ptx::tmem_ld_wait();
-              if (mine) {
+          for (int half = 0; half < 2; ++half) {
+            uint32_t v[32];
+            ptx::tmem_ld_32x32(lanes + acc * kBN + half * 32, v);
+            ptx::tmem_ld_wait();
+            if (mine) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                  uint4* at = reinterpret_cast<uint4*>(row + (((half * 4 + c) ^ (r & 7)) << 4));
-                  uint4 y = *at;
-                  y.x = pair(low(y.x) + __uint_as_float(v[8 * c]), high(y.x) + __uint_as_float(v[8 * c + 1]));
-                  y.y = pair(low(y.y) + __uint_as_float(v[8 * c + 2]), high(y.y) + __uint_as_float(v[8 * c + 3]));
-                  y.z = pair(low(y.z) + __uint_as_float(v[8 * c + 4]), high(y.z) + __uint_as_float(v[8 * c + 5]));
-                  y.w = pair(low(y.w) + __uint_as_float(v[8 * c + 6]), high(y.w) + __uint_as_float(v[8 * c + 7]));
-                  *at = y;
-                }
+              for (int c = 0; c < 4; ++c) {
+                uint4* at = reinterpret_cast<uint4*>(row + (((half * 4 + c) ^ (r & 7)) << 4));
+                uint4 y = *at;
+                y.x = pair(low(y.x) + __uint_as_float(v[8 * c]), high(y.x) + __uint_as_float(v[8 * c + 1]));
+                y.y = pair(low(y.y) + __uint_as_float(v[8 * c + 2]), high(y.y) + __uint_as_float(v[8 * c + 3]));
+                y.z = pair(low(y.z) + __uint_as_float(v[8 * c + 4]), high(y.z) + __uint_as_float(v[8 * c + 5]));
+                y.w = pair(low(y.w) + __uint_as_float(v[8 * c + 6]), high(y.w) + __uint_as_float(v[8 * c + 7]));
+                *at = y;
               }
             }
-            ptx::tc_fence_before_sync();
           }
-          __syncwarp();
-          if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&bar.acc_empty[acc]));
-          if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+          ptx::tc_fence_before_sync();
         }
-        if (!ok && lane == 0) timed_out(p, 6);
-        ptx::fence_proxy_async_smem();
-        if (epilogue_meets(!ok)) break;                    // one verdict for the four warps
-        if (warp == 2 && lane == 0) {
-          ptx::tma_store_2d(&tm_out, y_at + ys * kYBytes, i * kBN, static_cast<int>(row0));
-          ptx::bulk_commit_group();
-          ptx::bulk_wait_group_read_but_one();
-          if (i > n0) ptx::mbar_arrive(ptx::smem_u32(&bar.y_empty[ys == 0 ? kYStages - 1 : ys - 1]));
-        }
-        if (++ys == kYStages) { ys = 0; y_phase ^= 1u; }
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&bar.acc_empty[acc]));
+        if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
       }
-      if (warp == 2 && lane == 0) ptx::bulk_wait_group_read_all();
-      __syncwarp();
+      if (!ok && lane == 0) timed_out(p, 6);
+      ptx::fence_proxy_async_smem();
+      if (epilogue_meets(!ok)) break;                    // one verdict for the four warps
+      if (warp == 2 && lane == 0) {
+        ptx::tma_store_2d(&tm_out, y_at + ys * kYBytes, i * kBN, static_cast<int>(row0));
+        ptx::bulk_commit_group();
+        if (i > n0 && i - 1 + ahead < n1) {                // the tile before this has left: a later one takes its place
+          const int free = ys == 0 ? kYStages - 1 : ys - 1;
+          const uint32_t y_full = ptx::smem_u32(&bar.y_full[free]);
+          ptx::bulk_wait_group_read_but_one();
+          ptx::mbar_expect_tx(y_full, kYBytes);
+          ptx::tma_load_2d(y_at + free * kYBytes, &tm_in, y_full, (i - 1 + ahead) * kBN, static_cast<int>(row0));
+        }
+      }
+      if (++ys == kYStages) { ys = 0; y_phase ^= 1u; }
     }
+    if (warp == 2 && lane == 0) ptx::bulk_wait_group_read_all();
+    __syncwarp();
   }
   finish(&bar, warp);
 }
@@ -468,49 +480,57 @@ int expand_smem(int rank) {
   return 1024 + 2 * atoms * kAtomA + kYStages * kYBytes + kBStages * atoms * kAtomB;
 }
 
-}  // namespace
-
-namespace moe {
-
-int adapter_tile_splits(const moe_ctx* ctx, long long rows, int K, int) {
+// Parts of K: as many as two CTAs per SM take, at most a portable cluster.
+int splits_of(const moe_ctx* ctx, long long rows, int K) {
   const long long tiles = (rows + kTileRows - 1) / kTileRows;
   const int blocks = (K + kBK - 1) / kBK;
-  long long s = tiles > 0 ? 2LL * ctx->num_sms / tiles : 1;
+  long long s = 2LL * ctx->num_sms / tiles;
   if (s > kMaxSplits) s = kMaxSplits;
   if (s > blocks) s = blocks;
   return s < 1 ? 1 : static_cast<int>(s);
 }
 
+}  // namespace
+
+namespace moe {
+
+size_t adapter_tile_scratch_bytes(long long rows, int rank) { return static_cast<size_t>(rows) * rank * 4; }
+
 moe_status launch_adapter_tiles(moe_ctx* ctx, AdapterParams p, cudaStream_t stream) {
   const int rank16 = (p.rank + 15) / 16 * 16;
-  CUtensorMap tm_x, tm_a, tm_b, tm_in, tm_out;
+  CUtensorMap tm_x, tm_a, tm_t, tm_b, tm_in, tm_out;
   if (!encode(ctx, &tm_x, p.x, p.rows, p.K, kTileRows) ||
       !encode(ctx, &tm_a, p.a, static_cast<uint64_t>(p.adapters) * p.rank, p.K, rank16) ||
+      !encode(ctx, &tm_t, p.t, 2 * static_cast<uint64_t>(p.rows), p.rank, kTileRows) ||
       !encode(ctx, &tm_b, p.b, static_cast<uint64_t>(p.adapters) * p.N, p.rank, kBN) ||
       !encode(ctx, &tm_in, p.y_in, p.rows, p.N, kTileRows) || !encode(ctx, &tm_out, p.y_out, p.rows, p.N, kTileRows))
     return MOE_ERR_CUDA;
-  p.splits = adapter_tile_splits(ctx, p.rows, p.K, p.rank);
+  p.splits = splits_of(ctx, p.rows, p.K);
   const long long tiles = (p.rows + kTileRows - 1) / kTileRows;
   const int stages = 3;
-  adapter_shrink_tiles<<<static_cast<unsigned>(tiles * p.splits), kThreads, shrink_smem(stages), stream>>>(tm_x, tm_a, p, stages,
-                                                                                                  rank16);
-  if (cudaGetLastError() != cudaSuccess) return MOE_ERR_CUDA;
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr{};
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = stream;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  cfg.gridDim = dim3(static_cast<unsigned>(tiles * p.splits));
+  cfg.dynamicSmemBytes = shrink_smem(stages);
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = static_cast<unsigned>(p.splits);
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  if (cudaLaunchKernelEx(&cfg, adapter_shrink_tiles, tm_x, tm_a, p, stages, rank16) != cudaSuccess) return MOE_ERR_CUDA;
   const int n_tiles = (p.N - 1) / kBN + 1;
   long long groups = 2LL * ctx->num_sms / tiles;
   if (groups > n_tiles) groups = n_tiles;
   if (groups < 1) groups = 1;
-  cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(static_cast<unsigned>(tiles * groups));
-  cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = expand_smem(p.rank);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr{};
+  attr = cudaLaunchAttribute{};
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
   ctx->last_launches += 2;
-  return cudaLaunchKernelEx(&cfg, adapter_expand_tiles, tm_b, tm_in, tm_out, p, static_cast<int>(groups)) == cudaSuccess
+  return cudaLaunchKernelEx(&cfg, adapter_expand_tiles, tm_t, tm_b, tm_in, tm_out, p, static_cast<int>(groups)) == cudaSuccess
              ? MOE_OK
              : MOE_ERR_CUDA;
 }

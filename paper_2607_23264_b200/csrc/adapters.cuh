@@ -47,7 +47,7 @@ __device__ __forceinline__ int adapter_of_row(const AdapterParams& p, const int3
 }
 
 // Long segments: tiles of 128 rows on the tensor cores.
-int adapter_tile_splits(const moe_ctx* ctx, long long rows, int K, int rank);
+size_t adapter_tile_scratch_bytes(long long rows, int rank);
 moe_status launch_adapter_tiles(moe_ctx* ctx, AdapterParams p, cudaStream_t stream);
 
 }  // namespace moe
