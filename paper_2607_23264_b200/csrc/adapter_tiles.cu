@@ -1,18 +1,20 @@
-// Adapters over long segments: tiles of 128 rows on the tensor cores.
+// Adapters over long segments: tiles of up to 128 rows of one segment on the tensor cores, both products in one launch.
 //
-// A tile's rows may belong to several adapters.  Neither product masks anything: an adapter's columns of the accumulator are
-// computed for all 128 rows, and a row takes those of its own adapter.
+// A cluster of up to eight CTAs takes a tile.  First t = x a^T: each CTA has a part of K, x and a come through a TMA ring of 64-deep
+// stages, and the cluster adds its parts in order through distributed shared memory, scales them and cuts them into two bf16
+// terms (16 bits: the error of one term would be that of the output's rounding).  Then y += t b^T: each CTA has a range of
+// columns, the terms of t stay in shared memory as the A operand, y and b come through TMA rings in tiles of 64 columns, the sum
+// is formed in y's place in shared memory and leaves by TMA.
 //
-// adapter_shrink_tiles : t = x a^T, a CTA per tile and part of K.  x and the factors of the tile's adapters (up to 128 columns of the
-//                        accumulator in a pass) come through a TMA ring of 64-deep stages; warp 0 loads, warp 1 issues the
-//                        products, warps 2-5 write each row's part of t to the scratch, one fp32 copy per part of K.
-// adapter_expand_tiles : y += t b^T, a CTA per tile and range of columns.  t is summed over the parts of K, scaled, and cut into two bf16
-//                        terms (16 bits; the error of one term would be that of the output's rounding) that stay in shared
-//                        memory as the A operand; y and b come through TMA rings in tiles of 64 columns, the sum is formed in
-//                        y's place in shared memory and leaves by TMA.  Rows without an adapter pass through untouched.  Starts
-//                        while the first kernel runs (programmatic launch): its loads do not depend on t.
+// A tile begins where its segment does or 128 rows later: a TMA box may start at any row.  What a box brings of the rows behind
+// the segment's last is computed and not used; tiles of up to 16 rows use boxes of 16.  Segment s has the clusters from
+// offsets[s] / 128 + s on, so no list of tiles is built; the rows behind the last segment are one more segment without an adapter.
+//
+// Warp 0 loads, warp 1 issues the products, warps 2-5 move between accumulator and shared memory; y is on its way while the
+// parts of t are added.
 #include "adapters.cuh"
 #include "ptx_sm100.cuh"
+#include "warp_search.cuh"
 
 namespace {
 
@@ -20,92 +22,49 @@ using moe::AdapterParams;
 
 constexpr unsigned kFull = 0xFFFFFFFFu;
 constexpr int kTileRows = 128;
-constexpr int kThreads = 192;             // TMA, MMA and four epilogue warps
+constexpr int kShortRows = 16;            // tiles of up to so many rows load that many
+constexpr int kThreads = 192;
 constexpr int kBK = 64;                   // values of K in a stage: 128 bytes of bf16
-constexpr int kCols = 128;                // accumulator columns of a shrink pass, and both accumulators of the expansion
+constexpr int kCols = 128;                // accumulator columns: t's, later two tiles of y
 constexpr int kXBytes = kTileRows * 128;
-constexpr int kStageBytes = kXBytes + kCols * 128;
 constexpr int kMaxStages = 6;
-constexpr int kBN = 64;                   // columns of an expand tile
+constexpr int kBN = 64;                   // columns of a tile of y
 constexpr int kYBytes = kTileRows * 128;
 constexpr int kAtomA = kTileRows * 128;   // 64 ranks of one term of t
 constexpr int kAtomB = kBN * 128;         // 64 ranks of b
 constexpr int kYStages = 3, kBStages = 3;
-constexpr int kCachedOffsets = 513;
-constexpr int kMaxSplits = 8;            // CTAs of a cluster
+constexpr int kMaxCluster = 8;
 
-struct alignas(16) TileIds {
-  int id[kTileRows];                      // adapter of each row, -1 without one
-  int slot[kTileRows];                    // its place in `list`
-  int list[kTileRows];                    // the tile's adapters in order of their first row
-  int place[kTileRows];
-  int warp_count[4];
-  int32_t offsets[kCachedOffsets];
-};
 struct Barriers {
-  uint64_t full[kMaxStages], empty[kMaxStages], y_full[kYStages], acc_full[2], acc_empty[2], t_full;
+  uint64_t full[kMaxStages], empty[kMaxStages], y_full[kYStages], b_full[kBStages], b_empty[kBStages], acc_full[2], acc_empty[2],
+      sums_full, t_full;
   uint32_t tmem;
   int abort_flag;
+};
+
+// Shared memory of a CTA, from a 1024-byte boundary on: in the second phase the terms of t, y's ring and b's ring; in the
+// first the ring of x and a from the start, and the exchanged sums at the end.
+struct Layout {
+  int atoms, rank16, stage_bytes, stages, y_at, b_at, sums_at, bytes;
+  __host__ __device__ explicit Layout(int rank) {
+    atoms = (rank + 63) / 64;
+    rank16 = (rank + 15) / 16 * 16;
+    y_at = 2 * atoms * kAtomA;
+    b_at = y_at + kYStages * kYBytes;
+    bytes = b_at + kBStages * atoms * kAtomB;              // 104 KiB: two CTAs on an SM; 160 above 64 ranks
+    stage_bytes = kXBytes + rank16 * 128;
+    stages = bytes / stage_bytes < kMaxStages ? bytes / stage_bytes : kMaxStages;
+    sums_at = bytes - kTileRows * (rank + 4) * 4;
+  }
+};
+
+struct Maps {
+  CUtensorMap x, x_short, a, t, b, in, in_short, out;
 };
 
 __device__ __forceinline__ void timed_out(const AdapterParams& p, int where) {
   atomicCAS(&p.status[0], 0, MOE_ERR_TIMEOUT);
   atomicCAS(&p.status[1], 0, 200 + where);
-}
-
-// Fills `s` for the tile at row0; by the whole CTA.  Returns the number of adapters.
-__device__ int collect(const AdapterParams& p, long long row0, TileIds* s, bool report) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int32_t* offsets = p.offsets;
-  if (offsets != nullptr && p.segments < kCachedOffsets) {
-    for (int i = tid; i <= p.segments; i += kThreads) s->offsets[i] = __ldg(offsets + i);
-    offsets = s->offsets;
-  }
-  __syncthreads();
-  if (tid < kTileRows) s->id[tid] = moe::adapter_of_row(p, offsets, row0 + tid, report);
-  __syncthreads();
-  int id = -1, first = tid;
-  unsigned leaders = 0;
-  if (tid < kTileRows) {
-    id = s->id[tid];
-    first = warp * 32 + __ffs(__match_any_sync(kFull, id)) - 1;
-    const int4* rows = reinterpret_cast<const int4*>(s->id);
-    for (int r = 8 * warp - 1; r >= 0; --r) {              // earlier warps' rows, the lowest last
-      const int4 v = rows[r];
-      if (v.w == id) first = 4 * r + 3;
-      if (v.z == id) first = 4 * r + 2;
-      if (v.y == id) first = 4 * r + 1;
-      if (v.x == id) first = 4 * r;
-    }
-    leaders = __ballot_sync(kFull, id >= 0 && first == tid);
-    if (lane == 0) s->warp_count[warp] = __popc(leaders);
-  }
-  __syncthreads();
-  int total = 0;
-  if (tid < kTileRows && id >= 0 && first == tid) {
-    int at = __popc(leaders & ((1u << lane) - 1));
-    for (int w = 0; w < warp; ++w) at += s->warp_count[w];
-    s->list[at] = id;
-    s->place[tid] = at;
-  }
-  for (int w = 0; w < 4; ++w) total += s->warp_count[w];
-  __syncthreads();
-  if (tid < kTileRows) s->slot[tid] = id >= 0 ? s->place[first] : -1;
-  __syncthreads();
-  return total;
-}
-
-// Frees what the CTA holds; after a wait that gave up, copies in flight get time to land first.
-__device__ __forceinline__ void finish(Barriers* bar, int warp) {
-  __syncthreads();
-  if (bar->abort_flag) {
-    for (int i = 0; i < 2000; ++i) __nanosleep(1000);
-    __syncthreads();
-  }
-  if (warp == 1) {
-    ptx::tc_fence_after_sync();
-    ptx::tmem_dealloc(bar->tmem, kCols);
-  }
 }
 
 // Eight values as two terms of bf16: v - hi is exact, so hi + lo keeps 16 bits.
@@ -127,163 +86,9 @@ __device__ __forceinline__ void two_terms(const float (&v)[8], uint4& hi, uint4&
   hi = make_uint4(h[0], h[1], h[2], h[3]);
   lo = make_uint4(l[0], l[1], l[2], l[3]);
 }
-
-// Grid: a cluster of p.splits CTAs per tile.
-__global__ void __launch_bounds__(kThreads)
-adapter_shrink_tiles(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_a, const AdapterParams p,
-                     int stages, int rank16) {
-  extern __shared__ unsigned char smem_raw[];
-  __shared__ TileIds ids;
-  __shared__ Barriers bar;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int tile = blockIdx.x / p.splits, split = blockIdx.x - tile * p.splits;
-  const long long row0 = static_cast<long long>(tile) * kTileRows;
-  unsigned char* base = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
-  const uint32_t ring = ptx::smem_u32(base);
-  const int blocks = (p.K + kBK - 1) / kBK;
-  const int kb0 = static_cast<int>(static_cast<long long>(blocks) * split / p.splits);
-  const int kb1 = static_cast<int>(static_cast<long long>(blocks) * (split + 1) / p.splits);
-  const int ahead = min(stages, kb1 - kb0);                // stages whose x is on its way before the adapters are known
-  ptx::launch_dependents();
-  if (threadIdx.x == 0) {
-    for (int i = 0; i < stages; ++i) {
-      ptx::mbar_init(ptx::smem_u32(&bar.full[i]), 2);      // x and the factors report on their own
-      ptx::mbar_init(ptx::smem_u32(&bar.empty[i]), 1);
-    }
-    ptx::mbar_init(ptx::smem_u32(&bar.acc_full[0]), 1);
-    bar.abort_flag = 0;
-    ptx::fence_barrier_init();
-    for (int i = 0; i < ahead; ++i) {
-      ptx::mbar_expect_tx(ptx::smem_u32(&bar.full[i]), kXBytes);
-      ptx::tma_load_2d(ring + i * kStageBytes, &tm_x, ptx::smem_u32(&bar.full[i]), (kb0 + i) * kBK, static_cast<int>(row0));
-    }
-  }
-  if (warp == 1) {
-    ptx::tmem_alloc(ptx::smem_u32(&bar.tmem), kCols);
-    ptx::tmem_relinquish();
-    ptx::tc_fence_before_sync();
-  }
-  const int count = collect(p, row0, &ids, split == 0);    // (its barriers order the initialisation above as well)
-  ptx::tc_fence_after_sync();
-  const uint32_t tmem = bar.tmem;
-  volatile int* abort_flag = &bar.abort_flag;
-  const int per_round = kCols / rank16;                    // adapters
-  const int pitch = p.rank + 4;                            // floats of a row of the exchanged sums: an odd number of 16 bytes
-
-  int stage = 0;
-  uint32_t phase = warp == 0 ? 1 : 0;
-  for (int s0 = 0, round = 0; s0 < count; s0 += per_round, ++round) {
-    const int n = min(per_round, count - s0);
-    if (warp == 0) {
-      if (lane == 0) {
-        for (int kb = kb0; kb < kb1; ++kb) {
-          if (!ptx::mbar_wait(ptx::smem_u32(&bar.empty[stage]), phase, abort_flag)) {
-            timed_out(p, 1);
-            break;
-          }
-          const uint32_t full = ptx::smem_u32(&bar.full[stage]), at = ring + stage * kStageBytes;
-          if (round > 0 || kb >= kb0 + ahead) {
-            ptx::mbar_expect_tx(full, kXBytes);
-            ptx::tma_load_2d(at, &tm_x, full, kb * kBK, static_cast<int>(row0));
-          }
-          ptx::mbar_expect_tx(full, n * rank16 * 128);
-          for (int i = 0; i < n; ++i)
-            ptx::tma_load_2d(at + kXBytes + i * rank16 * 128, &tm_a, full, kb * kBK, ids.list[s0 + i] * p.rank);
-          if (++stage == stages) { stage = 0; phase ^= 1u; }
-        }
-      }
-      __syncwarp();
-    } else if (warp == 1) {
-      if (lane == 0) {
-        const uint32_t idesc = ptx::idesc_bf16_f32(kTileRows, n * rank16);
-        bool ok = true;
-        for (int kb = kb0; kb < kb1; ++kb) {
-          ok = ptx::mbar_wait(ptx::smem_u32(&bar.full[stage]), phase, abort_flag);
-          if (!ok) break;
-          ptx::tc_fence_after_sync();
-          const uint32_t at = ring + stage * kStageBytes;
-          const uint64_t a = ptx::smem_desc_sw128(at), b = ptx::smem_desc_sw128(at + kXBytes);
-#pragma unroll
-          for (int k = 0; k < kBK / 16; ++k) ptx::tc_mma_bf16(tmem, a + 2 * k, b + 2 * k, idesc, kb > kb0 || k > 0);
-          ptx::tc_commit(ptx::smem_u32(&bar.empty[stage]));
-          if (++stage == stages) { stage = 0; phase ^= 1u; }
-        }
-        if (ok) ptx::tc_commit(ptx::smem_u32(&bar.acc_full[0]));
-        else timed_out(p, 2);
-      }
-      __syncwarp();
-    } else {
-      // each row's sums into the ring's place: every stage has been consumed when the accumulator is complete
-      const int quarter = warp & 3, r = quarter * 32 + lane, slot = ids.slot[r];
-      const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
-      if (!__all_sync(kFull, ptx::mbar_wait(ptx::smem_u32(&bar.acc_full[0]), round & 1, abort_flag))) {
-        if (lane == 0) timed_out(p, 3);
-      } else {
-        ptx::tc_fence_after_sync();
-        float* dst = reinterpret_cast<float*>(base) + r * pitch;
-        for (int i = 0; i < n; ++i) {
-          const bool mine = slot == s0 + i;
-          if (!__any_sync(kFull, mine)) continue;
-          for (int j = 0; j < p.rank; j += 8) {
-            uint32_t v[8];
-            ptx::tmem_ld_32x8(lanes + i * rank16 + j, v);
-            ptx::tmem_ld_wait();
-            if (mine) {
-              *reinterpret_cast<uint4*>(dst + j) = make_uint4(v[0], v[1], v[2], v[3]);
-              *reinterpret_cast<uint4*>(dst + j + 4) = make_uint4(v[4], v[5], v[6], v[7]);
-            }
-          }
-        }
-        ptx::tc_fence_before_sync();
-      }
-    }
-    // the cluster's sums over its parts of K, a share of the rows per CTA; two terms of bf16
-    ptx::cluster_sync();
-    ptx::tc_fence_after_sync();
-    const int r0 = kTileRows * split / p.splits, r1 = kTileRows * (split + 1) / p.splits, chunks = p.rank / 8;
-    for (int i = threadIdx.x; i < (r1 - r0) * chunks; i += kThreads) {
-      const int r = r0 + i / chunks, j = 8 * (i % chunks), slot = ids.slot[r];
-      if (slot < s0 || slot >= s0 + n) continue;
-      const uint32_t at = ring + (r * pitch + j) * 4;
-      float4 a[kMaxSplits], b[kMaxSplits];
-#pragma unroll
-      for (int s = 0; s < kMaxSplits; ++s) {
-        a[s] = b[s] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (s < p.splits) {
-          const uint32_t from = ptx::map_to_cta(at, s);
-          a[s] = ptx::ld_cluster_f4(from);
-          b[s] = ptx::ld_cluster_f4(from + 16);
-        }
-      }
-      float v[8] = {a[0].x, a[0].y, a[0].z, a[0].w, b[0].x, b[0].y, b[0].z, b[0].w};
-#pragma unroll
-      for (int s = 1; s < kMaxSplits; ++s) {
-        if (s < p.splits) {
-          v[0] += a[s].x; v[1] += a[s].y; v[2] += a[s].z; v[3] += a[s].w;
-          v[4] += b[s].x; v[5] += b[s].y; v[6] += b[s].z; v[7] += b[s].w;
-        }
-      }
-      if (p.scale != nullptr) {
-        const float f = __ldg(p.scale + ids.id[r]);
-#pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] *= f;
-      }
-      uint4 hi, lo;
-      two_terms(v, hi, lo);
-      __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(p.t) + (row0 + r) * p.rank + j;
-      *reinterpret_cast<uint4*>(to) = hi;
-      *reinterpret_cast<uint4*>(to + static_cast<size_t>(p.rows) * p.rank) = lo;
-    }
-    ptx::fence_proxy_async_smem();                         // the sums' place becomes the ring again
-    ptx::cluster_sync();
-  }
-  if (count == 0 && threadIdx.x == 0) {                    // nothing asks for the x on its way: it lands first
-    for (int i = 0; i < ahead; ++i) {
-      ptx::mbar_arrive(ptx::smem_u32(&bar.full[i]));
-      ptx::mbar_wait(ptx::smem_u32(&bar.full[i]), 0, abort_flag);
-    }
-  }
-  finish(&bar, warp);
+// y + d in bf16.
+__device__ __forceinline__ uint32_t add_pair(uint32_t y, uint32_t d0, uint32_t d1) {
+  return pair(low(y) + __uint_as_float(d0), high(y) + __uint_as_float(d1));
 }
 
 // The four epilogue warps meet; whether any of them has given up.
@@ -302,98 +107,238 @@ __device__ __forceinline__ bool epilogue_meets(bool gave_up) {
   return any != 0;
 }
 
+// Grid: a cluster of `cluster` CTAs per tile.
 __global__ void __launch_bounds__(kThreads)
-adapter_expand_tiles(const __grid_constant__ CUtensorMap tm_t, const __grid_constant__ CUtensorMap tm_b,
-                     const __grid_constant__ CUtensorMap tm_in, const __grid_constant__ CUtensorMap tm_out,
-                     const AdapterParams p, int groups) {
+adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int cluster) {
   extern __shared__ unsigned char smem_raw[];
-  __shared__ TileIds ids;
   __shared__ Barriers bar;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int tile = blockIdx.x / groups, group = blockIdx.x - tile * groups;
-  const long long row0 = static_cast<long long>(tile) * kTileRows;
-  const int atoms = (p.rank + 63) / 64;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3;
+  const int tile = blockIdx.x / cluster, part = blockIdx.x - tile * cluster;
+
+  // the tile's segment, rows and adapter: each warp finds them by itself
+  auto bound = [&](int s) {
+    const long long o = __ldg(p.offsets + s);
+    return o < 0 ? 0LL : o > p.rows ? p.rows : o;
+  };
+  const int seg = moe::last_at_or_below(p.segments + 1, tile, lane, [&](int s) { return bound(s) / kTileRows + s; });
+  if (seg < 0) return;                                     // (offsets that do not begin with 0)
+  const long long begin = bound(seg), end = seg < p.segments ? bound(seg + 1) : p.rows;
+  const long long row0 = begin + (tile - (begin / kTileRows + seg)) * kTileRows;
+  if (row0 >= end) return;                                 // (the whole cluster)
+  const int m = static_cast<int>(end - row0 < kTileRows ? end - row0 : kTileRows);
+  int id = seg < p.segments ? __ldg(p.adapter_of + seg) : -1;
+  if (id >= p.adapters) {
+    if (part == 0 && threadIdx.x == 0) {
+      atomicCAS(&p.status[0], 0, MOE_ERR_BAD_ROUTING);
+      atomicCAS(&p.status[1], 0, seg);
+    }
+    id = -1;
+  }
+  const bool has = id >= 0;
+  if (!has && p.y_in == p.y_out) return;                   // nothing to add and nothing to copy
+
+  const Layout lay(p.rank);
   unsigned char* base = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
-  unsigned char* ybase = base + 2 * atoms * kAtomA;        // A: the atoms of the first terms, then of the second
-  const uint32_t a_at = ptx::smem_u32(base), y_at = ptx::smem_u32(ybase), b_at = y_at + kYStages * kYBytes;
+  const uint32_t base_at = ptx::smem_u32(base);
+  const int blocks = (p.K + kBK - 1) / kBK, parts = min(cluster, blocks);
+  const bool sums = has && part < parts;                   // this CTA has a part of K
+  const int kb0 = sums ? static_cast<int>(static_cast<long long>(blocks) * part / parts) : 0;
+  const int kb1 = sums ? static_cast<int>(static_cast<long long>(blocks) * (part + 1) / parts) : 0;
   const int tiles = (p.N - 1) / kBN + 1;
-  const int n0 = static_cast<int>(static_cast<long long>(tiles) * group / groups);
-  const int n1 = static_cast<int>(static_cast<long long>(tiles) * (group + 1) / groups);
-  const int ahead = min(kYStages, n1 - n0);                // tiles of y on their way before the adapters are known
+  const int n0 = static_cast<int>(static_cast<long long>(tiles) * part / cluster);
+  const int n1 = static_cast<int>(static_cast<long long>(tiles) * (part + 1) / cluster);
+  const int y_ahead = min(kYStages, n1 - n0);
+  const bool few = m <= kShortRows;
+  const CUtensorMap* tm_x = few ? &maps.x_short : &maps.x;
+  const CUtensorMap* tm_in = few ? &maps.in_short : &maps.in;
+  const uint32_t tile_bytes = few ? kShortRows * 128 : kTileRows * 128;    // of x in a stage, and of a tile of y
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kBStages; ++i) {
+    for (int i = 0; i < lay.stages; ++i) {
       ptx::mbar_init(ptx::smem_u32(&bar.full[i]), 1);
       ptx::mbar_init(ptx::smem_u32(&bar.empty[i]), 1);
     }
     for (int i = 0; i < kYStages; ++i) ptx::mbar_init(ptx::smem_u32(&bar.y_full[i]), 1);
+    for (int i = 0; i < kBStages; ++i) {
+      ptx::mbar_init(ptx::smem_u32(&bar.b_full[i]), 1);
+      ptx::mbar_init(ptx::smem_u32(&bar.b_empty[i]), 1);
+    }
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(ptx::smem_u32(&bar.acc_full[i]), 1);
       ptx::mbar_init(ptx::smem_u32(&bar.acc_empty[i]), 4);
     }
+    ptx::mbar_init(ptx::smem_u32(&bar.sums_full), 1);
     ptx::mbar_init(ptx::smem_u32(&bar.t_full), 1);
     bar.abort_flag = 0;
     ptx::fence_barrier_init();
-    for (int i = 0; i < ahead; ++i) {
-      ptx::mbar_expect_tx(ptx::smem_u32(&bar.y_full[i]), kYBytes);
-      ptx::tma_load_2d(y_at + i * kYBytes, &tm_in, ptx::smem_u32(&bar.y_full[i]), (n0 + i) * kBN, static_cast<int>(row0));
-    }
   }
   if (warp == 1) {
     ptx::tmem_alloc(ptx::smem_u32(&bar.tmem), kCols);
     ptx::tmem_relinquish();
     ptx::tc_fence_before_sync();
   }
-  const int count = collect(p, row0, &ids, false);
+  __syncthreads();
   ptx::tc_fence_after_sync();
-  const uint32_t tmem = bar.tmem;
+  const uint32_t tmem = bar.tmem, lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
   volatile int* abort_flag = &bar.abort_flag;
+  const int r = quarter * 32 + lane;                       // the row of an epilogue thread
+  int y_issued = 0;                                        // (warp 0's lane 0)
+  auto load_y = [&](int slot, int n) {
+    const uint32_t full = ptx::smem_u32(&bar.y_full[slot]);
+    ptx::mbar_expect_tx(full, tile_bytes);
+    ptx::tma_load_2d(base_at + lay.y_at + slot * kYBytes, tm_in, full, n * kBN, static_cast<int>(row0));
+  };
 
+  // ------------------------------------------------------------------------------------------------ t = x a^T
+  if (has) {
+    const int pitch = p.rank + 4;                          // floats of a row of sums: an odd number of 16 bytes
+    if (warp == 0) {
+      if (lane == 0 && sums) {
+        int stage = 0;
+        uint32_t phase = 1;
+        bool ok = true;
+        for (int kb = kb0; kb < kb1; ++kb) {
+          ok = ptx::mbar_wait(ptx::smem_u32(&bar.empty[stage]), phase, abort_flag);
+          if (!ok) break;
+          const uint32_t full = ptx::smem_u32(&bar.full[stage]), at = base_at + stage * lay.stage_bytes;
+          ptx::mbar_expect_tx(full, tile_bytes + lay.rank16 * 128);
+          ptx::tma_load_2d(at, tm_x, full, kb * kBK, static_cast<int>(row0));
+          ptx::tma_load_2d(at + kXBytes, &maps.a, full, kb * kBK, id * p.rank);
+          if (++stage == lay.stages) { stage = 0; phase ^= 1u; }
+        }
+        ok = ok && ptx::mbar_wait(ptx::smem_u32(&bar.sums_full), 0, abort_flag);
+        if (!ok) timed_out(p, 1);
+      }
+      // nothing reads the ring any more: y's tiles in front of the sums may come
+      if (lane == 0 && !*abort_flag)
+        for (; y_issued < y_ahead && lay.y_at + (y_issued + 1) * kYBytes <= lay.sums_at; ++y_issued)
+          load_y(y_issued, n0 + y_issued);
+      __syncwarp();
+    } else if (warp == 1) {
+      if (lane == 0 && sums) {
+        const uint32_t idesc = ptx::idesc_bf16_f32(kTileRows, lay.rank16);
+        int stage = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (int kb = kb0; kb < kb1; ++kb) {
+          ok = ptx::mbar_wait(ptx::smem_u32(&bar.full[stage]), phase, abort_flag);
+          if (!ok) break;
+          ptx::tc_fence_after_sync();
+          const uint32_t at = base_at + stage * lay.stage_bytes;
+          const uint64_t a = ptx::smem_desc_sw128(at), b = ptx::smem_desc_sw128(at + kXBytes);
+#pragma unroll
+          for (int k = 0; k < kBK / 16; ++k) ptx::tc_mma_bf16(tmem, a + 2 * k, b + 2 * k, idesc, kb > kb0 || k > 0);
+          ptx::tc_commit(ptx::smem_u32(&bar.empty[stage]));
+          if (++stage == lay.stages) { stage = 0; phase ^= 1u; }
+        }
+        if (ok) ptx::tc_commit(ptx::smem_u32(&bar.sums_full));
+        else timed_out(p, 2);
+      }
+      __syncwarp();
+    } else if (sums) {
+      if (!__all_sync(kFull, ptx::mbar_wait(ptx::smem_u32(&bar.sums_full), 0, abort_flag))) {
+        if (lane == 0) timed_out(p, 3);
+      } else if (quarter * 32 < m) {
+        ptx::tc_fence_after_sync();
+        float* dst = reinterpret_cast<float*>(base + lay.sums_at) + r * pitch;
+        for (int j = 0; j < p.rank; j += 16) {
+          uint32_t v[16];
+          ptx::tmem_ld_32x16(lanes + j, v);
+          ptx::tmem_ld_wait();
+#pragma unroll
+          for (int q = 0; q < 16; q += 4)
+            if (q < 8 || j + 8 < p.rank)
+              *reinterpret_cast<uint4*>(dst + j + q) = make_uint4(v[q], v[q + 1], v[q + 2], v[q + 3]);
+        }
+        ptx::tc_fence_before_sync();
+      }
+    }
+    // the cluster's sums over its parts of K in order, a share of the rows per CTA
+    ptx::cluster_sync();
+    ptx::tc_fence_after_sync();
+    const float f = p.scale != nullptr ? __ldg(p.scale + id) : 1.f;
+    const int r0 = m * part / cluster, r1 = m * (part + 1) / cluster, chunks = p.rank / 8;
+    for (int i = threadIdx.x; i < (r1 - r0) * chunks; i += kThreads) {
+      const int row = r0 + i / chunks, j = 8 * (i % chunks);
+      const uint32_t at = base_at + lay.sums_at + (row * pitch + j) * 4;
+      float4 a[kMaxCluster], b[kMaxCluster];
+#pragma unroll
+      for (int s = 0; s < kMaxCluster; ++s) {
+        if (s < parts) {
+          const uint32_t from = ptx::map_to_cta(at, s);
+          a[s] = ptx::ld_cluster_f4(from);
+          b[s] = ptx::ld_cluster_f4(from + 16);
+        }
+      }
+      float v[8] = {a[0].x, a[0].y, a[0].z, a[0].w, b[0].x, b[0].y, b[0].z, b[0].w};
+#pragma unroll
+      for (int s = 1; s < kMaxCluster; ++s) {
+        if (s < parts) {
+          v[0] += a[s].x; v[1] += a[s].y; v[2] += a[s].z; v[3] += a[s].w;
+          v[4] += b[s].x; v[5] += b[s].y; v[6] += b[s].z; v[7] += b[s].w;
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] *= f;
+      uint4 hi, lo;
+      two_terms(v, hi, lo);
+      __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(p.t) + (row0 + row) * p.rank + j;
+      *reinterpret_cast<uint4*>(to) = hi;
+      *reinterpret_cast<uint4*>(to + static_cast<size_t>(p.rows) * p.rank) = lo;
+    }
+    // t is read by TMA in every CTA of the cluster, and the sums' place belongs to TMA again
+    __syncwarp();
+    __threadfence();
+    ptx::fence_proxy_async_all();
+    ptx::cluster_sync();
+  }
+
+  // ------------------------------------------------------------------------------------------------ y += t b^T
   if (warp == 0) {
     if (lane == 0) {
+      bool ok = true;
+      if (has) {
+        ptx::fence_proxy_async_all();
+        ptx::mbar_expect_tx(ptx::smem_u32(&bar.t_full), 2 * lay.atoms * kAtomA);
+        for (int term = 0; term < 2; ++term)
+          for (int k = 0; k < lay.atoms; ++k)
+            ptx::tma_load_2d(base_at + (term * lay.atoms + k) * kAtomA, &maps.t, ptx::smem_u32(&bar.t_full), k * 64,
+                             static_cast<int>(term * p.rows + row0));
+      }
+      for (; y_issued < y_ahead; ++y_issued) load_y(y_issued, n0 + y_issued);
       int bs = 0;
       uint32_t b_phase = 1;
-      bool ok = true;
-      for (int i = n0; i < n1 && ok; ++i) {
-        for (int s = 0; s < count; ++s) {
-          ok = ptx::mbar_wait(ptx::smem_u32(&bar.empty[bs]), b_phase, abort_flag);
-          if (!ok) break;
-          const uint32_t full = ptx::smem_u32(&bar.full[bs]);
-          ptx::mbar_expect_tx(full, atoms * kAtomB);
-          for (int k = 0; k < atoms; ++k)
-            ptx::tma_load_2d(b_at + (bs * atoms + k) * kAtomB, &tm_b, full, k * 64, ids.list[s] * p.N + i * kBN);
-          if (++bs == kBStages) { bs = 0; b_phase ^= 1u; }
-        }
+      for (int i = n0; i < n1 && has; ++i) {
+        ok = ptx::mbar_wait(ptx::smem_u32(&bar.b_empty[bs]), b_phase, abort_flag);
+        if (!ok) break;
+        const uint32_t full = ptx::smem_u32(&bar.b_full[bs]);
+        ptx::mbar_expect_tx(full, lay.atoms * kAtomB);
+        for (int k = 0; k < lay.atoms; ++k)
+          ptx::tma_load_2d(base_at + lay.b_at + (bs * lay.atoms + k) * kAtomB, &maps.b, full, k * 64, id * p.N + i * kBN);
+        if (++bs == kBStages) { bs = 0; b_phase ^= 1u; }
       }
       if (!ok) timed_out(p, 4);
     }
     __syncwarp();
   } else if (warp == 1) {
-    if (lane == 0 && count > 0) {
-      ptx::wait_for_previous_kernel();
-      ptx::mbar_expect_tx(ptx::smem_u32(&bar.t_full), 2 * atoms * kAtomA);
-      for (int term = 0; term < 2; ++term)
-        for (int k = 0; k < atoms; ++k)
-          ptx::tma_load_2d(a_at + (term * atoms + k) * kAtomA, &tm_t, ptx::smem_u32(&bar.t_full), k * 64,
-                           static_cast<int>(term * p.rows + row0));
+    if (lane == 0 && has) {
       const uint32_t idesc = ptx::idesc_bf16_f32(kTileRows, kBN);
-      const int steps = (p.rank + 15) / 16;
       int bs = 0, acc = 0;
       uint32_t b_phase = 0, acc_phase = 1;
+      // (also where this CTA has no columns: what it asked for lands)
       bool ok = ptx::mbar_wait(ptx::smem_u32(&bar.t_full), 0, abort_flag);
-      const int units = (n1 - n0) * count;
-      for (int u = 0; u < units && ok; ++u) {
-        ok = ptx::mbar_wait(ptx::smem_u32(&bar.full[bs]), b_phase, abort_flag) &&
+      for (int i = n0; i < n1 && ok; ++i) {
+        ok = ptx::mbar_wait(ptx::smem_u32(&bar.b_full[bs]), b_phase, abort_flag) &&
              ptx::mbar_wait(ptx::smem_u32(&bar.acc_empty[acc]), acc_phase, abort_flag);
         if (!ok) break;
         ptx::tc_fence_after_sync();
         for (int term = 0; term < 2; ++term) {
-          for (int k = 0; k < steps; ++k) {
-            const uint64_t a = ptx::smem_desc_sw128(a_at + (term * atoms + (k >> 2)) * kAtomA) + 2 * (k & 3);
-            const uint64_t b = ptx::smem_desc_sw128(b_at + (bs * atoms + (k >> 2)) * kAtomB) + 2 * (k & 3);
+          for (int k = 0; k < lay.rank16 / 16; ++k) {
+            const uint64_t a = ptx::smem_desc_sw128(base_at + (term * lay.atoms + (k >> 2)) * kAtomA) + 2 * (k & 3);
+            const uint64_t b = ptx::smem_desc_sw128(base_at + lay.b_at + (bs * lay.atoms + (k >> 2)) * kAtomB) + 2 * (k & 3);
             ptx::tc_mma_bf16(tmem + acc * kBN, a, b, idesc, term > 0 || k > 0);
           }
         }
-        ptx::tc_commit(ptx::smem_u32(&bar.empty[bs]));
+        ptx::tc_commit(ptx::smem_u32(&bar.b_empty[bs]));
         ptx::tc_commit(ptx::smem_u32(&bar.acc_full[acc]));
         if (++bs == kBStages) { bs = 0; b_phase ^= 1u; }
         if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
@@ -402,58 +347,56 @@ adapter_expand_tiles(const __grid_constant__ CUtensorMap tm_t, const __grid_cons
     }
     __syncwarp();
   } else {
-    ptx::wait_for_previous_kernel();
-    const int quarter = warp & 3, r = quarter * 32 + lane, slot = ids.slot[r];
-    const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
+    const bool whole = m == kTileRows, live = quarter * 32 < m;
     int ys = 0, acc = 0;
     uint32_t y_phase = 0, acc_phase = 0;
-    bool ok = true;
-    const bool idle = count == 0 && p.y_in == p.y_out;     // nothing to add and nothing to copy: what was asked for lands
-    for (int i = 0; idle && i < ahead; ++i) ptx::mbar_wait(ptx::smem_u32(&bar.y_full[i]), 0, abort_flag);
-    for (int i = n0; i < n1 && !idle; ++i) {
-      ok = __all_sync(kFull, ptx::mbar_wait(ptx::smem_u32(&bar.y_full[ys]), y_phase, abort_flag));
-      unsigned char* row = ybase + ys * kYBytes + r * 128;
-      for (int s = 0; s < count && ok; ++s) {
-        ok = __all_sync(kFull, ptx::mbar_wait(ptx::smem_u32(&bar.acc_full[acc]), acc_phase, abort_flag));
-        const bool mine = slot == s;
-        if (ok && __any_sync(kFull, mine)) {
-          ptx::tc_fence_after_sync();
+    for (int i = n0; i < n1; ++i) {
+      bool ok = __all_sync(kFull, ptx::mbar_wait(ptx::smem_u32(&bar.y_full[ys]), y_phase, abort_flag) &&
+                                      (!has || ptx::mbar_wait(ptx::smem_u32(&bar.acc_full[acc]), acc_phase, abort_flag)));
+      unsigned char* row = base + lay.y_at + ys * kYBytes + r * 128;
+      if (ok && live && (has || !whole)) {
+        ptx::tc_fence_after_sync();
+        __nv_bfloat16* out = p.y_out + static_cast<size_t>(row0 + r) * p.N + i * kBN;
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            uint32_t v[32];
+        for (int half = 0; half < 2; ++half) {
+          uint32_t v[32];
+          if (has) {
             ptx::tmem_ld_32x32(lanes + acc * kBN + half * 32, v);
             ptx::tmem_ld_wait();
-            if (mine) {
-#pragma unroll
-              for (int c = 0; c < 4; ++c) {
-                uint4* at = reinterpret_cast<uint4*>(row + (((half * 4 + c) ^ (r & 7)) << 4));
-                uint4 y = *at;
-                y.x = pair(low(y.x) + __uint_as_float(v[8 * c]), high(y.x) + __uint_as_float(v[8 * c + 1]));
-                y.y = pair(low(y.y) + __uint_as_float(v[8 * c + 2]), high(y.y) + __uint_as_float(v[8 * c + 3]));
-                y.z = pair(low(y.z) + __uint_as_float(v[8 * c + 4]), high(y.z) + __uint_as_float(v[8 * c + 5]));
-                y.w = pair(low(y.w) + __uint_as_float(v[8 * c + 6]), high(y.w) + __uint_as_float(v[8 * c + 7]));
-                *at = y;
-              }
-            }
           }
-          ptx::tc_fence_before_sync();
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            uint4* at = reinterpret_cast<uint4*>(row + (((half * 4 + c) ^ (r & 7)) << 4));
+            uint4 y = *at;
+            if (has) {
+              y.x = add_pair(y.x, v[8 * c], v[8 * c + 1]);
+              y.y = add_pair(y.y, v[8 * c + 2], v[8 * c + 3]);
+              y.z = add_pair(y.z, v[8 * c + 4], v[8 * c + 5]);
+              y.w = add_pair(y.w, v[8 * c + 6], v[8 * c + 7]);
+            }
+            // a whole tile leaves by TMA, the rows of another one by themselves
+            if (whole) *at = y;
+            else if (r < m && i * kBN + half * 32 + c * 8 < p.N) *reinterpret_cast<uint4*>(out + half * 32 + c * 8) = y;
+          }
         }
-        __syncwarp();
+        ptx::tc_fence_before_sync();
+      }
+      __syncwarp();
+      if (has) {
         if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&bar.acc_empty[acc]));
         if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
       }
       if (!ok && lane == 0) timed_out(p, 6);
       ptx::fence_proxy_async_smem();
-      if (epilogue_meets(!ok)) break;                    // one verdict for the four warps
+      if (epilogue_meets(!ok)) break;                      // one verdict for the four warps
       if (warp == 2 && lane == 0) {
-        ptx::tma_store_2d(&tm_out, y_at + ys * kYBytes, i * kBN, static_cast<int>(row0));
-        ptx::bulk_commit_group();
-        if (i > n0 && i - 1 + ahead < n1) {                // the tile before this has left: a later one takes its place
-          const int free = ys == 0 ? kYStages - 1 : ys - 1;
-          const uint32_t y_full = ptx::smem_u32(&bar.y_full[free]);
+        if (whole) {
+          ptx::tma_store_2d(&maps.out, base_at + lay.y_at + ys * kYBytes, i * kBN, static_cast<int>(row0));
+          ptx::bulk_commit_group();
+        }
+        if (i > n0 && i - 1 + y_ahead < n1) {              // the tile before this has left: a later one takes its place
           ptx::bulk_wait_group_read_but_one();
-          ptx::mbar_expect_tx(y_full, kYBytes);
-          ptx::tma_load_2d(y_at + free * kYBytes, &tm_in, y_full, (i - 1 + ahead) * kBN, static_cast<int>(row0));
+          load_y(ys == 0 ? kYStages - 1 : ys - 1, i - 1 + y_ahead);
         }
       }
       if (++ys == kYStages) { ys = 0; y_phase ^= 1u; }
@@ -461,7 +404,17 @@ adapter_expand_tiles(const __grid_constant__ CUtensorMap tm_t, const __grid_cons
     if (warp == 2 && lane == 0) ptx::bulk_wait_group_read_all();
     __syncwarp();
   }
-  finish(&bar, warp);
+
+  // Frees what the CTA holds; after a wait that gave up, copies in flight get time to land first.
+  __syncthreads();
+  if (bar.abort_flag) {
+    for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+    __syncthreads();
+  }
+  if (warp == 1) {
+    ptx::tc_fence_after_sync();
+    ptx::tmem_dealloc(tmem, kCols);
+  }
 }
 
 bool encode(moe_ctx* ctx, CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows) {
@@ -474,20 +427,15 @@ bool encode(moe_ctx* ctx, CUtensorMap* map, const void* base, uint64_t rows, uin
                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-int shrink_smem(int stages) { return 1024 + stages * kStageBytes; }
-int expand_smem(int rank) {
-  const int atoms = (rank + 63) / 64;
-  return 1024 + 2 * atoms * kAtomA + kYStages * kYBytes + kBStages * atoms * kAtomB;
-}
+long long tiles_of(long long rows, int segments) { return rows / kTileRows + segments + 1; }
 
-// Parts of K: as many as two CTAs per SM take, at most a portable cluster.
-int splits_of(const moe_ctx* ctx, long long rows, int K) {
-  const long long tiles = (rows + kTileRows - 1) / kTileRows;
-  const int blocks = (K + kBK - 1) / kBK;
-  long long s = 2LL * ctx->num_sms / tiles;
-  if (s > kMaxSplits) s = kMaxSplits;
-  if (s > blocks) s = blocks;
-  return s < 1 ? 1 : static_cast<int>(s);
+// CTAs of a tile: as many as are resident at once (two on an SM, one above 64 ranks), at most a portable cluster.
+int cluster_of(const moe_ctx* ctx, long long tiles, int rank, int N, int K) {
+  const int most = (N - 1) / kBN + 1 > (K - 1) / kBK + 1 ? (N - 1) / kBN + 1 : (K - 1) / kBK + 1;
+  long long c = (rank > 64 ? 1LL : 2LL) * ctx->num_sms / tiles;
+  if (c > kMaxCluster) c = kMaxCluster;
+  if (c > most) c = most;
+  return c < 1 ? 1 : static_cast<int>(c);
 }
 
 }  // namespace
@@ -496,51 +444,35 @@ namespace moe {
 
 size_t adapter_tile_scratch_bytes(long long rows, int rank) { return static_cast<size_t>(rows) * rank * 4; }
 
-moe_status launch_adapter_tiles(moe_ctx* ctx, AdapterParams p, cudaStream_t stream) {
-  const int rank16 = (p.rank + 15) / 16 * 16;
-  CUtensorMap tm_x, tm_a, tm_t, tm_b, tm_in, tm_out;
-  if (!encode(ctx, &tm_x, p.x, p.rows, p.K, kTileRows) ||
-      !encode(ctx, &tm_a, p.a, static_cast<uint64_t>(p.adapters) * p.rank, p.K, rank16) ||
-      !encode(ctx, &tm_t, p.t, 2 * static_cast<uint64_t>(p.rows), p.rank, kTileRows) ||
-      !encode(ctx, &tm_b, p.b, static_cast<uint64_t>(p.adapters) * p.N, p.rank, kBN) ||
-      !encode(ctx, &tm_in, p.y_in, p.rows, p.N, kTileRows) || !encode(ctx, &tm_out, p.y_out, p.rows, p.N, kTileRows))
+moe_status launch_adapter_tiles(moe_ctx* ctx, const AdapterParams& p, cudaStream_t stream) {
+  Maps m;
+  const uint64_t factor_rows = static_cast<uint64_t>(p.adapters) * p.rank, out_rows = static_cast<uint64_t>(p.adapters) * p.N;
+  if (!encode(ctx, &m.x, p.x, p.rows, p.K, kTileRows) || !encode(ctx, &m.x_short, p.x, p.rows, p.K, kShortRows) ||
+      !encode(ctx, &m.a, p.a, factor_rows, p.K, Layout(p.rank).rank16) ||
+      !encode(ctx, &m.t, p.t, 2 * static_cast<uint64_t>(p.rows), p.rank, kTileRows) ||
+      !encode(ctx, &m.b, p.b, out_rows, p.rank, kBN) || !encode(ctx, &m.in, p.y_in, p.rows, p.N, kTileRows) ||
+      !encode(ctx, &m.in_short, p.y_in, p.rows, p.N, kShortRows) || !encode(ctx, &m.out, p.y_out, p.rows, p.N, kTileRows))
     return MOE_ERR_CUDA;
-  p.splits = splits_of(ctx, p.rows, p.K);
-  const long long tiles = (p.rows + kTileRows - 1) / kTileRows;
-  const int stages = 3;
+  const long long tiles = tiles_of(p.rows, p.segments);
+  const int cluster = cluster_of(ctx, tiles, p.rank, p.N, p.K);
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr{};
+  cfg.gridDim = dim3(static_cast<unsigned>(tiles * cluster));
   cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = 1024 + Layout(p.rank).bytes;
   cfg.stream = stream;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  cfg.gridDim = dim3(static_cast<unsigned>(tiles * p.splits));
-  cfg.dynamicSmemBytes = shrink_smem(stages);
   attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = static_cast<unsigned>(p.splits);
+  attr.val.clusterDim.x = static_cast<unsigned>(cluster);
   attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  if (cudaLaunchKernelEx(&cfg, adapter_shrink_tiles, tm_x, tm_a, p, stages, rank16) != cudaSuccess) return MOE_ERR_CUDA;
-  const int n_tiles = (p.N - 1) / kBN + 1;
-  long long groups = 2LL * ctx->num_sms / tiles;
-  if (groups > n_tiles) groups = n_tiles;
-  if (groups < 1) groups = 1;
-  cfg.gridDim = dim3(static_cast<unsigned>(tiles * groups));
-  cfg.dynamicSmemBytes = expand_smem(p.rank);
-  attr = cudaLaunchAttribute{};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  ctx->last_launches += 2;
-  return cudaLaunchKernelEx(&cfg, adapter_expand_tiles, tm_t, tm_b, tm_in, tm_out, p, static_cast<int>(groups)) == cudaSuccess
-             ? MOE_OK
-             : MOE_ERR_CUDA;
+  ctx->last_launches += 1;
+  return cudaLaunchKernelEx(&cfg, adapter_tiles, m, p, cluster) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
 cudaError_t prepare_adapter_tiles(moe_ctx* ctx) {
   (void)ctx;
-  const cudaError_t e = cudaFuncSetAttribute(adapter_shrink_tiles, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                             shrink_smem(kMaxStages));
-  if (e != cudaSuccess) return e;
-  return cudaFuncSetAttribute(adapter_expand_tiles, cudaFuncAttributeMaxDynamicSharedMemorySize, expand_smem(128));
+  return cudaFuncSetAttribute(adapter_tiles, cudaFuncAttributeMaxDynamicSharedMemorySize, 1024 + Layout(128).bytes);
 }
 
 }  // namespace moe

@@ -33,7 +33,7 @@ adapter_shrink(const AdapterParams p) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
   const long long row0 = static_cast<long long>(blockIdx.x) * kRows;
   const int split = blockIdx.y;
-  if (threadIdx.x < kRows) s_id[threadIdx.x] = moe::adapter_of_row(p, p.offsets, row0 + threadIdx.x, split == 0);
+  if (threadIdx.x < kRows) s_id[threadIdx.x] = moe::adapter_of_row(p, p.offsets, p.adapter_of, row0 + threadIdx.x, split == 0);
   __syncthreads();
   const int my_id = s_id[lane & 15];
   unsigned left = __ballot_sync(kFull, my_id >= 0) & 0xFFFFu;
@@ -97,7 +97,7 @@ adapter_expand(const AdapterParams p) {
   const int tid = threadIdx.x;
   const long long row0 = static_cast<long long>(blockIdx.x) * kRows;
   const int n = blockIdx.y * kThreads + tid;
-  if (tid < kRows) s_id[tid] = moe::adapter_of_row(p, p.offsets, row0 + tid, false);
+  if (tid < kRows) s_id[tid] = moe::adapter_of_row(p, p.offsets, p.adapter_of, row0 + tid, false);
   __syncthreads();
   for (int i = tid; i < kRows * p.rank; i += kThreads) {
     const int r = i / p.rank, j = i - r * p.rank;

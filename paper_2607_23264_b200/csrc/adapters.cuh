@@ -21,8 +21,9 @@ struct AdapterParams {
   int N, K, rank, adapters, segments, splits;
 };
 
-// The adapter of a row, -1 without one.  `offsets` is p.offsets or a copy of it.
-__device__ __forceinline__ int adapter_of_row(const AdapterParams& p, const int32_t* offsets, long long row, bool report) {
+// The adapter of a row, -1 without one.  `offsets` and `adapter_of` are p's or copies of them.
+__device__ __forceinline__ int adapter_of_row(const AdapterParams& p, const int32_t* offsets, const int32_t* adapter_of,
+                                              long long row, bool report) {
   if (row >= p.rows) return -1;
   int seg = static_cast<int>(row);
   if (offsets != nullptr) {
@@ -35,7 +36,7 @@ __device__ __forceinline__ int adapter_of_row(const AdapterParams& p, const int3
     if (lo < 0 || row >= offsets[lo + 1]) return -1;
     seg = lo;
   }
-  const int id = __ldg(p.adapter_of + seg);
+  const int id = adapter_of[seg];
   if (id >= p.adapters) {
     if (report) {
       atomicCAS(&p.status[0], 0, MOE_ERR_BAD_ROUTING);
@@ -48,6 +49,6 @@ __device__ __forceinline__ int adapter_of_row(const AdapterParams& p, const int3
 
 // Long segments: tiles of 128 rows on the tensor cores.
 size_t adapter_tile_scratch_bytes(long long rows, int rank);
-moe_status launch_adapter_tiles(moe_ctx* ctx, AdapterParams p, cudaStream_t stream);
+moe_status launch_adapter_tiles(moe_ctx* ctx, const AdapterParams& p, cudaStream_t stream);
 
 }  // namespace moe

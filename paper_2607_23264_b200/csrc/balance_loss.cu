@@ -12,6 +12,7 @@
 
 #include "moe_internal.h"
 #include "route_scored.cuh"
+#include "warp_search.cuh"
 
 namespace {
 
@@ -65,22 +66,6 @@ __device__ __forceinline__ int offset_at(const int32_t* offsets, int q, int T) {
   const int o = __ldg(offsets + q);
   return min(max(o, 0), T);
 }
-// The last i in [0, n) with key(i) <= at, or -1; key ascends.  By a whole warp, 32 candidates a step.
-template <typename Key>
-__device__ __forceinline__ int last_at_or_below(int n, long long at, int lane, Key key) {
-  int lo = -1, hi = n;                                     // key(lo) <= at < key(hi)
-  while (hi - lo > 1) {
-    const int step = (hi - lo - 1 + 31) / 32;
-    const int i = lo + 1 + lane * step;
-    const unsigned below = __ballot_sync(kFull, i < hi && key(i) <= at);
-    const int found = 32 - __clz(below);                   // candidates at or below form a prefix
-    const int base = lo;
-    if (found > 0) lo = base + 1 + (found - 1) * step;
-    hi = min(hi, base + 1 + found * step);
-  }
-  return lo;
-}
-
 // Probabilities of one token over its lanes: x becomes p; returns what else the losses need.
 struct Token {
   float lse;                                               // log of the sum of exponentials, -inf when all are masked
@@ -144,7 +129,7 @@ balance_partial(const BalanceParams p) {
   if (slot == 0 && threadIdx.x == 0) *p.scratch.ticket = 0;
   for (int e = threadIdx.x; e < p.E; e += kThreads) s_count[e] = 0;
 
-  const int q = last_at_or_below(p.sequences, slot, lane, [&](int i) {
+  const int q = moe::last_at_or_below(p.sequences, slot, lane, [&](int i) {
     return static_cast<long long>(offset_at(p.offsets, i, p.T) / kSlotTokens) + i;
   });
   int t0 = 0, t1 = 0;
@@ -335,7 +320,7 @@ balance_backward(const BalanceParams p, const int32_t* __restrict__ counts, cons
   }
   int q = 0;
   if (p.offsets != nullptr) {
-    q = last_at_or_below(p.sequences, t, lane, [&](int i) { return static_cast<long long>(offset_at(p.offsets, i, p.T)); });
+    q = moe::last_at_or_below(p.sequences, t, lane, [&](int i) { return static_cast<long long>(offset_at(p.offsets, i, p.T)); });
     if (q < 0 || t >= offset_at(p.offsets, q + 1, p.T)) q = -1;
   }
   if (p.mask != nullptr && p.mask[t] == 0) q = -1;
