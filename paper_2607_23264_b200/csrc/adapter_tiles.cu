@@ -1,17 +1,17 @@
 // Adapters over long segments: tiles of up to 128 rows of one segment on the tensor cores, both products in one launch.
 //
 // A cluster of up to eight CTAs takes a tile.  First t = x a^T: each CTA has a part of K, x and a come through a TMA ring of 64-deep
-// stages, and the cluster adds its parts in order through distributed shared memory, scales them and cuts them into two bf16
-// terms (16 bits: the error of one term would be that of the output's rounding).  Then y += t b^T: each CTA has a range of
-// columns, the terms of t stay in shared memory as the A operand, y and b come through TMA rings in tiles of 64 columns, the sum
-// is formed in y's place in shared memory and leaves by TMA.
+// stages; every CTA sends the others their rows of its sums through distributed shared memory, adds the parts of its own rows
+// in order, scales them and sends them on as two bf16 terms (16 bits: the error of one term would be that of the output's
+// rounding).  Then y += t b^T: each CTA has a range of columns, the terms of t lie in shared memory as the A operand, y and b come
+// through TMA rings in tiles of 64 columns, the sum is formed in y's place in shared memory and leaves by TMA.
 //
 // A tile begins where its segment does or 128 rows later: a TMA box may start at any row.  What a box brings of the rows behind
 // the segment's last is computed and not used; tiles of up to 16 rows use boxes of 16.  Segment s has the clusters from
 // offsets[s] / 128 + s on, so no list of tiles is built; the rows behind the last segment are one more segment without an adapter.
 //
-// Warp 0 loads, warp 1 issues the products, warps 2-5 move between accumulator and shared memory; y is on its way while the
-// parts of t are added.
+// Warp 0 loads, warp 1 issues the products, warps 2-5 move between accumulator and shared memory; the first of y and b are on
+// their way while the parts of t are added.
 #include "adapters.cuh"
 #include "ptx_sm100.cuh"
 #include "warp_search.cuh"
@@ -34,32 +34,35 @@ constexpr int kAtomA = kTileRows * 128;   // 64 ranks of one term of t
 constexpr int kAtomB = kBN * 128;         // 64 ranks of b
 constexpr int kYStages = 3, kBStages = 3;
 constexpr int kMaxCluster = 8;
+constexpr int kSumRows = 136;             // a share of the rows from each CTA, rounded up: c ceil(128 / c) for c <= 8
 
 struct Barriers {
   uint64_t full[kMaxStages], empty[kMaxStages], y_full[kYStages], b_full[kBStages], b_empty[kBStages], acc_full[2], acc_empty[2],
-      sums_full, t_full;
+      sums_full;
   uint32_t tmem;
   int abort_flag;
 };
 
-// Shared memory of a CTA, from a 1024-byte boundary on: in the second phase the terms of t, y's ring and b's ring; in the
-// first the ring of x and a from the start, and the exchanged sums at the end.
+// Shared memory of a CTA, from a 1024-byte boundary on: in the second phase the terms of t, b's ring and y's ring; in the first
+// the ring of x and a from the start, and behind it the sums that the cluster sends, in the place of y's last tiles.
 struct Layout {
-  int atoms, rank16, stage_bytes, stages, y_at, b_at, sums_at, bytes;
+  int atoms, rank16, pitch, stage_bytes, stages, b_at, y_at, sums_at, bytes;
   __host__ __device__ explicit Layout(int rank) {
     atoms = (rank + 63) / 64;
     rank16 = (rank + 15) / 16 * 16;
-    y_at = 2 * atoms * kAtomA;
-    b_at = y_at + kYStages * kYBytes;
-    bytes = b_at + kBStages * atoms * kAtomB;              // 104 KiB: two CTAs on an SM; 160 above 64 ranks
+    pitch = rank + 4;                                      // floats of a row of sums: an odd number of 16 bytes
+    b_at = 2 * atoms * kAtomA;
+    y_at = b_at + kBStages * atoms * kAtomB;
+    const int sums = kSumRows * pitch * 4;
+    bytes = y_at + kYBytes + (sums > (kYStages - 1) * kYBytes ? sums : (kYStages - 1) * kYBytes);
+    sums_at = bytes - sums;
     stage_bytes = kXBytes + rank16 * 128;
-    stages = bytes / stage_bytes < kMaxStages ? bytes / stage_bytes : kMaxStages;
-    sums_at = bytes - kTileRows * (rank + 4) * 4;
+    stages = sums_at / stage_bytes < kMaxStages ? sums_at / stage_bytes : kMaxStages;
   }
 };
 
 struct Maps {
-  CUtensorMap x, x_short, a, t, b, in, in_short, out;
+  CUtensorMap x, x_short, a, b, in, in_short, out;
 };
 
 __device__ __forceinline__ void timed_out(const AdapterParams& p, int where) {
@@ -91,6 +94,11 @@ __device__ __forceinline__ uint32_t add_pair(uint32_t y, uint32_t d0, uint32_t d
   return pair(low(y) + __uint_as_float(d0), high(y) + __uint_as_float(d1));
 }
 
+// 16 bytes into the shared memory of any CTA of the cluster.
+__device__ __forceinline__ void st_cluster(uint32_t at, const uint4& v) {
+  asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
 // The four epilogue warps meet; whether any of them has given up.
 __device__ __forceinline__ bool epilogue_meets(bool gave_up) {
   uint32_t any;
@@ -115,6 +123,10 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3;
   const int tile = blockIdx.x / cluster, part = blockIdx.x - tile * cluster;
 
+  if (threadIdx.x == 0) {
+    ptx::prefetch_tensormap(&maps.x);
+    ptx::prefetch_tensormap(&maps.a);
+  }
   // the tile's segment, rows and adapter: each warp finds them by itself
   auto bound = [&](int s) {
     const long long o = __ldg(p.offsets + s);
@@ -167,7 +179,6 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
       ptx::mbar_init(ptx::smem_u32(&bar.acc_empty[i]), 4);
     }
     ptx::mbar_init(ptx::smem_u32(&bar.sums_full), 1);
-    ptx::mbar_init(ptx::smem_u32(&bar.t_full), 1);
     bar.abort_flag = 0;
     ptx::fence_barrier_init();
   }
@@ -177,20 +188,28 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
     ptx::tc_fence_before_sync();
   }
   __syncthreads();
+  if (has) ptx::cluster_arrive();                          // (waited for before anything is sent: every CTA has begun)
   ptx::tc_fence_after_sync();
   const uint32_t tmem = bar.tmem, lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
   volatile int* abort_flag = &bar.abort_flag;
   const int r = quarter * 32 + lane;                       // the row of an epilogue thread
-  int y_issued = 0;                                        // (warp 0's lane 0)
+  int y_issued = 0, b_issued = 0;                          // (warp 0's lane 0)
   auto load_y = [&](int slot, int n) {
     const uint32_t full = ptx::smem_u32(&bar.y_full[slot]);
     ptx::mbar_expect_tx(full, tile_bytes);
     ptx::tma_load_2d(base_at + lay.y_at + slot * kYBytes, tm_in, full, n * kBN, static_cast<int>(row0));
   };
 
+  auto load_b = [&](int slot, int n) {
+    const uint32_t full = ptx::smem_u32(&bar.b_full[slot]);
+    ptx::mbar_expect_tx(full, lay.atoms * kAtomB);
+    for (int k = 0; k < lay.atoms; ++k)
+      ptx::tma_load_2d(base_at + lay.b_at + (slot * lay.atoms + k) * kAtomB, &maps.b, full, k * 64, id * p.N + n * kBN);
+  };
+
   // ------------------------------------------------------------------------------------------------ t = x a^T
   if (has) {
-    const int pitch = p.rank + 4;                          // floats of a row of sums: an odd number of 16 bytes
+    const int share = (m + cluster - 1) / cluster;         // rows of a CTA, at most
     if (warp == 0) {
       if (lane == 0 && sums) {
         int stage = 0;
@@ -208,11 +227,14 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
         ok = ok && ptx::mbar_wait(ptx::smem_u32(&bar.sums_full), 0, abort_flag);
         if (!ok) timed_out(p, 1);
       }
-      // nothing reads the ring any more: y's tiles in front of the sums may come
-      if (lane == 0 && !*abort_flag)
+      // nothing reads the ring any more: b, and y's tiles in front of the sums, may come
+      if (lane == 0 && !*abort_flag) {
+        for (; b_issued < min(kBStages, n1 - n0); ++b_issued) load_b(b_issued, n0 + b_issued);
         for (; y_issued < y_ahead && lay.y_at + (y_issued + 1) * kYBytes <= lay.sums_at; ++y_issued)
           load_y(y_issued, n0 + y_issued);
+      }
       __syncwarp();
+      ptx::cluster_wait();
     } else if (warp == 1) {
       if (lane == 0 && sums) {
         const uint32_t idesc = ptx::idesc_bf16_f32(kTileRows, lay.rank16);
@@ -234,60 +256,67 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
         else timed_out(p, 2);
       }
       __syncwarp();
-    } else if (sums) {
-      if (!__all_sync(kFull, ptx::mbar_wait(ptx::smem_u32(&bar.sums_full), 0, abort_flag))) {
-        if (lane == 0) timed_out(p, 3);
-      } else if (quarter * 32 < m) {
+      ptx::cluster_wait();
+    } else {
+      const bool ok = !sums || __all_sync(kFull, ptx::mbar_wait(ptx::smem_u32(&bar.sums_full), 0, abort_flag));
+      __syncwarp();
+      ptx::cluster_wait();
+      if (!ok && lane == 0) timed_out(p, 3);
+      if (ok && sums && quarter * 32 < m) {
         ptx::tc_fence_after_sync();
-        float* dst = reinterpret_cast<float*>(base + lay.sums_at) + r * pitch;
+        // row r goes to the CTA in whose share it lies: the last q with m q / cluster <= r
+        const int owner = ((r + 1) * cluster + m - 1) / m - 1, first = m * owner / cluster;
+        const uint32_t dst = ptx::map_to_cta(base_at + lay.sums_at + (part * share + r - first) * lay.pitch * 4, min(owner, cluster - 1));
         for (int j = 0; j < p.rank; j += 16) {
           uint32_t v[16];
           ptx::tmem_ld_32x16(lanes + j, v);
           ptx::tmem_ld_wait();
+          if (r < m) {
 #pragma unroll
-          for (int q = 0; q < 16; q += 4)
-            if (q < 8 || j + 8 < p.rank)
-              *reinterpret_cast<uint4*>(dst + j + q) = make_uint4(v[q], v[q + 1], v[q + 2], v[q + 3]);
+            for (int q = 0; q < 16; q += 4)
+              if (q < 8 || j + 8 < p.rank) st_cluster(dst + (j + q) * 4, make_uint4(v[q], v[q + 1], v[q + 2], v[q + 3]));
+          }
         }
         ptx::tc_fence_before_sync();
       }
     }
-    // the cluster's sums over its parts of K in order, a share of the rows per CTA
+    __syncwarp();
     ptx::cluster_sync();
     ptx::tc_fence_after_sync();
+    // this CTA's rows: the parts of K in order, and the terms to every CTA; eight ranks a step
     const float f = p.scale != nullptr ? __ldg(p.scale + id) : 1.f;
-    const int r0 = m * part / cluster, r1 = m * (part + 1) / cluster, chunks = p.rank / 8;
+    const int r0 = m * part / cluster, r1 = m * (part + 1) / cluster, chunks = lay.rank16 / 8;
     for (int i = threadIdx.x; i < (r1 - r0) * chunks; i += kThreads) {
-      const int row = r0 + i / chunks, j = 8 * (i % chunks);
-      const uint32_t at = base_at + lay.sums_at + (row * pitch + j) * 4;
-      float4 a[kMaxCluster], b[kMaxCluster];
+      const int local = i / chunks, row = r0 + local, j = i - local * chunks;
+      uint4 hi = make_uint4(0u, 0u, 0u, 0u), lo = hi;      // (up to whole steps of the product: zeros)
+      if (8 * j < p.rank) {
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        const float* src = reinterpret_cast<const float*>(base + lay.sums_at) + local * lay.pitch + 8 * j;
 #pragma unroll
-      for (int s = 0; s < kMaxCluster; ++s) {
-        if (s < parts) {
-          const uint32_t from = ptx::map_to_cta(at, s);
-          a[s] = ptx::ld_cluster_f4(from);
-          b[s] = ptx::ld_cluster_f4(from + 16);
+        for (int s = 0; s < kMaxCluster; ++s) {
+          if (s < parts) {
+            const float4 a = *reinterpret_cast<const float4*>(src + s * share * lay.pitch);
+            const float4 b = *reinterpret_cast<const float4*>(src + s * share * lay.pitch + 4);
+            v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
+            v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+          }
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] *= f;
+        two_terms(v, hi, lo);
+      }
+      const uint32_t at = base_at + (j >> 3) * kAtomA + row * 128 + (((j & 7) ^ (row & 7)) << 4);
+#pragma unroll
+      for (int q = 0; q < kMaxCluster; ++q) {
+        if (q < cluster) {
+          const uint32_t to = ptx::map_to_cta(at, q);
+          st_cluster(to, hi);
+          st_cluster(to + lay.atoms * kAtomA, lo);
         }
       }
-      float v[8] = {a[0].x, a[0].y, a[0].z, a[0].w, b[0].x, b[0].y, b[0].z, b[0].w};
-#pragma unroll
-      for (int s = 1; s < kMaxCluster; ++s) {
-        if (s < parts) {
-          v[0] += a[s].x; v[1] += a[s].y; v[2] += a[s].z; v[3] += a[s].w;
-          v[4] += b[s].x; v[5] += b[s].y; v[6] += b[s].z; v[7] += b[s].w;
-        }
-      }
-#pragma unroll
-      for (int q = 0; q < 8; ++q) v[q] *= f;
-      uint4 hi, lo;
-      two_terms(v, hi, lo);
-      __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(p.t) + (row0 + row) * p.rank + j;
-      *reinterpret_cast<uint4*>(to) = hi;
-      *reinterpret_cast<uint4*>(to + static_cast<size_t>(p.rows) * p.rank) = lo;
     }
-    // t is read by TMA in every CTA of the cluster, and the sums' place belongs to TMA again
+    // the terms are read by the products, and the sums' place belongs to TMA again
     __syncwarp();
-    __threadfence();
     ptx::fence_proxy_async_all();
     ptx::cluster_sync();
   }
@@ -296,24 +325,15 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
   if (warp == 0) {
     if (lane == 0) {
       bool ok = true;
-      if (has) {
-        ptx::fence_proxy_async_all();
-        ptx::mbar_expect_tx(ptx::smem_u32(&bar.t_full), 2 * lay.atoms * kAtomA);
-        for (int term = 0; term < 2; ++term)
-          for (int k = 0; k < lay.atoms; ++k)
-            ptx::tma_load_2d(base_at + (term * lay.atoms + k) * kAtomA, &maps.t, ptx::smem_u32(&bar.t_full), k * 64,
-                             static_cast<int>(term * p.rows + row0));
-      }
       for (; y_issued < y_ahead; ++y_issued) load_y(y_issued, n0 + y_issued);
       int bs = 0;
       uint32_t b_phase = 1;
       for (int i = n0; i < n1 && has; ++i) {
-        ok = ptx::mbar_wait(ptx::smem_u32(&bar.b_empty[bs]), b_phase, abort_flag);
-        if (!ok) break;
-        const uint32_t full = ptx::smem_u32(&bar.b_full[bs]);
-        ptx::mbar_expect_tx(full, lay.atoms * kAtomB);
-        for (int k = 0; k < lay.atoms; ++k)
-          ptx::tma_load_2d(base_at + lay.b_at + (bs * lay.atoms + k) * kAtomB, &maps.b, full, k * 64, id * p.N + i * kBN);
+        if (i - n0 >= b_issued) {
+          ok = ptx::mbar_wait(ptx::smem_u32(&bar.b_empty[bs]), b_phase, abort_flag);
+          if (!ok) break;
+          load_b(bs, i);
+        }
         if (++bs == kBStages) { bs = 0; b_phase ^= 1u; }
       }
       if (!ok) timed_out(p, 4);
@@ -324,8 +344,8 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
       const uint32_t idesc = ptx::idesc_bf16_f32(kTileRows, kBN);
       int bs = 0, acc = 0;
       uint32_t b_phase = 0, acc_phase = 1;
-      // (also where this CTA has no columns: what it asked for lands)
-      bool ok = ptx::mbar_wait(ptx::smem_u32(&bar.t_full), 0, abort_flag);
+      bool ok = true;
+      ptx::fence_proxy_async_all();
       for (int i = n0; i < n1 && ok; ++i) {
         ok = ptx::mbar_wait(ptx::smem_u32(&bar.b_full[bs]), b_phase, abort_flag) &&
              ptx::mbar_wait(ptx::smem_u32(&bar.acc_empty[acc]), acc_phase, abort_flag);
@@ -356,27 +376,30 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
       unsigned char* row = base + lay.y_at + ys * kYBytes + r * 128;
       if (ok && live && (has || !whole)) {
         ptx::tc_fence_after_sync();
-        __nv_bfloat16* out = p.y_out + static_cast<size_t>(row0 + r) * p.N + i * kBN;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
+        for (int half = 0; half < 2 && has; ++half) {
           uint32_t v[32];
-          if (has) {
-            ptx::tmem_ld_32x32(lanes + acc * kBN + half * 32, v);
-            ptx::tmem_ld_wait();
-          }
+          ptx::tmem_ld_32x32(lanes + acc * kBN + half * 32, v);
+          ptx::tmem_ld_wait();
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             uint4* at = reinterpret_cast<uint4*>(row + (((half * 4 + c) ^ (r & 7)) << 4));
             uint4 y = *at;
-            if (has) {
-              y.x = add_pair(y.x, v[8 * c], v[8 * c + 1]);
-              y.y = add_pair(y.y, v[8 * c + 2], v[8 * c + 3]);
-              y.z = add_pair(y.z, v[8 * c + 4], v[8 * c + 5]);
-              y.w = add_pair(y.w, v[8 * c + 6], v[8 * c + 7]);
-            }
-            // a whole tile leaves by TMA, the rows of another one by themselves
-            if (whole) *at = y;
-            else if (r < m && i * kBN + half * 32 + c * 8 < p.N) *reinterpret_cast<uint4*>(out + half * 32 + c * 8) = y;
+            y.x = add_pair(y.x, v[8 * c], v[8 * c + 1]);
+            y.y = add_pair(y.y, v[8 * c + 2], v[8 * c + 3]);
+            y.z = add_pair(y.z, v[8 * c + 4], v[8 * c + 5]);
+            y.w = add_pair(y.w, v[8 * c + 6], v[8 * c + 7]);
+            *at = y;
+          }
+        }
+        if (!whole) {                                      // a whole tile leaves by TMA, the rows of another one from here
+          __syncwarp();
+#pragma unroll
+          for (int it = 0; it < 8; ++it) {
+            const int rr = quarter * 32 + it * 4 + (lane >> 3), c = lane & 7;
+            if (rr < m && i * kBN + 8 * c < p.N)
+              *reinterpret_cast<uint4*>(p.y_out + static_cast<size_t>(row0 + rr) * p.N + i * kBN + 8 * c) =
+                  *reinterpret_cast<const uint4*>(base + lay.y_at + ys * kYBytes + rr * 128 + ((c ^ (rr & 7)) << 4));
           }
         }
         ptx::tc_fence_before_sync();
@@ -442,14 +465,11 @@ int cluster_of(const moe_ctx* ctx, long long tiles, int rank, int N, int K) {
 
 namespace moe {
 
-size_t adapter_tile_scratch_bytes(long long rows, int rank) { return static_cast<size_t>(rows) * rank * 4; }
-
 moe_status launch_adapter_tiles(moe_ctx* ctx, const AdapterParams& p, cudaStream_t stream) {
   Maps m;
   const uint64_t factor_rows = static_cast<uint64_t>(p.adapters) * p.rank, out_rows = static_cast<uint64_t>(p.adapters) * p.N;
   if (!encode(ctx, &m.x, p.x, p.rows, p.K, kTileRows) || !encode(ctx, &m.x_short, p.x, p.rows, p.K, kShortRows) ||
       !encode(ctx, &m.a, p.a, factor_rows, p.K, Layout(p.rank).rank16) ||
-      !encode(ctx, &m.t, p.t, 2 * static_cast<uint64_t>(p.rows), p.rank, kTileRows) ||
       !encode(ctx, &m.b, p.b, out_rows, p.rank, kBN) || !encode(ctx, &m.in, p.y_in, p.rows, p.N, kTileRows) ||
       !encode(ctx, &m.in_short, p.y_in, p.rows, p.N, kShortRows) || !encode(ctx, &m.out, p.y_out, p.rows, p.N, kTileRows))
     return MOE_ERR_CUDA;

@@ -148,9 +148,7 @@ int splits_of(const moe_ctx* ctx, long long rows, int K) {
 namespace moe {
 
 size_t adapter_scratch_bytes(const moe_ctx* ctx, long long rows, int K, int rank) {
-  const size_t a = static_cast<size_t>(splits_of(ctx, rows, K)) * static_cast<size_t>(rows) * rank * 4;
-  const size_t b = adapter_tile_scratch_bytes(rows, rank);
-  return a > b ? a : b;
+  return static_cast<size_t>(splits_of(ctx, rows, K)) * static_cast<size_t>(rows) * rank * 4;
 }
 
 moe_status launch_add_adapters(moe_ctx* ctx, const moe_adapter_args& a, cudaStream_t stream) {

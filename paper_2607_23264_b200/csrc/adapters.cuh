@@ -48,7 +48,6 @@ __device__ __forceinline__ int adapter_of_row(const AdapterParams& p, const int3
 }
 
 // Long segments: tiles of 128 rows on the tensor cores.
-size_t adapter_tile_scratch_bytes(long long rows, int rank);
 moe_status launch_adapter_tiles(moe_ctx* ctx, const AdapterParams& p, cudaStream_t stream);
 
 }  // namespace moe

@@ -275,6 +275,9 @@ __device__ __forceinline__ uint32_t map_to_cta(uint32_t smem_addr, uint32_t rank
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// Its halves: every thread arrives, does something else, and waits before the next arrival.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 // 32-bit load from the shared memory of any CTA of the cluster (shared::cluster address from map_to_cta); volatile:
 // used to poll a word the other CTA keeps writing
 __device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t cluster_addr) {
