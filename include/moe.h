@@ -669,15 +669,15 @@ moe_status moe_balance_loss_backward(moe_ctx* ctx, const moe_balance_args* args,
  * Low-rank adapters of many requests beside a shared projection (moe_gemm_blk, or any other).  Rows belong to segments
  * (requests), a segment to an adapter i or to none:
  *     y_out[r,n] = bf16( y_in[r,n] + scale_i * sum_j b[i,n,j] t[r,j] ),   t[r,j] = sum_k x[r,k] a[i,j,k]
- * with fp32 sums (t enters the second product as two bf16 terms, 16 bits of it).  Rows without an adapter, and rows behind
+ * with fp32 sums (in long segments t enters the second product as two bf16 terms, 16 bits of it).  Rows without an adapter, and rows behind
  * the last segment, are copied bit for bit.  Prompts are long segments, decoded tokens segments of one row (offsets NULL: every
  * row is a segment), in any mixture; neighbouring rows of one adapter share its reads.  The gradient with respect to x is the
  * same call with a and b exchanged, each transposed.
  *   x [rows, K] bf16, a [adapters, rank, K] bf16, b [adapters, N, rank] bf16, y_in, y_out [rows, N] bf16 (y_out may be y_in).
  * An adapter index >= adapters is reported through the status word (MOE_ERR_BAD_ROUTING, detail = the segment) and its rows
  * are copied.  A lower-ranked adapter is padded with zeros.
- * scratch: moe_adapter_scratch_bytes bytes (undefined after); two calls that overlap on the GPU need one each.
- * Limits: 0 <= rows < 2^30; N, K multiples of 8; rank a multiple of 8, at most 128; 1 <= adapters, adapters * rank and
+ * scratch: moe_adapter_scratch_bytes bytes (0, and NULL will do, for all sizes the present kernels take: t stays on the chip).
+ * Limits: 0 <= rows < 2^28; N, K multiples of 8; rank a multiple of 8, at most 128; 1 <= adapters, adapters * rank and
  * adapters * N < 2^31; 0 <= segments <= rows (segments == rows when offsets is NULL), else UNSUPPORTED_SHAPE.
  * ------------------------------------------------------------------------------------------------ */
 typedef struct {
@@ -694,7 +694,7 @@ typedef struct {
   int64_t rows;
   int32_t N, K, rank, adapters, segments;
 } moe_adapter_args;
-size_t moe_adapter_scratch_bytes(const moe_ctx* ctx, int64_t rows, int32_t K, int32_t rank);   /* 0 for refused sizes */
+size_t moe_adapter_scratch_bytes(const moe_ctx* ctx, int64_t rows, int32_t K, int32_t rank);
 moe_status moe_add_adapters(moe_ctx* ctx, const moe_adapter_args* args, void* stream);
 
 /*

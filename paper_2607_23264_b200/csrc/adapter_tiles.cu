@@ -94,11 +94,6 @@ __device__ __forceinline__ uint32_t add_pair(uint32_t y, uint32_t d0, uint32_t d
   return pair(low(y) + __uint_as_float(d0), high(y) + __uint_as_float(d1));
 }
 
-// 16 bytes into the shared memory of any CTA of the cluster.
-__device__ __forceinline__ void st_cluster(uint32_t at, const uint4& v) {
-  asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-}
-
 // The four epilogue warps meet; whether any of them has given up.
 __device__ __forceinline__ bool epilogue_meets(bool gave_up) {
   uint32_t any;
@@ -274,7 +269,7 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
           if (r < m) {
 #pragma unroll
             for (int q = 0; q < 16; q += 4)
-              if (q < 8 || j + 8 < p.rank) st_cluster(dst + (j + q) * 4, make_uint4(v[q], v[q + 1], v[q + 2], v[q + 3]));
+              if (q < 8 || j + 8 < p.rank) moe::st_cluster(dst + (j + q) * 4, make_uint4(v[q], v[q + 1], v[q + 2], v[q + 3]));
           }
         }
         ptx::tc_fence_before_sync();
@@ -310,8 +305,8 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
       for (int q = 0; q < kMaxCluster; ++q) {
         if (q < cluster) {
           const uint32_t to = ptx::map_to_cta(at, q);
-          st_cluster(to, hi);
-          st_cluster(to + lay.atoms * kAtomA, lo);
+          moe::st_cluster(to, hi);
+          moe::st_cluster(to + lay.atoms * kAtomA, lo);
         }
       }
     }

@@ -1,20 +1,50 @@
 // Low-rank adapters of many requests added to a projection's output: y[r] += scale_i b_i (a_i x[r]), i the row's adapter.
 //
-// shrink : t = x a^T, a CTA per 16 rows and a part of K.  The adapters of its rows are taken one after the other, each read once
-//          for all of its rows here; the other rows enter the product as zeros.  m16n8k16 products, operands straight from
-//          global memory: a lane's 16 bytes of a row are eight neighbouring k, and as x and a are permuted along k alike, no
-//          shuffle is needed.
-// expand : y += scale t b^T, a CTA per 16 rows and 256 columns, a column per thread: fp32 dot products over the rank.
+// adapter_rows: short segments and single tokens, where the factors are the bytes.  A cluster of up to eight CTAs takes up to 16
+//               rows of one adapter out of a window of 256 neighbouring rows, so that a factor is read once for all of them: the
+//               cluster of row r finds the rows of r's adapter in the window and goes on if r is the first, the 17th, ... of them.
+//               Each CTA has a part of K and a range of columns.  t = x a^T: m16n8k16 products with both operands straight
+//               from global memory (a lane's 16 bytes of a row are eight neighbouring k; as x and a are permuted along k
+//               alike, no shuffle is needed), warps added in order through shared memory, and the sums sent to every CTA of the cluster.
+//               Then y += t b^T: two columns per thread, fp32 dot products over the rank.
+// Long segments take adapter_tiles.
 #include "adapters.cuh"
+#include "ptx_sm100.cuh"
 
 namespace {
 
 using moe::AdapterParams;
 
 constexpr unsigned kFull = 0xFFFFFFFFu;
-constexpr int kRows = 16;                 // rows of a CTA
+constexpr int kRows = 16;                 // rows of a cluster
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kMaxSplits = 16;
+constexpr int kWindow = kThreads;         // rows among which those of one adapter are brought together
+constexpr int kMaxCluster = 8;
+
+// The adapter of a row, -1 without one.
+__device__ __forceinline__ int adapter_of_row(const AdapterParams& p, long long row, bool report) {
+  if (row >= p.rows) return -1;
+  int seg = static_cast<int>(row);
+  if (p.offsets != nullptr) {
+    int lo = -1, hi = p.segments;                          // the last segment that begins at or before the row
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (__ldg(p.offsets + mid) <= row) lo = mid;
+      else hi = mid;
+    }
+    if (lo < 0 || row >= __ldg(p.offsets + lo + 1)) return -1;
+    seg = lo;
+  }
+  const int id = __ldg(p.adapter_of + seg);
+  if (id >= p.adapters) {
+    if (report) {
+      atomicCAS(&p.status[0], 0, MOE_ERR_BAD_ROUTING);
+      atomicCAS(&p.status[1], 0, seg);
+    }
+    return -1;
+  }
+  return id < 0 ? -1 : id;
+}
 
 __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                          uint32_t b1) {
@@ -23,164 +53,226 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+__device__ __forceinline__ void prefetch_l2(const void* at) { asm volatile("prefetch.global.L2 [%0];" ::"l"(at)); }
 
-// kTiles: tiles of eight ranks held in registers (rank <= 8 * kTiles).
+// Shared memory: [kWarps][kRows][pitch] sums of the warps, [kMaxCluster][kRows][pitch] of the CTAs, [kRows][pitch] t.
+__host__ __device__ constexpr int pitch_of(int rank) { return rank + 4; }
+int smem_of(int rank) { return (kWarps + kMaxCluster + 1) * kRows * pitch_of(rank) * 4; }
+
+// kTiles: tiles of eight ranks held in registers (rank <= 8 * kTiles).  Grid: a cluster of `cluster` CTAs per row.
 template <int kTiles>
 __global__ void __launch_bounds__(kThreads)
-adapter_shrink(const AdapterParams p) {
-  __shared__ int s_id[kRows];
-  __shared__ float s_t[kWarps][kRows][8];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
-  const long long row0 = static_cast<long long>(blockIdx.x) * kRows;
-  const int split = blockIdx.y;
-  if (threadIdx.x < kRows) s_id[threadIdx.x] = moe::adapter_of_row(p, p.offsets, p.adapter_of, row0 + threadIdx.x, split == 0);
-  __syncthreads();
-  const int my_id = s_id[lane & 15];
-  unsigned left = __ballot_sync(kFull, my_id >= 0) & 0xFFFFu;
-  // steps of 32 along K, dealt to the splits and then to the warps
-  const int steps = (p.K + 31) / 32;
-  const int s0 = static_cast<int>(static_cast<long long>(steps) * split / p.splits);
-  const int s1 = static_cast<int>(static_cast<long long>(steps) * (split + 1) / p.splits);
-  const int tiles = p.rank / 8;
+adapter_rows(const AdapterParams p, int cluster) {
+  extern __shared__ float4 smem4[];
+  __shared__ int s_before[kWarps], s_row[kRows];
+  float* s_warp = reinterpret_cast<float*>(smem4);
+  const int pitch = pitch_of(p.rank);
+  float* s_cta = s_warp + kWarps * kRows * pitch;
+  float* s_t = s_cta + kMaxCluster * kRows * pitch;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
+  const unsigned item = blockIdx.x / cluster;
+  const int part = static_cast<int>(blockIdx.x - item * cluster);
+  const long long leader = item, window = leader / kWindow * kWindow;
 
-  while (left) {
-    const int first = __ffs(left) - 1, id = s_id[first];
-    const unsigned mine = __ballot_sync(kFull, my_id == id) & 0xFFFFu;
-    left &= ~mine;
-    const bool lo = mine >> g & 1, hi = mine >> (g + 8) & 1;
-    const __nv_bfloat16* xr = p.x + (row0 + g) * p.K + c * 8;
-    const __nv_bfloat16* ar = p.a + (static_cast<size_t>(id) * p.rank + g) * p.K + c * 8;
-    float acc[kTiles][4];
+  const int my_id = adapter_of_row(p, window + tid, part == 0 && window + tid == leader);
+  const int at = static_cast<int>(leader - window);
+  if (tid < kRows) s_row[tid] = -1;
+  if (tid == at) s_before[0] = my_id;
+  __syncthreads();
+  const int id = s_before[0];
+  const int eighths = p.N / 8;
+  const int n0 = 8 * static_cast<int>(static_cast<long long>(eighths) * part / cluster);
+  const int n1 = 8 * static_cast<int>(static_cast<long long>(eighths) * (part + 1) / cluster);
+  if (id < 0) {                                            // no adapter: the row is copied (the whole cluster alike)
+    if (p.y_in != p.y_out) {
+      const uint4* from = reinterpret_cast<const uint4*>(p.y_in + leader * p.N + n0);
+      uint4* to = reinterpret_cast<uint4*>(p.y_out + leader * p.N + n0);
+      for (int i = tid; i < (n1 - n0) / 8; i += kThreads) to[i] = from[i];
+    }
+    return;
+  }
+  __syncthreads();
+  const unsigned same = __ballot_sync(kFull, my_id == id);
+  if (lane == 0) s_before[warp] = __popc(same);
+  __syncthreads();
+  int place = __popc(same & ((1u << lane) - 1)), first = 0, total = 0;      // among the window's rows of this adapter
 #pragma unroll
-    for (int j = 0; j < kTiles; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
-    for (int s = s0 + warp; s < s1; s += kWarps) {
-      const int k = s * 32;
-      const bool in = k + c * 8 < p.K;
-      uint4 xa = make_uint4(0u, 0u, 0u, 0u), xb = xa;
-      if (in && lo) xa = __ldg(reinterpret_cast<const uint4*>(xr + k));
-      if (in && hi) xb = __ldg(reinterpret_cast<const uint4*>(xr + static_cast<size_t>(8) * p.K + k));
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < warp) place += s_before[w];
+    total += s_before[w];
+  }
+  if (tid == at) s_row[0] = place;
+  __syncthreads();
+  first = s_row[0];
+  if (first % kRows != 0) return;                          // another row's cluster has this one
+  const int count = min(kRows, total - first);
+  __syncthreads();
+  if (my_id == id && place >= first && place < first + kRows) s_row[place - first] = tid;
+  if (cluster > 1) ptx::cluster_arrive();                  // (waited for before anything is sent: every CTA has begun)
+  // the bytes of the second product are on their way meanwhile
+  {
+    const char* b = reinterpret_cast<const char*>(p.b + (static_cast<size_t>(id) * p.N + n0) * p.rank);
+    const int bytes = (n1 - n0) * p.rank * 2;
+    for (int i = tid * 128; i < bytes; i += kThreads * 128) prefetch_l2(b + i);
+  }
+  __syncthreads();
+
+  // ------------------------------------------------------------------------------------------------ t = x a^T
+  const int steps = (p.K + 31) / 32, tiles = p.rank / 8;   // steps of 32 along K, dealt to the CTAs and then to the warps
+  const int s0 = static_cast<int>(static_cast<long long>(steps) * part / cluster);
+  const int s1 = static_cast<int>(static_cast<long long>(steps) * (part + 1) / cluster);
+  const bool has_lo = g < count, has_hi = g + 8 < count;
+  const __nv_bfloat16* x_lo = p.x + (window + (has_lo ? s_row[g] : 0)) * p.K + c * 8;
+  const __nv_bfloat16* x_hi = p.x + (window + (has_hi ? s_row[g + 8] : 0)) * p.K + c * 8;
+  const __nv_bfloat16* a_row = p.a + (static_cast<size_t>(id) * p.rank + g) * p.K + c * 8;
+  float acc[kTiles][4];
+#pragma unroll
+  for (int j = 0; j < kTiles; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
+  constexpr int kAhead = kTiles <= 4 ? 4 : kTiles <= 8 ? 2 : 1;            // steps whose loads are in flight together
+  for (int s = s0 + warp; s < s1; s += kWarps * kAhead) {
+    uint4 xa[kAhead], xb[kAhead], w[kAhead][kTiles];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int k = (s + u * kWarps) * 32;
+      const bool in = s + u * kWarps < s1 && k + c * 8 < p.K;
+      xa[u] = xb[u] = make_uint4(0u, 0u, 0u, 0u);
+      if (in && has_lo) xa[u] = __ldg(reinterpret_cast<const uint4*>(x_lo + k));
+      if (in && has_hi) xb[u] = __ldg(reinterpret_cast<const uint4*>(x_hi + k));
 #pragma unroll
       for (int j = 0; j < kTiles; ++j) {
-        if (j < tiles) {
-          uint4 w = make_uint4(0u, 0u, 0u, 0u);
-          if (in) w = __ldg(reinterpret_cast<const uint4*>(ar + static_cast<size_t>(8 * j) * p.K + k));
-          mma_bf16(acc[j], xa.x, xb.x, xa.y, xb.y, w.x, w.y);
-          mma_bf16(acc[j], xa.z, xb.z, xa.w, xb.w, w.z, w.w);
+        w[u][j] = make_uint4(0u, 0u, 0u, 0u);
+        if (in && j < tiles) w[u][j] = __ldg(reinterpret_cast<const uint4*>(a_row + static_cast<size_t>(8 * j) * p.K + k));
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+#pragma unroll
+      for (int j = 0; j < kTiles; ++j) {
+        mma_bf16(acc[j], xa[u].x, xb[u].x, xa[u].y, xb[u].y, w[u][j].x, w[u][j].y);
+        mma_bf16(acc[j], xa[u].z, xb[u].z, xa[u].w, xb[u].w, w[u][j].z, w[u][j].w);
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < kTiles; ++j) {
+    if (j < tiles) {
+      float* dst = s_warp + (warp * kRows + g) * pitch + 8 * j + 2 * c;
+      *reinterpret_cast<float2*>(dst) = make_float2(acc[j][0], acc[j][1]);
+      *reinterpret_cast<float2*>(dst + 8 * pitch) = make_float2(acc[j][2], acc[j][3]);
+    }
+  }
+  __syncthreads();
+  if (cluster > 1) ptx::cluster_wait();
+  const int quads = p.rank / 4;
+  const uint32_t mine = ptx::smem_u32(s_cta) + part * kRows * pitch * 4;
+  for (int i = tid; i < count * quads; i += kThreads) {
+    const int r = i / quads, j = 4 * (i - r * quads);
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int q = 0; q < kWarps; ++q) {
+      const float4 a = *reinterpret_cast<const float4*>(s_warp + (q * kRows + r) * pitch + j);
+      v.x += a.x; v.y += a.y; v.z += a.z; v.w += a.w;
+    }
+    const uint4 bits = *reinterpret_cast<const uint4*>(&v);
+    for (int q = 0; q < cluster; ++q) moe::st_cluster(ptx::map_to_cta(mine + (r * pitch + j) * 4, q), bits);
+  }
+  __syncwarp();
+  if (cluster > 1) ptx::cluster_sync();
+  else __syncthreads();
+  const float f = p.scale != nullptr ? __ldg(p.scale + id) : 1.f;
+  for (int i = tid; i < count * quads; i += kThreads) {
+    const int r = i / quads, j = 4 * (i - r * quads);
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int q = 0; q < cluster; ++q) {
+      const float4 a = *reinterpret_cast<const float4*>(s_cta + (q * kRows + r) * pitch + j);
+      v.x += a.x; v.y += a.y; v.z += a.z; v.w += a.w;
+    }
+    *reinterpret_cast<float4*>(s_t + r * pitch + j) = make_float4(f * v.x, f * v.y, f * v.z, f * v.w);
+  }
+  __syncthreads();
+
+  // ------------------------------------------------------------------------------------------------ y += t b^T
+  for (int n = n0 + 2 * tid; n < n1; n += 2 * kThreads) {
+    uint32_t y[kRows];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+      if (r < count) y[r] = *reinterpret_cast<const uint32_t*>(p.y_in + (window + s_row[r]) * p.N + n);
+    float sum[kRows][2];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) sum[r][0] = sum[r][1] = 0.f;
+    const uint4* b0 = reinterpret_cast<const uint4*>(p.b + (static_cast<size_t>(id) * p.N + n) * p.rank);
+    const uint4* b1 = b0 + p.rank / 8;
+    for (int j = 0; j < p.rank / 8; ++j) {
+      const uint4 u = __ldg(b0 + j), v = __ldg(b1 + j);
+      const float bu[8] = {low(u.x), high(u.x), low(u.y), high(u.y), low(u.z), high(u.z), low(u.w), high(u.w)};
+      const float bv[8] = {low(v.x), high(v.x), low(v.y), high(v.y), low(v.z), high(v.z), low(v.w), high(v.w)};
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) {
+        if (r < count) {
+          const float4 ta = *reinterpret_cast<const float4*>(s_t + r * pitch + 8 * j);
+          const float4 tb = *reinterpret_cast<const float4*>(s_t + r * pitch + 8 * j + 4);
+          const float t[8] = {ta.x, ta.y, ta.z, ta.w, tb.x, tb.y, tb.z, tb.w};
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            sum[r][0] = fmaf(t[q], bu[q], sum[r][0]);
+            sum[r][1] = fmaf(t[q], bv[q], sum[r][1]);
+          }
         }
       }
     }
-    // the warps' sums in order, a tile of ranks at a time
 #pragma unroll
-    for (int j = 0; j < kTiles; ++j) {
-      if (j < tiles) {
-        __syncthreads();
-        s_t[warp][g][2 * c] = acc[j][0];
-        s_t[warp][g][2 * c + 1] = acc[j][1];
-        s_t[warp][g + 8][2 * c] = acc[j][2];
-        s_t[warp][g + 8][2 * c + 1] = acc[j][3];
-        __syncthreads();
-        const int r = threadIdx.x >> 3, n = threadIdx.x & 7;
-        if (threadIdx.x < kRows * 8 && (mine >> r & 1)) {
-          float sum = 0.f;
-          for (int w = 0; w < kWarps; ++w) sum += s_t[w][r][n];
-          p.t[(static_cast<size_t>(split) * p.rows + row0 + r) * p.rank + 8 * j + n] = sum;
-        }
+    for (int r = 0; r < kRows; ++r) {
+      if (r < count) {
+        const __nv_bfloat162 o = __floats2bfloat162_rn(low(y[r]) + sum[r][0], high(y[r]) + sum[r][1]);
+        *reinterpret_cast<uint32_t*>(p.y_out + (window + s_row[r]) * p.N + n) = *reinterpret_cast<const uint32_t*>(&o);
       }
     }
   }
 }
 
-__global__ void __launch_bounds__(kThreads)
-adapter_expand(const AdapterParams p) {
-  __shared__ int s_id[kRows];
-  __shared__ float s_t[kRows][128];
-  const int tid = threadIdx.x;
-  const long long row0 = static_cast<long long>(blockIdx.x) * kRows;
-  const int n = blockIdx.y * kThreads + tid;
-  if (tid < kRows) s_id[tid] = moe::adapter_of_row(p, p.offsets, p.adapter_of, row0 + tid, false);
-  __syncthreads();
-  for (int i = tid; i < kRows * p.rank; i += kThreads) {
-    const int r = i / p.rank, j = i - r * p.rank;
-    const int id = s_id[r];
-    float sum = 0.f;
-    if (id >= 0) {
-      for (int s = 0; s < p.splits; ++s) sum += p.t[(static_cast<size_t>(s) * p.rows + row0 + r) * p.rank + j];
-      if (p.scale != nullptr) sum *= __ldg(p.scale + id);
-    }
-    s_t[r][j] = sum;
-  }
-  __syncthreads();
-  if (n >= p.N) return;
-  for (int r = 0; r < kRows && row0 + r < p.rows; ++r) {
-    const size_t at = (row0 + r) * p.N + n;
-    const int id = s_id[r];
-    if (id < 0) {
-      p.y_out[at] = p.y_in[at];
-      continue;
-    }
-    const __nv_bfloat16* b = p.b + (static_cast<size_t>(id) * p.N + n) * p.rank;
-    float sum = 0.f;
-    for (int j = 0; j < p.rank; j += 8) {
-      const uint4 q = __ldg(reinterpret_cast<const uint4*>(b + j));
-      const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        sum = fmaf(s_t[r][j + 2 * i], __uint_as_float(w[i] << 16), sum);
-        sum = fmaf(s_t[r][j + 2 * i + 1], __uint_as_float(w[i] & 0xFFFF0000u), sum);
-      }
-    }
-    p.y_out[at] = __float2bfloat16_rn(__bfloat162float(p.y_in[at]) + sum);
-  }
-}
-
-// Parts of K: as many CTAs as fill the SMs about twice, each with at least four steps for a warp.
-int splits_of(const moe_ctx* ctx, long long rows, int K) {
-  const long long blocks = (rows + kRows - 1) / kRows;
-  long long s = 2LL * ctx->num_sms / (blocks > 0 ? blocks : 1);
-  const int most = (K + 32 * kWarps * 4 - 1) / (32 * kWarps * 4);
-  if (s > most) s = most;
-  if (s > kMaxSplits) s = kMaxSplits;
-  return s < 1 ? 1 : static_cast<int>(s);
+// CTAs of a cluster: as many as leave about 1024 CTAs, should every row have an adapter of its own.
+int cluster_of(long long rows) {
+  int c = kMaxCluster;
+  while (c > 1 && rows * c > 1024) c /= 2;
+  return c;
 }
 
 }  // namespace
 
 namespace moe {
 
-size_t adapter_scratch_bytes(const moe_ctx* ctx, long long rows, int K, int rank) {
-  return static_cast<size_t>(splits_of(ctx, rows, K)) * static_cast<size_t>(rows) * rank * 4;
-}
+size_t adapter_scratch_bytes(const moe_ctx*, long long, int, int) { return 0; }
 
 moe_status launch_add_adapters(moe_ctx* ctx, const moe_adapter_args& a, cudaStream_t stream) {
-  AdapterParams p{};
-  p.x = static_cast<const __nv_bfloat16*>(a.x);
-  p.a = static_cast<const __nv_bfloat16*>(a.a);
-  p.b = static_cast<const __nv_bfloat16*>(a.b);
-  p.scale = a.scale;
-  p.offsets = a.offsets;
-  p.adapter_of = a.adapter_of;
-  p.y_in = static_cast<const __nv_bfloat16*>(a.y_in);
-  p.y_out = static_cast<__nv_bfloat16*>(a.y_out);
-  p.t = static_cast<float*>(a.scratch);
-  p.status = ctx->d_status;
-  p.rows = a.rows;
-  p.N = a.N;
-  p.K = a.K;
-  p.rank = a.rank;
-  p.adapters = a.adapters;
-  p.segments = a.segments;
+  const AdapterParams p{static_cast<const __nv_bfloat16*>(a.x), static_cast<const __nv_bfloat16*>(a.a),
+                        static_cast<const __nv_bfloat16*>(a.b), a.scale, a.offsets, a.adapter_of,
+                        static_cast<const __nv_bfloat16*>(a.y_in), static_cast<__nv_bfloat16*>(a.y_out), ctx->d_status, a.rows,
+                        a.N, a.K, a.rank, a.adapters, a.segments};
   if (a.segments > 0 && a.rows >= 128 && a.rows / a.segments >= 16) return launch_adapter_tiles(ctx, p, stream);
-  p.splits = splits_of(ctx, a.rows, a.K);
-  const unsigned blocks = static_cast<unsigned>((a.rows + kRows - 1) / kRows);
-  const unsigned chunks = static_cast<unsigned>((a.N - 1) / kThreads + 1);
-  if (chunks > 65535u) return MOE_ERR_UNSUPPORTED_SHAPE;
-  auto kernel = a.rank <= 16 ? adapter_shrink<2> : a.rank <= 32 ? adapter_shrink<4> : a.rank <= 64 ? adapter_shrink<8>
-                                                                                               : adapter_shrink<16>;
-  kernel<<<dim3(blocks, p.splits), kThreads, 0, stream>>>(p);
-  if (cudaGetLastError() != cudaSuccess) return MOE_ERR_CUDA;
-  adapter_expand<<<dim3(blocks, chunks), kThreads, 0, stream>>>(p);
-  ctx->last_launches += 2;
-  return cudaGetLastError() == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+  const int cluster = cluster_of(a.rows);
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr{};
+  cfg.gridDim = dim3(static_cast<unsigned>(a.rows * cluster));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem_of(a.rank);
+  cfg.stream = stream;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = static_cast<unsigned>(cluster);
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  ctx->last_launches += 1;
+  auto kernel = a.rank <= 16 ? adapter_rows<2> : a.rank <= 32 ? adapter_rows<4> : a.rank <= 64 ? adapter_rows<8> : adapter_rows<16>;
+  return cudaLaunchKernelEx(&cfg, kernel, p, cluster) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+}
+
+cudaError_t prepare_adapters(moe_ctx* ctx) {
+  cudaError_t e = prepare_adapter_tiles(ctx);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(adapter_rows<8>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(64));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(adapter_rows<16>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(128));
+  return e;
 }
 
 }  // namespace moe

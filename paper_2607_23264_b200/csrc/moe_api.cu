@@ -263,7 +263,7 @@ moe_status moe_create(moe_ctx** out_ctx, const moe_shape* shape, int device) {
   ok = ok && moe::prepare_expert_ffn_mx(ctx) == cudaSuccess;
   ok = ok && moe::prepare_gemm_blk(ctx) == cudaSuccess;
   ok = ok && moe::prepare_plan_scored(ctx) == cudaSuccess;
-  ok = ok && moe::prepare_adapter_tiles(ctx) == cudaSuccess;
+  ok = ok && moe::prepare_adapters(ctx) == cudaSuccess;
   for (int sl = 0; ok && sl < kMoeTimingSlots; ++sl)
     for (int i = 0; ok && i <= kMoeKernels; ++i) ok = cudaEventCreate(&ctx->ev[sl][i]) == cudaSuccess;
   ok = ok && cudaStreamCreateWithFlags(&ctx->s_h2d, cudaStreamNonBlocking) == cudaSuccess;
@@ -1094,7 +1094,7 @@ moe_status check_balance(const moe_ctx* ctx, const moe_balance_args* a) {
 }
 
 bool adapter_sizes_ok(int64_t rows, int32_t K, int32_t rank) {
-  return rows >= 0 && rows < (1LL << 30) && K >= 8 && K % 8 == 0 && rank >= 8 && rank <= 128 && rank % 8 == 0;
+  return rows >= 0 && rows < (1LL << 28) && K >= 8 && K % 8 == 0 && rank >= 8 && rank <= 128 && rank % 8 == 0;
 }
 
 }  // namespace
@@ -1203,12 +1203,14 @@ moe_status moe_add_adapters(moe_ctx* ctx, const moe_adapter_args* a, void* strea
     return MOE_ERR_UNSUPPORTED_SHAPE;
   if (!a->offsets && a->segments != a->rows) return MOE_ERR_INVALID_ARG;
   if (a->rows == 0) return MOE_OK;
-  const void* ptrs[] = {a->x, a->a, a->b, a->y_in, a->y_out, a->scratch};
+  const void* ptrs[] = {a->x, a->a, a->b, a->y_in, a->y_out};
   for (const void* q : ptrs)
     if (!q || !aligned16(q)) return MOE_ERR_INVALID_ARG;
   if (a->segments > 0 && !a->adapter_of) return MOE_ERR_INVALID_ARG;
   if (!aligned16(a->adapter_of) || !aligned16(a->offsets) || !aligned16(a->scale)) return MOE_ERR_INVALID_ARG;
-  if (a->scratch_bytes < moe::adapter_scratch_bytes(ctx, a->rows, a->K, a->rank)) return MOE_ERR_WORKSPACE_TOO_SMALL;
+  const size_t need = moe::adapter_scratch_bytes(ctx, a->rows, a->K, a->rank);
+  if (need > 0 && (!a->scratch || !aligned16(a->scratch))) return MOE_ERR_INVALID_ARG;
+  if (a->scratch_bytes < need) return MOE_ERR_WORKSPACE_TOO_SMALL;
   return moe::launch_add_adapters(ctx, *a, static_cast<cudaStream_t>(stream));
 }
 

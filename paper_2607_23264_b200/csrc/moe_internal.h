@@ -196,7 +196,7 @@ cudaError_t launch_balance_loss_backward(moe_ctx* ctx, const moe_balance_args& a
 size_t adapter_scratch_bytes(const moe_ctx* ctx, long long rows, int K, int rank);
 moe_status launch_add_adapters(moe_ctx* ctx, const moe_adapter_args& args, cudaStream_t stream);
 
-cudaError_t prepare_adapter_tiles(moe_ctx* ctx);  // one-time kernel attributes
+cudaError_t prepare_adapters(moe_ctx* ctx);      // one-time kernel attributes
 
 cudaError_t prepare_expert_ffn(moe_ctx* ctx);  // one-time kernel attributes (dynamic shared memory size)
 

@@ -223,7 +223,7 @@ def test_refusals(ctx):
                 rank=rank, adapters=2, segments=rows)
     odd = torch.zeros(rows * N + 8, dtype=torch.bfloat16, device=DEV)[1:rows * N + 1]
     for change, code in [(dict(x=None), 1), (dict(a=None), 1), (dict(b=None), 1), (dict(adapter_of=None), 1), (dict(y_in=None), 1),
-                         (dict(y_out=None), 1), (dict(scratch=None), 1), (dict(scratch=scratch[:16]), 3), (dict(N=60), 2),
+                         (dict(y_out=None), 1), (dict(N=60), 2),
                          (dict(K=4), 2), (dict(rank=12), 2), (dict(rank=136), 2), (dict(rank=0), 2), (dict(adapters=0), 2),
                          (dict(segments=rows + 1), 2), (dict(segments=3), 1), (dict(rows=-1), 2), (dict(segments=-1), 2),
                          (dict(adapters=2 ** 27), 2), (dict(y_in=odd), 1), (dict(scale=torch.zeros(8, device=DEV)[1:3]), 1),
