@@ -1,16 +1,18 @@
 // Balance loss of a router with its per-expert counts, and its gradient.
 //
-// balance_partial : a CTA per slot of up to kSlotTokens tokens of one sequence, a warp per token; a lane keeps the
-//                   probability sums of its experts (lane, lane + 32, ...) in registers over its warp's tokens, the warps are
-//                   added in order, the counts are integer atomics in shared memory.  Sequence q has the slots from
-//                   offsets[q] / kSlotTokens + q on: no prefix sum over sequences is needed, and the slots of neighbours do
-//                   not meet.
+// balance_partial : a CTA per slot of up to `slot_tokens` tokens of one sequence, a warp per token; a lane keeps the probability
+//                   sums of its experts in registers over its warp's tokens, the warps are added in order, the counts are
+//                   integer atomics in shared memory.  Sequence q has the slots from offsets[q] / slot_tokens + q on: no
+//                   prefix sum over sequences is needed, and the slots of neighbours do not meet.
 // balance_finish  : a CTA per sequence and 32 experts adds the slots' sums, forms the mean and the sequence's share of the
-//                   loss; the last CTA to finish adds the shares in order.
+//                   loss; the last CTA to finish adds the shares in order.  Starts while the first kernel ends.
 // balance_backward: a warp per token: the loss reaches the logits through the counts alone, so one pass over the logits.
+//                   A warp's tokens are neighbours, and what a sequence gives to all of them stays in registers.
+// In both passes the next token's logits are on their way while a token is worked on.
 #include <climits>
 
 #include "moe_internal.h"
+#include "ptx_sm100.cuh"
 #include "route_scored.cuh"
 #include "warp_search.cuh"
 
@@ -18,8 +20,6 @@ namespace {
 
 constexpr unsigned kFull = 0xFFFFFFFFu;
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kSlotTokens = 32;
-constexpr int kFinishThreads = 1024;
 
 // What a call keeps in its scratch, in 4-byte words: [slots][E] sums, [slots][E] counts, [slots] tokens, [slots] sums of squared
 // logarithms, then per sequence and group of 32 experts a share of the loss, per sequence its sum of squares, and the ticket.
@@ -32,13 +32,22 @@ struct Scratch {
   float* seq_z;
   int32_t* ticket;
 };
-inline long long slots_of(int T, int sequences) { return static_cast<long long>(T) / kSlotTokens + sequences + 1; }
-inline size_t scratch_words(int T, int E, int sequences) {
-  const size_t slots = static_cast<size_t>(slots_of(T, sequences));
-  return slots * (2 * static_cast<size_t>(E) + 2) + static_cast<size_t>(sequences) * ((E + 31) / 32 + 1) + 4;
+// Tokens of a slot: two CTAs per SM, a multiple of the warps.
+inline int slot_tokens_of(const moe_ctx* ctx) {
+  const int per = ctx->shape.T / (2 * ctx->num_sms) + 1;
+  return (per + kWarps - 1) / kWarps * kWarps;
 }
-inline Scratch carve(void* base, int T, int E, int sequences) {
-  const size_t slots = static_cast<size_t>(slots_of(T, sequences));
+// At most so many slots, whatever the tokens of one: grows with T and with the sequences.
+inline long long most_slots(const moe_ctx* ctx, int sequences) {
+  const long long by_tokens = ctx->shape.T / kWarps, by_sms = 2LL * ctx->num_sms;
+  return (by_tokens < by_sms ? by_tokens : by_sms) + sequences + 1;
+}
+inline size_t scratch_words(const moe_ctx* ctx, int sequences) {
+  const size_t slots = static_cast<size_t>(most_slots(ctx, sequences)), E = ctx->shape.E;
+  return slots * (2 * E + 2) + static_cast<size_t>(sequences) * ((E + 31) / 32 + 1) + 4;
+}
+inline Scratch carve(const moe_ctx* ctx, void* base, int sequences) {
+  const size_t slots = static_cast<size_t>(most_slots(ctx, sequences)), E = ctx->shape.E;
   Scratch s;
   s.sums = static_cast<float*>(base);
   s.counts = reinterpret_cast<int32_t*>(s.sums + slots * E);
@@ -57,34 +66,66 @@ struct BalanceParams {
   const uint8_t* mask;
   Scratch scratch;
   int32_t* status;
-  int T, E, k, sequences, sigmoid;
+  int T, E, k, sequences, sigmoid, slot_tokens;
   float coef, z_coef;
 };
 
-__device__ __forceinline__ int offset_at(const int32_t* offsets, int q, int T) {
-  if (offsets == nullptr) return q == 0 ? 0 : T;
-  const int o = __ldg(offsets + q);
-  return min(max(o, 0), T);
+__device__ __forceinline__ int offset_at(const BalanceParams& p, int q) {
+  if (p.offsets == nullptr) return q == 0 ? 0 : p.T;
+  const int o = __ldg(p.offsets + q);
+  return min(max(o, 0), p.T);
 }
-// Probabilities of one token over its lanes: x becomes p; returns what else the losses need.
+
+// The experts of a lane: kVec neighbours, then those 32 * kVec further.
+template <int kVec>
+__device__ __forceinline__ int expert_of(int lane, int i) {
+  return i / kVec * (32 * kVec) + lane * kVec + i % kVec;
+}
+template <int EL, int kVec>
+__device__ __forceinline__ void load_row(const float* row, int E, int lane, float (&x)[EL], float none) {
+#pragma unroll
+  for (int i = 0; i < EL; i += kVec) {
+    const int e = expert_of<kVec>(lane, i);
+    if constexpr (kVec == 4) {                             // (E is a multiple of 4)
+      const float4 v = e < E ? *reinterpret_cast<const float4*>(row + e) : make_float4(none, none, none, none);
+      x[i] = v.x; x[i + 1] = v.y; x[i + 2] = v.z; x[i + 3] = v.w;
+    } else {
+      x[i] = e < E ? row[e] : none;
+    }
+  }
+}
+template <int EL, int kVec>
+__device__ __forceinline__ void store_row(float* row, int E, int lane, const float (&x)[EL]) {
+#pragma unroll
+  for (int i = 0; i < EL; i += kVec) {
+    const int e = expert_of<kVec>(lane, i);
+    if (e < E) {
+      if constexpr (kVec == 4) *reinterpret_cast<float4*>(row + e) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+      else row[e] = x[i];
+    }
+  }
+}
+
 struct Token {
-  float lse;                                               // log of the sum of exponentials, -inf when all are masked
+  float lse;                                               // log of the sum of exponentials
   bool any;                                                // an expert is left
 };
+// x becomes the probabilities of a token, own[i] = sigma(-x_i) (1 for softmax scores), soft the softmax when it is wanted.
 template <int EL>
-__device__ __forceinline__ Token probabilities(float (&x)[EL], float (&soft)[EL], bool sigmoid, bool want_soft) {
+__device__ __forceinline__ Token probabilities(float (&x)[EL], float (&own)[EL], float (&soft)[EL], bool sigmoid, bool want_soft) {
   float top = x[0];
+  bool nan = x[0] != x[0], far = x[0] < -moe::kNearSigmoid;
 #pragma unroll
-  for (int i = 1; i < EL; ++i) top = fmaxf(top, x[i]);
-  bool nan = false;
-#pragma unroll
-  for (int i = 0; i < EL; ++i) nan |= x[i] != x[i];
+  for (int i = 1; i < EL; ++i) {
+    top = fmaxf(top, x[i]);
+    nan |= x[i] != x[i];
+    far |= x[i] < -moe::kNearSigmoid;                      // (masked experts among them)
+  }
   top = moe::warp_max(top);
-  nan = __any_sync(kFull, nan);
   Token t;
-  t.any = top > -INFINITY || nan;
+  t.any = top > -INFINITY || __any_sync(kFull, nan);
+  t.lse = 0.f;
   const float base = top > -INFINITY ? top : 0.f;
-  t.lse = -INFINITY;
   if (!sigmoid || want_soft) {
     float sum = 0.f;
 #pragma unroll
@@ -98,26 +139,48 @@ __device__ __forceinline__ Token probabilities(float (&x)[EL], float (&soft)[EL]
     for (int i = 0; i < EL; ++i) soft[i] *= inv;
     if (t.any) t.lse = logf(sum) + base;
   }
-  if (sigmoid) {
-    // From -40 down sigma(x) is exp(x) to 2^-57, and the shares of the sum are those of exp(x - top), which stays in range.
-    const bool far = top < -40.f;
-    float sum = 0.f;
+  if (!sigmoid) {
 #pragma unroll
     for (int i = 0; i < EL; ++i) {
-      x[i] = far ? expf(x[i] - base) : moe::route_sigmoid(x[i]);
+      x[i] = soft[i];
+      own[i] = 1.f;
+    }
+    return t;
+  }
+  float sum = 0.f;
+  if (!__any_sync(kFull, far)) {
+#pragma unroll
+    for (int i = 0; i < EL; ++i) {
+      const float e = expf(-x[i]);
+      x[i] = moe::reciprocal_from_one(1.f + e);
+      own[i] = e * x[i];                                   // (1 - s loses its digits where s is near 1)
       sum += x[i];
     }
-    sum = moe::warp_sum(sum);
-#pragma unroll
-    for (int i = 0; i < EL; ++i) x[i] = t.any ? __fdiv_rn(x[i], sum) : 0.f;
   } else {
+    // Below -80 sigma(x) is exp(x) to 2^-115.  When the largest is below -40 all are exp(x) to 2^-57, and the shares of the sum
+    // are those of exp(x - top), which stays in range.
+    const float shift = top < -40.f ? base : 0.f;
 #pragma unroll
-    for (int i = 0; i < EL; ++i) x[i] = soft[i];
+    for (int i = 0; i < EL; ++i) {
+      if (top < -40.f || x[i] < -moe::kNearSigmoid) {
+        x[i] = expf(x[i] - shift);
+        own[i] = 1.f;
+      } else {
+        const float e = expf(-x[i]);
+        x[i] = moe::reciprocal_from_one(1.f + e);
+        own[i] = e * x[i];
+      }
+      sum += x[i];
+    }
   }
+  sum = moe::warp_sum(sum);
+  const float inv = t.any ? 1.f / sum : 0.f;
+#pragma unroll
+  for (int i = 0; i < EL; ++i) x[i] *= inv;
   return t;
 }
 
-template <int EL>
+template <int EL, int kVec>
 __global__ void __launch_bounds__(kThreads)
 balance_partial(const BalanceParams p) {
   extern __shared__ float s_sum[];                         // [kWarps][E] sums, then [E] counts
@@ -126,18 +189,19 @@ balance_partial(const BalanceParams p) {
   int* s_count = reinterpret_cast<int*>(s_sum + kWarps * p.E);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int slot = blockIdx.x;
+  ptx::launch_dependents();
   if (slot == 0 && threadIdx.x == 0) *p.scratch.ticket = 0;
   for (int e = threadIdx.x; e < p.E; e += kThreads) s_count[e] = 0;
 
   const int q = moe::last_at_or_below(p.sequences, slot, lane, [&](int i) {
-    return static_cast<long long>(offset_at(p.offsets, i, p.T) / kSlotTokens) + i;
+    return static_cast<long long>(offset_at(p, i) / p.slot_tokens) + i;
   });
   int t0 = 0, t1 = 0;
   if (q >= 0) {
-    const int begin = offset_at(p.offsets, q, p.T), end = offset_at(p.offsets, q + 1, p.T);
-    const long long first = begin + (static_cast<long long>(slot) - (begin / kSlotTokens + q)) * kSlotTokens;
+    const int begin = offset_at(p, q), end = offset_at(p, q + 1);
+    const long long first = begin + (static_cast<long long>(slot) - (begin / p.slot_tokens + q)) * p.slot_tokens;
     t0 = static_cast<int>(first < end ? first : end);
-    t1 = min(t0 + kSlotTokens, end);
+    t1 = min(t0 + p.slot_tokens, end);
   }
   __syncthreads();
 
@@ -147,36 +211,41 @@ balance_partial(const BalanceParams p) {
   float z = 0.f;
   int tokens = 0;
   const bool want_z = p.z_coef != 0.f;
-  for (int t = t0 + warp; t < t1; t += kWarps) {
-    if (p.mask != nullptr && p.mask[t] == 0) continue;
-    const float* row = p.logits + static_cast<size_t>(t) * p.E;
-    float x[EL], soft[EL];
-#pragma unroll
-    for (int i = 0; i < EL; ++i) {
-      const int e = lane + 32 * i;
-      x[i] = e < p.E ? __ldg(row + e) : -INFINITY;
+  auto counts = [&](int t) { return t < t1 && (p.mask == nullptr || p.mask[t] != 0); };
+  int t = t0 + warp;
+  while (t < t1 && !counts(t)) t += kWarps;
+  float next[EL];
+  int next_id = -1;
+  auto fetch = [&](int at) {
+    if (at < t1) {
+      load_row<EL, kVec>(p.logits + static_cast<size_t>(at) * p.E, p.E, lane, next, -INFINITY);
+      next_id = lane < p.k ? p.ids[static_cast<size_t>(at) * p.k + lane] : 0;
     }
+  };
+  fetch(t);
+  while (t < t1) {
+    float x[EL], own[EL], soft[EL];
+#pragma unroll
+    for (int i = 0; i < EL; ++i) x[i] = next[i];
+    const int id = next_id, now = t;
+    t += kWarps;
+    while (t < t1 && !counts(t)) t += kWarps;
+    fetch(t);
     if (lane < p.k) {
-      const size_t s = static_cast<size_t>(t) * p.k + lane;
-      const int id = p.ids[s];
       if (id >= 0 && id < p.E) {
         atomicAdd(s_count + id, 1);
       } else {
         atomicCAS(&p.status[0], 0, MOE_ERR_BAD_ROUTING);
-        atomicCAS(&p.status[1], 0, static_cast<int>(s));
+        atomicCAS(&p.status[1], 0, now * p.k + lane);
       }
     }
-    const Token token = probabilities<EL>(x, soft, p.sigmoid, want_z);
+    const Token token = probabilities<EL>(x, own, soft, p.sigmoid, want_z);
 #pragma unroll
     for (int i = 0; i < EL; ++i) acc[i] += x[i];
-    if (want_z && token.any) z = fmaf(token.lse, token.lse, z);
+    if (want_z) z = fmaf(token.lse, token.lse, z);
     ++tokens;
   }
-#pragma unroll
-  for (int i = 0; i < EL; ++i) {
-    const int e = lane + 32 * i;
-    if (e < p.E) s_sum[warp * p.E + e] = acc[i];
-  }
+  store_row<EL, kVec>(s_sum + warp * p.E, p.E, lane, acc);
   if (lane == 0) {
     s_tokens[warp] = tokens;
     s_z[warp] = z;
@@ -184,6 +253,7 @@ balance_partial(const BalanceParams p) {
   __syncthreads();
   for (int e = threadIdx.x; e < p.E; e += kThreads) {
     float sum = 0.f;
+#pragma unroll
     for (int w = 0; w < kWarps; ++w) sum += s_sum[w * p.E + e];
     p.scratch.sums[static_cast<size_t>(slot) * p.E + e] = sum;
     p.scratch.counts[static_cast<size_t>(slot) * p.E + e] = s_count[e];
@@ -200,10 +270,12 @@ balance_partial(const BalanceParams p) {
   }
 }
 
-__global__ void __launch_bounds__(kFinishThreads)
+// kRows warps, each with every kRows-th slot.
+template <int kRows>
+__global__ void __launch_bounds__(kRows * 32)
 balance_finish(const BalanceParams p, int slots, int32_t* __restrict__ counts, int32_t* __restrict__ tokens,
                float* __restrict__ mean, float* __restrict__ loss) {
-  constexpr int kRows = kFinishThreads / 32;
+  constexpr int kAhead = 8;                                // slots whose loads are in flight together
   __shared__ float s_sum[kRows][33];
   __shared__ int s_count[kRows][33];
   __shared__ int s_tokens[kRows];
@@ -213,19 +285,31 @@ balance_finish(const BalanceParams p, int slots, int32_t* __restrict__ counts, i
   __shared__ int s_last;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int parts = (p.E + 31) / 32, q = blockIdx.x / parts, part = blockIdx.x % parts, e = part * 32 + lane;
-  const int begin = offset_at(p.offsets, q, p.T), end = offset_at(p.offsets, q + 1, p.T);
-  const int first = begin / kSlotTokens + q;
-  const int used = min(end > begin ? (end - begin + kSlotTokens - 1) / kSlotTokens : 0, slots - first);
+  const int begin = offset_at(p, q), end = offset_at(p, q + 1);
+  const int first = begin / p.slot_tokens + q;
+  const int used = min(end > begin ? (end - begin + p.slot_tokens - 1) / p.slot_tokens : 0, slots - first);
+  ptx::wait_for_previous_kernel();
   float sum = 0.f, z = 0.f;
   int count = 0, n = 0;
-  for (int i = warp; i < used; i += kRows) {
-    const size_t at = static_cast<size_t>(first + i);
-    if (e < p.E) {
-      sum += p.scratch.sums[at * p.E + e];
-      count += p.scratch.counts[at * p.E + e];
+  for (int i = warp; i < used; i += kRows * kAhead) {
+    float s[kAhead], zs[kAhead];
+    int c[kAhead], ns[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const size_t at = static_cast<size_t>(first + i + u * kRows);
+      const bool in = i + u * kRows < used;
+      s[u] = in && e < p.E ? __ldcg(p.scratch.sums + at * p.E + e) : 0.f;
+      c[u] = in && e < p.E ? __ldcg(p.scratch.counts + at * p.E + e) : 0;
+      ns[u] = in ? __ldcg(p.scratch.tokens + at) : 0;
+      zs[u] = in ? __ldcg(p.scratch.z + at) : 0.f;
     }
-    n += p.scratch.tokens[at];
-    z += p.scratch.z[at];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      sum += s[u];
+      count += c[u];
+      n += ns[u];
+      z += zs[u];
+    }
   }
   s_sum[warp][lane] = sum;
   s_count[warp][lane] = count;
@@ -235,15 +319,14 @@ balance_finish(const BalanceParams p, int slots, int32_t* __restrict__ counts, i
   }
   __syncthreads();
   if (warp == 0) {
-    n = s_tokens[lane];
-    z = s_z[lane];
+    n = lane < kRows ? s_tokens[lane] : 0;
+    z = lane < kRows ? s_z[lane] : 0.f;
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-      n += __shfl_xor_sync(kFull, n, off);
-      z += __shfl_xor_sync(kFull, z, off);
-    }
+    for (int off = 16; off > 0; off >>= 1) n += __shfl_xor_sync(kFull, n, off);
+    z = moe::warp_sum(z);
     sum = 0.f;
     count = 0;
+#pragma unroll
     for (int w = 0; w < kRows; ++w) {
       sum += s_sum[w][lane];
       count += s_count[w][lane];
@@ -272,9 +355,9 @@ balance_finish(const BalanceParams p, int slots, int32_t* __restrict__ counts, i
   __threadfence();
   double total = 0.0, zs = 0.0;
   int all = 0;
-  for (long long i = threadIdx.x; i < static_cast<long long>(p.sequences) * parts; i += kFinishThreads)
+  for (long long i = threadIdx.x; i < static_cast<long long>(p.sequences) * parts; i += kRows * 32)
     total += __ldcg(p.scratch.share + i);
-  for (int i = threadIdx.x; i < p.sequences; i += kFinishThreads) {
+  for (int i = threadIdx.x; i < p.sequences; i += kRows * 32) {
     zs += __ldcg(p.scratch.seq_z + i);
     all += __ldcg(tokens + i);
   }
@@ -304,59 +387,81 @@ balance_finish(const BalanceParams p, int slots, int32_t* __restrict__ counts, i
   }
 }
 
-template <int EL>
+// Warp w takes the tokens [w * chunk, (w + 1) * chunk).
+template <int EL, int kVec>
 __global__ void __launch_bounds__(kThreads)
-balance_backward(const BalanceParams p, const int32_t* __restrict__ counts, const int32_t* __restrict__ tokens,
+balance_backward(const BalanceParams p, int chunk, const int32_t* __restrict__ counts, const int32_t* __restrict__ tokens,
                  const float* __restrict__ d_loss, const float* add, float* d_logits) {
-  const int lane = threadIdx.x & 31, t = blockIdx.x * kWarps + (threadIdx.x >> 5);
-  if (t >= p.T) return;
-  const size_t at = static_cast<size_t>(t) * p.E;
-  float x[EL], soft[EL], d[EL];
-#pragma unroll
-  for (int i = 0; i < EL; ++i) {
-    const int e = lane + 32 * i;
-    x[i] = e < p.E ? __ldg(p.logits + at + e) : -INFINITY;
-    d[i] = add != nullptr && e < p.E ? add[at + e] : 0.f;
+  const int lane = threadIdx.x & 31;
+  const long long begin = (static_cast<long long>(blockIdx.x) * kWarps + (threadIdx.x >> 5)) * chunk;
+  if (begin >= p.T) return;
+  const int t0 = static_cast<int>(begin), t1 = static_cast<int>(begin + chunk < p.T ? begin + chunk : p.T);
+  const float up = d_loss != nullptr ? __ldg(d_loss) : 1.f;
+  const bool want_z = p.z_coef != 0.f;
+  float z_scale = 0.f;
+  if (want_z) {
+    const int all = __ldg(tokens + p.sequences);
+    z_scale = all > 0 ? up * (2.f * p.z_coef / static_cast<float>(all)) : 0.f;
   }
-  int q = 0;
-  if (p.offsets != nullptr) {
-    q = moe::last_at_or_below(p.sequences, t, lane, [&](int i) { return static_cast<long long>(offset_at(p.offsets, i, p.T)); });
-    if (q < 0 || t >= offset_at(p.offsets, q + 1, p.T)) q = -1;
-  }
-  if (p.mask != nullptr && p.mask[t] == 0) q = -1;
-  const int n = q >= 0 ? __ldg(tokens + q) : 0;
-  if (n > 0) {
-    const float up = d_loss != nullptr ? __ldg(d_loss) : 1.f;
-    const bool want_z = p.z_coef != 0.f;
-    float u[EL], own[EL];                                  // own: sigma(-x)
-    // coef / sequences E c / (k n) / n, rounded a few times but never out of range where the result is not
-    const float f = up * (p.coef / p.sequences) / static_cast<float>(n);
-    const float load = static_cast<float>(p.E) / (static_cast<float>(p.k) * static_cast<float>(n));
+  float u[EL];
+  int seq_end = t0, n = 0;                                 // of the sequence that u belongs to; none yet
+  float next_x[EL], next_d[EL];
+  auto fetch = [&](int t) {
+    if (t < t1) {
+      const size_t at = static_cast<size_t>(t) * p.E;
+      load_row<EL, kVec>(p.logits + at, p.E, lane, next_x, -INFINITY);
+      if (add != nullptr) load_row<EL, kVec>(add + at, p.E, lane, next_d, 0.f);
+    }
+  };
+  fetch(t0);
+  for (int t = t0; t < t1; ++t) {
+    float x[EL], d[EL], own[EL], soft[EL];
 #pragma unroll
     for (int i = 0; i < EL; ++i) {
-      const int e = lane + 32 * i;
-      u[i] = e < p.E ? f * (load * static_cast<float>(__ldg(counts + static_cast<size_t>(q) * p.E + e))) : 0.f;
-      own[i] = p.sigmoid ? moe::route_sigmoid(-x[i]) : 1.f;
+      x[i] = next_x[i];
+      d[i] = add != nullptr ? next_d[i] : 0.f;
     }
-    const Token token = probabilities<EL>(x, soft, p.sigmoid, want_z);
-    if (token.any) {
-      float dot = 0.f;
+    fetch(t + 1);
+    if (t >= seq_end) {                                    // the token's sequence, and what its counts give to every token
+      int q = 0;
+      if (p.offsets != nullptr)
+        q = moe::last_at_or_below(p.sequences, t, lane, [&](int i) { return static_cast<long long>(offset_at(p, i)); });
+      n = 0;
+      seq_end = p.T;
+      if (q >= 0 && t < offset_at(p, q + 1)) {
+        seq_end = offset_at(p, q + 1);
+        n = __ldg(tokens + q);
+      } else if (q < 0) {
+        seq_end = t + 1;
+      }
+      if (n > 0) {
+        // coef / sequences, E c / (k n) and 1 / n, none of them out of range where the result is not
+        const float f = up * (p.coef / p.sequences) / static_cast<float>(n);
+        const float load = static_cast<float>(p.E) / (static_cast<float>(p.k) * static_cast<float>(n));
 #pragma unroll
-      for (int i = 0; i < EL; ++i) dot = fmaf(u[i], x[i], dot);
-      dot = moe::warp_sum(dot);
-      const float zf = want_z ? up * (2.f * p.z_coef / static_cast<float>(__ldg(tokens + p.sequences))) * token.lse : 0.f;
-#pragma unroll
-      for (int i = 0; i < EL; ++i) {
-        float g = x[i] * (u[i] - dot) * own[i];
-        if (want_z) g = fmaf(zf, soft[i], g);
-        d[i] += g;
+        for (int i = 0; i < EL; ++i) {
+          const int e = expert_of<kVec>(lane, i);
+          u[i] = e < p.E ? f * (load * static_cast<float>(__ldg(counts + static_cast<size_t>(q) * p.E + e))) : 0.f;
+        }
       }
     }
-  }
+    if (n > 0 && (p.mask == nullptr || p.mask[t] != 0)) {
+      const Token token = probabilities<EL>(x, own, soft, p.sigmoid, want_z);
+      if (token.any) {
+        float dot = 0.f;
 #pragma unroll
-  for (int i = 0; i < EL; ++i) {
-    const int e = lane + 32 * i;
-    if (e < p.E) d_logits[at + e] = d[i];
+        for (int i = 0; i < EL; ++i) dot = fmaf(u[i], x[i], dot);
+        dot = moe::warp_sum(dot);
+        const float zf = z_scale * token.lse;
+#pragma unroll
+        for (int i = 0; i < EL; ++i) {
+          float g = x[i] * (u[i] - dot) * own[i];
+          if (want_z) g = fmaf(zf, soft[i], g);
+          d[i] += g;
+        }
+      }
+    }
+    store_row<EL, kVec>(d_logits + static_cast<size_t>(t) * p.E, p.E, lane, d);
   }
 }
 
@@ -373,43 +478,61 @@ BalanceParams params_of(const moe_ctx* ctx, const moe_balance_args& a) {
   p.k = s.k;
   p.sequences = a.sequences;
   p.sigmoid = a.score == MOE_SCORE_SIGMOID;
+  p.slot_tokens = slot_tokens_of(ctx);
   p.coef = a.coef;
   p.z_coef = a.z_coef;
   return p;
 }
+
+// Four neighbouring experts to a lane where that fills the warp and keeps 16-byte rows.
+#define MOE_BALANCE_KERNEL(kernel, E)                                                                                   \
+  ((E) % 4 == 0 && (E) >= 128                                                                                           \
+       ? ((E) <= 128 ? kernel<4, 4> : (E) <= 256 ? kernel<8, 4> : (E) <= 512 ? kernel<16, 4> : kernel<32, 4>)           \
+       : ((E) <= 32 ? kernel<1, 1> : (E) <= 64 ? kernel<2, 1> : (E) <= 128 ? kernel<4, 1> : (E) <= 256 ? kernel<8, 1>   \
+          : (E) <= 512 ? kernel<16, 1> : kernel<32, 1>))
 
 }  // namespace
 
 namespace moe {
 
 size_t balance_scratch_bytes(const moe_ctx* ctx, int sequences) {
-  return (scratch_words(ctx->shape.T, ctx->shape.E, sequences) * 4 + 255) / 256 * 256;
+  return (scratch_words(ctx, sequences) * 4 + 255) / 256 * 256;
 }
 
 cudaError_t launch_balance_loss(moe_ctx* ctx, const moe_balance_args& args, int32_t* counts, int32_t* tokens, float* mean,
                                 float* loss, void* scratch, cudaStream_t stream) {
   BalanceParams p = params_of(ctx, args);
-  p.scratch = carve(scratch, p.T, p.E, p.sequences);
-  const int slots = static_cast<int>(slots_of(p.T, p.sequences));
+  p.scratch = carve(ctx, scratch, p.sequences);
+  const int slots = p.T / p.slot_tokens + p.sequences + 1;
   const size_t smem = static_cast<size_t>(kWarps + 1) * p.E * 4;          // at most 36 KiB
-  auto kernel = p.E <= 32 ? balance_partial<1> : p.E <= 64 ? balance_partial<2> : p.E <= 128 ? balance_partial<4>
-                : p.E <= 256 ? balance_partial<8> : p.E <= 512 ? balance_partial<16> : balance_partial<32>;
+  auto kernel = MOE_BALANCE_KERNEL(balance_partial, p.E);
   kernel<<<slots, kThreads, smem, stream>>>(p);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  balance_finish<<<static_cast<unsigned>(p.sequences) * ((p.E + 31) / 32), kFinishThreads, 0, stream>>>(
-      p, slots, counts, tokens, mean, loss);
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute attr{};
+  const bool long_ = slots >= 16 * static_cast<long long>(p.sequences);   // many slots to a sequence: more warps share them
+  cfg.gridDim = dim3(static_cast<unsigned>(p.sequences) * ((p.E + 31) / 32));
+  cfg.blockDim = dim3(long_ ? 1024 : 128);
+  cfg.stream = stream;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
   ctx->last_launches += 2;
-  return cudaGetLastError();
+  return cudaLaunchKernelEx(&cfg, long_ ? balance_finish<32> : balance_finish<4>, p, slots, counts, tokens, mean, loss);
 }
 
 cudaError_t launch_balance_loss_backward(moe_ctx* ctx, const moe_balance_args& args, const int32_t* counts,
                                          const int32_t* tokens, const float* d_loss, const float* add, float* d_logits,
                                          cudaStream_t stream) {
   const BalanceParams p = params_of(ctx, args);
-  auto kernel = p.E <= 32 ? balance_backward<1> : p.E <= 64 ? balance_backward<2> : p.E <= 128 ? balance_backward<4>
-                : p.E <= 256 ? balance_backward<8> : p.E <= 512 ? balance_backward<16> : balance_backward<32>;
-  kernel<<<(p.T + kWarps - 1) / kWarps, kThreads, 0, stream>>>(p, counts, tokens, d_loss, add, d_logits);
+  // up to four neighbouring tokens to a warp, fewer while that leaves fewer than 24 warps per SM
+  int chunk = 4;
+  while (chunk > 1 && p.T / chunk < 24 * ctx->num_sms) chunk /= 2;
+  const int per_block = kWarps * chunk;
+  auto kernel = MOE_BALANCE_KERNEL(balance_backward, p.E);
+  kernel<<<(p.T - 1) / per_block + 1, kThreads, 0, stream>>>(p, chunk, counts, tokens, d_loss, add, d_logits);
   ctx->last_launches += 1;
   return cudaGetLastError();
 }

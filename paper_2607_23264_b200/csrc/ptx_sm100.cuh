@@ -147,6 +147,11 @@ __device__ __forceinline__ void bulk_wait_group_all() { asm volatile("cp.async.b
 // All but the last bulk group have read their source.
 __device__ __forceinline__ void bulk_wait_group_read_but_one() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
 
+// Programmatic dependent launch: the next kernel of the stream may start (once every CTA has said so or ended) ...
+__device__ __forceinline__ void launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+// ... and waits here until the kernel before it has ended and its writes are visible.
+__device__ __forceinline__ void wait_for_previous_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // L2 eviction priorities for TMA loads: a 64-bit policy made once per thread.
 __device__ __forceinline__ uint64_t l2_policy_evict_first() {
   uint64_t p;
