@@ -111,21 +111,30 @@ struct Token {
   bool any;                                                // an expert is left
 };
 // x becomes the probabilities of a token, own[i] = sigma(-x_i) (1 for softmax scores), soft the softmax when it is wanted.
+// Logits within +-80, the usual ones, need neither their maximum over the warp nor a look at masks: the exponentials and their
+// sum stay in range, and NaN passes through.  (bits of `here`: the lane's experts that exist.)
 template <int EL>
-__device__ __forceinline__ Token probabilities(float (&x)[EL], float (&own)[EL], float (&soft)[EL], bool sigmoid, bool want_soft) {
-  float top = x[0];
-  bool nan = x[0] != x[0], far = x[0] < -moe::kNearSigmoid;
+__device__ __forceinline__ Token probabilities(float (&x)[EL], float (&own)[EL], float (&soft)[EL], uint32_t here, bool sigmoid,
+                                               bool want_soft) {
+  constexpr float kNear = moe::kNearSigmoid;
+  constexpr uint32_t kAll = EL == 32 ? 0xFFFFFFFFu : (1u << EL) - 1;
+  float most = -INFINITY, least = INFINITY;
 #pragma unroll
-  for (int i = 1; i < EL; ++i) {
-    top = fmaxf(top, x[i]);
-    nan |= x[i] != x[i];
-    far |= x[i] < -moe::kNearSigmoid;                      // (masked experts among them)
+  for (int i = 0; i < EL; ++i) {
+    most = fmaxf(most, x[i]);
+    least = fminf(least, x[i]);
   }
-  top = moe::warp_max(top);
-  Token t;
-  t.any = top > -INFINITY || __any_sync(kFull, nan);
-  t.lse = 0.f;
-  const float base = top > -INFINITY ? top : 0.f;
+  Token t{0.f, true};
+  float base = 0.f;
+  const bool near = __all_sync(kFull, most <= kNear && least >= -kNear && here == kAll);
+  if (!near) {
+    bool nan = false;
+#pragma unroll
+    for (int i = 0; i < EL; ++i) nan |= x[i] != x[i];
+    most = moe::warp_max(most);
+    t.any = most > -INFINITY || __any_sync(kFull, nan);
+    base = most > -INFINITY ? most : 0.f;
+  }
   if (!sigmoid || want_soft) {
     float sum = 0.f;
 #pragma unroll
@@ -137,7 +146,7 @@ __device__ __forceinline__ Token probabilities(float (&x)[EL], float (&own)[EL],
     const float inv = t.any ? 1.f / sum : 0.f;
 #pragma unroll
     for (int i = 0; i < EL; ++i) soft[i] *= inv;
-    if (t.any) t.lse = logf(sum) + base;
+    if (want_soft && t.any) t.lse = logf(sum) + base;
   }
   if (!sigmoid) {
 #pragma unroll
@@ -148,7 +157,7 @@ __device__ __forceinline__ Token probabilities(float (&x)[EL], float (&own)[EL],
     return t;
   }
   float sum = 0.f;
-  if (!__any_sync(kFull, far)) {
+  if (near) {
 #pragma unroll
     for (int i = 0; i < EL; ++i) {
       const float e = expf(-x[i]);
@@ -158,18 +167,15 @@ __device__ __forceinline__ Token probabilities(float (&x)[EL], float (&own)[EL],
     }
   } else {
     // Below -80 sigma(x) is exp(x) to 2^-115.  When the largest is below -40 all are exp(x) to 2^-57, and the shares of the sum
-    // are those of exp(x - top), which stays in range.
-    const float shift = top < -40.f ? base : 0.f;
+    // are those of exp(x - most), which stays in range.
+    const bool low = most < -40.f;
+    const float shift = low ? base : 0.f;
 #pragma unroll
     for (int i = 0; i < EL; ++i) {
-      if (top < -40.f || x[i] < -moe::kNearSigmoid) {
-        x[i] = expf(x[i] - shift);
-        own[i] = 1.f;
-      } else {
-        const float e = expf(-x[i]);
-        x[i] = moe::reciprocal_from_one(1.f + e);
-        own[i] = e * x[i];
-      }
+      const bool by_exp = low || x[i] < -kNear;
+      const float e = expf(by_exp ? x[i] - shift : -x[i]), s = moe::reciprocal_from_one(1.f + e);
+      x[i] = by_exp ? e : s;
+      own[i] = by_exp ? 1.f : e * s;
       sum += x[i];
     }
   }
@@ -179,8 +185,16 @@ __device__ __forceinline__ Token probabilities(float (&x)[EL], float (&own)[EL],
   for (int i = 0; i < EL; ++i) x[i] *= inv;
   return t;
 }
-
+// The experts of a lane that exist, a bit each.
 template <int EL, int kVec>
+__device__ __forceinline__ uint32_t experts_here(int E, int lane) {
+  uint32_t here = 0;
+#pragma unroll
+  for (int i = 0; i < EL; ++i) here |= (expert_of<kVec>(lane, i) < E ? 1u : 0u) << i;
+  return here;
+}
+
+template <int EL, int kVec, bool kSigmoid>
 __global__ void __launch_bounds__(kThreads)
 balance_partial(const BalanceParams p) {
   extern __shared__ float s_sum[];                         // [kWarps][E] sums, then [E] counts
@@ -208,6 +222,7 @@ balance_partial(const BalanceParams p) {
   float acc[EL];
 #pragma unroll
   for (int i = 0; i < EL; ++i) acc[i] = 0.f;
+  const uint32_t here = experts_here<EL, kVec>(p.E, lane);
   float z = 0.f;
   int tokens = 0;
   const bool want_z = p.z_coef != 0.f;
@@ -239,7 +254,7 @@ balance_partial(const BalanceParams p) {
         atomicCAS(&p.status[1], 0, now * p.k + lane);
       }
     }
-    const Token token = probabilities<EL>(x, own, soft, p.sigmoid, want_z);
+    const Token token = probabilities<EL>(x, own, soft, here, kSigmoid, want_z);
 #pragma unroll
     for (int i = 0; i < EL; ++i) acc[i] += x[i];
     if (want_z) z = fmaf(token.lse, token.lse, z);
@@ -280,8 +295,7 @@ balance_finish(const BalanceParams p, int slots, int32_t* __restrict__ counts, i
   __shared__ int s_count[kRows][33];
   __shared__ int s_tokens[kRows];
   __shared__ float s_z[kRows];
-  __shared__ double s_loss[kRows][2];
-  __shared__ int s_n[kRows];
+  __shared__ float s_loss[kRows][2];
   __shared__ int s_last;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int parts = (p.E + 31) / 32, q = blockIdx.x / parts, part = blockIdx.x % parts, e = part * 32 + lane;
@@ -353,42 +367,44 @@ balance_finish(const BalanceParams p, int slots, int32_t* __restrict__ counts, i
   __syncthreads();
   if (!s_last) return;
   __threadfence();
-  double total = 0.0, zs = 0.0;
-  int all = 0;
-  for (long long i = threadIdx.x; i < static_cast<long long>(p.sequences) * parts; i += kRows * 32)
-    total += __ldcg(p.scratch.share + i);
-  for (int i = threadIdx.x; i < p.sequences; i += kRows * 32) {
-    zs += __ldcg(p.scratch.seq_z + i);
-    all += __ldcg(tokens + i);
+  // the shares in a fixed order, by one warp when they are few
+  const int shares = p.sequences * parts, warps = shares <= 256 ? 1 : kRows;
+  if (warp >= warps) return;
+  float total = 0.f;
+  z = 0.f;
+  n = 0;
+  for (int i = threadIdx.x; i < shares; i += 32 * warps) total += __ldcg(p.scratch.share + i);
+  for (int i = threadIdx.x; i < p.sequences; i += 32 * warps) {
+    z += __ldcg(p.scratch.seq_z + i);
+    n += __ldcg(tokens + i);
   }
+  total = moe::warp_sum(total);
+  z = moe::warp_sum(z);
 #pragma unroll
-  for (int off = 16; off > 0; off >>= 1) {
-    total += __shfl_xor_sync(kFull, total, off);
-    zs += __shfl_xor_sync(kFull, zs, off);
-    all += __shfl_xor_sync(kFull, all, off);
+  for (int off = 16; off > 0; off >>= 1) n += __shfl_xor_sync(kFull, n, off);
+  if (warps > 1) {
+    if (lane == 0) {
+      s_loss[warp][0] = total;
+      s_loss[warp][1] = z;
+      s_tokens[warp] = n;
+    }
+    __syncthreads();
+    if (warp > 0) return;
+    total = moe::warp_sum(lane < kRows ? s_loss[lane][0] : 0.f);
+    z = moe::warp_sum(lane < kRows ? s_loss[lane][1] : 0.f);
+    n = lane < kRows ? s_tokens[lane] : 0;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) n += __shfl_xor_sync(kFull, n, off);
   }
   if (lane == 0) {
-    s_loss[warp][0] = total;
-    s_loss[warp][1] = zs;
-    s_n[warp] = all;
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    total = zs = 0.0;
-    all = 0;
-    for (int w = 0; w < kRows; ++w) {
-      total += s_loss[w][0];
-      zs += s_loss[w][1];
-      all += s_n[w];
-    }
-    loss[0] = static_cast<float>(total * p.coef / p.sequences);
-    loss[1] = all > 0 ? static_cast<float>(zs * p.z_coef / all) : 0.f;
-    tokens[p.sequences] = all;
+    loss[0] = total * (p.coef / static_cast<float>(p.sequences));
+    loss[1] = n > 0 ? z * p.z_coef / static_cast<float>(n) : 0.f;
+    tokens[p.sequences] = n;
   }
 }
 
 // Warp w takes the tokens [w * chunk, (w + 1) * chunk).
-template <int EL, int kVec>
+template <int EL, int kVec, bool kSigmoid>
 __global__ void __launch_bounds__(kThreads)
 balance_backward(const BalanceParams p, int chunk, const int32_t* __restrict__ counts, const int32_t* __restrict__ tokens,
                  const float* __restrict__ d_loss, const float* add, float* d_logits) {
@@ -403,6 +419,7 @@ balance_backward(const BalanceParams p, int chunk, const int32_t* __restrict__ c
     const int all = __ldg(tokens + p.sequences);
     z_scale = all > 0 ? up * (2.f * p.z_coef / static_cast<float>(all)) : 0.f;
   }
+  const uint32_t here = experts_here<EL, kVec>(p.E, lane);
   float u[EL];
   int seq_end = t0, n = 0;                                 // of the sequence that u belongs to; none yet
   float next_x[EL], next_d[EL];
@@ -446,7 +463,7 @@ balance_backward(const BalanceParams p, int chunk, const int32_t* __restrict__ c
       }
     }
     if (n > 0 && (p.mask == nullptr || p.mask[t] != 0)) {
-      const Token token = probabilities<EL>(x, own, soft, p.sigmoid, want_z);
+      const Token token = probabilities<EL>(x, own, soft, here, kSigmoid, want_z);
       if (token.any) {
         float dot = 0.f;
 #pragma unroll
@@ -485,11 +502,11 @@ BalanceParams params_of(const moe_ctx* ctx, const moe_balance_args& a) {
 }
 
 // Four neighbouring experts to a lane where that fills the warp and keeps 16-byte rows.
-#define MOE_BALANCE_KERNEL(kernel, E)                                                                                   \
-  ((E) % 4 == 0 && (E) >= 128                                                                                           \
-       ? ((E) <= 128 ? kernel<4, 4> : (E) <= 256 ? kernel<8, 4> : (E) <= 512 ? kernel<16, 4> : kernel<32, 4>)           \
-       : ((E) <= 32 ? kernel<1, 1> : (E) <= 64 ? kernel<2, 1> : (E) <= 128 ? kernel<4, 1> : (E) <= 256 ? kernel<8, 1>   \
-          : (E) <= 512 ? kernel<16, 1> : kernel<32, 1>))
+#define MOE_BALANCE_KERNEL(kernel, E, S)                                                                                    \
+  ((E) % 4 == 0 && (E) >= 128                                                                                               \
+       ? ((E) <= 128 ? kernel<4, 4, S> : (E) <= 256 ? kernel<8, 4, S> : (E) <= 512 ? kernel<16, 4, S> : kernel<32, 4, S>)   \
+       : ((E) <= 32 ? kernel<1, 1, S> : (E) <= 64 ? kernel<2, 1, S> : (E) <= 128 ? kernel<4, 1, S>                          \
+          : (E) <= 256 ? kernel<8, 1, S> : (E) <= 512 ? kernel<16, 1, S> : kernel<32, 1, S>))
 
 }  // namespace
 
@@ -505,7 +522,7 @@ cudaError_t launch_balance_loss(moe_ctx* ctx, const moe_balance_args& args, int3
   p.scratch = carve(ctx, scratch, p.sequences);
   const int slots = p.T / p.slot_tokens + p.sequences + 1;
   const size_t smem = static_cast<size_t>(kWarps + 1) * p.E * 4;          // at most 36 KiB
-  auto kernel = MOE_BALANCE_KERNEL(balance_partial, p.E);
+  auto kernel = p.sigmoid ? MOE_BALANCE_KERNEL(balance_partial, p.E, true) : MOE_BALANCE_KERNEL(balance_partial, p.E, false);
   kernel<<<slots, kThreads, smem, stream>>>(p);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
@@ -531,7 +548,7 @@ cudaError_t launch_balance_loss_backward(moe_ctx* ctx, const moe_balance_args& a
   int chunk = 4;
   while (chunk > 1 && p.T / chunk < 24 * ctx->num_sms) chunk /= 2;
   const int per_block = kWarps * chunk;
-  auto kernel = MOE_BALANCE_KERNEL(balance_backward, p.E);
+  auto kernel = p.sigmoid ? MOE_BALANCE_KERNEL(balance_backward, p.E, true) : MOE_BALANCE_KERNEL(balance_backward, p.E, false);
   kernel<<<(p.T - 1) / per_block + 1, kThreads, 0, stream>>>(p, chunk, counts, tokens, d_loss, add, d_logits);
   ctx->last_launches += 1;
   return cudaGetLastError();
