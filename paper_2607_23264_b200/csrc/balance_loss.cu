@@ -19,7 +19,9 @@
 namespace {
 
 constexpr unsigned kFull = 0xFFFFFFFFu;
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kThreads = 256, kWarps = kThreads / 32;      // of balance_backward
+// Warps of balance_partial: sixteen, eight where sixteen rows of sums would not fit into 48 KiB.
+__host__ __device__ constexpr int partial_warps(int experts_per_lane) { return experts_per_lane <= 16 ? 16 : 8; }
 
 // What a call keeps in its scratch, in 4-byte words: [slots][E] sums, [slots][E] counts, [slots] tokens, [slots] sums of squared
 // logarithms, then per sequence and group of 32 experts a share of the loss, per sequence its sum of squares, and the ticket.
@@ -32,14 +34,14 @@ struct Scratch {
   float* seq_z;
   int32_t* ticket;
 };
-// Tokens of a slot: two CTAs per SM, a multiple of the warps.
+// Tokens of a slot: two CTAs per SM, a multiple of eight.
 inline int slot_tokens_of(const moe_ctx* ctx) {
   const int per = ctx->shape.T / (2 * ctx->num_sms) + 1;
-  return (per + kWarps - 1) / kWarps * kWarps;
+  return (per + 7) / 8 * 8;
 }
 // At most so many slots, whatever the tokens of one: grows with T and with the sequences.
 inline long long most_slots(const moe_ctx* ctx, int sequences) {
-  const long long by_tokens = ctx->shape.T / kWarps, by_sms = 2LL * ctx->num_sms;
+  const long long by_tokens = ctx->shape.T / 8, by_sms = 2LL * ctx->num_sms;
   return (by_tokens < by_sms ? by_tokens : by_sms) + sequences + 1;
 }
 inline size_t scratch_words(const moe_ctx* ctx, int sequences) {
@@ -195,8 +197,9 @@ __device__ __forceinline__ uint32_t experts_here(int E, int lane) {
 }
 
 template <int EL, int kVec, bool kSigmoid>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(32 * partial_warps(EL))
 balance_partial(const BalanceParams p) {
+  constexpr int kWarps = partial_warps(EL), kThreads = 32 * kWarps;
   extern __shared__ float s_sum[];                         // [kWarps][E] sums, then [E] counts
   __shared__ int s_tokens[kWarps];
   __shared__ float s_z[kWarps];
@@ -405,7 +408,7 @@ balance_finish(const BalanceParams p, int slots, int32_t* __restrict__ counts, i
 
 // Warp w takes the tokens [w * chunk, (w + 1) * chunk).
 template <int EL, int kVec, bool kSigmoid>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, EL <= 8 ? 3 : 1)
 balance_backward(const BalanceParams p, int chunk, const int32_t* __restrict__ counts, const int32_t* __restrict__ tokens,
                  const float* __restrict__ d_loss, const float* add, float* d_logits) {
   const int lane = threadIdx.x & 31;
@@ -521,9 +524,10 @@ cudaError_t launch_balance_loss(moe_ctx* ctx, const moe_balance_args& args, int3
   BalanceParams p = params_of(ctx, args);
   p.scratch = carve(ctx, scratch, p.sequences);
   const int slots = p.T / p.slot_tokens + p.sequences + 1;
-  const size_t smem = static_cast<size_t>(kWarps + 1) * p.E * 4;          // at most 36 KiB
+  const int warps = partial_warps(p.E <= 512 ? 16 : 32);
+  const size_t smem = static_cast<size_t>(warps + 1) * p.E * 4;           // at most 36 KiB
   auto kernel = p.sigmoid ? MOE_BALANCE_KERNEL(balance_partial, p.E, true) : MOE_BALANCE_KERNEL(balance_partial, p.E, false);
-  kernel<<<slots, kThreads, smem, stream>>>(p);
+  kernel<<<slots, 32 * warps, smem, stream>>>(p);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
@@ -544,9 +548,7 @@ cudaError_t launch_balance_loss_backward(moe_ctx* ctx, const moe_balance_args& a
                                          const int32_t* tokens, const float* d_loss, const float* add, float* d_logits,
                                          cudaStream_t stream) {
   const BalanceParams p = params_of(ctx, args);
-  // up to four neighbouring tokens to a warp, fewer while that leaves fewer than 24 warps per SM
-  int chunk = 4;
-  while (chunk > 1 && p.T / chunk < 24 * ctx->num_sms) chunk /= 2;
+  const int chunk = (p.T - 1) / (24 * ctx->num_sms) + 1;   // neighbouring tokens of a warp: all warps are resident at once
   const int per_block = kWarps * chunk;
   auto kernel = p.sigmoid ? MOE_BALANCE_KERNEL(balance_backward, p.E, true) : MOE_BALANCE_KERNEL(balance_backward, p.E, false);
   kernel<<<(p.T - 1) / per_block + 1, kThreads, 0, stream>>>(p, chunk, counts, tokens, d_loss, add, d_logits);
