@@ -263,6 +263,7 @@ moe_status moe_create(moe_ctx** out_ctx, const moe_shape* shape, int device) {
   ok = ok && moe::prepare_expert_ffn_mx(ctx) == cudaSuccess;
   ok = ok && moe::prepare_gemm_blk(ctx) == cudaSuccess;
   ok = ok && moe::prepare_plan_scored(ctx) == cudaSuccess;
+  ok = ok && moe::prepare_rms_norm(ctx) == cudaSuccess;
   ok = ok && moe::prepare_adapters(ctx) == cudaSuccess;
   for (int sl = 0; ok && sl < kMoeTimingSlots; ++sl)
     for (int i = 0; ok && i <= kMoeKernels; ++i) ok = cudaEventCreate(&ctx->ev[sl][i]) == cudaSuccess;

@@ -181,6 +181,7 @@ moe_status launch_expert_ffn_blk(moe_ctx* ctx, const moe_blk_ffn_args* args, cud
 
 // Residual addition and RMS norm with its outputs, and its gradients (arguments already checked).
 cudaError_t launch_add_rms_norm(moe_ctx* ctx, const moe_rms_norm_args& args, cudaStream_t stream);
+cudaError_t prepare_rms_norm(moe_ctx* ctx);      // one-time kernel attributes
 size_t rms_norm_scratch_bytes(const moe_ctx* ctx, long long rows, int cols);
 cudaError_t launch_rms_norm_backward(moe_ctx* ctx, const moe_rms_norm_grad_args& args, cudaStream_t stream);
 

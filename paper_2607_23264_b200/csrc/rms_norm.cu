@@ -1,22 +1,24 @@
 // Residual addition and RMS norm with an output in bf16, in 8 bits with scales, or both; and the norm's gradients.
 //
-// add_rms_norm  : kWarps warps per row, the row in registers (kVecs vectors of eight values per lane) from its one read to
-//                 its last write.  s = bf16(x + residual): the fp32 sum of two bf16 numbers is exact, or so near the larger
-//                 one that rounding it again gives that one, so s has one rounding.  The statistics are sums over s as
-//                 stored: the gradient then sees the same function, from the same tensor.
-// norm_backward : the same ownership of a row, persistent over rows, so that a lane's columns stay its own and the gain's
-//                 gradient is summed in registers; one partial row per CTA, summed by norm_gain_sum in a fixed order.
+// The statistics are sums over s = bf16(x + residual) as stored: the gradient then sees the same function, from the same tensor.
+//
+// add_rms_norm  : one row by as few warps as hold it, the row in registers from its one read to its last write.
+// norm_backward : the CTAs stay and take every gridDim-th group of rows; the rows to come are on their way into a ring in shared
+//                 memory by bulk copies; a lane's columns are the same in all rows, so its gains stay in registers, and the
+//                 gain's gradient is summed there: one partial row per CTA, added by norm_gain_sum in a fixed order.
 #include <cuda_bf16.h>
 
 #include "blk_quant.cuh"
 #include "moe_internal.h"
 #include "mx_quant.cuh"
+#include "ptx_sm100.cuh"
 #include "route_scored.cuh"
 
 namespace {
 
 constexpr unsigned kFull = 0xFFFFFFFFu;
-constexpr int kBlock = 256;               // threads of a CTA, unless one row takes more
+constexpr int kMaxRing = 4;
+constexpr int kRingBytes = 216 * 1024;    // of shared memory for the rings of an SM
 
 struct NormParams {
   const uint4* x;
@@ -27,9 +29,8 @@ struct NormParams {
   uint2* codes;
   void* scales;
   long long rows;
-  int vecs, cols;                         // vectors and values of a row
+  int vecs, cols;                         // vectors of eight values, and values, of a row
   float eps, gain_offset;
-  int gain_fp32, form;
 };
 
 struct NormGradParams {
@@ -39,10 +40,11 @@ struct NormGradParams {
   const uint4* d_sum;
   uint4* d_x;
   float* partial;                         // [CTAs][cols], or null
+  int32_t* status;
   long long rows;
   int vecs, cols;
   float eps, gain_offset;
-  int gain_fp32;
+  int ring;
 };
 
 __device__ __forceinline__ void unpack8(const uint4& q, float (&v)[8]) {
@@ -60,8 +62,24 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 __device__ __forceinline__ uint4 pack8(const float (&v)[8]) {
   return make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
 }
-__device__ __forceinline__ void load_gain(const void* gain, int fp32, float offset, int v, float (&g)[8]) {
-  if (fp32) {
+// x + residual in bf16 pairs: one rounding to nearest even.
+__device__ __forceinline__ uint32_t add2(uint32_t x, uint32_t r) {
+  const __nv_bfloat162 v = __hadd2(*reinterpret_cast<const __nv_bfloat162*>(&x), *reinterpret_cast<const __nv_bfloat162*>(&r));
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint4 add8(const uint4& x, const uint4& r) {
+  return make_uint4(add2(x.x, r.x), add2(x.y, r.y), add2(x.z, r.z), add2(x.w, r.w));
+}
+__device__ __forceinline__ float squares8(const uint4& q, float ss) {
+  float a[8];
+  unpack8(q, a);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) ss = fmaf(a[j], a[j], ss);
+  return ss;
+}
+template <bool kFp32>
+__device__ __forceinline__ void load_gain(const void* gain, float offset, int v, float (&g)[8]) {
+  if constexpr (kFp32) {
     const float4 a = __ldg(static_cast<const float4*>(gain) + 2 * v), b = __ldg(static_cast<const float4*>(gain) + 2 * v + 1);
     g[0] = a.x; g[1] = a.y; g[2] = a.z; g[3] = a.w;
     g[4] = b.x; g[5] = b.y; g[6] = b.z; g[7] = b.w;
@@ -72,30 +90,34 @@ __device__ __forceinline__ void load_gain(const void* gain, int fp32, float offs
   for (int i = 0; i < 8; ++i) g[i] += offset;
 }
 
+// How a CTA's threads share rows: `warps` warps to a row, `rows` rows to a CTA.
+struct Share {
+  int warps, rows;
+};
 // The warps of one row meet (named barriers: a CTA's last rows may be missing).
-template <int kWarps>
-__device__ __forceinline__ void row_sync(int group) {
-  asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(32 * kWarps) : "memory");
+__device__ __forceinline__ void row_sync(int group, int warps) {
+  asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(32 * warps) : "memory");
 }
-// Sum (or maximum) over the row's warps in a fixed order.  `part` holds kWarps floats per row of the CTA and may be written
-// again once every warp of the row has met after the reads.
-template <int kWarps>
-__device__ __forceinline__ float row_sum(float v, float* part, int group, int warp, int lane) {
-  v = moe::warp_sum(v);
-  if constexpr (kWarps > 1) {
-    if (lane == 0) part[warp] = v;
-    row_sync<kWarps>(group);
-    v = moe::warp_sum(lane < kWarps ? part[lane] : 0.f);
+// Sum over the row's warps in a fixed order.  `part` holds the warps' sums, and zeros up to the eighth.
+__device__ __forceinline__ float sum_of(const float* part, int warps, int lane) {
+  if (warps <= 8) {
+    const float4 a = *reinterpret_cast<const float4*>(part), b = *reinterpret_cast<const float4*>(part + 4);
+    return ((a.x + a.y) + (a.z + a.w)) + ((b.x + b.y) + (b.z + b.w));
   }
-  return v;
+  return moe::warp_sum(lane < warps ? part[lane] : 0.f);
 }
-template <int kWarps>
-__device__ __forceinline__ float row_max(float v, float* part, int group, int warp, int lane) {
+// Floats of a row's sums in shared memory.
+constexpr int kParts = 32;
+// ... for the most rows of a CTA (eight of one warp each take eight floats).
+__device__ __forceinline__ float* part_of(float* parts, int group, int warps) { return parts + group * (warps <= 8 ? 8 : kParts); }
+constexpr int kPartFloats = 64;
+
+__device__ __forceinline__ float row_max(float v, float* part, int group, int warps, int warp, int lane) {
   v = moe::warp_max(v);
-  if constexpr (kWarps > 1) {
+  if (warps > 1) {
     if (lane == 0) part[warp] = v;
-    row_sync<kWarps>(group);
-    v = moe::warp_max(lane < kWarps ? part[lane] : 0.f);
+    row_sync(group, warps);
+    v = moe::warp_max(lane < warps ? part[lane] : 0.f);
   }
   return v;
 }
@@ -111,90 +133,79 @@ __device__ __forceinline__ float rstd_of(float sum_of_squares, int cols, float e
   return __frsqrt_rn(__fdiv_rn(sum_of_squares, static_cast<float>(cols)) + eps);
 }
 
-template <int kWarps, int kVecs>
-__global__ void __launch_bounds__(kWarps * 32 > kBlock ? kWarps * 32 : kBlock)
-add_rms_norm(const NormParams p) {
-  constexpr int kGroups = kWarps * 32 >= kBlock ? 1 : kBlock / (kWarps * 32);
-  constexpr int kLanes = kWarps * 32;
-  __shared__ float s_part[2][kGroups * kWarps];
-  const int lane = threadIdx.x & 31, group = threadIdx.x / kLanes, tid = threadIdx.x % kLanes, warp = tid >> 5;
-  const long long row = static_cast<long long>(blockIdx.x) * kGroups + group;
+template <int kVecs, int kThreads, int kForm, bool kFp32>
+__global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 4 : 1)
+add_rms_norm(const NormParams p, const Share share) {
+  __shared__ __align__(16) float s_part[2][kPartFloats];
+  const int lanes = 32 * share.warps, group = threadIdx.x / lanes, tid = threadIdx.x - group * lanes;
+  const int lane = tid & 31, warp = tid >> 5;
+  const long long row = static_cast<long long>(blockIdx.x) * share.rows + group;
+  if (threadIdx.x < kPartFloats) s_part[0][threadIdx.x] = 0.f;
+  __syncthreads();
   if (row >= p.rows) return;                               // (all warps of a row alike)
   const size_t at = static_cast<size_t>(row) * p.vecs;
 
-  uint4 q[kVecs];
+  uint4 q[kVecs], r[kVecs];
+#pragma unroll
+  for (int i = 0; i < kVecs; ++i) {
+    const int v = tid + i * lanes;
+    q[i] = r[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (v < p.vecs) {
+      q[i] = p.x[at + v];
+      if (p.residual != nullptr) r[i] = p.residual[at + v];
+    }
+  }
   float ss = 0.f;
 #pragma unroll
   for (int i = 0; i < kVecs; ++i) {
-    const int v = tid + i * kLanes;
-    q[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (v < p.vecs) q[i] = p.x[at + v];
-  }
-  if (p.residual != nullptr) {
-    uint4 r[kVecs];
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-      const int v = tid + i * kLanes;
-      r[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (v < p.vecs) r[i] = p.residual[at + v];
-    }
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-      float a[8], b[8];
-      unpack8(q[i], a);
-      unpack8(r[i], b);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) a[j] += b[j];
-      q[i] = pack8(a);
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < kVecs; ++i) {
-    float a[8];
-    unpack8(q[i], a);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) ss = fmaf(a[j], a[j], ss);
-    const int v = tid + i * kLanes;
+    if (p.residual != nullptr) q[i] = add8(q[i], r[i]);
+    ss = squares8(q[i], ss);
+    const int v = tid + i * lanes;
     if (p.sum != nullptr && v < p.vecs) p.sum[at + v] = q[i];
   }
-  ss = row_sum<kWarps>(ss, s_part[0] + group * kWarps, group, warp, lane);
+  ss = moe::warp_sum(ss);
+  if (share.warps > 1) {
+    float* part = part_of(s_part[0], group, share.warps);
+    if (lane == 0) part[warp] = ss;
+    row_sync(group, share.warps);
+    ss = sum_of(part, share.warps, lane);
+  }
   const float rstd = rstd_of(ss, p.cols, p.eps);
 
   float row_scale = 1.f;
-  if (p.form == MOE_FORM_ROWS) {
+  if constexpr (kForm == MOE_FORM_ROWS) {
     float m = 0.f;
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-      const int v = tid + i * kLanes;
+      const int v = tid + i * lanes;
       if (v < p.vecs) {
         float a[8], g[8];
         unpack8(q[i], a);
-        load_gain(p.gain, p.gain_fp32, p.gain_offset, v, g);
+        load_gain<kFp32>(p.gain, p.gain_offset, v, g);
 #pragma unroll
         for (int j = 0; j < 8; ++j) a[j] = a[j] * rstd * g[j];
         m = fmaxf(m, amax8(a));
       }
     }
-    m = row_max<kWarps>(m, s_part[1] + group * kWarps, group, warp, lane);
+    m = row_max(m, part_of(s_part[1], group, share.warps), group, share.warps, warp, lane);
     row_scale = blk::scale_of(m);
     if (tid == 0) static_cast<float*>(p.scales)[row] = row_scale;
   }
-
 #pragma unroll
   for (int i = 0; i < kVecs; ++i) {
-    const int v = tid + i * kLanes;
-    if (i * kLanes >= p.vecs) break;                       // (uniform: the shuffles need every lane)
+    const int v = tid + i * lanes;
+    if (i * lanes >= p.vecs) break;                       // (uniform: the shuffles need every lane)
     const bool mine = v < p.vecs;
     float a[8];
     unpack8(q[i], a);
     if (mine) {
       float g[8];
-      load_gain(p.gain, p.gain_fp32, p.gain_offset, v, g);
+      load_gain<kFp32>(p.gain, p.gain_offset, v, g);
 #pragma unroll
       for (int j = 0; j < 8; ++j) a[j] = a[j] * rstd * g[j];
       if (p.out != nullptr) p.out[at + v] = pack8(a);
     }
-    if (p.form == MOE_FORM_BLK) {                          // 16 lanes hold a block of 128
+    if constexpr (kForm == MOE_FORM_BLK) {                          // 16 lanes hold a block of 128
       float m = amax8(a);
 #pragma unroll
       for (int off = 8; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor_sync(kFull, m, off));
@@ -205,7 +216,7 @@ add_rms_norm(const NormParams p) {
         p.codes[at + v] = make_uint2(w[0], w[1]);
         if ((lane & 15) == 0) static_cast<float*>(p.scales)[static_cast<size_t>(v >> 4) * p.rows + row] = sc;
       }
-    } else if (p.form == MOE_FORM_MX) {                    // four lanes a block of 32, sixteen a word of scale bytes
+    } else if constexpr (kForm == MOE_FORM_MX) {                    // four lanes a block of 32, sixteen a word of scale bytes
       float m = amax8(a);
       m = fmaxf(m, __shfl_xor_sync(kFull, m, 1));
       m = fmaxf(m, __shfl_xor_sync(kFull, m, 2));
@@ -219,7 +230,7 @@ add_rms_norm(const NormParams p) {
                                      mx::pack4(a[4] * inv, a[5] * inv, a[6] * inv, a[7] * inv));
         if ((lane & 15) == 0) static_cast<uint32_t*>(p.scales)[static_cast<size_t>(v >> 4) * p.rows + row] = word;
       }
-    } else if (p.form == MOE_FORM_ROWS) {
+    } else if constexpr (kForm == MOE_FORM_ROWS) {
       uint32_t w[2];
       blk::pack(a, row_scale, w);
       if (mine) p.codes[at + v] = make_uint2(w[0], w[1]);
@@ -227,44 +238,101 @@ add_rms_norm(const NormParams p) {
   }
 }
 
-// Rows group, group + groups, ...; the columns of a lane are the same in all of them.
-template <int kWarps, int kVecs>
-__global__ void __launch_bounds__(kWarps * 32 > kBlock ? kWarps * 32 : kBlock)
-norm_backward(const NormGradParams p) {
-  constexpr int kGroups = kWarps * 32 >= kBlock ? 1 : kBlock / (kWarps * 32);
-  constexpr int kLanes = kWarps * 32;
-  __shared__ float s_part[4][kGroups * kWarps];
-  extern __shared__ float s_gain[];                        // [kGroups - 1][cols]
-  const int lane = threadIdx.x & 31, group = threadIdx.x / kLanes, tid = threadIdx.x % kLanes, warp = tid >> 5;
-  float acc[kVecs][8];
+// The ring: groups of neighbouring rows of up to three tensors, `depth` groups deep, filled by one thread.
+struct Ring {
+  uint64_t full[kMaxRing];
+  int abort_flag;
+};
+__device__ __forceinline__ void ring_init(Ring* ring, int depth) {
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < depth; ++i) ptx::mbar_init(ptx::smem_u32(&ring->full[i]), 1);
+    ring->abort_flag = 0;
+    ptx::fence_barrier_init();
+  }
+  __syncthreads();
+}
+// A wait gave up (never in a sound run): reported, and copies in flight get time to land before the CTA ends.
+__device__ __forceinline__ void ring_gave_up(int32_t* status, int where) {
+  if (threadIdx.x == 0) {
+    atomicCAS(&status[0], 0, MOE_ERR_TIMEOUT);
+    atomicCAS(&status[1], 0, where);
+  }
+  for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+}
+
+template <int kVecs, int kThreads, int kCtas, bool kFp32>
+__global__ void __launch_bounds__(kThreads, kCtas)
+norm_backward(const NormGradParams p, const Share share) {
+  extern __shared__ __align__(16) unsigned char s_ring[];
+  __shared__ __align__(16) float s_part[4][kPartFloats];
+  __shared__ Ring ring;
+  const int lanes = 32 * share.warps, group = threadIdx.x / lanes, tid = threadIdx.x - group * lanes;
+  const int lane = tid & 31, warp = tid >> 5, groups = share.rows;
+  for (int i = threadIdx.x; i < 4 * kPartFloats; i += blockDim.x) s_part[0][i] = 0.f;
+  const bool with_sum = p.d_sum != nullptr && p.d_x != nullptr;
+  ptx::launch_dependents();
+  const uint32_t row_bytes = p.cols * 2, tensor_bytes = groups * row_bytes;
+  const uint32_t slot_bytes = with_sum ? 3 * tensor_bytes : 2 * tensor_bytes;
+  const long long step = static_cast<long long>(gridDim.x) * groups;
+  ring_init(&ring, p.ring);
+  auto fill = [&](int slot, long long row) {
+    if (row >= p.rows) return;
+    const uint32_t bytes = static_cast<uint32_t>(p.rows - row < groups ? p.rows - row : groups) * row_bytes;
+    const uint32_t full = ptx::smem_u32(&ring.full[slot]), dst = ptx::smem_u32(s_ring) + slot * slot_bytes;
+    ptx::mbar_expect_tx(full, with_sum ? 3 * bytes : 2 * bytes);
+    ptx::bulk_load(dst, p.s + row * p.vecs, bytes, full);
+    ptx::bulk_load(dst + tensor_bytes, p.d_out + row * p.vecs, bytes, full);
+    if (with_sum) ptx::bulk_load(dst + 2 * tensor_bytes, p.d_sum + row * p.vecs, bytes, full);
+  };
+  long long row0 = static_cast<long long>(blockIdx.x) * groups;
+  if (threadIdx.x == 0)
+    for (int i = 0; i < p.ring; ++i) fill(i, row0 + i * step);
+
+  // a lane's columns are the same in all rows: its gains stay in registers, where a thread has enough of them
+  constexpr bool kKeepGain = kThreads <= 256;
+  float acc[kVecs][8], gains[kKeepGain ? kVecs : 1][8];
 #pragma unroll
   for (int i = 0; i < kVecs; ++i)
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[i][j] = 0.f;
-
-  int turn = 0;
-  for (long long row = static_cast<long long>(blockIdx.x) * kGroups + group; row < p.rows;
-       row += static_cast<long long>(gridDim.x) * kGroups) {
-    const size_t at = static_cast<size_t>(row) * p.vecs;
-    uint4 sq[kVecs], dq[kVecs];
+  if constexpr (kKeepGain) {
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-      const int v = tid + i * kLanes;
-      sq[i] = dq[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (v < p.vecs) {
-        sq[i] = p.s[at + v];
-        dq[i] = p.d_out[at + v];
-      }
+    for (int i = 0; i < kVecs; ++i)
+      if (tid + i * lanes < p.vecs) load_gain<kFp32>(p.gain, p.gain_offset, tid + i * lanes, gains[i]);
+  }
+  auto gain_of = [&](int i, int v, float (&g)[8]) {
+    if constexpr (kKeepGain) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) g[j] = gains[i][j];
+    } else {
+      load_gain<kFp32>(p.gain, p.gain_offset, v, g);
     }
+  };
+  int slot = 0, turn = 0;
+  uint32_t phase = 0;
+  for (; row0 < p.rows; row0 += step) {
+    const bool ok = ptx::mbar_wait(ptx::smem_u32(&ring.full[slot]), phase, &ring.abort_flag);
+    const long long row = row0 + group;
+    const bool live = row < p.rows;
+    const size_t at = static_cast<size_t>(row) * p.vecs;
+    const unsigned char* base = s_ring + slot * slot_bytes + group * row_bytes;
+    const uint4* ss_row = reinterpret_cast<const uint4*>(base);
+    const uint4* d_row = reinterpret_cast<const uint4*>(base + tensor_bytes);
+    const uint4* e_row = reinterpret_cast<const uint4*>(base + 2 * tensor_bytes);
+    uint4 sq[kVecs], dq[kVecs], eq[kVecs];
     float ss = 0.f, dot = 0.f;                             // sums of s^2 and of s d_out gain
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-      const int v = tid + i * kLanes;
-      if (v < p.vecs) {
+      const int v = tid + i * lanes;
+      sq[i] = dq[i] = eq[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (live && v < p.vecs) {
+        sq[i] = ss_row[v];
+        dq[i] = d_row[v];
+        if (with_sum) eq[i] = e_row[v];
         float s[8], d[8], g[8];
         unpack8(sq[i], s);
         unpack8(dq[i], d);
-        load_gain(p.gain, p.gain_fp32, p.gain_offset, v, g);
+        gain_of(i, v, g);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           ss = fmaf(s[j], s[j], ss);
@@ -272,56 +340,56 @@ norm_backward(const NormGradParams p) {
         }
       }
     }
-    // two pairs of arrays in turn: a row's reads are over when the next row but one writes (the warps meet in between)
     ss = moe::warp_sum(ss);
     dot = moe::warp_sum(dot);
-    if constexpr (kWarps > 1) {
-      float* part_s = s_part[2 * turn] + group * kWarps;
-      float* part_d = s_part[2 * turn + 1] + group * kWarps;
-      if (lane == 0) {
-        part_s[warp] = ss;
-        part_d[warp] = dot;
-      }
-      row_sync<kWarps>(group);
-      ss = moe::warp_sum(lane < kWarps ? part_s[lane] : 0.f);
-      dot = moe::warp_sum(lane < kWarps ? part_d[lane] : 0.f);
-      turn ^= 1;
+    // two pairs of arrays in turn: a row's reads are over when the next row but one writes (the CTA meets in between)
+    float* part_s = part_of(s_part[2 * turn], group, share.warps);
+    float* part_d = part_of(s_part[2 * turn + 1], group, share.warps);
+    if (share.warps > 1 && lane == 0) {
+      part_s[warp] = ss;
+      part_d[warp] = dot;
     }
+    if (__syncthreads_or(!ok)) {                           // the slot has been read, the warps' sums are written
+      ring_gave_up(p.status, 301);
+      return;
+    }
+    if (threadIdx.x == 0) fill(slot, row0 + p.ring * step);
+    if (++slot == p.ring) { slot = 0; phase ^= 1u; }
+    if (share.warps > 1) {
+      ss = sum_of(part_s, share.warps, lane);
+      dot = sum_of(part_d, share.warps, lane);
+    }
+    turn ^= 1;
     const float rstd = rstd_of(ss, p.cols, p.eps);
     const float mean = __fdiv_rn(dot * rstd, static_cast<float>(p.cols));   // mean of g h
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-      const int v = tid + i * kLanes;
-      if (v < p.vecs) {
-        float s[8], d[8], g[8], o[8];
+      const int v = tid + i * lanes;
+      if (live && v < p.vecs) {
+        float s[8], d[8], o[8], g[8];
         unpack8(sq[i], s);
         unpack8(dq[i], d);
-        load_gain(p.gain, p.gain_fp32, p.gain_offset, v, g);
+        unpack8(eq[i], o);
+        gain_of(i, v, g);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const float h = s[j] * rstd;
           acc[i][j] = fmaf(d[j], h, acc[i][j]);
-          o[j] = rstd * (d[j] * g[j] - h * mean);
+          o[j] += rstd * (d[j] * g[j] - h * mean);
         }
-        if (p.d_x != nullptr) {
-          if (p.d_sum != nullptr) {
-            float a[8];
-            unpack8(p.d_sum[at + v], a);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] += a[j];
-          }
-          p.d_x[at + v] = pack8(o);
-        }
+        if (p.d_x != nullptr) p.d_x[at + v] = pack8(o);
       }
     }
   }
 
   if (p.partial == nullptr) return;
-  if constexpr (kGroups > 1) {                             // the CTA's rows in the order of their groups
+  if (groups > 1) {                             // the CTA's rows in the order of their groups
+    float* s_gain = reinterpret_cast<float*>(s_ring);      // [groups - 1][cols]: the ring is idle
+    __syncthreads();
     if (group > 0) {
 #pragma unroll
       for (int i = 0; i < kVecs; ++i) {
-        const int v = tid + i * kLanes;
+        const int v = tid + i * lanes;
         if (v < p.vecs) {
           float4* d = reinterpret_cast<float4*>(s_gain + static_cast<size_t>(group - 1) * p.cols) + 2 * v;
           d[0] = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
@@ -333,9 +401,9 @@ norm_backward(const NormGradParams p) {
     if (group > 0) return;
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-      const int v = tid + i * kLanes;
+      const int v = tid + i * lanes;
       if (v < p.vecs) {
-        for (int o = 0; o < kGroups - 1; ++o) {
+        for (int o = 0; o < groups - 1; ++o) {
           const float* src = s_gain + static_cast<size_t>(o) * p.cols + 8 * v;
 #pragma unroll
           for (int j = 0; j < 8; ++j) acc[i][j] += src[j];
@@ -346,7 +414,7 @@ norm_backward(const NormGradParams p) {
   float4* dst = reinterpret_cast<float4*>(p.partial + static_cast<size_t>(blockIdx.x) * p.cols);
 #pragma unroll
   for (int i = 0; i < kVecs; ++i) {
-    const int v = tid + i * kLanes;
+    const int v = tid + i * lanes;
     if (v < p.vecs) {
       dst[2 * v] = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
       dst[2 * v + 1] = make_float4(acc[i][4], acc[i][5], acc[i][6], acc[i][7]);
@@ -354,70 +422,91 @@ norm_backward(const NormGradParams p) {
   }
 }
 
-// d_gain of 32 columns: eight warps take every eighth partial row, then the eight sums in order.
-__global__ void __launch_bounds__(kBlock)
+// d_gain of 32 columns: the CTA's warps take every kSumWarps-th partial row, then the warps' sums in order.
+constexpr int kSumWarps = 32;
+__global__ void __launch_bounds__(kSumWarps * 32)
 norm_gain_sum(const float* __restrict__ partial, int parts, int cols, float* __restrict__ d_gain) {
-  __shared__ float s_sum[kBlock / 32][32];
+  constexpr int kAhead = 8;                                // rows whose loads are in flight together
+  __shared__ float s_sum[kSumWarps][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+  ptx::wait_for_previous_kernel();
   float sum = 0.f;
-  if (c < cols)
-    for (int i = warp; i < parts; i += kBlock / 32) sum += partial[static_cast<size_t>(i) * cols + c];
+  if (c < cols) {
+    for (int i = warp; i < parts; i += kSumWarps * kAhead) {
+      float v[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        v[u] = i + u * kSumWarps < parts ? __ldcg(partial + static_cast<size_t>(i + u * kSumWarps) * cols + c) : 0.f;
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) sum += v[u];
+    }
+  }
   s_sum[warp][lane] = sum;
   __syncthreads();
   if (warp == 0 && c < cols) {
     sum = 0.f;
-    for (int i = 0; i < kBlock / 32; ++i) sum += s_sum[i][lane];
+#pragma unroll
+    for (int i = 0; i < kSumWarps; ++i) sum += s_sum[i][lane];
     d_gain[c] = sum;
   }
 }
 
-// Warps per row: the smallest power of two with which `vecs` vectors fit, kVecs to a lane.
-int warps_of(int vecs, int per_lane) {
-  int w = 1;
-  while (w < 32 && w * 32 * per_lane < vecs) w *= 2;
-  return w;
+// As few warps to a row as hold its vectors, `per_lane` to a lane, and as many rows to a CTA as fit into 256 threads.
+Share share_of(int vecs, int per_lane) {
+  Share s;
+  s.warps = (vecs - 1) / (32 * per_lane) + 1;
+  s.rows = s.warps >= 8 ? 1 : 8 / s.warps;
+  return s;
 }
-// Vectors per lane: 4, so that a row's loads are in flight together and few warps have to meet.
-int vecs_per_lane(int) { return 4; }
+int threads_of(const Share& s) { return 32 * s.warps * s.rows; }
 
+using NormKernel = void (*)(NormParams, Share);
+template <int kVecs, int kThreads>
+NormKernel norm_kernel(const moe_rms_norm_args& a) {
+  switch (a.form) {
+    case MOE_FORM_ROWS:
+      return a.gain_fp32 ? add_rms_norm<kVecs, kThreads, MOE_FORM_ROWS, true> : add_rms_norm<kVecs, kThreads, MOE_FORM_ROWS, false>;
+    case MOE_FORM_MX:
+      return a.gain_fp32 ? add_rms_norm<kVecs, kThreads, MOE_FORM_MX, true> : add_rms_norm<kVecs, kThreads, MOE_FORM_MX, false>;
+    case MOE_FORM_BLK:
+      return a.gain_fp32 ? add_rms_norm<kVecs, kThreads, MOE_FORM_BLK, true> : add_rms_norm<kVecs, kThreads, MOE_FORM_BLK, false>;
+    default:
+      return a.gain_fp32 ? add_rms_norm<kVecs, kThreads, MOE_FORM_NONE, true> : add_rms_norm<kVecs, kThreads, MOE_FORM_NONE, false>;
+  }
+}
+
+// norm_backward: vectors of a lane, and the CTAs of an SM that its registers allow.
+struct BackwardPlan {
+  Share share;
+  int vecs, ctas, depth;
+  size_t bytes;                           // of the ring
+};
+BackwardPlan backward_plan(const moe_ctx* ctx, int cols) {
+  constexpr size_t kSm = kRingBytes;
+  BackwardPlan b;
+  const int vecs = cols / 8;
+  b.vecs = vecs <= 512 ? moe_knob_value(ctx, "norm_bv", 2) : 4;
+  b.share = share_of(vecs, b.vecs);
+  const int threads = threads_of(b.share);
+  const size_t slot = static_cast<size_t>(3) * b.share.rows * cols * 2;   // (as if d_sum were given)
+  b.ctas = threads > 256 ? 1 : b.vecs == 2 ? 3 : 2;
+  if (slot * 2 * b.ctas > kSm) b.ctas = slot * 4 <= kSm ? 2 : 1;
+  b.depth = static_cast<int>(kSm / b.ctas / slot);
+  if (b.depth > kMaxRing) b.depth = kMaxRing;
+  if (b.depth < 1) b.depth = 1;
+  b.bytes = b.depth * slot;
+  return b;
+}
+using BackwardKernel = void (*)(NormGradParams, Share);
+template <bool kFp32>
+BackwardKernel backward_kernel(const BackwardPlan& b) {
+  return b.vecs == 2 ? norm_backward<2, 256, 3, kFp32> : threads_of(b.share) <= 256 ? norm_backward<4, 256, 2, kFp32>
+                                                                                  : norm_backward<4, 1024, 1, kFp32>;
+}
 // CTAs of norm_backward, the same for its scratch and its launch.
-int backward_ctas(const moe_ctx* ctx, long long rows, int vecs) {
-  const int lanes = 32 * warps_of(vecs, vecs_per_lane(vecs));
-  const int groups = lanes >= kBlock ? 1 : kBlock / lanes;
-  const long long need = (rows + groups - 1) / groups, room = static_cast<long long>(ctx->num_sms) * (lanes > kBlock ? 1 : 2);
+int backward_ctas(const moe_ctx* ctx, long long rows, const BackwardPlan& b) {
+  const long long need = (rows + b.share.rows - 1) / b.share.rows, room = static_cast<long long>(ctx->num_sms) * b.ctas;
   return static_cast<int>(need < room ? need : room);
-}
-
-template <int kVecs>
-cudaError_t launch_norm(const NormParams& p, int warps, cudaStream_t stream) {
-  const int groups = warps * 32 >= kBlock ? 1 : kBlock / (warps * 32);
-  const int threads = warps * 32 > kBlock ? warps * 32 : kBlock;
-  const unsigned grid = static_cast<unsigned>((p.rows + groups - 1) / groups);
-  switch (warps) {
-    case 1: add_rms_norm<1, kVecs><<<grid, threads, 0, stream>>>(p); break;
-    case 2: add_rms_norm<2, kVecs><<<grid, threads, 0, stream>>>(p); break;
-    case 4: add_rms_norm<4, kVecs><<<grid, threads, 0, stream>>>(p); break;
-    case 8: add_rms_norm<8, kVecs><<<grid, threads, 0, stream>>>(p); break;
-    case 16: add_rms_norm<16, kVecs><<<grid, threads, 0, stream>>>(p); break;
-    default: add_rms_norm<32, kVecs><<<grid, threads, 0, stream>>>(p); break;
-  }
-  return cudaGetLastError();
-}
-
-template <int kVecs>
-cudaError_t launch_backward(const NormGradParams& p, int warps, int ctas, cudaStream_t stream) {
-  const int groups = warps * 32 >= kBlock ? 1 : kBlock / (warps * 32);
-  const int threads = warps * 32 > kBlock ? warps * 32 : kBlock;
-  const size_t smem = p.partial ? static_cast<size_t>(groups - 1) * p.cols * 4 : 0;   // at most 7 x 1024 values
-  switch (warps) {
-    case 1: norm_backward<1, kVecs><<<ctas, threads, smem, stream>>>(p); break;
-    case 2: norm_backward<2, kVecs><<<ctas, threads, smem, stream>>>(p); break;
-    case 4: norm_backward<4, kVecs><<<ctas, threads, smem, stream>>>(p); break;
-    case 8: norm_backward<8, kVecs><<<ctas, threads, smem, stream>>>(p); break;
-    case 16: norm_backward<16, kVecs><<<ctas, threads, smem, stream>>>(p); break;
-    default: norm_backward<32, kVecs><<<ctas, threads, smem, stream>>>(p); break;
-  }
-  return cudaGetLastError();
 }
 
 }  // namespace
@@ -425,30 +514,58 @@ cudaError_t launch_backward(const NormGradParams& p, int warps, int ctas, cudaSt
 namespace moe {
 
 cudaError_t launch_add_rms_norm(moe_ctx* ctx, const moe_rms_norm_args& a, cudaStream_t stream) {
-  const NormParams p{static_cast<const uint4*>(a.x), static_cast<const uint4*>(a.residual), a.gain,
-                     static_cast<uint4*>(a.sum_out), static_cast<uint4*>(a.out), static_cast<uint2*>(a.codes), a.scales,
-                     a.rows, a.cols / 8, a.cols, a.eps, a.gain_offset, a.gain_fp32, a.form};
+  const NormParams p{static_cast<const uint4*>(a.x), static_cast<const uint4*>(a.residual), a.gain, static_cast<uint4*>(a.sum_out),
+                     static_cast<uint4*>(a.out), static_cast<uint2*>(a.codes), a.scales, a.rows, a.cols / 8, a.cols, a.eps,
+                     a.gain_offset};
   ctx->last_launches += 1;
-  return launch_norm<4>(p, warps_of(p.vecs, 4), stream);
+  const bool few = moe_knob_value(ctx, "norm_vecs", a.rows * p.vecs <= 2048LL * ctx->num_sms ? 1 : 4) == 1 && p.vecs <= 1024;
+  const Share share = share_of(p.vecs, few ? 1 : 4);
+  const int threads = threads_of(share);
+  const unsigned grid = static_cast<unsigned>((a.rows + share.rows - 1) / share.rows);
+  auto kernel = few ? norm_kernel<1, 1024>(a) : threads <= 256 ? norm_kernel<4, 256>(a) : norm_kernel<4, 1024>(a);
+  kernel<<<grid, threads, 0, stream>>>(p, share);
+  return cudaGetLastError();
 }
 
 size_t rms_norm_scratch_bytes(const moe_ctx* ctx, long long rows, int cols) {
-  return static_cast<size_t>(backward_ctas(ctx, rows, cols / 8)) * cols * 4;
+  return static_cast<size_t>(backward_ctas(ctx, rows, backward_plan(ctx, cols))) * cols * 4;
 }
 
 cudaError_t launch_rms_norm_backward(moe_ctx* ctx, const moe_rms_norm_grad_args& a, cudaStream_t stream) {
   if (a.rows == 0) return a.d_gain ? cudaMemsetAsync(a.d_gain, 0, static_cast<size_t>(a.cols) * 4, stream) : cudaSuccess;
-  const int vecs = a.cols / 8, ctas = backward_ctas(ctx, a.rows, vecs);
+  const BackwardPlan b = backward_plan(ctx, a.cols);
+  const int ctas = backward_ctas(ctx, a.rows, b), threads = threads_of(b.share);
   const NormGradParams p{static_cast<const uint4*>(a.s), a.gain, static_cast<const uint4*>(a.d_out),
                          static_cast<const uint4*>(a.d_sum), static_cast<uint4*>(a.d_x),
-                         a.d_gain ? static_cast<float*>(a.scratch) : nullptr, a.rows, vecs, a.cols, a.eps, a.gain_offset,
-                         a.gain_fp32};
-  cudaError_t e = launch_backward<4>(p, warps_of(vecs, 4), ctas, stream);
+                         a.d_gain ? static_cast<float*>(a.scratch) : nullptr, ctx->d_status, a.rows, a.cols / 8, a.cols, a.eps,
+                         a.gain_offset, b.depth};
+  // (the ring's bytes also hold the groups' sums of the gain: 4 (rows - 1) cols of at least 6 rows cols)
+  auto kernel = a.gain_fp32 ? backward_kernel<true>(b) : backward_kernel<false>(b);
+  kernel<<<ctas, threads, b.bytes, stream>>>(p, b.share);
+  cudaError_t e = cudaGetLastError();
   ctx->last_launches += 1;
   if (e == cudaSuccess && a.d_gain) {
-    norm_gain_sum<<<(a.cols + 31) / 32, kBlock, 0, stream>>>(p.partial, ctas, a.cols, a.d_gain);
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute attr{};
+    cfg.gridDim = dim3((a.cols + 31) / 32);
+    cfg.blockDim = dim3(kSumWarps * 32);
+    cfg.stream = stream;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
     ctx->last_launches += 1;
-    e = cudaGetLastError();
+    e = cudaLaunchKernelEx(&cfg, norm_gain_sum, static_cast<const float*>(p.partial), ctas, static_cast<int>(a.cols), a.d_gain);
+  }
+  return e;
+}
+
+cudaError_t prepare_rms_norm(moe_ctx* ctx) {
+  cudaError_t e = cudaSuccess;
+  for (const int cols : {1024, 8192, 32768}) {             // a plan of each kind
+    const BackwardPlan b = backward_plan(ctx, cols);
+    for (const BackwardKernel kernel : {backward_kernel<false>(b), backward_kernel<true>(b)})
+      if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes);
   }
   return e;
 }
