@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libmoe_b200.so")
@@ -136,6 +137,16 @@ class moe_adapter_args(C.Structure):
         (n, C.c_int32) for n in ("N", "K", "rank", "adapters", "segments")]
 
 
+def _packer(layout):
+    """Packs a call's arguments as the C structure `layout` holds them: a third of the time that building one takes, which
+    counts where the kernel itself takes a few microseconds."""
+    codes = {C.c_void_p: "P", C.c_int64: "q", C.c_size_t: "N", C.c_int32: "i", C.c_float: "f"}
+    return struct.Struct("@" + "".join(codes[kind] for _, kind in layout._fields_)).pack
+
+
+_pack_rms_norm, _pack_rms_norm_grad = _packer(moe_rms_norm_args), _packer(moe_rms_norm_grad_args)
+_pack_balance, _pack_adapter = _packer(moe_balance_args), _packer(moe_adapter_args)
+
 _lib = None
 
 
@@ -200,11 +211,9 @@ def load_library() -> C.CDLL:
     lib.moe_get_workspace_layout_blk.argtypes = [C.POINTER(moe_shape), C.POINTER(moe_workspace_layout_blk)]
     lib.moe_fused_forward_blk.argtypes = [vp, vp, f32p, f32p, C.POINTER(moe_route_rule), vp, f32p, vp, f32p, vp, f32p,
                                           vp, vp, C.c_size_t, vp]
-    lib.moe_add_rms_norm.argtypes = [vp, C.POINTER(moe_rms_norm_args), vp]
-    lib.moe_rms_norm_backward.argtypes = [vp, C.POINTER(moe_rms_norm_grad_args), vp]
-    lib.moe_balance_loss.argtypes = [vp, C.POINTER(moe_balance_args), i32p, i32p, f32p, f32p, vp, C.c_size_t, vp]
-    lib.moe_balance_loss_backward.argtypes = [vp, C.POINTER(moe_balance_args), i32p, i32p, f32p, f32p, f32p, vp]
-    lib.moe_add_adapters.argtypes = [vp, C.POINTER(moe_adapter_args), vp]
+    lib.moe_add_rms_norm.argtypes = lib.moe_rms_norm_backward.argtypes = lib.moe_add_adapters.argtypes = [vp, vp, vp]
+    lib.moe_balance_loss.argtypes = [vp, vp, i32p, i32p, f32p, f32p, vp, C.c_size_t, vp]
+    lib.moe_balance_loss_backward.argtypes = [vp, vp, i32p, i32p, f32p, f32p, f32p, vp]
     lib.moe_rms_norm_scratch_bytes.argtypes = [vp, C.c_int64, C.c_int32]
     lib.moe_balance_scratch_bytes.argtypes = [vp, C.c_int32]
     lib.moe_adapter_scratch_bytes.argtypes = [vp, C.c_int64, C.c_int32, C.c_int32]
@@ -238,6 +247,15 @@ def _ptr(t):
     return t.data_ptr()
 
 
+def _addr(t):
+    """Device address of a tensor, None -> 0."""
+    if t is None:
+        return 0
+    if t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError("tensors passed to the MoE library must be contiguous")
+
+
 _torch = None
 
 
@@ -251,7 +269,7 @@ def _stream(stream):
     raw = getattr(_torch._C, "_cuda_getCurrentRawStream", None)      # the handle without a Stream object around it
     if raw is None:
         return _torch.cuda.current_stream().cuda_stream
-    return raw(_torch.cuda.current_device())
+    return raw(_torch._C._cuda_getDevice())
 
 
 def _check(code: int, where: str):
@@ -278,13 +296,16 @@ def _lookup(table, name, what):
 
 def _gain_fp32(gain):
     """1 for an fp32 gain, 0 for a bf16 one."""
-    if gain is None or gain.element_size() not in (2, 4):
-        raise ValueError("the gain is a bf16 or fp32 tensor")
-    return 1 if gain.element_size() == 4 else 0
+    size = 0 if gain is None else gain.element_size()
+    if size == 2:
+        return 0
+    if size == 4:
+        return 1
+    raise ValueError("the gain is a bf16 or fp32 tensor")
 
 
 def _size(t):
-    return 0 if t is None else t.numel() * t.element_size()
+    return 0 if t is None else t.nbytes
 
 
 def moe_parse_tuning(text):
@@ -563,9 +584,9 @@ class Context:
     def moe_add_rms_norm(self, x, residual, gain, rows, cols, sum_out=None, out=None, codes=None, scales=None,
                          form="none", eps=1e-6, gain_offset=0.0, stream=None):
         """residual may be None; form is "none", "rows", "mx" or "blk"; the gain is bf16 or fp32."""
-        args = moe_rms_norm_args(_ptr(x), _ptr(residual), _ptr(gain), _ptr(sum_out), _ptr(out), _ptr(codes), _ptr(scales),
-                                 rows, cols, _gain_fp32(gain), _lookup(FORMS, form, "form"), eps, gain_offset)
-        _check(self._lib.moe_add_rms_norm(self._handle, C.byref(args), _stream(stream)), "moe_add_rms_norm")
+        args = _pack_rms_norm(_addr(x), _addr(residual), _addr(gain), _addr(sum_out), _addr(out), _addr(codes),
+                              _addr(scales), rows, cols, _gain_fp32(gain), _lookup(FORMS, form, "form"), eps, gain_offset)
+        _check(self._lib.moe_add_rms_norm(self._handle, args, _stream(stream)), "moe_add_rms_norm")
 
     def rms_norm_scratch_bytes(self, rows, cols) -> int:
         """Bytes of the scratch moe_rms_norm_backward needs when d_gain is asked for."""
@@ -574,9 +595,9 @@ class Context:
     def moe_rms_norm_backward(self, s, gain, d_out, rows, cols, d_x, d_gain, scratch=None, d_sum=None, eps=1e-6,
                               gain_offset=0.0, stream=None):
         """d_x or d_gain may be None; scratch is needed for d_gain only."""
-        args = moe_rms_norm_grad_args(_ptr(s), _ptr(gain), _ptr(d_out), _ptr(d_sum), _ptr(d_x), _ptr(d_gain),
-                                      _ptr(scratch), _size(scratch), rows, cols, _gain_fp32(gain), eps, gain_offset)
-        _check(self._lib.moe_rms_norm_backward(self._handle, C.byref(args), _stream(stream)), "moe_rms_norm_backward")
+        args = _pack_rms_norm_grad(_addr(s), _addr(gain), _addr(d_out), _addr(d_sum), _addr(d_x), _addr(d_gain),
+                                   _addr(scratch), _size(scratch), rows, cols, _gain_fp32(gain), eps, gain_offset)
+        _check(self._lib.moe_rms_norm_backward(self._handle, args, _stream(stream)), "moe_rms_norm_backward")
 
     # ---- balance loss of the router
     def balance_scratch_bytes(self, sequences=1) -> int:
@@ -584,18 +605,18 @@ class Context:
 
     def moe_balance_loss(self, logits, topk_ids, counts, tokens, mean, loss, scratch, score="softmax", coef=1.0,
                          z_coef=0.0, sequences=1, seq_offsets=None, token_mask=None, stream=None):
-        args = moe_balance_args(_ptr(logits), _ptr(topk_ids), _ptr(seq_offsets), _ptr(token_mask), sequences,
-                                _lookup(SCORES, score, "score"), coef, z_coef)
-        _check(self._lib.moe_balance_loss(self._handle, C.byref(args), _ptr(counts), _ptr(tokens), _ptr(mean), _ptr(loss),
-                                          _ptr(scratch), _size(scratch), _stream(stream)), "moe_balance_loss")
+        args = _pack_balance(_addr(logits), _addr(topk_ids), _addr(seq_offsets), _addr(token_mask), sequences,
+                             _lookup(SCORES, score, "score"), coef, z_coef)
+        _check(self._lib.moe_balance_loss(self._handle, args, _addr(counts), _addr(tokens), _addr(mean), _addr(loss),
+                                          _addr(scratch), _size(scratch), _stream(stream)), "moe_balance_loss")
 
     def moe_balance_loss_backward(self, logits, counts, tokens, d_logits, d_loss=None, add=None, score="softmax", coef=1.0,
                                   z_coef=0.0, sequences=1, seq_offsets=None, token_mask=None, stream=None):
         """d_loss: one fp32 on the device (None: 1); add: a gradient to add to, d_logits itself allowed."""
-        args = moe_balance_args(_ptr(logits), None, _ptr(seq_offsets), _ptr(token_mask), sequences,
-                                _lookup(SCORES, score, "score"), coef, z_coef)
-        _check(self._lib.moe_balance_loss_backward(self._handle, C.byref(args), _ptr(counts), _ptr(tokens), _ptr(d_loss),
-                                                   _ptr(add), _ptr(d_logits), _stream(stream)),
+        args = _pack_balance(_addr(logits), 0, _addr(seq_offsets), _addr(token_mask), sequences,
+                             _lookup(SCORES, score, "score"), coef, z_coef)
+        _check(self._lib.moe_balance_loss_backward(self._handle, args, _addr(counts), _addr(tokens), _addr(d_loss),
+                                                   _addr(add), _addr(d_logits), _stream(stream)),
                "moe_balance_loss_backward")
 
     # ---- adapters beside a shared projection
@@ -605,9 +626,9 @@ class Context:
     def moe_add_adapters(self, x, a, b, adapter_of, y_in, y_out, scratch, rows, N, K, rank, adapters, segments, offsets=None,
                          scale=None, stream=None):
         """offsets None: every row is a segment of its own; scale None: 1."""
-        args = moe_adapter_args(_ptr(x), _ptr(a), _ptr(b), _ptr(scale), _ptr(offsets), _ptr(adapter_of), _ptr(y_in),
-                                _ptr(y_out), _ptr(scratch), _size(scratch), rows, N, K, rank, adapters, segments)
-        _check(self._lib.moe_add_adapters(self._handle, C.byref(args), _stream(stream)), "moe_add_adapters")
+        args = _pack_adapter(_addr(x), _addr(a), _addr(b), _addr(scale), _addr(offsets), _addr(adapter_of), _addr(y_in),
+                             _addr(y_out), _addr(scratch), _size(scratch), rows, N, K, rank, adapters, segments)
+        _check(self._lib.moe_add_adapters(self._handle, args, _stream(stream)), "moe_add_adapters")
 
     def moe_last_device_status(self, stream=None):
         code, detail = C.c_int32(0), C.c_int32(0)
