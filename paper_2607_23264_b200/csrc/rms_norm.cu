@@ -55,6 +55,8 @@ __device__ __forceinline__ void unpack8(const uint4& q, float (&v)[8]) {
     v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
   }
 }
+// Keeps a vector packed over a point of the program: the compiler would otherwise hold the eight values it once unpacked.
+__device__ __forceinline__ void stay_packed(uint4& q) { asm volatile("" : "+r"(q.x), "+r"(q.y), "+r"(q.z), "+r"(q.w)); }
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&p);
@@ -145,24 +147,34 @@ add_rms_norm(const NormParams p, const Share share) {
   if (row >= p.rows) return;                               // (all warps of a row alike)
   const size_t at = static_cast<size_t>(row) * p.vecs;
 
-  uint4 q[kVecs], r[kVecs];
+  uint4 q[kVecs];
 #pragma unroll
   for (int i = 0; i < kVecs; ++i) {
     const int v = tid + i * lanes;
-    q[i] = r[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (v < p.vecs) {
-      q[i] = p.x[at + v];
-      if (p.residual != nullptr) r[i] = p.residual[at + v];
+    q[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (v < p.vecs) q[i] = p.x[at + v];
+  }
+  if (p.residual != nullptr) {
+    uint4 r[kVecs];
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      const int v = tid + i * lanes;
+      r[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (v < p.vecs) r[i] = p.residual[at + v];
+    }
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) q[i] = add8(q[i], r[i]);
+  }
+  if (p.sum != nullptr) {
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      const int v = tid + i * lanes;
+      if (v < p.vecs) p.sum[at + v] = q[i];
     }
   }
   float ss = 0.f;
 #pragma unroll
-  for (int i = 0; i < kVecs; ++i) {
-    if (p.residual != nullptr) q[i] = add8(q[i], r[i]);
-    ss = squares8(q[i], ss);
-    const int v = tid + i * lanes;
-    if (p.sum != nullptr && v < p.vecs) p.sum[at + v] = q[i];
-  }
+  for (int i = 0; i < kVecs; ++i) ss = squares8(q[i], ss);
   ss = moe::warp_sum(ss);
   if (share.warps > 1) {
     float* part = part_of(s_part[0], group, share.warps);
@@ -177,15 +189,12 @@ add_rms_norm(const NormParams p, const Share share) {
     float m = 0.f;
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-      const int v = tid + i * lanes;
-      if (v < p.vecs) {
-        float a[8], g[8];
-        unpack8(q[i], a);
-        load_gain<kFp32>(p.gain, p.gain_offset, v, g);
+      float a[8], g[8];
+      unpack8(q[i], a);
+      load_gain<kFp32>(p.gain, p.gain_offset, min(tid + i * lanes, p.vecs - 1), g);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) a[j] = a[j] * rstd * g[j];
-        m = fmaxf(m, amax8(a));
-      }
+      for (int j = 0; j < 8; ++j) a[j] = a[j] * rstd * g[j];
+      m = fmaxf(m, amax8(a));
     }
     m = row_max(m, part_of(s_part[1], group, share.warps), group, share.warps, warp, lane);
     row_scale = blk::scale_of(m);
@@ -196,15 +205,13 @@ add_rms_norm(const NormParams p, const Share share) {
     const int v = tid + i * lanes;
     if (i * lanes >= p.vecs) break;                       // (uniform: the shuffles need every lane)
     const bool mine = v < p.vecs;
-    float a[8];
+    // (a lane behind the row works on zeros: what it finds does not count in a maximum, even where it is NaN)
+    float a[8], g[8];
     unpack8(q[i], a);
-    if (mine) {
-      float g[8];
-      load_gain<kFp32>(p.gain, p.gain_offset, v, g);
+    load_gain<kFp32>(p.gain, p.gain_offset, min(v, p.vecs - 1), g);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) a[j] = a[j] * rstd * g[j];
-      if (p.out != nullptr) p.out[at + v] = pack8(a);
-    }
+    for (int j = 0; j < 8; ++j) a[j] = a[j] * rstd * g[j];
+    if (p.out != nullptr && mine) p.out[at + v] = pack8(a);
     if constexpr (kForm == MOE_FORM_BLK) {                          // 16 lanes hold a block of 128
       float m = amax8(a);
 #pragma unroll
@@ -260,9 +267,10 @@ __device__ __forceinline__ void ring_gave_up(int32_t* status, int where) {
   for (int i = 0; i < 2000; ++i) __nanosleep(1000);
 }
 
-template <int kVecs, int kThreads, int kCtas, bool kFp32>
-__global__ void __launch_bounds__(kThreads, kCtas)
+template <int kThreads, bool kFp32>
+__global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 2 : 1)
 norm_backward(const NormGradParams p, const Share share) {
+  constexpr int kVecs = 4;
   extern __shared__ __align__(16) unsigned char s_ring[];
   __shared__ __align__(16) float s_part[4][kPartFloats];
   __shared__ Ring ring;
@@ -270,7 +278,6 @@ norm_backward(const NormGradParams p, const Share share) {
   const int lane = tid & 31, warp = tid >> 5, groups = share.rows;
   for (int i = threadIdx.x; i < 4 * kPartFloats; i += blockDim.x) s_part[0][i] = 0.f;
   const bool with_sum = p.d_sum != nullptr && p.d_x != nullptr;
-  ptx::launch_dependents();
   const uint32_t row_bytes = p.cols * 2, tensor_bytes = groups * row_bytes;
   const uint32_t slot_bytes = with_sum ? 3 * tensor_bytes : 2 * tensor_bytes;
   const long long step = static_cast<long long>(gridDim.x) * groups;
@@ -297,15 +304,14 @@ norm_backward(const NormGradParams p, const Share share) {
     for (int j = 0; j < 8; ++j) acc[i][j] = 0.f;
   if constexpr (kKeepGain) {
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i)
-      if (tid + i * lanes < p.vecs) load_gain<kFp32>(p.gain, p.gain_offset, tid + i * lanes, gains[i]);
+    for (int i = 0; i < kVecs; ++i) load_gain<kFp32>(p.gain, p.gain_offset, min(tid + i * lanes, p.vecs - 1), gains[i]);
   }
-  auto gain_of = [&](int i, int v, float (&g)[8]) {
+  auto gain_of = [&](int i, float (&g)[8]) {               // (a lane behind the row multiplies zeros, or is not looked at)
     if constexpr (kKeepGain) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) g[j] = gains[i][j];
     } else {
-      load_gain<kFp32>(p.gain, p.gain_offset, v, g);
+      load_gain<kFp32>(p.gain, p.gain_offset, min(tid + i * lanes, p.vecs - 1), g);
     }
   };
   int slot = 0, turn = 0;
@@ -315,29 +321,36 @@ norm_backward(const NormGradParams p, const Share share) {
     const long long row = row0 + group;
     const bool live = row < p.rows;
     const size_t at = static_cast<size_t>(row) * p.vecs;
-    const unsigned char* base = s_ring + slot * slot_bytes + group * row_bytes;
-    const uint4* ss_row = reinterpret_cast<const uint4*>(base);
-    const uint4* d_row = reinterpret_cast<const uint4*>(base + tensor_bytes);
-    const uint4* e_row = reinterpret_cast<const uint4*>(base + 2 * tensor_bytes);
+    const uint4* in = reinterpret_cast<const uint4*>(s_ring + slot * slot_bytes + group * row_bytes);
+    const int pitch = tensor_bytes / 16;                   // vectors between the tensors' rows
     uint4 sq[kVecs], dq[kVecs], eq[kVecs];
-    float ss = 0.f, dot = 0.f;                             // sums of s^2 and of s d_out gain
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
       const int v = tid + i * lanes;
       sq[i] = dq[i] = eq[i] = make_uint4(0u, 0u, 0u, 0u);
       if (live && v < p.vecs) {
-        sq[i] = ss_row[v];
-        dq[i] = d_row[v];
-        if (with_sum) eq[i] = e_row[v];
-        float s[8], d[8], g[8];
-        unpack8(sq[i], s);
-        unpack8(dq[i], d);
-        gain_of(i, v, g);
+        sq[i] = in[v];
+        dq[i] = in[v + pitch];
+      }
+    }
+    if (with_sum) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          ss = fmaf(s[j], s[j], ss);
-          dot = fmaf(s[j], d[j] * g[j], dot);
-        }
+      for (int i = 0; i < kVecs; ++i) {
+        const int v = tid + i * lanes;
+        if (live && v < p.vecs) eq[i] = in[v + 2 * pitch];
+      }
+    }
+    float ss = 0.f, dot = 0.f;                             // sums of s^2 and of s d_out gain
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      float s[8], d[8], g[8];
+      unpack8(sq[i], s);
+      unpack8(dq[i], d);
+      gain_of(i, g);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        ss = fmaf(s[j], s[j], ss);
+        dot = fmaf(s[j], d[j] * g[j], dot);
       }
     }
     ss = moe::warp_sum(ss);
@@ -364,21 +377,21 @@ norm_backward(const NormGradParams p, const Share share) {
     const float mean = __fdiv_rn(dot * rstd, static_cast<float>(p.cols));   // mean of g h
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-      const int v = tid + i * lanes;
-      if (live && v < p.vecs) {
-        float s[8], d[8], o[8], g[8];
-        unpack8(sq[i], s);
-        unpack8(dq[i], d);
-        unpack8(eq[i], o);
-        gain_of(i, v, g);
+      float s[8], d[8], o[8], g[8];
+      stay_packed(sq[i]);
+      stay_packed(dq[i]);
+      unpack8(sq[i], s);
+      unpack8(dq[i], d);
+      unpack8(eq[i], o);
+      gain_of(i, g);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float h = s[j] * rstd;
-          acc[i][j] = fmaf(d[j], h, acc[i][j]);
-          o[j] += rstd * (d[j] * g[j] - h * mean);
-        }
-        if (p.d_x != nullptr) p.d_x[at + v] = pack8(o);
+      for (int j = 0; j < 8; ++j) {
+        const float h = s[j] * rstd;
+        acc[i][j] = fmaf(d[j], h, acc[i][j]);
+        o[j] = fmaf(rstd, fmaf(-h, mean, d[j] * g[j]), o[j]);
       }
+      const int v = tid + i * lanes;
+      if (p.d_x != nullptr && live && v < p.vecs) p.d_x[at + v] = pack8(o);
     }
   }
 
@@ -429,7 +442,6 @@ norm_gain_sum(const float* __restrict__ partial, int parts, int cols, float* __r
   constexpr int kAhead = 8;                                // rows whose loads are in flight together
   __shared__ float s_sum[kSumWarps][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
-  ptx::wait_for_previous_kernel();
   float sum = 0.f;
   if (c < cols) {
     for (int i = warp; i < parts; i += kSumWarps * kAhead) {
@@ -475,38 +487,34 @@ NormKernel norm_kernel(const moe_rms_norm_args& a) {
   }
 }
 
-// norm_backward: vectors of a lane, and the CTAs of an SM that its registers allow.
+// norm_backward: the CTAs of an SM that its registers and rings allow, and the rings' depth.
 struct BackwardPlan {
   Share share;
-  int vecs, ctas, depth;
-  size_t bytes;                           // of the ring
+  int ctas, depth;
+  size_t bytes;                           // of a ring
 };
-BackwardPlan backward_plan(const moe_ctx* ctx, int cols) {
-  constexpr size_t kSm = kRingBytes;
+BackwardPlan backward_plan(int cols) {
   BackwardPlan b;
-  const int vecs = cols / 8;
-  b.vecs = vecs <= 512 ? moe_knob_value(ctx, "norm_bv", 2) : 4;
-  b.share = share_of(vecs, b.vecs);
-  const int threads = threads_of(b.share);
+  b.share = share_of(cols / 8, 4);
   const size_t slot = static_cast<size_t>(3) * b.share.rows * cols * 2;   // (as if d_sum were given)
-  b.ctas = threads > 256 ? 1 : b.vecs == 2 ? 3 : 2;
-  if (slot * 2 * b.ctas > kSm) b.ctas = slot * 4 <= kSm ? 2 : 1;
-  b.depth = static_cast<int>(kSm / b.ctas / slot);
+  b.ctas = threads_of(b.share) <= 256 && 4 * slot <= kRingBytes ? 2 : 1;
+  b.depth = static_cast<int>(kRingBytes / b.ctas / slot);
   if (b.depth > kMaxRing) b.depth = kMaxRing;
-  if (b.depth < 1) b.depth = 1;
-  b.bytes = b.depth * slot;
+  b.bytes = b.depth * slot;               // (the longest row takes 192 KiB)
   return b;
 }
 using BackwardKernel = void (*)(NormGradParams, Share);
 template <bool kFp32>
 BackwardKernel backward_kernel(const BackwardPlan& b) {
-  return b.vecs == 2 ? norm_backward<2, 256, 3, kFp32> : threads_of(b.share) <= 256 ? norm_backward<4, 256, 2, kFp32>
-                                                                                  : norm_backward<4, 1024, 1, kFp32>;
+  return threads_of(b.share) <= 256 ? norm_backward<256, kFp32> : norm_backward<1024, kFp32>;
 }
-// CTAs of norm_backward, the same for its scratch and its launch.
-int backward_ctas(const moe_ctx* ctx, long long rows, const BackwardPlan& b) {
-  const long long need = (rows + b.share.rows - 1) / b.share.rows, room = static_cast<long long>(ctx->num_sms) * b.ctas;
-  return static_cast<int>(need < room ? need : room);
+// CTAs of norm_backward: no more than it takes to be done in as few rounds as all that fit would be, since each leaves a row of
+// fp32 sums.  `most`: all that fit, which the scratch is measured by, so that one for many rows does for fewer.
+int backward_ctas(const moe_ctx* ctx, long long rows, const BackwardPlan& b, bool most) {
+  const long long groups = (rows + b.share.rows - 1) / b.share.rows, room = static_cast<long long>(ctx->num_sms) * b.ctas;
+  const long long rounds = most || groups == 0 ? 1 : (groups + room - 1) / room;
+  const long long ctas = (groups + rounds - 1) / rounds;
+  return static_cast<int>(ctas < room ? ctas : room);
 }
 
 }  // namespace
@@ -518,7 +526,9 @@ cudaError_t launch_add_rms_norm(moe_ctx* ctx, const moe_rms_norm_args& a, cudaSt
                      static_cast<uint4*>(a.out), static_cast<uint2*>(a.codes), a.scales, a.rows, a.cols / 8, a.cols, a.eps,
                      a.gain_offset};
   ctx->last_launches += 1;
-  const bool few = moe_knob_value(ctx, "norm_vecs", a.rows * p.vecs <= 2048LL * ctx->num_sms ? 1 : 4) == 1 && p.vecs <= 1024;
+  // Four vectors to a lane keep a row's loads in flight together and few warps meeting; one, where all vectors of the batch are
+  // resident at once even so, is quicker done.  64 x 7168: 4.2 us against 6.2; 1000 x 2048: 6.3 / 8.3; 592 x 7168: 10.3 / 8.3.
+  const bool few = a.rows * p.vecs <= 2048LL * ctx->num_sms && p.vecs <= 1024;
   const Share share = share_of(p.vecs, few ? 1 : 4);
   const int threads = threads_of(share);
   const unsigned grid = static_cast<unsigned>((a.rows + share.rows - 1) / share.rows);
@@ -528,13 +538,13 @@ cudaError_t launch_add_rms_norm(moe_ctx* ctx, const moe_rms_norm_args& a, cudaSt
 }
 
 size_t rms_norm_scratch_bytes(const moe_ctx* ctx, long long rows, int cols) {
-  return static_cast<size_t>(backward_ctas(ctx, rows, backward_plan(ctx, cols))) * cols * 4;
+  return static_cast<size_t>(backward_ctas(ctx, rows, backward_plan(cols), true)) * cols * 4;
 }
 
 cudaError_t launch_rms_norm_backward(moe_ctx* ctx, const moe_rms_norm_grad_args& a, cudaStream_t stream) {
   if (a.rows == 0) return a.d_gain ? cudaMemsetAsync(a.d_gain, 0, static_cast<size_t>(a.cols) * 4, stream) : cudaSuccess;
-  const BackwardPlan b = backward_plan(ctx, a.cols);
-  const int ctas = backward_ctas(ctx, a.rows, b), threads = threads_of(b.share);
+  const BackwardPlan b = backward_plan(a.cols);
+  const int ctas = backward_ctas(ctx, a.rows, b, false), threads = threads_of(b.share);
   const NormGradParams p{static_cast<const uint4*>(a.s), a.gain, static_cast<const uint4*>(a.d_out),
                          static_cast<const uint4*>(a.d_sum), static_cast<uint4*>(a.d_x),
                          a.d_gain ? static_cast<float*>(a.scratch) : nullptr, ctx->d_status, a.rows, a.cols / 8, a.cols, a.eps,
@@ -545,25 +555,18 @@ cudaError_t launch_rms_norm_backward(moe_ctx* ctx, const moe_rms_norm_grad_args&
   cudaError_t e = cudaGetLastError();
   ctx->last_launches += 1;
   if (e == cudaSuccess && a.d_gain) {
-    cudaLaunchConfig_t cfg{};
-    cudaLaunchAttribute attr{};
-    cfg.gridDim = dim3((a.cols + 31) / 32);
-    cfg.blockDim = dim3(kSumWarps * 32);
-    cfg.stream = stream;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
+    norm_gain_sum<<<(a.cols + 31) / 32, kSumWarps * 32, 0, stream>>>(p.partial, ctas, a.cols, a.d_gain);
     ctx->last_launches += 1;
-    e = cudaLaunchKernelEx(&cfg, norm_gain_sum, static_cast<const float*>(p.partial), ctas, static_cast<int>(a.cols), a.d_gain);
+    e = cudaGetLastError();
   }
   return e;
 }
 
 cudaError_t prepare_rms_norm(moe_ctx* ctx) {
+  (void)ctx;
   cudaError_t e = cudaSuccess;
-  for (const int cols : {1024, 8192, 32768}) {             // a plan of each kind
-    const BackwardPlan b = backward_plan(ctx, cols);
+  for (const int cols : {8192, 32768}) {                   // a plan of each kind
+    const BackwardPlan b = backward_plan(cols);
     for (const BackwardKernel kernel : {backward_kernel<false>(b), backward_kernel<true>(b)})
       if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes);
   }
