@@ -118,6 +118,17 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3;
   const int tile = blockIdx.x / cluster, part = blockIdx.x - tile * cluster;
 
+  // Tensor memory first: the SM takes its second CTA only when the first has given up the right to allocate (with the search in
+  // front of it, half of the CTAs began 2.4 us later).
+  if (warp == 1) {
+    ptx::tmem_alloc(ptx::smem_u32(&bar.tmem), kCols);
+    ptx::tmem_relinquish();
+    ptx::tc_fence_before_sync();
+    __syncwarp();
+  }
+  auto leave = [&]() {
+    if (warp == 1) ptx::tmem_dealloc(*static_cast<volatile uint32_t*>(&bar.tmem), kCols);
+  };
   if (threadIdx.x == 0) {
     ptx::prefetch_tensormap(&maps.x);
     ptx::prefetch_tensormap(&maps.a);
@@ -128,10 +139,10 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
     return o < 0 ? 0LL : o > p.rows ? p.rows : o;
   };
   const int seg = moe::last_at_or_below(p.segments + 1, tile, lane, [&](int s) { return bound(s) / kTileRows + s; });
-  if (seg < 0) return;                                     // (offsets that do not begin with 0)
+  if (seg < 0) return leave();                             // (offsets that do not begin with 0)
   const long long begin = bound(seg), end = seg < p.segments ? bound(seg + 1) : p.rows;
   const long long row0 = begin + (tile - (begin / kTileRows + seg)) * kTileRows;
-  if (row0 >= end) return;                                 // (the whole cluster)
+  if (row0 >= end) return leave();                         // (the whole cluster)
   const int m = static_cast<int>(end - row0 < kTileRows ? end - row0 : kTileRows);
   int id = seg < p.segments ? __ldg(p.adapter_of + seg) : -1;
   if (id >= p.adapters) {
@@ -142,15 +153,14 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
     id = -1;
   }
   const bool has = id >= 0;
-  if (!has && p.y_in == p.y_out) return;                   // nothing to add and nothing to copy
+  if (!has && p.y_in == p.y_out) return leave();           // nothing to add and nothing to copy
 
   const Layout lay(p.rank);
   unsigned char* base = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
   const uint32_t base_at = ptx::smem_u32(base);
   const int blocks = (p.K + kBK - 1) / kBK, parts = min(cluster, blocks);
   const bool sums = has && part < parts;                   // this CTA has a part of K
-  const int kb0 = sums ? static_cast<int>(static_cast<long long>(blocks) * part / parts) : 0;
-  const int kb1 = sums ? static_cast<int>(static_cast<long long>(blocks) * (part + 1) / parts) : 0;
+  // (every parts-th block of K: the cluster reads neighbouring lines of x at a time)
   const int tiles = (p.N - 1) / kBN + 1;
   const int n0 = static_cast<int>(static_cast<long long>(tiles) * part / cluster);
   const int n1 = static_cast<int>(static_cast<long long>(tiles) * (part + 1) / cluster);
@@ -176,11 +186,6 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
     ptx::mbar_init(ptx::smem_u32(&bar.sums_full), 1);
     bar.abort_flag = 0;
     ptx::fence_barrier_init();
-  }
-  if (warp == 1) {
-    ptx::tmem_alloc(ptx::smem_u32(&bar.tmem), kCols);
-    ptx::tmem_relinquish();
-    ptx::tc_fence_before_sync();
   }
   __syncthreads();
   if (has) ptx::cluster_arrive();                          // (waited for before anything is sent: every CTA has begun)
@@ -210,7 +215,7 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
         int stage = 0;
         uint32_t phase = 1;
         bool ok = true;
-        for (int kb = kb0; kb < kb1; ++kb) {
+        for (int kb = part; kb < blocks; kb += parts) {
           ok = ptx::mbar_wait(ptx::smem_u32(&bar.empty[stage]), phase, abort_flag);
           if (!ok) break;
           const uint32_t full = ptx::smem_u32(&bar.full[stage]), at = base_at + stage * lay.stage_bytes;
@@ -236,14 +241,14 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
         int stage = 0;
         uint32_t phase = 0;
         bool ok = true;
-        for (int kb = kb0; kb < kb1; ++kb) {
+        for (int kb = part; kb < blocks; kb += parts) {
           ok = ptx::mbar_wait(ptx::smem_u32(&bar.full[stage]), phase, abort_flag);
           if (!ok) break;
           ptx::tc_fence_after_sync();
           const uint32_t at = base_at + stage * lay.stage_bytes;
           const uint64_t a = ptx::smem_desc_sw128(at), b = ptx::smem_desc_sw128(at + kXBytes);
 #pragma unroll
-          for (int k = 0; k < kBK / 16; ++k) ptx::tc_mma_bf16(tmem, a + 2 * k, b + 2 * k, idesc, kb > kb0 || k > 0);
+          for (int k = 0; k < kBK / 16; ++k) ptx::tc_mma_bf16(tmem, a + 2 * k, b + 2 * k, idesc, kb > part || k > 0);
           ptx::tc_commit(ptx::smem_u32(&bar.empty[stage]));
           if (++stage == lay.stages) { stage = 0; phase ^= 1u; }
         }
@@ -262,14 +267,14 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
         // row r goes to the CTA in whose share it lies: the last q with m q / cluster <= r
         const int owner = ((r + 1) * cluster + m - 1) / m - 1, first = m * owner / cluster;
         const uint32_t dst = ptx::map_to_cta(base_at + lay.sums_at + (part * share + r - first) * lay.pitch * 4, min(owner, cluster - 1));
-        for (int j = 0; j < p.rank; j += 16) {
-          uint32_t v[16];
-          ptx::tmem_ld_32x16(lanes + j, v);
+        for (int j = 0; j < p.rank; j += 32) {             // (columns behind the rank hold something, or nothing yet)
+          uint32_t v[32];
+          ptx::tmem_ld_32x32(lanes + j, v);
           ptx::tmem_ld_wait();
           if (r < m) {
 #pragma unroll
-            for (int q = 0; q < 16; q += 4)
-              if (q < 8 || j + 8 < p.rank) moe::st_cluster(dst + (j + q) * 4, make_uint4(v[q], v[q + 1], v[q + 2], v[q + 3]));
+            for (int q = 0; q < 32; q += 4)
+              if (j + q < p.rank) moe::st_cluster(dst + (j + q) * 4, make_uint4(v[q], v[q + 1], v[q + 2], v[q + 3]));
           }
         }
         ptx::tc_fence_before_sync();
