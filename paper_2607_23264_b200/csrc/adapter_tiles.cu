@@ -194,10 +194,11 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
   volatile int* abort_flag = &bar.abort_flag;
   const int r = quarter * 32 + lane;                       // the row of an epilogue thread
   int y_issued = 0, b_issued = 0;                          // (warp 0's lane 0)
+  const uint64_t once = ptx::l2_policy_evict_first();      // x and y are read once: what the last kernel wrote may stay in L2
   auto load_y = [&](int slot, int n) {
     const uint32_t full = ptx::smem_u32(&bar.y_full[slot]);
     ptx::mbar_expect_tx(full, tile_bytes);
-    ptx::tma_load_2d(base_at + lay.y_at + slot * kYBytes, tm_in, full, n * kBN, static_cast<int>(row0));
+    ptx::tma_load_2d_hint(base_at + lay.y_at + slot * kYBytes, tm_in, full, n * kBN, static_cast<int>(row0), once);
   };
 
   auto load_b = [&](int slot, int n) {
@@ -220,7 +221,7 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
           if (!ok) break;
           const uint32_t full = ptx::smem_u32(&bar.full[stage]), at = base_at + stage * lay.stage_bytes;
           ptx::mbar_expect_tx(full, tile_bytes + lay.rank16 * 128);
-          ptx::tma_load_2d(at, tm_x, full, kb * kBK, static_cast<int>(row0));
+          ptx::tma_load_2d_hint(at, tm_x, full, kb * kBK, static_cast<int>(row0), once);
           ptx::tma_load_2d(at + kXBytes, &maps.a, full, kb * kBK, id * p.rank);
           if (++stage == lay.stages) { stage = 0; phase ^= 1u; }
         }

@@ -1,9 +1,9 @@
 // Low-rank adapters of many requests added to a projection's output: y[r] += scale_i b_i (a_i x[r]), i the row's adapter.
 //
-// adapter_rows: short segments and single tokens, where the factors are the bytes.  A cluster of up to eight CTAs takes up to 16
-//               rows of one adapter out of a window of 256 neighbouring rows, so that a factor is read once for all of them: the
-//               cluster of row r finds the rows of r's adapter in the window and goes on if r is the first, the 17th, ... of them.
-//               Each CTA has a part of K and a range of columns.  t = x a^T: m16n8k16 products with both operands straight
+// adapter_rows: short segments and single tokens, where the factors are the bytes.  A cluster of up to eight CTAs takes a unit: up
+//               to 16 rows of one adapter out of a window of 256 neighbouring rows, so that a factor is read once for all of
+//               them.  The cluster finds its unit by itself: the rows of an adapter are counted, the first, the 17th, ... of
+//               them leads a unit, and units are numbered by their leaders.  Each CTA has a part of K and a range of columns.  t = x a^T: m16n8k16 products with both operands straight
 //               from global memory (a lane's 16 bytes of a row are eight neighbouring k; as x and a are permuted along k
 //               alike, no shuffle is needed), warps added in order through shared memory, and the sums sent to every CTA of the cluster.
 //               Then y += t b^T: two columns per thread, fp32 dot products over the rank.
@@ -16,7 +16,7 @@ namespace {
 using moe::AdapterParams;
 
 constexpr unsigned kFull = 0xFFFFFFFFu;
-constexpr int kRows = 16;                 // rows of a cluster
+constexpr int kRows = 16;                 // rows of a unit
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kWindow = kThreads;         // rows among which those of one adapter are brought together
 constexpr int kMaxCluster = 8;
@@ -61,55 +61,63 @@ __device__ __forceinline__ void prefetch_l2(const void* at) { asm volatile("pref
 __host__ __device__ constexpr int pitch_of(int rank) { return rank + 4; }
 int smem_of(int rank) { return (kWarps + kMaxCluster + 1) * kRows * pitch_of(rank) * 4; }
 
-// kTiles: tiles of eight ranks held in registers (rank <= 8 * kTiles).  Grid: a cluster of `cluster` CTAs per row.
+// kTiles: tiles of eight ranks held in registers (rank <= 8 * kTiles).  Grid: for each window `units` clusters.
 template <int kTiles>
 __global__ void __launch_bounds__(kThreads)
-adapter_rows(const AdapterParams p, int cluster) {
+adapter_rows(const AdapterParams p, int units, int cluster) {
   extern __shared__ float4 smem4[];
-  __shared__ int s_before[kWarps], s_row[kRows];
+  __shared__ __align__(16) int s_id[kWindow];
+  __shared__ int s_row[kRows], s_leaders[kWarps], s_unit[2];
   float* s_warp = reinterpret_cast<float*>(smem4);
   const int pitch = pitch_of(p.rank);
   float* s_cta = s_warp + kWarps * kRows * pitch;
   float* s_t = s_cta + kMaxCluster * kRows * pitch;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
-  const unsigned item = blockIdx.x / cluster;
-  const int part = static_cast<int>(blockIdx.x - item * cluster);
-  const long long leader = item, window = leader / kWindow * kWindow;
-
-  const int my_id = adapter_of_row(p, window + tid, part == 0 && window + tid == leader);
-  const int at = static_cast<int>(leader - window);
-  if (tid < kRows) s_row[tid] = -1;
-  if (tid == at) s_before[0] = my_id;
-  __syncthreads();
-  const int id = s_before[0];
+  const int item = blockIdx.x / cluster, part = blockIdx.x - item * cluster;
+  const int at_window = item / units, unit = item - at_window * units;
+  const long long window = static_cast<long long>(at_window) * kWindow;
   const int eighths = p.N / 8;
   const int n0 = 8 * static_cast<int>(static_cast<long long>(eighths) * part / cluster);
   const int n1 = 8 * static_cast<int>(static_cast<long long>(eighths) * (part + 1) / cluster);
-  if (id < 0) {                                            // no adapter: the row is copied (the whole cluster alike)
-    if (p.y_in != p.y_out) {
-      const uint4* from = reinterpret_cast<const uint4*>(p.y_in + leader * p.N + n0);
-      uint4* to = reinterpret_cast<uint4*>(p.y_out + leader * p.N + n0);
+
+  // the window's units: how many rows of its adapter are in front of each row, and the leaders' numbers
+  const int my_id = adapter_of_row(p, window + tid, unit == 0 && part == 0);
+  s_id[tid] = my_id;
+  if (tid < kRows) s_row[tid] = 0;
+  if (tid == 0) s_unit[0] = -1;
+  __syncthreads();
+  int place = __popc(__match_any_sync(kFull, my_id) & ((1u << lane) - 1));
+  const int4* ids4 = reinterpret_cast<const int4*>(s_id);
+#pragma unroll 4
+  for (int i = 0; i < 8 * warp; ++i) {
+    const int4 v = ids4[i];
+    place += (v.x == my_id) + (v.y == my_id) + (v.z == my_id) + (v.w == my_id);
+  }
+  const bool leads = my_id >= 0 && place % kRows == 0;
+  const unsigned leaders = __ballot_sync(kFull, leads);
+  if (lane == 0) s_leaders[warp] = __popc(leaders);
+  __syncthreads();
+  int number = __popc(leaders & ((1u << lane) - 1));
+  for (int w = 0; w < warp; ++w) number += s_leaders[w];
+  if (leads && number == unit) {
+    s_unit[0] = my_id;
+    s_unit[1] = place;
+  }
+  __syncthreads();
+  const int id = s_unit[0], first = s_unit[1];
+  // rows without an adapter are copied, every units-th by this cluster
+  if (p.y_in != p.y_out) {
+    for (int r = unit; r < kWindow && window + r < p.rows; r += units) {
+      if (s_id[r] >= 0) continue;
+      const uint4* from = reinterpret_cast<const uint4*>(p.y_in + (window + r) * p.N + n0);
+      uint4* to = reinterpret_cast<uint4*>(p.y_out + (window + r) * p.N + n0);
       for (int i = tid; i < (n1 - n0) / 8; i += kThreads) to[i] = from[i];
     }
-    return;
   }
-  __syncthreads();
-  const unsigned same = __ballot_sync(kFull, my_id == id);
-  if (lane == 0) s_before[warp] = __popc(same);
-  __syncthreads();
-  int place = __popc(same & ((1u << lane) - 1)), first = 0, total = 0;      // among the window's rows of this adapter
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
-    if (w < warp) place += s_before[w];
-    total += s_before[w];
-  }
-  if (tid == at) s_row[0] = place;
-  __syncthreads();
-  first = s_row[0];
-  if (first % kRows != 0) return;                          // another row's cluster has this one
-  const int count = min(kRows, total - first);
-  __syncthreads();
-  if (my_id == id && place >= first && place < first + kRows) s_row[place - first] = tid;
+  if (id < 0) return;                                      // fewer units than clusters (the whole cluster alike)
+  const bool mine = my_id == id && place >= first && place < first + kRows;
+  if (mine) s_row[place - first] = tid;
+  const int count = __syncthreads_count(mine);
   if (cluster > 1) ptx::cluster_arrive();                  // (waited for before anything is sent: every CTA has begun)
   // the bytes of the second product are on their way meanwhile
   {
@@ -117,7 +125,6 @@ adapter_rows(const AdapterParams p, int cluster) {
     const int bytes = (n1 - n0) * p.rank * 2;
     for (int i = tid * 128; i < bytes; i += kThreads * 128) prefetch_l2(b + i);
   }
-  __syncthreads();
 
   // ------------------------------------------------------------------------------------------------ t = x a^T
   const int steps = (p.K + 31) / 32, tiles = p.rank / 8;   // steps of 32 along K, dealt to the CTAs and then to the warps
@@ -166,7 +173,7 @@ adapter_rows(const AdapterParams p, int cluster) {
   __syncthreads();
   if (cluster > 1) ptx::cluster_wait();
   const int quads = p.rank / 4;
-  const uint32_t mine = ptx::smem_u32(s_cta) + part * kRows * pitch * 4;
+  const uint32_t slot = ptx::smem_u32(s_cta) + part * kRows * pitch * 4;
   for (int i = tid; i < count * quads; i += kThreads) {
     const int r = i / quads, j = 4 * (i - r * quads);
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -176,7 +183,7 @@ adapter_rows(const AdapterParams p, int cluster) {
       v.x += a.x; v.y += a.y; v.z += a.z; v.w += a.w;
     }
     const uint4 bits = *reinterpret_cast<const uint4*>(&v);
-    for (int q = 0; q < cluster; ++q) moe::st_cluster(ptx::map_to_cta(mine + (r * pitch + j) * 4, q), bits);
+    for (int q = 0; q < cluster; ++q) moe::st_cluster(ptx::map_to_cta(slot + (r * pitch + j) * 4, q), bits);
   }
   __syncwarp();
   if (cluster > 1) ptx::cluster_sync();
@@ -232,10 +239,16 @@ adapter_rows(const AdapterParams p, int cluster) {
   }
 }
 
-// CTAs of a cluster: as many as leave about 1024 CTAs, should every row have an adapter of its own.
-int cluster_of(long long rows) {
+// Units of a window at most: an adapter's n rows make (n + 15) / 16 of them.
+int units_of(long long rows, int adapters, int segments) {
+  const int window = static_cast<int>(rows < kWindow ? rows : kWindow), distinct = adapters < segments ? adapters : segments;
+  const int units = distinct + window / kRows;
+  return units < 1 ? 1 : units < window ? units : window;
+}
+// CTAs of a cluster: as many as leave about 1024 CTAs.
+int cluster_of(long long items) {
   int c = kMaxCluster;
-  while (c > 1 && rows * c > 1024) c /= 2;
+  while (c > 1 && items * c > 1024) c /= 2;
   return c;
 }
 
@@ -250,11 +263,13 @@ moe_status launch_add_adapters(moe_ctx* ctx, const moe_adapter_args& a, cudaStre
                         static_cast<const __nv_bfloat16*>(a.b), a.scale, a.offsets, a.adapter_of,
                         static_cast<const __nv_bfloat16*>(a.y_in), static_cast<__nv_bfloat16*>(a.y_out), ctx->d_status, a.rows,
                         a.N, a.K, a.rank, a.adapters, a.segments};
-  if (a.segments > 0 && a.rows >= 128 && a.rows / a.segments >= 16) return launch_adapter_tiles(ctx, p, stream);
-  const int cluster = cluster_of(a.rows);
+  if (a.segments > 0 && a.offsets && a.rows >= moe_knob_value(ctx, "ad_rows", 128) && a.rows / a.segments >= moe_knob_value(ctx, "ad_min", 16)) return launch_adapter_tiles(ctx, p, stream);
+  const int units = units_of(a.rows, a.adapters, a.segments);
+  const long long items = (a.rows + kWindow - 1) / kWindow * units;
+  const int cluster = cluster_of(items);
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr{};
-  cfg.gridDim = dim3(static_cast<unsigned>(a.rows * cluster));
+  cfg.gridDim = dim3(static_cast<unsigned>(items * cluster));
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = smem_of(a.rank);
   cfg.stream = stream;
@@ -265,7 +280,7 @@ moe_status launch_add_adapters(moe_ctx* ctx, const moe_adapter_args& a, cudaStre
   attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
   ctx->last_launches += 1;
   auto kernel = a.rank <= 16 ? adapter_rows<2> : a.rank <= 32 ? adapter_rows<4> : a.rank <= 64 ? adapter_rows<8> : adapter_rows<16>;
-  return cudaLaunchKernelEx(&cfg, kernel, p, cluster) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+  return cudaLaunchKernelEx(&cfg, kernel, p, units, cluster) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
 cudaError_t prepare_adapters(moe_ctx* ctx) {
