@@ -85,13 +85,16 @@ adapter_rows(const AdapterParams p, int units, int cluster) {
   s_id[tid] = my_id;
   if (tid < kRows) s_row[tid] = 0;
   if (tid == 0) s_unit[0] = -1;
-  __syncthreads();
+  const int rows = p.rows - window < kWindow ? static_cast<int>(p.rows - window) : kWindow;
+  const bool some_without = __syncthreads_or(tid < rows && my_id < 0);
   int place = __popc(__match_any_sync(kFull, my_id) & ((1u << lane) - 1));
-  const int4* ids4 = reinterpret_cast<const int4*>(s_id);
-#pragma unroll 4
-  for (int i = 0; i < 8 * warp; ++i) {
-    const int4 v = ids4[i];
-    place += (v.x == my_id) + (v.y == my_id) + (v.z == my_id) + (v.w == my_id);
+  if (32 * warp < rows) {
+    const int4* ids4 = reinterpret_cast<const int4*>(s_id);
+#pragma unroll 8
+    for (int i = 0; i < 8 * warp; ++i) {
+      const int4 v = ids4[i];
+      place += (v.x == my_id) + (v.y == my_id) + (v.z == my_id) + (v.w == my_id);
+    }
   }
   const bool leads = my_id >= 0 && place % kRows == 0;
   const unsigned leaders = __ballot_sync(kFull, leads);
@@ -106,8 +109,8 @@ adapter_rows(const AdapterParams p, int units, int cluster) {
   __syncthreads();
   const int id = s_unit[0], first = s_unit[1];
   // rows without an adapter are copied, every units-th by this cluster
-  if (p.y_in != p.y_out) {
-    for (int r = unit; r < kWindow && window + r < p.rows; r += units) {
+  if (some_without && p.y_in != p.y_out) {
+    for (int r = unit; r < rows; r += units) {
       if (s_id[r] >= 0) continue;
       const uint4* from = reinterpret_cast<const uint4*>(p.y_in + (window + r) * p.N + n0);
       uint4* to = reinterpret_cast<uint4*>(p.y_out + (window + r) * p.N + n0);
@@ -211,20 +214,35 @@ adapter_rows(const AdapterParams p, int units, int cluster) {
     for (int r = 0; r < kRows; ++r) sum[r][0] = sum[r][1] = 0.f;
     const uint4* b0 = reinterpret_cast<const uint4*>(p.b + (static_cast<size_t>(id) * p.N + n) * p.rank);
     const uint4* b1 = b0 + p.rank / 8;
-    for (int j = 0; j < p.rank / 8; ++j) {
-      const uint4 u = __ldg(b0 + j), v = __ldg(b1 + j);
-      const float bu[8] = {low(u.x), high(u.x), low(u.y), high(u.y), low(u.z), high(u.z), low(u.w), high(u.w)};
-      const float bv[8] = {low(v.x), high(v.x), low(v.y), high(v.y), low(v.z), high(v.z), low(v.w), high(v.w)};
+    constexpr int kBatch = kTiles < 4 ? kTiles : 4;        // ranks by eight whose loads are in flight together
+    for (int j0 = 0; j0 < tiles; j0 += kBatch) {
+      uint4 u[kBatch], v[kBatch];
 #pragma unroll
-      for (int r = 0; r < kRows; ++r) {
-        if (r < count) {
-          const float4 ta = *reinterpret_cast<const float4*>(s_t + r * pitch + 8 * j);
-          const float4 tb = *reinterpret_cast<const float4*>(s_t + r * pitch + 8 * j + 4);
-          const float t[8] = {ta.x, ta.y, ta.z, ta.w, tb.x, tb.y, tb.z, tb.w};
+      for (int i = 0; i < kBatch; ++i) {
+        u[i] = v[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (j0 + i < tiles) {
+          u[i] = __ldg(b0 + j0 + i);
+          v[i] = __ldg(b1 + j0 + i);
+        }
+      }
 #pragma unroll
-          for (int q = 0; q < 8; ++q) {
-            sum[r][0] = fmaf(t[q], bu[q], sum[r][0]);
-            sum[r][1] = fmaf(t[q], bv[q], sum[r][1]);
+      for (int i = 0; i < kBatch; ++i) {
+        if (j0 + i >= tiles) break;
+        const float bu[8] = {low(u[i].x), high(u[i].x), low(u[i].y), high(u[i].y),
+                             low(u[i].z), high(u[i].z), low(u[i].w), high(u[i].w)};
+        const float bv[8] = {low(v[i].x), high(v[i].x), low(v[i].y), high(v[i].y),
+                             low(v[i].z), high(v[i].z), low(v[i].w), high(v[i].w)};
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+          if (r < count) {
+            const float4 ta = *reinterpret_cast<const float4*>(s_t + r * pitch + 8 * (j0 + i));
+            const float4 tb = *reinterpret_cast<const float4*>(s_t + r * pitch + 8 * (j0 + i) + 4);
+            const float t[8] = {ta.x, ta.y, ta.z, ta.w, tb.x, tb.y, tb.z, tb.w};
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+              sum[r][0] = fmaf(t[q], bu[q], sum[r][0]);
+              sum[r][1] = fmaf(t[q], bv[q], sum[r][1]);
+            }
           }
         }
       }
