@@ -6,7 +6,7 @@
 //               them leads a unit, and units are numbered by their leaders.  Each CTA has a part of K and a range of columns.  t = x a^T: m16n8k16 products with both operands straight
 //               from global memory (a lane's 16 bytes of a row are eight neighbouring k; as x and a are permuted along k
 //               alike, no shuffle is needed), warps added in order through shared memory, and the sums sent to every CTA of the cluster.
-//               Then y += t b^T: two columns per thread, fp32 dot products over the rank.
+//               Then y += t b^T by the same products, t as two bf16 terms (16 bits of it).
 // Long segments take adapter_tiles.
 #include "adapters.cuh"
 #include "ptx_sm100.cuh"
@@ -55,6 +55,12 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
 }
 __device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+__device__ __forceinline__ uint32_t pair(float a, float b) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+// y + d in bf16.
+__device__ __forceinline__ uint32_t add_pair(uint32_t y, float d0, float d1) { return pair(low(y) + d0, high(y) + d1); }
 __device__ __forceinline__ void prefetch_l2(const void* at) { asm volatile("prefetch.global.L2 [%0];" ::"l"(at)); }
 
 // Shared memory: [kWarps][kRows][pitch] sums of the warps, [kMaxCluster][kRows][pitch] of the CTAs, [kRows][pitch] t.
@@ -188,6 +194,44 @@ adapter_rows(const AdapterParams p, int units, int cluster) {
     const uint4 bits = *reinterpret_cast<const uint4*>(&v);
     for (int q = 0; q < cluster; ++q) moe::st_cluster(ptx::map_to_cta(slot + (r * pitch + j) * 4, q), bits);
   }
+  // The first of b and y are on their way meanwhile.  A warp takes 32 columns at a time, as four products of eight: in product j
+  // a lane's two columns are 2 j and 2 j + 1 of the eight neighbours it keeps, so that it reads and writes 16 bytes of a row.
+  constexpr int kSteps = kTiles / 2;                       // steps of 16 ranks
+  auto rank_of = [](int s, int lane4) { return kTiles == 2 ? 4 * lane4 : 32 * (s / 2) + 8 * lane4 + 4 * (s % 2); };
+  const int groups = (n1 - n0 + 31) / 32;
+  const size_t y_lo = static_cast<size_t>(window + (has_lo ? s_row[g] : 0)) * p.N;
+  const size_t y_hi = static_cast<size_t>(window + (has_hi ? s_row[g + 8] : 0)) * p.N;
+  const __nv_bfloat16* b_base = p.b + static_cast<size_t>(id) * p.N * p.rank;
+  uint32_t b[4][2 * kSteps];
+  uint4 y[2];
+  auto load_group = [&](int at) {
+    const int n = n0 + 32 * at;
+    y[0] = y[1] = make_uint4(0u, 0u, 0u, 0u);
+    if (has_lo && n + 8 * c < n1) y[0] = *reinterpret_cast<const uint4*>(p.y_in + y_lo + n + 8 * c);
+    if (has_hi && n + 8 * c < n1) y[1] = *reinterpret_cast<const uint4*>(p.y_in + y_hi + n + 8 * c);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int row = n + (g >> 1) * 8 + 2 * j + (g & 1);
+      const __nv_bfloat16* from = b_base + static_cast<size_t>(row) * p.rank;
+      if constexpr (kTiles == 2) {
+        uint2 v = make_uint2(0u, 0u);
+        if (row < n1 && 4 * c < p.rank) v = __ldg(reinterpret_cast<const uint2*>(from + 4 * c));
+        b[j][0] = v.x;
+        b[j][1] = v.y;
+      } else {
+#pragma unroll
+        for (int s = 0; s < kSteps / 2; ++s) {
+          uint4 v = make_uint4(0u, 0u, 0u, 0u);
+          if (row < n1 && 32 * s + 8 * c < p.rank) v = __ldg(reinterpret_cast<const uint4*>(from + 32 * s + 8 * c));
+          b[j][4 * s] = v.x;
+          b[j][4 * s + 1] = v.y;
+          b[j][4 * s + 2] = v.z;
+          b[j][4 * s + 3] = v.w;
+        }
+      }
+    }
+  };
+  if (warp < groups) load_group(warp);
   __syncwarp();
   if (cluster > 1) ptx::cluster_sync();
   else __syncthreads();
@@ -204,54 +248,45 @@ adapter_rows(const AdapterParams p, int units, int cluster) {
   __syncthreads();
 
   // ------------------------------------------------------------------------------------------------ y += t b^T
-  for (int n = n0 + 2 * tid; n < n1; n += 2 * kThreads) {
-    uint32_t y[kRows];
+  uint32_t hi[kSteps][4], lo[kSteps][4];                   // the terms of t, in the order in which b's lanes hold the ranks
 #pragma unroll
-    for (int r = 0; r < kRows; ++r)
-      if (r < count) y[r] = *reinterpret_cast<const uint32_t*>(p.y_in + (window + s_row[r]) * p.N + n);
-    float sum[kRows][2];
+  for (int s = 0; s < kSteps; ++s) {
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) sum[r][0] = sum[r][1] = 0.f;
-    const uint4* b0 = reinterpret_cast<const uint4*>(p.b + (static_cast<size_t>(id) * p.N + n) * p.rank);
-    const uint4* b1 = b0 + p.rank / 8;
-    constexpr int kBatch = kTiles < 4 ? kTiles : 4;        // ranks by eight whose loads are in flight together
-    for (int j0 = 0; j0 < tiles; j0 += kBatch) {
-      uint4 u[kBatch], v[kBatch];
+    for (int h = 0; h < 2; ++h) {                          // rows g and g + 8
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
-        u[i] = v[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (j0 + i < tiles) {
-          u[i] = __ldg(b0 + j0 + i);
-          v[i] = __ldg(b1 + j0 + i);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
-        if (j0 + i >= tiles) break;
-        const float bu[8] = {low(u[i].x), high(u[i].x), low(u[i].y), high(u[i].y),
-                             low(u[i].z), high(u[i].z), low(u[i].w), high(u[i].w)};
-        const float bv[8] = {low(v[i].x), high(v[i].x), low(v[i].y), high(v[i].y),
-                             low(v[i].z), high(v[i].z), low(v[i].w), high(v[i].w)};
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-          if (r < count) {
-            const float4 ta = *reinterpret_cast<const float4*>(s_t + r * pitch + 8 * (j0 + i));
-            const float4 tb = *reinterpret_cast<const float4*>(s_t + r * pitch + 8 * (j0 + i) + 4);
-            const float t[8] = {ta.x, ta.y, ta.z, ta.w, tb.x, tb.y, tb.z, tb.w};
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-              sum[r][0] = fmaf(t[q], bu[q], sum[r][0]);
-              sum[r][1] = fmaf(t[q], bv[q], sum[r][1]);
-            }
-          }
-        }
+      for (int e = 0; e < 2; ++e) {                          // ranks 0, 1 and 2, 3 of the step
+        const int k = rank_of(s, c) + 2 * e;
+        const float* t = s_t + (g + 8 * h) * pitch + k;
+        const bool in = g + 8 * h < count && k < p.rank;
+        const float t0 = in ? t[0] : 0.f, t1 = in ? t[1] : 0.f;
+        const uint32_t first_term = pair(t0, t1);
+        // (an infinite or NaN value: the first term says it all)
+        const float r0 = t0 - low(first_term), r1 = t1 - high(first_term);
+        hi[s][2 * e + h] = first_term;
+        lo[s][2 * e + h] = pair(r0 == r0 ? r0 : 0.f, r1 == r1 ? r1 : 0.f);
       }
     }
+  }
+  for (int at = warp; at < groups; at += kWarps) {
+    if (at != warp) load_group(at);
+    float acc_y[4][4];
 #pragma unroll
-    for (int r = 0; r < kRows; ++r) {
-      if (r < count) {
-        const __nv_bfloat162 o = __floats2bfloat162_rn(low(y[r]) + sum[r][0], high(y[r]) + sum[r][1]);
-        *reinterpret_cast<uint32_t*>(p.y_out + (window + s_row[r]) * p.N + n) = *reinterpret_cast<const uint32_t*>(&o);
+    for (int j = 0; j < 4; ++j) {
+      acc_y[j][0] = acc_y[j][1] = acc_y[j][2] = acc_y[j][3] = 0.f;
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        mma_bf16(acc_y[j], hi[s][0], hi[s][1], hi[s][2], hi[s][3], b[j][2 * s], b[j][2 * s + 1]);
+        mma_bf16(acc_y[j], lo[s][0], lo[s][1], lo[s][2], lo[s][3], b[j][2 * s], b[j][2 * s + 1]);
+      }
+    }
+    const int n = n0 + 32 * at + 8 * c;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if ((h == 0 ? has_lo : has_hi) && n < n1) {
+        const uint4 q = y[h];
+        *reinterpret_cast<uint4*>(p.y_out + (h == 0 ? y_lo : y_hi) + n) =
+            make_uint4(add_pair(q.x, acc_y[0][2 * h], acc_y[0][2 * h + 1]), add_pair(q.y, acc_y[1][2 * h], acc_y[1][2 * h + 1]),
+                       add_pair(q.z, acc_y[2][2 * h], acc_y[2][2 * h + 1]), add_pair(q.w, acc_y[3][2 * h], acc_y[3][2 * h + 1]));
       }
     }
   }
