@@ -63,21 +63,21 @@ __device__ __forceinline__ uint32_t pair(float a, float b) {
 __device__ __forceinline__ uint32_t add_pair(uint32_t y, float d0, float d1) { return pair(low(y) + d0, high(y) + d1); }
 __device__ __forceinline__ void prefetch_l2(const void* at) { asm volatile("prefetch.global.L2 [%0];" ::"l"(at)); }
 
-// Shared memory: [kWarps][kRows][pitch] sums of the warps, [kMaxCluster][kRows][pitch] of the CTAs, [kRows][pitch] t.
+// Shared memory: [kWarps][kRows][pitch] sums of the warps, [kRows][pitch] t, [cluster][kRows][pitch] sums of the CTAs.
 __host__ __device__ constexpr int pitch_of(int rank) { return rank + 4; }
-int smem_of(int rank) { return (kWarps + kMaxCluster + 1) * kRows * pitch_of(rank) * 4; }
+int smem_of(int rank, int cluster) { return (kWarps + cluster + 1) * kRows * pitch_of(rank) * 4; }
 
 // kTiles: tiles of eight ranks held in registers (rank <= 8 * kTiles).  Grid: for each window `units` clusters.
 template <int kTiles>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 2)
 adapter_rows(const AdapterParams p, int units, int cluster) {
   extern __shared__ float4 smem4[];
   __shared__ __align__(16) int s_id[kWindow];
   __shared__ int s_row[kRows], s_leaders[kWarps], s_unit[2];
   float* s_warp = reinterpret_cast<float*>(smem4);
   const int pitch = pitch_of(p.rank);
-  float* s_cta = s_warp + kWarps * kRows * pitch;
-  float* s_t = s_cta + kMaxCluster * kRows * pitch;
+  float* s_t = s_warp + kWarps * kRows * pitch;
+  float* s_cta = s_t + kRows * pitch;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
   const int item = blockIdx.x / cluster, part = blockIdx.x - item * cluster;
   const int at_window = item / units, unit = item - at_window * units;
@@ -146,7 +146,7 @@ adapter_rows(const AdapterParams p, int units, int cluster) {
   float acc[kTiles][4];
 #pragma unroll
   for (int j = 0; j < kTiles; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
-  constexpr int kAhead = kTiles <= 4 ? 4 : kTiles <= 8 ? 2 : 1;            // steps whose loads are in flight together
+  constexpr int kAhead = kTiles <= 4 ? 4 : 1;            // steps whose loads are in flight together
   for (int s = s0 + warp; s < s1; s += kWarps * kAhead) {
     uint4 xa[kAhead], xb[kAhead], w[kAhead][kTiles];
 #pragma unroll
@@ -298,11 +298,22 @@ int units_of(long long rows, int adapters, int segments) {
   const int units = distinct + window / kRows;
   return units < 1 ? 1 : units < window ? units : window;
 }
-// CTAs of a cluster: as many as leave about 1024 CTAs.
+// CTAs of a cluster: as many as leave about 512 CTAs, a little more than are resident at once, since there are fewer units than
+// clusters (1024 rows of 8 adapters, rank 32, 4096 x 4096, segments of 64: 24.7 us; 33.4 with 1024 CTAs, 20.6 to 34.4 with 300).
 int cluster_of(long long items) {
   int c = kMaxCluster;
-  while (c > 1 && items * c > 1024) c /= 2;
+  while (c > 1 && items * c > 512) c /= 2;
   return c;
+}
+// Whether tiles of 128 rows are quicker.  A unit of 16 rows reads a factor again, so the rows' cost grows with the rank; a tile costs
+// the same with few rows in it, and twenty microseconds to come through.  Above 64 ranks a unit's sums leave an SM room for few
+// CTAs.  Measured at 4096 x 7168, 8 adapters (rows / tiles, us): rank 64, segments of 64: 1024 rows 37 / 29, 4096 rows 75 / 62;
+// segments of 16: 39 / 45, 117 / 150; rank 16, segments of 256: 2048 rows 23 / 29, 4096 rows 43 / 37; rank 128 (1024 x 1024), segments
+// of 16: 256 rows 31 / 19, 1024 rows 49 / 27.
+bool tiles_are_quicker(const moe_adapter_args& a) {
+  if (!a.offsets || a.segments == 0) return false;
+  const long long rank = a.rank > 64 ? 2 * a.rank : a.rank;
+  return a.rows / a.segments * rank >= 4096 && a.rows * rank >= 65536;
 }
 
 }  // namespace
@@ -316,7 +327,8 @@ moe_status launch_add_adapters(moe_ctx* ctx, const moe_adapter_args& a, cudaStre
                         static_cast<const __nv_bfloat16*>(a.b), a.scale, a.offsets, a.adapter_of,
                         static_cast<const __nv_bfloat16*>(a.y_in), static_cast<__nv_bfloat16*>(a.y_out), ctx->d_status, a.rows,
                         a.N, a.K, a.rank, a.adapters, a.segments};
-  if (a.segments > 0 && a.offsets && a.rows >= moe_knob_value(ctx, "ad_rows", 128) && a.rows / a.segments >= moe_knob_value(ctx, "ad_min", 16)) return launch_adapter_tiles(ctx, p, stream);
+  if (moe_knob_value(ctx, "adapter_tiles", tiles_are_quicker(a) ? 1 : 0) != 0 && a.offsets && a.segments > 0)
+    return launch_adapter_tiles(ctx, p, stream);
   const int units = units_of(a.rows, a.adapters, a.segments);
   const long long items = (a.rows + kWindow - 1) / kWindow * units;
   const int cluster = cluster_of(items);
@@ -324,7 +336,7 @@ moe_status launch_add_adapters(moe_ctx* ctx, const moe_adapter_args& a, cudaStre
   cudaLaunchAttribute attr{};
   cfg.gridDim = dim3(static_cast<unsigned>(items * cluster));
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem_of(a.rank);
+  cfg.dynamicSmemBytes = smem_of(a.rank, cluster);
   cfg.stream = stream;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
@@ -338,8 +350,8 @@ moe_status launch_add_adapters(moe_ctx* ctx, const moe_adapter_args& a, cudaStre
 
 cudaError_t prepare_adapters(moe_ctx* ctx) {
   cudaError_t e = prepare_adapter_tiles(ctx);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(adapter_rows<8>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(64));
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(adapter_rows<16>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(128));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(adapter_rows<8>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(64, kMaxCluster));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(adapter_rows<16>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(128, kMaxCluster));
   return e;
 }
 
