@@ -604,7 +604,8 @@ moe_status moe_add_rms_norm(moe_ctx* ctx, const moe_rms_norm_args* args, void* s
  *     d_x    = bf16( d_sum + rstd (g - h mean(g h)) )   (the gradient of x and of residual alike)
  *     d_gain = sum over rows of d_out h                 (fp32, fixed order)
  * scratch: moe_rms_norm_scratch_bytes bytes on the device when d_gain is asked for (undefined after).  d_x may be the buffer of
- * d_out or d_sum.  rows == 0 gives a d_gain of zeros.  Limits as above.  Errors: as above, and WORKSPACE_TOO_SMALL.
+ * d_out or d_sum.  rows == 0 gives a d_gain of zeros.  A scratch measured for more rows of the same length does for fewer.
+ * Limits as above.  Errors: as above, and WORKSPACE_TOO_SMALL; TIMEOUT through the status word (detail 301).
  */
 typedef struct {
   const void* s;            /* bf16 [rows, cols]: what the forward call normalised (its sum_out, or x) */
@@ -677,6 +678,7 @@ moe_status moe_balance_loss_backward(moe_ctx* ctx, const moe_balance_args* args,
  * An adapter index >= adapters is reported through the status word (MOE_ERR_BAD_ROUTING, detail = the segment) and its rows
  * are copied.  A lower-ranked adapter is padded with zeros.
  * scratch: moe_adapter_scratch_bytes bytes (0, and NULL will do, for all sizes the present kernels take: t stays on the chip).
+ * TIMEOUT through the status word: detail 201 to 206.
  * Limits: 0 <= rows < 2^28; N, K multiples of 8; rank a multiple of 8, at most 128; 1 <= adapters, adapters * rank and
  * adapters * N < 2^31; 0 <= segments <= rows (segments == rows when offsets is NULL), else UNSUPPORTED_SHAPE.
  * ------------------------------------------------------------------------------------------------ */

@@ -139,10 +139,10 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
     return o < 0 ? 0LL : o > p.rows ? p.rows : o;
   };
   const int seg = moe::last_at_or_below(p.segments + 1, tile, lane, [&](int s) { return bound(s) / kTileRows + s; });
-  if (seg < 0) return leave();                             // (offsets that do not begin with 0)
+  if (seg < 0) return leave();
   const long long begin = bound(seg), end = seg < p.segments ? bound(seg + 1) : p.rows;
   const long long row0 = begin + (tile - (begin / kTileRows + seg)) * kTileRows;
-  if (row0 >= end) return leave();                         // (the whole cluster)
+  if (row0 < begin || row0 >= end) return leave();         // (the whole cluster; below begin: offsets that do not ascend)
   const int m = static_cast<int>(end - row0 < kTileRows ? end - row0 : kTileRows);
   int id = seg < p.segments ? __ldg(p.adapter_of + seg) : -1;
   if (id >= p.adapters) {

@@ -217,8 +217,10 @@ balance_partial(const BalanceParams p) {
   if (q >= 0) {
     const int begin = offset_at(p, q), end = offset_at(p, q + 1);
     const long long first = begin + (static_cast<long long>(slot) - (begin / p.slot_tokens + q)) * p.slot_tokens;
-    t0 = static_cast<int>(first < end ? first : end);
-    t1 = min(t0 + p.slot_tokens, end);
+    if (first >= begin && first < end) {                   // (below begin: offsets that do not ascend)
+      t0 = static_cast<int>(first);
+      t1 = min(t0 + p.slot_tokens, end);
+    }
   }
   __syncthreads();
 

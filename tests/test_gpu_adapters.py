@@ -3,6 +3,8 @@
 Bound of an element: half a bf16 step of y (2^-8), and in fp32 roundings of 2^-24: t sums K exact products in pieces of 16
 ((K / 16 + 64) of the magnitudes |x||a|, carried through |b|); the second product adds the rank's terms (rank + 8 of |t||b|), and t
 enters it as two bf16 terms (2^-16 of |t||b|)."""
+import os
+
 import numpy as np
 import pytest
 import torch
@@ -15,9 +17,21 @@ pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
 
 
-@pytest.fixture(scope="module")
-def ctx():
-    return binding.Context(1, 64, 64, 1, 1)
+@pytest.fixture(scope="module", params=["rule", "rows", "tiles"])
+def ctx(request):
+    """Every test runs three times: with the kernel that the sizes choose, and with either of them (calls without offsets have
+    one kernel)."""
+    before = os.environ.get("MOE_TUNING")
+    if request.param != "rule":
+        os.environ["MOE_TUNING"] = f"x.adapter_tiles={int(request.param == 'tiles')}"
+    try:
+        made = binding.Context(1, 64, 64, 1, 1)
+    finally:
+        if before is None:
+            os.environ.pop("MOE_TUNING", None)
+        else:
+            os.environ["MOE_TUNING"] = before
+    return made
 
 
 def bf16(v):
@@ -94,6 +108,44 @@ def test_segments(ctx, rows, N, K, rank, adapters, segments, tail):
     ids = rng.integers(-1 if segments > 2 else 0, adapters, segments)
     check(p, ids, offsets, run(ctx, p, ids, offsets))
     assert ctx.moe_last_device_status() == (0, 0)
+
+
+@pytest.mark.parametrize("rows,N,K,rank,adapters,segments,tail", [
+    (1, 8, 8, 8, 1, 1, 0), (15, 64, 64, 16, 2, 1, 3), (17, 72, 136, 24, 2, 2, 0), (127, 200, 520, 40, 3, 3, 0), (5000, 264, 264, 16, 3, 4, 9),
+    (9000, 72, 72, 8, 2, 3, 1), (1100, 4096, 1032, 64, 2, 2, 0), (600, 1032, 4096, 128, 2, 3, 0), (300, 16, 8, 72, 3, 2, 5),
+    (2300, 8, 512, 48, 4, 6, 0), (1030, 3000, 24, 56, 5, 3, 0)])
+def test_long_segments_of_odd_sizes(ctx, rows, N, K, rank, adapters, segments, tail):
+    p, rng = make(rows + rank, rows, N, K, rank, adapters)
+    offsets = cut(rng, rows, segments, tail)
+    ids = rng.integers(-1 if segments > 2 else 0, adapters, segments)
+    check(p, ids, offsets, run(ctx, p, ids, offsets))
+
+
+def test_segments_without_rows(ctx):
+    """Many empty segments at the same row, in front, between and behind."""
+    p, rng = make(12, 400, 136, 200, 16, 5)
+    offsets = np.array([0] * 40 + [150] * 70 + [151, 151, 280] + [400] * 50)
+    ids = rng.integers(0, 5, len(offsets) - 1)
+    check(p, ids, offsets, run(ctx, p, ids, offsets))
+
+
+def test_rows_behind_the_32nd_bit(ctx):
+    """x and y of more than 2^32 bytes: the first and the last rows."""
+    rows, N, K, rank = 280_000, 8192, 8192, 16
+    x = torch.zeros(rows, K, dtype=torch.bfloat16, device=DEV)
+    y = torch.zeros(rows, N, dtype=torch.bfloat16, device=DEV)
+    rng = np.random.default_rng(13)
+    q = dict(rows=rows, N=N, K=K, rank=rank, adapters=2, x=x, y=y, scale=None, scalev=None)
+    for name, v in (("a", rng.standard_normal((2, rank, K)) / np.sqrt(K)), ("b", rng.standard_normal((2, N, rank)) / np.sqrt(rank))):
+        q[name], q[name + "v"] = bf16(v)
+    part = 130
+    ends, values = bf16(rng.standard_normal((2 * part, K)))
+    x[:part], x[-part:] = ends[:part], ends[part:]
+    out = run(ctx, q, [0, 1], [0, rows // 2, rows], out=y)                          # in place
+    got = torch.cat([out[:part], out[-part:]])
+    few = dict(q, rows=2 * part, xv=values, yv=np.zeros((2 * part, N)), y=torch.zeros_like(got))
+    check(few, [0, 1], [0, part, 2 * part], got)
+    assert (out[part:-part] == 0).all()
 
 
 def test_one_long_segment_among_single_rows(ctx):
