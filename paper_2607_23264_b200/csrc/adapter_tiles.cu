@@ -32,32 +32,34 @@ constexpr int kBN = 64;                   // columns of a tile of y
 constexpr int kYBytes = kTileRows * 128;
 constexpr int kAtomA = kTileRows * 128;   // 64 ranks of one term of t
 constexpr int kAtomB = kBN * 128;         // 64 ranks of b
-constexpr int kYStages = 3, kBStages = 3;
+constexpr int kMaxYStages = 6, kBStages = 2;
 constexpr int kMaxCluster = 8;
 constexpr int kSumRows = 136;             // a share of the rows from each CTA, rounded up: c ceil(128 / c) for c <= 8
 
 struct Barriers {
-  uint64_t full[kMaxStages], empty[kMaxStages], y_full[kYStages], b_full[kBStages], b_empty[kBStages], acc_full[2], acc_empty[2],
+  uint64_t full[kMaxStages], empty[kMaxStages], y_full[kMaxYStages], b_full[kBStages], b_empty[kBStages], acc_full[2], acc_empty[2],
       sums_full;
   uint32_t tmem;
   int abort_flag;
 };
 
-// Shared memory of a CTA, from a 1024-byte boundary on: in the second phase the terms of t, b's ring and y's ring; in the first
-// the ring of x and a from the start, and behind it the sums that the cluster sends, in the place of y's last tiles.
+// Shared memory of a CTA: in the second phase the terms of t, b's ring and y's ring; in the first the ring of x and a from the
+// start, and behind it the sums that the cluster sends, in the place of y's last tiles; then the barriers.  112 KiB, of which an
+// SM holds two, and 192 above 64 ranks.
 struct Layout {
-  int atoms, rank16, pitch, stage_bytes, stages, b_at, y_at, sums_at, bytes;
+  int atoms, rank16, pitch, stage_bytes, stages, y_stages, b_at, y_at, sums_at, barriers_at, bytes;
   __host__ __device__ explicit Layout(int rank) {
     atoms = (rank + 63) / 64;
     rank16 = (rank + 15) / 16 * 16;
     pitch = rank + 4;                                      // floats of a row of sums: an odd number of 16 bytes
+    y_stages = atoms == 1 ? 4 : kMaxYStages;
     b_at = 2 * atoms * kAtomA;
     y_at = b_at + kBStages * atoms * kAtomB;
-    const int sums = kSumRows * pitch * 4;
-    bytes = y_at + kYBytes + (sums > (kYStages - 1) * kYBytes ? sums : (kYStages - 1) * kYBytes);
-    sums_at = bytes - sums;
+    barriers_at = y_at + y_stages * kYBytes;               // (the sums leave y's first tile alone: 136 x 132 x 4 < 5 x 16384)
+    sums_at = barriers_at - kSumRows * pitch * 4;
     stage_bytes = kXBytes + rank16 * 128;
     stages = sums_at / stage_bytes < kMaxStages ? sums_at / stage_bytes : kMaxStages;
+    bytes = barriers_at + static_cast<int>(sizeof(Barriers));
   }
 };
 
@@ -113,8 +115,9 @@ __device__ __forceinline__ bool epilogue_meets(bool gave_up) {
 // Grid: a cluster of `cluster` CTAs per tile.
 __global__ void __launch_bounds__(kThreads)
 adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int cluster) {
-  extern __shared__ unsigned char smem_raw[];
-  __shared__ Barriers bar;
+  extern __shared__ __align__(1024) unsigned char base[];
+  const Layout lay(p.rank);
+  Barriers& bar = *reinterpret_cast<Barriers*>(base + lay.barriers_at);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3;
   const int tile = blockIdx.x / cluster, part = blockIdx.x - tile * cluster;
 
@@ -155,8 +158,6 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
   const bool has = id >= 0;
   if (!has && p.y_in == p.y_out) return leave();           // nothing to add and nothing to copy
 
-  const Layout lay(p.rank);
-  unsigned char* base = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
   const uint32_t base_at = ptx::smem_u32(base);
   const int blocks = (p.K + kBK - 1) / kBK, parts = min(cluster, blocks);
   const bool sums = has && part < parts;                   // this CTA has a part of K
@@ -164,7 +165,7 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
   const int tiles = (p.N - 1) / kBN + 1;
   const int n0 = static_cast<int>(static_cast<long long>(tiles) * part / cluster);
   const int n1 = static_cast<int>(static_cast<long long>(tiles) * (part + 1) / cluster);
-  const int y_ahead = min(kYStages, n1 - n0);
+  const int y_ahead = min(lay.y_stages, n1 - n0);
   const bool few = m <= kShortRows;
   const CUtensorMap* tm_x = few ? &maps.x_short : &maps.x;
   const CUtensorMap* tm_in = few ? &maps.in_short : &maps.in;
@@ -174,7 +175,7 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
       ptx::mbar_init(ptx::smem_u32(&bar.full[i]), 1);
       ptx::mbar_init(ptx::smem_u32(&bar.empty[i]), 1);
     }
-    for (int i = 0; i < kYStages; ++i) ptx::mbar_init(ptx::smem_u32(&bar.y_full[i]), 1);
+    for (int i = 0; i < lay.y_stages; ++i) ptx::mbar_init(ptx::smem_u32(&bar.y_full[i]), 1);
     for (int i = 0; i < kBStages; ++i) {
       ptx::mbar_init(ptx::smem_u32(&bar.b_full[i]), 1);
       ptx::mbar_init(ptx::smem_u32(&bar.b_empty[i]), 1);
@@ -377,20 +378,20 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
       unsigned char* row = base + lay.y_at + ys * kYBytes + r * 128;
       if (ok && live && (has || !whole)) {
         ptx::tc_fence_after_sync();
+        if (has) {
+          uint32_t v[32], w[32];
+          ptx::tmem_ld_32x32(lanes + acc * kBN, v);
+          ptx::tmem_ld_32x32(lanes + acc * kBN + 32, w);
+          uint4 y[8];
 #pragma unroll
-        for (int half = 0; half < 2 && has; ++half) {
-          uint32_t v[32];
-          ptx::tmem_ld_32x32(lanes + acc * kBN + half * 32, v);
+          for (int c = 0; c < 8; ++c) y[c] = *reinterpret_cast<const uint4*>(row + ((c ^ (r & 7)) << 4));
           ptx::tmem_ld_wait();
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint4* at = reinterpret_cast<uint4*>(row + (((half * 4 + c) ^ (r & 7)) << 4));
-            uint4 y = *at;
-            y.x = add_pair(y.x, v[8 * c], v[8 * c + 1]);
-            y.y = add_pair(y.y, v[8 * c + 2], v[8 * c + 3]);
-            y.z = add_pair(y.z, v[8 * c + 4], v[8 * c + 5]);
-            y.w = add_pair(y.w, v[8 * c + 6], v[8 * c + 7]);
-            *at = y;
+          for (int c = 0; c < 8; ++c) {
+            const uint32_t* d = c < 4 ? v + 8 * c : w + 8 * (c - 4);
+            y[c] = make_uint4(add_pair(y[c].x, d[0], d[1]), add_pair(y[c].y, d[2], d[3]), add_pair(y[c].z, d[4], d[5]),
+                              add_pair(y[c].w, d[6], d[7]));
+            *reinterpret_cast<uint4*>(row + ((c ^ (r & 7)) << 4)) = y[c];
           }
         }
         if (!whole) {                                      // a whole tile leaves by TMA, the rows of another one from here
@@ -420,10 +421,10 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
         }
         if (i > n0 && i - 1 + y_ahead < n1) {              // the tile before this has left: a later one takes its place
           ptx::bulk_wait_group_read_but_one();
-          load_y(ys == 0 ? kYStages - 1 : ys - 1, i - 1 + y_ahead);
+          load_y(ys == 0 ? lay.y_stages - 1 : ys - 1, i - 1 + y_ahead);
         }
       }
-      if (++ys == kYStages) { ys = 0; y_phase ^= 1u; }
+      if (++ys == lay.y_stages) { ys = 0; y_phase ^= 1u; }
     }
     if (warp == 2 && lane == 0) ptx::bulk_wait_group_read_all();
     __syncwarp();
@@ -480,7 +481,7 @@ moe_status launch_adapter_tiles(moe_ctx* ctx, const AdapterParams& p, cudaStream
   cudaLaunchAttribute attr{};
   cfg.gridDim = dim3(static_cast<unsigned>(tiles * cluster));
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = 1024 + Layout(p.rank).bytes;
+  cfg.dynamicSmemBytes = Layout(p.rank).bytes;
   cfg.stream = stream;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
@@ -493,7 +494,7 @@ moe_status launch_adapter_tiles(moe_ctx* ctx, const AdapterParams& p, cudaStream
 
 cudaError_t prepare_adapter_tiles(moe_ctx* ctx) {
   (void)ctx;
-  return cudaFuncSetAttribute(adapter_tiles, cudaFuncAttributeMaxDynamicSharedMemorySize, 1024 + Layout(128).bytes);
+  return cudaFuncSetAttribute(adapter_tiles, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout(128).bytes);
 }
 
 }  // namespace moe
