@@ -23,6 +23,7 @@ using moe::AdapterParams;
 constexpr unsigned kFull = 0xFFFFFFFFu;
 constexpr int kTileRows = 128;
 constexpr int kShortRows = 16;            // tiles of up to so many rows load that many
+constexpr int kSlabRows = 32;
 constexpr int kThreads = 192;
 constexpr int kBK = 64;                   // values of K in a stage: 128 bytes of bf16
 constexpr int kCols = 128;                // accumulator columns: t's, later two tiles of y
@@ -30,6 +31,7 @@ constexpr int kXBytes = kTileRows * 128;
 constexpr int kMaxStages = 6;
 constexpr int kBN = 64;                   // columns of a tile of y
 constexpr int kYBytes = kTileRows * 128;
+constexpr int kSlabBytes = kYBytes / 4;   // 32 rows of it: what one epilogue warp loads, changes and stores by itself
 constexpr int kAtomA = kTileRows * 128;   // 64 ranks of one term of t
 constexpr int kAtomB = kBN * 128;         // 64 ranks of b
 constexpr int kMaxYStages = 6, kBStages = 2;
@@ -37,7 +39,7 @@ constexpr int kMaxCluster = 8;
 constexpr int kSumRows = 136;             // a share of the rows from each CTA, rounded up: c ceil(128 / c) for c <= 8
 
 struct Barriers {
-  uint64_t full[kMaxStages], empty[kMaxStages], y_full[kMaxYStages], b_full[kBStages], b_empty[kBStages], acc_full[2], acc_empty[2],
+  uint64_t full[kMaxStages], empty[kMaxStages], y_full[kMaxYStages][4], b_full[kBStages], b_empty[kBStages], acc_full[2], acc_empty[2],
       sums_full;
   uint32_t tmem;
   int abort_flag;
@@ -96,22 +98,6 @@ __device__ __forceinline__ uint32_t add_pair(uint32_t y, uint32_t d0, uint32_t d
   return pair(low(y) + __uint_as_float(d0), high(y) + __uint_as_float(d1));
 }
 
-// The four epilogue warps meet; whether any of them has given up.
-__device__ __forceinline__ bool epilogue_meets(bool gave_up) {
-  uint32_t any;
-  asm volatile(
-      "{\n"
-      ".reg .pred p, q;\n"
-      "setp.ne.b32 p, %1, 0;\n"
-      "barrier.cta.red.or.pred q, 2, 128, p;\n"
-      "selp.u32 %0, 1, 0, q;\n"
-      "}\n"
-      : "=r"(any)
-      : "r"(static_cast<uint32_t>(gave_up))
-      : "memory");
-  return any != 0;
-}
-
 // Grid: a cluster of `cluster` CTAs per tile.
 __global__ void __launch_bounds__(kThreads)
 adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int cluster) {
@@ -168,14 +154,14 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
   const int y_ahead = min(lay.y_stages, n1 - n0);
   const bool few = m <= kShortRows;
   const CUtensorMap* tm_x = few ? &maps.x_short : &maps.x;
-  const CUtensorMap* tm_in = few ? &maps.in_short : &maps.in;
-  const uint32_t tile_bytes = few ? kShortRows * 128 : kTileRows * 128;    // of x in a stage, and of a tile of y
+  const uint32_t x_bytes = few ? kShortRows * 128 : kXBytes;                 // of x in a stage
   if (threadIdx.x == 0) {
     for (int i = 0; i < lay.stages; ++i) {
       ptx::mbar_init(ptx::smem_u32(&bar.full[i]), 1);
       ptx::mbar_init(ptx::smem_u32(&bar.empty[i]), 1);
     }
-    for (int i = 0; i < lay.y_stages; ++i) ptx::mbar_init(ptx::smem_u32(&bar.y_full[i]), 1);
+    for (int i = 0; i < lay.y_stages; ++i)
+      for (int w = 0; w < 4; ++w) ptx::mbar_init(ptx::smem_u32(&bar.y_full[i][w]), 1);
     for (int i = 0; i < kBStages; ++i) {
       ptx::mbar_init(ptx::smem_u32(&bar.b_full[i]), 1);
       ptx::mbar_init(ptx::smem_u32(&bar.b_empty[i]), 1);
@@ -196,12 +182,13 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
   const int r = quarter * 32 + lane;                       // the row of an epilogue thread
   int y_issued = 0, b_issued = 0;                          // (warp 0's lane 0)
   const uint64_t once = ptx::l2_policy_evict_first();      // x and y are read once: what the last kernel wrote may stay in L2
-  auto load_y = [&](int slot, int n) {
-    const uint32_t full = ptx::smem_u32(&bar.y_full[slot]);
-    ptx::mbar_expect_tx(full, tile_bytes);
-    ptx::tma_load_2d_hint(base_at + lay.y_at + slot * kYBytes, tm_in, full, n * kBN, static_cast<int>(row0), once);
+  auto load_y = [&](int slot, int n, int w) {              // rows 32 w and on
+    if (32 * w >= m) return;
+    const uint32_t full = ptx::smem_u32(&bar.y_full[slot][w]);
+    ptx::mbar_expect_tx(full, few ? kShortRows * 128 : kSlabBytes);
+    ptx::tma_load_2d_hint(base_at + lay.y_at + slot * kYBytes + w * kSlabBytes, few ? &maps.in_short : &maps.in, full, n * kBN,
+                          static_cast<int>(row0) + 32 * w, once);
   };
-
   auto load_b = [&](int slot, int n) {
     const uint32_t full = ptx::smem_u32(&bar.b_full[slot]);
     ptx::mbar_expect_tx(full, lay.atoms * kAtomB);
@@ -221,7 +208,7 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
           ok = ptx::mbar_wait(ptx::smem_u32(&bar.empty[stage]), phase, abort_flag);
           if (!ok) break;
           const uint32_t full = ptx::smem_u32(&bar.full[stage]), at = base_at + stage * lay.stage_bytes;
-          ptx::mbar_expect_tx(full, tile_bytes + lay.rank16 * 128);
+          ptx::mbar_expect_tx(full, x_bytes + lay.rank16 * 128);
           ptx::tma_load_2d_hint(at, tm_x, full, kb * kBK, static_cast<int>(row0), once);
           ptx::tma_load_2d(at + kXBytes, &maps.a, full, kb * kBK, id * p.rank);
           if (++stage == lay.stages) { stage = 0; phase ^= 1u; }
@@ -233,7 +220,7 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
       if (lane == 0 && !*abort_flag) {
         for (; b_issued < min(kBStages, n1 - n0); ++b_issued) load_b(b_issued, n0 + b_issued);
         for (; y_issued < y_ahead && lay.y_at + (y_issued + 1) * kYBytes <= lay.sums_at; ++y_issued)
-          load_y(y_issued, n0 + y_issued);
+          for (int w = 0; w < 4; ++w) load_y(y_issued, n0 + y_issued, w);
       }
       __syncwarp();
       ptx::cluster_wait();
@@ -327,7 +314,8 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
   if (warp == 0) {
     if (lane == 0) {
       bool ok = true;
-      for (; y_issued < y_ahead; ++y_issued) load_y(y_issued, n0 + y_issued);
+      for (; y_issued < y_ahead; ++y_issued)
+        for (int w = 0; w < 4; ++w) load_y(y_issued, n0 + y_issued, w);
       int bs = 0;
       uint32_t b_phase = 1;
       for (int i = n0; i < n1 && has; ++i) {
@@ -369,64 +357,67 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
     }
     __syncwarp();
   } else {
-    const bool whole = m == kTileRows, live = quarter * 32 < m;
+    const bool whole = quarter * 32 + 32 <= m, live = quarter * 32 < m;      // the warp's rows: all of them, any of them
     int ys = 0, acc = 0;
     uint32_t y_phase = 0, acc_phase = 0;
     for (int i = n0; i < n1; ++i) {
-      bool ok = __all_sync(kFull, ptx::mbar_wait(ptx::smem_u32(&bar.y_full[ys]), y_phase, abort_flag) &&
-                                      (!has || ptx::mbar_wait(ptx::smem_u32(&bar.acc_full[acc]), acc_phase, abort_flag)));
-      unsigned char* row = base + lay.y_at + ys * kYBytes + r * 128;
-      if (ok && live && (has || !whole)) {
+      const bool ok =
+          __all_sync(kFull, (!live || ptx::mbar_wait(ptx::smem_u32(&bar.y_full[ys][quarter]), y_phase, abort_flag)) &&
+                                (!has || ptx::mbar_wait(ptx::smem_u32(&bar.acc_full[acc]), acc_phase, abort_flag)));
+      if (!ok) {
+        if (lane == 0) timed_out(p, 6);
+        break;
+      }
+      unsigned char* slab = base + lay.y_at + ys * kYBytes + quarter * kSlabBytes;
+      if (live && has) {
+        unsigned char* row = slab + lane * 128;
         ptx::tc_fence_after_sync();
-        if (has) {
-          uint32_t v[32], w[32];
-          ptx::tmem_ld_32x32(lanes + acc * kBN, v);
-          ptx::tmem_ld_32x32(lanes + acc * kBN + 32, w);
-          uint4 y[8];
+        uint32_t v[32], w[32];
+        ptx::tmem_ld_32x32(lanes + acc * kBN, v);
+        ptx::tmem_ld_32x32(lanes + acc * kBN + 32, w);
+        uint4 y[8];
 #pragma unroll
-          for (int c = 0; c < 8; ++c) y[c] = *reinterpret_cast<const uint4*>(row + ((c ^ (r & 7)) << 4));
-          ptx::tmem_ld_wait();
+        for (int c = 0; c < 8; ++c) y[c] = *reinterpret_cast<const uint4*>(row + ((c ^ (lane & 7)) << 4));
+        ptx::tmem_ld_wait();
 #pragma unroll
-          for (int c = 0; c < 8; ++c) {
-            const uint32_t* d = c < 4 ? v + 8 * c : w + 8 * (c - 4);
-            y[c] = make_uint4(add_pair(y[c].x, d[0], d[1]), add_pair(y[c].y, d[2], d[3]), add_pair(y[c].z, d[4], d[5]),
-                              add_pair(y[c].w, d[6], d[7]));
-            *reinterpret_cast<uint4*>(row + ((c ^ (r & 7)) << 4)) = y[c];
-          }
-        }
-        if (!whole) {                                      // a whole tile leaves by TMA, the rows of another one from here
-          __syncwarp();
-#pragma unroll
-          for (int it = 0; it < 8; ++it) {
-            const int rr = quarter * 32 + it * 4 + (lane >> 3), c = lane & 7;
-            if (rr < m && i * kBN + 8 * c < p.N)
-              *reinterpret_cast<uint4*>(p.y_out + static_cast<size_t>(row0 + rr) * p.N + i * kBN + 8 * c) =
-                  *reinterpret_cast<const uint4*>(base + lay.y_at + ys * kYBytes + rr * 128 + ((c ^ (rr & 7)) << 4));
-          }
+        for (int c = 0; c < 8; ++c) {
+          const uint32_t* d = c < 4 ? v + 8 * c : w + 8 * (c - 4);
+          y[c] = make_uint4(add_pair(y[c].x, d[0], d[1]), add_pair(y[c].y, d[2], d[3]), add_pair(y[c].z, d[4], d[5]),
+                            add_pair(y[c].w, d[6], d[7]));
+          *reinterpret_cast<uint4*>(row + ((c ^ (lane & 7)) << 4)) = y[c];
         }
         ptx::tc_fence_before_sync();
       }
+      if (whole) ptx::fence_proxy_async_smem();
       __syncwarp();
       if (has) {
         if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&bar.acc_empty[acc]));
         if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
       }
-      if (!ok && lane == 0) timed_out(p, 6);
-      ptx::fence_proxy_async_smem();
-      if (epilogue_meets(!ok)) break;                      // one verdict for the four warps
-      if (warp == 2 && lane == 0) {
+      if (live && !whole) {                                // all 32 rows leave by TMA, the rows of a segment's end from here
+#pragma unroll
+        for (int it = 0; it < 8; ++it) {
+          const int rr = it * 4 + (lane >> 3), c = lane & 7;
+          if (quarter * 32 + rr < m && i * kBN + 8 * c < p.N)
+            *reinterpret_cast<uint4*>(p.y_out + static_cast<size_t>(row0 + quarter * 32 + rr) * p.N + i * kBN + 8 * c) =
+                *reinterpret_cast<const uint4*>(slab + rr * 128 + ((c ^ (rr & 7)) << 4));
+        }
+        __syncwarp();
+      }
+      if (lane == 0) {
         if (whole) {
-          ptx::tma_store_2d(&maps.out, base_at + lay.y_at + ys * kYBytes, i * kBN, static_cast<int>(row0));
+          ptx::tma_store_2d(&maps.out, base_at + lay.y_at + ys * kYBytes + quarter * kSlabBytes, i * kBN,
+                            static_cast<int>(row0) + quarter * 32);
           ptx::bulk_commit_group();
         }
-        if (i > n0 && i - 1 + y_ahead < n1) {              // the tile before this has left: a later one takes its place
+        if (i > n0 && i - 1 + y_ahead < n1) {              // the rows before these have left: later ones take their place
           ptx::bulk_wait_group_read_but_one();
-          load_y(ys == 0 ? lay.y_stages - 1 : ys - 1, i - 1 + y_ahead);
+          load_y(ys == 0 ? lay.y_stages - 1 : ys - 1, i - 1 + y_ahead, quarter);
         }
       }
       if (++ys == lay.y_stages) { ys = 0; y_phase ^= 1u; }
     }
-    if (warp == 2 && lane == 0) ptx::bulk_wait_group_read_all();
+    if (lane == 0) ptx::bulk_wait_group_read_all();
     __syncwarp();
   }
 
@@ -472,8 +463,8 @@ moe_status launch_adapter_tiles(moe_ctx* ctx, const AdapterParams& p, cudaStream
   const uint64_t factor_rows = static_cast<uint64_t>(p.adapters) * p.rank, out_rows = static_cast<uint64_t>(p.adapters) * p.N;
   if (!encode(ctx, &m.x, p.x, p.rows, p.K, kTileRows) || !encode(ctx, &m.x_short, p.x, p.rows, p.K, kShortRows) ||
       !encode(ctx, &m.a, p.a, factor_rows, p.K, Layout(p.rank).rank16) ||
-      !encode(ctx, &m.b, p.b, out_rows, p.rank, kBN) || !encode(ctx, &m.in, p.y_in, p.rows, p.N, kTileRows) ||
-      !encode(ctx, &m.in_short, p.y_in, p.rows, p.N, kShortRows) || !encode(ctx, &m.out, p.y_out, p.rows, p.N, kTileRows))
+      !encode(ctx, &m.b, p.b, out_rows, p.rank, kBN) || !encode(ctx, &m.in, p.y_in, p.rows, p.N, kSlabRows) ||
+      !encode(ctx, &m.in_short, p.y_in, p.rows, p.N, kShortRows) || !encode(ctx, &m.out, p.y_out, p.rows, p.N, kSlabRows))
     return MOE_ERR_CUDA;
   const long long tiles = tiles_of(p.rows, p.segments);
   const int cluster = cluster_of(ctx, tiles, p.rank, p.N, p.K);
