@@ -34,12 +34,12 @@ constexpr int kYBytes = kTileRows * 128;
 constexpr int kSlabBytes = kYBytes / 4;   // 32 rows of it: what one epilogue warp loads, changes and stores by itself
 constexpr int kAtomA = kTileRows * 128;   // 64 ranks of one term of t
 constexpr int kAtomB = kBN * 128;         // 64 ranks of b
-constexpr int kMaxYStages = 6, kBStages = 2;
+constexpr int kMaxYStages = 6, kMaxBStages = 4;
 constexpr int kMaxCluster = 8;
 constexpr int kSumRows = 136;             // a share of the rows from each CTA, rounded up: c ceil(128 / c) for c <= 8
 
 struct Barriers {
-  uint64_t full[kMaxStages], empty[kMaxStages], y_full[kMaxYStages][4], b_full[kBStages], b_empty[kBStages], acc_full[2], acc_empty[2],
+  uint64_t full[kMaxStages], empty[kMaxStages], y_full[kMaxYStages][4], b_full[kMaxBStages], b_empty[kMaxBStages], acc_full[2], acc_empty[2],
       sums_full;
   uint32_t tmem;
   int abort_flag;
@@ -49,14 +49,15 @@ struct Barriers {
 // start, and behind it the sums that the cluster sends, in the place of y's last tiles; then the barriers.  112 KiB, of which an
 // SM holds two, and 192 above 64 ranks.
 struct Layout {
-  int atoms, rank16, pitch, stage_bytes, stages, y_stages, b_at, y_at, sums_at, barriers_at, bytes;
+  int atoms, rank16, pitch, stage_bytes, stages, y_stages, b_stages, b_at, y_at, sums_at, barriers_at, bytes;
   __host__ __device__ explicit Layout(int rank) {
     atoms = (rank + 63) / 64;
     rank16 = (rank + 15) / 16 * 16;
     pitch = rank + 4;                                      // floats of a row of sums: an odd number of 16 bytes
     y_stages = atoms == 1 ? 4 : kMaxYStages;
+    b_stages = atoms == 1 ? 2 : kMaxBStages;
     b_at = 2 * atoms * kAtomA;
-    y_at = b_at + kBStages * atoms * kAtomB;
+    y_at = b_at + b_stages * atoms * kAtomB;
     barriers_at = y_at + y_stages * kYBytes;               // (the sums leave y's first tile alone: 136 x 132 x 4 < 5 x 16384)
     sums_at = barriers_at - kSumRows * pitch * 4;
     stage_bytes = kXBytes + rank16 * 128;
@@ -162,7 +163,7 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
     }
     for (int i = 0; i < lay.y_stages; ++i)
       for (int w = 0; w < 4; ++w) ptx::mbar_init(ptx::smem_u32(&bar.y_full[i][w]), 1);
-    for (int i = 0; i < kBStages; ++i) {
+    for (int i = 0; i < lay.b_stages; ++i) {
       ptx::mbar_init(ptx::smem_u32(&bar.b_full[i]), 1);
       ptx::mbar_init(ptx::smem_u32(&bar.b_empty[i]), 1);
     }
@@ -218,31 +219,33 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
       }
       // nothing reads the ring any more: b, and y's tiles in front of the sums, may come
       if (lane == 0 && !*abort_flag) {
-        for (; b_issued < min(kBStages, n1 - n0); ++b_issued) load_b(b_issued, n0 + b_issued);
+        for (; b_issued < min(lay.b_stages, n1 - n0); ++b_issued) load_b(b_issued, n0 + b_issued);
         for (; y_issued < y_ahead && lay.y_at + (y_issued + 1) * kYBytes <= lay.sums_at; ++y_issued)
           for (int w = 0; w < 4; ++w) load_y(y_issued, n0 + y_issued, w);
       }
       __syncwarp();
       ptx::cluster_wait();
     } else if (warp == 1) {
-      if (lane == 0 && sums) {
+      if (sums) {
+        // (the whole warp runs the loop, one lane issues: the descriptors stay warp-uniform)
         const uint32_t idesc = ptx::idesc_bf16_f32(kTileRows, lay.rank16);
+        const uint64_t a0 = ptx::smem_desc_sw128(base_at);
         int stage = 0;
         uint32_t phase = 0;
-        bool ok = true;
         for (int kb = part; kb < blocks; kb += parts) {
-          ok = ptx::mbar_wait(ptx::smem_u32(&bar.full[stage]), phase, abort_flag);
-          if (!ok) break;
+          ptx::mbar_wait_or_flag(ptx::smem_u32(&bar.full[stage]), phase, abort_flag, 2);
           ptx::tc_fence_after_sync();
-          const uint32_t at = base_at + stage * lay.stage_bytes;
-          const uint64_t a = ptx::smem_desc_sw128(at), b = ptx::smem_desc_sw128(at + kXBytes);
+          if (ptx::elect_one()) {
+            const uint64_t a = a0 + static_cast<uint32_t>(stage * lay.stage_bytes) / 16, b = a + kXBytes / 16;
 #pragma unroll
-          for (int k = 0; k < kBK / 16; ++k) ptx::tc_mma_bf16(tmem, a + 2 * k, b + 2 * k, idesc, kb > part || k > 0);
-          ptx::tc_commit(ptx::smem_u32(&bar.empty[stage]));
+            for (int k = 0; k < kBK / 16; ++k) ptx::tc_mma_bf16(tmem, a + 2 * k, b + 2 * k, idesc, kb > part || k > 0);
+            ptx::tc_commit(ptx::smem_u32(&bar.empty[stage]));
+          }
+          __syncwarp();
           if (++stage == lay.stages) { stage = 0; phase ^= 1u; }
         }
-        if (ok) ptx::tc_commit(ptx::smem_u32(&bar.sums_full));
-        else timed_out(p, 2);
+        if (ptx::elect_one()) ptx::tc_commit(ptx::smem_u32(&bar.sums_full));
+        if (*abort_flag && lane == 0) timed_out(p, 2);
       }
       __syncwarp();
       ptx::cluster_wait();
@@ -324,36 +327,42 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
           if (!ok) break;
           load_b(bs, i);
         }
-        if (++bs == kBStages) { bs = 0; b_phase ^= 1u; }
+        if (++bs == lay.b_stages) { bs = 0; b_phase ^= 1u; }
       }
       if (!ok) timed_out(p, 4);
     }
     __syncwarp();
   } else if (warp == 1) {
-    if (lane == 0 && has) {
+    if (has) {
       const uint32_t idesc = ptx::idesc_bf16_f32(kTileRows, kBN);
+      const uint64_t a0 = ptx::smem_desc_sw128(base_at), b0 = ptx::smem_desc_sw128(base_at + lay.b_at);
+      const int steps = lay.rank16 / 16;
       int bs = 0, acc = 0;
       uint32_t b_phase = 0, acc_phase = 1;
-      bool ok = true;
       ptx::fence_proxy_async_all();
-      for (int i = n0; i < n1 && ok; ++i) {
-        ok = ptx::mbar_wait(ptx::smem_u32(&bar.b_full[bs]), b_phase, abort_flag) &&
-             ptx::mbar_wait(ptx::smem_u32(&bar.acc_empty[acc]), acc_phase, abort_flag);
-        if (!ok) break;
+      for (int i = n0; i < n1; ++i) {
+        ptx::mbar_wait_or_flag(ptx::smem_u32(&bar.b_full[bs]), b_phase, abort_flag, 5);
+        ptx::mbar_wait_or_flag(ptx::smem_u32(&bar.acc_empty[acc]), acc_phase, abort_flag, 5);
         ptx::tc_fence_after_sync();
-        for (int term = 0; term < 2; ++term) {
-          for (int k = 0; k < lay.rank16 / 16; ++k) {
-            const uint64_t a = ptx::smem_desc_sw128(base_at + (term * lay.atoms + (k >> 2)) * kAtomA) + 2 * (k & 3);
-            const uint64_t b = ptx::smem_desc_sw128(base_at + lay.b_at + (bs * lay.atoms + (k >> 2)) * kAtomB) + 2 * (k & 3);
-            ptx::tc_mma_bf16(tmem + acc * kBN, a, b, idesc, term > 0 || k > 0);
+        if (ptx::elect_one()) {
+          const uint32_t d = tmem + acc * kBN;
+          const uint64_t b = b0 + static_cast<uint32_t>(bs * lay.atoms * kAtomB) / 16;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {                    // both terms of 16 ranks on the same 16 of b
+            if (k < steps) {
+              const uint64_t at = a0 + (k >> 2) * (kAtomA / 16) + 2 * (k & 3), with = b + (k >> 2) * (kAtomB / 16) + 2 * (k & 3);
+              ptx::tc_mma_bf16(d, at, with, idesc, k > 0);
+              ptx::tc_mma_bf16(d, at + lay.atoms * (kAtomA / 16), with, idesc, 1);
+            }
           }
+          ptx::tc_commit(ptx::smem_u32(&bar.b_empty[bs]));
+          ptx::tc_commit(ptx::smem_u32(&bar.acc_full[acc]));
         }
-        ptx::tc_commit(ptx::smem_u32(&bar.b_empty[bs]));
-        ptx::tc_commit(ptx::smem_u32(&bar.acc_full[acc]));
-        if (++bs == kBStages) { bs = 0; b_phase ^= 1u; }
+        __syncwarp();
+        if (++bs == lay.b_stages) { bs = 0; b_phase ^= 1u; }
         if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
       }
-      if (!ok) timed_out(p, 5);
+      if (*abort_flag && lane == 0) timed_out(p, 5);
     }
     __syncwarp();
   } else {
