@@ -67,9 +67,10 @@ __device__ __forceinline__ void prefetch_l2(const void* at) { asm volatile("pref
 __host__ __device__ constexpr int pitch_of(int rank) { return rank + 4; }
 int smem_of(int rank, int cluster) { return (kWarps + cluster + 1) * kRows * pitch_of(rank) * 4; }
 
-// kTiles: tiles of eight ranks held in registers (rank <= 8 * kTiles).  Grid: for each window `units` clusters.
+// kTiles: tiles of eight ranks held in registers (rank <= 8 * kTiles).  Grid: for each window `units` clusters.  Above 64 ranks one
+// CTA to an SM has the registers (rank 128, 64 tokens of 32 adapters, 4096 x 4096: 24.6 us; 41.1 at half as many, which spill).
 template <int kTiles>
-__global__ void __launch_bounds__(kThreads, 2)
+__global__ void __launch_bounds__(kThreads, kTiles <= 8 ? 2 : 1)
 adapter_rows(const AdapterParams p, int units, int cluster) {
   extern __shared__ float4 smem4[];
   __shared__ __align__(16) int s_id[kWindow];
@@ -146,7 +147,9 @@ adapter_rows(const AdapterParams p, int units, int cluster) {
   float acc[kTiles][4];
 #pragma unroll
   for (int j = 0; j < kTiles; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
-  constexpr int kAhead = kTiles <= 4 ? 4 : 1;            // steps whose loads are in flight together
+  // Steps whose loads are in flight together, as far as registers go: rank 16, 64 tokens of 32 adapters 8.5 us against 9.3 with two
+  // and 10.2 with one; rank 32, 256 tokens of 32 adapters 14.5 us against 15.2 with four; rank 64 16.5 against 18.2 with two.
+  constexpr int kAhead = kTiles <= 2 ? 4 : kTiles <= 4 ? 2 : 1;
   for (int s = s0 + warp; s < s1; s += kWarps * kAhead) {
     uint4 xa[kAhead], xb[kAhead], w[kAhead][kTiles];
 #pragma unroll

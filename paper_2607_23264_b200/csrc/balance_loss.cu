@@ -34,9 +34,11 @@ struct Scratch {
   float* seq_z;
   int32_t* ticket;
 };
-// Tokens of a slot: two CTAs per SM, a multiple of eight.
+// Tokens of a slot, a multiple of eight: one slot per SM where its sixteen warps then have four tokens or more (balance_finish
+// reads half as much: 16384 tokens of 256 experts 12.0 us against 13.4 with two), two where there are fewer (4099 tokens of 64
+// experts 7.9 us against 8.7 with one, four 10).
 inline int slot_tokens_of(const moe_ctx* ctx) {
-  const int per = ctx->shape.T / (2 * ctx->num_sms) + 1;
+  const int per = ctx->shape.T / ((ctx->shape.T >= 64 * ctx->num_sms ? 1 : 2) * ctx->num_sms) + 1;
   return (per + 7) / 8 * 8;
 }
 // At most so many slots, whatever the tokens of one: grows with T and with the sequences.
@@ -408,9 +410,10 @@ balance_finish(const BalanceParams p, int slots, int32_t* __restrict__ counts, i
   }
 }
 
-// Warp w takes the tokens [w * chunk, (w + 1) * chunk).
+// Warp w takes the tokens [w * chunk, (w + 1) * chunk).  Two CTAs on an SM for up to 512 experts, at 128 registers: 16384 tokens
+// of 512 experts, loss and gradient, 45.5 us against 49.8 with one of more registers.
 template <int EL, int kVec, bool kSigmoid>
-__global__ void __launch_bounds__(kThreads, EL <= 8 ? 3 : 1)
+__global__ void __launch_bounds__(kThreads, EL <= 8 ? 3 : EL <= 16 ? 2 : 1)
 balance_backward(const BalanceParams p, int chunk, const int32_t* __restrict__ counts, const int32_t* __restrict__ tokens,
                  const float* __restrict__ d_loss, const float* add, float* d_logits) {
   const int lane = threadIdx.x & 31;
