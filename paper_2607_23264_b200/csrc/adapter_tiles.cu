@@ -12,6 +12,10 @@
 //
 // Warp 0 loads, warp 1 issues the products, warps 2-5 move between accumulator and shared memory; the first of y and b are on
 // their way while the parts of t are added.
+//
+// Bound by HBM in both phases (x in, then y in and out), with a gap of about 8 us between them in which the sums change hands:
+// nothing but the first tiles of y is in flight there.  8192 rows in 4 segments, 7168 -> 4096, rank 64: 51.5 us, 5.0 TB/s of the
+// 257 MB (39.2 us at the rate of a copy); rank 128: 55 us of kernel.  With scratch for t and two launches it took 62.
 #include "adapters.cuh"
 #include "ptx_sm100.cuh"
 #include "warp_search.cuh"
@@ -182,7 +186,7 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
   volatile int* abort_flag = &bar.abort_flag;
   const int r = quarter * 32 + lane;                       // the row of an epilogue thread
   int y_issued = 0, b_issued = 0;                          // (warp 0's lane 0)
-  const uint64_t once = ptx::l2_policy_evict_first();      // x and y are read once: what the last kernel wrote may stay in L2
+  const uint64_t once = ptx::l2_policy_evict_first();      // x and y are read once: b, a and y's writes may stay in L2 (51.5 us; 57.5 without)
   auto load_y = [&](int slot, int n, int w) {              // rows 32 w and on
     if (32 * w >= m) return;
     const uint32_t full = ptx::smem_u32(&bar.y_full[slot][w]);
@@ -454,7 +458,8 @@ bool encode(moe_ctx* ctx, CUtensorMap* map, const void* base, uint64_t rows, uin
 
 long long tiles_of(long long rows, int segments) { return rows / kTileRows + segments + 1; }
 
-// CTAs of a tile: as many as are resident at once (two on an SM, one above 64 ranks), at most a portable cluster.
+// CTAs of a tile: as many as are resident at once (two on an SM, one above 64 ranks), at most a portable cluster.  8192 rows, rank 64:
+// 51.5 us; 71.8 with one CTA to an SM.  8192 rows, rank 128: 69.9 us from one kernel to the next; 103 with clusters for two.
 int cluster_of(const moe_ctx* ctx, long long tiles, int rank, int N, int K) {
   const int most = (N - 1) / kBN + 1 > (K - 1) / kBK + 1 ? (N - 1) / kBN + 1 : (K - 1) / kBK + 1;
   long long c = (rank > 64 ? 1LL : 2LL) * ctx->num_sms / tiles;

@@ -3,10 +3,15 @@
 // adapter_rows: short segments and single tokens, where the factors are the bytes.  A cluster of up to eight CTAs takes a unit: up
 //               to 16 rows of one adapter out of a window of 256 neighbouring rows, so that a factor is read once for all of
 //               them.  The cluster finds its unit by itself: the rows of an adapter are counted, the first, the 17th, ... of
-//               them leads a unit, and units are numbered by their leaders.  Each CTA has a part of K and a range of columns.  t = x a^T: m16n8k16 products with both operands straight
-//               from global memory (a lane's 16 bytes of a row are eight neighbouring k; as x and a are permuted along k
-//               alike, no shuffle is needed), warps added in order through shared memory, and the sums sent to every CTA of the cluster.
-//               Then y += t b^T by the same products, t as two bf16 terms (16 bits of it).
+//               them leads a unit, and units are numbered by their leaders.  Each CTA has a part of K and a range of columns.
+//               t = x a^T: m16n8k16 products with both operands straight from global memory (a lane's 16 bytes of a row are
+//               eight neighbouring k; as x and a are permuted along k alike, no shuffle is needed), warps added in order
+//               through shared memory, and the sums sent to every CTA of the cluster.  Then y += t b^T by the same products, t
+//               as two bf16 terms: 16 bits of it, since one term's rounding would be as large as the output's.
+//
+// Bound by latencies: the search for the unit (about 1 us), a's and x's first lines, the exchange of the sums (2 us), b's and y's
+// lines.  64 tokens of 32 adapters, rank 16, 7168 -> 4096: 8.4 us, 1.6 TB/s of the 13.5 MB; 1501 rows in 40 uneven segments,
+// rank 24, 4112 -> 2104: 18.5 us.
 // Long segments take adapter_tiles.
 #include "adapters.cuh"
 #include "ptx_sm100.cuh"
@@ -301,22 +306,26 @@ int units_of(long long rows, int adapters, int segments) {
   const int units = distinct + window / kRows;
   return units < 1 ? 1 : units < window ? units : window;
 }
-// CTAs of a cluster: as many as leave about 512 CTAs, a little more than are resident at once, since there are fewer units than
-// clusters (1024 rows of 8 adapters, rank 32, 4096 x 4096, segments of 64: 24.7 us; 33.4 with 1024 CTAs, 20.6 to 34.4 with 300).
-int cluster_of(long long items) {
+// CTAs of a cluster: as many as leave 400 CTAs in all, 200 above 64 ranks: a little more than are resident at once, since there are
+// fewer units than clusters.  At 4096 x 4096 (us at 200 / 400 / 512): 200 tokens of 100 adapters, rank 16, 18.5 / 15.1 / 20.5; 1001 rows
+// of 16 adapters, rank 64, 35 / 30 / 37; rank 128, 64 tokens of 32 adapters 18.6 / 24.7 / 24.7, 300 of 8 22.6 / 32.9 / 32.9.
+int cluster_of(long long items, int rank) {
+  const int most = rank > 64 ? 200 : 400;
   int c = kMaxCluster;
-  while (c > 1 && items * c > 512) c /= 2;
+  while (c > 1 && items * c > most) c /= 2;
   return c;
 }
 // Whether tiles of 128 rows are quicker.  A unit of 16 rows reads a factor again, so the rows' cost grows with the rank; a tile costs
-// the same with few rows in it, and twenty microseconds to come through.  Above 64 ranks a unit's sums leave an SM room for few
-// CTAs.  Measured at 4096 x 7168, 8 adapters (rows / tiles, us): rank 64, segments of 64: 1024 rows 37 / 29, 4096 rows 75 / 62;
-// segments of 16: 39 / 45, 117 / 150; rank 16, segments of 256: 2048 rows 23 / 29, 4096 rows 43 / 37; rank 128 (1024 x 1024), segments
-// of 16: 256 rows 31 / 19, 1024 rows 49 / 27.
+// the same with few rows in it, and fifteen microseconds to come through.  Above 64 ranks a unit's sums and registers leave an SM
+// room for one CTA.  Measured at 4096 x 4096, 8 adapters (rows / tiles, us).  Rank 16: 1024 rows in segments of 256 14 / 20, 4096
+// rows in segments of 64 38 / 43, of 128 36 / 36, of 256 36 / 29.  Rank 64: 256 rows 15 / 19, 1024 rows in segments of 64 30 / 23,
+// 4096 rows in segments of 16 99 / 104, of 64 62 / 47, of 256 59 / 33.  Rank 128: 256 rows in segments of 8 31 / 30, of 32
+// 30 / 20, 4096 rows in segments of 8 168 / 315, of 32 131 / 99, of 256 129 / 44.
 bool tiles_are_quicker(const moe_adapter_args& a) {
   if (!a.offsets || a.segments == 0) return false;
-  const long long rank = a.rank > 64 ? 2 * a.rank : a.rank;
-  return a.rows / a.segments * rank >= 4096 && a.rows * rank >= 65536;
+  const bool one_cta = a.rank > 64;
+  const long long cost = one_cta ? 2 * a.rank : a.rank;
+  return a.rows / a.segments * cost >= 4096 && a.rows * cost >= (one_cta ? 40960 : 65536);
 }
 
 }  // namespace
@@ -334,7 +343,7 @@ moe_status launch_add_adapters(moe_ctx* ctx, const moe_adapter_args& a, cudaStre
     return launch_adapter_tiles(ctx, p, stream);
   const int units = units_of(a.rows, a.adapters, a.segments);
   const long long items = (a.rows + kWindow - 1) / kWindow * units;
-  const int cluster = cluster_of(items);
+  const int cluster = cluster_of(items, a.rank);
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr{};
   cfg.gridDim = dim3(static_cast<unsigned>(items * cluster));

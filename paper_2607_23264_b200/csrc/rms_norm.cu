@@ -6,6 +6,14 @@
 // norm_backward : the CTAs stay and take every gridDim-th group of rows; the rows to come are on their way into a ring in shared
 //                 memory by bulk copies; a lane's columns are the same in all rows, so its gains stay in registers, and the
 //                 gain's gradient is summed there: one partial row per CTA, added by norm_gain_sum in a fixed order.
+//
+// n = s rstd (gain + offset) with rstd = (mean s^2 + eps)^-1/2; with h = s rstd and g = (gain + offset) d_out,
+// dx = d_sum + rstd (g - h mean(g h)) and d_gain = sum over rows of d_out h.  All of it fp32; s, out and dx are rounded to bf16
+// once, codes from the fp32 n.
+//
+// Bound by HBM for many rows: 8192 x 7168 with residual, bf16 and 8-bit outputs 85.9 us, 6.2 TB/s (80.8 at the rate of a copy); the
+// gradients of 8192 x 4096 54 us, 44 of them norm_backward at 6.1 TB/s, 4.8 norm_gain_sum, the rest between the two.  64 x 7168:
+// 4.2 us, of which the launch is half; the gradients of 301 x 7168 12.4 us: two launches of two loads' latency each.
 #include <cuda_bf16.h>
 
 #include "blk_quant.cuh"
@@ -295,7 +303,8 @@ norm_backward(const NormGradParams p, const Share share) {
   if (threadIdx.x == 0)
     for (int i = 0; i < p.ring; ++i) fill(i, row0 + i * step);
 
-  // a lane's columns are the same in all rows: its gains stay in registers, where a thread has enough of them
+  // a lane's columns are the same in all rows: its gains stay in registers, where a thread has enough of them (8192 x 4096 53.8 us,
+  // 57.5 with the gains read from L1 for each row)
   constexpr bool kKeepGain = kThreads <= 256;
   float acc[kVecs][8], gains[kKeepGain ? kVecs : 1][8];
 #pragma unroll
@@ -487,7 +496,8 @@ NormKernel norm_kernel(const moe_rms_norm_args& a) {
   }
 }
 
-// norm_backward: the CTAs of an SM that its registers and rings allow, and the rings' depth.
+// norm_backward: the CTAs of an SM that its registers and rings allow, and the rings' depth.  Two CTAs for up to 8192 columns: 8192 x
+// 7168 81.8 us against 96.4 with one, 8192 x 4096 53.8 against 53.4.
 struct BackwardPlan {
   Share share;
   int ctas, depth;
