@@ -674,7 +674,8 @@ moe_status moe_balance_loss_backward(moe_ctx* ctx, const moe_balance_args* args,
  * the last segment, are copied bit for bit.  Prompts are long segments, decoded tokens segments of one row (offsets NULL: every
  * row is a segment), in any mixture; neighbouring rows of one adapter share its reads.  The gradient with respect to x is the
  * same call with a and b exchanged, each transposed.
- *   x [rows, K] bf16, a [adapters, rank, K] bf16, b [adapters, N, rank] bf16, y_in, y_out [rows, N] bf16 (y_out may be y_in).
+ *   x [rows, K] bf16, a [adapters, rank, K] bf16, b [adapters, N, rank] bf16, y_in, y_out [rows, N] bf16 (y_out may be y_in;
+ * no other buffers may overlap).
  * An adapter index >= adapters is reported through the status word (MOE_ERR_BAD_ROUTING, detail = the segment) and its rows
  * are copied.  A lower-ranked adapter is padded with zeros.
  * scratch: moe_adapter_scratch_bytes bytes (0, and NULL will do, for all sizes the present kernels take: t stays on the chip).

@@ -141,7 +141,7 @@ def _packer(layout):
     """Packs a call's arguments as the C structure `layout` holds them: a third of the time that building one takes, which
     counts where the kernel itself takes a few microseconds."""
     codes = {C.c_void_p: "P", C.c_int64: "q", C.c_size_t: "N", C.c_int32: "i", C.c_float: "f"}
-    return struct.Struct("@" + "".join(codes[kind] for _, kind in layout._fields_)).pack
+    return struct.Struct("@" + "".join(codes[kind] for _, kind in layout._fields_) + "0P").pack
 
 
 _pack_rms_norm, _pack_rms_norm_grad = _packer(moe_rms_norm_args), _packer(moe_rms_norm_grad_args)
