@@ -13,6 +13,8 @@
 // lines.  64 tokens of 32 adapters, rank 16, 7168 -> 4096: 8.4 us, 1.6 TB/s of the 13.5 MB; 1501 rows in 40 uneven segments,
 // rank 24, 4112 -> 2104: 18.5 us.
 // Long segments take adapter_tiles.
+#include <cmath>
+
 #include "adapters.cuh"
 #include "ptx_sm100.cuh"
 
@@ -306,13 +308,19 @@ int units_of(long long rows, int adapters, int segments) {
   const int units = distinct + window / kRows;
   return units < 1 ? 1 : units < window ? units : window;
 }
-// CTAs of a cluster: as many as leave 400 CTAs in all, 200 above 64 ranks: a little more than are resident at once, since there are
-// fewer units than clusters.  At 4096 x 4096 (us at 200 / 400 / 512): 200 tokens of 100 adapters, rank 16, 18.5 / 15.1 / 20.5; 1001 rows
-// of 16 adapters, rank 64, 35 / 30 / 37; rank 128, 64 tokens of 32 adapters 18.6 / 24.7 / 24.7, 300 of 8 22.6 / 32.9 / 32.9.
-int cluster_of(long long items, int rank) {
-  const int most = rank > 64 ? 200 : 400;
+// CTAs of a cluster: as many as are resident at once when clusters without a unit are left out.  What is to be expected of a window of n
+// rows: s segments that choose among A adapters leave A (1 - e^(-s/A)) of them, and those make (n + 15 distinct) / 16 units at most.
+// At 4096 x 4096 (us with 2 / 4 / 8 CTAs to a unit, the choice in brackets): 256 tokens of 32 adapters, rank 32, 12.4 (4) / 14.5 with
+// 8; 200 tokens of 100, rank 16, 15.1 (2) / 20.5 with 4; rank 128, 64 tokens of 32 adapters 18.6 (4) / 24.7 with 8.
+int cluster_of(long long rows, int segments, bool offsets, int adapters, int rank) {
+  const double most = rank > 64 ? 160 : 320;               // (one CTA to an SM, or two; a few more do no harm)
+  auto units = [&](double n) {
+    const double s = offsets ? n * segments / rows + 1 : n;
+    return (n + 15 * adapters * (1 - exp(-s / adapters))) / 16;
+  };
+  const double all = static_cast<double>(rows / kWindow) * units(kWindow) + (rows % kWindow ? units(static_cast<double>(rows % kWindow)) : 0);
   int c = kMaxCluster;
-  while (c > 1 && items * c > most) c /= 2;
+  while (c > 1 && all * c > most) c /= 2;
   return c;
 }
 // Whether tiles of 128 rows are quicker.  A unit of 16 rows reads a factor again, so the rows' cost grows with the rank; a tile costs
@@ -343,7 +351,7 @@ moe_status launch_add_adapters(moe_ctx* ctx, const moe_adapter_args& a, cudaStre
     return launch_adapter_tiles(ctx, p, stream);
   const int units = units_of(a.rows, a.adapters, a.segments);
   const long long items = (a.rows + kWindow - 1) / kWindow * units;
-  const int cluster = cluster_of(items, a.rank);
+  const int cluster = cluster_of(a.rows, a.segments, a.offsets != nullptr, a.adapters, a.rank);
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr{};
   cfg.gridDim = dim3(static_cast<unsigned>(items * cluster));

@@ -496,8 +496,9 @@ NormKernel norm_kernel(const moe_rms_norm_args& a) {
   }
 }
 
-// norm_backward: the CTAs of an SM that its registers and rings allow, and the rings' depth.  Two CTAs for up to 8192 columns: 8192 x
-// 7168 81.8 us against 96.4 with one, 8192 x 4096 53.8 against 53.4.
+// norm_backward: the CTAs of an SM that its registers and rings allow, and the rings' depth.  Two CTAs for up to 8192 columns, three
+// where a row takes five warps (and a CTA one row): 8192 x 7168 81.8 us against 96.4 with one, 8192 x 4096 53.8 against 53.4; 7774 x
+// 4152 49.3 with three against 59.5 with two.
 struct BackwardPlan {
   Share share;
   int ctas, depth;
@@ -507,7 +508,7 @@ BackwardPlan backward_plan(int cols) {
   BackwardPlan b;
   b.share = share_of(cols / 8, 4);
   const size_t slot = static_cast<size_t>(3) * b.share.rows * cols * 2;   // (as if d_sum were given)
-  b.ctas = threads_of(b.share) <= 256 && 4 * slot <= kRingBytes ? 2 : 1;
+  b.ctas = threads_of(b.share) > 256 || 4 * slot > kRingBytes ? 1 : threads_of(b.share) <= 160 ? 3 : 2;
   b.depth = static_cast<int>(kRingBytes / b.ctas / slot);
   if (b.depth > kMaxRing) b.depth = kMaxRing;
   b.bytes = b.depth * slot;               // (the longest row takes 192 KiB)
