@@ -313,3 +313,26 @@ def test_refusals_of_the_gradient(ctx):
     with pytest.raises(ValueError):
         ctx.moe_add_rms_norm(t[:, ::2], None, g, rows, cols // 2, out=t)
     assert ctx.rms_norm_scratch_bytes(1, 4) == 0 and ctx.rms_norm_scratch_bytes(-1, 8) == 0
+
+
+@pytest.mark.parametrize("rows,cols", [(2500, 1032), (450, 7168), (20011, 128), (1203, 4104), (445, 6152), (1300, 2048)])
+@pytest.mark.parametrize("gain,offset", [("bf16", 0.0), ("fp32", 1.0)])
+def test_more_rows_than_are_resident_without_residual_and_codes(ctx, rows, cols, gain, offset):
+    rng = np.random.default_rng(rows + cols)
+    x, xv, _, _, g, gv = make(rng, rows, cols, gain)
+    x[1], xv[1] = 0, 0
+    x[rows // 2, 3] = float("nan")                             # spoils its own row, and none that the CTA takes before or after
+    o = outputs(rows, cols, "none", extra=2)
+    ctx.moe_add_rms_norm(x, None, g, rows, cols, eps=EPS, gain_offset=offset, **o)
+    torch.cuda.synchronize()
+    assert ctx.moe_last_launch_count() == 1
+    n = ao.rms_norm(xv, gv, EPS, offset)
+    keep = np.arange(rows) != rows // 2
+    got = dev_bf16_to_f64(o["out"][:rows])
+    assert np.isnan(got[~keep]).all()
+    assert (np.abs(got - n) <= (2.0 ** -8 + 30 * U) * np.abs(n) + 2.0 ** -134)[keep].all()
+    assert torch.equal(o["sum_out"][:rows].view(torch.int16), x.view(torch.int16))
+    assert o["out"][rows:].isnan().all() and o["sum_out"][rows:].isnan().all()
+    again = x.clone()                                          # in place, the same bits
+    ctx.moe_add_rms_norm(again, None, g, rows, cols, out=again, eps=EPS, gain_offset=offset)
+    assert torch.equal(again.view(torch.int16), o["out"][:rows].view(torch.int16))
