@@ -415,6 +415,7 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
             *reinterpret_cast<uint4*>(p.y_out + static_cast<size_t>(row0 + quarter * 32 + rr) * p.N + i * kBN + 8 * c) =
                 *reinterpret_cast<const uint4*>(slab + rr * 128 + ((c ^ (rr & 7)) << 4));
         }
+        ptx::fence_proxy_async_smem();                     // TMA writes the slab next: behind these writes and reads
         __syncwarp();
       }
       if (lane == 0) {
