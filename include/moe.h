@@ -670,10 +670,10 @@ moe_status moe_balance_loss_backward(moe_ctx* ctx, const moe_balance_args* args,
  * Low-rank adapters of many requests beside a shared projection (moe_gemm_blk, or any other).  Rows belong to segments
  * (requests), a segment to an adapter i or to none:
  *     y_out[r,n] = bf16( y_in[r,n] + scale_i * sum_j b[i,n,j] t[r,j] ),   t[r,j] = sum_k x[r,k] a[i,j,k]
- * with fp32 sums (t enters the second product as two bf16 terms, 16 bits of it).  Rows without an adapter, and rows behind
- * the last segment, are copied bit for bit.  Prompts are long segments, decoded tokens segments of one row (offsets NULL: every
- * row is a segment), in any mixture; neighbouring rows of one adapter share its reads.  The gradient with respect to x is the
- * same call with a and b exchanged, each transposed.
+ * with fp32 sums (t enters the second product as two bf16 terms, 16 bits of it); infinities and NaN of any operand come out
+ * as the formula has them.  Rows without an adapter, and rows behind the last segment, are copied bit for bit.  Prompts are long
+ * segments, decoded tokens segments of one row (offsets NULL: every row is a segment), in any mixture; neighbouring rows of one
+ * adapter share its reads.  The gradient with respect to x is the same call with a and b exchanged, each transposed.
  *   x [rows, K] bf16, a [adapters, rank, K] bf16, b [adapters, N, rank] bf16, y_in, y_out [rows, N] bf16 (y_out may be y_in;
  * no other buffers may overlap).
  * An adapter index >= adapters is reported through the status word (MOE_ERR_BAD_ROUTING, detail = the segment) and its rows

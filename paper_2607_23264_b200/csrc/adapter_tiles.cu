@@ -79,28 +79,41 @@ __device__ __forceinline__ void timed_out(const AdapterParams& p, int where) {
   atomicCAS(&p.status[1], 0, 200 + where);
 }
 
-// Eight values as two terms of bf16: v - hi is exact, so hi + lo keeps 16 bits.
-__device__ __forceinline__ uint32_t pair(float a, float b) {
-  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
-__device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+// Eight values as two terms of bf16.
 __device__ __forceinline__ void two_terms(const float (&v)[8], uint4& hi, uint4& lo) {
-  uint32_t h[4], l[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    h[i] = pair(v[2 * i], v[2 * i + 1]);
-    // (an infinite or NaN value: the first term says it all)
-    const float a = v[2 * i] - low(h[i]), b = v[2 * i + 1] - high(h[i]);
-    l[i] = pair(a == a ? a : 0.f, b == b ? b : 0.f);
-  }
-  hi = make_uint4(h[0], h[1], h[2], h[3]);
-  lo = make_uint4(l[0], l[1], l[2], l[3]);
+  moe::two_terms(v[0], v[1], hi.x, lo.x);
+  moe::two_terms(v[2], v[3], hi.y, lo.y);
+  moe::two_terms(v[4], v[5], hi.z, lo.z);
+  moe::two_terms(v[6], v[7], hi.w, lo.w);
 }
 // y + d in bf16.
 __device__ __forceinline__ uint32_t add_pair(uint32_t y, uint32_t d0, uint32_t d1) {
-  return pair(low(y) + __uint_as_float(d0), high(y) + __uint_as_float(d1));
+  return moe::pair(moe::low(y) + __uint_as_float(d0), moe::high(y) + __uint_as_float(d1));
+}
+
+// The NaN of a row's `cols` columns formed again: y + t b with t = hi + lo.  `row`, `hi`, `lo`: 128 bytes of a swizzled atom, whose
+// 16-byte chunk c lies at c ^ swizzle; b and y begin at the first column.
+__device__ __forceinline__ void sum_again(unsigned char* row, const unsigned char* hi, const unsigned char* lo, int swizzle,
+                                          const __nv_bfloat16* b, const __nv_bfloat16* y, int cols, int rank) {
+#pragma unroll 1
+  for (int n = 0; n < cols; ++n) {
+    __nv_bfloat16* at = reinterpret_cast<__nv_bfloat16*>(row + (((n >> 3) ^ swizzle) << 4)) + (n & 7);
+    if (!moe::is_nan(__bfloat16_as_ushort(*at))) continue;
+    float d = 0.f;
+#pragma unroll 1
+    for (int j = 0; j < rank; j += 8) {
+      const int chunk = (j >> 6) * kAtomA + ((((j >> 3) & 7) ^ swizzle) << 4);
+      const uint4 h = *reinterpret_cast<const uint4*>(hi + chunk), l = *reinterpret_cast<const uint4*>(lo + chunk);
+      const uint4 w = __ldg(reinterpret_cast<const uint4*>(b + static_cast<size_t>(n) * rank + j));
+      const uint32_t hs[4] = {h.x, h.y, h.z, h.w}, ls[4] = {l.x, l.y, l.z, l.w}, ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        d = fmaf(moe::low(hs[q]) + moe::low(ls[q]), moe::low(ws[q]), d);
+        d = fmaf(moe::high(hs[q]) + moe::high(ls[q]), moe::high(ws[q]), d);
+      }
+    }
+    *at = __float2bfloat16_rn(__bfloat162float(y[n]) + d);
+  }
 }
 
 // Grid: a cluster of `cluster` CTAs per tile.
@@ -399,6 +412,21 @@ adapter_tiles(const __grid_constant__ Maps maps, const AdapterParams p, int clus
                             add_pair(y[c].w, d[6], d[7]));
           *reinterpret_cast<uint4*>(row + ((c ^ (lane & 7)) << 4)) = y[c];
         }
+        uint32_t most[4] = {y[0].x, y[0].y, y[0].z, y[0].w};
+#pragma unroll
+        for (int c = 1; c < 7; c += 2) {
+          most[0] = moe::largest(most[0], y[c].x, y[c + 1].x);
+          most[1] = moe::largest(most[1], y[c].y, y[c + 1].y);
+          most[2] = moe::largest(most[2], y[c].z, y[c + 1].z);
+          most[3] = moe::largest(most[3], y[c].w, y[c + 1].w);
+        }
+        const uint32_t nan = moe::largest(moe::largest(most[0], most[1], y[7].x), moe::largest(most[2], most[3], y[7].y),
+                                          moe::largest(y[7].z, y[7].w, y[7].w));
+        if (r < m && moe::has_nan(nan))
+          // (y as it was: what leaves goes by this warp, later)
+          sum_again(row, base + r * 128, base + r * 128 + lay.atoms * kAtomA, lane & 7,
+                    p.b + (static_cast<size_t>(id) * p.N + i * kBN) * p.rank, p.y_in + static_cast<size_t>(row0 + r) * p.N + i * kBN,
+                    min(kBN, p.N - i * kBN), p.rank);
         ptx::tc_fence_before_sync();
       }
       if (whole) ptx::fence_proxy_async_smem();

@@ -60,14 +60,28 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
-__device__ __forceinline__ uint32_t pair(float a, float b) {
-  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
 // y + d in bf16.
-__device__ __forceinline__ uint32_t add_pair(uint32_t y, float d0, float d1) { return pair(low(y) + d0, high(y) + d1); }
+__device__ __forceinline__ uint32_t add_pair(uint32_t y, float d0, float d1) { return moe::pair(moe::low(y) + d0, moe::high(y) + d1); }
+// The NaN of eight sums formed again: y + t b, b with the first of the eight columns.
+__device__ __forceinline__ uint4 sums_again(const uint4 y, uint4 sum, const float* t, const __nv_bfloat16* b, int rank) {
+  const uint32_t old[4] = {y.x, y.y, y.z, y.w};
+  uint32_t w[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float v[2] = {moe::low(w[i]), moe::high(w[i])};
+    if (!moe::has_nan(w[i])) continue;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (v[h] == v[h]) continue;
+      float d = 0.f;
+#pragma unroll 1
+      for (int j = 0; j < rank; ++j) d = fmaf(t[j], __bfloat162float(b[static_cast<size_t>(2 * i + h) * rank + j]), d);
+      v[h] = (h == 0 ? moe::low(old[i]) : moe::high(old[i])) + d;
+    }
+    w[i] = moe::pair(v[0], v[1]);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
 __device__ __forceinline__ void prefetch_l2(const void* at) { asm volatile("prefetch.global.L2 [%0];" ::"l"(at)); }
 
 // Shared memory: [kWarps][kRows][pitch] sums of the warps, [kRows][pitch] t, [cluster][kRows][pitch] sums of the CTAs.
@@ -268,12 +282,7 @@ adapter_rows(const AdapterParams p, int units, int cluster) {
         const int k = rank_of(s, c) + 2 * e;
         const float* t = s_t + (g + 8 * h) * pitch + k;
         const bool in = g + 8 * h < count && k < p.rank;
-        const float t0 = in ? t[0] : 0.f, t1 = in ? t[1] : 0.f;
-        const uint32_t first_term = pair(t0, t1);
-        // (an infinite or NaN value: the first term says it all)
-        const float r0 = t0 - low(first_term), r1 = t1 - high(first_term);
-        hi[s][2 * e + h] = first_term;
-        lo[s][2 * e + h] = pair(r0 == r0 ? r0 : 0.f, r1 == r1 ? r1 : 0.f);
+        moe::two_terms(in ? t[0] : 0.f, in ? t[1] : 0.f, hi[s][2 * e + h], lo[s][2 * e + h]);
       }
     }
   }
@@ -294,9 +303,11 @@ adapter_rows(const AdapterParams p, int units, int cluster) {
     for (int h = 0; h < 2; ++h) {
       if ((h == 0 ? has_lo : has_hi) && n < n1) {
         const uint4 q = y[h];
-        *reinterpret_cast<uint4*>(p.y_out + (h == 0 ? y_lo : y_hi) + n) =
-            make_uint4(add_pair(q.x, acc_y[0][2 * h], acc_y[0][2 * h + 1]), add_pair(q.y, acc_y[1][2 * h], acc_y[1][2 * h + 1]),
-                       add_pair(q.z, acc_y[2][2 * h], acc_y[2][2 * h + 1]), add_pair(q.w, acc_y[3][2 * h], acc_y[3][2 * h + 1]));
+        uint4 v = make_uint4(add_pair(q.x, acc_y[0][2 * h], acc_y[0][2 * h + 1]), add_pair(q.y, acc_y[1][2 * h], acc_y[1][2 * h + 1]),
+                             add_pair(q.z, acc_y[2][2 * h], acc_y[2][2 * h + 1]), add_pair(q.w, acc_y[3][2 * h], acc_y[3][2 * h + 1]));
+        if (moe::has_nan(moe::largest(moe::largest(v.x, v.y, v.z), v.w, v.w)))
+          v = sums_again(q, v, s_t + (g + 8 * h) * pitch, b_base + static_cast<size_t>(n) * p.rank, p.rank);
+        *reinterpret_cast<uint4*>(p.y_out + (h == 0 ? y_lo : y_hi) + n) = v;
       }
     }
   }

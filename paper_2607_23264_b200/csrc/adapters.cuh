@@ -1,4 +1,4 @@
-// What the kernels of the adapters share: arguments, and the adapter of a row.
+// What the kernels of the adapters share: arguments, t as two bf16 terms, and sums that the terms cannot form.
 #pragma once
 #include <cuda_bf16.h>
 
@@ -24,6 +24,28 @@ struct AdapterParams {
 __device__ __forceinline__ void st_cluster(uint32_t at, const uint4& v) {
   asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
+
+__device__ __forceinline__ uint32_t pair(float a, float b) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// Two values as two terms of bf16 each: v - hi is exact, so hi + lo keeps 16 bits.
+__device__ __forceinline__ void two_terms(float v0, float v1, uint32_t& hi, uint32_t& lo) {
+  hi = pair(v0, v1);
+  // (an infinite or NaN value: the first term says it all)
+  const float r0 = v0 - low(hi), r1 = v1 - high(hi);
+  lo = pair(r0 == r0 ? r0 : 0.f, r1 == r1 ? r1 : 0.f);
+}
+
+// Where b is infinite, hi b + lo b is NaN although t b is an infinity: 0 inf where t needs one term only, infinities of both signs
+// where the terms differ in sign.  So sums that came out NaN are formed again from whole t.
+// A NaN sum is packed as 0x7FFF, which as an integer lies above all other bf16: the largest of pairs shows one.
+__device__ __forceinline__ uint32_t largest(uint32_t a, uint32_t b, uint32_t c) { return __vimax3_s16x2(a, b, c); }
+__device__ __forceinline__ bool has_nan(uint32_t w) { return low(w) != low(w) || high(w) != high(w); }
+__device__ __forceinline__ bool is_nan(uint16_t bits) { return (bits & 0x7FFF) > 0x7F80; }
 
 // Long segments: tiles of 128 rows on the tensor cores.
 moe_status launch_adapter_tiles(moe_ctx* ctx, const AdapterParams& p, cudaStream_t stream);
