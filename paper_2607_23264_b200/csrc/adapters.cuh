@@ -32,12 +32,11 @@ __device__ __forceinline__ uint32_t pair(float a, float b) {
 __device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
-// Two values as two terms of bf16 each: v - hi is exact, so hi + lo keeps 16 bits.
+// Two values as two terms of bf16 each: v - hi is exact, so hi + lo keeps 16 bits.  hi stays finite: a value near fp32's end would
+// round to an infinity, whose lo were one of the other sign (an infinite v: the largest bf16 and an infinity).
 __device__ __forceinline__ void two_terms(float v0, float v1, uint32_t& hi, uint32_t& lo) {
-  hi = pair(v0, v1);
-  // (an infinite or NaN value: the first term says it all)
-  const float r0 = v0 - low(hi), r1 = v1 - high(hi);
-  lo = pair(r0 == r0 ? r0 : 0.f, r1 == r1 ? r1 : 0.f);
+  asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(hi) : "f"(v1), "f"(v0));
+  lo = pair(v0 - low(hi), v1 - high(hi));
 }
 
 // Where b is infinite, hi b + lo b is NaN although t b is an infinity: 0 inf where t needs one term only, infinities of both signs

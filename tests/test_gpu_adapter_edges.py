@@ -94,3 +94,21 @@ def test_factors_that_are_not_finite(contexts, kernel, rows, N, K, rank, bounds)
     y = p["y"].clone()
     run(ctx, p, ids, bounds, y=y, out=y)
     assert torch.equal(y.view(torch.int16), out.view(torch.int16))
+
+
+@pytest.mark.parametrize("kernel,bounds", [("rows", None), ("rows", [0, 20, 150]), ("tiles", [0, 20, 150])])
+def test_sums_beyond_the_largest_bf16(contexts, kernel, bounds):
+    """A sum of x a that fp32 holds and a rounding to bf16 would make infinite."""
+    rows, N, K, rank = 150, 136, 72, 24
+    p, rng = make(1, rows, N, K, rank, 2, scaled=False)
+    x, a, b = p["xv"], p["av"], 2.0 ** -100 * p["bv"]
+    x[:, :2] = 0
+    x[5], x[149] = 0, 0
+    x[5, :2], x[149, :2] = 2.0 ** 64, -2.0 ** 64
+    a[:, 4, 0], a[:, 4, 1] = 1.9921875 * 2.0 ** 63, 1.5 * 2.0 ** 55       # the largest bf16 and three quarters of its step
+    b[:, 7, 4] = 0
+    for name, v in (("x", x), ("a", a), ("b", b)):
+        p[name], p[name + "v"] = bf16(v)
+    ids = np.arange(rows) % 2 if bounds is None else [0, 1]
+    ref = compare(p, ids, bounds, run(contexts[kernel], p, ids, bounds))
+    assert np.isfinite(ref).all() and np.abs(ref).max() > 1e6
