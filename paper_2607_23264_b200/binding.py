@@ -296,10 +296,13 @@ def _lookup(table, name, what):
 
 def _gain_fp32(gain):
     """1 for an fp32 gain, 0 for a bf16 one."""
-    size = 0 if gain is None else gain.element_size()
-    if size == 2:
+    global _torch
+    if _torch is None:
+        import torch as _torch
+    dtype = getattr(gain, "dtype", None)
+    if dtype is _torch.bfloat16:
         return 0
-    if size == 4:
+    if dtype is _torch.float32:
         return 1
     raise ValueError("the gain is a bf16 or fp32 tensor")
 
