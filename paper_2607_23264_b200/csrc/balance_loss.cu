@@ -209,7 +209,7 @@ template <int EL, int kVec, bool kSigmoid>
 __global__ void __launch_bounds__(32 * partial_warps(EL))
 balance_partial(const BalanceParams p) {
   constexpr int kWarps = partial_warps(EL), kThreads = 32 * kWarps;
-  extern __shared__ float s_sum[];                         // [kWarps][E] sums, then [E] counts
+  extern __shared__ __align__(16) float s_sum[];           // [kWarps][E] sums, then [E] counts
   __shared__ int s_tokens[kWarps];
   __shared__ float s_z[kWarps];
   int* s_count = reinterpret_cast<int*>(s_sum + kWarps * p.E);
