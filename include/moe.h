@@ -604,7 +604,8 @@ moe_status moe_add_rms_norm(moe_ctx* ctx, const moe_rms_norm_args* args, void* s
  *     d_x    = bf16( d_sum + rstd (g - h mean(g h)) )   (the gradient of x and of residual alike)
  *     d_gain = sum over rows of d_out h                 (fp32, fixed order)
  * scratch: moe_rms_norm_scratch_bytes bytes on the device when d_gain is asked for (undefined after).  d_x may be the buffer of
- * d_out or d_sum.  rows == 0 gives a d_gain of zeros.  A scratch measured for more rows of the same length does for fewer.
+ * d_out or d_sum.  rows == 0 gives a d_gain of zeros.  A row whose sum of squares leaves fp32 passes d_sum on; where its sum of s g
+ * leaves fp32, d_x is not finite.  A scratch measured for more rows of the same length does for fewer.
  * Limits as above.  Errors: as above, and WORKSPACE_TOO_SMALL; TIMEOUT through the status word (detail 301).
  */
 typedef struct {
@@ -640,9 +641,9 @@ moe_status moe_rms_norm_backward(moe_ctx* ctx, const moe_rms_norm_grad_args* arg
  * and 0 for tokens that do not count.  d_logits = add + that (add: e.g. the gradient moe_routing_backward wrote; NULL for 0;
  * may be d_logits itself).
  * Masks: a logit of -inf takes no part and gets no gradient; a token whose logits are all -inf has p = 0 and adds nothing to either
- * loss (it counts in n).  A NaN logit (or +inf: see moe_routing_backward) of a counted token makes its own row of d_logits
- * and the losses NaN.  An id outside [0, E) is reported through the status word (MOE_ERR_BAD_ROUTING, detail = the flat slot
- * t*k+j) and not counted.
+ * loss (it counts in n).  A NaN logit of a counted token makes its own row of d_logits and the losses NaN, and so does +inf where
+ * a softmax or the logarithm sees it (sigmoid scores alone take it as sigma = 1).  An id outside [0, E) is reported through the
+ * status word (MOE_ERR_BAD_ROUTING, detail = the flat slot t*k+j) and not counted.
  * Sums are fp32 in a fixed order: the same bits every time.  scratch: moe_balance_scratch_bytes bytes (undefined after);
  * two calls that overlap on the GPU need one each.
  * Limits: 1 <= sequences <= 2^20; coef, z_coef finite; seq_offsets NULL only with one sequence.
@@ -676,8 +677,8 @@ moe_status moe_balance_loss_backward(moe_ctx* ctx, const moe_balance_args* args,
  * adapter share its reads.  The gradient with respect to x is the same call with a and b exchanged, each transposed.
  *   x [rows, K] bf16, a [adapters, rank, K] bf16, b [adapters, N, rank] bf16, y_in, y_out [rows, N] bf16 (y_out may be y_in;
  * no other buffers may overlap).
- * An adapter index >= adapters is reported through the status word (MOE_ERR_BAD_ROUTING, detail = the segment) and its rows
- * are copied.  A lower-ranked adapter is padded with zeros.
+ * An adapter index >= adapters of a segment with rows is reported through the status word (MOE_ERR_BAD_ROUTING, detail = the
+ * segment) and its rows are copied.  A lower-ranked adapter is padded with zeros.
  * scratch: moe_adapter_scratch_bytes bytes (0, and NULL will do, for all sizes the present kernels take: t stays on the chip).
  * TIMEOUT through the status word: detail 201 to 206.
  * Limits: 0 <= rows < 2^28; N, K multiples of 8; rank a multiple of 8, at most 128; 1 <= adapters, adapters * rank and
