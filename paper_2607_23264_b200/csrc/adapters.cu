@@ -62,8 +62,12 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
 }
 // y + d in bf16.
 __device__ __forceinline__ uint32_t add_pair(uint32_t y, float d0, float d1) { return moe::pair(moe::low(y) + d0, moe::high(y) + d1); }
-// The NaN of eight sums formed again: y + t b, b with the first of the eight columns.
+// The NaN of eight sums formed again: y + t b, b with the first of the eight columns.  What is NaN by y, t or b is soon given up.
 __device__ __forceinline__ uint4 sums_again(const uint4 y, uint4 sum, const float* t, const __nv_bfloat16* b, int rank) {
+  float all = 0.f;
+#pragma unroll 1
+  for (int j = 0; j < rank; ++j) all += fabsf(t[j]);
+  if (all != all) return sum;
   const uint32_t old[4] = {y.x, y.y, y.z, y.w};
   uint32_t w[4] = {sum.x, sum.y, sum.z, sum.w};
 #pragma unroll
@@ -72,11 +76,17 @@ __device__ __forceinline__ uint4 sums_again(const uint4 y, uint4 sum, const floa
     if (!moe::has_nan(w[i])) continue;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      if (v[h] == v[h]) continue;
+      const float was = h == 0 ? moe::low(old[i]) : moe::high(old[i]);
+      if (v[h] == v[h] || was != was) continue;
       float d = 0.f;
 #pragma unroll 1
-      for (int j = 0; j < rank; ++j) d = fmaf(t[j], __bfloat162float(b[static_cast<size_t>(2 * i + h) * rank + j]), d);
-      v[h] = (h == 0 ? moe::low(old[i]) : moe::high(old[i])) + d;
+      for (int j = 0; j < rank && d == d; j += 8) {
+        const uint4 q = __ldg(reinterpret_cast<const uint4*>(b + static_cast<size_t>(2 * i + h) * rank + j));
+        const uint32_t qs[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int u = 0; u < 4; ++u) d = fmaf(t[j + 2 * u + 1], moe::high(qs[u]), fmaf(t[j + 2 * u], moe::low(qs[u]), d));
+      }
+      v[h] = was + d;
     }
     w[i] = moe::pair(v[0], v[1]);
   }
