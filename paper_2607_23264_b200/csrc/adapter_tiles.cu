@@ -51,10 +51,12 @@ struct Barriers {
 
 // Shared memory of a CTA: in the second phase the terms of t, b's ring and y's ring; in the first the ring of x and a from the
 // start, and behind it the sums that the cluster sends, in the place of y's last tiles; then the barriers.  112 KiB, of which an
-// SM holds two, and 192 above 64 ranks.
+// SM holds two, and 224 above 64 ranks.
 struct Layout {
   int atoms, rank16, pitch, stage_bytes, stages, y_stages, b_stages, b_at, y_at, sums_at, barriers_at, bytes;
-  __host__ __device__ explicit Layout(int rank) {
+  __host__ __device__ constexpr explicit Layout(int rank)
+      : atoms(0), rank16(0), pitch(0), stage_bytes(0), stages(0), y_stages(0), b_stages(0), b_at(0), y_at(0), sums_at(0), barriers_at(0),
+        bytes(0) {
     atoms = (rank + 63) / 64;
     rank16 = (rank + 15) / 16 * 16;
     pitch = rank + 4;                                      // floats of a row of sums: an odd number of 16 bytes
@@ -69,6 +71,10 @@ struct Layout {
     bytes = barriers_at + static_cast<int>(sizeof(Barriers));
   }
 };
+
+static_assert(Layout(128).bytes <= 227 * 1024 && 2 * (Layout(64).bytes + 1024) <= 228 * 1024, "one CTA to an SM, or two");
+static_assert(Layout(128).sums_at >= Layout(128).y_at + kYBytes && Layout(64).sums_at >= Layout(64).y_at + kYBytes,
+              "the sums leave y's first tile alone");
 
 struct Maps {
   CUtensorMap x, x_short, a, b, in, in_short, out;

@@ -14,7 +14,9 @@
 //
 // Bound by HBM for many rows: 8192 x 7168 with residual, bf16 and 8-bit outputs 85.9 us, 6.2 TB/s (80.8 at the rate of a copy); the
 // gradients of 8192 x 4096 54 us, 44 of them norm_backward at 6.1 TB/s, 4.8 norm_gain_sum, the rest between the two.  64 x 7168:
-// 4.2 us, of which the launch is half; the gradients of 301 x 7168 12.4 us: two launches of two loads' latency each.
+// 4.2 us, of which the launch is half; the gradients of 301 x 7168 12.4 us: two launches of two loads' latency each.  Gradients of
+// rows above 8192 columns are bound by registers: up to 32 warps to a row leave a thread 64 for four vectors of three tensors and
+// their sums, which spill (4096 x 8192 53 us, 4096 x 9216 286, 4096 x 12288 323; the bytes take 41, 46 and 61).
 #include <cuda_bf16.h>
 
 #include "blk_quant.cuh"
